@@ -100,7 +100,8 @@ enum {
   SCALIFY_OP_STATISTIC = 4,     /* d0 = number of elements */
   SCALIFY_OP_CROSS_ENTROPY = 5, /* d0 = number of rows */
   SCALIFY_OP_COLSUM = 6,        /* d0 = rows, d1 = columns */
-  SCALIFY_OP_MATMUL_SPLITK = 7  /* d0 = M, d1 = N: room for the partial products of a split contraction */
+  SCALIFY_OP_MATMUL_SPLITK = 7, /* d0 = M, d1 = N: room for the partial products of a split contraction */
+  SCALIFY_OP_RMSNORM_BWD = 8    /* d0 = rows, d1 = row length */
 };
 
 /* Bytes of workspace the given call needs (an upper bound; always >= 4096).
@@ -358,6 +359,50 @@ int scalify_scaled_layernorm_bwd_delayed(const scalify_array* G, const scalify_a
                                          const float* stat_in, int stat_dx, scalify_array* dX,
                                          scalify_array* dgamma, scalify_array* dbeta,
                                          void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Residual addition and root-mean-square norm in one pass, with an 8-bit output (a norm without mean and bias; the add
+ * rule of Section 3.2 and the normalisation rule of Section 3.2.1 / Appendix C.2):
+ *   H_s = max(X_s, R_s),   H_d = cast(X_d*(X_s/H_s) + R_d*(R_s/H_s))          (bit for bit scalify_scaled_add)
+ *   n = H_d * rinv,   rinv = 1 / sqrt(mean(H_d^2) + eps)                        (of H as stored; scale 1)
+ *   Y_s = gamma_s (1 without gamma),   Y_d = cast(n * gamma_d)
+ * and, with Ymx instead of Y, the same values quantised with one exponent per 32 elements as scalify_mx_quantize does
+ * (Ymx_s = gamma_s), ready for scalify_mx_matmul.
+ * X: [rows,d], F16/BF16/F32: the branch that is added.  R: the residual stream, of X's dtype or F32; H: the new
+ * residual stream, of R's dtype, which may be R's or X's own buffer (same row stride).  With R == NULL there is no
+ * addition: H must be NULL and X is the stream that is normalised.  Y: any dtype.  Exactly one of Y and Ymx is given;
+ * Ymx: rows of d = K elements, not transposed.  gamma: [d], F16/BF16/F32, or NULL.  rinv: optional fp32 [rows]
+ * (device), needed by the backward call.  d <= 16384, any; rows may be strided.  A row of zeros gives zeros.
+ * status: optional DEVICE word (SCALIFY_DEV_BAD_SCALE).
+ * Errors: NULL, DTYPE, SHAPE, ALIGNMENT, UNSUPPORTED (both Y and Ymx, transposed Ymx), VALUE (eps < 0), ALIAS (an
+ * output overlapping an input other than as above, or a scale word shared with another array of the call).
+ */
+struct scalify_mx_array;
+int scalify_scaled_add_rmsnorm(const scalify_array* X, const scalify_array* R, const scalify_array* gamma, float eps,
+                               scalify_array* H, scalify_array* Y, struct scalify_mx_array* Ymx, float* rinv,
+                               uint32_t* status, void* stream);
+
+/*
+ * Its gradient (the exact derivative at H as stored; the block exponents and the 8-bit rounding of the forward output
+ * are passed straight through):
+ *   g = G_d*gamma_d,  dh = rinv*(g - n*mean(g*n)),  scale G_s*gamma_s/H_s
+ *   dX_s = max(G_s*gamma_s/H_s, Gr_s),   dX_d = cast(dh + Gr by the add rule)      (gradient of X and of R alike)
+ *   dXq_d = cast(dX_d / r), dXq_s = dX_s*r:   the 8-bit copy of the STORED dX that the next matmuls read; r is the
+ *       power of two at or below *stat_in, the statistic of an earlier step (delayed rescaling, Section 3.3), or 1
+ *       with stat_in == NULL or a statistic that defines no scale
+ *   dgamma_d = sum_rows(G_d*n)/kf(rows), scale G_s*kf(rows)
+ * G: [rows,d], F16/BF16/F32, gradient of Y.  H, rinv: from the forward call (with R == NULL, H is its X).  Gr: gradient
+ * of H from the residual path, of H's dtype, or NULL.  dX: H's dtype; may be Gr's or G's own buffer (same dtype and
+ * row stride).  H's dtype is G's or F32.  dXq: E4M3/E5M2 or NULL.  dgamma: [d] F16/BF16/F32 or NULL.  stat_dx: statistic
+ * of the stored dX data, left at workspace offset 16 (stat_in may be that word's copy, not the word itself).
+ * Sums over rows are fp32 per block and fp64 over the blocks, in a fixed order: results do not depend on scheduling.
+ * Workspace: SCALIFY_OP_RMSNORM_BWD (rows, d); may be NULL without dgamma and stat_dx.
+ * Errors: NULL, DTYPE, SHAPE, ALIGNMENT, VALUE, ALIAS, WORKSPACE.
+ */
+int scalify_scaled_add_rmsnorm_bwd(const scalify_array* G, const scalify_array* Gr, const scalify_array* H,
+                                   const scalify_array* gamma, const float* rinv, scalify_array* dX, scalify_array* dXq,
+                                   const float* stat_in, int stat_dx, scalify_array* dgamma, void* workspace,
+                                   size_t workspace_bytes, void* stream);
 
 /*
  * Scaled GELU forward / backward (Section 3.2.1 and Appendix C.1):

@@ -24,6 +24,7 @@ E4M3, E5M2, F16, BF16, F32 = 0, 1, 2, 3, 4
 STAT_NONE, STAT_AMAX, STAT_L2 = 0, 1, 2
 OP_MATMUL, OP_RESCALE, OP_LAYERNORM_BWD, OP_ADAM, OP_STATISTIC, OP_CROSS_ENTROPY, OP_COLSUM, OP_MATMUL_SPLITK = (
     0, 1, 2, 3, 4, 5, 6, 7)
+OP_RMSNORM_BWD = 8
 DEV_TIMEOUT, DEV_BAD_SCALE, DEV_NONFINITE_STAT, DEV_BAD_INDEX = 1, 2, 4, 8
 
 _DTYPE_CODE = {torch.float8_e4m3fn: E4M3, torch.float8_e5m2: E5M2, torch.float16: F16,
@@ -112,7 +113,9 @@ def lib() -> ctypes.CDLL:
         L.scalify_scaled_softmax_bwd.argtypes = [P, P, P, vp]
         L.scalify_scaled_cross_entropy.argtypes = [P, i64, vp, vp, P, vp, sz, vp]
         L.scalify_scaled_adam_step_static.argtypes = [i32, P, P, P, P, f32, f32, f32, f32, i64, vp, vp]
-        for name in ("scalify_workspace_init", "scalify_check_status", "scalify_scaled_matmul", "scalify_scaled_matmul_delayed",
+        L.scalify_scaled_add_rmsnorm.argtypes = [P, P, P, f32, P, P, vp, vp, vp, vp]
+        L.scalify_scaled_add_rmsnorm_bwd.argtypes = [P, P, P, P, vp, P, P, vp, i32, P, vp, sz, vp]
+        for name in ("scalify_scaled_add_rmsnorm", "scalify_scaled_add_rmsnorm_bwd", "scalify_workspace_init", "scalify_check_status", "scalify_scaled_matmul", "scalify_scaled_matmul_delayed",
                      "scalify_statistic",
                      "scalify_rescale", "scalify_scaled_add", "scalify_scaled_layernorm",
                      "scalify_scaled_layernorm_bwd", "scalify_scaled_gelu", "scalify_scaled_gelu_bwd",
@@ -546,3 +549,65 @@ def scalify_scaled_attention_bwd(Q: ScaledTensor, K: ScaledTensor, V: ScaledTens
                                               int(bool(causal)), _ref(ds), _ref(dq), _ref(dk), _ref(dv), _ref(dpd),
                                               _ptr(status), _stream(stream)),
            "scalify_scaled_attention_bwd")
+
+
+def _call(name: str, device: torch.device, stream, *args) -> None:
+    """Calls an entry point with ``device`` current (its stream is that device's current one unless given)."""
+    fn = getattr(lib(), name)
+    if device.type != "cuda":
+        raise ValueError(f"{name}: arrays must be on a CUDA device")
+    if device.index == torch.cuda.current_device():
+        _check(fn(*args, _stream(stream)), name)
+    else:
+        with torch.cuda.device(device):
+            _check(fn(*args, _stream(stream)), name)
+
+
+def _same_device(name: str, first: torch.Tensor, *others) -> torch.device:
+    """The device of ``first``; every other tensor (None skipped) has to be there too."""
+    dev = first.device
+    for t in others:
+        if t is not None and t.device != dev:
+            raise ValueError(f"{name}: arrays on {dev} and {t.device}")
+    return dev
+
+
+def _rows_vector(name: str, t: Optional[torch.Tensor], n: int, what: str, dtype=torch.float32) -> None:
+    if t is not None and (t.dtype != dtype or t.numel() != n or not t.is_contiguous()):
+        raise ValueError(f"{name}: {what} must be a contiguous {dtype} tensor of {n} elements")
+
+
+def _data(t) -> Optional[torch.Tensor]:
+    return None if t is None else t.data
+
+
+def scalify_scaled_add_rmsnorm(X: ScaledTensor, R: Optional[ScaledTensor], gamma: Optional[ScaledTensor],
+                               H: Optional[ScaledTensor], Y, *, eps: float = 1e-5, rinv: Optional[torch.Tensor] = None,
+                               status: Optional[torch.Tensor] = None, stream=None) -> None:
+    """H = X + R (add rule) and Y = RMSNorm(H) * gamma; Y is a ScaledTensor of any dtype or an MxTensor (block scales).
+    Without R, H is None and X itself is normalised.  ``rinv``: fp32 [rows] for the backward call."""
+    name = "scalify_scaled_add_rmsnorm"
+    dev = _same_device(name, X.data, _data(R), _data(gamma), _data(H), _data(Y), rinv, status)
+    d = X.data.shape[-1]
+    _rows_vector(name, rinv, X.data.numel() // d if d else 0, "rinv")
+    x, r, g, h = _desc(X), _desc(R), _desc(gamma), _desc(H)
+    y, mx = (None, ctypes.addressof(Y._d)) if isinstance(Y, MxTensor) else (_desc(Y), None)
+    _call(name, dev, stream, _ref(x), _ref(r), _ref(g), float(eps), _ref(h), _ref(y), mx, _ptr(rinv), _ptr(status))
+
+
+def scalify_scaled_add_rmsnorm_bwd(G: ScaledTensor, Gr: Optional[ScaledTensor], H: ScaledTensor,
+                                   gamma: Optional[ScaledTensor], rinv: torch.Tensor, dX: ScaledTensor,
+                                   ws: Optional[Workspace] = None, *, dXq: Optional[ScaledTensor] = None,
+                                   stat_in: Optional[torch.Tensor] = None, stat_dx: int = STAT_NONE,
+                                   dgamma: Optional[ScaledTensor] = None, stream=None) -> None:
+    """Gradient of scalify_scaled_add_rmsnorm: dX (for X and R alike) = norm's gradient + Gr, its 8-bit copy dXq
+    (rebalanced by the power of two of ``stat_in``), dgamma, and the statistic of dX in the workspace."""
+    name = "scalify_scaled_add_rmsnorm_bwd"
+    dev = _same_device(name, G.data, _data(Gr), _data(H), _data(gamma), rinv, _data(dX), _data(dXq), stat_in,
+                       _data(dgamma), None if ws is None else ws.buf)
+    d = H.data.shape[-1]
+    _rows_vector(name, rinv, H.data.numel() // d if d else 0, "rinv")
+    _rows_vector(name, stat_in, 1, "stat_in")
+    g, gr, h, gm, dx, dq, dg = (_desc(G), _desc(Gr), _desc(H), _desc(gamma), _desc(dX), _desc(dXq), _desc(dgamma))
+    _call(name, dev, stream, _ref(g), _ref(gr), _ref(h), _ref(gm), _ptr(rinv), _ref(dx), _ref(dq), _ptr(stat_in),
+          int(stat_dx), _ref(dg), None if ws is None else ws.ptr, 0 if ws is None else ws.nbytes)

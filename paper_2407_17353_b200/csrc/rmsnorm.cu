@@ -1,0 +1,502 @@
+// Residual addition + root-mean-square norm with an 8-bit (or wide) output, and its gradient.
+//
+// Forward, per row of d elements (add rule of Section 3.2, normalisation rule of Section 3.2.1 / Appendix C.2):
+//   H_s = max(X_s, R_s),   H_d = round(X_d X_s/H_s + R_d R_s/H_s)
+//   n = H_d rinv,  rinv = (mean(H_d^2) + eps)^(-1/2)        (the data component; the result carries scale 1)
+//   Y_s = gamma_s,  Y_d = round(n gamma_d);  block-scaled: round(n gamma_d 2^-e), one exponent per 32 elements
+// The norm is taken of H AS STORED: the gradient, which reads H, is then the derivative of what was computed, and the
+// call equals scalify_scaled_add followed by the norm of its output bit for bit.
+//
+// Backward, with g = G_d gamma_d:   dh = rinv (g - n mean(g n)),  scale G_s gamma_s / H_s, then the add rule with the
+// gradient of H itself (residual path):  dX_s = max(G_s gamma_s / H_s, Gr_s);  dgamma = sum_rows G_d n / kf(R).
+//
+// Both directions are bound by HBM: every array is read or written once.  A row lives in the registers of a team: one
+// warp for d <= 1024 (1 to 4 vectors of 8 elements per lane, several rows per block, no barrier), otherwise one block of
+// up to 512 threads with 2 vectors per thread (4 above d = 8192) and two barriers per row.
+#include "scalify_common.cuh"
+#include "scalify_launch.h"
+
+namespace scalify {
+
+namespace {
+
+constexpr int kVec = 8;          // elements per vector: 16 bytes of a 16-bit format
+constexpr int kWarpRows = 4;     // rows (warps) per block of the warp-per-row forms
+constexpr int kWarpMaxD = 1024;  // longest row one warp holds
+constexpr int kBlockThreads = 512;  // most threads of the block-per-row forms (leaves 128 registers a thread)
+
+// Raw words of vector v of a row (n = elements of it inside the row; the rest read as zero).
+template <int DT>
+__device__ __forceinline__ void load_vec(const char* row, int v, int n, uint32_t* w) {
+  constexpr int ES = ElemBytes<DT>::v;
+  if (n >= kVec) {
+    ld_raw_stream<kVec * ES>(row + static_cast<int64_t>(v) * (kVec * ES), w);
+  } else {
+    float f[kVec];
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) f[e] = e < n ? load_elem<DT>(row, static_cast<int64_t>(v) * kVec + e) : 0.f;
+    encode_vec<DT, kVec>(f, w);
+  }
+}
+template <int DT>
+__device__ __forceinline__ void store_vec(char* row, int v, int n, const float* f) {
+  constexpr int ES = ElemBytes<DT>::v;
+  if (n >= kVec) {
+    uint32_t w[kVec * ES / 4];
+    encode_vec<DT, kVec>(f, w);
+    st_raw<kVec * ES>(row + static_cast<int64_t>(v) * (kVec * ES), w);
+  } else {
+#pragma unroll
+    for (int e = 0; e < kVec; ++e)
+      if (e < n) store_elem<DT>(row, static_cast<int64_t>(v) * kVec + e, f[e]);
+  }
+}
+// one uniform branch per vector on the output's type: a template per type would multiply the kernels by five
+__device__ __forceinline__ void store_vec_dt(int dt, char* row, int v, int n, const float* f) {
+  SCALIFY_DISPATCH_DTYPE(dt, DT, store_vec<DT>(row, v, n, f))
+}
+__device__ __forceinline__ void load_gamma(const void* gamma, int dt, int v, int n, float* f) {
+  if (!gamma) {
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) f[e] = 1.0f;
+    return;
+  }
+  const char* p = static_cast<const char*>(gamma);
+  SCALIFY_DISPATCH_WIDE(dt, DT, {
+    uint32_t w[kVec * ElemBytes<DT>::v / 4];
+    if (n >= kVec) {
+      ld_raw<kVec * ElemBytes<DT>::v>(p + static_cast<int64_t>(v) * (kVec * ElemBytes<DT>::v), w);
+      decode_vec<DT, kVec>(w, f);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) f[e] = e < n ? load_elem<DT>(p, static_cast<int64_t>(v) * kVec + e) : 0.f;
+    }
+  })
+}
+
+// sum over the team that holds a row; every thread returns it (fixed order)
+template <bool BLOCK>
+__device__ __forceinline__ float team_sum(float x, float* s_red) {
+  x = warp_sum_f32(x);
+  if constexpr (BLOCK) {
+    __syncthreads();  // the previous use of s_red is over
+    if ((threadIdx.x & 31) == 0) s_red[threadIdx.x >> 5] = x;
+    __syncthreads();
+    const int nw = blockDim.x >> 5;
+    x = (threadIdx.x & 31) < nw ? s_red[threadIdx.x & 31] : 0.f;
+    x = warp_sum_f32(x);
+  }
+  return x;
+}
+
+}  // namespace
+
+// ------------------------------------------------------------------------------------------------- forward
+template <int XDT, int HDT, int VPT, bool BLOCK>
+__global__ void __launch_bounds__(BLOCK ? kBlockThreads : 32 * kWarpRows) add_rmsnorm_kernel(const RmsNormArgs a) {
+  asm volatile("griddepcontrol.launch_dependents;");  // a programmatic dependent may set up while this grid runs
+  __shared__ float s_red[32];
+  const int team = BLOCK ? blockDim.x : 32;
+  const int lane = BLOCK ? threadIdx.x : threadIdx.x & 31;
+  const int64_t row = BLOCK ? blockIdx.x : static_cast<int64_t>(blockIdx.x) * kWarpRows + (threadIdx.x >> 5);
+  const float xs = load_scale(a.x_scale), rs = a.R ? load_scale(a.r_scale) : 0.f, gs = a.gamma ? load_scale(a.gamma_scale) : 1.0f;
+  const float hs = fmaxf(xs, rs);
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    if (a.h_scale) *a.h_scale = hs;
+    if (a.y_scale) *a.y_scale = gs;
+    if (a.status && !(is_pow2_scale(xs) && (!a.R || is_pow2_scale(rs)) && is_pow2_scale(gs)))
+      atomicOr(a.status, static_cast<uint32_t>(SCALIFY_DEV_BAD_SCALE));
+  }
+  const bool live = row < a.rows;
+  if (!live && !a.sf) return;
+  const int n_vec = (a.d + kVec - 1) / kVec;
+  float h[VPT][kVec];
+  if (live) {
+    constexpr int XW = kVec * ElemBytes<XDT>::v / 4, HW = kVec * ElemBytes<HDT>::v / 4;
+    const char* xrow = static_cast<const char*>(a.X) + row * a.x_ld * (a.R ? ElemBytes<XDT>::v : ElemBytes<HDT>::v);
+    const char* rrow = a.R ? static_cast<const char*>(a.R) + row * a.r_ld * ElemBytes<HDT>::v : nullptr;
+    char* hrow = a.R ? static_cast<char*>(a.H) + row * a.h_ld * ElemBytes<HDT>::v : nullptr;
+    float ss = 0.f;
+    if (a.R) {
+      const float fx = xs / hs, fr = rs / hs;  // powers of two: exact
+      uint32_t wx[VPT][XW], wr[VPT][HW];
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) {
+        const int v = lane + i * team;
+        if (v < n_vec) {
+          load_vec<XDT>(xrow, v, a.d - v * kVec, wx[i]);
+          load_vec<HDT>(rrow, v, a.d - v * kVec, wr[i]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) {
+        const int v = lane + i * team;
+        float x[kVec];
+        if (v < n_vec) {
+          decode_vec<XDT, kVec>(wx[i], x);
+          decode_vec<HDT, kVec>(wr[i], h[i]);
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) h[i][e] = round_through<HDT>(fmaf(x[e], fx, h[i][e] * fr));
+          store_vec<HDT>(hrow, v, a.d - v * kVec, h[i]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) h[i][e] = 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) ss = fmaf(h[i][e], h[i][e], ss);
+      }
+    } else {
+      uint32_t wr[VPT][HW];
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) {
+        const int v = lane + i * team;
+        if (v < n_vec) load_vec<HDT>(xrow, v, a.d - v * kVec, wr[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) {
+        if (lane + i * team < n_vec) decode_vec<HDT, kVec>(wr[i], h[i]);
+        else {
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) h[i][e] = 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) ss = fmaf(h[i][e], h[i][e], ss);
+      }
+    }
+    ss = team_sum<BLOCK>(ss, s_red);
+    const float rinv = __frsqrt_rn(ss / static_cast<float>(a.d) + a.eps);
+    if (lane == 0 && a.rinv) a.rinv[row] = rinv;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      const int v = lane + i * team;
+      if (v < n_vec) {
+        float g[kVec];
+        load_gamma(a.gamma, a.gamma_dt, v, a.d - v * kVec, g);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) h[i][e] = h[i][e] * rinv * g[e];
+        if (!a.sf) store_vec_dt(a.y_dt, static_cast<char*>(a.Y) + row * a.y_ld * a.y_es, v, a.d - v * kVec, h[i]);
+      }
+    }
+  }
+  if (!a.sf) return;
+  // Block scales (d is a multiple of 128, so a vector is whole and the four lanes of a block of 32 act together).
+  // The exponent is that of scalify_mx_quantize; sixteen lanes hold the four blocks of one 128-element tile row, whose
+  // bytes are neighbours.  Rows between `rows` and the next multiple of 256 get the code 127.
+  const int emax = a.y_dt == SCALIFY_E4M3 ? 8 : 15;
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) {
+    const int v = lane + i * team;
+    const bool in = v < n_vec;
+    uint32_t amax = 0u;
+    if (live && in) {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) amax = max(amax, abs_bits(h[i][e]));
+    }
+    amax = max(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
+    amax = max(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
+    int ex = 0;
+    if (amax != 0u && amax < 0x7F800000u) {
+      ex = static_cast<int>(amax >> 23) - 127;
+      if ((amax >> 23) == 0u) ex = -127 - __clz(amax << 9);
+      ex = max(-127, min(127, ex - emax));
+    }
+    uint32_t code = static_cast<uint32_t>(ex + 127);
+    const int l0 = threadIdx.x & 16;
+    const uint32_t c1 = __shfl_sync(0xFFFFFFFFu, code, l0 + 4), c2 = __shfl_sync(0xFFFFFFFFu, code, l0 + 8),
+                   c3 = __shfl_sync(0xFFFFFFFFu, code, l0 + 12);
+    if (in) {
+      if (live) {
+        const uint32_t field = static_cast<uint32_t>(127 - ex);
+        const float s = __uint_as_float(field ? field << 23 : 0x00400000u);  // 2^-ex, exact
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) h[i][e] *= s;
+        char* yrow = static_cast<char*>(a.Y) + row * a.y_ld;
+        if (a.y_dt == SCALIFY_E4M3) store_vec<SCALIFY_E4M3>(yrow, v, kVec, h[i]);
+        else store_vec<SCALIFY_E5M2>(yrow, v, kVec, h[i]);
+      }
+      if ((threadIdx.x & 15) == 0) {
+        const uint32_t w = code | (c1 << 8) | (c2 << 16) | (c3 << 24);
+        uint8_t* p = a.sf + (row / 128 * (a.d / 128) + v / 16) * 512 + (row % 32) * 16 + (row % 128) / 32 * 4;
+        st_raw<4>(p, &w);
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------- backward
+// Persistent teams walk the rows (grid stride); a team keeps its columns' share of dgamma in registers over all its
+// rows and leaves it in the workspace, one line per block, added in block order by the second launch: the result does
+// not depend on scheduling.  The statistic of the stored dX travels the same way.
+template <int GDT, int HDT, int VPT, bool BLOCK>
+__global__ void __launch_bounds__(BLOCK ? kBlockThreads : 32 * kWarpRows) add_rmsnorm_bwd_kernel(const RmsNormBwdArgs a) {
+  asm volatile("griddepcontrol.launch_dependents;");  // a programmatic dependent may set up while this grid runs
+  extern __shared__ float s_dg[];  // warp-per-row form: [kWarpRows][d] to add up the block's warps
+  __shared__ float s_red[32];
+  __shared__ double s_stat[32];
+  const int team = BLOCK ? blockDim.x : 32;
+  const int lane = BLOCK ? threadIdx.x : threadIdx.x & 31;
+  const int warp = threadIdx.x >> 5;
+  const int64_t first = BLOCK ? blockIdx.x : static_cast<int64_t>(blockIdx.x) * kWarpRows + warp;
+  const int64_t stride = BLOCK ? gridDim.x : static_cast<int64_t>(gridDim.x) * kWarpRows;
+  const float g_s = load_scale(a.g_scale), h_s = load_scale(a.h_scale), gam_s = a.gamma ? load_scale(a.gamma_scale) : 1.0f;
+  const float branch_s = g_s * gam_s / h_s, res_s = a.Gr ? load_scale(a.gr_scale) : 0.f;
+  const float dx_s = fmaxf(branch_s, res_s);
+  const float fb = branch_s / dx_s, fr = res_s / dx_s;  // powers of two
+  bool nonfinite = false;
+  const float r_q = a.stat_in ? rescale_factor(__ldg(a.stat_in), &nonfinite) : 1.0f;
+  const float inv_rq = 1.0f / r_q;
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    if (a.dx_scale) *a.dx_scale = dx_s;
+    if (a.dxq_scale) *a.dxq_scale = dx_s * r_q;
+    if (a.dgamma_scale) *a.dgamma_scale = g_s * a.kf;
+    if (a.status) {
+      uint32_t bits = 0u;
+      if (!(is_pow2_scale(g_s) && is_pow2_scale(h_s) && is_pow2_scale(gam_s) && (!a.Gr || is_pow2_scale(res_s))))
+        bits |= SCALIFY_DEV_BAD_SCALE;
+      if (nonfinite) bits |= SCALIFY_DEV_NONFINITE_STAT;
+      if (bits) atomicOr(a.status, bits);
+    }
+  }
+  const int n_vec = (a.d + kVec - 1) / kVec;
+  constexpr int GW = kVec * ElemBytes<GDT>::v / 4, HW = kVec * ElemBytes<HDT>::v / 4;
+  const float inv_d = 1.0f / static_cast<float>(a.d);
+  float dg[VPT][kVec];
+#pragma unroll
+  for (int i = 0; i < VPT; ++i)
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) dg[i][e] = 0.f;
+  uint32_t amax = 0u;
+  double ssq = 0.0;
+  for (int64_t row = first; row < a.rows; row += stride) {
+    const char* grow = static_cast<const char*>(a.G) + row * a.g_ld * ElemBytes<GDT>::v;
+    const char* hrow = static_cast<const char*>(a.H) + row * a.h_ld * ElemBytes<HDT>::v;
+    const char* rrow = a.Gr ? static_cast<const char*>(a.Gr) + row * a.gr_ld * ElemBytes<HDT>::v : nullptr;
+    uint32_t wg[VPT][GW], wh[VPT][HW], wr[VPT][HW];
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      const int v = lane + i * team;
+      if (v < n_vec) {
+        load_vec<GDT>(grow, v, a.d - v * kVec, wg[i]);
+        load_vec<HDT>(hrow, v, a.d - v * kVec, wh[i]);
+        if (rrow) load_vec<HDT>(rrow, v, a.d - v * kVec, wr[i]);
+      } else {
+#pragma unroll
+        for (int q = 0; q < GW; ++q) wg[i][q] = 0u;
+#pragma unroll
+        for (int q = 0; q < HW; ++q) wh[i][q] = 0u;
+      }
+    }
+    const float rinv = __ldg(a.rinv + row);
+    float dot = 0.f;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      const int v = lane + i * team;
+      float g[kVec], h[kVec], gam[kVec];
+      decode_vec<GDT, kVec>(wg[i], g);
+      decode_vec<HDT, kVec>(wh[i], h);
+      if (v < n_vec) load_gamma(a.gamma, a.gamma_dt, v, a.d - v * kVec, gam);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        const float n = h[e] * rinv;
+        dg[i][e] = fmaf(g[e], n, dg[i][e]);
+        if (v < n_vec) dot = fmaf(g[e] * gam[e], n, dot);
+      }
+    }
+    dot = team_sum<BLOCK>(dot, s_red) * inv_d;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      const int v = lane + i * team;
+      if (v < n_vec) {
+        const int n = a.d - v * kVec;
+        float g[kVec], h[kVec], gam[kVec], r[kVec];
+        decode_vec<GDT, kVec>(wg[i], g);
+        decode_vec<HDT, kVec>(wh[i], h);
+        load_gamma(a.gamma, a.gamma_dt, v, n, gam);
+        if (rrow) decode_vec<HDT, kVec>(wr[i], r);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) {
+          const float dh = rinv * fmaf(-h[e] * rinv, dot, g[e] * gam[e]);
+          g[e] = round_through<HDT>(rrow ? fmaf(r[e], fr, dh * fb) : dh);
+          if (e < n) {
+            amax = max(amax, abs_bits(g[e]));
+            if (a.stat == SCALIFY_STAT_L2) ssq += static_cast<double>(g[e]) * g[e];
+          }
+        }
+        store_vec<HDT>(static_cast<char*>(a.dX) + row * a.dx_ld * ElemBytes<HDT>::v, v, n, g);
+        if (a.dXq) {
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) g[e] *= inv_rq;
+          char* qrow = static_cast<char*>(a.dXq) + row * a.dxq_ld;
+          if (a.dxq_dt == SCALIFY_E4M3) store_vec<SCALIFY_E4M3>(qrow, v, n, g);
+          else store_vec<SCALIFY_E5M2>(qrow, v, n, g);
+        }
+      }
+    }
+  }
+  if (a.partial) {
+    float* line = a.partial + static_cast<int64_t>(blockIdx.x) * a.partial_ld;
+    if constexpr (BLOCK) {
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) {
+        const int v = lane + i * team;
+        if (v < n_vec) {
+          uint32_t w[kVec];
+          encode_vec<SCALIFY_F32, kVec>(dg[i], w);
+          st_raw<32>(line + v * kVec, w);  // (the line is padded to whole vectors)
+        }
+      }
+    } else {
+      const int ld = n_vec * kVec;
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) {
+        const int v = lane + i * team;
+        if (v < n_vec) {
+#pragma unroll
+          for (int e = 0; e < kVec; e += 4)
+            *reinterpret_cast<float4*>(s_dg + warp * ld + v * kVec + e) = make_float4(dg[i][e], dg[i][e + 1], dg[i][e + 2], dg[i][e + 3]);
+        }
+      }
+      __syncthreads();
+      for (int c = threadIdx.x; c < ld; c += blockDim.x) {
+        float t = 0.f;
+#pragma unroll
+        for (int k = 0; k < kWarpRows; ++k) t += s_dg[k * ld + c];
+        line[c] = t;
+      }
+    }
+  }
+  if (a.stat != SCALIFY_STAT_NONE) {
+    const double mine = a.stat == SCALIFY_STAT_AMAX ? static_cast<double>(warp_max_u32(amax)) : warp_sum_f64(ssq);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) s_stat[warp] = mine;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      double t = 0.0;
+      for (int k = 0; k < static_cast<int>(blockDim.x >> 5); ++k) t = a.stat == SCALIFY_STAT_AMAX ? fmax(t, s_stat[k]) : t + s_stat[k];
+      a.stat_partial[blockIdx.x] = t;
+    }
+  }
+}
+
+// Adds the blocks' lines in block order: a block takes 32 columns, each of its 8 warps every eighth line; the last block
+// of the grid reduces the statistic instead.
+template <int ODT>
+__global__ void __launch_bounds__(256) add_rmsnorm_bwd_finish_kernel(const float* __restrict__ partial, int64_t ld, int lines,
+                                                                     int d, void* __restrict__ dgamma, float inv_kf,
+                                                                     const double* __restrict__ stat_partial, int stat,
+                                                                     double count, float* stat_word) {
+  asm volatile("griddepcontrol.launch_dependents;");  // a programmatic dependent may set up while this grid runs
+  __shared__ double s[8][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (stat != SCALIFY_STAT_NONE && blockIdx.x == gridDim.x - 1) {
+    double t = 0.0;
+    for (int i = threadIdx.x; i < lines; i += 256) t = stat == SCALIFY_STAT_AMAX ? fmax(t, stat_partial[i]) : t + stat_partial[i];
+    t = stat == SCALIFY_STAT_AMAX ? static_cast<double>(warp_max_u32(static_cast<uint32_t>(t))) : warp_sum_f64(t);
+    if (lane == 0) s[0][warp] = t;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      t = 0.0;
+      for (int k = 0; k < 8; ++k) t = stat == SCALIFY_STAT_AMAX ? fmax(t, s[0][k]) : t + s[0][k];
+      *stat_word = stat == SCALIFY_STAT_AMAX ? __uint_as_float(static_cast<uint32_t>(t)) : static_cast<float>(sqrt(t / count));
+    }
+    return;
+  }
+  const int col = blockIdx.x * 32 + lane;
+  double t = 0.0;
+  if (col < d) {
+    int i = warp;
+    for (; i + 24 < lines; i += 32) {  // four loads in flight
+      const float p0 = __ldcs(partial + static_cast<int64_t>(i) * ld + col), p1 = __ldcs(partial + static_cast<int64_t>(i + 8) * ld + col),
+                  p2 = __ldcs(partial + static_cast<int64_t>(i + 16) * ld + col), p3 = __ldcs(partial + static_cast<int64_t>(i + 24) * ld + col);
+      t += (static_cast<double>(p0) + p1) + (static_cast<double>(p2) + p3);
+    }
+    for (; i < lines; i += 8) t += __ldcs(partial + static_cast<int64_t>(i) * ld + col);
+  }
+  s[warp][lane] = t;
+  __syncthreads();
+  if (warp == 0 && col < d) {
+    t = 0.0;
+    for (int k = 0; k < 8; ++k) t += s[k][lane];
+    store_elem<ODT>(dgamma, col, static_cast<float>(t) * inv_kf);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------- launches
+static int block_threads(int d) {
+  const int n_vec = (d + kVec - 1) / kVec, vpt = n_vec <= 2 * kBlockThreads ? 2 : 4;
+  return ((n_vec + vpt - 1) / vpt + 31) / 32 * 32;
+}
+static int bwd_grid_cap(int d) {  // resident blocks: about 16 warps per SM (the row state takes most registers)
+  if (d <= kWarpMaxD) return sm_count() * 4;
+  const int per_sm = 512 / block_threads(d);
+  return sm_count() * (per_sm < 1 ? 1 : per_sm);
+}
+size_t rmsnorm_bwd_ws_bytes(int64_t rows, int64_t d) {
+  if (d < 1 || d > kRmsNormMaxD) return kWsMin;
+  const size_t cap = static_cast<size_t>(bwd_grid_cap(static_cast<int>(d)));
+  return kWsHeader + cap * (static_cast<size_t>((d + kVec - 1) / kVec * kVec) * sizeof(float) + sizeof(double)) + 256;
+}
+
+#define SCALIFY_RMS_VPT(X, H, KERNEL, ...)                                  \
+  do {                                                                      \
+    if (block && n_vec <= 2 * kBlockThreads) KERNEL<X, H, 2, true><<<grid, threads, smem, st>>>(__VA_ARGS__); \
+    else if (block) KERNEL<X, H, 4, true><<<grid, threads, smem, st>>>(__VA_ARGS__);        \
+    else if (n_vec <= 32) KERNEL<X, H, 1, false><<<grid, threads, smem, st>>>(__VA_ARGS__); \
+    else if (n_vec <= 64) KERNEL<X, H, 2, false><<<grid, threads, smem, st>>>(__VA_ARGS__); \
+    else if (n_vec <= 96) KERNEL<X, H, 3, false><<<grid, threads, smem, st>>>(__VA_ARGS__); \
+    else KERNEL<X, H, 4, false><<<grid, threads, smem, st>>>(__VA_ARGS__);  \
+  } while (0)
+#define SCALIFY_RMS_TYPES(xdt, hdt, KERNEL, ...)                                                                 \
+  do {                                                                                                           \
+    if (hdt == SCALIFY_F32) {                                                                                    \
+      if (xdt == SCALIFY_BF16) SCALIFY_RMS_VPT(SCALIFY_BF16, SCALIFY_F32, KERNEL, __VA_ARGS__);                  \
+      else if (xdt == SCALIFY_F16) SCALIFY_RMS_VPT(SCALIFY_F16, SCALIFY_F32, KERNEL, __VA_ARGS__);               \
+      else SCALIFY_RMS_VPT(SCALIFY_F32, SCALIFY_F32, KERNEL, __VA_ARGS__);                                       \
+    } else if (hdt == SCALIFY_BF16) SCALIFY_RMS_VPT(SCALIFY_BF16, SCALIFY_BF16, KERNEL, __VA_ARGS__);            \
+    else SCALIFY_RMS_VPT(SCALIFY_F16, SCALIFY_F16, KERNEL, __VA_ARGS__);                                         \
+  } while (0)
+
+int launch_add_rmsnorm(const RmsNormArgs& a, int x_dt, int h_dt, cudaStream_t st) {
+  const bool block = a.d > kWarpMaxD;
+  const int n_vec = (a.d + kVec - 1) / kVec;
+  const int64_t rows = a.sf ? (a.rows + 255) / 256 * 256 : a.rows;
+  const int threads = block ? block_threads(a.d) : 32 * kWarpRows;
+  const unsigned grid = static_cast<unsigned>(block ? rows : (rows + kWarpRows - 1) / kWarpRows);
+  const size_t smem = 0;
+  SCALIFY_RMS_TYPES(x_dt, h_dt, add_rmsnorm_kernel, a);
+  SCALIFY_CUDA_TRY(cudaGetLastError());
+  return SCALIFY_OK;
+}
+
+int launch_add_rmsnorm_bwd(RmsNormBwdArgs a, int g_dt, int h_dt, void* dgamma, int dgamma_dt, void* ws, cudaStream_t st) {
+  const bool block = a.d > kWarpMaxD;
+  const int n_vec = (a.d + kVec - 1) / kVec;
+  const int threads = block ? block_threads(a.d) : 32 * kWarpRows;
+  const int64_t want = block ? a.rows : (a.rows + kWarpRows - 1) / kWarpRows;
+  const int cap = bwd_grid_cap(a.d);
+  const unsigned grid = static_cast<unsigned>(want < cap ? want : cap);
+  const size_t smem = (!block && dgamma) ? static_cast<size_t>(kWarpRows) * n_vec * kVec * sizeof(float) : 0;
+  a.partial = nullptr;
+  a.stat_partial = nullptr;
+  float* stat_word = nullptr;
+  a.partial_ld = static_cast<int64_t>(n_vec) * kVec;
+  if (ws) {
+    WsView v = ws_view(ws);
+    a.status = v.status;
+    stat_word = v.stat;
+    if (dgamma) a.partial = static_cast<float*>(v.area);
+    a.stat_partial = reinterpret_cast<double*>(static_cast<float*>(v.area) + static_cast<int64_t>(cap) * a.partial_ld);
+  }
+  SCALIFY_RMS_TYPES(g_dt, h_dt, add_rmsnorm_bwd_kernel, a);
+  SCALIFY_CUDA_TRY(cudaGetLastError());
+  if (!dgamma && a.stat == SCALIFY_STAT_NONE) return SCALIFY_OK;
+  const unsigned blocks = (dgamma ? (a.d + 31) / 32 : 0) + (a.stat != SCALIFY_STAT_NONE ? 1 : 0);
+  const double count = static_cast<double>(a.rows) * a.d;
+  SCALIFY_DISPATCH_WIDE(dgamma_dt, ODT, add_rmsnorm_bwd_finish_kernel<ODT><<<blocks, 256, 0, st>>>(
+                                            a.partial, a.partial_ld, static_cast<int>(grid), dgamma ? a.d : 0, dgamma,
+                                            1.0f / a.kf, a.stat_partial, a.stat, count, stat_word))
+  SCALIFY_CUDA_TRY(cudaGetLastError());
+  return SCALIFY_OK;
+}
+
+}  // namespace scalify

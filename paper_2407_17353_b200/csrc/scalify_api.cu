@@ -87,6 +87,37 @@ static int as_rows(const scalify_array* a, int64_t* rows, int64_t* cols, int64_t
   return SCALIFY_ERR_SHAPE;
 }
 
+// The bytes between an array's first and last element, as [lo, hi); empty arrays span nothing.
+struct Span { uintptr_t lo, hi; };
+static Span span_of(const scalify_array* a) {
+  int64_t last = 0;
+  for (int i = 0; i < a->ndim; ++i) {
+    if (a->shape[i] == 0) return Span{0, 0};
+    last += (a->shape[i] - 1) * a->stride[i];
+  }
+  const uintptr_t lo = reinterpret_cast<uintptr_t>(a->data);
+  return Span{lo, lo + static_cast<uintptr_t>(last + 1) * elem_size(a->dtype)};
+}
+static bool overlap(Span a, Span b) { return a.lo < b.hi && b.lo < a.hi; }
+// Whether an output may share memory with an input: not at all, or as the very same rows (every element is read by the
+// thread that writes it).
+static bool disjoint_or_same(const scalify_array* out, int64_t out_ld, const scalify_array* in, int64_t in_ld) {
+  if (!in || !overlap(span_of(out), span_of(in))) return true;
+  return out->data == in->data && out->dtype == in->dtype && out_ld == in_ld;
+}
+static bool disjoint(const scalify_array* a, const scalify_array* b) { return !a || !b || !overlap(span_of(a), span_of(b)); }
+// Scale words an entry point writes (null entries skipped): none of them twice, none of them an input's.
+static int check_scale_words(const float* const* out, int n_out, const float* const* in, int n_in) {
+  for (int i = 0; i < n_out; ++i) {
+    if (!out[i]) continue;
+    for (int k = 0; k < i; ++k)
+      if (out[k] == out[i]) return SCALIFY_ERR_ALIAS;
+    for (int k = 0; k < n_in; ++k)
+      if (in[k] == out[i]) return SCALIFY_ERR_ALIAS;
+  }
+  return SCALIFY_OK;
+}
+
 }  // namespace scalify
 
 using namespace scalify;
@@ -127,6 +158,7 @@ size_t scalify_workspace_bytes(int op, int64_t d0, int64_t d1) {
     case SCALIFY_OP_ADAM: n = adam_ws_bytes(d0); break;
     case SCALIFY_OP_CROSS_ENTROPY: n = cross_entropy_ws_bytes(d0); break;
     case SCALIFY_OP_COLSUM: n = colsum_ws_bytes(d1); break;
+    case SCALIFY_OP_RMSNORM_BWD: n = rmsnorm_bwd_ws_bytes(d0, d1); break;
     case SCALIFY_OP_MATMUL_SPLITK: n = matmul_splitk_ws_bytes(d0, d1); break;
     default: break;
   }
@@ -472,6 +504,150 @@ int scalify_mx_matmul(const scalify_mx_array* A, const scalify_mx_array* B, scal
   a.transA = A->transposed;
   a.transB = B->transposed;
   return launch_mx_matmul(a, workspace, static_cast<cudaStream_t>(stream));
+}
+
+int scalify_scaled_add_rmsnorm(const scalify_array* X, const scalify_array* R, const scalify_array* gamma, float eps,
+                               scalify_array* H, scalify_array* Y, scalify_mx_array* Ymx, float* rinv, uint32_t* status,
+                               void* stream) {
+  int rc = check_array(X);
+  if (rc) return rc;
+  if (!is_wide(X->dtype)) return SCALIFY_ERR_DTYPE;
+  if ((R != nullptr) != (H != nullptr)) return SCALIFY_ERR_NULL;
+  if (!Y && !Ymx) return SCALIFY_ERR_NULL;
+  if (Y && Ymx) return SCALIFY_ERR_UNSUPPORTED;
+  if (!(eps >= 0.f) || isinf(eps)) return SCALIFY_ERR_VALUE;
+  RmsNormArgs a = {};
+  int64_t d;
+  if (as_rows(X, &a.rows, &d, &a.x_ld)) return SCALIFY_ERR_SHAPE;
+  if (d < 1 || d > kRmsNormMaxD || a.rows > 0x7FFFFFFF) return SCALIFY_ERR_SHAPE;
+  int64_t r2, d2;
+  if (R) {
+    rc = check_array(R);
+    if (!rc) rc = check_array(H);
+    if (rc) return rc;
+    if ((R->dtype != X->dtype && R->dtype != SCALIFY_F32) || H->dtype != R->dtype) return SCALIFY_ERR_DTYPE;
+    if (as_rows(R, &r2, &d2, &a.r_ld) || r2 != a.rows || d2 != d) return SCALIFY_ERR_SHAPE;
+    if (as_rows(H, &r2, &d2, &a.h_ld) || r2 != a.rows || d2 != d) return SCALIFY_ERR_SHAPE;
+    if (!disjoint_or_same(H, a.h_ld, R, a.r_ld) || !disjoint_or_same(H, a.h_ld, X, a.x_ld)) return SCALIFY_ERR_ALIAS;
+  }
+  if (gamma) {
+    rc = check_array(gamma);
+    if (rc) return rc;
+    if (!is_wide(gamma->dtype)) return SCALIFY_ERR_DTYPE;
+    if (gamma->ndim != 1 || gamma->shape[0] != d) return SCALIFY_ERR_SHAPE;
+    if (!disjoint(gamma, H)) return SCALIFY_ERR_ALIAS;
+  }
+  scalify_array mx_data = {};  // the block-scaled output's elements as a plain array
+  const scalify_array* out = Y;
+  if (Ymx) {
+    rc = check_mx(Ymx);
+    if (rc) return rc;
+    if (Ymx->transposed) return SCALIFY_ERR_UNSUPPORTED;
+    if (Ymx->rows != a.rows || Ymx->K != d) return SCALIFY_ERR_SHAPE;
+    mx_data.data = Ymx->data; mx_data.dtype = Ymx->dtype; mx_data.ndim = 2;
+    mx_data.shape[0] = a.rows; mx_data.shape[1] = d; mx_data.stride[0] = d; mx_data.stride[1] = 1;
+    mx_data.scale = Ymx->scale;
+    out = &mx_data;
+    a.sf = Ymx->sf;
+    a.y_ld = d;
+  } else {
+    rc = check_array(Y);
+    if (rc) return rc;
+    if (as_rows(Y, &r2, &d2, &a.y_ld) || r2 != a.rows || d2 != d) return SCALIFY_ERR_SHAPE;
+  }
+  if (!disjoint(out, X) || !disjoint(out, R) || !disjoint(out, H) || !disjoint(out, gamma)) return SCALIFY_ERR_ALIAS;
+  {
+    const float* outs[2] = {H ? H->scale : nullptr, out->scale};
+    const float* ins[3] = {X->scale, R ? R->scale : nullptr, gamma ? gamma->scale : nullptr};
+    rc = check_scale_words(outs, 2, ins, 3);
+    if (rc) return rc;
+  }
+  if (a.rows == 0) return SCALIFY_OK;
+  a.d = static_cast<int>(d);
+  a.eps = eps;
+  a.X = X->data; a.x_scale = X->scale;
+  if (R) { a.R = R->data; a.r_scale = R->scale; a.H = H->data; a.h_scale = H->scale; }
+  if (gamma) { a.gamma = gamma->data; a.gamma_dt = gamma->dtype; a.gamma_scale = gamma->scale; }
+  a.Y = out->data; a.y_dt = out->dtype; a.y_es = elem_size(out->dtype); a.y_scale = out->scale;
+  a.rinv = rinv;
+  a.status = status;
+  return launch_add_rmsnorm(a, X->dtype, R ? R->dtype : X->dtype, static_cast<cudaStream_t>(stream));
+}
+
+int scalify_scaled_add_rmsnorm_bwd(const scalify_array* G, const scalify_array* Gr, const scalify_array* H,
+                                   const scalify_array* gamma, const float* rinv, scalify_array* dX, scalify_array* dXq,
+                                   const float* stat_in, int stat_dx, scalify_array* dgamma, void* workspace,
+                                   size_t workspace_bytes, void* stream) {
+  int rc = check_array(G);
+  if (!rc) rc = check_array(H);
+  if (!rc) rc = check_array(dX);
+  if (rc) return rc;
+  if (!rinv) return SCALIFY_ERR_NULL;
+  if (!valid_stat(stat_dx)) return SCALIFY_ERR_VALUE;
+  if (stat_in && !dXq) return SCALIFY_ERR_NULL;  // nothing to rescale
+  if (!is_wide(G->dtype) || (H->dtype != G->dtype && H->dtype != SCALIFY_F32) || dX->dtype != H->dtype) return SCALIFY_ERR_DTYPE;
+  RmsNormBwdArgs a = {};
+  int64_t d, r2, d2;
+  if (as_rows(H, &a.rows, &d, &a.h_ld)) return SCALIFY_ERR_SHAPE;
+  if (a.rows < 1 || a.rows > 0x7FFFFFFF || d < 1 || d > kRmsNormMaxD) return SCALIFY_ERR_SHAPE;
+  if (as_rows(G, &r2, &d2, &a.g_ld) || r2 != a.rows || d2 != d) return SCALIFY_ERR_SHAPE;
+  if (as_rows(dX, &r2, &d2, &a.dx_ld) || r2 != a.rows || d2 != d) return SCALIFY_ERR_SHAPE;
+  if (Gr) {
+    rc = check_array(Gr);
+    if (rc) return rc;
+    if (Gr->dtype != H->dtype) return SCALIFY_ERR_DTYPE;
+    if (as_rows(Gr, &r2, &d2, &a.gr_ld) || r2 != a.rows || d2 != d) return SCALIFY_ERR_SHAPE;
+  }
+  if (gamma) {
+    rc = check_array(gamma);
+    if (rc) return rc;
+    if (!is_wide(gamma->dtype)) return SCALIFY_ERR_DTYPE;
+    if (gamma->ndim != 1 || gamma->shape[0] != d) return SCALIFY_ERR_SHAPE;
+  }
+  if (dgamma) {
+    rc = check_array(dgamma);
+    if (rc) return rc;
+    if (!is_wide(dgamma->dtype)) return SCALIFY_ERR_DTYPE;
+    if (dgamma->ndim != 1 || dgamma->shape[0] != d) return SCALIFY_ERR_SHAPE;
+  }
+  if (dXq) {
+    rc = check_array(dXq);
+    if (rc) return rc;
+    if (!is_fp8(dXq->dtype)) return SCALIFY_ERR_DTYPE;
+    if (as_rows(dXq, &r2, &d2, &a.dxq_ld) || r2 != a.rows || d2 != d) return SCALIFY_ERR_SHAPE;
+  }
+  if (!disjoint_or_same(dX, a.dx_ld, G, a.g_ld) || !disjoint_or_same(dX, a.dx_ld, Gr, a.gr_ld) || !disjoint(dX, H) ||
+      !disjoint(dX, gamma) || !disjoint(dX, dgamma) || !disjoint(dX, dXq))
+    return SCALIFY_ERR_ALIAS;
+  for (const scalify_array* o : {static_cast<const scalify_array*>(dXq), static_cast<const scalify_array*>(dgamma)})
+    if (o && (!disjoint(o, G) || !disjoint(o, Gr) || !disjoint(o, H) || !disjoint(o, gamma))) return SCALIFY_ERR_ALIAS;
+  if (!disjoint(dXq, dgamma)) return SCALIFY_ERR_ALIAS;
+  {
+    const float* outs[3] = {dX->scale, dXq ? dXq->scale : nullptr, dgamma ? dgamma->scale : nullptr};
+    const float* ins[5] = {G->scale, Gr ? Gr->scale : nullptr, H->scale, gamma ? gamma->scale : nullptr, stat_in};
+    rc = check_scale_words(outs, 3, ins, 5);
+    if (rc) return rc;
+  }
+  if (workspace || dgamma || stat_dx != SCALIFY_STAT_NONE) {
+    rc = check_ws(workspace, workspace_bytes, scalify_workspace_bytes(SCALIFY_OP_RMSNORM_BWD, a.rows, d));
+    if (rc) return rc;
+    if (stat_in && stat_in == ws_view(workspace).stat && stat_dx != SCALIFY_STAT_NONE) return SCALIFY_ERR_ALIAS;
+  }
+  a.d = static_cast<int>(d);
+  a.G = G->data; a.g_scale = G->scale;
+  if (Gr) { a.Gr = Gr->data; a.gr_scale = Gr->scale; }
+  a.H = H->data; a.h_scale = H->scale;
+  if (gamma) { a.gamma = gamma->data; a.gamma_dt = gamma->dtype; a.gamma_scale = gamma->scale; }
+  a.rinv = rinv;
+  a.dX = dX->data; a.dx_scale = dX->scale;
+  if (dXq) { a.dXq = dXq->data; a.dxq_dt = dXq->dtype; a.dxq_scale = dXq->scale; }
+  a.stat_in = stat_in;
+  a.dgamma_scale = dgamma ? dgamma->scale : nullptr;
+  a.stat = stat_dx;
+  a.kf = kfactor(a.rows);
+  return launch_add_rmsnorm_bwd(a, G->dtype, H->dtype, dgamma ? dgamma->data : nullptr,
+                                dgamma ? dgamma->dtype : static_cast<int>(SCALIFY_F32), workspace,
+                                static_cast<cudaStream_t>(stream));
 }
 
 int scalify_scaled_colsum(const scalify_array* X, scalify_array* Y, void* workspace, size_t workspace_bytes,

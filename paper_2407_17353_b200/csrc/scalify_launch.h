@@ -157,6 +157,42 @@ struct AttentionBwdArgs {
   uint32_t* status;
 };
 int launch_attention_bwd(const AttentionBwdArgs& a, cudaStream_t st);
+// Residual addition + RMS norm.  With R == nullptr, X is the residual stream itself (its dtype is the H dtype of the
+// launch) and H is not written.  sf != nullptr: block-scaled output.
+constexpr int kRmsNormMaxD = 16384;
+struct RmsNormArgs {
+  const void* X; int64_t x_ld; const float* x_scale;
+  const void* R; int64_t r_ld; const float* r_scale;
+  const void* gamma; int gamma_dt; const float* gamma_scale;
+  void* H; int64_t h_ld; float* h_scale;
+  void* Y; int64_t y_ld; int y_dt, y_es; float* y_scale;
+  uint8_t* sf;
+  float* rinv;
+  uint32_t* status;
+  int64_t rows;
+  int d;
+  float eps;
+};
+int launch_add_rmsnorm(const RmsNormArgs& a, int x_dt, int h_dt, cudaStream_t st);
+struct RmsNormBwdArgs {
+  const void* G; int64_t g_ld; const float* g_scale;
+  const void* Gr; int64_t gr_ld; const float* gr_scale;   // gradient of H itself, or nullptr
+  const void* H; int64_t h_ld; const float* h_scale;
+  const void* gamma; int gamma_dt; const float* gamma_scale;
+  const float* rinv;
+  void* dX; int64_t dx_ld; float* dx_scale;
+  void* dXq; int64_t dxq_ld; int dxq_dt; float* dxq_scale;
+  const float* stat_in;
+  float* dgamma_scale;
+  int stat;
+  float kf;
+  int64_t rows;
+  int d;
+  // set by the launcher: workspace areas
+  float* partial; int64_t partial_ld; double* stat_partial; uint32_t* status;
+};
+size_t rmsnorm_bwd_ws_bytes(int64_t rows, int64_t d);
+int launch_add_rmsnorm_bwd(RmsNormBwdArgs a, int g_dt, int h_dt, void* dgamma, int dgamma_dt, void* ws, cudaStream_t st);
 int launch_mx_quantize_t(const void* X, int x_dt, int64_t rows, int64_t K, int64_t ldx, void* data, int elem_dt,
                          uint8_t* sf, const float* x_scale, float* y_scale, uint32_t* status, cudaStream_t st);
 int launch_mx_quantize(const void* X, int x_dt, int64_t rows, int64_t K, int64_t ldx, void* data, int elem_dt,

@@ -1,0 +1,141 @@
+"""Host-side refusals of the norm, embedding and optimiser entry points, and the plain 64-bit gradients against
+differences (no GPU needed: a call that fails validation launches nothing)."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2407_17353_b200 as sc
+import plain64 as p64
+
+R = ctypes.byref
+NULL, DTYPE, SHAPE, ALIGN, WORKSPACE, UNSUPPORTED, ALIAS, VALUE = -1, -2, -3, -4, -5, -6, -8, -9
+MB = 1 << 20
+
+
+def arr(mb, dtype, shape, stride=None, scale=None, offset=0):
+    """Descriptor of a made-up array that begins `mb` megabytes into the address space."""
+    a = sc.scalify_array()
+    a.data, a.dtype, a.ndim = mb * MB + offset, dtype, len(shape)
+    if stride is None:
+        stride, n = [], 1
+        for s in reversed(shape):
+            stride.insert(0, n)
+            n *= s
+    for i, (s, t) in enumerate(zip(shape, stride)):
+        a.shape[i], a.stride[i] = s, t
+    a.scale = scale
+    return a
+
+
+def mx(mb, dtype, rows, K, transposed=0):
+    return sc.scalify_mx_array(mb * MB, dtype, rows, K, mb * MB + (MB >> 1), None, transposed)
+
+
+def norm_call(X=None, Rr=None, gamma=None, eps=1e-5, H=None, Y=None, Ymx=None):
+    p = lambda a: None if a is None else R(a)  # noqa: E731
+    return sc.lib().scalify_scaled_add_rmsnorm(p(X), p(Rr), p(gamma), eps, p(H), p(Y),
+                                               None if Ymx is None else ctypes.addressof(Ymx), None, None, None)
+
+
+def test_norm_refusals():
+    B, F, Q = sc.BF16, sc.F32, sc.E4M3
+    x, r, h, y = arr(1, B, (4, 128)), arr(2, B, (4, 128)), arr(3, B, (4, 128)), arr(4, Q, (4, 128))
+    assert norm_call(None, r, None, 1e-5, h, y) == NULL
+    assert norm_call(x, r, None, 1e-5, None, y) == NULL          # a residual without the sum
+    assert norm_call(x, None, None, 1e-5, h, y) == NULL          # a sum without a residual
+    assert norm_call(x, r, None, 1e-5, h, None) == NULL          # no output
+    assert norm_call(x, r, None, 1e-5, h, y, mx(5, Q, 4, 128)) == UNSUPPORTED
+    assert norm_call(x, r, None, 1e-5, h, None, mx(5, Q, 16, 128, 1)) == UNSUPPORTED
+    assert norm_call(x, r, None, 1e-5, h, None, mx(5, Q, 5, 128)) == SHAPE
+    assert norm_call(arr(1, B, (4, 64)), None, None, 1e-5, None, None, mx(5, Q, 4, 64)) == SHAPE
+    assert norm_call(arr(1, Q, (4, 128)), r, None, 1e-5, h, y) == DTYPE
+    assert norm_call(x, arr(2, sc.F16, (4, 128)), None, 1e-5, arr(3, sc.F16, (4, 128)), y) == DTYPE
+    assert norm_call(x, arr(2, F, (4, 128)), None, 1e-5, h, y) == DTYPE
+    assert norm_call(arr(1, F, (4, 128)), r, None, 1e-5, h, y) == DTYPE
+    assert norm_call(x, arr(2, B, (4, 120)), None, 1e-5, h, y) == SHAPE
+    assert norm_call(x, r, None, 1e-5, h, arr(4, Q, (5, 128))) == SHAPE
+    assert norm_call(arr(1, B, (1, 16392)), None, None, 1e-5, None, arr(4, B, (1, 16392))) == SHAPE
+    assert norm_call(x, r, arr(5, F, (127,)), 1e-5, h, y) == SHAPE
+    assert norm_call(x, r, arr(5, Q, (128,)), 1e-5, h, y) == DTYPE
+    assert norm_call(x, r, None, -1.0, h, y) == VALUE
+    assert norm_call(x, r, None, float("nan"), h, y) == VALUE
+    assert norm_call(x, r, None, float("inf"), h, y) == VALUE
+    assert norm_call(x, r, None, 1e-5, h, arr(4, Q, (4, 128), offset=8)) == ALIGN
+    assert norm_call(x, r, None, 1e-5, h, arr(4, Q, (4, 128), (136, 1))) == ALIGN
+    assert norm_call(x, r, None, 1e-5, arr(1, B, (4, 128), offset=16), y) == ALIAS   # overlaps X, not the same rows
+    assert norm_call(x, r, None, 1e-5, arr(2, B, (4, 128), (136, 1)), y) == ALIAS    # R's buffer, other stride
+    assert norm_call(x, r, None, 1e-5, h, arr(1, B, (4, 128))) == ALIAS              # Y over X
+    assert norm_call(x, r, None, 1e-5, h, arr(3, B, (4, 128))) == ALIAS              # Y over H
+    assert norm_call(arr(1, B, (4, 128), scale=64), r, None, 1e-5, arr(3, B, (4, 128), scale=64), y) == ALIAS
+    assert norm_call(x, r, None, 1e-5, arr(3, B, (4, 128), scale=64), arr(4, Q, (4, 128), scale=64)) == ALIAS
+
+
+def norm_bwd(G=None, Gr=None, H=None, gamma=None, rinv=8 * MB, dX=None, dXq=None, stat_in=None, stat=0, dg=None, ws=None, nb=0):
+    p = lambda a: None if a is None else R(a)  # noqa: E731
+    return sc.lib().scalify_scaled_add_rmsnorm_bwd(p(G), p(Gr), p(H), p(gamma), rinv, p(dX), p(dXq), stat_in, stat, p(dg), ws,
+                                                   nb, None)
+
+
+def test_norm_backward_refusals():
+    B, F, Q = sc.BF16, sc.F32, sc.E5M2
+    g, h, dx = arr(1, B, (4, 128)), arr(2, B, (4, 128)), arr(3, B, (4, 128))
+    ok = dict(G=g, H=h, dX=dx)
+    assert norm_bwd(**{**ok, "G": None}) == NULL
+    assert norm_bwd(**ok, rinv=None) == NULL
+    assert norm_bwd(**ok, stat_in=64) == NULL                          # a rescale without the copy it applies to
+    assert norm_bwd(**{**ok, "dX": arr(3, F, (4, 128))}) == DTYPE
+    assert norm_bwd(**{**ok, "H": arr(2, sc.F16, (4, 128)), "dX": arr(3, sc.F16, (4, 128))}) == DTYPE
+    assert norm_bwd(**ok, Gr=arr(4, F, (4, 128))) == DTYPE
+    assert norm_bwd(**ok, dXq=arr(4, B, (4, 128))) == DTYPE
+    assert norm_bwd(**ok, dXq=arr(4, Q, (4, 112))) == SHAPE
+    assert norm_bwd(**{**ok, "G": arr(1, B, (3, 128))}) == SHAPE
+    assert norm_bwd(G=arr(1, B, (0, 128)), H=arr(2, B, (0, 128)), dX=arr(3, B, (0, 128))) == SHAPE
+    assert norm_bwd(**ok, stat=3) == VALUE
+    assert norm_bwd(**ok, dg=arr(4, F, (128,))) == WORKSPACE
+    assert norm_bwd(**ok, stat=1) == WORKSPACE
+    assert norm_bwd(**ok, stat=1, ws=16 * MB, nb=300) == WORKSPACE
+    assert norm_bwd(**ok, stat=1, ws=16 * MB + 64, nb=64 * MB) == WORKSPACE
+    assert norm_bwd(**{**ok, "dX": arr(2, B, (4, 128))}) == ALIAS        # dX over H
+    assert norm_bwd(**ok, dXq=arr(1, Q, (4, 128))) == ALIAS              # the copy over G
+    assert norm_bwd(**ok, Gr=arr(3, B, (4, 128), offset=16)) == ALIAS
+    assert norm_bwd(**ok, dXq=arr(4, Q, (4, 128)), stat_in=16 * MB + 16, stat=1, ws=16 * MB, nb=64 * MB) == ALIAS
+    assert norm_bwd(**{**ok, "dX": arr(3, B, (4, 128), scale=64), "H": arr(2, B, (4, 128), scale=64)}) == ALIAS
+
+
+def test_arrays_of_different_devices_are_refused_by_the_binding():
+    x = sc.ScaledTensor(torch.zeros(4, 64, dtype=torch.bfloat16))
+    with pytest.raises(ValueError):
+        sc.scalify_scaled_add_rmsnorm(x, None, None, None, sc.ScaledTensor(torch.zeros(4, 64, dtype=torch.bfloat16)))
+    with pytest.raises(ValueError):
+        sc.scalify_scaled_add_rmsnorm(x, None, None, None, sc.ScaledTensor(torch.zeros(4, 64, dtype=torch.bfloat16, device="meta")))
+    with pytest.raises(ValueError):
+        sc.scalify_scaled_add_rmsnorm(x, None, None, None, x, rinv=torch.zeros(3))
+
+
+def test_plain_norm_gradient_against_differences():
+    torch.manual_seed(0)
+    rows, d, eps = 3, 10, 1e-3
+    x, r, gam, up = (torch.randn(*s, dtype=torch.float64) for s in ((rows, d), (rows, d), (d,), (rows, d)))
+    res = torch.randn(rows, d, dtype=torch.float64)
+    xs, rs = 0.5, 2.0
+
+    def loss(x, gam):
+        total, hs, norm = p64.add_rmsnorm(x, xs, r, rs, gam, eps)
+        return float((norm(total)[0] * up).sum() + (total * hs * res).sum())
+    total, hs, norm = p64.add_rmsnorm(x, xs, r, rs, gam, eps)
+    _, rinv = norm(total)
+    got = p64.add_rmsnorm_bwd(up, 1.0, res, 1.0, total, hs, gam, 1.0, rinv)
+    dx, step = got["dX"] * got["dX_s"], 1e-6
+    for i, j in ((0, 0), (1, 4), (2, 9)):
+        e = torch.zeros_like(x)
+        e[i, j] = step
+        # the derivative with respect to the VALUE of x: its data move by step / xs
+        diff = (loss(x + e / xs, gam) - loss(x - e / xs, gam)) / (2 * step)
+        assert abs(diff - float(dx[i, j])) < 1e-6 * max(1.0, abs(diff))
+    dg = got["dgamma"] * got["dgamma_s"]
+    for j in (0, 5):
+        e = torch.zeros_like(gam)
+        e[j] = step
+        diff = (loss(x, gam + e) - loss(x, gam - e)) / (2 * step)
+        assert abs(diff - float(dg[j])) < 1e-6 * max(1.0, abs(diff))
