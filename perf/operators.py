@@ -219,7 +219,7 @@ def _library(s):
     elif op == "lookup_grad":
         s["args"] = [T(s["G"], s["G_s"]), T(s["W"], s["W_s"])]
         s["addend"] = T(s["A"], s["A_s"]) if c["tied"] else None
-        s["ws"] = sc.Workspace(sc.scalify_workspace_bytes(sc.OP_EMBEDDING_GRAD, c["n"], c["vocab"]))
+        s["ws"] = sc.Workspace(sc.scalify_workspace_bytes(sc.OP_EMBEDDING_GRAD, c["n"], c["d"]))
     elif op == "orthogonalize":
         s["args"] = [T(s["X"], s["X_s"]), T(s["O"], s["O_s"])]
         s["ws"] = sc.Workspace(sc.scalify_muon_workspace_bytes([s["args"][0]]))
