@@ -101,7 +101,8 @@ enum {
   SCALIFY_OP_CROSS_ENTROPY = 5, /* d0 = number of rows */
   SCALIFY_OP_COLSUM = 6,        /* d0 = rows, d1 = columns */
   SCALIFY_OP_MATMUL_SPLITK = 7, /* d0 = M, d1 = N: room for the partial products of a split contraction */
-  SCALIFY_OP_RMSNORM_BWD = 8    /* d0 = rows, d1 = row length */
+  SCALIFY_OP_RMSNORM_BWD = 8,   /* d0 = rows, d1 = row length */
+  SCALIFY_OP_EMBEDDING_GRAD = 9 /* d0 = number of tokens, d1 = row length */
 };
 
 /* Bytes of workspace the given call needs (an upper bound; always >= 4096).
@@ -501,6 +502,35 @@ int scalify_scaled_embedding(const int64_t* ids, int64_t n, int64_t seq_len, con
                              const scalify_array* wpe, scalify_array* Y, uint32_t* status, void* stream);
 int scalify_scaled_embedding_bwd(const int64_t* ids, int64_t n, int64_t seq_len, const scalify_array* dY,
                                  scalify_array* dwte, scalify_array* dwpe, void* stream);
+
+/*
+ * Embedding lookup with a constant factor c > 0 (a scalar constant, Section 3.4: its power of two goes into the scale,
+ * the rest, in [1, 2), into the data):
+ *   Y_s = wte_s * p2(c),   Y_d[i] = cast(wte_d[ids[i]] * (c / p2(c)))
+ * ids: DEVICE int64 [n].  A token equal to padding_id gives a row of zeros (INT64_MIN: no padding); any other token
+ * outside [0, vocab) does too, and sets SCALIFY_DEV_BAD_INDEX in *status (optional DEVICE word).  wte: [vocab,d] of any
+ * dtype; Y: [n,d] of any dtype; any d; rows may be strided.
+ * Errors: NULL, DTYPE, SHAPE, ALIGNMENT, VALUE (c not a positive normal number), ALIAS.
+ */
+int scalify_scaled_embedding_lookup(const int64_t* ids, int64_t n, int64_t padding_id, const scalify_array* wte, float c,
+                                    scalify_array* Y, uint32_t* status, void* stream);
+
+/*
+ * Its gradient, summed over SORTED tokens (scalify_scaled_embedding_bwd uses atomics, whose order changes the last bits;
+ * here the token ids alone fix the order of every sum, and the same call gives the same bits every time):
+ *   dwte_d[v] = (c / p2(c)) * sum of the rows of dY_d whose token is v,   scale dY_s * p2(c)
+ * (no static factor: the number of addends depends on the data), sums in fp32.  With `addend` (the gradient of a tied
+ * output layer) the result is addend + that by the add rule, rounded once: dwte_s = max(dY_s * p2(c), addend_s).
+ * Every row of dwte is written: a token that does not occur, and the padding token, get zeros (or the addend).
+ * ids, padding_id, c as for the lookup (an unknown token sets SCALIFY_DEV_BAD_INDEX in the workspace status word and is
+ * left out).  dY: [n,d] of any dtype; dwte: [vocab,d], F16/BF16/F32; addend: dwte's dtype and shape, or NULL, and may be
+ * dwte's own buffer (same row stride: the gradient is then accumulated in place).  n may be 0.  n, vocab < 2^31.
+ * Workspace: SCALIFY_OP_EMBEDDING_GRAD (n, d).
+ * Errors: NULL, DTYPE, SHAPE, ALIGNMENT, VALUE, ALIAS, WORKSPACE.
+ */
+int scalify_scaled_embedding_grad(const int64_t* ids, int64_t n, int64_t padding_id, const scalify_array* dY, float c,
+                                  const scalify_array* addend, scalify_array* dwte, void* workspace,
+                                  size_t workspace_bytes, void* stream);
 
 /*
  * Row softmax of the VALUES S_d*S_s over the last dimension, optionally causal (row i of each

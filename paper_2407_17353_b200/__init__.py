@@ -24,7 +24,7 @@ E4M3, E5M2, F16, BF16, F32 = 0, 1, 2, 3, 4
 STAT_NONE, STAT_AMAX, STAT_L2 = 0, 1, 2
 OP_MATMUL, OP_RESCALE, OP_LAYERNORM_BWD, OP_ADAM, OP_STATISTIC, OP_CROSS_ENTROPY, OP_COLSUM, OP_MATMUL_SPLITK = (
     0, 1, 2, 3, 4, 5, 6, 7)
-OP_RMSNORM_BWD = 8
+OP_RMSNORM_BWD, OP_EMBEDDING_GRAD = 8, 9
 DEV_TIMEOUT, DEV_BAD_SCALE, DEV_NONFINITE_STAT, DEV_BAD_INDEX = 1, 2, 4, 8
 
 _DTYPE_CODE = {torch.float8_e4m3fn: E4M3, torch.float8_e5m2: E5M2, torch.float16: F16,
@@ -115,7 +115,10 @@ def lib() -> ctypes.CDLL:
         L.scalify_scaled_adam_step_static.argtypes = [i32, P, P, P, P, f32, f32, f32, f32, i64, vp, vp]
         L.scalify_scaled_add_rmsnorm.argtypes = [P, P, P, f32, P, P, vp, vp, vp, vp]
         L.scalify_scaled_add_rmsnorm_bwd.argtypes = [P, P, P, P, vp, P, P, vp, i32, P, vp, sz, vp]
-        for name in ("scalify_scaled_add_rmsnorm", "scalify_scaled_add_rmsnorm_bwd", "scalify_workspace_init", "scalify_check_status", "scalify_scaled_matmul", "scalify_scaled_matmul_delayed",
+        L.scalify_scaled_embedding_lookup.argtypes = [vp, i64, i64, P, f32, P, vp, vp]
+        L.scalify_scaled_embedding_grad.argtypes = [vp, i64, i64, P, f32, P, P, vp, sz, vp]
+        for name in ("scalify_scaled_add_rmsnorm", "scalify_scaled_add_rmsnorm_bwd", "scalify_scaled_embedding_lookup",
+                     "scalify_scaled_embedding_grad", "scalify_workspace_init", "scalify_check_status", "scalify_scaled_matmul", "scalify_scaled_matmul_delayed",
                      "scalify_statistic",
                      "scalify_rescale", "scalify_scaled_add", "scalify_scaled_layernorm",
                      "scalify_scaled_layernorm_bwd", "scalify_scaled_gelu", "scalify_scaled_gelu_bwd",
@@ -611,3 +614,31 @@ def scalify_scaled_add_rmsnorm_bwd(G: ScaledTensor, Gr: Optional[ScaledTensor], 
     g, gr, h, gm, dx, dq, dg = (_desc(G), _desc(Gr), _desc(H), _desc(gamma), _desc(dX), _desc(dXq), _desc(dgamma))
     _call(name, dev, stream, _ref(g), _ref(gr), _ref(h), _ref(gm), _ptr(rinv), _ref(dx), _ref(dq), _ptr(stat_in),
           int(stat_dx), _ref(dg), None if ws is None else ws.ptr, 0 if ws is None else ws.nbytes)
+
+
+def _token_ids(name: str, ids: torch.Tensor, padding_id: Optional[int]) -> int:
+    if ids.dtype != torch.int64 or not ids.is_contiguous():
+        raise ValueError(f"{name}: ids must be a contiguous int64 tensor")
+    return -(1 << 63) if padding_id is None else int(padding_id)
+
+
+def scalify_scaled_embedding_lookup(ids: torch.Tensor, wte: ScaledTensor, Y: ScaledTensor, *, c: float = 1.0,
+                                    padding_id: Optional[int] = None, status: Optional[torch.Tensor] = None,
+                                    stream=None) -> None:
+    """Y[i] = c * wte[ids[i]]; padding (and unknown) tokens give rows of zeros."""
+    name = "scalify_scaled_embedding_lookup"
+    pad = _token_ids(name, ids, padding_id)
+    dev = _same_device(name, wte.data, ids, Y.data, status)
+    w, y = _desc(wte), _desc(Y)
+    _call(name, dev, stream, ids.data_ptr(), ids.numel(), pad, _ref(w), float(c), _ref(y), _ptr(status))
+
+
+def scalify_scaled_embedding_grad(ids: torch.Tensor, dY: ScaledTensor, dwte: ScaledTensor, ws: Workspace, *,
+                                  c: float = 1.0, padding_id: Optional[int] = None,
+                                  addend: Optional[ScaledTensor] = None, stream=None) -> None:
+    """dwte = (addend +) c * sum of the rows of dY per token, in an order that the ids alone determine."""
+    name = "scalify_scaled_embedding_grad"
+    pad = _token_ids(name, ids, padding_id)
+    dev = _same_device(name, dwte.data, ids, dY.data, _data(addend), ws.buf)
+    g, w, a = _desc(dY), _desc(dwte), _desc(addend)
+    _call(name, dev, stream, ids.data_ptr(), ids.numel(), pad, _ref(g), float(c), _ref(a), _ref(w), ws.ptr, ws.nbytes)

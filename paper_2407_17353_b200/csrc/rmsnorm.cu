@@ -23,6 +23,8 @@ namespace {
 constexpr int kVec = 8;          // elements per vector: 16 bytes of a 16-bit format
 constexpr int kWarpRows = 4;     // rows (warps) per block of the warp-per-row forms
 constexpr int kWarpMaxD = 1024;  // longest row one warp holds
+constexpr int kPrefetchThreads = 384;  // of the backward form that loads the next row ahead (168 registers a thread)
+constexpr int kBwdWarpBlocks = 4;      // resident blocks per SM of the backward warp-per-row form
 constexpr int kBlockThreads = 512;  // most threads of the block-per-row forms (leaves 128 registers a thread)
 
 // Raw words of vector v of a row (n = elements of it inside the row; the rest read as zero).
@@ -227,12 +229,18 @@ __global__ void __launch_bounds__(BLOCK ? kBlockThreads : 32 * kWarpRows) add_rm
 // Persistent teams walk the rows (grid stride); a team keeps its columns' share of dgamma in registers over all its
 // rows and leaves it in the workspace, one line per block, added in block order by the second launch: the result does
 // not depend on scheduling.  The statistic of the stored dX travels the same way.
+// The launch bounds leave 128 registers a thread to the warp-per-row form (four blocks of four warps per SM, which is
+// what covers the load latency there).  The block-per-row form with 2 vectors per thread holds the NEXT row's words in
+// registers while it works on the current one, so that the two barriers of a row do not leave the memory idle; the form
+// for very long rows has no registers left for that.
 template <int GDT, int HDT, int VPT, bool BLOCK>
-__global__ void __launch_bounds__(BLOCK ? kBlockThreads : 32 * kWarpRows) add_rmsnorm_bwd_kernel(const RmsNormBwdArgs a) {
+__global__ void __launch_bounds__(BLOCK ? (VPT == 2 ? kPrefetchThreads : kBlockThreads) : 32 * kWarpRows,
+                                  BLOCK ? 1 : kBwdWarpBlocks) add_rmsnorm_bwd_kernel(const RmsNormBwdArgs a) {
   asm volatile("griddepcontrol.launch_dependents;");  // a programmatic dependent may set up while this grid runs
-  extern __shared__ float s_dg[];  // warp-per-row form: [kWarpRows][d] to add up the block's warps
+  extern __shared__ float s_dyn[];  // warp-per-row form: gamma [d], then [kWarpRows][d] to add up the block's warps
   __shared__ float s_red[32];
   __shared__ double s_stat[32];
+  constexpr bool kPrefetch = BLOCK && VPT == 2;
   const int team = BLOCK ? blockDim.x : 32;
   const int lane = BLOCK ? threadIdx.x : threadIdx.x & 31;
   const int warp = threadIdx.x >> 5;
@@ -261,45 +269,94 @@ __global__ void __launch_bounds__(BLOCK ? kBlockThreads : 32 * kWarpRows) add_rm
   constexpr int GW = kVec * ElemBytes<GDT>::v / 4, HW = kVec * ElemBytes<HDT>::v / 4;
   const float inv_d = 1.0f / static_cast<float>(a.d);
   float dg[VPT][kVec];
+  float gam_reg[BLOCK ? VPT : 1][kVec];  // a thread meets the same columns in every row
 #pragma unroll
-  for (int i = 0; i < VPT; ++i)
+  for (int i = 0; i < VPT; ++i) {
+    const int v = lane + i * team;
 #pragma unroll
     for (int e = 0; e < kVec; ++e) dg[i][e] = 0.f;
+    if constexpr (BLOCK) {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) gam_reg[i][e] = 0.f;
+      if (v < n_vec) load_gamma(a.gamma, a.gamma_dt, v, a.d - v * kVec, gam_reg[i]);
+    } else if (warp == 0 && v < n_vec) {
+      load_gamma(a.gamma, a.gamma_dt, v, a.d - v * kVec, gam_reg[0]);
+#pragma unroll
+      for (int e = 0; e < kVec; e += 4)
+        *reinterpret_cast<float4*>(s_dyn + v * kVec + e) = make_float4(gam_reg[0][e], gam_reg[0][e + 1], gam_reg[0][e + 2], gam_reg[0][e + 3]);
+    }
+  }
+  if constexpr (!BLOCK) __syncthreads();
+  auto gamma_of = [&](int i, int v, float* gam) {
+    if constexpr (BLOCK) {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) gam[e] = gam_reg[i][e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < kVec; e += 4) {
+        const float4 t = *reinterpret_cast<const float4*>(s_dyn + v * kVec + e);
+        gam[e] = t.x; gam[e + 1] = t.y; gam[e + 2] = t.z; gam[e + 3] = t.w;
+      }
+    }
+  };
   uint32_t amax = 0u;
   double ssq = 0.0;
-  for (int64_t row = first; row < a.rows; row += stride) {
+  uint32_t wg[VPT][GW], wh[VPT][HW], wr[VPT][HW];
+  float rinv = 0.f;
+  // words of one row; vectors outside the row stay zero, so that they add nothing to any sum below
+  auto load_row = [&](int64_t row, uint32_t (&xg)[VPT][GW], uint32_t (&xh)[VPT][HW], uint32_t (&xr)[VPT][HW], float& ri) {
     const char* grow = static_cast<const char*>(a.G) + row * a.g_ld * ElemBytes<GDT>::v;
     const char* hrow = static_cast<const char*>(a.H) + row * a.h_ld * ElemBytes<HDT>::v;
     const char* rrow = a.Gr ? static_cast<const char*>(a.Gr) + row * a.gr_ld * ElemBytes<HDT>::v : nullptr;
-    uint32_t wg[VPT][GW], wh[VPT][HW], wr[VPT][HW];
+    ri = __ldg(a.rinv + row);
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       const int v = lane + i * team;
       if (v < n_vec) {
-        load_vec<GDT>(grow, v, a.d - v * kVec, wg[i]);
-        load_vec<HDT>(hrow, v, a.d - v * kVec, wh[i]);
-        if (rrow) load_vec<HDT>(rrow, v, a.d - v * kVec, wr[i]);
-      } else {
-#pragma unroll
-        for (int q = 0; q < GW; ++q) wg[i][q] = 0u;
-#pragma unroll
-        for (int q = 0; q < HW; ++q) wh[i][q] = 0u;
+        load_vec<GDT>(grow, v, a.d - v * kVec, xg[i]);
+        load_vec<HDT>(hrow, v, a.d - v * kVec, xh[i]);
+        if (rrow) load_vec<HDT>(rrow, v, a.d - v * kVec, xr[i]);
       }
     }
-    const float rinv = __ldg(a.rinv + row);
+  };
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) {
+#pragma unroll
+    for (int q = 0; q < GW; ++q) wg[i][q] = 0u;
+#pragma unroll
+    for (int q = 0; q < HW; ++q) wh[i][q] = wr[i][q] = 0u;
+  }
+  if (kPrefetch && first < a.rows) load_row(first, wg, wh, wr, rinv);
+  for (int64_t row = first; row < a.rows; row += stride) {
+    uint32_t ng[VPT][GW], nh[VPT][HW], nr[VPT][HW];
+    float nri = 0.f;
+    if constexpr (kPrefetch) {
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) {
+#pragma unroll
+        for (int q = 0; q < GW; ++q) ng[i][q] = 0u;
+#pragma unroll
+        for (int q = 0; q < HW; ++q) nh[i][q] = nr[i][q] = 0u;
+      }
+      if (row + stride < a.rows) load_row(row + stride, ng, nh, nr, nri);
+    } else {
+      load_row(row, wg, wh, wr, rinv);
+    }
     float dot = 0.f;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       const int v = lane + i * team;
-      float g[kVec], h[kVec], gam[kVec];
-      decode_vec<GDT, kVec>(wg[i], g);
-      decode_vec<HDT, kVec>(wh[i], h);
-      if (v < n_vec) load_gamma(a.gamma, a.gamma_dt, v, a.d - v * kVec, gam);
+      if (v < n_vec) {
+        float g[kVec], h[kVec], gam[kVec];
+        decode_vec<GDT, kVec>(wg[i], g);
+        decode_vec<HDT, kVec>(wh[i], h);
+        gamma_of(i, v, gam);
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        const float n = h[e] * rinv;
-        dg[i][e] = fmaf(g[e], n, dg[i][e]);
-        if (v < n_vec) dot = fmaf(g[e] * gam[e], n, dot);
+        for (int e = 0; e < kVec; ++e) {
+          const float n = h[e] * rinv;
+          dg[i][e] = fmaf(g[e], n, dg[i][e]);
+          dot = fmaf(g[e] * gam[e], n, dot);
+        }
       }
     }
     dot = team_sum<BLOCK>(dot, s_red) * inv_d;
@@ -311,16 +368,17 @@ __global__ void __launch_bounds__(BLOCK ? kBlockThreads : 32 * kWarpRows) add_rm
         float g[kVec], h[kVec], gam[kVec], r[kVec];
         decode_vec<GDT, kVec>(wg[i], g);
         decode_vec<HDT, kVec>(wh[i], h);
-        load_gamma(a.gamma, a.gamma_dt, v, n, gam);
-        if (rrow) decode_vec<HDT, kVec>(wr[i], r);
+        gamma_of(i, v, gam);
+        if (a.Gr) decode_vec<HDT, kVec>(wr[i], r);
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
           const float dh = rinv * fmaf(-h[e] * rinv, dot, g[e] * gam[e]);
-          g[e] = round_through<HDT>(rrow ? fmaf(r[e], fr, dh * fb) : dh);
-          if (e < n) {
-            amax = max(amax, abs_bits(g[e]));
-            if (a.stat == SCALIFY_STAT_L2) ssq += static_cast<double>(g[e]) * g[e];
-          }
+          g[e] = round_through<HDT>(a.Gr ? fmaf(r[e], fr, dh * fb) : dh);
+          amax = max(amax, abs_bits(g[e]));
+        }
+        if (a.stat == SCALIFY_STAT_L2) {
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) ssq += static_cast<double>(g[e]) * g[e];
         }
         store_vec<HDT>(static_cast<char*>(a.dX) + row * a.dx_ld * ElemBytes<HDT>::v, v, n, g);
         if (a.dXq) {
@@ -330,6 +388,16 @@ __global__ void __launch_bounds__(BLOCK ? kBlockThreads : 32 * kWarpRows) add_rm
           if (a.dxq_dt == SCALIFY_E4M3) store_vec<SCALIFY_E4M3>(qrow, v, n, g);
           else store_vec<SCALIFY_E5M2>(qrow, v, n, g);
         }
+      }
+    }
+    if constexpr (kPrefetch) {
+      rinv = nri;
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) {
+#pragma unroll
+        for (int q = 0; q < GW; ++q) wg[i][q] = ng[i][q];
+#pragma unroll
+        for (int q = 0; q < HW; ++q) { wh[i][q] = nh[i][q]; wr[i][q] = nr[i][q]; }
       }
     }
   }
@@ -347,20 +415,21 @@ __global__ void __launch_bounds__(BLOCK ? kBlockThreads : 32 * kWarpRows) add_rm
       }
     } else {
       const int ld = n_vec * kVec;
+      float* s_lines = s_dyn + ld;
 #pragma unroll
       for (int i = 0; i < VPT; ++i) {
         const int v = lane + i * team;
         if (v < n_vec) {
 #pragma unroll
           for (int e = 0; e < kVec; e += 4)
-            *reinterpret_cast<float4*>(s_dg + warp * ld + v * kVec + e) = make_float4(dg[i][e], dg[i][e + 1], dg[i][e + 2], dg[i][e + 3]);
+            *reinterpret_cast<float4*>(s_lines + warp * ld + v * kVec + e) = make_float4(dg[i][e], dg[i][e + 1], dg[i][e + 2], dg[i][e + 3]);
         }
       }
       __syncthreads();
       for (int c = threadIdx.x; c < ld; c += blockDim.x) {
         float t = 0.f;
 #pragma unroll
-        for (int k = 0; k < kWarpRows; ++k) t += s_dg[k * ld + c];
+        for (int k = 0; k < kWarpRows; ++k) t += s_lines[k * ld + c];
         line[c] = t;
       }
     }
@@ -378,25 +447,25 @@ __global__ void __launch_bounds__(BLOCK ? kBlockThreads : 32 * kWarpRows) add_rm
   }
 }
 
-// Adds the blocks' lines in block order: a block takes 32 columns, each of its 8 warps every eighth line; the last block
-// of the grid reduces the statistic instead.
+// Adds the blocks' lines in block order: a block takes 32 columns, each of its 32 warps every 32nd line (a handful of
+// loads, all in flight together); the last block of the grid reduces the statistic instead.
+constexpr int kFinishThreads = 1024;
 template <int ODT>
-__global__ void __launch_bounds__(256) add_rmsnorm_bwd_finish_kernel(const float* __restrict__ partial, int64_t ld, int lines,
-                                                                     int d, void* __restrict__ dgamma, float inv_kf,
-                                                                     const double* __restrict__ stat_partial, int stat,
-                                                                     double count, float* stat_word) {
+__global__ void __launch_bounds__(kFinishThreads) add_rmsnorm_bwd_finish_kernel(
+    const float* __restrict__ partial, int64_t ld, int lines, int d, void* __restrict__ dgamma, float inv_kf,
+    const double* __restrict__ stat_partial, int stat, double count, float* stat_word) {
   asm volatile("griddepcontrol.launch_dependents;");  // a programmatic dependent may set up while this grid runs
-  __shared__ double s[8][32];
+  __shared__ double s[32][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (stat != SCALIFY_STAT_NONE && blockIdx.x == gridDim.x - 1) {
     double t = 0.0;
-    for (int i = threadIdx.x; i < lines; i += 256) t = stat == SCALIFY_STAT_AMAX ? fmax(t, stat_partial[i]) : t + stat_partial[i];
+    for (int i = threadIdx.x; i < lines; i += kFinishThreads) t = stat == SCALIFY_STAT_AMAX ? fmax(t, stat_partial[i]) : t + stat_partial[i];
     t = stat == SCALIFY_STAT_AMAX ? static_cast<double>(warp_max_u32(static_cast<uint32_t>(t))) : warp_sum_f64(t);
     if (lane == 0) s[0][warp] = t;
     __syncthreads();
     if (threadIdx.x == 0) {
       t = 0.0;
-      for (int k = 0; k < 8; ++k) t = stat == SCALIFY_STAT_AMAX ? fmax(t, s[0][k]) : t + s[0][k];
+      for (int k = 0; k < 32; ++k) t = stat == SCALIFY_STAT_AMAX ? fmax(t, s[0][k]) : t + s[0][k];
       *stat_word = stat == SCALIFY_STAT_AMAX ? __uint_as_float(static_cast<uint32_t>(t)) : static_cast<float>(sqrt(t / count));
     }
     return;
@@ -404,31 +473,30 @@ __global__ void __launch_bounds__(256) add_rmsnorm_bwd_finish_kernel(const float
   const int col = blockIdx.x * 32 + lane;
   double t = 0.0;
   if (col < d) {
-    int i = warp;
-    for (; i + 24 < lines; i += 32) {  // four loads in flight
-      const float p0 = __ldcs(partial + static_cast<int64_t>(i) * ld + col), p1 = __ldcs(partial + static_cast<int64_t>(i + 8) * ld + col),
-                  p2 = __ldcs(partial + static_cast<int64_t>(i + 16) * ld + col), p3 = __ldcs(partial + static_cast<int64_t>(i + 24) * ld + col);
-      t += (static_cast<double>(p0) + p1) + (static_cast<double>(p2) + p3);
+    for (int i = warp; i < lines; i += 32 * 8) {
+      float p[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) p[u] = i + 32 * u < lines ? __ldcg(partial + static_cast<int64_t>(i + 32 * u) * ld + col) : 0.f;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) t += p[u];
     }
-    for (; i < lines; i += 8) t += __ldcs(partial + static_cast<int64_t>(i) * ld + col);
   }
   s[warp][lane] = t;
   __syncthreads();
-  if (warp == 0 && col < d) {
-    t = 0.0;
-    for (int k = 0; k < 8; ++k) t += s[k][lane];
-    store_elem<ODT>(dgamma, col, static_cast<float>(t) * inv_kf);
-  }
+  t = warp_sum_f64(s[lane][warp]);  // warp w adds up column w of the block's 32
+  if (lane == 0 && blockIdx.x * 32 + warp < d) store_elem<ODT>(dgamma, blockIdx.x * 32 + warp, static_cast<float>(t) * inv_kf);
 }
 
 // ------------------------------------------------------------------------------------------------- launches
-static int block_threads(int d) {
-  const int n_vec = (d + kVec - 1) / kVec, vpt = n_vec <= 2 * kBlockThreads ? 2 : 4;
+// backward: 2 vectors per thread while the row fits the threads of the prefetching form; forward: while it fits 512
+static int block_vpt(int d, bool bwd) { return (d + kVec - 1) / kVec <= 2 * (bwd ? kPrefetchThreads : kBlockThreads) ? 2 : 4; }
+static int block_threads(int d, bool bwd) {
+  const int n_vec = (d + kVec - 1) / kVec, vpt = block_vpt(d, bwd);
   return ((n_vec + vpt - 1) / vpt + 31) / 32 * 32;
 }
-static int bwd_grid_cap(int d) {  // resident blocks: about 16 warps per SM (the row state takes most registers)
-  if (d <= kWarpMaxD) return sm_count() * 4;
-  const int per_sm = 512 / block_threads(d);
+static int bwd_grid_cap(int d) {  // resident blocks, by the register budgets above
+  if (d <= kWarpMaxD) return sm_count() * kBwdWarpBlocks;
+  const int per_sm = kPrefetchThreads / block_threads(d, true);
   return sm_count() * (per_sm < 1 ? 1 : per_sm);
 }
 size_t rmsnorm_bwd_ws_bytes(int64_t rows, int64_t d) {
@@ -439,7 +507,7 @@ size_t rmsnorm_bwd_ws_bytes(int64_t rows, int64_t d) {
 
 #define SCALIFY_RMS_VPT(X, H, KERNEL, ...)                                  \
   do {                                                                      \
-    if (block && n_vec <= 2 * kBlockThreads) KERNEL<X, H, 2, true><<<grid, threads, smem, st>>>(__VA_ARGS__); \
+    if (block && vpt == 2) KERNEL<X, H, 2, true><<<grid, threads, smem, st>>>(__VA_ARGS__); \
     else if (block) KERNEL<X, H, 4, true><<<grid, threads, smem, st>>>(__VA_ARGS__);        \
     else if (n_vec <= 32) KERNEL<X, H, 1, false><<<grid, threads, smem, st>>>(__VA_ARGS__); \
     else if (n_vec <= 64) KERNEL<X, H, 2, false><<<grid, threads, smem, st>>>(__VA_ARGS__); \
@@ -460,7 +528,7 @@ int launch_add_rmsnorm(const RmsNormArgs& a, int x_dt, int h_dt, cudaStream_t st
   const bool block = a.d > kWarpMaxD;
   const int n_vec = (a.d + kVec - 1) / kVec;
   const int64_t rows = a.sf ? (a.rows + 255) / 256 * 256 : a.rows;
-  const int threads = block ? block_threads(a.d) : 32 * kWarpRows;
+  const int threads = block ? block_threads(a.d, false) : 32 * kWarpRows, vpt = block_vpt(a.d, false);
   const unsigned grid = static_cast<unsigned>(block ? rows : (rows + kWarpRows - 1) / kWarpRows);
   const size_t smem = 0;
   SCALIFY_RMS_TYPES(x_dt, h_dt, add_rmsnorm_kernel, a);
@@ -471,11 +539,11 @@ int launch_add_rmsnorm(const RmsNormArgs& a, int x_dt, int h_dt, cudaStream_t st
 int launch_add_rmsnorm_bwd(RmsNormBwdArgs a, int g_dt, int h_dt, void* dgamma, int dgamma_dt, void* ws, cudaStream_t st) {
   const bool block = a.d > kWarpMaxD;
   const int n_vec = (a.d + kVec - 1) / kVec;
-  const int threads = block ? block_threads(a.d) : 32 * kWarpRows;
+  const int threads = block ? block_threads(a.d, true) : 32 * kWarpRows, vpt = block_vpt(a.d, true);
   const int64_t want = block ? a.rows : (a.rows + kWarpRows - 1) / kWarpRows;
   const int cap = bwd_grid_cap(a.d);
   const unsigned grid = static_cast<unsigned>(want < cap ? want : cap);
-  const size_t smem = (!block && dgamma) ? static_cast<size_t>(kWarpRows) * n_vec * kVec * sizeof(float) : 0;
+  const size_t smem = block ? 0 : static_cast<size_t>(dgamma ? 1 + kWarpRows : 1) * n_vec * kVec * sizeof(float);
   a.partial = nullptr;
   a.stat_partial = nullptr;
   float* stat_word = nullptr;
@@ -492,7 +560,7 @@ int launch_add_rmsnorm_bwd(RmsNormBwdArgs a, int g_dt, int h_dt, void* dgamma, i
   if (!dgamma && a.stat == SCALIFY_STAT_NONE) return SCALIFY_OK;
   const unsigned blocks = (dgamma ? (a.d + 31) / 32 : 0) + (a.stat != SCALIFY_STAT_NONE ? 1 : 0);
   const double count = static_cast<double>(a.rows) * a.d;
-  SCALIFY_DISPATCH_WIDE(dgamma_dt, ODT, add_rmsnorm_bwd_finish_kernel<ODT><<<blocks, 256, 0, st>>>(
+  SCALIFY_DISPATCH_WIDE(dgamma_dt, ODT, add_rmsnorm_bwd_finish_kernel<ODT><<<blocks, kFinishThreads, 0, st>>>(
                                             a.partial, a.partial_ld, static_cast<int>(grid), dgamma ? a.d : 0, dgamma,
                                             1.0f / a.kf, a.stat_partial, a.stat, count, stat_word))
   SCALIFY_CUDA_TRY(cudaGetLastError());

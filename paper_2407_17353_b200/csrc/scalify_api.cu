@@ -159,6 +159,7 @@ size_t scalify_workspace_bytes(int op, int64_t d0, int64_t d1) {
     case SCALIFY_OP_CROSS_ENTROPY: n = cross_entropy_ws_bytes(d0); break;
     case SCALIFY_OP_COLSUM: n = colsum_ws_bytes(d1); break;
     case SCALIFY_OP_RMSNORM_BWD: n = rmsnorm_bwd_ws_bytes(d0, d1); break;
+    case SCALIFY_OP_EMBEDDING_GRAD: n = embedding_grad_ws_bytes(d0, d1); break;
     case SCALIFY_OP_MATMUL_SPLITK: n = matmul_splitk_ws_bytes(d0, d1); break;
     default: break;
   }
@@ -1213,6 +1214,77 @@ int scalify_scaled_embedding_bwd(const int64_t* ids, int64_t n, int64_t seq_len,
                               vocab, dY->data, dY->dtype, dY->scale, static_cast<float*>(dwte->data), dwte->scale,
                               dwpe ? static_cast<float*>(dwpe->data) : nullptr, dwpe ? dwpe->scale : nullptr,
                               static_cast<cudaStream_t>(stream));
+}
+
+// c as a power of two times a rest in [1, 2); false if c is not a positive normal number
+static bool split_constant(float c, float* pow2, float* rest) {
+  if (!(c >= 1.17549435e-38f) || isinf(c)) return false;
+  int ex;
+  const double m = frexp(static_cast<double>(c), &ex);
+  *pow2 = static_cast<float>(ldexp(1.0, ex - 1));
+  *rest = static_cast<float>(2.0 * m);
+  return true;
+}
+
+int scalify_scaled_embedding_lookup(const int64_t* ids, int64_t n, int64_t padding_id, const scalify_array* wte, float c,
+                                    scalify_array* Y, uint32_t* status, void* stream) {
+  int rc = check_array(wte);
+  if (!rc && !Y) rc = SCALIFY_ERR_NULL;
+  if (!rc && n != 0) rc = check_array(Y);  // (an empty batch may have no memory)
+  if (rc) return rc;
+  if (!ids && n > 0) return SCALIFY_ERR_NULL;
+  EmbeddingArgs a = {};
+  if (!split_constant(c, &a.c_pow2, &a.c_rest)) return SCALIFY_ERR_VALUE;
+  if (wte->ndim != 2 || Y->ndim != 2 || n < 0 || n > 0x7FFFFFFF) return SCALIFY_ERR_SHAPE;
+  const int64_t d = wte->shape[1];
+  if (d < 1 || d > 0x7FFFFFF0 || wte->shape[0] < 1 || Y->shape[0] != n || Y->shape[1] != d) return SCALIFY_ERR_SHAPE;
+  if (n == 0) return SCALIFY_OK;
+  if (!disjoint(wte, Y)) return SCALIFY_ERR_ALIAS;
+  if (Y->scale && Y->scale == wte->scale) return SCALIFY_ERR_ALIAS;
+  a.ids = reinterpret_cast<const long long*>(ids);
+  a.n = n; a.vocab = wte->shape[0]; a.padding_id = padding_id; a.d = static_cast<int>(d);
+  a.src = wte->data; a.src_ld = wte->stride[0]; a.src_scale = wte->scale;
+  a.out = Y->data; a.out_ld = Y->stride[0]; a.out_dt = Y->dtype; a.out_es = elem_size(Y->dtype); a.out_scale = Y->scale;
+  a.status = status;
+  return launch_embedding_lookup(a, wte->dtype, static_cast<cudaStream_t>(stream));
+}
+
+int scalify_scaled_embedding_grad(const int64_t* ids, int64_t n, int64_t padding_id, const scalify_array* dY, float c,
+                                  const scalify_array* addend, scalify_array* dwte, void* workspace,
+                                  size_t workspace_bytes, void* stream) {
+  int rc = check_array(dwte);
+  if (rc) return rc;
+  if (!ids && n > 0) return SCALIFY_ERR_NULL;
+  if (!is_wide(dwte->dtype)) return SCALIFY_ERR_DTYPE;
+  EmbeddingArgs a = {};
+  if (!split_constant(c, &a.c_pow2, &a.c_rest)) return SCALIFY_ERR_VALUE;
+  if (dwte->ndim != 2 || n < 0 || n > 0x7FFFFFFE) return SCALIFY_ERR_SHAPE;
+  const int64_t vocab = dwte->shape[0], d = dwte->shape[1];
+  if (d < 1 || d > 0x7FFFFFF0 || vocab < 1 || vocab > 0x7FFFFFFE) return SCALIFY_ERR_SHAPE;
+  if (!dY) return SCALIFY_ERR_NULL;
+  if (n > 0) {
+    rc = check_array(dY);
+    if (rc) return rc;
+  }
+  if (dY->ndim != 2 || dY->shape[0] != n || dY->shape[1] != d) return SCALIFY_ERR_SHAPE;
+  if (n > 0 && !disjoint(dwte, dY)) return SCALIFY_ERR_ALIAS;
+  if (addend) {
+    rc = check_array(addend);
+    if (rc) return rc;
+    if (addend->dtype != dwte->dtype) return SCALIFY_ERR_DTYPE;
+    if (!same_shape(addend, dwte)) return SCALIFY_ERR_SHAPE;
+    if (!disjoint_or_same(dwte, dwte->stride[0], addend, addend->stride[0])) return SCALIFY_ERR_ALIAS;
+  }
+  if (dwte->scale && (dwte->scale == dY->scale || (addend && dwte->scale == addend->scale))) return SCALIFY_ERR_ALIAS;
+  rc = check_ws(workspace, workspace_bytes, scalify_workspace_bytes(SCALIFY_OP_EMBEDDING_GRAD, n, d));
+  if (rc) return rc;
+  a.ids = reinterpret_cast<const long long*>(ids);
+  a.n = n; a.vocab = vocab; a.padding_id = padding_id; a.d = static_cast<int>(d);
+  a.src = dY->data; a.src_ld = dY->stride[0]; a.src_scale = dY->scale;
+  if (addend) { a.addend = addend->data; a.addend_ld = addend->stride[0]; a.addend_scale = addend->scale; }
+  a.out = dwte->data; a.out_ld = dwte->stride[0]; a.out_dt = dwte->dtype; a.out_es = elem_size(dwte->dtype);
+  a.out_scale = dwte->scale;
+  return launch_embedding_grad(a, dY->dtype, workspace, static_cast<cudaStream_t>(stream));
 }
 
 int scalify_scaled_softmax(const scalify_array* S, int causal, scalify_array* P, void* stream) {

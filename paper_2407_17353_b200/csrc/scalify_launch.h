@@ -193,6 +193,21 @@ struct RmsNormBwdArgs {
 };
 size_t rmsnorm_bwd_ws_bytes(int64_t rows, int64_t d);
 int launch_add_rmsnorm_bwd(RmsNormBwdArgs a, int g_dt, int h_dt, void* dgamma, int dgamma_dt, void* ws, cudaStream_t st);
+// Embedding lookup (src: the table [vocab, d], out: the rows [n, d]) and its gradient by sorted tokens (src: the rows'
+// gradient [n, d], out: the table's [vocab, d], addend: of out's dtype, or nullptr).  c_pow2 * c_rest is the factor.
+struct EmbeddingArgs {
+  const long long* ids; int64_t n, vocab; long long padding_id;
+  const void* src; int64_t src_ld; const float* src_scale;
+  const void* addend; int64_t addend_ld; const float* addend_scale;
+  void* out; int64_t out_ld; int out_dt, out_es; float* out_scale;
+  float c_pow2, c_rest;
+  int d;
+  uint32_t* status;
+};
+int launch_embedding_lookup(const EmbeddingArgs& a, int w_dt, cudaStream_t st);
+size_t embedding_grad_ws_bytes(int64_t n, int64_t d);
+int launch_embedding_grad(const EmbeddingArgs& a, int g_dt, void* ws, cudaStream_t st);
+
 int launch_mx_quantize_t(const void* X, int x_dt, int64_t rows, int64_t K, int64_t ldx, void* data, int elem_dt,
                          uint8_t* sf, const float* x_scale, float* y_scale, uint32_t* status, cudaStream_t st);
 int launch_mx_quantize(const void* X, int x_dt, int64_t rows, int64_t K, int64_t ldx, void* data, int elem_dt,

@@ -72,3 +72,33 @@ def add_rmsnorm_bwd(g, gs, gr, grs, h, hs, gamma, gammas, rinv):
     k = kf(rows)
     return {"dX": dx, "dX_s": ds, "mag": mag, "dgamma": (g * n).sum(0) / k, "dgamma_s": gs * k,
             "dgamma_mag": (g * n).abs().sum(0) / k}
+
+
+def embedding_lookup(ids, w, c, padding_id, vocab):
+    """Data of the looked-up rows (scale: the table's times p2(c)); padding and unknown tokens are rows of zeros."""
+    known = (ids >= 0) & (ids < vocab) & (ids != padding_id)
+    return w.double()[ids.clamp(0, vocab - 1)] * known[:, None] * (c / p2(c))
+
+
+def embedding_grad(ids, g, gs, vocab, c, padding_id, addend=None, addend_s=0.0):
+    """(data, scale, magnitude of the terms of the sums, largest number of terms of a row)."""
+    known = (ids >= 0) & (ids < vocab) & (ids != padding_id)
+    out = torch.zeros(vocab, g.shape[1], dtype=torch.float64, device=g.device)
+    mag = torch.zeros_like(out)
+    count = torch.zeros(vocab, dtype=torch.int64, device=g.device)
+    for i in range(ids.numel()) if ids.numel() < 4096 else ():
+        if bool(known[i]):
+            out[ids[i]] += g[i].double()
+            mag[ids[i]] += g[i].double().abs()
+    if ids.numel() >= 4096:
+        out.index_put_((ids[known],), g[known].double(), accumulate=True)
+        mag.index_put_((ids[known],), g[known].double().abs(), accumulate=True)
+    count.index_put_((ids[known],), torch.ones_like(ids[known]), accumulate=True)
+    scale, f = gs * p2(c), c / p2(c)
+    out, mag = out * f, mag * f
+    if addend is not None:
+        s = max(scale, addend_s)
+        out = out * (scale / s) + addend.double() * (addend_s / s)
+        mag = mag * (scale / s) + addend.double().abs() * (addend_s / s)
+        scale = s
+    return out, scale, mag, int(count.max()) if count.numel() else 0

@@ -139,3 +139,58 @@ def test_plain_norm_gradient_against_differences():
         e[j] = step
         diff = (loss(x, gam + e) - loss(x, gam - e)) / (2 * step)
         assert abs(diff - float(dg[j])) < 1e-6 * max(1.0, abs(diff))
+
+
+def test_embedding_refusals():
+    B, F, Q = sc.BF16, sc.F32, sc.E4M3
+    L = sc.lib()
+    w, y, ids = arr(1, B, (50, 64)), arr(2, B, (7, 64)), 8 * MB
+
+    def look(ids=ids, n=7, w=w, c=1.0, y=y):
+        return L.scalify_scaled_embedding_lookup(ids, n, -1, None if w is None else R(w), c, None if y is None else R(y), None, None)
+    assert look(ids=None) == NULL and look(w=None) == NULL and look(y=None) == NULL
+    assert look(n=6) == SHAPE and look(n=-1) == SHAPE and look(y=arr(2, B, (7, 56))) == SHAPE
+    assert look(w=arr(1, B, (64,))) == SHAPE and look(w=arr(1, B, (0, 64))) == SHAPE
+    for c in (0.0, -1.0, float("nan"), float("inf"), 1e-45):
+        assert look(c=c) == VALUE
+    assert look(y=arr(1, B, (7, 64), offset=64)) == ALIAS
+    assert look(w=arr(1, B, (50, 64), scale=64), y=arr(2, B, (7, 64), scale=64)) == ALIAS
+    assert look(w=arr(1, B, (50, 60))) == ALIGN
+
+    g, dw = arr(2, B, (7, 64)), arr(1, F, (50, 64))
+    big = 64 * MB
+
+    def grad(ids=ids, n=7, g=g, c=1.0, a=None, dw=dw, ws=16 * MB, nb=big):
+        p = lambda t: None if t is None else R(t)  # noqa: E731
+        return L.scalify_scaled_embedding_grad(ids, n, -1, p(g), c, p(a), p(dw), ws, nb, None)
+    assert grad(ids=None) == NULL and grad(g=None) == NULL and grad(dw=None) == NULL
+    assert grad(dw=arr(1, Q, (50, 64))) == DTYPE
+    assert grad(g=arr(2, B, (6, 64))) == SHAPE and grad(g=arr(2, B, (7, 56))) == SHAPE and grad(n=-1) == SHAPE
+    assert grad(a=arr(3, B, (50, 64))) == DTYPE and grad(a=arr(3, F, (49, 64))) == SHAPE
+    assert grad(a=arr(1, F, (50, 64), offset=256)) == ALIAS and grad(g=arr(1, B, (7, 64), offset=256)) == ALIAS
+    assert grad(dw=arr(1, F, (50, 64), scale=64), g=arr(2, B, (7, 64), scale=64)) == ALIAS
+    assert grad(c=0.0) == VALUE
+    assert grad(ws=None) == WORKSPACE and grad(nb=4095) == WORKSPACE and grad(ws=16 * MB + 16) == WORKSPACE
+    assert sc.scalify_workspace_bytes(sc.OP_EMBEDDING_GRAD, 1 << 20, 64) > (1 << 24)
+
+
+def test_token_ids_are_checked_by_the_binding():
+    w, y = sc.ScaledTensor(torch.zeros(4, 64)), sc.ScaledTensor(torch.zeros(2, 64))
+    for ids in (torch.zeros(2, dtype=torch.int32), torch.zeros(4, dtype=torch.int64)[::2]):
+        with pytest.raises(ValueError):
+            sc.scalify_scaled_embedding_lookup(ids, w, y)
+
+
+def test_plain_embedding_gradient_against_differences():
+    torch.manual_seed(1)
+    ids = torch.tensor([2, 0, 2, -1, 4, 2])
+    w, up = torch.randn(5, 3, dtype=torch.float64), torch.randn(6, 3, dtype=torch.float64)
+    c = 3.3
+    got, scale, _, count = p64.embedding_grad(ids, up, 1.0, 5, c, -1)
+    f = lambda w: float((p64.embedding_lookup(ids, w, c, -1, 5) * p64.p2(c) * up).sum())  # noqa: E731
+    for i in range(5):
+        for j in range(3):
+            e = torch.zeros_like(w)
+            e[i, j] = 1e-6
+            assert abs((f(w + e) - f(w - e)) / 2e-6 - float(got[i, j]) * scale) < 1e-6
+    assert count == 3
