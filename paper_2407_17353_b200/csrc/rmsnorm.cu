@@ -11,48 +11,24 @@
 // gradient of H itself (residual path):  dX_s = max(G_s gamma_s / H_s, Gr_s);  dgamma = sum_rows G_d n / kf(R).
 //
 // Both directions are bound by HBM: every array is read or written once.  A row lives in the registers of a team: one
-// warp for d <= 1024 (1 to 4 vectors of 8 elements per lane, several rows per block, no barrier), otherwise one block of
-// up to 512 threads with 2 vectors per thread (4 above d = 8192) and two barriers per row.
+// warp for d <= 1024 (gradient: 768; 1 to 4 vectors of 8 elements per lane, several rows per block, no barrier), otherwise
+// one block with 2 vectors per thread (4 above d = 8192; gradient: 6144) and two barriers per row.
 #include "scalify_common.cuh"
 #include "scalify_launch.h"
+#include "vec8.cuh"
 
 namespace scalify {
 
 namespace {
 
-constexpr int kVec = 8;          // elements per vector: 16 bytes of a 16-bit format
-constexpr int kWarpRows = 4;     // rows (warps) per block of the warp-per-row forms
-constexpr int kWarpMaxD = 1024;  // longest row one warp holds
+constexpr int kWarpRows = 4;     // rows (warps) per block of the warp-per-row forms: forward ...
+constexpr int kBwdRows = 8;      // ... and backward (a line of column sums per block)
+constexpr int kWarpMaxD = 1024;  // longest row one warp holds: forward ...
+constexpr int kBwdWarpMaxD = 768;  // ... and backward
 constexpr int kPrefetchThreads = 384;  // of the backward form that loads the next row ahead (168 registers a thread)
-constexpr int kBwdWarpBlocks = 4;      // resident blocks per SM of the backward warp-per-row form
+constexpr int kBwdWarpBlocks = 2;      // resident blocks per SM of the backward warp-per-row form
 constexpr int kBlockThreads = 512;  // most threads of the block-per-row forms (leaves 128 registers a thread)
 
-// Raw words of vector v of a row (n = elements of it inside the row; the rest read as zero).
-template <int DT>
-__device__ __forceinline__ void load_vec(const char* row, int v, int n, uint32_t* w) {
-  constexpr int ES = ElemBytes<DT>::v;
-  if (n >= kVec) {
-    ld_raw_stream<kVec * ES>(row + static_cast<int64_t>(v) * (kVec * ES), w);
-  } else {
-    float f[kVec];
-#pragma unroll
-    for (int e = 0; e < kVec; ++e) f[e] = e < n ? load_elem<DT>(row, static_cast<int64_t>(v) * kVec + e) : 0.f;
-    encode_vec<DT, kVec>(f, w);
-  }
-}
-template <int DT>
-__device__ __forceinline__ void store_vec(char* row, int v, int n, const float* f) {
-  constexpr int ES = ElemBytes<DT>::v;
-  if (n >= kVec) {
-    uint32_t w[kVec * ES / 4];
-    encode_vec<DT, kVec>(f, w);
-    st_raw<kVec * ES>(row + static_cast<int64_t>(v) * (kVec * ES), w);
-  } else {
-#pragma unroll
-    for (int e = 0; e < kVec; ++e)
-      if (e < n) store_elem<DT>(row, static_cast<int64_t>(v) * kVec + e, f[e]);
-  }
-}
 // one uniform branch per vector on the output's type: a template per type would multiply the kernels by five
 __device__ __forceinline__ void store_vec_dt(int dt, char* row, int v, int n, const float* f) {
   SCALIFY_DISPATCH_DTYPE(dt, DT, store_vec<DT>(row, v, n, f))
@@ -67,7 +43,7 @@ __device__ __forceinline__ void load_gamma(const void* gamma, int dt, int v, int
   SCALIFY_DISPATCH_WIDE(dt, DT, {
     uint32_t w[kVec * ElemBytes<DT>::v / 4];
     if (n >= kVec) {
-      ld_raw<kVec * ElemBytes<DT>::v>(p + static_cast<int64_t>(v) * (kVec * ElemBytes<DT>::v), w);
+      ld_bytes<kVec * ElemBytes<DT>::v, false>(p + static_cast<int64_t>(v) * (kVec * ElemBytes<DT>::v), w);
       decode_vec<DT, kVec>(w, f);
     } else {
 #pragma unroll
@@ -89,6 +65,23 @@ __device__ __forceinline__ float team_sum(float x, float* s_red) {
     x = warp_sum_f32(x);
   }
   return x;
+}
+
+// max of `m` and the magnitudes of one vector's words, as DT bit patterns (16-bit formats two at a time, in both halves)
+template <int DT>
+__device__ __forceinline__ uint32_t max_bits(const uint32_t* w, uint32_t m) {
+#pragma unroll
+  for (int q = 0; q < kVec * ElemBytes<DT>::v / 4; ++q)
+    m = ElemBytes<DT>::v == 2 ? __vmaxu2(m, w[q] & 0x7FFF7FFFu) : max(m, w[q] & 0x7FFFFFFFu);
+  return m;
+}
+// ... and as the fp32 bit pattern of the value
+template <int DT>
+__device__ __forceinline__ uint32_t max_bits_to_f32(uint32_t m) {
+  if constexpr (DT == SCALIFY_F32) return m;
+  const uint32_t h = max(m & 0xFFFFu, m >> 16);
+  if constexpr (DT == SCALIFY_BF16) return h << 16;
+  return __float_as_uint(__half2float(__ushort_as_half(static_cast<unsigned short>(h))));
 }
 
 }  // namespace
@@ -126,8 +119,8 @@ __global__ void __launch_bounds__(BLOCK ? kBlockThreads : 32 * kWarpRows) add_rm
       for (int i = 0; i < VPT; ++i) {
         const int v = lane + i * team;
         if (v < n_vec) {
-          load_vec<XDT>(xrow, v, a.d - v * kVec, wx[i]);
-          load_vec<HDT>(rrow, v, a.d - v * kVec, wr[i]);
+          load_vec<XDT, true>(xrow, v, a.d - v * kVec, wx[i]);
+          load_vec<HDT, true>(rrow, v, a.d - v * kVec, wr[i]);
         }
       }
 #pragma unroll
@@ -152,7 +145,7 @@ __global__ void __launch_bounds__(BLOCK ? kBlockThreads : 32 * kWarpRows) add_rm
 #pragma unroll
       for (int i = 0; i < VPT; ++i) {
         const int v = lane + i * team;
-        if (v < n_vec) load_vec<HDT>(xrow, v, a.d - v * kVec, wr[i]);
+        if (v < n_vec) load_vec<HDT, true>(xrow, v, a.d - v * kVec, wr[i]);
       }
 #pragma unroll
       for (int i = 0; i < VPT; ++i) {
@@ -229,23 +222,24 @@ __global__ void __launch_bounds__(BLOCK ? kBlockThreads : 32 * kWarpRows) add_rm
 // Persistent teams walk the rows (grid stride); a team keeps its columns' share of dgamma in registers over all its
 // rows and leaves it in the workspace, one line per block, added in block order by the second launch: the result does
 // not depend on scheduling.  The statistic of the stored dX travels the same way.
-// The launch bounds leave 128 registers a thread to the warp-per-row form (four blocks of four warps per SM, which is
+// The launch bounds leave 128 registers a thread to the warp-per-row form (two blocks of eight warps per SM, which is
 // what covers the load latency there).  The block-per-row form with 2 vectors per thread holds the NEXT row's words in
 // registers while it works on the current one, so that the two barriers of a row do not leave the memory idle; the form
 // for very long rows has no registers left for that.
 template <int GDT, int HDT, int VPT, bool BLOCK>
-__global__ void __launch_bounds__(BLOCK ? (VPT == 2 ? kPrefetchThreads : kBlockThreads) : 32 * kWarpRows,
+__global__ void __launch_bounds__(BLOCK ? (VPT == 2 ? kPrefetchThreads : kBlockThreads) : 32 * kBwdRows,
                                   BLOCK ? 1 : kBwdWarpBlocks) add_rmsnorm_bwd_kernel(const RmsNormBwdArgs a) {
   asm volatile("griddepcontrol.launch_dependents;");  // a programmatic dependent may set up while this grid runs
-  extern __shared__ float s_dyn[];  // warp-per-row form: gamma [d], then [kWarpRows][d] to add up the block's warps
+  extern __shared__ float s_dyn[];  // warp-per-row form: gamma [d], then [kBwdRows][d] to add up the block's warps
   __shared__ float s_red[32];
   __shared__ double s_stat[32];
   constexpr bool kPrefetch = BLOCK && VPT == 2;
+  constexpr bool kLean = BLOCK && VPT == 4;  // very long rows: gamma and Gr are read where they are needed
   const int team = BLOCK ? blockDim.x : 32;
   const int lane = BLOCK ? threadIdx.x : threadIdx.x & 31;
   const int warp = threadIdx.x >> 5;
-  const int64_t first = BLOCK ? blockIdx.x : static_cast<int64_t>(blockIdx.x) * kWarpRows + warp;
-  const int64_t stride = BLOCK ? gridDim.x : static_cast<int64_t>(gridDim.x) * kWarpRows;
+  const int64_t first = BLOCK ? blockIdx.x : static_cast<int64_t>(blockIdx.x) * kBwdRows + warp;
+  const int64_t stride = BLOCK ? gridDim.x : static_cast<int64_t>(gridDim.x) * kBwdRows;
   const float g_s = load_scale(a.g_scale), h_s = load_scale(a.h_scale), gam_s = a.gamma ? load_scale(a.gamma_scale) : 1.0f;
   const float branch_s = g_s * gam_s / h_s, res_s = a.Gr ? load_scale(a.gr_scale) : 0.f;
   const float dx_s = fmaxf(branch_s, res_s);
@@ -269,13 +263,14 @@ __global__ void __launch_bounds__(BLOCK ? (VPT == 2 ? kPrefetchThreads : kBlockT
   constexpr int GW = kVec * ElemBytes<GDT>::v / 4, HW = kVec * ElemBytes<HDT>::v / 4;
   const float inv_d = 1.0f / static_cast<float>(a.d);
   float dg[VPT][kVec];
-  float gam_reg[BLOCK ? VPT : 1][kVec];  // a thread meets the same columns in every row
+  float gam_reg[BLOCK && !kLean ? VPT : 1][kVec];  // a thread meets the same columns in every row
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
     const int v = lane + i * team;
 #pragma unroll
     for (int e = 0; e < kVec; ++e) dg[i][e] = 0.f;
-    if constexpr (BLOCK) {
+    if constexpr (kLean) {
+    } else if constexpr (BLOCK) {
 #pragma unroll
       for (int e = 0; e < kVec; ++e) gam_reg[i][e] = 0.f;
       if (v < n_vec) load_gamma(a.gamma, a.gamma_dt, v, a.d - v * kVec, gam_reg[i]);
@@ -288,7 +283,9 @@ __global__ void __launch_bounds__(BLOCK ? (VPT == 2 ? kPrefetchThreads : kBlockT
   }
   if constexpr (!BLOCK) __syncthreads();
   auto gamma_of = [&](int i, int v, float* gam) {
-    if constexpr (BLOCK) {
+    if constexpr (kLean) {
+      load_gamma(a.gamma, a.gamma_dt, v, a.d - v * kVec, gam);
+    } else if constexpr (BLOCK) {
 #pragma unroll
       for (int e = 0; e < kVec; ++e) gam[e] = gam_reg[i][e];
     } else {
@@ -313,9 +310,9 @@ __global__ void __launch_bounds__(BLOCK ? (VPT == 2 ? kPrefetchThreads : kBlockT
     for (int i = 0; i < VPT; ++i) {
       const int v = lane + i * team;
       if (v < n_vec) {
-        load_vec<GDT>(grow, v, a.d - v * kVec, xg[i]);
-        load_vec<HDT>(hrow, v, a.d - v * kVec, xh[i]);
-        if (rrow) load_vec<HDT>(rrow, v, a.d - v * kVec, xr[i]);
+        load_vec<GDT, true>(grow, v, a.d - v * kVec, xg[i]);
+        load_vec<HDT, true>(hrow, v, a.d - v * kVec, xh[i]);
+        if (rrow && !kLean) load_vec<HDT, true>(rrow, v, a.d - v * kVec, xr[i]);
       }
     }
   };
@@ -342,51 +339,77 @@ __global__ void __launch_bounds__(BLOCK ? (VPT == 2 ? kPrefetchThreads : kBlockT
     } else {
       load_row(row, wg, wh, wr, rinv);
     }
-    float dot = 0.f;
+    // Two elements per instruction (two-wide fp32): the kernel is otherwise bound by instruction issue, not by HBM.
+    // dot = sum g gamma h;   dX = (G_s gamma_s/H_s/dX_s rinv) g gamma - (.. rinv^2 dot/d rinv) h + Gr (Gr_s/dX_s)
+    float2 dot2 = make_float2(0.f, 0.f);
+    const float2 rinv2 = make_float2(rinv, rinv);
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       const int v = lane + i * team;
       if (v < n_vec) {
-        float g[kVec], h[kVec], gam[kVec];
+        float g[kVec], h[kVec];
         decode_vec<GDT, kVec>(wg[i], g);
         decode_vec<HDT, kVec>(wh[i], h);
+        float gam[kVec];
         gamma_of(i, v, gam);
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) {
-          const float n = h[e] * rinv;
-          dg[i][e] = fmaf(g[e], n, dg[i][e]);
-          dot = fmaf(g[e] * gam[e], n, dot);
+        for (int e = 0; e < kVec; e += 2) {
+          const float2 g2 = make_float2(g[e], g[e + 1]), h2 = make_float2(h[e], h[e + 1]);
+          const float2 d2 = __ffma2_rn(g2, __fmul2_rn(h2, rinv2), make_float2(dg[i][e], dg[i][e + 1]));
+          dg[i][e] = d2.x;
+          dg[i][e + 1] = d2.y;
+          const float2 t2 = __fmul2_rn(g2, make_float2(gam[e], gam[e + 1]));
+          dot2 = __ffma2_rn(t2, h2, dot2);
         }
       }
     }
-    dot = team_sum<BLOCK>(dot, s_red) * inv_d;
+    const float dot = team_sum<BLOCK>(dot2.x + dot2.y, s_red) * inv_d;  // mean of g gamma h
+    const float cg = rinv * fb, ch = -cg * rinv * (rinv * dot);
+    const float2 cg2 = make_float2(cg, cg), ch2 = make_float2(ch, ch), fr2 = make_float2(fr, fr), iq2 = make_float2(inv_rq, inv_rq);
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       const int v = lane + i * team;
       if (v < n_vec) {
         const int n = a.d - v * kVec;
-        float g[kVec], h[kVec], gam[kVec], r[kVec];
+        float g[kVec], h[kVec], gam[kVec], x[kVec];
         decode_vec<GDT, kVec>(wg[i], g);
         decode_vec<HDT, kVec>(wh[i], h);
         gamma_of(i, v, gam);
-        if (a.Gr) decode_vec<HDT, kVec>(wr[i], r);
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) {
-          const float dh = rinv * fmaf(-h[e] * rinv, dot, g[e] * gam[e]);
-          g[e] = round_through<HDT>(a.Gr ? fmaf(r[e], fr, dh * fb) : dh);
-          amax = max(amax, abs_bits(g[e]));
+        if (a.Gr) {
+          if constexpr (kLean) load_vec<HDT, true>(static_cast<const char*>(a.Gr) + row * a.gr_ld * ElemBytes<HDT>::v, v, n, wr[0]);
+          decode_vec<HDT, kVec>(wr[kLean ? 0 : i], x);
         }
-        if (a.stat == SCALIFY_STAT_L2) {
 #pragma unroll
-          for (int e = 0; e < kVec; ++e) ssq += static_cast<double>(g[e]) * g[e];
+        for (int e = 0; e < kVec; e += 2) {
+          float2 x2 = a.Gr ? __fmul2_rn(make_float2(x[e], x[e + 1]), fr2) : make_float2(0.f, 0.f);
+          x2 = __ffma2_rn(make_float2(h[e], h[e + 1]), ch2, x2);
+          x2 = __ffma2_rn(__fmul2_rn(make_float2(g[e], g[e + 1]), make_float2(gam[e], gam[e + 1])), cg2, x2);
+          x[e] = x2.x;
+          x[e + 1] = x2.y;
         }
-        store_vec<HDT>(static_cast<char*>(a.dX) + row * a.dx_ld * ElemBytes<HDT>::v, v, n, g);
-        if (a.dXq) {
+        uint32_t ow[HW];
+        encode_vec<HDT, kVec>(x, ow);
+        char* xrow = static_cast<char*>(a.dX) + row * a.dx_ld * ElemBytes<HDT>::v;
+        if (n >= kVec) st_bytes<kVec * ElemBytes<HDT>::v>(xrow + static_cast<int64_t>(v) * (kVec * ElemBytes<HDT>::v), ow);
+        else store_vec<HDT>(xrow, v, n, x);
+        if (a.stat == SCALIFY_STAT_AMAX) amax = max_bits<HDT>(ow, amax);
+        if (a.dXq || a.stat == SCALIFY_STAT_L2) {
+          decode_vec<HDT, kVec>(ow, x);  // the stored values
+          if (a.stat == SCALIFY_STAT_L2) {
 #pragma unroll
-          for (int e = 0; e < kVec; ++e) g[e] *= inv_rq;
-          char* qrow = static_cast<char*>(a.dXq) + row * a.dxq_ld;
-          if (a.dxq_dt == SCALIFY_E4M3) store_vec<SCALIFY_E4M3>(qrow, v, n, g);
-          else store_vec<SCALIFY_E5M2>(qrow, v, n, g);
+            for (int e = 0; e < kVec; ++e) ssq += static_cast<double>(x[e]) * x[e];
+          }
+          if (a.dXq) {
+#pragma unroll
+            for (int e = 0; e < kVec; e += 2) {
+              const float2 x2 = __fmul2_rn(make_float2(x[e], x[e + 1]), iq2);
+              x[e] = x2.x;
+              x[e + 1] = x2.y;
+            }
+            char* qrow = static_cast<char*>(a.dXq) + row * a.dxq_ld;
+            if (a.dxq_dt == SCALIFY_E4M3) store_vec<SCALIFY_E4M3>(qrow, v, n, x);
+            else store_vec<SCALIFY_E5M2>(qrow, v, n, x);
+          }
         }
       }
     }
@@ -429,13 +452,13 @@ __global__ void __launch_bounds__(BLOCK ? (VPT == 2 ? kPrefetchThreads : kBlockT
       for (int c = threadIdx.x; c < ld; c += blockDim.x) {
         float t = 0.f;
 #pragma unroll
-        for (int k = 0; k < kWarpRows; ++k) t += s_lines[k * ld + c];
+        for (int k = 0; k < kBwdRows; ++k) t += s_lines[k * ld + c];
         line[c] = t;
       }
     }
   }
   if (a.stat != SCALIFY_STAT_NONE) {
-    const double mine = a.stat == SCALIFY_STAT_AMAX ? static_cast<double>(warp_max_u32(amax)) : warp_sum_f64(ssq);
+    const double mine = a.stat == SCALIFY_STAT_AMAX ? static_cast<double>(warp_max_u32(max_bits_to_f32<HDT>(amax))) : warp_sum_f64(ssq);
     __syncthreads();
     if ((threadIdx.x & 31) == 0) s_stat[warp] = mine;
     __syncthreads();
@@ -473,12 +496,12 @@ __global__ void __launch_bounds__(kFinishThreads) add_rmsnorm_bwd_finish_kernel(
   const int col = blockIdx.x * 32 + lane;
   double t = 0.0;
   if (col < d) {
-    for (int i = warp; i < lines; i += 32 * 8) {
-      float p[8];
+    for (int i = warp; i < lines; i += 32 * 10) {
+      float p[10];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) p[u] = i + 32 * u < lines ? __ldcg(partial + static_cast<int64_t>(i + 32 * u) * ld + col) : 0.f;
+      for (int u = 0; u < 10; ++u) p[u] = i + 32 * u < lines ? __ldcg(partial + static_cast<int64_t>(i + 32 * u) * ld + col) : 0.f;
 #pragma unroll
-      for (int u = 0; u < 8; ++u) t += p[u];
+      for (int u = 0; u < 10; ++u) t += p[u];
     }
   }
   s[warp][lane] = t;
@@ -495,7 +518,7 @@ static int block_threads(int d, bool bwd) {
   return ((n_vec + vpt - 1) / vpt + 31) / 32 * 32;
 }
 static int bwd_grid_cap(int d) {  // resident blocks, by the register budgets above
-  if (d <= kWarpMaxD) return sm_count() * kBwdWarpBlocks;
+  if (d <= kBwdWarpMaxD) return sm_count() * kBwdWarpBlocks;
   const int per_sm = kPrefetchThreads / block_threads(d, true);
   return sm_count() * (per_sm < 1 ? 1 : per_sm);
 }
@@ -512,7 +535,7 @@ size_t rmsnorm_bwd_ws_bytes(int64_t rows, int64_t d) {
     else if (n_vec <= 32) KERNEL<X, H, 1, false><<<grid, threads, smem, st>>>(__VA_ARGS__); \
     else if (n_vec <= 64) KERNEL<X, H, 2, false><<<grid, threads, smem, st>>>(__VA_ARGS__); \
     else if (n_vec <= 96) KERNEL<X, H, 3, false><<<grid, threads, smem, st>>>(__VA_ARGS__); \
-    else KERNEL<X, H, 4, false><<<grid, threads, smem, st>>>(__VA_ARGS__);  \
+    else KERNEL<X, H, kMaxWarpVpt, false><<<grid, threads, smem, st>>>(__VA_ARGS__);        \
   } while (0)
 #define SCALIFY_RMS_TYPES(xdt, hdt, KERNEL, ...)                                                                 \
   do {                                                                                                           \
@@ -531,19 +554,20 @@ int launch_add_rmsnorm(const RmsNormArgs& a, int x_dt, int h_dt, cudaStream_t st
   const int threads = block ? block_threads(a.d, false) : 32 * kWarpRows, vpt = block_vpt(a.d, false);
   const unsigned grid = static_cast<unsigned>(block ? rows : (rows + kWarpRows - 1) / kWarpRows);
   const size_t smem = 0;
+  constexpr int kMaxWarpVpt = 4;
   SCALIFY_RMS_TYPES(x_dt, h_dt, add_rmsnorm_kernel, a);
   SCALIFY_CUDA_TRY(cudaGetLastError());
   return SCALIFY_OK;
 }
 
 int launch_add_rmsnorm_bwd(RmsNormBwdArgs a, int g_dt, int h_dt, void* dgamma, int dgamma_dt, void* ws, cudaStream_t st) {
-  const bool block = a.d > kWarpMaxD;
+  const bool block = a.d > kBwdWarpMaxD;
   const int n_vec = (a.d + kVec - 1) / kVec;
-  const int threads = block ? block_threads(a.d, true) : 32 * kWarpRows, vpt = block_vpt(a.d, true);
-  const int64_t want = block ? a.rows : (a.rows + kWarpRows - 1) / kWarpRows;
+  const int threads = block ? block_threads(a.d, true) : 32 * kBwdRows, vpt = block_vpt(a.d, true);
+  const int64_t want = block ? a.rows : (a.rows + kBwdRows - 1) / kBwdRows;
   const int cap = bwd_grid_cap(a.d);
   const unsigned grid = static_cast<unsigned>(want < cap ? want : cap);
-  const size_t smem = block ? 0 : static_cast<size_t>(dgamma ? 1 + kWarpRows : 1) * n_vec * kVec * sizeof(float);
+  const size_t smem = block ? 0 : static_cast<size_t>(dgamma ? 1 + kBwdRows : 1) * n_vec * kVec * sizeof(float);
   a.partial = nullptr;
   a.stat_partial = nullptr;
   float* stat_word = nullptr;
@@ -555,6 +579,7 @@ int launch_add_rmsnorm_bwd(RmsNormBwdArgs a, int g_dt, int h_dt, void* dgamma, i
     if (dgamma) a.partial = static_cast<float*>(v.area);
     a.stat_partial = reinterpret_cast<double*>(static_cast<float*>(v.area) + static_cast<int64_t>(cap) * a.partial_ld);
   }
+  constexpr int kMaxWarpVpt = kBwdWarpMaxD / (32 * kVec);
   SCALIFY_RMS_TYPES(g_dt, h_dt, add_rmsnorm_bwd_kernel, a);
   SCALIFY_CUDA_TRY(cudaGetLastError());
   if (!dgamma && a.stat == SCALIFY_STAT_NONE) return SCALIFY_OK;

@@ -1260,7 +1260,7 @@ int scalify_scaled_embedding_grad(const int64_t* ids, int64_t n, int64_t padding
   if (!split_constant(c, &a.c_pow2, &a.c_rest)) return SCALIFY_ERR_VALUE;
   if (dwte->ndim != 2 || n < 0 || n > 0x7FFFFFFE) return SCALIFY_ERR_SHAPE;
   const int64_t vocab = dwte->shape[0], d = dwte->shape[1];
-  if (d < 1 || d > 0x7FFFFFF0 || vocab < 1 || vocab > 0x7FFFFFFE) return SCALIFY_ERR_SHAPE;
+  if (d < 1 || d > 0x7FFFFFF0 || vocab < 1 || vocab > kEmbeddingMaxVocab) return SCALIFY_ERR_SHAPE;
   if (!dY) return SCALIFY_ERR_NULL;
   if (n > 0) {
     rc = check_array(dY);

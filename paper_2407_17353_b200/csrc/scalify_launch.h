@@ -195,6 +195,7 @@ size_t rmsnorm_bwd_ws_bytes(int64_t rows, int64_t d);
 int launch_add_rmsnorm_bwd(RmsNormBwdArgs a, int g_dt, int h_dt, void* dgamma, int dgamma_dt, void* ws, cudaStream_t st);
 // Embedding lookup (src: the table [vocab, d], out: the rows [n, d]) and its gradient by sorted tokens (src: the rows'
 // gradient [n, d], out: the table's [vocab, d], addend: of out's dtype, or nullptr).  c_pow2 * c_rest is the factor.
+constexpr int64_t kEmbeddingMaxVocab = int64_t(1) << 24;  // of the gradient: a bit each in the workspace
 struct EmbeddingArgs {
   const long long* ids; int64_t n, vocab; long long padding_id;
   const void* src; int64_t src_ld; const float* src_scale;
