@@ -601,6 +601,50 @@ int scalify_scaled_adam_step_cast(int n_tensors, const scalify_array* grads, sca
                                   float eps, int64_t step, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Orthogonalisation of matrices by Newton-Schulz products (the update of the Muon optimiser; no counterpart in the
+ * paper, whose optimiser is Adam).  Per matrix U [rows, cols] (its data component: the result does not depend on scale):
+ *   Z = U / (|U|_F + eps);   `steps` times:  A = Z Z^T,  Z = a Z + (b A + c A^2) Z    (on the shorter side, so that A is
+ *   min(rows, cols) square);   O = Z
+ * With (a, b, c) = (3.4445, -4.7750, 2.0315), used when coef is NULL, five steps bring the singular values to about
+ * 1 +- 0.3, which is what the optimiser wants.  coef: HOST array of three floats.
+ * The products run on the tensor cores with FP16 operands at a power-of-two scale and fp32 accumulation; the iterates
+ * are held in FP16 (11 bits), which the products square and multiply: O agrees with the definition to about 1e-3 of its
+ * norm.  O is therefore a 16-bit array.
+ *   X: [rows, cols] or [batch, rows, cols], any dtype; rows may be strided.  O: the same shape, F16 or BF16.
+ *   O_s = 1 / kf(max(rows, cols)) (a matrix with singular values 1 has entries of about 1/sqrt(longer side)).
+ *   A matrix of zeros gives zeros; one with an infinity or NaN gives NaN.  1 <= rows, cols <= 32768; 1 <= steps <= 16.
+ * Errors: NULL, DTYPE, SHAPE, ALIGNMENT, VALUE (eps < 0, a non-finite coefficient, steps), ALIAS, WORKSPACE.
+ */
+int scalify_orthogonalize(const scalify_array* X, int steps, const float* coef, float eps, scalify_array* O,
+                          void* workspace, size_t workspace_bytes, void* stream);
+/* Bytes of workspace that the two calls need for this list of matrices (shapes only; >= 4096; 0 for a bad shape). */
+size_t scalify_muon_workspace_bytes(int n_tensors, const scalify_array* w);
+
+/* How a step's length goes with the matrix: factor = 1; sqrt(max(1, rows/cols)) (bounds the change of the output's
+ * root mean square); 0.2 sqrt(max(rows, cols)) (the root mean square of an Adam step). */
+enum { SCALIFY_MUON_UNIT = 0, SCALIFY_MUON_SPECTRAL = 1, SCALIFY_MUON_RMS = 2 };
+
+/*
+ * Scaled Muon step over a list of matrices, beside scalify_scaled_adam_step for the other parameters.  In value space
+ *   m' = mu*m + (1-mu)*g;   u = nesterov ? mu*m' + (1-mu)*g : m';   O = orthogonalised u (of u / m'_s)
+ *   w' = w - lr*weight_decay*w - lr*factor*O
+ * and the scales follow the static rules as for Adam (a scalar constant c carries "c rounded down to a power of two"):
+ *   m'_s = max(p2(mu)*m_s, p2(1-mu)*g_s)  (without the first term for mu = 0);
+ *   w'_s = max(w_s, p2(lr*factor) / kf(max(rows, cols)))
+ * m' and w' are rounded once from fp32 arithmetic (u is not rounded before its norm).
+ *   grads[i]: [rows, cols], any dtype; m[i]: F16 or F32; w[i]: F16, BF16 or F32; w_cast[i] (or w_cast == NULL): E4M3, E5M2,
+ *   F16 or BF16, receives cast(stored w') with w'_s, as for scalify_scaled_adam_step_cast.  Row strides are free; one
+ *   dtype per list.  m and w (data and scale words) are updated in place; all their scale words are required and
+ *   distinct, and none is a gradient's.
+ *   0 <= momentum < 1;  lr >= 0;  0 <= lr*weight_decay < 1.  Matrices of one shape (or transposed) run as one batch.
+ * Errors: NULL, DTYPE, SHAPE, ALIGNMENT, VALUE, ALIAS, WORKSPACE (scalify_muon_workspace_bytes of w).
+ */
+int scalify_scaled_muon_step(int n_tensors, const scalify_array* grads, scalify_array* m, scalify_array* w,
+                             scalify_array* w_cast, float lr, float momentum, int nesterov, float weight_decay, int steps,
+                             const float* coef, float eps, int factor, void* workspace, size_t workspace_bytes,
+                             void* stream);
+
+/*
  * Block scales (Section 2: the scale component may be any array that broadcasts
  * against the data; the paper names the E8M0 exponent byte and the OCP
  * micro-scaling formats as the standard it follows, and works with one scalar

@@ -25,6 +25,7 @@ STAT_NONE, STAT_AMAX, STAT_L2 = 0, 1, 2
 OP_MATMUL, OP_RESCALE, OP_LAYERNORM_BWD, OP_ADAM, OP_STATISTIC, OP_CROSS_ENTROPY, OP_COLSUM, OP_MATMUL_SPLITK = (
     0, 1, 2, 3, 4, 5, 6, 7)
 OP_RMSNORM_BWD, OP_EMBEDDING_GRAD = 8, 9
+MUON_UNIT, MUON_SPECTRAL, MUON_RMS = 0, 1, 2
 DEV_TIMEOUT, DEV_BAD_SCALE, DEV_NONFINITE_STAT, DEV_BAD_INDEX = 1, 2, 4, 8
 
 _DTYPE_CODE = {torch.float8_e4m3fn: E4M3, torch.float8_e5m2: E5M2, torch.float16: F16,
@@ -117,7 +118,11 @@ def lib() -> ctypes.CDLL:
         L.scalify_scaled_add_rmsnorm_bwd.argtypes = [P, P, P, P, vp, P, P, vp, i32, P, vp, sz, vp]
         L.scalify_scaled_embedding_lookup.argtypes = [vp, i64, i64, P, f32, P, vp, vp]
         L.scalify_scaled_embedding_grad.argtypes = [vp, i64, i64, P, f32, P, P, vp, sz, vp]
-        for name in ("scalify_scaled_add_rmsnorm", "scalify_scaled_add_rmsnorm_bwd", "scalify_scaled_embedding_lookup",
+        L.scalify_orthogonalize.argtypes = [P, i32, vp, f32, P, vp, sz, vp]
+        L.scalify_muon_workspace_bytes.restype = sz
+        L.scalify_muon_workspace_bytes.argtypes = [i32, P]
+        L.scalify_scaled_muon_step.argtypes = [i32, P, P, P, P, f32, f32, i32, f32, i32, vp, f32, i32, vp, sz, vp]
+        for name in ("scalify_orthogonalize", "scalify_scaled_muon_step", "scalify_scaled_add_rmsnorm", "scalify_scaled_add_rmsnorm_bwd", "scalify_scaled_embedding_lookup",
                      "scalify_scaled_embedding_grad", "scalify_workspace_init", "scalify_check_status", "scalify_scaled_matmul", "scalify_scaled_matmul_delayed",
                      "scalify_statistic",
                      "scalify_rescale", "scalify_scaled_add", "scalify_scaled_layernorm",
@@ -642,3 +647,56 @@ def scalify_scaled_embedding_grad(ids: torch.Tensor, dY: ScaledTensor, dwte: Sca
     dev = _same_device(name, dwte.data, ids, dY.data, _data(addend), ws.buf)
     g, w, a = _desc(dY), _desc(dwte), _desc(addend)
     _call(name, dev, stream, ids.data_ptr(), ids.numel(), pad, _ref(g), float(c), _ref(a), _ref(w), ws.ptr, ws.nbytes)
+
+
+def scalify_muon_workspace_bytes(w: Sequence[ScaledTensor]) -> int:
+    """Workspace of scalify_scaled_muon_step for these weights, or of scalify_orthogonalize for [X]."""
+    n = int(lib().scalify_muon_workspace_bytes(len(w), _desc_array(w)))
+    if n == 0:
+        raise ValueError("scalify_muon_workspace_bytes: matrices of 1 to 32768 rows and columns")
+    return n
+
+
+def _coef(coef: Optional[Sequence[float]]):
+    if coef is None:
+        return None
+    if len(coef) != 3:
+        raise ValueError("coef: three coefficients (a, b, c) of a Z + b (Z Z^T) Z + c (Z Z^T)^2 Z")
+    return ctypes.cast((ctypes.c_float * 3)(*coef), ctypes.c_void_p)
+
+
+def scalify_orthogonalize(X: ScaledTensor, O: ScaledTensor, ws: Workspace, *, steps: int = 5,
+                          coef: Optional[Sequence[float]] = None, eps: float = 1e-7, stream=None) -> None:
+    """O = the orthogonalised matrix (or batch of matrices) X, by `steps` Newton-Schulz iterations."""
+    name = "scalify_orthogonalize"
+    dev = _same_device(name, X.data, O.data, ws.buf)
+    x, o = _desc(X), _desc(O)
+    _call(name, dev, stream, _ref(x), int(steps), _coef(coef), float(eps), _ref(o), ws.ptr, ws.nbytes)
+
+
+class MuonTensors:
+    """Marshalled descriptor arrays of a fixed list of matrices (built once, reused every step)."""
+
+    def __init__(self, grads: Sequence[ScaledTensor], m: Sequence[ScaledTensor], w: Sequence[ScaledTensor],
+                 w_cast: Optional[Sequence[ScaledTensor]] = None):
+        if not len(grads) == len(m) == len(w) or (w_cast is not None and len(w_cast) != len(w)):
+            raise ValueError("MuonTensors: lists of one length")
+        self.n = len(w)
+        self.keep = (list(grads), list(m), list(w), None if w_cast is None else list(w_cast))
+        self.g, self.m, self.w = _desc_array(grads), _desc_array(m), _desc_array(w)
+        self.w_cast = None if w_cast is None else _desc_array(w_cast)
+        every = [t.data for ts in self.keep if ts is not None for t in ts]
+        self.device = _same_device("MuonTensors", *every) if every else None
+
+
+def scalify_scaled_muon_step(tensors: MuonTensors, ws: Workspace, *, lr: float, momentum: float = 0.95,
+                             nesterov: bool = True, weight_decay: float = 0.0, steps: int = 5,
+                             coef: Optional[Sequence[float]] = None, eps: float = 1e-7, factor: int = MUON_SPECTRAL,
+                             stream=None) -> None:
+    """Muon step over the list: momentum, orthogonalisation, weight update and (optionally) its low-precision copy."""
+    name = "scalify_scaled_muon_step"
+    if tensors.n == 0:
+        return
+    _same_device(name, ws.buf, tensors.keep[2][0].data)
+    _call(name, tensors.device, stream, tensors.n, tensors.g, tensors.m, tensors.w, tensors.w_cast, float(lr), float(momentum),
+          int(bool(nesterov)), float(weight_decay), int(steps), _coef(coef), float(eps), int(factor), ws.ptr, ws.nbytes)

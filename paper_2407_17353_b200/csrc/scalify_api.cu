@@ -1343,4 +1343,151 @@ int scalify_scaled_cross_entropy(const scalify_array* logits, int64_t n_classes,
                               dlogits ? dlogits->scale : nullptr, workspace, static_cast<cudaStream_t>(stream));
 }
 
+// ---------------------------------------------------------------- orthogonalisation and the Muon step
+namespace {
+constexpr int64_t kMuonMaxSide = 32768;
+constexpr int kMuonMaxTensors = 65536;
+
+// rows x cols of one matrix; the row stride
+int matrix_of(const scalify_array* a, int64_t* rows, int64_t* cols, int64_t* ld) {
+  if (a->ndim != 2) return SCALIFY_ERR_SHAPE;
+  *rows = a->shape[0]; *cols = a->shape[1]; *ld = a->stride[0];
+  return (*rows < 1 || *cols < 1 || *rows > kMuonMaxSide || *cols > kMuonMaxSide) ? SCALIFY_ERR_SHAPE : SCALIFY_OK;
+}
+int check_newton_schulz(int steps, const float* coef, float eps, MuonHyper* h) {
+  static const float kDefault[3] = {3.4445f, -4.7750f, 2.0315f};
+  const float* c = coef ? coef : kDefault;
+  if (steps < 1 || steps > 16 || !(eps >= 0.f) || isinf(eps)) return SCALIFY_ERR_VALUE;
+  for (int i = 0; i < 3; ++i)
+    if (!isfinite(c[i])) return SCALIFY_ERR_VALUE;
+  h->steps = steps; h->eps = eps; h->a = c[0]; h->b = c[1]; h->c = c[2];
+  return SCALIFY_OK;
+}
+// The matrices of a list of [rows, cols] or [batch, rows, cols] arrays, one entry each (shapes only); 0 if one does not fit
+int count_matrices(int n, const scalify_array* w) {
+  int64_t total = 0;
+  for (int i = 0; i < n; ++i) {
+    const int nd = w[i].ndim;
+    if (nd != 2 && nd != 3) return 0;
+    const int64_t b = nd == 3 ? w[i].shape[0] : 1, r = w[i].shape[nd - 2], c = w[i].shape[nd - 1];
+    if (b < 1 || b > kMuonMaxTensors || r < 1 || c < 1 || r > kMuonMaxSide || c > kMuonMaxSide) return 0;
+    total += b;
+    if (total > kMuonMaxTensors) return 0;
+  }
+  return static_cast<int>(total);
+}
+struct MuonList {  // (no exceptions across the C boundary: a failed allocation leaves p null)
+  MuonTensor* p;
+  explicit MuonList(int n) : p(new (std::nothrow) MuonTensor[n > 0 ? n : 1]()) {}
+  ~MuonList() { delete[] p; }
+};
+void list_shapes(int n, const scalify_array* w, MuonTensor* out) {
+  for (int i = 0, k = 0; i < n; ++i) {
+    const int nd = w[i].ndim;
+    const int64_t b = nd == 3 ? w[i].shape[0] : 1;
+    for (int64_t j = 0; j < b; ++j, ++k) { out[k].rows = static_cast<int>(w[i].shape[nd - 2]); out[k].cols = static_cast<int>(w[i].shape[nd - 1]); }
+  }
+}
+}  // namespace
+
+size_t scalify_muon_workspace_bytes(int n_tensors, const scalify_array* w) {
+  if (n_tensors < 0 || (n_tensors > 0 && !w)) return 0;
+  const int total = count_matrices(n_tensors, w);
+  if (total == 0) return n_tensors == 0 ? kWsMin : 0;
+  MuonList list(total);
+  if (!list.p) return 0;
+  list_shapes(n_tensors, w, list.p);
+  return muon_ws_bytes(total, list.p);
+}
+
+int scalify_orthogonalize(const scalify_array* X, int steps, const float* coef, float eps, scalify_array* O, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+  int rc = check_array(X);
+  if (!rc) rc = check_array(O);
+  if (rc) return rc;
+  if (O->dtype != SCALIFY_F16 && O->dtype != SCALIFY_BF16) return SCALIFY_ERR_DTYPE;
+  MuonHyper h = {};
+  rc = check_newton_schulz(steps, coef, eps, &h);
+  if (rc) return rc;
+  if (!same_shape(X, O)) return SCALIFY_ERR_SHAPE;
+  const int total = count_matrices(1, X), nd = X->ndim;
+  if (total == 0) return SCALIFY_ERR_SHAPE;
+  if (!disjoint(X, O) || (O->scale && O->scale == X->scale)) return SCALIFY_ERR_ALIAS;
+  rc = check_ws(workspace, workspace_bytes, kWsMin);
+  if (rc) return rc;
+  MuonList list(total);
+  if (!list.p) return SCALIFY_ERR_WORKSPACE;
+  for (int i = 0; i < total; ++i) {
+    MuonTensor& t = list.p[i];
+    t.g = static_cast<const char*>(X->data) + (nd == 3 ? i * X->stride[0] : 0) * elem_size(X->dtype);
+    t.g_ld = X->stride[nd - 2]; t.g_dt = static_cast<int8_t>(X->dtype); t.g_scale = X->scale;
+    t.w = static_cast<char*>(O->data) + (nd == 3 ? i * O->stride[0] : 0) * elem_size(O->dtype);
+    t.w_ld = O->stride[nd - 2]; t.w_dt = static_cast<int8_t>(O->dtype); t.w_scale = i == 0 ? O->scale : nullptr;
+    t.rows = static_cast<int>(X->shape[nd - 2]); t.cols = static_cast<int>(X->shape[nd - 1]);
+  }
+  if (workspace_bytes < muon_ws_bytes(total, list.p)) return SCALIFY_ERR_WORKSPACE;
+  return launch_muon(total, list.p, h, workspace, static_cast<cudaStream_t>(stream));
+}
+
+int scalify_scaled_muon_step(int n_tensors, const scalify_array* grads, scalify_array* m, scalify_array* w,
+                             scalify_array* w_cast, float lr, float momentum, int nesterov, float weight_decay, int steps,
+                             const float* coef, float eps, int factor, void* workspace, size_t workspace_bytes,
+                             void* stream) {
+  if (n_tensors < 0 || n_tensors > kMuonMaxTensors) return SCALIFY_ERR_SHAPE;
+  if (n_tensors > 0 && (!grads || !m || !w)) return SCALIFY_ERR_NULL;
+  MuonHyper h = {};
+  int rc = check_newton_schulz(steps, coef, eps, &h);
+  if (rc) return rc;
+  if (!(momentum >= 0.f && momentum < 1.f) || !(lr >= 0.f) || isinf(lr) || !(weight_decay >= 0.f) || isinf(weight_decay)) return SCALIFY_ERR_VALUE;
+  if (factor != SCALIFY_MUON_UNIT && factor != SCALIFY_MUON_SPECTRAL && factor != SCALIFY_MUON_RMS) return SCALIFY_ERR_VALUE;
+  h.decay = static_cast<float>(static_cast<double>(lr) * weight_decay);
+  if (!(h.decay < 1.f)) return SCALIFY_ERR_VALUE;
+  h.momentum = momentum; h.lr = lr; h.nesterov = nesterov ? 1 : 0; h.factor = factor;
+  MuonList list(n_tensors);
+  const void** words = new (std::nothrow) const void*[3 * static_cast<size_t>(n_tensors) + 1];
+  struct Free { const void** p; ~Free() { delete[] p; } } free_words{words};
+  if (!list.p || !words) return SCALIFY_ERR_WORKSPACE;
+  int n_words = 0;
+  for (int i = 0; i < n_tensors; ++i) {
+    rc = check_array(&grads[i]);
+    if (!rc) rc = check_array(&m[i]);
+    if (!rc) rc = check_array(&w[i]);
+    if (!rc && w_cast) rc = check_array(&w_cast[i]);
+    if (rc) return rc;
+    if (!m[i].scale || !w[i].scale || (w_cast && !w_cast[i].scale)) return SCALIFY_ERR_NULL;
+    if ((m[i].dtype != SCALIFY_F16 && m[i].dtype != SCALIFY_F32) || !is_wide(w[i].dtype)) return SCALIFY_ERR_DTYPE;
+    if (w_cast && (w_cast[i].dtype == SCALIFY_F32 || elem_size(w_cast[i].dtype) > elem_size(w[i].dtype))) return SCALIFY_ERR_DTYPE;
+    if (grads[i].dtype != grads[0].dtype || m[i].dtype != m[0].dtype || w[i].dtype != w[0].dtype ||
+        (w_cast && w_cast[i].dtype != w_cast[0].dtype))
+      return SCALIFY_ERR_DTYPE;
+    MuonTensor& t = list.p[i];
+    int64_t rows, cols, r2, c2;
+    if (matrix_of(&w[i], &rows, &cols, &t.w_ld)) return SCALIFY_ERR_SHAPE;
+    if (matrix_of(&grads[i], &r2, &c2, &t.g_ld) || r2 != rows || c2 != cols) return SCALIFY_ERR_SHAPE;
+    if (matrix_of(&m[i], &r2, &c2, &t.m_ld) || r2 != rows || c2 != cols) return SCALIFY_ERR_SHAPE;
+    if (w_cast && (matrix_of(&w_cast[i], &r2, &c2, &t.wc_ld) || r2 != rows || c2 != cols)) return SCALIFY_ERR_SHAPE;
+    const scalify_array* wc = w_cast ? &w_cast[i] : nullptr;
+    if (!disjoint(&m[i], &grads[i]) || !disjoint(&w[i], &grads[i]) || !disjoint(&m[i], &w[i]) || !disjoint(wc, &grads[i]) ||
+        !disjoint(wc, &m[i]) || !disjoint(wc, &w[i]))
+      return SCALIFY_ERR_ALIAS;
+    t.g = grads[i].data; t.g_dt = static_cast<int8_t>(grads[i].dtype); t.g_scale = grads[i].scale;
+    t.m = m[i].data; t.m_dt = static_cast<int8_t>(m[i].dtype); t.m_scale = m[i].scale;
+    t.w = w[i].data; t.w_dt = static_cast<int8_t>(w[i].dtype); t.w_scale = w[i].scale;
+    if (wc) { t.wc = wc->data; t.wc_dt = static_cast<int8_t>(wc->dtype); t.wc_scale = wc->scale; }
+    t.rows = static_cast<int>(rows); t.cols = static_cast<int>(cols);
+    words[n_words++] = m[i].scale;
+    words[n_words++] = w[i].scale;
+    if (wc) words[n_words++] = wc->scale;
+  }
+  std::sort(words, words + n_words);
+  for (int i = 1; i < n_words; ++i)
+    if (words[i] == words[i - 1]) return SCALIFY_ERR_ALIAS;
+  for (int i = 0; i < n_tensors; ++i)
+    if (grads[i].scale && std::binary_search(words, words + n_words, static_cast<const void*>(grads[i].scale))) return SCALIFY_ERR_ALIAS;
+  if (n_tensors == 0) return SCALIFY_OK;
+  rc = check_ws(workspace, workspace_bytes, muon_ws_bytes(n_tensors, list.p));
+  if (rc) return rc;
+  return launch_muon(n_tensors, list.p, h, workspace, static_cast<cudaStream_t>(stream));
+}
+
 }  // extern "C"

@@ -209,6 +209,23 @@ int launch_embedding_lookup(const EmbeddingArgs& a, int w_dt, cudaStream_t st);
 size_t embedding_grad_ws_bytes(int64_t n, int64_t d);
 int launch_embedding_grad(const EmbeddingArgs& a, int g_dt, void* ws, cudaStream_t st);
 
+// Orthogonalisation and the optimiser step on it: one matrix each.
+struct MuonTensor {
+  const void* g; int64_t g_ld; const float* g_scale;   // gradient, or the matrix itself
+  void* m; int64_t m_ld; float* m_scale;               // momentum (nullptr: orthogonalisation only)
+  void* w; int64_t w_ld; float* w_scale;               // weight, or the output
+  void* wc; int64_t wc_ld; float* wc_scale;            // 8-bit / 16-bit copy of the weight, or nullptr
+  int rows, cols;
+  int8_t g_dt, m_dt, w_dt, wc_dt;
+};
+struct MuonHyper {
+  float a, b, c, eps;                     // quintic coefficients, and what is added to the norm
+  int steps;
+  float momentum, lr, decay;              // decay = lr * weight_decay
+  int nesterov, factor;
+};
+size_t muon_ws_bytes(int n, const MuonTensor* t);
+int launch_muon(int n, const MuonTensor* t, const MuonHyper& h, void* ws, cudaStream_t st);
 int launch_mx_quantize_t(const void* X, int x_dt, int64_t rows, int64_t K, int64_t ldx, void* data, int elem_dt,
                          uint8_t* sf, const float* x_scale, float* y_scale, uint32_t* status, cudaStream_t st);
 int launch_mx_quantize(const void* X, int x_dt, int64_t rows, int64_t K, int64_t ldx, void* data, int elem_dt,

@@ -102,3 +102,63 @@ def embedding_grad(ids, g, gs, vocab, c, padding_id, addend=None, addend_s=0.0):
         mag = mag * (scale / s) + addend.double().abs() * (addend_s / s)
         scale = s
     return out, scale, mag, int(count.max()) if count.numel() else 0
+
+
+COEF = (3.4445, -4.7750, 2.0315)
+
+
+def newton_schulz(u, steps=5, coef=COEF, eps=1e-7):
+    """[batch, rows, cols] float64 -> the iterate after `steps`, by the definition on the shorter side."""
+    tall = u.shape[1] > u.shape[2]
+    z = u.double()
+    z = z.transpose(1, 2) if tall else z
+    z = z / (z.square().sum((1, 2), keepdim=True).sqrt() + eps)
+    for _ in range(steps):
+        a = z @ z.transpose(1, 2)
+        z = coef[0] * z + (coef[1] * a + coef[2] * (a @ a)) @ z
+    return z.transpose(1, 2) if tall else z
+
+
+def newton_schulz_bar(u, steps=1, coef=COEF, eps=1e-7):
+    """A bound, element by element and to first order, on the error of the iterate when Z, A and D are rounded to FP16
+    (h = 2^-11 relative, and half the smallest subnormal at the scale each is held at) and products are accumulated in
+    fp32 (k terms: k 2^-24 of their magnitudes).  The magnitudes are carried along in absolute values."""
+    tall = u.shape[1] > u.shape[2]
+    z = u.double()
+    z = z.transpose(1, 2) if tall else z
+    z = z / (z.square().sum((1, 2), keepdim=True).sqrt() + eps)
+    n, k = z.shape[1], z.shape[2]
+    h, sub = 2.0 ** -11, 2.0 ** -25
+    eye = torch.eye(n, dtype=torch.float64, device=u.device)
+    ez = (h + 8 * U) * z.abs() + sub / kf(k)
+    for _ in range(steps):
+        a = z @ z.transpose(1, 2)
+        za = z.abs()
+        mag = za @ za.transpose(1, 2)
+        ea = (h + 2 * U) * a.abs() + (k * U) * mag + 2 * (ez @ za.transpose(1, 2)) + sub / 4096
+        ea = torch.maximum(ea, ea.transpose(1, 2))
+        d = coef[0] * eye + coef[1] * a + coef[2] * (a @ a)
+        aa = a.abs()
+        ed = (h + 4 * U) * d.abs() + abs(coef[1]) * ea + abs(coef[2]) * (n * U * (aa @ aa) + 2 * (ea @ aa)) + sub / 4096
+        ed = torch.maximum(ed, ed.transpose(1, 2))
+        new = d @ z
+        ez = (h + 2 * U) * new.abs() + ed @ za + d.abs() @ ez + n * U * (d.abs() @ za) + sub / kf(k)
+        z = new
+    return ez.transpose(1, 2) * 1.02 if tall else ez * 1.02  # 2 %: the products of two errors
+
+
+def muon_step(g, gs, m, ms, w, ws, *, lr, momentum, nesterov, decay, steps, factor, coef=COEF, eps=1e-7):
+    """Data and scales of m' and w' before rounding, u (in units of m'_s), the orthogonalised u, and w's step length."""
+    rows, cols = w.shape
+    m_s = gs * p2(1 - momentum)
+    if momentum > 0:
+        m_s = max(m_s, p2(momentum) * ms)
+    gd, md = g.double() * (gs / m_s), m.double() * (ms / m_s)
+    new_m = momentum * md + (1 - momentum) * gd
+    u = momentum * new_m + (1 - momentum) * gd if nesterov else new_m
+    o = newton_schulz(u[None], steps, coef, eps)[0]
+    kappa = {0: 1.0, 1: math.sqrt(max(1.0, rows / cols)), 2: 0.2 * math.sqrt(max(rows, cols))}[factor]
+    step = lr * kappa
+    w_s = max(ws, p2(step) / kf(max(rows, cols))) if step > 0 else ws
+    new_w = (1 - decay) * (ws / w_s) * w.double() - (step / w_s) * o
+    return dict(m=new_m, m_s=m_s, w=new_w, w_s=w_s, u=u, o=o, step=step)

@@ -194,3 +194,85 @@ def test_plain_embedding_gradient_against_differences():
             e[i, j] = 1e-6
             assert abs((f(w + e) - f(w - e)) / 2e-6 - float(got[i, j]) * scale) < 1e-6
     assert count == 3
+
+
+def test_orthogonalize_refusals():
+    B, F = sc.BF16, sc.F32
+    L = sc.lib()
+    coef = (ctypes.c_float * 3)(2.0, -1.5, 0.5)
+    x, o, big = arr(1, F, (64, 96)), arr(2, B, (64, 96)), 256 * MB
+
+    def call(x=x, steps=5, coef=None, eps=1e-7, o=o, ws=16 * MB, nb=big):
+        p = lambda a: None if a is None else R(a)  # noqa: E731
+        return L.scalify_orthogonalize(p(x), steps, coef, eps, p(o), ws, nb, None)
+    assert call(x=None) == NULL and call(o=None) == NULL
+    assert call(o=arr(2, F, (64, 96))) == DTYPE and call(o=arr(2, sc.E4M3, (64, 96))) == DTYPE
+    assert call(o=arr(2, B, (96, 64))) == SHAPE and call(x=arr(1, F, (96,)), o=arr(2, B, (96,))) == SHAPE
+    assert call(x=arr(1, F, (32776, 8)), o=arr(2, B, (32776, 8))) == SHAPE
+    assert call(x=arr(1, F, (0, 8)), o=arr(2, B, (0, 8))) == SHAPE
+    assert call(steps=0) == VALUE and call(steps=17) == VALUE and call(eps=-1.0) == VALUE and call(eps=float("nan")) == VALUE
+    for i in range(3):
+        bad = (ctypes.c_float * 3)(*coef)
+        bad[i] = float("inf")
+        assert call(coef=bad) == VALUE
+    assert call(o=arr(1, B, (64, 96), offset=256)) == ALIAS
+    assert call(x=arr(1, F, (64, 96), scale=64), o=arr(2, B, (64, 96), scale=64)) == ALIAS
+    assert call(ws=None) == WORKSPACE and call(nb=4096) == WORKSPACE and call(ws=16 * MB + 16) == WORKSPACE
+    need = L.scalify_muon_workspace_bytes(1, R(x))
+    assert need > 2 * 2 * 64 * 96 and call(nb=need - 1) == WORKSPACE
+    assert L.scalify_muon_workspace_bytes(1, R(arr(1, F, (96,)))) == 0
+    assert L.scalify_muon_workspace_bytes(-1, None) == 0 and L.scalify_muon_workspace_bytes(0, None) >= 4096
+
+
+def test_muon_refusals():
+    L = sc.lib()
+    H, Q = sc.F16, sc.E4M3
+    words = iter(range(64, 100000, 4))
+
+    def lists(n=2, g=sc.E5M2, m=H, w=H, c=Q, shape=(64, 96), **over):
+        out = []
+        for k, dt in enumerate((g, m, w, c)):
+            a = (sc.scalify_array * n)()
+            for i in range(n):
+                a[i] = arr(1 + 8 * k + i, dt, shape, scale=next(words))
+            out.append(a)
+        for key, v in over.items():
+            out["gmwc".index(key[0])][int(key[1])] = v
+        return out
+
+    def call(ls, n=2, lr=0.02, mu=0.95, wd=0.0, steps=5, eps=1e-7, factor=1, ws=64 * MB, nb=256 * MB):
+        return L.scalify_scaled_muon_step(n, *ls, lr, mu, 1, wd, steps, None, eps, factor, ws, nb, None)
+    assert call([None] * 4, n=0) == 0 and call([None] * 4) == NULL and call(lists(), n=-1) == SHAPE
+    for lr, mu, wd in ((-1.0, 0.9, 0.0), (0.1, 1.0, 0.0), (0.1, -0.1, 0.0), (0.1, 0.9, -1.0), (0.5, 0.9, 2.0), (float("nan"), 0.9, 0.0)):
+        assert call(lists(), lr=lr, mu=mu, wd=wd) == VALUE
+    assert call(lists(), factor=3) == VALUE and call(lists(), steps=0) == VALUE and call(lists(), eps=-1.0) == VALUE
+    assert call(lists(m=sc.BF16)) == DTYPE and call(lists(w=Q)) == DTYPE and call(lists(c=sc.F32)) == DTYPE
+    assert call(lists(g1=arr(2, sc.BF16, (64, 96), scale=next(words)))) == DTYPE          # one dtype per list
+    assert call(lists(g1=arr(2, sc.E5M2, (96, 64), scale=next(words)))) == SHAPE
+    assert call(lists(w0=arr(17, H, (64 * 96,), scale=next(words)))) == SHAPE
+    assert call(lists(m0=arr(9, H, (64, 96)))) == NULL and call(lists(c1=arr(26, Q, (64, 96)))) == NULL  # no scale word
+    same = next(words)
+    assert call(lists(m0=arr(9, H, (64, 96), scale=same), w1=arr(18, H, (64, 96), scale=same))) == ALIAS
+    assert call(lists(g0=arr(1, sc.E5M2, (64, 96), scale=same), w1=arr(18, H, (64, 96), scale=same))) == ALIAS
+    assert call(lists(m0=arr(17, H, (64, 96), scale=next(words)))) == ALIAS               # m over w
+    assert call(lists(c0=arr(17, Q, (64, 96), scale=next(words)))) == ALIAS               # the copy over w
+    assert call(lists(), ws=None) == WORKSPACE and call(lists(), nb=4096) == WORKSPACE
+
+
+def test_plain_newton_schulz_against_the_singular_values():
+    torch.manual_seed(2)
+    for shape in ((5, 8), (8, 5)):
+        u = torch.randn(1, *shape, dtype=torch.float64)
+        a, s, b = torch.linalg.svd(u[0], full_matrices=False)
+        s = s / s.square().sum().sqrt()
+        for _ in range(5):
+            s = p64.COEF[0] * s + p64.COEF[1] * s ** 3 + p64.COEF[2] * s ** 5
+        assert float((p64.newton_schulz(u, eps=0.0)[0] - a @ torch.diag(s) @ b).abs().max()) < 1e-10
+
+
+def test_muon_binding_checks():
+    t = sc.ScaledTensor(torch.zeros(4, 8))
+    with pytest.raises(ValueError):
+        sc.MuonTensors([t], [t, t], [t])
+    with pytest.raises(ValueError):
+        sc.scalify_muon_workspace_bytes([sc.ScaledTensor(torch.zeros(8))])
