@@ -10,9 +10,11 @@
 //   Z_d = Z / sigma, sigma = 1/kf(L) (an orthogonal Z has entries of about 1/sqrt(L));   A_d = 2^12 A;   D_d = 2^12 D.
 // FP16 rather than BF16 because the products run at the same rate and its 11 bits leave an eighth of the rounding error,
 // which the iteration passes on to small singular values multiplied by up to 3.4 a step.
-//   gram:   A_d = (sigma^2 2^12) Z_d Z_d^T            symmetric: tiles on and above the diagonal, stored twice
+//   gram:   A_d = (sigma^2 2^12) Z_d Z_d^T            symmetric: only the tiles on and above the diagonal exist
 //   poly:   D_d = (c 2^-12) A_d A_d^T + b A_d + 2^12 a I   likewise; b A_d + .. is added to the fp32 accumulator
 //   update: Z_d <- 2^-12 D_d Z_d                       Z_d is the MN-major operand: no transposed copy
+// Where a product needs a block of A or D below the diagonal it reads the block's mirror image as an MN-major operand:
+// the layout is a matter of each K block's copies and descriptors, and no tile is stored twice.
 // Bound: the tensor pipe for large batches (S S L + S S S + 2 S S L flops a step); for few or small matrices the latency of
 // the chain of 3 `steps` products.
 #include <cuda.h>
@@ -34,11 +36,10 @@ constexpr int kStepK = 16;        // of one MMA
 constexpr int kAccs = 2;          // accumulators of 256 TMEM columns: the epilogue overlaps the next tile's products
 constexpr int kEpiWarpsM = 8;
 constexpr int kNsThreads = 64 + 32 * kEpiWarpsM;
-constexpr int kTile16 = 32 * 64;  // bytes of a 32 x 32 FP16 tile
 constexpr float kGramScale = 4096.0f;
 
 constexpr int kMaxInst = 96;      // matrices per batch (their descriptors travel as a kernel argument)
-constexpr int kMaxParts = 64;     // partial sums of a matrix's norm
+constexpr int kMaxParts = 256;    // partial sums of a matrix's norm
 constexpr int kPreTile = 64;      // rows and columns of a tile of the element-wise passes
 
 enum { kGram = 0, kPoly = 1, kUpdate = 2 };
@@ -49,9 +50,8 @@ template <int NCTA> struct NsCfg {
   static constexpr int kBRows = kTN / NCTA;  // rows (or columns of an MN-major operand) of B staged per CTA
   static constexpr int kABytes = kTM * 128;
   static constexpr int kBBytes = kBRows * 128;
-  static constexpr int kStages = NCTA == 1 ? 3 : 5;
-  static constexpr int kEpiBytes = kEpiWarpsM * 4 * kTile16;  // per warp: two tiles, straight and transposed
-  static constexpr size_t kSmem = size_t(kStages) * (kABytes + kBBytes) + kEpiBytes + 1024 + 256;
+  static constexpr int kStages = NCTA == 1 ? 4 : 6;
+  static constexpr size_t kSmem = size_t(kStages) * (kABytes + kBBytes) + 1024 + 256;
 };
 
 struct NsParams {
@@ -59,8 +59,9 @@ struct NsParams {
   int tiles_m, tiles_n, tiles;  // tiles of one matrix (symmetric: on and above the diagonal)
   uint32_t idesc;
   float alpha, b, diag;      // out = alpha acc (+ b A_d[r, c] + diag [r == c])
-  const __half* A;           // poly: A_d [batch][S][ld]
-  long long ld;
+  __half* Y;                 // [batch][S][ldy]
+  long long ldy;
+  const __half* A;           // poly: A_d, laid out like Y
   uint32_t* status;
 };
 
@@ -90,6 +91,13 @@ __device__ __forceinline__ void ns_tile(const NsParams& p, int tile, int& b, int
   }
 }
 
+// Whether K block kb of the operand's rows in tile `rt` lies below the diagonal of a symmetric matrix (of which only the
+// 256-wide tiles on and above it exist), or is MN-major anyway
+template <int MODE> __device__ __forceinline__ bool a_transposed(int kb, int rt) { return MODE != kGram && kb / (kTN / kTK) < rt; }
+template <int MODE> __device__ __forceinline__ bool b_transposed(int kb, int rt) {
+  return MODE == kUpdate || (MODE == kPoly && kb / (kTN / kTK) < rt);
+}
+
 }  // namespace
 
 // Warp 0: TMA producer; warp 1: MMA issuer; warps 2-9: epilogue.  Persistent CTAs (pairs).  Every wait is bounded; on
@@ -97,7 +105,8 @@ __device__ __forceinline__ void ns_tile(const NsParams& p, int tile, int& b, int
 template <int MODE, int NCTA>
 __global__ void __launch_bounds__(kNsThreads, 1) ns_product_kernel(const __grid_constant__ CUtensorMap map_a,
                                                                   const __grid_constant__ CUtensorMap map_b,
-                                                                  const __grid_constant__ CUtensorMap map_y, const NsParams p) {
+                                                                  const __grid_constant__ CUtensorMap map_at,
+                                                                  const __grid_constant__ CUtensorMap map_bt, const NsParams p) {
   using C = NsCfg<NCTA>;
   constexpr int kStages = C::kStages;
   asm volatile("griddepcontrol.launch_dependents;");  // the next product may set up while this one runs
@@ -106,9 +115,8 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_product_kernel(const __grid_
   uint8_t* smem = smem_raw + (base - raw);
   const uint32_t smem_a = base, smem_b = base + kStages * C::kABytes;
   constexpr uint32_t kRing = kStages * (C::kABytes + C::kBBytes);
-  uint8_t* epi_mem = smem + kRing;
-  uint8_t* bar_mem = epi_mem + C::kEpiBytes;
-  const uint32_t bars = base + kRing + C::kEpiBytes;
+  uint8_t* bar_mem = smem + kRing;
+  const uint32_t bars = base + kRing;
   const uint32_t full_bar = bars, empty_bar = bars + 8 * kStages, acc_full = bars + 16 * kStages, acc_empty = acc_full + 8 * kAccs,
                  drain_bar = acc_empty + 8 * kAccs;
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(bar_mem + 16 * kStages + 16 * kAccs + 8);
@@ -124,6 +132,14 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_product_kernel(const __grid_
     mbar_init(drain_bar, 1);
     *abort_flag = 0u;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (threadIdx.x == 32 * 2) {  // (the maps are arguments: nothing the kernel before writes)
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_a)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_b)) : "memory");
+    if constexpr (MODE != kGram) {
+      asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_at)) : "memory");
+      asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_bt)) : "memory");
+    }
   }
   if (warp == 1) tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), kAccs * kTN);
   tc_fence_before();
@@ -146,27 +162,30 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_product_kernel(const __grid_
         for (int kb = 0; kb < num_kb; ++kb) {
           if (!mbar_wait(empty_bar + 8 * stage, phase ^ 1u, abort_flag)) { timed_out = true; break; }
           const uint32_t sa = smem_a + stage * C::kABytes, sb = smem_b + stage * C::kBBytes;
-          const int kx = kb * kTK * 2;  // byte coordinate of the K block
           uint32_t fb = full_bar + 8 * stage;
+          const bool a_mn = a_transposed<MODE>(kb, mt), b_mn = b_transposed<MODE>(kb, nt);
           if constexpr (NCTA == 2) {
             if (rank == 0u) mbar_expect_tx(fb, 2 * (C::kABytes + C::kBBytes));
             fb = map_to_cta(fb, 0u);  // both CTAs' copies are counted on the leader's barrier
-            tma_load_3d_pair(sa, &map_a, fb, kx, m0, b);
-            if constexpr (MODE == kUpdate) {
-#pragma unroll
-              for (int j = 0; j < C::kBRows / kTK; ++j) tma_load_3d_pair(sb + j * kTK * 128, &map_b, fb, (n0 + j * kTK) * 2, kb * kTK, b);
-            } else {
-              tma_load_3d_pair(sb, &map_b, fb, kx, n0, b);
-            }
           } else {
             mbar_expect_tx(fb, C::kABytes + C::kBBytes);
-            tma_load_3d(sa, &map_a, fb, kx, m0, b);
-            if constexpr (MODE == kUpdate) {
+          }
+          auto load = [&](uint32_t dst, const CUtensorMap* m, int x, int y) {
+            if constexpr (NCTA == 2) tma_load_3d_pair(dst, m, fb, x * 2, y, b);  // (the maps count bytes)
+            else tma_load_3d(dst, m, fb, x * 2, y, b);
+          };
+          // along K: one box of 64 elements x all rows; MN-major: boxes of 64 columns x the 64 lines of this K block
+          if (!a_mn) {
+            load(sa, &map_a, kb * kTK, m0);
+          } else {
 #pragma unroll
-              for (int j = 0; j < C::kBRows / kTK; ++j) tma_load_3d(sb + j * kTK * 128, &map_b, fb, (n0 + j * kTK) * 2, kb * kTK, b);
-            } else {
-              tma_load_3d(sb, &map_b, fb, kx, n0, b);
-            }
+            for (int j = 0; j < kTM / kTK; ++j) load(sa + j * kTK * 128, &map_at, m0 + j * kTK, kb * kTK);
+          }
+          if (!b_mn) {
+            load(sb, &map_b, kb * kTK, n0);
+          } else {
+#pragma unroll
+            for (int j = 0; j < C::kBRows / kTK; ++j) load(sb + j * kTK * 128, &map_bt, n0 + j * kTK, kb * kTK);
           }
           ++issued;
           if (++stage == kStages) { stage = 0; phase ^= 1u; }
@@ -186,24 +205,29 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_product_kernel(const __grid_
   } else if (warp == 1) {
     if (lane == 0 && rank == 0u) {
       uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
-      // MN-major B: atoms of 64 columns x 8 rows of K; along K they are 1024 bytes apart, the next 64 columns a K block's
-      // box (64 x 128 bytes) further on
-      const uint64_t a_desc0 = make_smem_desc(smem_a, 0u, 1024u);
-      const uint64_t b_desc0 = make_smem_desc(smem_b, MODE == kUpdate ? kTK * 128u : 0u, 1024u);
-      constexpr uint32_t a_inc = kStepK * 2 >> 4, b_inc = MODE == kUpdate ? (kStepK * 128 >> 4) : (kStepK * 2 >> 4);
+      // MN-major: atoms of 64 columns x 8 lines of K; along K they are 1024 bytes apart, the next 64 columns a box
+      // (64 x 128 bytes) further on
+      const uint64_t a_desc_k = make_smem_desc(smem_a, 0u, 1024u), a_desc_mn = make_smem_desc(smem_a, kTK * 128u, 1024u);
+      const uint64_t b_desc_k = make_smem_desc(smem_b, 0u, 1024u), b_desc_mn = make_smem_desc(smem_b, kTK * 128u, 1024u);
+      constexpr uint32_t k_inc = kStepK * 2 >> 4, mn_inc = kStepK * 128 >> 4;
       for (int tile = unit; tile < num_tiles && !timed_out; tile += num_units) {
         if (!mbar_wait(acc_empty + 8 * acc, acc_phase ^ 1u, abort_flag)) { timed_out = true; break; }
         tc_fence_after();
         const uint32_t d_tmem = tmem_base + acc * kTN;
+        int b, mt, nt;
+        ns_tile<MODE>(p, tile, b, mt, nt);
         for (int kb = 0; kb < num_kb; ++kb) {
+          const bool a_mn = a_transposed<MODE>(kb, mt), b_mn = b_transposed<MODE>(kb, nt);
+          const uint32_t idesc = p.idesc | (uint32_t(a_mn) << 15) | (uint32_t(b_mn) << 16);
+          const uint32_t a_inc = a_mn ? mn_inc : k_inc, b_inc = b_mn ? mn_inc : k_inc;
+          const uint64_t ad0 = (a_mn ? a_desc_mn : a_desc_k) + static_cast<uint64_t>(stage * (C::kABytes >> 4));
+          const uint64_t bd0 = (b_mn ? b_desc_mn : b_desc_k) + static_cast<uint64_t>(stage * (C::kBBytes >> 4));
           if (!mbar_wait(full_bar + 8 * stage, phase, abort_flag)) { timed_out = true; break; }
           tc_fence_after();
-          const uint64_t ad0 = a_desc0 + static_cast<uint64_t>(stage * (C::kABytes >> 4));
-          const uint64_t bd0 = b_desc0 + static_cast<uint64_t>(stage * (C::kBBytes >> 4));
 #pragma unroll
           for (int k = 0; k < kTK / kStepK; ++k) {
-            if constexpr (NCTA == 1) umma_f16(d_tmem, ad0 + k * a_inc, bd0 + k * b_inc, p.idesc, (kb | k) != 0 ? 1u : 0u);
-            else umma_f16_pair(d_tmem, ad0 + k * a_inc, bd0 + k * b_inc, p.idesc, (kb | k) != 0 ? 1u : 0u);
+            if constexpr (NCTA == 1) umma_f16(d_tmem, ad0 + k * a_inc, bd0 + k * b_inc, idesc, (kb | k) != 0 ? 1u : 0u);
+            else umma_f16_pair(d_tmem, ad0 + k * a_inc, bd0 + k * b_inc, idesc, (kb | k) != 0 ? 1u : 0u);
           }
           if constexpr (NCTA == 1) umma_commit(empty_bar + 8 * stage);
           else umma_commit_pair(empty_bar + 8 * stage);
@@ -224,32 +248,36 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_product_kernel(const __grid_
   } else {
     const int q = warp & 3, half = (warp - 2) / 4;  // TMEM lane quarter, half of the tile's columns
     constexpr int kChunks = kTN / 64;               // 32-column chunks per warp
-    uint8_t* stage_mem = epi_mem + (warp - 2) * 4 * kTile16;
-    uint32_t acc = 0, acc_phase = 0, buf = 0;
+    // Results go from registers to memory: a lane holds 32 columns of one row, two 32-byte stores.  (Staging them for the
+    // store engine in shared memory costs what the MMAs and the operand copies leave none of: its bandwidth.)
+    uint32_t acc = 0, acc_phase = 0;
     for (int tile = unit; tile < num_tiles; tile += num_units) {
       int b, mt, nt;
       ns_tile<MODE>(p, tile, b, mt, nt);
-      if (!mbar_wait(acc_full + 8 * acc, acc_phase, abort_flag)) { timed_out = true; break; }
-      tc_fence_after();
       const int c_first = half * kChunks, n0 = nt * kTN;
       const int n_chunks = max(0, min(kChunks, (p.N - n0 + 31) / 32 - c_first));  // chunks inside the matrix
-      const uint32_t t_addr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * kTN + c_first * 32;
-      const int row0 = mt * C::kTileM + static_cast<int>(rank) * kTM + q * 32, row = row0 + lane;
-      const bool mirror = MODE != kUpdate && mt != nt;
-      const __half* arow = nullptr;
-      if constexpr (MODE == kPoly) arow = p.A + (static_cast<long long>(b) * p.S + min(row, p.S - 1)) * p.ld;
-      uint32_t r[32];
-#pragma unroll 1
-      for (int c = 0; c < n_chunks; ++c) {
-        const int col0 = n0 + (c_first + c) * 32;
-        uint32_t wa[16];
-        tmem_ld32(t_addr + c * 32, r);
-        if constexpr (MODE == kPoly) {  // (the row's padding makes whole chunks readable)
+      const int row = mt * C::kTileM + static_cast<int>(rank) * kTM + q * 32 + lane;
+      __half* yrow = p.Y + (static_cast<long long>(b) * p.S + row) * p.ldy + n0 + c_first * 32;
+      // poly: this lane's row of A, read while the products run
+      uint4 wa[MODE == kPoly ? kChunks : 1][4];
+      if constexpr (MODE == kPoly) {
+        const __half* arow = p.A + (static_cast<long long>(b) * p.S + min(row, p.S - 1)) * p.ldy + n0 + c_first * 32;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) *reinterpret_cast<uint4*>(wa + 4 * j) = *reinterpret_cast<const uint4*>(arow + col0 + 8 * j);
-        }
+        for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            wa[c][j] = c < n_chunks ? *reinterpret_cast<const uint4*>(arow + c * 32 + 8 * j) : make_uint4(0u, 0u, 0u, 0u);
+      }
+      if (!mbar_wait(acc_full + 8 * acc, acc_phase, abort_flag)) { timed_out = true; break; }
+      tc_fence_after();
+      const uint32_t t_addr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * kTN + c_first * 32;
+#pragma unroll
+      for (int c2 = 0; c2 < kChunks; c2 += 2) {
+        uint32_t r[2][32];
+        tmem_ld32(t_addr + c2 * 32, r[0]);  // (columns past the matrix hold nothing of interest)
+        tmem_ld32(t_addr + (c2 + 1) * 32, r[1]);
         tmem_ld_wait();
-        if (c + 1 == n_chunks) {  // the accumulator has been read: the next tile may overwrite it
+        if (c2 + 2 == kChunks) {  // the accumulator has been read: the next tile may overwrite it
           tc_fence_before();
           __syncwarp();
           if (lane == 0) {
@@ -257,52 +285,31 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_product_kernel(const __grid_
             else mbar_arrive_cluster(map_to_cta(acc_empty + 8 * acc, 0u));
           }
         }
-        uint32_t o[16];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          float x = __uint_as_float(r[2 * j]) * p.alpha, y = __uint_as_float(r[2 * j + 1]) * p.alpha;
-          if constexpr (MODE == kPoly) {
-            const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&wa[j]));
-            x = fmaf(p.b, t.x, x) + (row == col0 + 2 * j ? p.diag : 0.f);
-            y = fmaf(p.b, t.y, y) + (row == col0 + 2 * j + 1 ? p.diag : 0.f);
+        for (int s = 0; s < 2; ++s) {
+          const int c = c2 + s, col0 = n0 + (c_first + c) * 32;
+          uint32_t o[16];
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            float x = __uint_as_float(r[s][2 * j]) * p.alpha, y = __uint_as_float(r[s][2 * j + 1]) * p.alpha;
+            if constexpr (MODE == kPoly) {
+              const uint4 w4 = wa[c][j / 4];
+              const uint32_t w = (j & 3) == 0 ? w4.x : (j & 3) == 1 ? w4.y : (j & 3) == 2 ? w4.z : w4.w;
+              const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w));
+              x = fmaf(p.b, v.x, x) + (row == col0 + 2 * j ? p.diag : 0.f);
+              y = fmaf(p.b, v.y, y) + (row == col0 + 2 * j + 1 ? p.diag : 0.f);
+            }
+            const __half2 hh = __floats2half2_rn(x, y);
+            o[j] = *reinterpret_cast<const uint32_t*>(&hh);
           }
-          const __half2 hh = __floats2half2_rn(x, y);
-          o[j] = *reinterpret_cast<const uint32_t*>(&hh);
-        }
-        if (lane == 0) bulk_wait_read<1>();  // the stores that used this buffer two chunks ago have read it
-        __syncwarp();
-        uint8_t* t_straight = stage_mem + buf * 2 * kTile16;
-        uint8_t* t_mirror = t_straight + kTile16;
-        uint4* ts = reinterpret_cast<uint4*>(t_straight);  // rows of 64 bytes, 16-byte pieces in the 64-byte swizzle
-#pragma unroll
-        for (int j = 0; j < 4; ++j) ts[lane * 4 + (j ^ ((lane >> 1) & 3))] = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
-        if (mirror) {  // element (row, col) to line col of the transposed tile
-#pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            const uint16_t v16 = static_cast<uint16_t>(o[j / 2] >> (16 * (j & 1)));
-            *reinterpret_cast<uint16_t*>(t_mirror + j * 64 + (((lane >> 3) ^ ((j >> 1) & 3)) << 4) + (lane & 7) * 2) = v16;
+          if (c < n_chunks && row < p.S) {  // (rows are padded to whole chunks)
+            st_bytes<32>(reinterpret_cast<char*>(yrow + c * 32), o);
+            st_bytes<32>(reinterpret_cast<char*>(yrow + c * 32 + 16), o + 8);
           }
-        }
-        fence_async_smem();
-        __syncwarp();
-        if (lane == 0) {
-          if (row0 < p.S) tma_store_3d(&map_y, smem_u32(t_straight), col0 * 2, row0, b);
-          if (mirror && row0 < p.S) tma_store_3d(&map_y, smem_u32(t_mirror), row0 * 2, col0, b);
-          bulk_commit();
-        }
-        buf ^= 1u;
-      }
-      if (n_chunks == 0) {
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) {
-          if constexpr (NCTA == 1) mbar_arrive(acc_empty + 8 * acc);
-          else mbar_arrive_cluster(map_to_cta(acc_empty + 8 * acc, 0u));
         }
       }
       if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
     }
-    if (lane == 0) bulk_wait_all();
   }
   if (timed_out) atomicOr(p.status, static_cast<uint32_t>(SCALIFY_DEV_TIMEOUT));
   tc_fence_before();
@@ -316,6 +323,8 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_product_kernel(const __grid_
 
 // ------------------------------------------------------------------------------------------------- element-wise passes
 namespace {
+
+template <int V> struct IntC { static constexpr int value = V; };
 
 struct MuonTable {
   MuonTensor t[kMaxInst];
@@ -361,28 +370,26 @@ __device__ __forceinline__ MuonFactors muon_factors(const MuonTensor& t, const M
   return f;
 }
 
-// u_d of one vector (and m'_d): u is the momentum, or its Nesterov form, in units of m'_s
-__device__ __forceinline__ void muon_vec(const MuonTensor& t, const MuonPass& p, const MuonFactors& f, int64_t row, int v, int n,
-                                         float* u, float* m) {
+// Words of one vector of a matrix (MDT < 0: no momentum), and u_d (and m'_d) from them: u is the momentum, or its Nesterov form, in units of m'_s
+template <int GDT, int MDT>
+struct MuonWords {
+  uint32_t g[kVec * ElemBytes<GDT>::v / 4], m[kVec * (MDT < 0 ? 4 : ElemBytes<MDT < 0 ? 4 : MDT>::v) / 4];
+};
+template <int GDT, int MDT>
+__device__ __forceinline__ void muon_load(const MuonTensor& t, int64_t row, int v, int n, MuonWords<GDT, MDT>& w) {
+  load_vec<GDT>(static_cast<const char*>(t.g) + row * t.g_ld * ElemBytes<GDT>::v, v, n, w.g);
+  if constexpr (MDT >= 0) load_vec<MDT>(static_cast<const char*>(t.m) + row * t.m_ld * ElemBytes<MDT>::v, v, n, w.m);
+}
+template <int GDT, int MDT>
+__device__ __forceinline__ void muon_vec(const MuonWords<GDT, MDT>& w, const MuonPass& p, const MuonFactors& f, float* u, float* m) {
   float g[kVec];
-  SCALIFY_DISPATCH_DTYPE(t.g_dt, DT, {
-    uint32_t w[kVec * ElemBytes<DT>::v / 4];
-    load_vec<DT>(static_cast<const char*>(t.g) + row * t.g_ld * ElemBytes<DT>::v, v, n, w);
-    decode_vec<DT, kVec>(w, g);
-  })
-  if (!t.m) {
+  decode_vec<GDT, kVec>(w.g, g);
+  if constexpr (MDT < 0) {
 #pragma unroll
     for (int e = 0; e < kVec; ++e) u[e] = g[e];
     return;
-  }
-  if (t.m_dt == SCALIFY_F16) {
-    uint32_t w[4];
-    load_vec<SCALIFY_F16>(static_cast<const char*>(t.m) + row * t.m_ld * 2, v, n, w);
-    decode_vec<SCALIFY_F16, kVec>(w, m);
   } else {
-    uint32_t w[8];
-    load_vec<SCALIFY_F32>(static_cast<const char*>(t.m) + row * t.m_ld * 4, v, n, w);
-    decode_vec<SCALIFY_F32, kVec>(w, m);
+    decode_vec<MDT, kVec>(w.m, m);
   }
 #pragma unroll
   for (int e = 0; e < kVec; ++e) {
@@ -395,6 +402,7 @@ __device__ __forceinline__ void muon_vec(const MuonTensor& t, const MuonPass& p,
 }  // namespace
 
 // |u|_F^2, one partial per block (fixed order within and between blocks), and the step's factors.
+template <int GDT, int MDT>
 __global__ void __launch_bounds__(256) muon_norm_kernel(const __grid_constant__ MuonTable tab, const MuonPass p) {
   asm volatile("griddepcontrol.launch_dependents;");  // a programmatic dependent may set up while this grid runs
   __shared__ double s_sum[8];
@@ -408,14 +416,24 @@ __global__ void __launch_bounds__(256) muon_norm_kernel(const __grid_constant__ 
   }
   const uint32_t nv = (t.cols + kVec - 1) / kVec, total = nv * static_cast<uint32_t>(t.rows);
   double sum = 0.0;
-  for (uint32_t i = blockIdx.x * 256u + threadIdx.x; i < total; i += gridDim.x * 256u) {
-    const uint32_t row = i / nv;
-    const int v = static_cast<int>(i - row * nv);
-    float u[kVec], m[kVec], ss = 0.f;
-    muon_vec(t, p, f, row, v, t.cols - v * kVec, u, m);
+  constexpr int kAhead = 4;  // vectors in flight per thread
+  for (uint32_t i0 = blockIdx.x * 256u * kAhead + threadIdx.x; i0 < total; i0 += gridDim.x * 256u * kAhead) {
+    MuonWords<GDT, MDT> w[kAhead];
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) ss = fmaf(u[e], u[e], ss);
-    sum += ss;
+    for (int k = 0; k < kAhead; ++k) {
+      const uint32_t i = i0 + k * 256u, row = i / nv;
+      const int v = static_cast<int>(i - row * nv);
+      if (i < total) muon_load<GDT, MDT>(t, row, v, t.cols - v * kVec, w[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (i0 + k * 256u >= total) break;
+      float u[kVec], m[kVec], ss = 0.f;
+      muon_vec<GDT, MDT>(w[k], p, f, u, m);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) ss = fmaf(u[e], u[e], ss);
+      sum += ss;
+    }
   }
   sum = warp_sum_f64(sum);
   if ((threadIdx.x & 31) == 0) s_sum[threadIdx.x >> 5] = sum;
@@ -429,6 +447,7 @@ __global__ void __launch_bounds__(256) muon_norm_kernel(const __grid_constant__ 
 
 // m' (stored once rounded) and Z_0 = u / (|u| + eps) / sigma in FP16, [S, L]; a 64 x 64 tile per block, turned over in shared
 // memory where the matrix is tall.  The new scale words are written here (nothing of this launch reads the old ones).
+template <int GDT, int MDT>
 __global__ void __launch_bounds__(256) muon_momentum_kernel(const __grid_constant__ MuonTable tab, const MuonPass p) {
   asm volatile("griddepcontrol.launch_dependents;");  // a programmatic dependent may set up while this grid runs
   __shared__ __align__(16) __half s_tile[kPreTile][kPreTile + 8];
@@ -452,6 +471,12 @@ __global__ void __launch_bounds__(256) muon_momentum_kernel(const __grid_constan
     }
   }
   const MuonFactors f = p.factors[inst];
+  MuonWords<GDT, MDT> w[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int i = threadIdx.x + k * 256, row = r0 + (i >> 3), col = c0 + (i & 7) * kVec;
+    if (row < t.rows && col < t.cols) muon_load<GDT, MDT>(t, row, col / kVec, t.cols - col, w[k]);
+  }
   __syncthreads();
   const float scale = s_scale;
   __half* Z = p.Z + static_cast<long long>(inst) * p.S * p.ld;
@@ -461,11 +486,8 @@ __global__ void __launch_bounds__(256) muon_momentum_kernel(const __grid_constan
     const int row = r0 + lr, col = c0 + lv * kVec, n = t.cols - col;
     if (row < t.rows && n > 0) {
       float u[kVec], m[kVec];
-      muon_vec(t, p, f, row, col / kVec, n, u, m);
-      if (t.m) {
-        if (t.m_dt == SCALIFY_F16) store_vec<SCALIFY_F16>(static_cast<char*>(t.m) + static_cast<int64_t>(row) * t.m_ld * 2, col / kVec, n, m);
-        else store_vec<SCALIFY_F32>(static_cast<char*>(t.m) + static_cast<int64_t>(row) * t.m_ld * 4, col / kVec, n, m);
-      }
+      muon_vec<GDT, MDT>(w[k], p, f, u, m);
+      if constexpr (MDT >= 0) store_vec<MDT>(static_cast<char*>(t.m) + static_cast<int64_t>(row) * t.m_ld * ElemBytes<MDT>::v, col / kVec, n, m);
 #pragma unroll
       for (int e = 0; e < kVec; ++e) u[e] *= scale;
       if (!tall) {  // (rows of Z are padded to whole vectors)
@@ -550,7 +572,7 @@ __global__ void __launch_bounds__(256) muon_update_kernel(const __grid_constant_
 
 // ------------------------------------------------------------------------------------------------- launches
 template <int MODE, int NCTA>
-static int launch_product_variant(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& y, const NsParams& p, cudaStream_t st) {
+static int launch_product_variant(const CUtensorMap (&m)[4], const NsParams& p, cudaStream_t st) {
   using C = NsCfg<NCTA>;
   auto kernel = ns_product_kernel<MODE, NCTA>;
   static DeviceOnce once;
@@ -580,7 +602,7 @@ static int launch_product_variant(const CUtensorMap& a, const CUtensorMap& b, co
   cfg.gridDim = dim3(static_cast<unsigned>((tiles < most ? tiles : most) * NCTA));
   cfg.blockDim = dim3(kNsThreads); cfg.dynamicSmemBytes = C::kSmem; cfg.stream = st;
   cfg.attrs = attrs; cfg.numAttrs = NCTA == 2 ? 2 : 1;
-  SCALIFY_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, a, b, y, p));
+  SCALIFY_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, m[0], m[1], m[2], m[3], p));
   return SCALIFY_OK;
 }
 
@@ -594,19 +616,21 @@ static int launch_product(const NsMatrix& A, const NsMatrix& B, const NsMatrix& 
     return make_byte_map(m, x.p, static_cast<uint64_t>(x.cols) * 2, x.rows, p.batch, x.ld * 2, static_cast<uint64_t>(x.rows) * x.ld * 2,
                          box_bytes, box_rows);
   };
-  CUtensorMap ma, mb, my;
-  int rc = map(&ma, A, 128, kTM);
-  if (!rc) rc = map(&mb, B, 128, MODE == kUpdate ? kTK : kTN / ncta);
-  if (!rc) rc = map(&my, Y, 64, 32);
+  CUtensorMap m[4];  // both operands with the contraction along their lines, and MN-major
+  int rc = map(&m[0], A, 128, kTM);
+  if (!rc) rc = map(&m[1], B, 128, kTN / ncta);
+  if (!rc) rc = map(&m[2], A, 128, kTK);
+  if (!rc) rc = map(&m[3], B, 128, kTK);
   if (rc) return rc;
   p.S = Y.rows; p.N = Y.cols; p.K = A.cols;
+  p.Y = Y.p; p.ldy = Y.ld;
   p.tiles_m = (Y.rows + tile_m - 1) / tile_m;
   p.tiles_n = (Y.cols + kTN - 1) / kTN;
   // symmetric products: the tile is square for CTA pairs; a single CTA's tile holds the whole matrix (S <= 128)
   p.tiles = MODE == kUpdate ? p.tiles_m * p.tiles_n : p.tiles_n * (p.tiles_n + 1) / 2;
-  p.idesc = (1u << 4) | (uint32_t(MODE == kUpdate) << 16) | (uint32_t(kTN >> 3) << 17) | (uint32_t(tile_m >> 4) << 24);
-  if (ncta == 2) return launch_product_variant<MODE, 2>(ma, mb, my, p, st);
-  return launch_product_variant<MODE, 1>(ma, mb, my, p, st);
+  p.idesc = (1u << 4) | (uint32_t(kTN >> 3) << 17) | (uint32_t(tile_m >> 4) << 24);
+  if (ncta == 2) return launch_product_variant<MODE, 2>(m, p, st);
+  return launch_product_variant<MODE, 1>(m, p, st);
 }
 
 static long long pad64(long long n) { return (n + 63) / 64 * 64; }
@@ -696,11 +720,17 @@ static int run_batch(const MuonTable& tab, int count, const MuonHyper& h, void* 
     p.p2_lr[tall] = p.lr[tall] > 0.f ? host_p2(p.lr[tall]) : 0.f;
   }
 
-  muon_norm_kernel<<<dim3(p.parts, count), 256, 0, st>>>(tab, p);
-  SCALIFY_CUDA_TRY(cudaGetLastError());
   const unsigned tl = static_cast<unsigned>((s.L + kPreTile - 1) / kPreTile), ts = static_cast<unsigned>((s.S + kPreTile - 1) / kPreTile);
   const dim3 tiles(tl * ts, 1, count);
-  muon_momentum_kernel<<<tiles, 256, 0, st>>>(tab, p);
+  auto enter = [&](auto g_dt, auto m_dt) {
+    muon_norm_kernel<decltype(g_dt)::value, decltype(m_dt)::value><<<dim3(p.parts, count), 256, 0, st>>>(tab, p);
+    muon_momentum_kernel<decltype(g_dt)::value, decltype(m_dt)::value><<<tiles, 256, 0, st>>>(tab, p);
+  };
+  SCALIFY_DISPATCH_DTYPE(tab.t[0].g_dt, GDT, {
+    if (!tab.t[0].m) enter(IntC<GDT>{}, IntC<-1>{});
+    else if (tab.t[0].m_dt == SCALIFY_F16) enter(IntC<GDT>{}, IntC<SCALIFY_F16>{});
+    else enter(IntC<GDT>{}, IntC<SCALIFY_F32>{});
+  })
   SCALIFY_CUDA_TRY(cudaGetLastError());
 
   NsParams np = {};
@@ -716,7 +746,6 @@ static int run_batch(const MuonTable& tab, int count, const MuonHyper& h, void* 
     q.b = h.b;
     q.diag = h.a * kGramScale;
     q.A = A.p;
-    q.ld = lda;
     rc = launch_product<kPoly>(A, A, D, q, st);
     if (rc) return rc;
     q = np;
