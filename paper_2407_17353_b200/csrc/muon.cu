@@ -16,7 +16,7 @@
 // Where a product needs a block of A or D below the diagonal it reads the block's mirror image as an MN-major operand:
 // the layout is a matter of each K block's copies and descriptors, and no tile is stored twice.
 // Bound: the tensor pipe for large batches (S S L + S S S + 2 S S L flops a step); for few or small matrices the latency of
-// the chain of 3 `steps` products.
+// the chain of 3 `steps` products, which then runs as ONE launch (ns_chain_kernel).
 #include <cuda.h>
 #include <math.h>
 
@@ -43,6 +43,7 @@ constexpr int kMaxParts = 256;    // partial sums of a matrix's norm
 constexpr int kPreTile = 64;      // rows and columns of a tile of the element-wise passes
 
 enum { kGram = 0, kPoly = 1, kUpdate = 2 };
+template <int K> struct KindC { static constexpr int value = K; };
 
 // Two CTAs (an SM pair) share a 256 x 256 tile; one CTA alone takes 128 x 256 where S fits 128 rows.
 template <int NCTA> struct NsCfg {
@@ -51,18 +52,19 @@ template <int NCTA> struct NsCfg {
   static constexpr int kABytes = kTM * 128;
   static constexpr int kBBytes = kBRows * 128;
   static constexpr int kStages = NCTA == 1 ? 4 : 6;
-  static constexpr size_t kSmem = size_t(kStages) * (kABytes + kBBytes) + 1024 + 256;
+  static constexpr uint32_t kRing = kStages * (kABytes + kBBytes);
+  static constexpr size_t kSmem = size_t(kRing) + 1024 + 256;
 };
 
-struct NsParams {
-  int S, N, K, batch;        // output [S, N], contraction K
-  int tiles_m, tiles_n, tiles;  // tiles of one matrix (symmetric: on and above the diagonal)
-  uint32_t idesc;
-  float alpha, b, diag;      // out = alpha acc (+ b A_d[r, c] + diag [r == c])
+// One product: Y = alpha A B^T (gram, poly) or alpha A B (update), of every matrix of the batch.
+struct NsProduct {
+  int S, N, K;               // output [S, N], contraction K
+  int tiles_m, tiles_n;
+  int tiles;                 // tiles of one matrix (symmetric: on and above the diagonal)
+  float alpha, b, diag;      // out = alpha acc (poly: + b A_d[r, c] + diag [r == c])
   __half* Y;                 // [batch][S][ldy]
   long long ldy;
   const __half* A;           // poly: A_d, laid out like Y
-  uint32_t* status;
 };
 
 __device__ __forceinline__ void umma_f16(uint32_t d_tmem, uint64_t ad, uint64_t bd, uint32_t idesc, uint32_t acc) {
@@ -76,11 +78,9 @@ __device__ __forceinline__ void umma_f16_pair(uint32_t d_tmem, uint64_t ad, uint
       "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem), "l"(ad), "l"(bd), "r"(idesc), "r"(acc) : "memory");
 }
 
-// tile index -> matrix, tile row and column (symmetric products: row by row of the upper triangle)
+// tile of a matrix -> tile row and column (symmetric products: row by row of the upper triangle)
 template <int MODE>
-__device__ __forceinline__ void ns_tile(const NsParams& p, int tile, int& b, int& mt, int& nt) {
-  b = tile / p.tiles;
-  int t = tile - b * p.tiles;
+__device__ __forceinline__ void ns_tile(const NsProduct& p, int t, int& mt, int& nt) {
   if constexpr (MODE == kUpdate) {
     nt = t / p.tiles_m;
     mt = t - nt * p.tiles_m;
@@ -98,41 +98,240 @@ template <int MODE> __device__ __forceinline__ bool b_transposed(int kb, int rt)
   return MODE == kUpdate || (MODE == kPoly && kb / (kTN / kTK) < rt);
 }
 
+// What a CTA's three roles share: shared memory, barriers, and each role's place in the ring.
+// Warp 0: TMA producer; warp 1: MMA issuer; warps 2-9: epilogue.  Every wait is bounded.
+template <int NCTA>
+struct NsEngine {
+  using C = NsCfg<NCTA>;
+  uint32_t smem_a, smem_b, full_bar, empty_bar, acc_full, acc_empty, drain_bar, tmem_base;
+  volatile uint32_t* tmem_slot;
+  volatile uint32_t* abort_flag;
+  uint32_t rank, leader;       // this CTA in its pair; the pair's leader in the cluster
+  int warp, lane;
+  uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
+  long long issued = 0;
+
+  __device__ __forceinline__ void set_up(uint8_t* smem_raw) {
+    const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+    uint8_t* bar_mem = smem_raw + (base - raw) + C::kRing;
+    smem_a = base;
+    smem_b = base + C::kStages * C::kABytes;
+    const uint32_t bars = base + C::kRing;
+    full_bar = bars;
+    empty_bar = bars + 8 * C::kStages;
+    acc_full = bars + 16 * C::kStages;
+    acc_empty = acc_full + 8 * kAccs;
+    drain_bar = acc_empty + 8 * kAccs;
+    tmem_slot = reinterpret_cast<volatile uint32_t*>(bar_mem + 16 * C::kStages + 16 * kAccs + 8);
+    abort_flag = tmem_slot + 1;
+    warp = threadIdx.x >> 5;
+    lane = threadIdx.x & 31;
+    const uint32_t r = NCTA == 2 ? cluster_ctarank() : 0u;
+    rank = r & 1u;
+    leader = r & ~1u;
+    if (threadIdx.x == 0) {
+      for (int s = 0; s < C::kStages; ++s) { mbar_init(full_bar + 8 * s, 1); mbar_init(empty_bar + 8 * s, 1); }
+      for (int s = 0; s < kAccs; ++s) { mbar_init(acc_full + 8 * s, 1); mbar_init(acc_empty + 8 * s, kEpiWarpsM * NCTA); }
+      mbar_init(drain_bar, 1);
+      *abort_flag = 0u;
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), kAccs * kTN);
+    tc_fence_before();
+  }
+  __device__ __forceinline__ void tear_down() {
+    if (warp == 1) {
+      tc_fence_after();
+      tmem_dealloc(tmem_base, kAccs * kTN);
+    }
+  }
+  // commit of the MMAs issued so far to a barrier of both CTAs of the pair
+  __device__ __forceinline__ void commit(uint32_t bar) {
+    if constexpr (NCTA == 1) {
+      umma_commit(bar);
+    } else {
+      const uint16_t mask = static_cast<uint16_t>(3u << leader);
+      asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"(mask) : "memory");
+    }
+  }
+
+  // ---- warp 0, lane 0: the operand blocks of one tile
+  template <int MODE>
+  __device__ __forceinline__ bool produce(const NsProduct& p, const CUtensorMap* map_a, const CUtensorMap* map_b,
+                                          const CUtensorMap* map_at, const CUtensorMap* map_bt, int b, int tile) {
+    int mt, nt;
+    ns_tile<MODE>(p, tile, mt, nt);
+    const int num_kb = (p.K + kTK - 1) / kTK;
+    const int m0 = mt * C::kTileM + static_cast<int>(rank) * kTM;
+    const int n0 = nt * kTN + static_cast<int>(rank) * C::kBRows * (NCTA - 1);
+    for (int kb = 0; kb < num_kb; ++kb) {
+      if (!mbar_wait(empty_bar + 8 * stage, phase ^ 1u, abort_flag)) return false;
+      const uint32_t sa = smem_a + stage * C::kABytes, sb = smem_b + stage * C::kBBytes;
+      uint32_t fb = full_bar + 8 * stage;
+      const bool a_mn = a_transposed<MODE>(kb, mt), b_mn = b_transposed<MODE>(kb, nt);
+      if constexpr (NCTA == 2) {
+        if (rank == 0u) mbar_expect_tx(fb, 2 * (C::kABytes + C::kBBytes));
+        fb = map_to_cta(fb, leader);  // both CTAs' copies are counted on the leader's barrier
+      } else {
+        mbar_expect_tx(fb, C::kABytes + C::kBBytes);
+      }
+      auto load = [&](uint32_t dst, const CUtensorMap* m, int x, int y) {
+        if constexpr (NCTA == 2) tma_load_3d_pair(dst, m, fb, x * 2, y, b);  // (the maps count bytes)
+        else tma_load_3d(dst, m, fb, x * 2, y, b);
+      };
+      // along K: one box of 64 elements x all rows; MN-major: boxes of 64 columns x the 64 lines of this K block
+      if (!a_mn) {
+        load(sa, map_a, kb * kTK, m0);
+      } else {
+#pragma unroll
+        for (int j = 0; j < kTM / kTK; ++j) load(sa + j * kTK * 128, map_at, m0 + j * kTK, kb * kTK);
+      }
+      if (!b_mn) {
+        load(sb, map_b, kb * kTK, n0);
+      } else {
+#pragma unroll
+        for (int j = 0; j < C::kBRows / kTK; ++j) load(sb + j * kTK * 128, map_bt, n0 + j * kTK, kb * kTK);
+      }
+      ++issued;
+      if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
+    }
+    return true;
+  }
+  // after a timeout: wait (bounded) for the last use of every ring slot, so that no copy is in flight when the CTA exits
+  __device__ __forceinline__ void drain_copies() {
+    if (rank != 0u) return;
+    const int pending = issued < C::kStages ? static_cast<int>(issued) : C::kStages;
+    uint32_t s = stage, ph = phase;
+    for (int i = 0; i < pending; ++i) {
+      if (s == 0) { s = C::kStages - 1; ph ^= 1u; } else { --s; }
+      const unsigned long long t0 = global_timer_ns();
+      while (!mbar_try_wait(full_bar + 8 * s, ph) && global_timer_ns() - t0 < kWaitLimitNs) {}
+    }
+  }
+
+  // ---- warp 1, lane 0 of the leader: the MMAs of one tile
+  template <int MODE>
+  __device__ __forceinline__ bool multiply(const NsProduct& p, int tile) {
+    // MN-major: atoms of 64 columns x 8 lines of K; along K they are 1024 bytes apart, the next 64 columns a box
+    // (64 x 128 bytes) further on
+    const uint64_t a_desc_k = make_smem_desc(smem_a, 0u, 1024u), a_desc_mn = make_smem_desc(smem_a, kTK * 128u, 1024u);
+    const uint64_t b_desc_k = make_smem_desc(smem_b, 0u, 1024u), b_desc_mn = make_smem_desc(smem_b, kTK * 128u, 1024u);
+    constexpr uint32_t k_inc = kStepK * 2 >> 4, mn_inc = kStepK * 128 >> 4;
+    constexpr uint32_t idesc0 = (1u << 4) | (uint32_t(kTN >> 3) << 17) | (uint32_t(C::kTileM >> 4) << 24);  // F16 x F16 -> fp32
+    int mt, nt;
+    ns_tile<MODE>(p, tile, mt, nt);
+    const int num_kb = (p.K + kTK - 1) / kTK;
+    if (!mbar_wait(acc_empty + 8 * acc, acc_phase ^ 1u, abort_flag)) return false;
+    tc_fence_after();
+    const uint32_t d_tmem = tmem_base + acc * kTN;
+    for (int kb = 0; kb < num_kb; ++kb) {
+      const bool a_mn = a_transposed<MODE>(kb, mt), b_mn = b_transposed<MODE>(kb, nt);
+      const uint32_t idesc = idesc0 | (uint32_t(a_mn) << 15) | (uint32_t(b_mn) << 16);
+      const uint32_t a_inc = a_mn ? mn_inc : k_inc, b_inc = b_mn ? mn_inc : k_inc;
+      const uint64_t ad0 = (a_mn ? a_desc_mn : a_desc_k) + static_cast<uint64_t>(stage * (C::kABytes >> 4));
+      const uint64_t bd0 = (b_mn ? b_desc_mn : b_desc_k) + static_cast<uint64_t>(stage * (C::kBBytes >> 4));
+      if (!mbar_wait(full_bar + 8 * stage, phase, abort_flag)) return false;
+      tc_fence_after();
+#pragma unroll
+      for (int k = 0; k < kTK / kStepK; ++k) {
+        if constexpr (NCTA == 1) umma_f16(d_tmem, ad0 + k * a_inc, bd0 + k * b_inc, idesc, (kb | k) != 0 ? 1u : 0u);
+        else umma_f16_pair(d_tmem, ad0 + k * a_inc, bd0 + k * b_inc, idesc, (kb | k) != 0 ? 1u : 0u);
+      }
+      commit(empty_bar + 8 * stage);  // the slot is free (in both CTAs) once these MMAs have read it
+      if (++stage == C::kStages) { stage = 0; phase ^= 1u; }
+    }
+    commit(acc_full + 8 * acc);
+    if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
+    return true;
+  }
+  // after a timeout: all MMAs issued so far must retire before the tensor memory is freed
+  __device__ __forceinline__ void drain_multiplies() {
+    commit(drain_bar);
+    const unsigned long long t0 = global_timer_ns();
+    while (!mbar_try_wait(drain_bar, 0u) && global_timer_ns() - t0 < kWaitLimitNs) {}
+  }
+
+  // ---- warps 2-9: accumulator -> memory.  Results go there from registers: a lane holds 32 columns of one row, two
+  // 32-byte stores.  (Staging them for the store engine in shared memory costs what the MMAs and the operand copies leave
+  // none of: its bandwidth.)
+  template <int MODE>
+  __device__ __forceinline__ bool finish(const NsProduct& p, int b, int tile) {
+    const int q = warp & 3, half = (warp - 2) / 4;  // TMEM lane quarter, half of the tile's columns
+    constexpr int kChunks = kTN / 64;               // 32-column chunks per warp
+    int mt, nt;
+    ns_tile<MODE>(p, tile, mt, nt);
+    const int c_first = half * kChunks, n0 = nt * kTN;
+    const int n_chunks = max(0, min(kChunks, (p.N - n0 + 31) / 32 - c_first));  // chunks inside the matrix
+    const int row = mt * C::kTileM + static_cast<int>(rank) * kTM + q * 32 + lane;
+    __half* yrow = p.Y + (static_cast<long long>(b) * p.S + row) * p.ldy + n0 + c_first * 32;
+    // poly: this lane's row of A, read while the products run (past the L1: it may hold an earlier step's A)
+    uint4 wa[MODE == kPoly ? kChunks : 1][4];
+    if constexpr (MODE == kPoly) {
+      const __half* arow = p.A + (static_cast<long long>(b) * p.S + min(row, p.S - 1)) * p.ldy + n0 + c_first * 32;
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          wa[c][j] = c < n_chunks ? __ldcg(reinterpret_cast<const uint4*>(arow + c * 32 + 8 * j)) : make_uint4(0u, 0u, 0u, 0u);
+    }
+    if (!mbar_wait(acc_full + 8 * acc, acc_phase, abort_flag)) return false;
+    tc_fence_after();
+    const uint32_t t_addr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * kTN + c_first * 32;
+#pragma unroll
+    for (int c2 = 0; c2 < kChunks; c2 += 2) {
+      uint32_t r[2][32];
+      tmem_ld32(t_addr + c2 * 32, r[0]);  // (columns past the matrix hold nothing of interest)
+      tmem_ld32(t_addr + (c2 + 1) * 32, r[1]);
+      tmem_ld_wait();
+      if (c2 + 2 == kChunks) {  // the accumulator has been read: the next tile may overwrite it
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if constexpr (NCTA == 1) mbar_arrive(acc_empty + 8 * acc);
+          else mbar_arrive_cluster(map_to_cta(acc_empty + 8 * acc, leader));
+        }
+      }
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const int c = c2 + s, col0 = n0 + (c_first + c) * 32;
+        uint32_t o[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          float x = __uint_as_float(r[s][2 * j]) * p.alpha, y = __uint_as_float(r[s][2 * j + 1]) * p.alpha;
+          if constexpr (MODE == kPoly) {
+            const uint4 w4 = wa[c][j / 4];
+            const uint32_t w = (j & 3) == 0 ? w4.x : (j & 3) == 1 ? w4.y : (j & 3) == 2 ? w4.z : w4.w;
+            const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w));
+            x = fmaf(p.b, v.x, x) + (row == col0 + 2 * j ? p.diag : 0.f);
+            y = fmaf(p.b, v.y, y) + (row == col0 + 2 * j + 1 ? p.diag : 0.f);
+          }
+          const __half2 hh = __floats2half2_rn(x, y);
+          o[j] = *reinterpret_cast<const uint32_t*>(&hh);
+        }
+        if (c < n_chunks && row < p.S) {  // (rows are padded to whole chunks)
+          st_bytes<32>(reinterpret_cast<char*>(yrow + c * 32), o);
+          st_bytes<32>(reinterpret_cast<char*>(yrow + c * 32 + 16), o + 8);
+        }
+      }
+    }
+    if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
+    return true;
+  }
+};
+
 }  // namespace
 
-// Warp 0: TMA producer; warp 1: MMA issuer; warps 2-9: epilogue.  Persistent CTAs (pairs).  Every wait is bounded; on
-// expiry the CTA records SCALIFY_DEV_TIMEOUT, drains its copies and MMAs, frees its tensor memory and returns.
+// One product of the whole batch: persistent CTAs (pairs).  On expiry of a wait the CTA records SCALIFY_DEV_TIMEOUT, drains
+// its copies and MMAs, frees its tensor memory and returns.
 template <int MODE, int NCTA>
 __global__ void __launch_bounds__(kNsThreads, 1) ns_product_kernel(const __grid_constant__ CUtensorMap map_a,
                                                                   const __grid_constant__ CUtensorMap map_b,
                                                                   const __grid_constant__ CUtensorMap map_at,
-                                                                  const __grid_constant__ CUtensorMap map_bt, const NsParams p) {
-  using C = NsCfg<NCTA>;
-  constexpr int kStages = C::kStages;
+                                                                  const __grid_constant__ CUtensorMap map_bt, const NsProduct p, int batch,
+                                                                  uint32_t* status) {
   asm volatile("griddepcontrol.launch_dependents;");  // the next product may set up while this one runs
   extern __shared__ uint8_t smem_raw[];
-  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-  uint8_t* smem = smem_raw + (base - raw);
-  const uint32_t smem_a = base, smem_b = base + kStages * C::kABytes;
-  constexpr uint32_t kRing = kStages * (C::kABytes + C::kBBytes);
-  uint8_t* bar_mem = smem + kRing;
-  const uint32_t bars = base + kRing;
-  const uint32_t full_bar = bars, empty_bar = bars + 8 * kStages, acc_full = bars + 16 * kStages, acc_empty = acc_full + 8 * kAccs,
-                 drain_bar = acc_empty + 8 * kAccs;
-  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(bar_mem + 16 * kStages + 16 * kAccs + 8);
-  volatile uint32_t* abort_flag = tmem_slot + 1;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t rank = NCTA == 2 ? cluster_ctarank() : 0u;
-  const int unit = blockIdx.x / NCTA, num_units = gridDim.x / NCTA;
-  const int num_kb = (p.K + kTK - 1) / kTK, num_tiles = p.tiles * p.batch;
-
-  if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) { mbar_init(full_bar + 8 * s, 1); mbar_init(empty_bar + 8 * s, 1); }
-    for (int s = 0; s < kAccs; ++s) { mbar_init(acc_full + 8 * s, 1); mbar_init(acc_empty + 8 * s, kEpiWarpsM * NCTA); }
-    mbar_init(drain_bar, 1);
-    *abort_flag = 0u;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
+  NsEngine<NCTA> e;
   if (threadIdx.x == 32 * 2) {  // (the maps are arguments: nothing the kernel before writes)
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_a)) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_b)) : "memory");
@@ -141,184 +340,94 @@ __global__ void __launch_bounds__(kNsThreads, 1) ns_product_kernel(const __grid_
       asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_bt)) : "memory");
     }
   }
-  if (warp == 1) tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), kAccs * kTN);
-  tc_fence_before();
+  e.set_up(smem_raw);
   __syncthreads();
   if constexpr (NCTA == 2) cluster_sync_all();
   tc_fence_after();
-  asm volatile("griddepcontrol.wait;" ::: "memory");  // nothing above touches global memory
-  const uint32_t tmem_base = *tmem_slot;
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // nothing above touches what the kernel before writes
+  e.tmem_base = *e.tmem_slot;
+  const int unit = blockIdx.x / NCTA, num_units = gridDim.x / NCTA, num_tiles = p.tiles * batch;
   bool timed_out = false;
-
-  if (warp == 0) {
-    if (lane == 0) {
-      uint32_t stage = 0, phase = 0;
-      long long issued = 0;
-      for (int tile = unit; tile < num_tiles && !timed_out; tile += num_units) {
-        int b, mt, nt;
-        ns_tile<MODE>(p, tile, b, mt, nt);
-        const int m0 = mt * C::kTileM + static_cast<int>(rank) * kTM;
-        const int n0 = nt * kTN + static_cast<int>(rank) * C::kBRows * (NCTA - 1);
-        for (int kb = 0; kb < num_kb; ++kb) {
-          if (!mbar_wait(empty_bar + 8 * stage, phase ^ 1u, abort_flag)) { timed_out = true; break; }
-          const uint32_t sa = smem_a + stage * C::kABytes, sb = smem_b + stage * C::kBBytes;
-          uint32_t fb = full_bar + 8 * stage;
-          const bool a_mn = a_transposed<MODE>(kb, mt), b_mn = b_transposed<MODE>(kb, nt);
-          if constexpr (NCTA == 2) {
-            if (rank == 0u) mbar_expect_tx(fb, 2 * (C::kABytes + C::kBBytes));
-            fb = map_to_cta(fb, 0u);  // both CTAs' copies are counted on the leader's barrier
-          } else {
-            mbar_expect_tx(fb, C::kABytes + C::kBBytes);
-          }
-          auto load = [&](uint32_t dst, const CUtensorMap* m, int x, int y) {
-            if constexpr (NCTA == 2) tma_load_3d_pair(dst, m, fb, x * 2, y, b);  // (the maps count bytes)
-            else tma_load_3d(dst, m, fb, x * 2, y, b);
-          };
-          // along K: one box of 64 elements x all rows; MN-major: boxes of 64 columns x the 64 lines of this K block
-          if (!a_mn) {
-            load(sa, &map_a, kb * kTK, m0);
-          } else {
-#pragma unroll
-            for (int j = 0; j < kTM / kTK; ++j) load(sa + j * kTK * 128, &map_at, m0 + j * kTK, kb * kTK);
-          }
-          if (!b_mn) {
-            load(sb, &map_b, kb * kTK, n0);
-          } else {
-#pragma unroll
-            for (int j = 0; j < C::kBRows / kTK; ++j) load(sb + j * kTK * 128, &map_bt, n0 + j * kTK, kb * kTK);
-          }
-          ++issued;
-          if (++stage == kStages) { stage = 0; phase ^= 1u; }
-        }
-      }
-      if ((timed_out || *abort_flag) && rank == 0u) {
-        // wait (bounded) for the last use of every ring slot, so that no copy is in flight when the CTA (pair) exits
-        const int pending = issued < kStages ? static_cast<int>(issued) : kStages;
-        uint32_t s = stage, ph = phase;
-        for (int i = 0; i < pending; ++i) {
-          if (s == 0) { s = kStages - 1; ph ^= 1u; } else { --s; }
-          const unsigned long long t0 = global_timer_ns();
-          while (!mbar_try_wait(full_bar + 8 * s, ph) && global_timer_ns() - t0 < kWaitLimitNs) {}
-        }
-      }
+  if (e.warp == 0) {
+    if (e.lane == 0) {
+      for (int tile = unit; tile < num_tiles && !timed_out; tile += num_units)
+        timed_out = !e.template produce<MODE>(p, &map_a, &map_b, &map_at, &map_bt, tile / p.tiles, tile % p.tiles);
+      if (timed_out || *e.abort_flag) e.drain_copies();
     }
-  } else if (warp == 1) {
-    if (lane == 0 && rank == 0u) {
-      uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
-      // MN-major: atoms of 64 columns x 8 lines of K; along K they are 1024 bytes apart, the next 64 columns a box
-      // (64 x 128 bytes) further on
-      const uint64_t a_desc_k = make_smem_desc(smem_a, 0u, 1024u), a_desc_mn = make_smem_desc(smem_a, kTK * 128u, 1024u);
-      const uint64_t b_desc_k = make_smem_desc(smem_b, 0u, 1024u), b_desc_mn = make_smem_desc(smem_b, kTK * 128u, 1024u);
-      constexpr uint32_t k_inc = kStepK * 2 >> 4, mn_inc = kStepK * 128 >> 4;
-      for (int tile = unit; tile < num_tiles && !timed_out; tile += num_units) {
-        if (!mbar_wait(acc_empty + 8 * acc, acc_phase ^ 1u, abort_flag)) { timed_out = true; break; }
-        tc_fence_after();
-        const uint32_t d_tmem = tmem_base + acc * kTN;
-        int b, mt, nt;
-        ns_tile<MODE>(p, tile, b, mt, nt);
-        for (int kb = 0; kb < num_kb; ++kb) {
-          const bool a_mn = a_transposed<MODE>(kb, mt), b_mn = b_transposed<MODE>(kb, nt);
-          const uint32_t idesc = p.idesc | (uint32_t(a_mn) << 15) | (uint32_t(b_mn) << 16);
-          const uint32_t a_inc = a_mn ? mn_inc : k_inc, b_inc = b_mn ? mn_inc : k_inc;
-          const uint64_t ad0 = (a_mn ? a_desc_mn : a_desc_k) + static_cast<uint64_t>(stage * (C::kABytes >> 4));
-          const uint64_t bd0 = (b_mn ? b_desc_mn : b_desc_k) + static_cast<uint64_t>(stage * (C::kBBytes >> 4));
-          if (!mbar_wait(full_bar + 8 * stage, phase, abort_flag)) { timed_out = true; break; }
-          tc_fence_after();
-#pragma unroll
-          for (int k = 0; k < kTK / kStepK; ++k) {
-            if constexpr (NCTA == 1) umma_f16(d_tmem, ad0 + k * a_inc, bd0 + k * b_inc, idesc, (kb | k) != 0 ? 1u : 0u);
-            else umma_f16_pair(d_tmem, ad0 + k * a_inc, bd0 + k * b_inc, idesc, (kb | k) != 0 ? 1u : 0u);
-          }
-          if constexpr (NCTA == 1) umma_commit(empty_bar + 8 * stage);
-          else umma_commit_pair(empty_bar + 8 * stage);
-          if (++stage == kStages) { stage = 0; phase ^= 1u; }
-        }
-        if (timed_out) break;
-        if constexpr (NCTA == 1) umma_commit(acc_full + 8 * acc);
-        else umma_commit_pair(acc_full + 8 * acc);
-        if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
-      }
-      if (timed_out || *abort_flag) {
-        if constexpr (NCTA == 1) umma_commit(drain_bar);
-        else umma_commit_pair(drain_bar);
-        const unsigned long long t0 = global_timer_ns();
-        while (!mbar_try_wait(drain_bar, 0u) && global_timer_ns() - t0 < kWaitLimitNs) {}
-      }
+  } else if (e.warp == 1) {
+    if (e.lane == 0 && e.rank == 0u) {
+      for (int tile = unit; tile < num_tiles && !timed_out; tile += num_units) timed_out = !e.template multiply<MODE>(p, tile % p.tiles);
+      if (timed_out || *e.abort_flag) e.drain_multiplies();
     }
   } else {
-    const int q = warp & 3, half = (warp - 2) / 4;  // TMEM lane quarter, half of the tile's columns
-    constexpr int kChunks = kTN / 64;               // 32-column chunks per warp
-    // Results go from registers to memory: a lane holds 32 columns of one row, two 32-byte stores.  (Staging them for the
-    // store engine in shared memory costs what the MMAs and the operand copies leave none of: its bandwidth.)
-    uint32_t acc = 0, acc_phase = 0;
-    for (int tile = unit; tile < num_tiles; tile += num_units) {
-      int b, mt, nt;
-      ns_tile<MODE>(p, tile, b, mt, nt);
-      const int c_first = half * kChunks, n0 = nt * kTN;
-      const int n_chunks = max(0, min(kChunks, (p.N - n0 + 31) / 32 - c_first));  // chunks inside the matrix
-      const int row = mt * C::kTileM + static_cast<int>(rank) * kTM + q * 32 + lane;
-      __half* yrow = p.Y + (static_cast<long long>(b) * p.S + row) * p.ldy + n0 + c_first * 32;
-      // poly: this lane's row of A, read while the products run
-      uint4 wa[MODE == kPoly ? kChunks : 1][4];
-      if constexpr (MODE == kPoly) {
-        const __half* arow = p.A + (static_cast<long long>(b) * p.S + min(row, p.S - 1)) * p.ldy + n0 + c_first * 32;
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c)
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            wa[c][j] = c < n_chunks ? *reinterpret_cast<const uint4*>(arow + c * 32 + 8 * j) : make_uint4(0u, 0u, 0u, 0u);
-      }
-      if (!mbar_wait(acc_full + 8 * acc, acc_phase, abort_flag)) { timed_out = true; break; }
-      tc_fence_after();
-      const uint32_t t_addr = tmem_base + (static_cast<uint32_t>(q * 32) << 16) + acc * kTN + c_first * 32;
-#pragma unroll
-      for (int c2 = 0; c2 < kChunks; c2 += 2) {
-        uint32_t r[2][32];
-        tmem_ld32(t_addr + c2 * 32, r[0]);  // (columns past the matrix hold nothing of interest)
-        tmem_ld32(t_addr + (c2 + 1) * 32, r[1]);
-        tmem_ld_wait();
-        if (c2 + 2 == kChunks) {  // the accumulator has been read: the next tile may overwrite it
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) {
-            if constexpr (NCTA == 1) mbar_arrive(acc_empty + 8 * acc);
-            else mbar_arrive_cluster(map_to_cta(acc_empty + 8 * acc, 0u));
-          }
-        }
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const int c = c2 + s, col0 = n0 + (c_first + c) * 32;
-          uint32_t o[16];
-#pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            float x = __uint_as_float(r[s][2 * j]) * p.alpha, y = __uint_as_float(r[s][2 * j + 1]) * p.alpha;
-            if constexpr (MODE == kPoly) {
-              const uint4 w4 = wa[c][j / 4];
-              const uint32_t w = (j & 3) == 0 ? w4.x : (j & 3) == 1 ? w4.y : (j & 3) == 2 ? w4.z : w4.w;
-              const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w));
-              x = fmaf(p.b, v.x, x) + (row == col0 + 2 * j ? p.diag : 0.f);
-              y = fmaf(p.b, v.y, y) + (row == col0 + 2 * j + 1 ? p.diag : 0.f);
-            }
-            const __half2 hh = __floats2half2_rn(x, y);
-            o[j] = *reinterpret_cast<const uint32_t*>(&hh);
-          }
-          if (c < n_chunks && row < p.S) {  // (rows are padded to whole chunks)
-            st_bytes<32>(reinterpret_cast<char*>(yrow + c * 32), o);
-            st_bytes<32>(reinterpret_cast<char*>(yrow + c * 32 + 16), o + 8);
-          }
-        }
-      }
-      if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
-    }
+    for (int tile = unit; tile < num_tiles && !timed_out; tile += num_units)
+      timed_out = !e.template finish<MODE>(p, tile / p.tiles, tile % p.tiles);
   }
-  if (timed_out) atomicOr(p.status, static_cast<uint32_t>(SCALIFY_DEV_TIMEOUT));
+  if (timed_out) atomicOr(status, static_cast<uint32_t>(SCALIFY_DEV_TIMEOUT));
   tc_fence_before();
   __syncthreads();
   if constexpr (NCTA == 2) cluster_sync_all();
-  if (warp == 1) {
-    tc_fence_after();
-    tmem_dealloc(tmem_base, kAccs * kTN);
+  e.tear_down();
+}
+
+// All products of all steps in one launch, for matrices of few tiles: one cluster per matrix (so no matrix waits for
+// another), its CTAs (pairs) share the matrix's tiles, and a cluster barrier takes the place of a launch between products.
+struct NsMaps {
+  CUtensorMap z[2], b_z[2], zt[2], a, b_a, at, d, dt;
+};
+struct NsChain {
+  NsProduct gram, poly, update[2];  // update[k]: reads z[k], writes z[k ^ 1]
+  int steps;
+  uint32_t* status;
+};
+template <int NCTA>
+__global__ void __launch_bounds__(kNsThreads, 1) ns_chain_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsChain c) {
+  asm volatile("griddepcontrol.launch_dependents;");  // a programmatic dependent may set up while this grid runs
+  extern __shared__ uint8_t smem_raw[];
+  NsEngine<NCTA> e;
+  e.set_up(smem_raw);
+  __syncthreads();
+  cluster_sync_all();
+  tc_fence_after();
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  e.tmem_base = *e.tmem_slot;
+  uint32_t cluster_size;
+  asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(cluster_size));
+  const int unit = static_cast<int>(cluster_ctarank()) / NCTA, num_units = static_cast<int>(cluster_size) / NCTA;
+  const int b = static_cast<int>(blockIdx.x / cluster_size);
+  bool timed_out = false;  // (a role that gave up keeps taking part in the barriers)
+  auto product = [&](auto mode, const NsProduct& p, const CUtensorMap* ma, const CUtensorMap* mb, const CUtensorMap* mat, const CUtensorMap* mbt) {
+    constexpr int MODE = decltype(mode)::value;
+    if (e.warp == 0) {
+      if (e.lane == 0) {
+        asm volatile("fence.proxy.async;" ::: "memory");  // the copies read what the other CTAs' stores have written
+        for (int tile = unit; tile < p.tiles && !timed_out; tile += num_units)
+          timed_out = !e.template produce<MODE>(p, ma, mb, mat, mbt, b, tile);
+      }
+      __syncwarp();
+    } else if (e.warp == 1) {
+      if (e.lane == 0 && e.rank == 0u)
+        for (int tile = unit; tile < p.tiles && !timed_out; tile += num_units) timed_out = !e.template multiply<MODE>(p, tile);
+      __syncwarp();
+    } else {
+      for (int tile = unit; tile < p.tiles && !timed_out; tile += num_units) timed_out = !e.template finish<MODE>(p, b, tile);
+      asm volatile("fence.proxy.async;" ::: "memory");
+    }
+    cluster_sync_all();
+  };
+  for (int k = 0; k < c.steps; ++k) {
+    const int z = k & 1;
+    product(KindC<kGram>{}, c.gram, &maps.z[z], &maps.b_z[z], nullptr, nullptr);
+    product(KindC<kPoly>{}, c.poly, &maps.a, &maps.b_a, &maps.at, &maps.at);
+    product(KindC<kUpdate>{}, c.update[z], &maps.d, nullptr, &maps.dt, &maps.zt[z]);
   }
+  if (e.warp == 0 && e.lane == 0 && *e.abort_flag) e.drain_copies();
+  if (e.warp == 1 && e.lane == 0 && e.rank == 0u && *e.abort_flag) e.drain_multiplies();
+  if (timed_out) atomicOr(c.status, static_cast<uint32_t>(SCALIFY_DEV_TIMEOUT));
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  e.tear_down();
 }
 
 // ------------------------------------------------------------------------------------------------- element-wise passes
@@ -571,66 +680,135 @@ __global__ void __launch_bounds__(256) muon_update_kernel(const __grid_constant_
 }
 
 // ------------------------------------------------------------------------------------------------- launches
+// The most clusters of `size` CTAs of a kernel that are resident at once, found once per device and size (size is a power
+// of two up to 16; more than 8 needs the kernel's consent).
+template <class K>
+static int max_clusters(K kernel, size_t smem, int size, DeviceOnce& once, int* value) {
+  return device_once(once, value, [&](int* v) {
+    SCALIFY_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+    if (size > 8) SCALIFY_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    cudaLaunchConfig_t qc = {};
+    qc.gridDim = dim3(static_cast<unsigned>(sm_count() / size * size)); qc.blockDim = dim3(kNsThreads); qc.dynamicSmemBytes = smem;
+    cudaLaunchAttribute qa[1];
+    qa[0].id = cudaLaunchAttributeClusterDimension;
+    qa[0].val.clusterDim.x = static_cast<unsigned>(size); qa[0].val.clusterDim.y = 1; qa[0].val.clusterDim.z = 1;
+    qc.attrs = qa; qc.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &qc) != cudaSuccess) { n = 0; cudaGetLastError(); }
+    *v = n;
+    return int(SCALIFY_OK);
+  });
+}
+
 template <int MODE, int NCTA>
-static int launch_product_variant(const CUtensorMap (&m)[4], const NsParams& p, cudaStream_t st) {
+static int launch_product_variant(const CUtensorMap (&m)[4], const NsProduct& p, int batch, uint32_t* status, cudaStream_t st) {
   using C = NsCfg<NCTA>;
   auto kernel = ns_product_kernel<MODE, NCTA>;
   static DeviceOnce once;
   int most = 0;  // CTAs or CTA pairs that fit the GPU
+  int rc = max_clusters(kernel, C::kSmem, NCTA, once, &most);
+  if (rc) return rc;
+  if (most < 1) return SCALIFY_ERR_UNSUPPORTED;
   cudaLaunchAttribute attrs[2];
   attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attrs[0].val.programmaticStreamSerializationAllowed = 1;
   attrs[1].id = cudaLaunchAttributeClusterDimension;
   attrs[1].val.clusterDim.x = NCTA; attrs[1].val.clusterDim.y = 1; attrs[1].val.clusterDim.z = 1;
-  int rc = device_once(once, &most, [&](int* value) {
-    SCALIFY_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(C::kSmem)));
-    *value = sm_count();
-    if (NCTA == 2) {
-      cudaLaunchConfig_t qc = {};
-      qc.gridDim = dim3(unsigned(sm_count() / 2 * 2)); qc.blockDim = dim3(kNsThreads); qc.dynamicSmemBytes = C::kSmem;
-      qc.attrs = attrs + 1; qc.numAttrs = 1;
-      int n = 0;
-      SCALIFY_CUDA_TRY(cudaOccupancyMaxActiveClusters(&n, kernel, &qc));
-      if (n < 1) return int(SCALIFY_ERR_UNSUPPORTED);
-      *value = n;
-    }
-    return int(SCALIFY_OK);
-  });
-  if (rc) return rc;
-  const long long tiles = static_cast<long long>(p.tiles) * p.batch;
+  const long long tiles = static_cast<long long>(p.tiles) * batch;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>((tiles < most ? tiles : most) * NCTA));
   cfg.blockDim = dim3(kNsThreads); cfg.dynamicSmemBytes = C::kSmem; cfg.stream = st;
-  cfg.attrs = attrs; cfg.numAttrs = NCTA == 2 ? 2 : 1;
-  SCALIFY_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, m[0], m[1], m[2], m[3], p));
+  cfg.attrs = attrs; cfg.numAttrs = 2;
+  SCALIFY_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, m[0], m[1], m[2], m[3], p, batch, status));
   return SCALIFY_OK;
 }
 
 struct NsMatrix { __half* p; int rows, cols; long long ld; };  // [batch][rows][ld]
-
-// Y = A B^T (gram, poly: B is [N, K]) or A B (update: B is [K, N])
-template <int MODE>
-static int launch_product(const NsMatrix& A, const NsMatrix& B, const NsMatrix& Y, NsParams p, cudaStream_t st) {
-  const int ncta = Y.rows > kTM ? 2 : 1, tile_m = kTM * ncta;
-  auto map = [&](CUtensorMap* m, const NsMatrix& x, uint32_t box_bytes, uint32_t box_rows) {
-    return make_byte_map(m, x.p, static_cast<uint64_t>(x.cols) * 2, x.rows, p.batch, x.ld * 2, static_cast<uint64_t>(x.rows) * x.ld * 2,
-                         box_bytes, box_rows);
-  };
-  CUtensorMap m[4];  // both operands with the contraction along their lines, and MN-major
-  int rc = map(&m[0], A, 128, kTM);
-  if (!rc) rc = map(&m[1], B, 128, kTN / ncta);
-  if (!rc) rc = map(&m[2], A, 128, kTK);
-  if (!rc) rc = map(&m[3], B, 128, kTK);
-  if (rc) return rc;
+static int ns_map(CUtensorMap* m, const NsMatrix& x, int batch, uint32_t box_rows) {
+  return make_byte_map(m, x.p, static_cast<uint64_t>(x.cols) * 2, x.rows, batch, x.ld * 2, static_cast<uint64_t>(x.rows) * x.ld * 2, 128, box_rows);
+}
+// CTA pairs wherever there is more than one row tile of a single CTA
+static int ns_ncta(int S) { return S > kTM ? 2 : 1; }
+// tiles of Y = A B^T (gram, poly: B is [N, K]) or A B (update: B is [K, N]), and the sizes
+static void ns_shape(int mode, const NsMatrix& A, const NsMatrix& Y, NsProduct& p) {
+  const int tile_m = kTM * ns_ncta(Y.rows);
   p.S = Y.rows; p.N = Y.cols; p.K = A.cols;
   p.Y = Y.p; p.ldy = Y.ld;
   p.tiles_m = (Y.rows + tile_m - 1) / tile_m;
   p.tiles_n = (Y.cols + kTN - 1) / kTN;
   // symmetric products: the tile is square for CTA pairs; a single CTA's tile holds the whole matrix (S <= 128)
-  p.tiles = MODE == kUpdate ? p.tiles_m * p.tiles_n : p.tiles_n * (p.tiles_n + 1) / 2;
-  p.idesc = (1u << 4) | (uint32_t(kTN >> 3) << 17) | (uint32_t(tile_m >> 4) << 24);
-  if (ncta == 2) return launch_product_variant<MODE, 2>(m, p, st);
-  return launch_product_variant<MODE, 1>(m, p, st);
+  p.tiles = mode == kUpdate ? p.tiles_m * p.tiles_n : p.tiles_n * (p.tiles_n + 1) / 2;
+}
+template <int MODE>
+static int launch_product(const NsMatrix& A, const NsMatrix& B, const NsProduct& p, int batch, uint32_t* status, cudaStream_t st) {
+  const int ncta = ns_ncta(p.S);
+  CUtensorMap m[4];  // both operands with the contraction along their lines, and MN-major
+  int rc = ns_map(&m[0], A, batch, kTM);
+  if (!rc) rc = ns_map(&m[1], B, batch, kTN / ncta);
+  if (!rc) rc = ns_map(&m[2], A, batch, kTK);
+  if (!rc) rc = ns_map(&m[3], B, batch, kTK);
+  if (rc) return rc;
+  if (ncta == 2) return launch_product_variant<MODE, 2>(m, p, batch, status, st);
+  return launch_product_variant<MODE, 1>(m, p, batch, status, st);
+}
+
+// Clusters of 1, 2, 4 or 8 units (CTAs, or pairs) per matrix
+constexpr int kChainSizes = 4;
+template <int NCTA>
+static int chain_clusters(int size_log, int* most) {
+  static DeviceOnce once[kChainSizes];
+  return max_clusters(ns_chain_kernel<NCTA>, NsCfg<NCTA>::kSmem, NCTA << size_log, once[size_log], most);
+}
+template <int NCTA>
+static int launch_chain(const NsMatrix (&z)[2], const NsMatrix& A, const NsMatrix& D, const NsChain& c, int batch, int size_log, cudaStream_t st) {
+  NsMaps maps;
+  int rc = SCALIFY_OK;
+  for (int k = 0; k < 2 && !rc; ++k) {
+    rc = ns_map(&maps.z[k], z[k], batch, kTM);
+    if (!rc) rc = ns_map(&maps.b_z[k], z[k], batch, kTN / NCTA);
+    if (!rc) rc = ns_map(&maps.zt[k], z[k], batch, kTK);
+  }
+  if (!rc) rc = ns_map(&maps.a, A, batch, kTM);
+  if (!rc) rc = ns_map(&maps.b_a, A, batch, kTN / NCTA);
+  if (!rc) rc = ns_map(&maps.at, A, batch, kTK);
+  if (!rc) rc = ns_map(&maps.d, D, batch, kTM);
+  if (!rc) rc = ns_map(&maps.dt, D, batch, kTK);
+  if (rc) return rc;
+  cudaLaunchAttribute attrs[2];
+  attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attrs[0].val.programmaticStreamSerializationAllowed = 1;
+  attrs[1].id = cudaLaunchAttributeClusterDimension;
+  attrs[1].val.clusterDim.x = NCTA << size_log; attrs[1].val.clusterDim.y = 1; attrs[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(batch) * (NCTA << size_log));
+  cfg.blockDim = dim3(kNsThreads); cfg.dynamicSmemBytes = NsCfg<NCTA>::kSmem; cfg.stream = st;
+  cfg.attrs = attrs; cfg.numAttrs = 2;
+  SCALIFY_CUDA_TRY(cudaLaunchKernelEx(&cfg, ns_chain_kernel<NCTA>, maps, c));
+  return SCALIFY_OK;
+}
+
+// One launch or one per product?  The times of a step, in K blocks of a tile (about 0.3 us): a unit's share of the tiles,
+// and what comes between two products: a cluster barrier with a cold start of the ring (8 blocks), or a launch (18; more
+// on the host).  *size_log < 0: one launch per product.
+template <int NCTA>
+static int choose_chain(const NsChain& c, int batch, int* size_log) {
+  auto blocks = [](const NsProduct& p) { return static_cast<double>((p.K + kTK - 1) / kTK); };
+  const NsProduct* all[3] = {&c.gram, &c.poly, &c.update[0]};
+  const double units = sm_count() / NCTA;
+  double best = 0.0;
+  for (const NsProduct* p : all) best += ceil(static_cast<double>(p->tiles) * batch / units) * blocks(*p) + 18.0;
+  *size_log = -1;
+  for (int s = 0; s < kChainSizes; ++s) {
+    int most = 0;
+    const int rc = chain_clusters<NCTA>(s, &most);
+    if (rc) return rc;
+    if (most < 1) continue;
+    double cost = 0.0;
+    for (const NsProduct* p : all) cost += ceil(static_cast<double>(p->tiles) / (1 << s)) * blocks(*p) + 8.0;
+    cost *= ceil(static_cast<double>(batch) / most);
+    if (cost < best) { best = cost; *size_log = s; }
+  }
+  return SCALIFY_OK;
 }
 
 static long long pad64(long long n) { return (n + 63) / 64 * 64; }
@@ -733,28 +911,37 @@ static int run_batch(const MuonTable& tab, int count, const MuonHyper& h, void* 
   })
   SCALIFY_CUDA_TRY(cudaGetLastError());
 
-  NsParams np = {};
-  np.batch = count;
-  np.status = view.status;
-  int cur = 0;
-  for (int k = 0; k < h.steps; ++k) {
-    NsParams q = np;
-    q.alpha = p.sigma * p.sigma * kGramScale;
-    int rc = launch_product<kGram>(z[cur], z[cur], A, q, st);
-    if (rc) return rc;
-    q.alpha = h.c / kGramScale;
-    q.b = h.b;
-    q.diag = h.a * kGramScale;
-    q.A = A.p;
-    rc = launch_product<kPoly>(A, A, D, q, st);
-    if (rc) return rc;
-    q = np;
-    q.alpha = 1.0f / kGramScale;
-    rc = launch_product<kUpdate>(D, z[cur], z[cur ^ 1], q, st);
-    if (rc) return rc;
-    cur ^= 1;
+  NsChain c = {};
+  c.steps = h.steps;
+  c.status = view.status;
+  ns_shape(kGram, z[0], A, c.gram);
+  c.gram.alpha = p.sigma * p.sigma * kGramScale;
+  ns_shape(kPoly, A, D, c.poly);
+  c.poly.alpha = h.c / kGramScale;
+  c.poly.b = h.b;
+  c.poly.diag = h.a * kGramScale;
+  c.poly.A = A.p;
+  for (int k = 0; k < 2; ++k) {
+    ns_shape(kUpdate, D, z[k ^ 1], c.update[k]);
+    c.update[k].alpha = 1.0f / kGramScale;
   }
-  p.Z = z[cur].p;
+  const bool pairs = ns_ncta(s.S) == 2;
+  int size_log = -1;
+  int rc = pairs ? choose_chain<2>(c, count, &size_log) : choose_chain<1>(c, count, &size_log);
+  if (rc) return rc;
+  if (size_log >= 0) {
+    rc = pairs ? launch_chain<2>(z, A, D, c, count, size_log, st) : launch_chain<1>(z, A, D, c, count, size_log, st);
+    if (rc) return rc;
+  } else {
+    for (int k = 0; k < h.steps; ++k) {
+      const int cur = k & 1;
+      rc = launch_product<kGram>(z[cur], z[cur], c.gram, count, c.status, st);
+      if (!rc) rc = launch_product<kPoly>(A, A, c.poly, count, c.status, st);
+      if (!rc) rc = launch_product<kUpdate>(D, z[cur], c.update[cur], count, c.status, st);
+      if (rc) return rc;
+    }
+  }
+  p.Z = z[h.steps & 1].p;
   muon_update_kernel<<<tiles, 256, 0, st>>>(tab, p);
   SCALIFY_CUDA_TRY(cudaGetLastError());
   return SCALIFY_OK;
