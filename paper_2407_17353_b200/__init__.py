@@ -114,11 +114,11 @@ def lib() -> ctypes.CDLL:
         L.scalify_scaled_softmax_bwd.argtypes = [P, P, P, vp]
         L.scalify_scaled_cross_entropy.argtypes = [P, i64, vp, vp, P, vp, sz, vp]
         L.scalify_scaled_adam_step_static.argtypes = [i32, P, P, P, P, f32, f32, f32, f32, i64, vp, vp]
-        L.scalify_scaled_add_rmsnorm.argtypes = [P, P, P, f32, P, P, vp, vp, vp, vp]
-        L.scalify_scaled_add_rmsnorm_bwd.argtypes = [P, P, P, P, vp, P, P, vp, i32, P, vp, sz, vp]
-        L.scalify_scaled_embedding_lookup.argtypes = [vp, i64, i64, P, f32, P, vp, vp]
-        L.scalify_scaled_embedding_grad.argtypes = [vp, i64, i64, P, f32, P, P, vp, sz, vp]
-        L.scalify_orthogonalize.argtypes = [P, i32, vp, f32, P, vp, sz, vp]
+        L.scalify_scaled_add_rmsnorm.argtypes = [vp, vp, vp, f32, vp, vp, vp, vp, vp, vp]
+        L.scalify_scaled_add_rmsnorm_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, sz, vp]
+        L.scalify_scaled_embedding_lookup.argtypes = [vp, i64, i64, vp, f32, vp, vp, vp]
+        L.scalify_scaled_embedding_grad.argtypes = [vp, i64, i64, vp, f32, vp, vp, vp, sz, vp]
+        L.scalify_orthogonalize.argtypes = [vp, i32, vp, f32, vp, vp, sz, vp]
         L.scalify_muon_workspace_bytes.restype = sz
         L.scalify_muon_workspace_bytes.argtypes = [i32, P]
         L.scalify_scaled_muon_step.argtypes = [i32, P, P, P, P, f32, f32, i32, f32, i32, vp, f32, i32, vp, sz, vp]
@@ -163,12 +163,14 @@ def _desc(t: Optional[ScaledTensor]):
     """ctypes descriptor of a ScaledTensor (None -> NULL); cached on the object while its buffers stay the same."""
     if t is None:
         return None
-    d = t.data
-    sp = 0 if t.scale is None else t.scale.data_ptr()
-    key = (d.data_ptr(), d.dtype, tuple(d.shape), d.stride(), sp)
+    d, scale = t.data, t.scale
+    dp, sp = d.data_ptr(), 0 if scale is None else scale.data_ptr()
+    shape, stride = d.shape, d.stride()
     cached = t.__dict__.get("_desc_cache")
-    if cached is not None and cached[0] == key:
-        return cached[1]
+    if cached is not None:
+        dp0, sp0, dtype0, shape0, stride0, a, _ = cached
+        if dp == dp0 and sp == sp0 and d.dtype is dtype0 and shape == shape0 and stride == stride0:
+            return a
     if d.dim() < 1 or d.dim() > 4:
         raise ValueError("scalify arrays have 1 to 4 dimensions")
     a = scalify_array()
@@ -184,7 +186,7 @@ def _desc(t: Optional[ScaledTensor]):
         a.scale = sp
     else:
         a.scale = None
-    t.__dict__["_desc_cache"] = (key, a)
+    t.__dict__["_desc_cache"] = (dp, sp, d.dtype, shape, stride, a, ctypes.addressof(a))
     return a
 
 
@@ -559,24 +561,35 @@ def scalify_scaled_attention_bwd(Q: ScaledTensor, K: ScaledTensor, V: ScaledTens
            "scalify_scaled_attention_bwd")
 
 
-def _call(name: str, device: torch.device, stream, *args) -> None:
+def _addr(t: Optional[ScaledTensor]):
+    """Address of a ScaledTensor's descriptor (kept alive on the object), None for None."""
+    if t is None:
+        return None
+    _desc(t)
+    return t.__dict__["_desc_cache"][6]
+
+
+def _call(name: str, device: int, stream, *args) -> None:
     """Calls an entry point with ``device`` current (its stream is that device's current one unless given)."""
-    fn = getattr(lib(), name)
-    if device.type != "cuda":
+    if device < 0:
         raise ValueError(f"{name}: arrays must be on a CUDA device")
-    if device.index == torch.cuda.current_device():
-        _check(fn(*args, _stream(stream)), name)
+    fn = getattr(lib(), name)
+    st = torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream)
+    if device == torch.cuda.current_device():
+        code = fn(*args, st)
     else:
         with torch.cuda.device(device):
-            _check(fn(*args, _stream(stream)), name)
+            code = fn(*args, st)
+    if code != 0:
+        raise ScalifyError(code, name)
 
 
-def _same_device(name: str, first: torch.Tensor, *others) -> torch.device:
-    """The device of ``first``; every other tensor (None skipped) has to be there too."""
-    dev = first.device
+def _same_device(name: str, first: torch.Tensor, *others) -> int:
+    """The CUDA device of ``first`` (-1: none); every other tensor (None skipped) has to be there too."""
+    dev = first.get_device()
     for t in others:
-        if t is not None and t.device != dev:
-            raise ValueError(f"{name}: arrays on {dev} and {t.device}")
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"{name}: arrays on {first.device} and {t.device}")
     return dev
 
 
@@ -598,9 +611,8 @@ def scalify_scaled_add_rmsnorm(X: ScaledTensor, R: Optional[ScaledTensor], gamma
     dev = _same_device(name, X.data, _data(R), _data(gamma), _data(H), _data(Y), rinv, status)
     d = X.data.shape[-1]
     _rows_vector(name, rinv, X.data.numel() // d if d else 0, "rinv")
-    x, r, g, h = _desc(X), _desc(R), _desc(gamma), _desc(H)
-    y, mx = (None, ctypes.addressof(Y._d)) if isinstance(Y, MxTensor) else (_desc(Y), None)
-    _call(name, dev, stream, _ref(x), _ref(r), _ref(g), float(eps), _ref(h), _ref(y), mx, _ptr(rinv), _ptr(status))
+    y, mx = (None, ctypes.addressof(Y._d)) if isinstance(Y, MxTensor) else (_addr(Y), None)
+    _call(name, dev, stream, _addr(X), _addr(R), _addr(gamma), eps, _addr(H), y, mx, _ptr(rinv), _ptr(status))
 
 
 def scalify_scaled_add_rmsnorm_bwd(G: ScaledTensor, Gr: Optional[ScaledTensor], H: ScaledTensor,
@@ -616,9 +628,8 @@ def scalify_scaled_add_rmsnorm_bwd(G: ScaledTensor, Gr: Optional[ScaledTensor], 
     d = H.data.shape[-1]
     _rows_vector(name, rinv, H.data.numel() // d if d else 0, "rinv")
     _rows_vector(name, stat_in, 1, "stat_in")
-    g, gr, h, gm, dx, dq, dg = (_desc(G), _desc(Gr), _desc(H), _desc(gamma), _desc(dX), _desc(dXq), _desc(dgamma))
-    _call(name, dev, stream, _ref(g), _ref(gr), _ref(h), _ref(gm), _ptr(rinv), _ref(dx), _ref(dq), _ptr(stat_in),
-          int(stat_dx), _ref(dg), None if ws is None else ws.ptr, 0 if ws is None else ws.nbytes)
+    _call(name, dev, stream, _addr(G), _addr(Gr), _addr(H), _addr(gamma), _ptr(rinv), _addr(dX), _addr(dXq), _ptr(stat_in),
+          int(stat_dx), _addr(dgamma), None if ws is None else ws.ptr, 0 if ws is None else ws.nbytes)
 
 
 def _token_ids(name: str, ids: torch.Tensor, padding_id: Optional[int]) -> int:
@@ -634,8 +645,7 @@ def scalify_scaled_embedding_lookup(ids: torch.Tensor, wte: ScaledTensor, Y: Sca
     name = "scalify_scaled_embedding_lookup"
     pad = _token_ids(name, ids, padding_id)
     dev = _same_device(name, wte.data, ids, Y.data, status)
-    w, y = _desc(wte), _desc(Y)
-    _call(name, dev, stream, ids.data_ptr(), ids.numel(), pad, _ref(w), float(c), _ref(y), _ptr(status))
+    _call(name, dev, stream, ids.data_ptr(), ids.numel(), pad, _addr(wte), float(c), _addr(Y), _ptr(status))
 
 
 def scalify_scaled_embedding_grad(ids: torch.Tensor, dY: ScaledTensor, dwte: ScaledTensor, ws: Workspace, *,
@@ -645,8 +655,7 @@ def scalify_scaled_embedding_grad(ids: torch.Tensor, dY: ScaledTensor, dwte: Sca
     name = "scalify_scaled_embedding_grad"
     pad = _token_ids(name, ids, padding_id)
     dev = _same_device(name, dwte.data, ids, dY.data, _data(addend), ws.buf)
-    g, w, a = _desc(dY), _desc(dwte), _desc(addend)
-    _call(name, dev, stream, ids.data_ptr(), ids.numel(), pad, _ref(g), float(c), _ref(a), _ref(w), ws.ptr, ws.nbytes)
+    _call(name, dev, stream, ids.data_ptr(), ids.numel(), pad, _addr(dY), float(c), _addr(addend), _addr(dwte), ws.ptr, ws.nbytes)
 
 
 def scalify_muon_workspace_bytes(w: Sequence[ScaledTensor]) -> int:
@@ -670,8 +679,7 @@ def scalify_orthogonalize(X: ScaledTensor, O: ScaledTensor, ws: Workspace, *, st
     """O = the orthogonalised matrix (or batch of matrices) X, by `steps` Newton-Schulz iterations."""
     name = "scalify_orthogonalize"
     dev = _same_device(name, X.data, O.data, ws.buf)
-    x, o = _desc(X), _desc(O)
-    _call(name, dev, stream, _ref(x), int(steps), _coef(coef), float(eps), _ref(o), ws.ptr, ws.nbytes)
+    _call(name, dev, stream, _addr(X), int(steps), _coef(coef), float(eps), _addr(O), ws.ptr, ws.nbytes)
 
 
 class MuonTensors:

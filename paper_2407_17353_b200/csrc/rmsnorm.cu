@@ -478,11 +478,12 @@ __global__ void __launch_bounds__(kFinishThreads) add_rmsnorm_bwd_finish_kernel(
     const float* __restrict__ partial, int64_t ld, int lines, int d, void* __restrict__ dgamma, float inv_kf,
     const double* __restrict__ stat_partial, int stat, double count, float* stat_word) {
   asm volatile("griddepcontrol.launch_dependents;");  // a programmatic dependent may set up while this grid runs
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // launched as a programmatic dependent: the gradient is complete
   __shared__ double s[32][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (stat != SCALIFY_STAT_NONE && blockIdx.x == gridDim.x - 1) {
     double t = 0.0;
-    for (int i = threadIdx.x; i < lines; i += kFinishThreads) t = stat == SCALIFY_STAT_AMAX ? fmax(t, stat_partial[i]) : t + stat_partial[i];
+    for (int i = threadIdx.x; i < lines; i += kFinishThreads) t = stat == SCALIFY_STAT_AMAX ? fmax(t, __ldcg(stat_partial + i)) : t + __ldcg(stat_partial + i);
     t = stat == SCALIFY_STAT_AMAX ? static_cast<double>(warp_max_u32(static_cast<uint32_t>(t))) : warp_sum_f64(t);
     if (lane == 0) s[0][warp] = t;
     __syncthreads();
@@ -585,10 +586,15 @@ int launch_add_rmsnorm_bwd(RmsNormBwdArgs a, int g_dt, int h_dt, void* dgamma, i
   if (!dgamma && a.stat == SCALIFY_STAT_NONE) return SCALIFY_OK;
   const unsigned blocks = (dgamma ? (a.d + 31) / 32 : 0) + (a.stat != SCALIFY_STAT_NONE ? 1 : 0);
   const double count = static_cast<double>(a.rows) * a.d;
-  SCALIFY_DISPATCH_WIDE(dgamma_dt, ODT, add_rmsnorm_bwd_finish_kernel<ODT><<<blocks, kFinishThreads, 0, st>>>(
-                                            a.partial, a.partial_ld, static_cast<int>(grid), dgamma ? a.d : 0, dgamma,
-                                            1.0f / a.kf, a.stat_partial, a.stat, count, stat_word))
-  SCALIFY_CUDA_TRY(cudaGetLastError());
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = dim3(blocks); cfg.blockDim = dim3(kFinishThreads); cfg.stream = st; cfg.attrs = attr; cfg.numAttrs = 1;
+  const float* partial = a.partial;
+  const double* stats = a.stat_partial;
+  SCALIFY_DISPATCH_WIDE(dgamma_dt, ODT, SCALIFY_CUDA_TRY(cudaLaunchKernelEx(&cfg, add_rmsnorm_bwd_finish_kernel<ODT>, partial, a.partial_ld,
+                                            static_cast<int>(grid), dgamma ? a.d : 0, dgamma, 1.0f / a.kf, stats, a.stat, count, stat_word)))
   return SCALIFY_OK;
 }
 

@@ -106,6 +106,8 @@ static bool disjoint_or_same(const scalify_array* out, int64_t out_ld, const sca
   return out->data == in->data && out->dtype == in->dtype && out_ld == in_ld;
 }
 static bool disjoint(const scalify_array* a, const scalify_array* b) { return !a || !b || !overlap(span_of(a), span_of(b)); }
+// An output's rows may not overlap one another.
+static bool rows_apart(int64_t rows, int64_t cols, int64_t ld) { return rows <= 1 || ld >= cols; }
 // Scale words an entry point writes (null entries skipped): none of them twice, none of them an input's.
 static int check_scale_words(const float* const* out, int n_out, const float* const* in, int n_in) {
   for (int i = 0; i < n_out; ++i) {
@@ -528,7 +530,7 @@ int scalify_scaled_add_rmsnorm(const scalify_array* X, const scalify_array* R, c
     if (rc) return rc;
     if ((R->dtype != X->dtype && R->dtype != SCALIFY_F32) || H->dtype != R->dtype) return SCALIFY_ERR_DTYPE;
     if (as_rows(R, &r2, &d2, &a.r_ld) || r2 != a.rows || d2 != d) return SCALIFY_ERR_SHAPE;
-    if (as_rows(H, &r2, &d2, &a.h_ld) || r2 != a.rows || d2 != d) return SCALIFY_ERR_SHAPE;
+    if (as_rows(H, &r2, &d2, &a.h_ld) || r2 != a.rows || d2 != d || !rows_apart(r2, d, a.h_ld)) return SCALIFY_ERR_SHAPE;
     if (!disjoint_or_same(H, a.h_ld, R, a.r_ld) || !disjoint_or_same(H, a.h_ld, X, a.x_ld)) return SCALIFY_ERR_ALIAS;
   }
   if (gamma) {
@@ -554,7 +556,7 @@ int scalify_scaled_add_rmsnorm(const scalify_array* X, const scalify_array* R, c
   } else {
     rc = check_array(Y);
     if (rc) return rc;
-    if (as_rows(Y, &r2, &d2, &a.y_ld) || r2 != a.rows || d2 != d) return SCALIFY_ERR_SHAPE;
+    if (as_rows(Y, &r2, &d2, &a.y_ld) || r2 != a.rows || d2 != d || !rows_apart(r2, d, a.y_ld)) return SCALIFY_ERR_SHAPE;
   }
   if (!disjoint(out, X) || !disjoint(out, R) || !disjoint(out, H) || !disjoint(out, gamma)) return SCALIFY_ERR_ALIAS;
   {
@@ -592,7 +594,7 @@ int scalify_scaled_add_rmsnorm_bwd(const scalify_array* G, const scalify_array* 
   if (as_rows(H, &a.rows, &d, &a.h_ld)) return SCALIFY_ERR_SHAPE;
   if (a.rows < 1 || a.rows > 0x7FFFFFFF || d < 1 || d > kRmsNormMaxD) return SCALIFY_ERR_SHAPE;
   if (as_rows(G, &r2, &d2, &a.g_ld) || r2 != a.rows || d2 != d) return SCALIFY_ERR_SHAPE;
-  if (as_rows(dX, &r2, &d2, &a.dx_ld) || r2 != a.rows || d2 != d) return SCALIFY_ERR_SHAPE;
+  if (as_rows(dX, &r2, &d2, &a.dx_ld) || r2 != a.rows || d2 != d || !rows_apart(r2, d, a.dx_ld)) return SCALIFY_ERR_SHAPE;
   if (Gr) {
     rc = check_array(Gr);
     if (rc) return rc;
@@ -615,7 +617,7 @@ int scalify_scaled_add_rmsnorm_bwd(const scalify_array* G, const scalify_array* 
     rc = check_array(dXq);
     if (rc) return rc;
     if (!is_fp8(dXq->dtype)) return SCALIFY_ERR_DTYPE;
-    if (as_rows(dXq, &r2, &d2, &a.dxq_ld) || r2 != a.rows || d2 != d) return SCALIFY_ERR_SHAPE;
+    if (as_rows(dXq, &r2, &d2, &a.dxq_ld) || r2 != a.rows || d2 != d || !rows_apart(r2, d, a.dxq_ld)) return SCALIFY_ERR_SHAPE;
   }
   if (!disjoint_or_same(dX, a.dx_ld, G, a.g_ld) || !disjoint_or_same(dX, a.dx_ld, Gr, a.gr_ld) || !disjoint(dX, H) ||
       !disjoint(dX, gamma) || !disjoint(dX, dgamma) || !disjoint(dX, dXq))
@@ -1237,7 +1239,7 @@ int scalify_scaled_embedding_lookup(const int64_t* ids, int64_t n, int64_t paddi
   if (!split_constant(c, &a.c_pow2, &a.c_rest)) return SCALIFY_ERR_VALUE;
   if (wte->ndim != 2 || Y->ndim != 2 || n < 0 || n > 0x7FFFFFFF) return SCALIFY_ERR_SHAPE;
   const int64_t d = wte->shape[1];
-  if (d < 1 || d > 0x7FFFFFF0 || wte->shape[0] < 1 || Y->shape[0] != n || Y->shape[1] != d) return SCALIFY_ERR_SHAPE;
+  if (d < 1 || d > 0x7FFFFFF0 || wte->shape[0] < 1 || Y->shape[0] != n || Y->shape[1] != d || !rows_apart(n, d, Y->stride[0])) return SCALIFY_ERR_SHAPE;
   if (n == 0) return SCALIFY_OK;
   if (!disjoint(wte, Y)) return SCALIFY_ERR_ALIAS;
   if (Y->scale && Y->scale == wte->scale) return SCALIFY_ERR_ALIAS;
@@ -1260,7 +1262,7 @@ int scalify_scaled_embedding_grad(const int64_t* ids, int64_t n, int64_t padding
   if (!split_constant(c, &a.c_pow2, &a.c_rest)) return SCALIFY_ERR_VALUE;
   if (dwte->ndim != 2 || n < 0 || n > 0x7FFFFFFE) return SCALIFY_ERR_SHAPE;
   const int64_t vocab = dwte->shape[0], d = dwte->shape[1];
-  if (d < 1 || d > 0x7FFFFFF0 || vocab < 1 || vocab > kEmbeddingMaxVocab) return SCALIFY_ERR_SHAPE;
+  if (d < 1 || d > 0x7FFFFFF0 || vocab < 1 || vocab > kEmbeddingMaxVocab || !rows_apart(vocab, d, dwte->stride[0])) return SCALIFY_ERR_SHAPE;
   if (!dY) return SCALIFY_ERR_NULL;
   if (n > 0) {
     rc = check_array(dY);
@@ -1412,6 +1414,8 @@ int scalify_orthogonalize(const scalify_array* X, int steps, const float* coef, 
   if (!same_shape(X, O)) return SCALIFY_ERR_SHAPE;
   const int total = count_matrices(1, X), nd = X->ndim;
   if (total == 0) return SCALIFY_ERR_SHAPE;
+  const int64_t o_rows = O->shape[nd - 2], o_cols = O->shape[nd - 1], o_ld = O->stride[nd - 2];
+  if (!rows_apart(o_rows, o_cols, o_ld) || (total > 1 && O->stride[0] < (o_rows - 1) * o_ld + o_cols)) return SCALIFY_ERR_SHAPE;
   if (!disjoint(X, O) || (O->scale && O->scale == X->scale)) return SCALIFY_ERR_ALIAS;
   rc = check_ws(workspace, workspace_bytes, kWsMin);
   if (rc) return rc;
@@ -1466,6 +1470,7 @@ int scalify_scaled_muon_step(int n_tensors, const scalify_array* grads, scalify_
     if (matrix_of(&grads[i], &r2, &c2, &t.g_ld) || r2 != rows || c2 != cols) return SCALIFY_ERR_SHAPE;
     if (matrix_of(&m[i], &r2, &c2, &t.m_ld) || r2 != rows || c2 != cols) return SCALIFY_ERR_SHAPE;
     if (w_cast && (matrix_of(&w_cast[i], &r2, &c2, &t.wc_ld) || r2 != rows || c2 != cols)) return SCALIFY_ERR_SHAPE;
+    if (!rows_apart(rows, cols, t.w_ld) || !rows_apart(rows, cols, t.m_ld) || (w_cast && !rows_apart(rows, cols, t.wc_ld))) return SCALIFY_ERR_SHAPE;
     const scalify_array* wc = w_cast ? &w_cast[i] : nullptr;
     if (!disjoint(&m[i], &grads[i]) || !disjoint(&w[i], &grads[i]) || !disjoint(&m[i], &w[i]) || !disjoint(wc, &grads[i]) ||
         !disjoint(wc, &m[i]) || !disjoint(wc, &w[i]))

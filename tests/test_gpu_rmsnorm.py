@@ -273,3 +273,18 @@ def test_bad_scale_word_is_reported():
     status = torch.zeros(1, dtype=torch.int32, device="cuda")
     sc.scalify_scaled_add_rmsnorm(X, None, None, None, Y, status=status)
     assert int(status.item()) == sc.DEV_BAD_SCALE
+
+
+def test_broadcast_rows():
+    """Inputs whose rows are one row (stride 0), ragged and not."""
+    for d in (100, 776, 1500, 5004):
+        rows = 9
+        H, _ = put(torch.randn(rows, d, generator=gen(d), device="cuda"), F32)
+        one = torch.zeros((-(-d // 8)) * 8, device="cuda", dtype=BF16)
+        one[:d] = torch.randn(d, generator=gen(d + 1), device="cuda").to(BF16)
+        G = one[:d].as_strided((rows, d), (0, 1))
+        rinv = ((H.double().square().mean(1) + 1e-5) ** -0.5).float()
+        dX = sc.ScaledTensor(rows_of(rows, d, F32)[0], torch.empty(1, device="cuda"))
+        sc.scalify_scaled_add_rmsnorm_bwd(scaled(G, 1.0), None, scaled(H, 1.0), None, rinv, dX)
+        want = p64.add_rmsnorm_bwd(G, 1.0, None, 0.0, H, 1.0, None, 1.0, rinv)
+        assert bool(p64.close(dX.data, want["dX"], U * want["mag"]).all())

@@ -276,3 +276,18 @@ def test_muon_binding_checks():
         sc.MuonTensors([t], [t, t], [t])
     with pytest.raises(ValueError):
         sc.scalify_muon_workspace_bytes([sc.ScaledTensor(torch.zeros(8))])
+
+
+def test_overlapping_output_rows_are_refused():
+    B, F = sc.BF16, sc.F32
+    L = sc.lib()
+    x, over = arr(1, B, (4, 128)), lambda mb, dt=B: arr(mb, dt, (4, 128), (64, 1))  # noqa: E731
+    assert norm_call(x, None, None, 1e-5, None, over(4)) == SHAPE
+    assert norm_call(x, arr(2, B, (4, 128)), None, 1e-5, over(3), arr(4, B, (4, 128))) == SHAPE
+    assert norm_bwd(G=x, H=arr(2, B, (4, 128)), dX=over(3)) == SHAPE
+    assert norm_bwd(G=x, H=arr(2, B, (4, 128)), dX=arr(3, B, (4, 128)), dXq=over(4, sc.E5M2)) == SHAPE
+    assert L.scalify_scaled_embedding_lookup(8 * MB, 4, -1, R(arr(1, B, (50, 128))), 1.0, R(over(2)), None, None) == SHAPE
+    assert L.scalify_scaled_embedding_grad(8 * MB, 4, -1, R(arr(2, B, (4, 128))), 1.0, None, R(over(1, F)), 16 * MB, 64 * MB, None) == SHAPE
+    assert L.scalify_orthogonalize(R(arr(1, F, (4, 128))), 5, None, 0.0, R(over(2)), 16 * MB, 64 * MB, None) == SHAPE
+    assert L.scalify_orthogonalize(R(arr(1, F, (2, 4, 128))), 5, None, 0.0, R(arr(2, B, (2, 4, 128), (256, 128, 1))), 16 * MB,
+                                   64 * MB, None) == SHAPE
