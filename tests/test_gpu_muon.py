@@ -60,7 +60,8 @@ def test_one_step(b, r, c, ot):
 
 
 @pytest.mark.parametrize("b,r,c,xt", [(4, 256, 320, BF16), (0, 768, 768, F32), (2, 1000, 333, BF16), (0, 640, 2304, BF16),
-                                      (130, 40, 30, F32), (1, 2048, 2048, BF16), (2, 64, 5000, F16), (0, 3, 2000, F32)])
+                                      (130, 40, 30, F32), (1, 2048, 2048, BF16), (2, 64, 5000, F16), (0, 3, 2000, F32), (1, 3333, 3400, BF16),
+                                      (24, 700, 760, BF16)])
 def test_five_steps(b, r, c, xt):
     O, X, unit = orth(b, r, c, xt, BF16, 5, seed=r)
     want = p64.newton_schulz(X, 5) / unit
