@@ -87,18 +87,30 @@ static int as_rows(const scalify_array* a, int64_t* rows, int64_t* cols, int64_t
   return SCALIFY_ERR_SHAPE;
 }
 
-// The bytes between an array's first and last element, as [lo, hi); empty arrays span nothing.
-struct Span { uintptr_t lo, hi; };
+// The bytes between an array's first and last element, as [lo, hi) (empty arrays span nothing), and its rows: `width` bytes
+// every `period` ones (period 0: no such pattern, or one row).
+struct Span { uintptr_t lo, hi, width, period; };
 static Span span_of(const scalify_array* a) {
   int64_t last = 0;
   for (int i = 0; i < a->ndim; ++i) {
-    if (a->shape[i] == 0) return Span{0, 0};
+    if (a->shape[i] == 0) return Span{0, 0, 0, 0};
     last += (a->shape[i] - 1) * a->stride[i];
   }
-  const uintptr_t lo = reinterpret_cast<uintptr_t>(a->data);
-  return Span{lo, lo + static_cast<uintptr_t>(last + 1) * elem_size(a->dtype)};
+  const uintptr_t es = elem_size(a->dtype), lo = reinterpret_cast<uintptr_t>(a->data);
+  Span s{lo, lo + static_cast<uintptr_t>(last + 1) * es, 0, 0};
+  const int64_t ld = a->ndim >= 2 ? a->stride[a->ndim - 2] : 0, cols = a->shape[a->ndim - 1];
+  bool rows = ld >= cols && ld > 0 && a->stride[a->ndim - 1] == 1;
+  for (int i = 0; i + 2 < a->ndim; ++i) rows = rows && a->stride[i] % ld == 0;
+  if (rows) { s.width = static_cast<uintptr_t>(cols) * es; s.period = static_cast<uintptr_t>(ld) * es; }
+  return s;
 }
-static bool overlap(Span a, Span b) { return a.lo < b.hi && b.lo < a.hi; }
+// (column slices of one buffer, rows alike far apart, do not overlap: b's bytes are [off, off + width) of each of a's periods)
+static bool overlap(Span a, Span b) {
+  if (!(a.lo < b.hi && b.lo < a.hi)) return false;
+  if (a.period == 0 || a.period != b.period) return true;
+  const uintptr_t off = a.lo <= b.lo ? (b.lo - a.lo) % a.period : (a.period - (a.lo - b.lo) % a.period) % a.period;
+  return off < a.width || off + b.width > a.period;
+}
 // Whether an output may share memory with an input: not at all, or as the very same rows (every element is read by the
 // thread that writes it).
 static bool disjoint_or_same(const scalify_array* out, int64_t out_ld, const scalify_array* in, int64_t in_ld) {

@@ -118,6 +118,45 @@ def test_grad_is_the_same_every_time():
         assert torch.equal(first, grad(ids, 50257, 128, BF16, F32, seed=6))
 
 
+def test_offsets_past_32_bits():
+    """Rows 2^27 elements apart: table, batch and gradient reach past 2^31 elements."""
+    base = torch.empty(20 * (1 << 27), dtype=BF16, device="cuda")
+    rows = base.view(20, 1 << 27)
+    ids = torch.tensor([19, 3, 19, 0, 18, 5, 5, 19, 7, 1, 1, 1, 1, 12, 19, 2, 2, 4, 19, 19], device="cuda")
+    W = torch.randn(20, 40, generator=gen(8), device="cuda").to(BF16)
+    rows[:, :40] = W
+    zeros = lambda: torch.zeros(1, device="cuda")
+    near, far = sc.ScaledTensor.empty((20, 40), BF16), sc.ScaledTensor(rows[:, 64:104], zeros())
+    sc.scalify_scaled_embedding_lookup(ids, sc.ScaledTensor.make(W, 1.0), near, c=1.5)
+    sc.scalify_scaled_embedding_lookup(ids, sc.ScaledTensor.make(rows[:, :40], 1.0), far, c=1.5)
+    assert torch.equal(near.data, far.data) and torch.equal(near.data, (W[ids].double() * 1.5).to(BF16))
+    ws = sc.Workspace(sc.scalify_workspace_bytes(sc.OP_EMBEDDING_GRAD, 20, 40))
+    a, b = sc.ScaledTensor.empty((20, 40), BF16), sc.ScaledTensor(rows[:, 128:168], zeros())
+    sc.scalify_scaled_embedding_grad(ids, near, a, ws)
+    sc.scalify_scaled_embedding_grad(ids, far, b, ws)
+    assert torch.equal(a.data, b.data) and torch.equal(rows[:, :40], W)
+    want, _, mag, count = p64.embedding_grad(ids, near.data, 1.0, 20, 1.0, -1)
+    assert bool(p64.close(b.data, want, (count + 4) * U * mag).all())
+
+
+def test_calls_on_two_streams_at_once():
+    """Two calls beside each other, each with its own workspace."""
+    ids = [zipf(20000, 5000, k) for k in (1, 2)]
+    G = [sc.ScaledTensor.make(torch.randn(20000, 264, generator=gen(k), device="cuda").to(BF16), 1.0) for k in (1, 2)]
+    ws = [sc.Workspace(sc.scalify_workspace_bytes(sc.OP_EMBEDDING_GRAD, 20000, 264)) for _ in (1, 2)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    outs = [[sc.ScaledTensor.empty((5000, 264), F32) for _ in (1, 2)] for _ in range(5)]
+    torch.cuda.synchronize()
+    for k, out in enumerate(outs):
+        for i in (0, 1):
+            sc.scalify_scaled_embedding_grad(ids[i], G[i], out[i], ws[i], stream=streams[i] if k else None)
+        if k == 0:
+            torch.cuda.synchronize()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a.data, b.data) for out in outs[1:] for a, b in zip(outs[0], out))
+    assert ws[0].check_status() == 0 == ws[1].check_status()
+
+
 def test_grad_agrees_with_the_atomic_form():
     n, T, vocab, d = 512, 64, 100, 64
     ids = torch.randint(0, vocab, (n,), device="cuda")

@@ -288,3 +288,25 @@ def test_broadcast_rows():
         sc.scalify_scaled_add_rmsnorm_bwd(scaled(G, 1.0), None, scaled(H, 1.0), None, rinv, dX)
         want = p64.add_rmsnorm_bwd(G, 1.0, None, 0.0, H, 1.0, None, 1.0, rinv)
         assert bool(p64.close(dX.data, want["dX"], U * want["mag"]).all())
+
+
+def test_offsets_past_32_bits():
+    """Rows 2^27 elements apart: every array of both directions reaches past 2^31 elements."""
+    rows, d = 20, 264
+    base = torch.empty(rows * (1 << 27), dtype=BF16, device="cuda")
+    wide = base.view(rows, 1 << 27)
+    x, r, g = (torch.randn(rows, d, generator=gen(k), device="cuda").to(BF16) for k in (1, 2, 3))
+    results = []
+    for far in (False, True):
+        def place(k, src=None):
+            v = wide[:, 512 * k:512 * k + d] if far else torch.empty(rows, d, dtype=BF16, device="cuda")
+            if src is not None:
+                v.copy_(src)
+            return sc.ScaledTensor(v, torch.ones(1, device="cuda"))
+        X, R, G, H, Y, dX = place(0, x), place(1, r), place(2, g), place(3), place(4), place(5)
+        rinv = torch.empty(rows, device="cuda")
+        sc.scalify_scaled_add_rmsnorm(X, R, None, H, Y, rinv=rinv)
+        sc.scalify_scaled_add_rmsnorm_bwd(G, None, H, None, rinv, dX)
+        results.append([t.data.clone() for t in (H, Y, dX)])
+        assert torch.equal(X.data, x) and torch.equal(R.data, r) and torch.equal(G.data, g)
+    assert all(torch.equal(a, b) for a, b in zip(*results))

@@ -291,3 +291,18 @@ def test_overlapping_output_rows_are_refused():
     assert L.scalify_orthogonalize(R(arr(1, F, (4, 128))), 5, None, 0.0, R(over(2)), 16 * MB, 64 * MB, None) == SHAPE
     assert L.scalify_orthogonalize(R(arr(1, F, (2, 4, 128))), 5, None, 0.0, R(arr(2, B, (2, 4, 128), (256, 128, 1))), 16 * MB,
                                    64 * MB, None) == SHAPE
+
+
+def test_overlapping_column_slices_are_refused():
+    """Slices of one buffer may lie side by side (the GPU tests do that), not across one another or a row's end."""
+    B = sc.BF16
+    L = sc.lib()
+    cols = lambda mb, first, n=128, ld=512, dt=B, rows=4: arr(mb, dt, (rows, n), (ld, 1), offset=2 * first)  # noqa: E731
+    x = cols(1, 128)
+    for first in (8, 128, 136, 248):
+        assert norm_call(x, None, None, 1e-5, None, cols(1, first)) == ALIAS, first
+    assert norm_call(x, None, None, 1e-5, None, cols(1, 512 + 120)) == ALIAS     # begins a row later
+    assert norm_call(x, None, None, 1e-5, None, cols(1, 384, n=128, ld=504)) == ALIAS  # rows that drift
+    assert norm_call(cols(1, 0), None, None, 1e-5, None, cols(1, 400, n=128)) == ALIAS  # runs into the next row
+    assert L.scalify_scaled_embedding_lookup(8 * MB, 4, -1, R(cols(1, 0, rows=50)), 1.0, R(cols(1, 120)), None, None) == ALIAS
+    assert L.scalify_orthogonalize(R(cols(1, 0)), 5, None, 0.0, R(cols(1, 64)), 16 * MB, 64 * MB, None) == ALIAS
