@@ -373,7 +373,8 @@ int scalify_scaled_layernorm_bwd_delayed(const scalify_array* G, const scalify_a
  * residual stream, of R's dtype, which may be R's or X's own buffer (same row stride).  With R == NULL there is no
  * addition: H must be NULL and X is the stream that is normalised.  Y: any dtype.  Exactly one of Y and Ymx is given;
  * Ymx: rows of d = K elements, not transposed.  gamma: [d], F16/BF16/F32, or NULL.  rinv: optional fp32 [rows]
- * (device), needed by the backward call.  d <= 16384, any; rows may be strided.  A row of zeros gives zeros.
+ * (device), needed by the backward call.  d <= 16384, any; rows may be strided.  A row of zeros gives zeros if
+ * eps > 0.
  * status: optional DEVICE word (SCALIFY_DEV_BAD_SCALE).
  * Errors: NULL, DTYPE, SHAPE, ALIGNMENT, UNSUPPORTED (both Y and Ymx, transposed Ymx), VALUE (eps < 0), ALIAS (an
  * output overlapping an input other than as above, or a scale word shared with another array of the call).
@@ -612,7 +613,9 @@ int scalify_scaled_adam_step_cast(int n_tensors, const scalify_array* grads, sca
  * norm.  O is therefore a 16-bit array.
  *   X: [rows, cols] or [batch, rows, cols], any dtype; rows may be strided.  O: the same shape, F16 or BF16.
  *   O_s = 1 / kf(max(rows, cols)) (a matrix with singular values 1 has entries of about 1/sqrt(longer side)).
- *   A matrix of zeros gives zeros; one with an infinity or NaN gives NaN.  1 <= rows, cols <= 32768; 1 <= steps <= 16.
+ *   A matrix of zeros gives zeros; one with an infinity or NaN gives NaN (and SCALIFY_DEV_NONFINITE_STAT).  A norm
+ *   (of the data component, whose squares are fp32) below 2^-60 counts as zero, one above 2^63 as infinite.
+ *   1 <= rows, cols <= 32768; 1 <= steps <= 16.
  * Errors: NULL, DTYPE, SHAPE, ALIGNMENT, VALUE (eps < 0, a non-finite coefficient, steps), ALIAS, WORKSPACE.
  */
 int scalify_orthogonalize(const scalify_array* X, int steps, const float* coef, float eps, scalify_array* O,

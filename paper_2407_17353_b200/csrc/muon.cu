@@ -594,13 +594,16 @@ __global__ void __launch_bounds__(256) muon_momentum_kernel(const __grid_constan
     double s = 0.0;
     for (int i = threadIdx.x; i < p.parts; i += 32) s += p.partial[inst * kMaxParts + i];
     s = warp_sum_f64(s);
-    if (threadIdx.x == 0) s_scale = p.inv_sigma / (static_cast<float>(sqrt(s)) + p.eps);
+    // fp32 holds the squares of a matrix with 2^-60 <= norm <= 2^63; below that it counts as zeros, above as infinite
+    const float norm = static_cast<float>(sqrt(s));
+    const bool finite = norm <= 0x1p63f;
+    if (threadIdx.x == 0) s_scale = !finite ? __int_as_float(0x7fc00000) : norm < 0x1p-60f ? 0.f : p.inv_sigma / (norm + p.eps);
     if (threadIdx.x == 0 && blockIdx.x == 0) {
       const MuonFactors f = p.factors[inst];
       if (t.m) *t.m_scale = f.m_s;
       if (t.w_scale) *t.w_scale = f.w_s;
       if (t.wc_scale) *t.wc_scale = f.w_s;
-      if (!(sqrt(s) < 3.4e38)) atomicOr(p.status, static_cast<uint32_t>(SCALIFY_DEV_NONFINITE_STAT));
+      if (!finite) atomicOr(p.status, static_cast<uint32_t>(SCALIFY_DEV_NONFINITE_STAT));
     }
   }
   const MuonFactors f = p.factors[inst];

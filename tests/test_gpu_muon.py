@@ -84,14 +84,66 @@ def test_zeros_and_nan_stay_in_their_matrix():
     good = sc.ScaledTensor.make(X.clone(), 1.0)
     X[2, 3, 4] = float("nan")
     out = []
-    for x in (good, sc.ScaledTensor.make(X, 1.0)):
+    for x, eps in ((good, 0.0), (sc.ScaledTensor.make(X, 1.0), 0.0)):
         O = sc.ScaledTensor.empty((3, 150, 304), BF16)
         ws = sc.Workspace(sc.scalify_muon_workspace_bytes([x]))
-        sc.scalify_orthogonalize(x, O, ws)
+        sc.scalify_orthogonalize(x, O, ws, eps=eps)
         out.append((O.data, ws.check_status()))
     (a, sa), (b, sb) = out
     assert sa == 0 and sb == sc.DEV_NONFINITE_STAT
     assert bool((a[1] == 0).all()) and torch.equal(a[:2], b[:2]) and bool(b[2].isnan().all())
+
+
+def test_norms_beyond_the_range_of_fp32_squares():
+    """A norm below 2^-60 counts as zero and one above 2^63 as infinite, with eps = 0 as well; nothing in between is lost."""
+    X = torch.randn(4, 150, 304, generator=gen(5), device="cuda")
+    plain = X[1].clone()
+    for k, e in enumerate((-75, -40, 40, 62)):
+        X[k] = plain * 2.0 ** e
+    x, O = sc.ScaledTensor.make(X, 1.0), sc.ScaledTensor.empty((4, 150, 304), BF16)
+    ws = sc.Workspace(sc.scalify_muon_workspace_bytes([x]))
+    sc.scalify_orthogonalize(x, O, ws, eps=0.0)
+    assert ws.check_status() == sc.DEV_NONFINITE_STAT
+    o, o1 = O.data, sc.ScaledTensor.empty((150, 304), BF16)
+    sc.scalify_orthogonalize(sc.ScaledTensor.make(plain, 1.0), o1, ws, eps=0.0)
+    assert bool((o[0] == 0).all()) and torch.equal(o[1], o1.data) and torch.equal(o[2], o1.data) and bool(o[3].isnan().all())
+
+
+def test_calls_on_several_streams_at_once():
+    """Calls that run beside each other, each with its own workspace, give what they give one after the other."""
+    sizes = [(6, 500, 900), (40, 120, 90), (1, 1030, 700)]
+    Xs = [sc.ScaledTensor.make(matrices(*s, BF16, seed=i)[0], 1.0) for i, s in enumerate(sizes)]
+    streams = [torch.cuda.Stream() for _ in Xs]
+    work = [sc.Workspace(sc.scalify_muon_workspace_bytes([x])) for x in Xs]
+    outs = [[sc.ScaledTensor(strided(*s, BF16)[0], torch.zeros(1, device="cuda")) for s in sizes] for _ in range(5)]
+    torch.cuda.synchronize()
+    for k, O in enumerate(outs):
+        for x, o, ws, st in zip(Xs, O, work, streams):
+            sc.scalify_orthogonalize(x, o, ws, stream=st if k else None)
+        if k == 0:
+            torch.cuda.synchronize()
+    torch.cuda.synchronize()
+    for O in outs[1:]:
+        assert all(torch.equal(a.data, b.data) for a, b in zip(outs[0], O))
+    assert all(ws.check_status() == 0 for ws in work)
+
+
+def test_offsets_past_32_bits():
+    """Rows 2^27 elements apart: the last one lies past 2^31 elements, for the gradient as for the weights."""
+    base = torch.empty(20 * (1 << 27), dtype=BF16, device="cuda")
+    rows = base.view(20, 1 << 27)
+    X = torch.randn(20, 48, generator=gen(3), device="cuda").to(BF16)
+    rows[:, :48] = X
+    far, near = sc.ScaledTensor.make(rows[:, :48], 1.0), sc.ScaledTensor.make(X, 1.0)
+    O = sc.ScaledTensor.empty((20, 48), BF16)
+    P = sc.ScaledTensor(rows[:, 64:112], torch.zeros(1, device="cuda"))
+    ws = sc.Workspace(sc.scalify_muon_workspace_bytes([near]))
+    sc.scalify_orthogonalize(near, O, ws)
+    out = sc.ScaledTensor.empty((20, 48), BF16)
+    sc.scalify_orthogonalize(far, out, ws)
+    assert torch.equal(out.data, O.data)
+    sc.scalify_orthogonalize(near, P, ws)
+    assert torch.equal(P.data, O.data) and torch.equal(rows[:, :48], X)
 
 
 def test_other_coefficients():
