@@ -503,10 +503,11 @@ __device__ __forceinline__ int64_t lower_bound(const uint2* sorted, int64_t n, u
   return lo;
 }
 
-// Long runs: a block looks at eight chunks, one per warp, for one in which such a run begins, and adds up its partial
-// rows over 256 columns: every warp an equal share of the chunks, then the shares in order.
+// Long runs: one warp per chunk and 256 columns looks whether such a run begins in its chunk.  A run of a few parts it adds up
+// itself; one of many parts (a frequent token) is left to the whole block, whose warps take equal shares of its chunks.
+constexpr int kWarpParts = 8;
 template <int ODT>
-__global__ void __launch_bounds__(256, 4) embedding_segment_join_kernel(const EmbeddingArgs a, const SegmentArgs s) {
+__global__ void __launch_bounds__(256, 3) embedding_segment_join_kernel(const EmbeddingArgs a, const SegmentArgs s) {
   asm volatile("griddepcontrol.launch_dependents;");  // a programmatic dependent may set up while this grid runs
   asm volatile("griddepcontrol.wait;" ::: "memory");  // launched as a programmatic dependent: the grid before is complete
   constexpr int kAhead = 4;
@@ -528,37 +529,46 @@ __global__ void __launch_bounds__(256, 4) embedding_segment_join_kernel(const Em
       parts = same != 0xFFFFFFFFu ? __popc(same) : (lower_bound(s.pair, s.n, key + 1u) - 1) / s.chunk - h;
     }
   }
-  if (lane == 0) { s_parts[warp] = parts; s_key[warp] = key; }
-  if (!__syncthreads_or(parts > 0)) return;
   float fg, fa;
   output_factors(a, &fg, &fa);
+  float acc[kVec];
+  auto begin_of = [&](int64_t c) {  // slot 1 of chunk c
+    uint32_t w[kVec];
+    load_vec<SCALIFY_F32>(reinterpret_cast<const char*>(s.partial + (c * 2 + 1) * s.line), v, kVec, w);
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) acc[e] = __uint_as_float(w[e]);
+  };
+  auto add_parts = [&](int64_t c0, int64_t c1) {  // slots 0 of chunks [c0, c1)
+    for (int64_t c = c0; c < c1; c += kAhead) {
+      uint32_t w[kAhead][kVec];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (c + u < c1) load_vec<SCALIFY_F32>(reinterpret_cast<const char*>(s.partial + (c + u) * 2 * s.line), v, kVec, w[u]);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (c + u < c1) {
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) acc[e] += __uint_as_float(w[u][e]);
+        }
+    }
+  };
+  if (parts > 0 && parts <= kWarpParts && n > 0) {
+    begin_of(h);
+    add_parts(h + 1, h + 1 + parts);
+    finish_row<ODT>(a, key, v, fg, fa, acc);
+  }
+  if (lane == 0) { s_parts[warp] = parts; s_key[warp] = key; }
+  if (!__syncthreads_or(parts > kWarpParts)) return;
   for (int q = 0; q < 8; ++q) {
     const int64_t count = s_parts[q];
-    if (count == 0) continue;  // the same for every thread
+    if (count <= kWarpParts) continue;  // the same for every thread
     const int64_t hq = static_cast<int64_t>(blockIdx.x) * 8 + q, share = (count + 7) / 8;
-    const int64_t c0 = hq + 1 + warp * share, c1 = min(hq + 1 + count, c0 + share);
-    float acc[kVec];
+    const int64_t c0 = hq + 1 + warp * share;
 #pragma unroll
     for (int e = 0; e < kVec; ++e) acc[e] = 0.f;
     if (n > 0) {
-      if (warp == 0) {
-        uint32_t w[kVec];
-        load_vec<SCALIFY_F32>(reinterpret_cast<const char*>(s.partial + (hq * 2 + 1) * s.line), v, kVec, w);
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) acc[e] = __uint_as_float(w[e]);
-      }
-      for (int64_t c = c0; c < c1; c += kAhead) {
-        uint32_t w[kAhead][kVec];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-          if (c + u < c1) load_vec<SCALIFY_F32>(reinterpret_cast<const char*>(s.partial + (c + u) * 2 * s.line), v, kVec, w[u]);
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-          if (c + u < c1) {
-#pragma unroll
-            for (int e = 0; e < kVec; ++e) acc[e] += __uint_as_float(w[u][e]);
-          }
-      }
+      if (warp == 0) begin_of(hq);
+      add_parts(c0, min(hq + 1 + count, c0 + share));
     }
 #pragma unroll
     for (int e = 0; e < kVec; ++e) s_part[warp][lane * kVec + e] = acc[e];
