@@ -42,13 +42,8 @@ __device__ __forceinline__ void load_gamma(const void* gamma, int dt, int v, int
   const char* p = static_cast<const char*>(gamma);
   SCALIFY_DISPATCH_WIDE(dt, DT, {
     uint32_t w[kVec * ElemBytes<DT>::v / 4];
-    if (n >= kVec) {
-      ld_bytes<kVec * ElemBytes<DT>::v, false>(p + static_cast<int64_t>(v) * (kVec * ElemBytes<DT>::v), w);
-      decode_vec<DT, kVec>(w, f);
-    } else {
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) f[e] = e < n ? load_elem<DT>(p, static_cast<int64_t>(v) * kVec + e) : 0.f;
-    }
+    load_vec<DT>(p, v, n, w);
+    decode_vec<DT, kVec>(w, f);
   })
 }
 
@@ -225,7 +220,10 @@ __global__ void __launch_bounds__(BLOCK ? kBlockThreads : 32 * kWarpRows) add_rm
 // The launch bounds leave 128 registers a thread to the warp-per-row form (two blocks of eight warps per SM, which is
 // what covers the load latency there).  The block-per-row form with 2 vectors per thread holds the NEXT row's words in
 // registers while it works on the current one, so that the two barriers of a row do not leave the memory idle; the form
-// for very long rows has no registers left for that.
+// for very long rows has no registers left for that and asks the L2 for its next row instead (4096 rows of 8192, BF16:
+// 100 us without, 90 with; the request costs the other form 1 to 4 us and gains it nothing).
+// Measured (bytes of G, Gr, H, dX and its 8-bit copy): 8192 x 768 BF16 19.4 us with its second launch (instruction issue;
+// 57 MB), 4099 x 5120 with an fp32 stream 57.8 us, 5.4 TB/s; 4099 x 5004 60.2 us; 4096 x 8192 BF16 90 us, 3.4 TB/s.
 template <int GDT, int HDT, int VPT, bool BLOCK>
 __global__ void __launch_bounds__(BLOCK ? (VPT == 2 ? kPrefetchThreads : kBlockThreads) : 32 * kBwdRows,
                                   BLOCK ? 1 : kBwdWarpBlocks) add_rmsnorm_bwd_kernel(const RmsNormBwdArgs a) {
@@ -316,6 +314,15 @@ __global__ void __launch_bounds__(BLOCK ? (VPT == 2 ? kPrefetchThreads : kBlockT
       }
     }
   };
+  auto prefetch_row = [&](int64_t row) {  // as far as the L2: one request per array
+    if (lane < 3 && row < a.rows) {
+      const char* p = lane == 0 ? static_cast<const char*>(a.G) + row * a.g_ld * ElemBytes<GDT>::v
+                    : lane == 1 ? static_cast<const char*>(a.H) + row * a.h_ld * ElemBytes<HDT>::v
+                                : static_cast<const char*>(a.Gr) + row * a.gr_ld * ElemBytes<HDT>::v;
+      const uint32_t bytes = static_cast<uint32_t>(a.d * (lane == 0 ? ElemBytes<GDT>::v : ElemBytes<HDT>::v)) & ~15u;
+      if (lane < 2 || a.Gr) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
+    }
+  };
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
 #pragma unroll
@@ -325,6 +332,7 @@ __global__ void __launch_bounds__(BLOCK ? (VPT == 2 ? kPrefetchThreads : kBlockT
   }
   if (kPrefetch && first < a.rows) load_row(first, wg, wh, wr, rinv);
   for (int64_t row = first; row < a.rows; row += stride) {
+    if constexpr (kLean) prefetch_row(row + stride);
     uint32_t ng[VPT][GW], nh[VPT][HW], nr[VPT][HW];
     float nri = 0.f;
     if constexpr (kPrefetch) {
@@ -520,7 +528,7 @@ static int block_threads(int d, bool bwd) {
 }
 static int bwd_grid_cap(int d) {  // resident blocks, by the register budgets above
   if (d <= kBwdWarpMaxD) return sm_count() * kBwdWarpBlocks;
-  const int per_sm = kPrefetchThreads / block_threads(d, true);
+  const int per_sm = (block_vpt(d, true) == 2 ? kPrefetchThreads : kBlockThreads) / block_threads(d, true);
   return sm_count() * (per_sm < 1 ? 1 : per_sm);
 }
 size_t rmsnorm_bwd_ws_bytes(int64_t rows, int64_t d) {
