@@ -146,13 +146,17 @@ def test_calls_on_two_streams_at_once():
     ws = [sc.Workspace(sc.scalify_workspace_bytes(sc.OP_EMBEDDING_GRAD, 20000, 264)) for _ in (1, 2)]
     streams = [torch.cuda.Stream(), torch.cuda.Stream()]
     outs = [[sc.ScaledTensor.empty((5000, 264), F32) for _ in (1, 2)] for _ in range(5)]
-    torch.cuda.synchronize()
-    for k, out in enumerate(outs):
-        for i in (0, 1):
-            sc.scalify_scaled_embedding_grad(ids[i], G[i], out[i], ws[i], stream=streams[i] if k else None)
-        if k == 0:
-            torch.cuda.synchronize()
-    torch.cuda.synchronize()
+    # once alone, every buffer: the first result, and what the bounds-checking build learns of it while nothing runs
+    for stream in (None, streams):
+        for k, out in enumerate(outs):
+            for i in (0, 1):
+                if stream is None or k:
+                    sc.scalify_scaled_embedding_grad(ids[i], G[i], out[i], ws[i], stream=None if stream is None else stream[i])
+                if stream is None:
+                    torch.cuda.synchronize()
+                    if k:
+                        out[i].data.fill_(float("nan"))
+        torch.cuda.synchronize()
     assert all(torch.equal(a.data, b.data) for out in outs[1:] for a, b in zip(outs[0], out))
     assert ws[0].check_status() == 0 == ws[1].check_status()
 

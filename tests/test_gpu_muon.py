@@ -116,13 +116,17 @@ def test_calls_on_several_streams_at_once():
     streams = [torch.cuda.Stream() for _ in Xs]
     work = [sc.Workspace(sc.scalify_muon_workspace_bytes([x])) for x in Xs]
     outs = [[sc.ScaledTensor(strided(*s, BF16)[0], torch.zeros(1, device="cuda")) for s in sizes] for _ in range(5)]
-    torch.cuda.synchronize()
-    for k, O in enumerate(outs):
-        for x, o, ws, st in zip(Xs, O, work, streams):
-            sc.scalify_orthogonalize(x, o, ws, stream=st if k else None)
-        if k == 0:
-            torch.cuda.synchronize()
-    torch.cuda.synchronize()
+    # once alone, every buffer: the first result, and what the bounds-checking build learns of it while nothing runs
+    for beside in (False, True):
+        for k, O in enumerate(outs):
+            for x, o, ws, st in zip(Xs, O, work, streams):
+                if k or not beside:
+                    sc.scalify_orthogonalize(x, o, ws, stream=st if beside else None)
+                if not beside:
+                    torch.cuda.synchronize()
+                    if k:
+                        o.data.fill_(float("nan"))
+        torch.cuda.synchronize()
     for O in outs[1:]:
         assert all(torch.equal(a.data, b.data) for a, b in zip(outs[0], O))
     assert all(ws.check_status() == 0 for ws in work)
