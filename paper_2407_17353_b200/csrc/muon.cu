@@ -347,6 +347,8 @@ struct NsEngine {
 
 // One product of the whole batch: persistent CTAs (pairs).  On expiry of a wait the CTA records SCALIFY_DEV_TIMEOUT, drains
 // its copies and MMAs, frees its tensor memory and returns.
+// 12 x 768 x 2304: gram 21 us (tensor pipe active 63%), poly 14 (31%), update 33 (59%): about 8 us of each are the first
+// copies, the last tile's epilogue and the hand-over to the next product.
 template <int MODE, int NCTA>
 __global__ void __launch_bounds__(kNsThreads, 1) ns_product_kernel(const __grid_constant__ CUtensorMap map_a,
                                                                   const __grid_constant__ CUtensorMap map_b,
@@ -534,7 +536,8 @@ __device__ __forceinline__ void muon_vec(const MuonWords<GDT, MDT>& w, const Muo
 
 }  // namespace
 
-// |u|_F^2, one partial per block (fixed order within and between blocks), and the step's factors.
+// |u|_F^2, one partial per block (fixed order within and between blocks), and the step's factors.  12 x 768 x 2304 with an
+// E5M2 gradient and FP16 momentum: 22 us (64 MB).
 template <int GDT, int MDT>
 __global__ void __launch_bounds__(256) muon_norm_kernel(const __grid_constant__ MuonTable tab, const MuonPass p) {
   asm volatile("griddepcontrol.launch_dependents;");  // a programmatic dependent may set up while this grid runs
@@ -579,7 +582,8 @@ __global__ void __launch_bounds__(256) muon_norm_kernel(const __grid_constant__ 
 }
 
 // m' (stored once rounded) and Z_0 = u / (|u| + eps) / sigma in FP16, [S, L]; a 64 x 64 tile per block, turned over in shared
-// memory where the matrix is tall.  The new scale words are written here (nothing of this launch reads the old ones).
+// memory where the matrix is tall (12 x 768 x 2304: 28 us, 149 MB, 5.3 TB/s).  The new scale
+// words are written here (nothing of this launch reads the old ones).
 template <int GDT, int MDT>
 __global__ void __launch_bounds__(256) muon_momentum_kernel(const __grid_constant__ MuonTable tab, const MuonPass p) {
   asm volatile("griddepcontrol.launch_dependents;");  // a programmatic dependent may set up while this grid runs
@@ -649,7 +653,7 @@ __global__ void __launch_bounds__(256) muon_momentum_kernel(const __grid_constan
   }
 }
 
-// w' = fw w - fo Z (and its copy), or the orthogonal matrix itself.
+// w' = fw w - fo Z (and its copy), or the orthogonal matrix itself (12 x 768 x 2304, FP16 with an E4M3 copy: 25 us, 5.9 TB/s).
 __global__ void __launch_bounds__(256) muon_update_kernel(const __grid_constant__ MuonTable tab, const MuonPass p) {
   asm volatile("griddepcontrol.launch_dependents;");  // a programmatic dependent may set up while this grid runs
   __shared__ __align__(16) __half s_tile[kPreTile][kPreTile + 8];
@@ -816,7 +820,8 @@ static int launch_chain(const NsMatrix (&z)[2], const NsMatrix& A, const NsMatri
 
 // One launch or one per product?  The times of a step, in K blocks of a tile (about 0.3 us): a unit's share of the tiles,
 // and what comes between two products: a cluster barrier with a cold start of the ring (8 blocks), or a launch (18; more
-// on the host).  *size_log < 0: one launch per product.
+// on the host).  Five steps in one launch and in fifteen: 4 x 256 x 320 90 and 99 us, 4 x 512 x 512 115 and 125;
+// 16 x 512 x 1024 229 and 166, 12 x 768 x 2304 434 and 377.  *size_log < 0: one launch per product.
 template <int NCTA>
 static int choose_chain(const NsChain& c, int batch, int* size_log) {
   auto blocks = [](const NsProduct& p) { return static_cast<double>((p.K + kTK - 1) / kTK); };

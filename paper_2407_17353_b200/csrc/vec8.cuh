@@ -52,8 +52,9 @@ __device__ __forceinline__ uint32_t ld_small(const char* p) {
 
 // Raw words of vector v of a row (n = elements from its first one to the row's end; those past it read as zero).  The words
 // of a row's last, partial vector are loads of their own, and nothing is computed from them here: a row that is loaded ahead
-// is not waited for because its length is no multiple of eight (norm gradient, 4099 rows of 5004: 78 -> 60 us; BF16 throughout: 92 -> 51).  Stores stay element by
-// element: word by word they change nothing there and cost the 65536 x 1024 embedding gradient 3 us.
+// is not waited for because its length is no multiple of eight (norm gradient, 4099 rows of 5004: 78 -> 60 us; BF16
+// throughout: 92 -> 51).  Stores stay element by element: word by word they change nothing there and cost the 65536 x 1024
+// embedding gradient 3 us.
 template <int DT, bool STREAM = false>
 __device__ __forceinline__ void load_vec(const char* row, int64_t v, int n, uint32_t* w) {
   constexpr int BYTES = kVec * ElemBytes<DT>::v;
