@@ -525,7 +525,8 @@ int scalify_scaled_embedding_lookup(const int64_t* ids, int64_t n, int64_t paddi
  * Every row of dwte is written: a token that does not occur, and the padding token, get zeros (or the addend).
  * ids, padding_id, c as for the lookup (an unknown token sets SCALIFY_DEV_BAD_INDEX in the workspace status word and is
  * left out).  dY: [n,d] of any dtype; dwte: [vocab,d], F16/BF16/F32; addend: dwte's dtype and shape, or NULL, and may be
- * dwte's own buffer (same row stride: the gradient is then accumulated in place).  n may be 0.  n < 2^31, vocab <= 2^24.
+ * dwte's own buffer (same row stride: the gradient is then accumulated in place).  n may be 0.  n < 2^31 - 1,
+ * vocab <= 2^24, d <= 256 * 65535, (n/8 + 1) * ceil(d/256) < 2^34.
  * Workspace: SCALIFY_OP_EMBEDDING_GRAD (n, d).
  * Errors: NULL, DTYPE, SHAPE, ALIGNMENT, VALUE, ALIAS, WORKSPACE.
  */

@@ -172,6 +172,8 @@ def test_embedding_refusals():
     assert grad(c=0.0) == VALUE
     assert grad(ws=None) == WORKSPACE and grad(nb=4095) == WORKSPACE and grad(ws=16 * MB + 16) == WORKSPACE
     assert sc.scalify_workspace_bytes(sc.OP_EMBEDDING_GRAD, 1 << 20, 64) > (1 << 24)
+    assert grad(n=1, g=arr(1000, B, (1, 1 << 24)), dw=arr(2000, F, (1, 1 << 24)), ws=4000 * MB, nb=1 << 40) == SHAPE   # too many columns
+    assert grad(dw=arr(1, F, ((1 << 24) + 1, 64)), g=arr(1 << 20, B, (7, 64))) == SHAPE                            # too many tokens
 
 
 def test_token_ids_are_checked_by_the_binding():
