@@ -624,9 +624,15 @@ int scalify_orthogonalize(const scalify_array* X, int steps, const float* coef, 
 /* Bytes of workspace that the two calls need for this list of matrices (shapes only; >= 4096; 0 for a bad shape). */
 size_t scalify_muon_workspace_bytes(int n_tensors, const scalify_array* w);
 
-/* How a step's length goes with the matrix: factor = 1; sqrt(max(1, rows/cols)) (bounds the change of the output's
- * root mean square); 0.2 sqrt(max(rows, cols)) (the root mean square of an Adam step). */
-enum { SCALIFY_MUON_UNIT = 0, SCALIFY_MUON_SPECTRAL = 1, SCALIFY_MUON_RMS = 2 };
+/* How a step's length goes with the matrix: factor =
+ *   UNIT             1
+ *   SPECTRAL         sqrt(max(1, rows/cols)), for a weight stored [outputs, inputs] (a transposed B operand of the matmul)
+ *   SPECTRAL_IN_OUT  sqrt(max(1, cols/rows)), for a weight stored [inputs, outputs] (a plain B operand: Y = X W)
+ *   RMS              0.2 sqrt(max(rows, cols)), the root mean square of an Adam step
+ * The spectral ones are sqrt(max(1, outputs/inputs)): a layer with at least as many outputs as inputs then changes the root
+ * mean square of its output by at most about lr times that of its input.  They need to know which side is which, so weights
+ * of the two layouts go into calls of their own. */
+enum { SCALIFY_MUON_UNIT = 0, SCALIFY_MUON_SPECTRAL = 1, SCALIFY_MUON_RMS = 2, SCALIFY_MUON_SPECTRAL_IN_OUT = 4 };
 
 /*
  * Scaled Muon step over a list of matrices, beside scalify_scaled_adam_step for the other parameters.  In value space

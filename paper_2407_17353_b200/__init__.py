@@ -25,7 +25,7 @@ STAT_NONE, STAT_AMAX, STAT_L2 = 0, 1, 2
 OP_MATMUL, OP_RESCALE, OP_LAYERNORM_BWD, OP_ADAM, OP_STATISTIC, OP_CROSS_ENTROPY, OP_COLSUM, OP_MATMUL_SPLITK = (
     0, 1, 2, 3, 4, 5, 6, 7)
 OP_RMSNORM_BWD, OP_EMBEDDING_GRAD = 8, 9
-MUON_UNIT, MUON_SPECTRAL, MUON_RMS = 0, 1, 2
+MUON_UNIT, MUON_SPECTRAL, MUON_RMS, MUON_SPECTRAL_IN_OUT = 0, 1, 2, 4
 DEV_TIMEOUT, DEV_BAD_SCALE, DEV_NONFINITE_STAT, DEV_BAD_INDEX = 1, 2, 4, 8
 
 _DTYPE_CODE = {torch.float8_e4m3fn: E4M3, torch.float8_e5m2: E5M2, torch.float16: F16,
@@ -701,7 +701,9 @@ def scalify_scaled_muon_step(tensors: MuonTensors, ws: Workspace, *, lr: float, 
                              nesterov: bool = True, weight_decay: float = 0.0, steps: int = 5,
                              coef: Optional[Sequence[float]] = None, eps: float = 1e-7, factor: int = MUON_SPECTRAL,
                              stream=None) -> None:
-    """Muon step over the list: momentum, orthogonalisation, weight update and (optionally) its low-precision copy."""
+    """Muon step over the list: momentum, orthogonalisation, weight update and (optionally) its low-precision copy.
+    ``factor``: MUON_SPECTRAL is for weights stored [outputs, inputs] (``transB=True`` in the matmul); weights stored
+    [inputs, outputs], which the matmul takes as they are, want MUON_SPECTRAL_IN_OUT."""
     name = "scalify_scaled_muon_step"
     if tensors.n == 0:
         return

@@ -924,7 +924,8 @@ static int run_batch(const MuonTable& tab, int count, const MuonHyper& h, void* 
   p.status = view.status;
   for (int tall = 0; tall < 2; ++tall) {
     double kappa = 1.0;
-    if (h.factor == SCALIFY_MUON_SPECTRAL && tall) kappa = sqrt(static_cast<double>(s.L) / s.S);
+    // outputs/inputs: rows/cols of a weight stored [outputs, inputs], cols/rows of one stored [inputs, outputs]
+    if (h.factor == SCALIFY_MUON_SPECTRAL ? tall == 1 : h.factor == SCALIFY_MUON_SPECTRAL_IN_OUT && tall == 0) kappa = sqrt(static_cast<double>(s.L) / s.S);
     else if (h.factor == SCALIFY_MUON_RMS) kappa = 0.2 * sqrt(static_cast<double>(s.L));
     p.lr[tall] = static_cast<float>(static_cast<double>(h.lr) * kappa);
     p.p2_lr[tall] = p.lr[tall] > 0.f ? host_p2(p.lr[tall]) : 0.f;

@@ -1455,7 +1455,8 @@ int scalify_scaled_muon_step(int n_tensors, const scalify_array* grads, scalify_
   int rc = check_newton_schulz(steps, coef, eps, &h);
   if (rc) return rc;
   if (!(momentum >= 0.f && momentum < 1.f) || !(lr >= 0.f) || isinf(lr) || !(weight_decay >= 0.f) || isinf(weight_decay)) return SCALIFY_ERR_VALUE;
-  if (factor != SCALIFY_MUON_UNIT && factor != SCALIFY_MUON_SPECTRAL && factor != SCALIFY_MUON_RMS) return SCALIFY_ERR_VALUE;
+  if (factor != SCALIFY_MUON_UNIT && factor != SCALIFY_MUON_SPECTRAL && factor != SCALIFY_MUON_RMS && factor != SCALIFY_MUON_SPECTRAL_IN_OUT)
+    return SCALIFY_ERR_VALUE;
   h.decay = static_cast<float>(static_cast<double>(lr) * weight_decay);
   if (!(h.decay < 1.f)) return SCALIFY_ERR_VALUE;
   h.momentum = momentum; h.lr = lr; h.nesterov = nesterov ? 1 : 0; h.factor = factor;

@@ -308,3 +308,12 @@ def test_overlapping_column_slices_are_refused():
     assert norm_call(cols(1, 0), None, None, 1e-5, None, cols(1, 400, n=128)) == ALIAS  # runs into the next row
     assert L.scalify_scaled_embedding_lookup(8 * MB, 4, -1, R(cols(1, 0, rows=50)), 1.0, R(cols(1, 120)), None, None) == ALIAS
     assert L.scalify_orthogonalize(R(cols(1, 0)), 5, None, 0.0, R(cols(1, 64)), 16 * MB, 64 * MB, None) == ALIAS
+
+
+def test_muon_factors():
+    """Every documented factor passes the checks of arguments (the call then lacks its workspace); no other value does."""
+    L = sc.lib()
+    ls = [(sc.scalify_array * 1)(arr(1 + k, dt, (64, 96), scale=64 + 4 * k)) for k, dt in enumerate((sc.E5M2, sc.F16, sc.F16, sc.E4M3))]
+    call = lambda f: L.scalify_scaled_muon_step(1, *ls, 0.02, 0.95, 1, 0.0, 5, None, 1e-7, f, None, 0, None)  # noqa: E731
+    assert all(call(f) == WORKSPACE for f in (sc.MUON_UNIT, sc.MUON_SPECTRAL, sc.MUON_RMS, sc.MUON_SPECTRAL_IN_OUT))
+    assert all(call(f) == VALUE for f in (-1, 3, 5, 8))
