@@ -608,7 +608,9 @@ int scalify_scaled_adam_step_cast(int n_tensors, const scalify_array* grads, sca
  *   Z = U / (|U|_F + eps);   `steps` times:  A = Z Z^T,  Z = a Z + (b A + c A^2) Z    (on the shorter side, so that A is
  *   min(rows, cols) square);   O = Z
  * With (a, b, c) = (3.4445, -4.7750, 2.0315), used when coef is NULL, five steps bring the singular values to about
- * 1 +- 0.3, which is what the optimiser wants.  coef: HOST array of three floats.
+ * 1 +- 0.3, which is what the optimiser wants.  coef: HOST array of three floats, whose products have to fit FP16 whatever the
+ * matrix is: with m = 33/32 at first and m = 33/32 max |a x + b x^3 + c x^5| over x <= m after each step,
+ *   m <= 3.875  and  max |a + b x^2 + c x^4| over x <= m  <= 15.5      at the beginning of every step (else VALUE).
  * The products run on the tensor cores with FP16 operands at a power-of-two scale and fp32 accumulation; the iterates
  * are held in FP16 (11 bits), which the products square and multiply: O agrees with the definition to about 1e-3 of its
  * norm.  O is therefore a 16-bit array.
@@ -617,7 +619,7 @@ int scalify_scaled_adam_step_cast(int n_tensors, const scalify_array* grads, sca
  *   A matrix of zeros gives zeros; one with an infinity or NaN gives NaN (and SCALIFY_DEV_NONFINITE_STAT).  A norm
  *   (of the data component, whose squares are fp32) below 2^-60 counts as zero, one above 2^63 as infinite.
  *   1 <= rows, cols <= 32768; 1 <= steps <= 16.
- * Errors: NULL, DTYPE, SHAPE, ALIGNMENT, VALUE (eps < 0, a non-finite coefficient, steps), ALIAS, WORKSPACE.
+ * Errors: NULL, DTYPE, SHAPE, ALIGNMENT, VALUE (eps < 0, coefficients, steps), ALIAS, WORKSPACE.
  */
 int scalify_orthogonalize(const scalify_array* X, int steps, const float* coef, float eps, scalify_array* O,
                           void* workspace, size_t workspace_bytes, void* stream);

@@ -1368,12 +1368,43 @@ int matrix_of(const scalify_array* a, int64_t* rows, int64_t* cols, int64_t* ld)
   *rows = a->shape[0]; *cols = a->shape[1]; *ld = a->stride[0];
   return (*rows < 1 || *cols < 1 || *rows > kMuonMaxSide || *cols > kMuonMaxSide) ? SCALIFY_ERR_SHAPE : SCALIFY_OK;
 }
+// The largest |a + b x^2 + c x^4| (odd: |a x + b x^3 + c x^5|) for 0 <= x <= m: at an end, or where the derivative is zero.
+double largest_on(const double* k, double m, bool odd) {
+  const double a = k[0], b = k[1], c = k[2];
+  auto value = [&](double s) { return fabs((a + s * (b + s * c)) * (odd ? sqrt(s) : 1.0)); };  // s = x^2
+  double most = fmax(value(0.0), value(m * m));
+  auto inside = [&](double s) { if (s > 0.0 && s < m * m) most = fmax(most, value(s)); };
+  if (!odd) {
+    if (c != 0.0) inside(-b / (2.0 * c));
+  } else {  // a + 3 b s + 5 c s^2 = 0, by the form that loses no digits
+    const double disc = 9.0 * b * b - 20.0 * a * c;
+    if (disc >= 0.0) {
+      const double q = -0.5 * (3.0 * b + copysign(sqrt(disc), b));
+      if (c != 0.0) inside(q / (5.0 * c));
+      if (q != 0.0) inside(a / q);
+    }
+  }
+  return most;
+}
+// Whether A = Z Z^T and D = a I + b A + c A^2 stay inside FP16 at their scale of 2^12 (magnitudes below 16) whatever the
+// matrix is.  No entry exceeds the largest singular value, which is at most m: 1 at first, then the largest that a step makes
+// of any value up to m; a thirty-second more each time for the roundings.
+bool coefficients_fit(const float* coef, int steps) {
+  const double k[3] = {coef[0], coef[1], coef[2]};
+  double m = 33.0 / 32.0;
+  for (int i = 0; i < steps; ++i) {
+    if (!(m <= 3.875) || !(largest_on(k, m, false) <= 15.5)) return false;
+    m = 33.0 / 32.0 * largest_on(k, m, true);
+  }
+  return true;
+}
 int check_newton_schulz(int steps, const float* coef, float eps, MuonHyper* h) {
   static const float kDefault[3] = {3.4445f, -4.7750f, 2.0315f};
   const float* c = coef ? coef : kDefault;
   if (steps < 1 || steps > 16 || !(eps >= 0.f) || isinf(eps)) return SCALIFY_ERR_VALUE;
   for (int i = 0; i < 3; ++i)
     if (!isfinite(c[i])) return SCALIFY_ERR_VALUE;
+  if (!coefficients_fit(c, steps)) return SCALIFY_ERR_VALUE;
   h->steps = steps; h->eps = eps; h->a = c[0]; h->b = c[1]; h->c = c[2];
   return SCALIFY_OK;
 }

@@ -317,3 +317,41 @@ def test_muon_factors():
     call = lambda f: L.scalify_scaled_muon_step(1, *ls, 0.02, 0.95, 1, 0.0, 5, None, 1e-7, f, None, 0, None)  # noqa: E731
     assert all(call(f) == WORKSPACE for f in (sc.MUON_UNIT, sc.MUON_SPECTRAL, sc.MUON_RMS, sc.MUON_SPECTRAL_IN_OUT))
     assert all(call(f) == VALUE for f in (-1, 3, 5, 8))
+
+
+def test_newton_schulz_coefficients_that_leave_fp16_are_refused():
+    """The iterate's products are held in FP16 at a scale of 2^12.  The rule of the header, here by brute force over x, at both
+    sides of its border; a call that passes it lacks its workspace."""
+    L = sc.lib()
+    x, o = arr(1, sc.F32, (64, 96)), arr(2, sc.BF16, (64, 96))
+    words = [(sc.scalify_array * 1)(arr(1 + k, dt, (64, 96), scale=64 + 4 * k)) for k, dt in enumerate((sc.E5M2, sc.F16, sc.F16))]
+
+    def call(coef, steps):
+        c = (ctypes.c_float * 3)(*coef)
+        a = L.scalify_orthogonalize(R(x), steps, c, 1e-7, R(o), None, 0, None)
+        b = L.scalify_scaled_muon_step(1, *words, None, 0.02, 0.95, 1, 0.0, steps, c, 1e-7, 1, None, 0, None)
+        assert a == b and a in (VALUE, WORKSPACE)
+        return a == WORKSPACE
+
+    assert call((3.4445, -4.7750, 2.0315), 5) and call((3.4445, -4.7750, 2.0315), 16) and call((2.0, -1.5, 0.5), 16)
+    assert call((8.25, -23.5, 17.25), 1) and call((0.0, 0.0, 0.0), 3) and call((15.4, 0.0, -15.4), 1)
+    assert not call((20.0, -30.0, 12.0), 1)       # the diagonal of D
+    assert not call((-16.0, 0.0, 0.0), 1) and not call((0.0, 0.0, 16.0), 1)
+    assert call((15.4, -30.0, 15.0), 1) and not call((15.4, -30.0, 15.0), 2)   # the iterate grows to 4.5
+    assert call((1.5, 0.0, 0.0), 3) and not call((1.5, 0.0, 0.0), 16)
+    g = torch.Generator().manual_seed(0)
+    seen = [0, 0]
+    for i in range(400):
+        steps = 1 + i % 6
+        coef = [float(torch.tensor(v, dtype=torch.float32)) for v in (torch.randn(3, generator=g, dtype=torch.float64) * torch.tensor([5.0, 8.0, 5.0])).tolist()]
+        m, ok, near = 33 / 32, True, False
+        for _ in range(steps):
+            xs = torch.linspace(0, m, 20001, dtype=torch.float64)
+            d = coef[0] + coef[1] * xs ** 2 + coef[2] * xs ** 4
+            ok = ok and m <= 3.875 and float(d.abs().max()) <= 15.5
+            near = near or abs(m - 3.875) < 1e-3 or abs(float(d.abs().max()) - 15.5) < 1e-3
+            m = min(33 / 32 * float((xs * d).abs().max()), 1e6)
+        if not near:
+            assert call(coef, steps) == ok, (coef, steps)
+            seen[ok] += 1
+    assert min(seen) > 50, seen
