@@ -607,18 +607,16 @@ int launch_embedding_lookup(const EmbeddingArgs& a, int w_dt, cudaStream_t st) {
   return SCALIFY_OK;
 }
 
-// Sorted tokens per work item: the largest power of two that still gives the SMs several rounds of warps (long chunks
-// leave fewer partial rows, short ones more loads in flight).  8192 x 768: 71.9 us with 8, 72.7 with 16; 65536 x 1024: 101.5
-// with 8, 88.9 with 16.
-static int chunk_of(int64_t n, int64_t slabs) {
-  int chunk = kMaxChunk;
-  while (chunk > kMinChunk && (n + chunk - 1) / chunk * slabs < 64ll * sm_count()) chunk /= 2;
-  return chunk;
-}
+// Sorted tokens per work item: long chunks leave fewer partial rows, short ones more loads in flight.  The number of tokens
+// alone decides, so that the order of the sums does not depend on the row length or the GPU.  us with 8 and with 16:
+// 64 x 768 62.3 and 65.4, 1000 x 768 67.4 and 69.5, 8192 x 768 72.0 and 73.4; 16384 x 1024 56.1 and 53.5, 20000 x 2048 95.7
+// and 89.4, 32768 x 64 36.4 and 32.9, 65536 x 64 51.8 and 47.7, 65536 x 1024 100.4 and 87.4.
+constexpr int64_t kLongBatch = 16384;
+static int chunk_of(int64_t n) { return n < kLongBatch ? kMinChunk : kMaxChunk; }
 static int64_t pad256(int64_t n) { return (n + 255) / 256 * 256; }
 size_t embedding_grad_ws_bytes(int64_t n, int64_t d) {
   if (n < 0 || d < 1 || n > 0x7FFFFFFF || d > 0x7FFFFFFF) return kWsMin;
-  const int64_t slabs = (d + kSlab - 1) / kSlab, chunk = chunk_of(n, slabs), chunks = (n + chunk - 1) / chunk;
+  const int64_t slabs = (d + kSlab - 1) / kSlab, chunk = chunk_of(n), chunks = (n + chunk - 1) / chunk;
   return kWsHeader + kMarkBytes + static_cast<size_t>(pad256(8 * n)) * 2 + static_cast<size_t>(chunks) * 2 * slabs * kSlab * sizeof(float) + 256;
 }
 
@@ -681,7 +679,7 @@ int launch_embedding_grad(const EmbeddingArgs& a, int g_dt, void* ws, cudaStream
   se.pair = so.pair[(so.passes - 1) & 1];
   se.n = a.n; se.vocab = a.vocab;
   se.slabs = (a.d + kSlab - 1) / kSlab;
-  se.chunk = chunk_of(a.n, se.slabs);
+  se.chunk = chunk_of(a.n);
   se.chunks = (a.n + se.chunk - 1) / se.chunk;
   se.line = static_cast<int64_t>(se.slabs) * kSlab;
   se.partial = reinterpret_cast<float*>(p);
