@@ -527,7 +527,7 @@ int scalify_scaled_embedding_lookup(const int64_t* ids, int64_t n, int64_t paddi
  * left out).  dY: [n,d] of any dtype; dwte: [vocab,d], F16/BF16/F32; addend: dwte's dtype and shape, or NULL, and may be
  * dwte's own buffer (same row stride: the gradient is then accumulated in place).  n may be 0.  n < 2^31 - 1,
  * vocab <= 2^24, d <= 256 * 65535, (n/8 + 1) * ceil(d/256) < 2^34.
- * Workspace: SCALIFY_OP_EMBEDDING_GRAD (n, d).
+ * Workspace: SCALIFY_OP_EMBEDDING_GRAD (n, d); one for n tokens serves every batch of at most n (2 MB of it whatever n is).
  * Errors: NULL, DTYPE, SHAPE, ALIGNMENT, VALUE, ALIAS, WORKSPACE.
  */
 int scalify_scaled_embedding_grad(const int64_t* ids, int64_t n, int64_t padding_id, const scalify_array* dY, float c,

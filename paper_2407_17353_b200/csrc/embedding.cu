@@ -613,11 +613,16 @@ int launch_embedding_lookup(const EmbeddingArgs& a, int w_dt, cudaStream_t st) {
 // and 89.4, 32768 x 64 36.4 and 32.9, 65536 x 64 51.8 and 47.7, 65536 x 1024 100.4 and 87.4.
 constexpr int64_t kLongBatch = 16384;
 static int chunk_of(int64_t n) { return n < kLongBatch ? kMinChunk : kMaxChunk; }
+// Chunks that a workspace has room for: those of every batch of at most n tokens (just below kLongBatch there are more of them)
+static int64_t chunk_room(int64_t n) {
+  const int64_t own = (n + chunk_of(n) - 1) / chunk_of(n), below = kLongBatch / kMinChunk;
+  return n < kLongBatch || own > below ? own : below;
+}
 static int64_t pad256(int64_t n) { return (n + 255) / 256 * 256; }
 size_t embedding_grad_ws_bytes(int64_t n, int64_t d) {
   if (n < 0 || d < 1 || n > 0x7FFFFFFF || d > 0x7FFFFFFF) return kWsMin;
-  const int64_t slabs = (d + kSlab - 1) / kSlab, chunk = chunk_of(n), chunks = (n + chunk - 1) / chunk;
-  return kWsHeader + kMarkBytes + static_cast<size_t>(pad256(8 * n)) * 2 + static_cast<size_t>(chunks) * 2 * slabs * kSlab * sizeof(float) + 256;
+  const int64_t slabs = (d + kSlab - 1) / kSlab;
+  return kWsHeader + kMarkBytes + static_cast<size_t>(pad256(8 * n)) * 2 + static_cast<size_t>(chunk_room(n)) * 2 * slabs * kSlab * sizeof(float) + 256;
 }
 
 int launch_embedding_grad(const EmbeddingArgs& a, int g_dt, void* ws, cudaStream_t st) {

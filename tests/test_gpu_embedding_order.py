@@ -21,3 +21,19 @@ def test_a_column_does_not_depend_on_the_others(n):
         sc.scalify_scaled_embedding_grad(ids, sc.ScaledTensor.make(G[:, :d], 1.0), W, ws)
         out.append(W.data)
     assert torch.equal(out[0], out[2][:, :64]) and torch.equal(out[1], out[2][:, :520])
+
+
+def test_one_workspace_for_batches_of_any_length():
+    """A workspace of the longest batch, used for shorter ones in between."""
+    d = 264
+    ws = sc.Workspace(sc.scalify_workspace_bytes(sc.OP_EMBEDDING_GRAD, 17000, d))
+    G = torch.randn(17000, d, generator=gen(1), device="cuda").to(torch.bfloat16)
+    ids = zipf(17000, 500, 1)
+    for n in (17000, 16383, 3, 16384, 12000, 0):
+        out = []
+        for w in (ws, sc.Workspace(sc.scalify_workspace_bytes(sc.OP_EMBEDDING_GRAD, n, d))):
+            W = sc.ScaledTensor.empty((500, d), torch.float32)
+            sc.scalify_scaled_embedding_grad(ids[:n], sc.ScaledTensor.make(G[:n], 1.0), W, w)
+            assert w.check_status() == 0
+            out.append(W.data)
+        assert torch.equal(*out)

@@ -355,3 +355,10 @@ def test_newton_schulz_coefficients_that_leave_fp16_are_refused():
             assert call(coef, steps) == ok, (coef, steps)
             seen[ok] += 1
     assert min(seen) > 50, seen
+
+
+def test_embedding_workspace_of_the_largest_batch_serves_smaller_ones():
+    for d in (8, 768, 2048):
+        sizes = [sc.scalify_workspace_bytes(sc.OP_EMBEDDING_GRAD, n, d) for n in sorted({*range(0, 300000, 511), 16383, 16384, 16385,
+                                                                                         18943, 18944, 37887, 37888, 151551, 151552})]
+        assert sizes == sorted(sizes), d
