@@ -377,7 +377,8 @@ int scalify_scaled_layernorm_bwd_delayed(const scalify_array* G, const scalify_a
  * eps > 0.  The squares of H_d are fp32 (|H_d| up to 2^56; an infinity or NaN reaches its own row only).
  * status: optional DEVICE word (SCALIFY_DEV_BAD_SCALE).
  * Errors: NULL, DTYPE, SHAPE, ALIGNMENT, UNSUPPORTED (both Y and Ymx, transposed Ymx), VALUE (eps < 0), ALIAS (an
- * output overlapping an input other than as above, or a scale word shared with another array of the call).
+ * output, rinv and the exponents among them, overlapping another array of the call other than as above, or a scale word
+ * shared with another array of the call).
  */
 struct scalify_mx_array;
 int scalify_scaled_add_rmsnorm(const scalify_array* X, const scalify_array* R, const scalify_array* gamma, float eps,

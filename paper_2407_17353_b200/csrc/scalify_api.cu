@@ -104,10 +104,16 @@ static Span span_of(const scalify_array* a) {
   if (rows) { s.width = static_cast<uintptr_t>(cols) * es; s.period = static_cast<uintptr_t>(ld) * es; }
   return s;
 }
-// (column slices of one buffer, rows alike far apart, do not overlap: b's bytes are [off, off + width) of each of a's periods)
+// (column slices of one buffer, rows alike far apart, do not overlap: b's bytes are [off, off + width) of each of a's periods;
+// nor does an unbroken range in the gap between two rows)
 static bool overlap(Span a, Span b) {
   if (!(a.lo < b.hi && b.lo < a.hi)) return false;
-  if (a.period == 0 || a.period != b.period) return true;
+  if (a.period == 0) std::swap(a, b);
+  if (a.period == 0 || (b.period != 0 && a.period != b.period)) return true;
+  if (b.period == 0) {
+    if (b.lo < a.lo) return true;
+    b.width = b.hi - b.lo;
+  }
   const uintptr_t off = a.lo <= b.lo ? (b.lo - a.lo) % a.period : (a.period - (a.lo - b.lo) % a.period) % a.period;
   return off < a.width || off + b.width > a.period;
 }
@@ -117,6 +123,12 @@ static bool disjoint_or_same(const scalify_array* out, int64_t out_ld, const sca
   if (!in || !overlap(span_of(out), span_of(in))) return true;
   return out->data == in->data && out->dtype == in->dtype && out_ld == in_ld;
 }
+// n plain elements of es bytes (a null pointer spans nothing)
+static Span span_of(const void* p, int64_t n, int es) {
+  const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
+  return p ? Span{lo, lo + static_cast<uintptr_t>(n) * es, 0, 0} : Span{0, 0, 0, 0};
+}
+static bool disjoint(const scalify_array* a, Span b) { return !a || !overlap(span_of(a), b); }
 static bool disjoint(const scalify_array* a, const scalify_array* b) { return !a || !b || !overlap(span_of(a), span_of(b)); }
 // An output's rows may not overlap one another.
 static bool rows_apart(int64_t rows, int64_t cols, int64_t ld) { return rows <= 1 || ld >= cols; }
@@ -571,6 +583,10 @@ int scalify_scaled_add_rmsnorm(const scalify_array* X, const scalify_array* R, c
     if (as_rows(Y, &r2, &d2, &a.y_ld) || r2 != a.rows || d2 != d || !rows_apart(r2, d, a.y_ld)) return SCALIFY_ERR_SHAPE;
   }
   if (!disjoint(out, X) || !disjoint(out, R) || !disjoint(out, H) || !disjoint(out, gamma)) return SCALIFY_ERR_ALIAS;
+  const Span s_rinv = span_of(rinv, a.rows, 4), s_sf = span_of(a.sf, Ymx ? static_cast<int64_t>(mx_sf_bytes(a.rows, d)) : 0, 1);
+  for (const scalify_array* t : {X, R, gamma, static_cast<const scalify_array*>(H), out})
+    if (!disjoint(t, s_rinv) || !disjoint(t, s_sf)) return SCALIFY_ERR_ALIAS;
+  if (overlap(s_rinv, s_sf)) return SCALIFY_ERR_ALIAS;
   {
     const float* outs[2] = {H ? H->scale : nullptr, out->scale};
     const float* ins[3] = {X->scale, R ? R->scale : nullptr, gamma ? gamma->scale : nullptr};
@@ -637,6 +653,8 @@ int scalify_scaled_add_rmsnorm_bwd(const scalify_array* G, const scalify_array* 
   for (const scalify_array* o : {static_cast<const scalify_array*>(dXq), static_cast<const scalify_array*>(dgamma)})
     if (o && (!disjoint(o, G) || !disjoint(o, Gr) || !disjoint(o, H) || !disjoint(o, gamma))) return SCALIFY_ERR_ALIAS;
   if (!disjoint(dXq, dgamma)) return SCALIFY_ERR_ALIAS;
+  const Span s_rinv = span_of(rinv, a.rows, 4);
+  if (!disjoint(dX, s_rinv) || !disjoint(dXq, s_rinv) || !disjoint(dgamma, s_rinv)) return SCALIFY_ERR_ALIAS;
   {
     const float* outs[3] = {dX->scale, dXq ? dXq->scale : nullptr, dgamma ? dgamma->scale : nullptr};
     const float* ins[5] = {G->scale, Gr ? Gr->scale : nullptr, H->scale, gamma ? gamma->scale : nullptr, stat_in};
@@ -1253,7 +1271,7 @@ int scalify_scaled_embedding_lookup(const int64_t* ids, int64_t n, int64_t paddi
   const int64_t d = wte->shape[1];
   if (d < 1 || d > 0x7FFFFFF0 || wte->shape[0] < 1 || Y->shape[0] != n || Y->shape[1] != d || !rows_apart(n, d, Y->stride[0])) return SCALIFY_ERR_SHAPE;
   if (n == 0) return SCALIFY_OK;
-  if (!disjoint(wte, Y)) return SCALIFY_ERR_ALIAS;
+  if (!disjoint(wte, Y) || !disjoint(Y, span_of(ids, n, 8))) return SCALIFY_ERR_ALIAS;
   if (Y->scale && Y->scale == wte->scale) return SCALIFY_ERR_ALIAS;
   a.ids = reinterpret_cast<const long long*>(ids);
   a.n = n; a.vocab = wte->shape[0]; a.padding_id = padding_id; a.d = static_cast<int>(d);
@@ -1281,7 +1299,7 @@ int scalify_scaled_embedding_grad(const int64_t* ids, int64_t n, int64_t padding
     if (rc) return rc;
   }
   if (dY->ndim != 2 || dY->shape[0] != n || dY->shape[1] != d) return SCALIFY_ERR_SHAPE;
-  if (n > 0 && !disjoint(dwte, dY)) return SCALIFY_ERR_ALIAS;
+  if (n > 0 && (!disjoint(dwte, dY) || !disjoint(dwte, span_of(ids, n, 8)))) return SCALIFY_ERR_ALIAS;
   if (addend) {
     rc = check_array(addend);
     if (rc) return rc;

@@ -362,3 +362,33 @@ def test_embedding_workspace_of_the_largest_batch_serves_smaller_ones():
         sizes = [sc.scalify_workspace_bytes(sc.OP_EMBEDDING_GRAD, n, d) for n in sorted({*range(0, 300000, 511), 16383, 16384, 16385,
                                                                                          18943, 18944, 37887, 37888, 151551, 151552})]
         assert sizes == sorted(sizes), d
+
+
+def test_outputs_over_the_plain_vectors_of_a_call_are_refused():
+    """rinv, the exponent bytes and the token ids are memory like any other: no output may lie over them, nor they over an input."""
+    B, F, Q = sc.BF16, sc.F32, sc.E4M3
+    L = sc.lib()
+    x, r, h, y, gam = arr(1, B, (4, 128)), arr(2, B, (4, 128)), arr(3, B, (4, 128)), arr(4, Q, (4, 128)), arr(5, F, (128,))
+
+    def fwd(rinv, Ymx=None):
+        return L.scalify_scaled_add_rmsnorm(R(x), R(r), R(gam), 1e-5, R(h), None if Ymx else R(y), ctypes.addressof(Ymx) if Ymx else None,
+                                            rinv, None, None)
+    for mb in (1, 2, 3, 4, 5):
+        assert fwd(mb * MB) == ALIAS and fwd(mb * MB - 12) == ALIAS and fwd(mb * MB + 500) == ALIAS, mb
+    m = lambda data, sf: sc.scalify_mx_array(data, Q, 4, 128, sf, None, 0)  # noqa: E731
+    assert fwd(4 * MB, m(4 * MB, 6 * MB)) == ALIAS and fwd(6 * MB + 1000, m(4 * MB, 6 * MB)) == ALIAS   # over data, exponents
+    for mb in (1, 2, 3, 4, 5):
+        assert fwd(8 * MB, m(4 * MB, mb * MB)) == ALIAS, mb
+    g, dx = arr(1, B, (4, 128)), arr(3, B, (4, 128))
+    for over in (dict(rinv=3 * MB), dict(rinv=4 * MB + 16, dXq=arr(4, sc.E5M2, (4, 128))), dict(rinv=6 * MB, dg=arr(6, F, (128,)))):
+        assert norm_bwd(G=g, H=r, dX=dx, **over) == ALIAS
+    # in the gap between the rows of dX it touches nothing: the call gets as far as its missing workspace
+    wide = arr(3, B, (4, 128), (512, 1))
+    assert norm_bwd(G=g, H=r, dX=wide, rinv=3 * MB + 256, stat=1) == WORKSPACE
+    assert norm_bwd(G=g, H=r, dX=wide, rinv=3 * MB + 1024 - 16, stat=1) == WORKSPACE
+    for off in (-4, 0, 252, 1024 - 12, 1024, 3 * 1024 + 252):
+        assert norm_bwd(G=g, H=r, dX=wide, rinv=3 * MB + off, stat=1) == ALIAS, off
+    w = arr(1, B, (50, 64))
+    assert L.scalify_scaled_embedding_lookup(2 * MB, 7, -1, R(w), 1.0, R(arr(2, B, (7, 64))), None, None) == ALIAS
+    assert L.scalify_scaled_embedding_grad(1 * MB + 64, 7, -1, R(arr(2, B, (7, 64))), 1.0, None, R(arr(1, F, (50, 64))), 16 * MB, 64 * MB,
+                                           None) == ALIAS
