@@ -648,7 +648,7 @@ enum { SCALIFY_MUON_UNIT = 0, SCALIFY_MUON_SPECTRAL = 1, SCALIFY_MUON_RMS = 2, S
  *   grads[i]: [rows, cols], any dtype; m[i]: F16 or F32; w[i]: F16, BF16 or F32; w_cast[i] (or w_cast == NULL): E4M3, E5M2,
  *   F16 or BF16, receives cast(stored w') with w'_s, as for scalify_scaled_adam_step_cast.  Row strides are free; one
  *   dtype per list.  m and w (data and scale words) are updated in place; all their scale words are required and
- *   distinct, and none is a gradient's.
+ *   distinct, and none is a gradient's; their data do not overlap each other or a gradient (gradients may share memory).
  *   0 <= momentum < 1;  lr >= 0;  0 <= lr*weight_decay < 1.  Matrices of one shape (or transposed) run as one batch.
  * Errors: NULL, DTYPE, SHAPE, ALIGNMENT, VALUE, ALIAS, WORKSPACE (scalify_muon_workspace_bytes of w).
  */

@@ -1451,6 +1451,25 @@ void list_shapes(int n, const scalify_array* w, MuonTensor* out) {
     for (int64_t j = 0; j < b; ++j, ++k) { out[k].rows = static_cast<int>(w[i].shape[nd - 2]); out[k].cols = static_cast<int>(w[i].shape[nd - 1]); }
   }
 }
+// Every momentum, weight and copy of the lists apart from everything else in them (gradients may share memory).
+int check_lists_apart(int n, const scalify_array* grads, const scalify_array* m, const scalify_array* w, const scalify_array* w_cast) {
+  struct Item { Span s; bool written; };
+  Item* items = new (std::nothrow) Item[4 * static_cast<size_t>(n)];
+  struct Free { Item* p; ~Free() { delete[] p; } } free_items{items};
+  if (!items) return SCALIFY_ERR_WORKSPACE;
+  Item* end = items;
+  for (int i = 0; i < n; ++i) {
+    *end++ = Item{span_of(&grads[i]), false};
+    *end++ = Item{span_of(&m[i]), true};
+    *end++ = Item{span_of(&w[i]), true};
+    if (w_cast) *end++ = Item{span_of(&w_cast[i]), true};
+  }
+  std::sort(items, end, [](const Item& a, const Item& b) { return a.s.lo < b.s.lo; });
+  for (Item* a = items; a != end; ++a)
+    for (Item* b = a + 1; b != end && b->s.lo < a->s.hi; ++b)
+      if ((a->written || b->written) && overlap(a->s, b->s)) return SCALIFY_ERR_ALIAS;
+  return SCALIFY_OK;
+}
 }  // namespace
 
 size_t scalify_muon_workspace_bytes(int n_tensors, const scalify_array* w) {
@@ -1534,9 +1553,6 @@ int scalify_scaled_muon_step(int n_tensors, const scalify_array* grads, scalify_
     if (w_cast && (matrix_of(&w_cast[i], &r2, &c2, &t.wc_ld) || r2 != rows || c2 != cols)) return SCALIFY_ERR_SHAPE;
     if (!rows_apart(rows, cols, t.w_ld) || !rows_apart(rows, cols, t.m_ld) || (w_cast && !rows_apart(rows, cols, t.wc_ld))) return SCALIFY_ERR_SHAPE;
     const scalify_array* wc = w_cast ? &w_cast[i] : nullptr;
-    if (!disjoint(&m[i], &grads[i]) || !disjoint(&w[i], &grads[i]) || !disjoint(&m[i], &w[i]) || !disjoint(wc, &grads[i]) ||
-        !disjoint(wc, &m[i]) || !disjoint(wc, &w[i]))
-      return SCALIFY_ERR_ALIAS;
     t.g = grads[i].data; t.g_dt = static_cast<int8_t>(grads[i].dtype); t.g_scale = grads[i].scale;
     t.m = m[i].data; t.m_dt = static_cast<int8_t>(m[i].dtype); t.m_scale = m[i].scale;
     t.w = w[i].data; t.w_dt = static_cast<int8_t>(w[i].dtype); t.w_scale = w[i].scale;
@@ -1552,6 +1568,8 @@ int scalify_scaled_muon_step(int n_tensors, const scalify_array* grads, scalify_
   for (int i = 0; i < n_tensors; ++i)
     if (grads[i].scale && std::binary_search(words, words + n_words, static_cast<const void*>(grads[i].scale))) return SCALIFY_ERR_ALIAS;
   if (n_tensors == 0) return SCALIFY_OK;
+  rc = check_lists_apart(n_tensors, grads, m, w, w_cast);
+  if (rc) return rc;
   rc = check_ws(workspace, workspace_bytes, muon_ws_bytes(n_tensors, list.p));
   if (rc) return rc;
   return launch_muon(n_tensors, list.p, h, workspace, static_cast<cudaStream_t>(stream));

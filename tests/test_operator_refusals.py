@@ -392,3 +392,30 @@ def test_outputs_over_the_plain_vectors_of_a_call_are_refused():
     assert L.scalify_scaled_embedding_lookup(2 * MB, 7, -1, R(w), 1.0, R(arr(2, B, (7, 64))), None, None) == ALIAS
     assert L.scalify_scaled_embedding_grad(1 * MB + 64, 7, -1, R(arr(2, B, (7, 64))), 1.0, None, R(arr(1, F, (50, 64))), 16 * MB, 64 * MB,
                                            None) == ALIAS
+
+
+def test_muon_lists_whose_matrices_overlap_are_refused():
+    """Outputs of one entry over anything of another entry (the same matrix twice among them); gradients may be shared, and
+    column slices of one buffer lie beside each other."""
+    L = sc.lib()
+    H, Q, G = sc.F16, sc.E4M3, sc.E5M2
+
+    def call(make, n=3):
+        ls, word = [], iter(range(64, 4096, 4))
+        for k, dt in enumerate((G, H, H, Q)):
+            a = (sc.scalify_array * n)()
+            for i in range(n):
+                a[i] = make("gmwc"[k], i, dt, next(word)) or arr(1 + 8 * k + i, dt, (64, 96), scale=next(word))
+            ls.append(a)
+        return L.scalify_scaled_muon_step(n, *ls, 0.02, 0.95, 1, 0.0, 5, None, 1e-7, 1, None, 0, None)
+    at = lambda which, index, mb, off=0: (lambda k, i, dt, word: arr(mb, dt, (64, 96), scale=word, offset=off) if (k, i) == (which, index) else None)  # noqa: E731,E501
+    assert call(lambda *a: None) == WORKSPACE
+    for which, base in (("m", 9), ("w", 17), ("c", 25)):
+        for other in (1, 9, 17, 25):       # entry 2's output over entry 0's gradient, momentum, weight, copy
+            assert call(at(which, 2, other)) == ALIAS, (which, other)
+        assert call(at(which, 2, base, 4096)) == ALIAS and call(at(which, 0, base + 2, -16)) == ALIAS
+    assert call(at("g", 2, 9)) == ALIAS                 # a gradient over another entry's momentum
+    assert call(at("g", 2, 1)) == WORKSPACE             # one gradient for two entries
+    cols = lambda first: (lambda k, i, dt, word: arr(17, dt, (64, 96), (512, 1), scale=word, offset=2 * first(i)) if k == "w" else None)  # noqa: E731,E501
+    assert call(cols(lambda i: 96 * i)) == WORKSPACE    # three slices side by side
+    assert call(cols(lambda i: 88 * i)) == ALIAS
