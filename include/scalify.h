@@ -374,7 +374,7 @@ int scalify_scaled_layernorm_bwd_delayed(const scalify_array* G, const scalify_a
  * addition: H must be NULL and X is the stream that is normalised.  Y: any dtype.  Exactly one of Y and Ymx is given;
  * Ymx: rows of d = K elements, not transposed.  gamma: [d], F16/BF16/F32, or NULL.  rinv: optional fp32 [rows]
  * (device), needed by the backward call.  d <= 16384, any; rows may be strided.  A row of zeros gives zeros if
- * eps > 0.  The squares of H_d are fp32 (|H_d| up to 2^56; an infinity or NaN reaches its own row only).
+ * eps > 0; with no rows at all the output scale words alone are written.  The squares of H_d are fp32 (|H_d| up to 2^56; an infinity or NaN reaches its own row only).
  * status: optional DEVICE word (SCALIFY_DEV_BAD_SCALE).
  * Errors: NULL, DTYPE, SHAPE, ALIGNMENT, UNSUPPORTED (both Y and Ymx, transposed Ymx), VALUE (eps < 0), ALIAS (an
  * output, rinv and the exponents among them, overlapping another array of the call other than as above, or a scale word
@@ -511,7 +511,7 @@ int scalify_scaled_embedding_bwd(const int64_t* ids, int64_t n, int64_t seq_len,
  *   Y_s = wte_s * p2(c),   Y_d[i] = cast(wte_d[ids[i]] * (c / p2(c)))
  * ids: DEVICE int64 [n].  A token equal to padding_id gives a row of zeros (INT64_MIN: no padding); any other token
  * outside [0, vocab) does too, and sets SCALIFY_DEV_BAD_INDEX in *status (optional DEVICE word).  wte: [vocab,d] of any
- * dtype; Y: [n,d] of any dtype; any d; rows may be strided.
+ * dtype; Y: [n,d] of any dtype; any d; rows may be strided.  n may be 0: Y's scale word alone is written.
  * Errors: NULL, DTYPE, SHAPE, ALIGNMENT, VALUE (c not a positive normal number), ALIAS.
  */
 int scalify_scaled_embedding_lookup(const int64_t* ids, int64_t n, int64_t padding_id, const scalify_array* wte, float c,

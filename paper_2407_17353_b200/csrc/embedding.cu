@@ -600,7 +600,7 @@ __global__ void __launch_bounds__(256, 3) embedding_segment_join_kernel(const Em
 // ------------------------------------------------------------------------------------------------- launches
 int launch_embedding_lookup(const EmbeddingArgs& a, int w_dt, cudaStream_t st) {
   const int n_vec = (a.d + kVec - 1) / kVec, parts = (n_vec + 32 * kLookupVpt - 1) / (32 * kLookupVpt);
-  const int64_t blocks = (a.n * parts + 7) / 8;
+  const int64_t blocks = a.n > 0 ? (a.n * parts + 7) / 8 : 1;  // (an empty batch still has its scale word written)
   if (blocks > 0x7FFFFFFF) return SCALIFY_ERR_SHAPE;
   SCALIFY_DISPATCH_DTYPE(w_dt, WDT, embedding_lookup_kernel<WDT><<<static_cast<unsigned>(blocks), 256, 0, st>>>(a, parts))
   SCALIFY_CUDA_TRY(cudaGetLastError());

@@ -561,7 +561,7 @@ size_t rmsnorm_bwd_ws_bytes(int64_t rows, int64_t d) {
 int launch_add_rmsnorm(const RmsNormArgs& a, int x_dt, int h_dt, cudaStream_t st) {
   const bool block = a.d > kWarpMaxD;
   const int n_vec = (a.d + kVec - 1) / kVec;
-  const int64_t rows = a.sf ? (a.rows + 255) / 256 * 256 : a.rows;
+  const int64_t rows = a.sf ? (a.rows + 255) / 256 * 256 : a.rows > 0 ? a.rows : 1;  // (no rows: the scale words alone are written)
   const int threads = block ? block_threads(a.d, false) : 32 * kWarpRows, vpt = block_vpt(a.d, false);
   const unsigned grid = static_cast<unsigned>(block ? rows : (rows + kWarpRows - 1) / kWarpRows);
   const size_t smem = 0;

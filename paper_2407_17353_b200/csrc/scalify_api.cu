@@ -593,7 +593,6 @@ int scalify_scaled_add_rmsnorm(const scalify_array* X, const scalify_array* R, c
     rc = check_scale_words(outs, 2, ins, 3);
     if (rc) return rc;
   }
-  if (a.rows == 0) return SCALIFY_OK;
   a.d = static_cast<int>(d);
   a.eps = eps;
   a.X = X->data; a.x_scale = X->scale;
@@ -1263,6 +1262,7 @@ int scalify_scaled_embedding_lookup(const int64_t* ids, int64_t n, int64_t paddi
   int rc = check_array(wte);
   if (!rc && !Y) rc = SCALIFY_ERR_NULL;
   if (!rc && n != 0) rc = check_array(Y);  // (an empty batch may have no memory)
+  if (!rc && !valid_dtype(Y->dtype)) rc = SCALIFY_ERR_DTYPE;
   if (rc) return rc;
   if (!ids && n > 0) return SCALIFY_ERR_NULL;
   EmbeddingArgs a = {};
@@ -1270,7 +1270,6 @@ int scalify_scaled_embedding_lookup(const int64_t* ids, int64_t n, int64_t paddi
   if (wte->ndim != 2 || Y->ndim != 2 || n < 0 || n > 0x7FFFFFFF) return SCALIFY_ERR_SHAPE;
   const int64_t d = wte->shape[1];
   if (d < 1 || d > 0x7FFFFFF0 || wte->shape[0] < 1 || Y->shape[0] != n || Y->shape[1] != d || !rows_apart(n, d, Y->stride[0])) return SCALIFY_ERR_SHAPE;
-  if (n == 0) return SCALIFY_OK;
   if (!disjoint(wte, Y) || !disjoint(Y, span_of(ids, n, 8))) return SCALIFY_ERR_ALIAS;
   if (Y->scale && Y->scale == wte->scale) return SCALIFY_ERR_ALIAS;
   a.ids = reinterpret_cast<const long long*>(ids);
