@@ -612,9 +612,14 @@ int scalify_scaled_adam_step_cast(int n_tensors, const scalify_array* grads, sca
  * 1 +- 0.3, which is what the optimiser wants.  coef: HOST array of three floats, whose products have to fit FP16 whatever the
  * matrix is: with m = 33/32 at first and m = 33/32 max |a x + b x^3 + c x^5| over x <= m after each step,
  *   m <= 3.875  and  max |a + b x^2 + c x^4| over x <= m  <= 15.5      at the beginning of every step (else VALUE).
- * The products run on the tensor cores with FP16 operands at a power-of-two scale and fp32 accumulation; the iterates
- * are held in FP16 (11 bits), which the products square and multiply: O agrees with the definition to about 1e-3 of its
- * norm.  O is therefore a 16-bit array.
+ * The products run on the tensor cores with FP16 operands at a power-of-two scale and fp32 accumulation, and the iterates
+ * are held in FP16 (11 bits).  O is therefore a 16-bit array, and its error is ABSOLUTE where the matrix has directions with
+ * little or nothing in them: what a rounding leaves there every step multiplies by a.  In the Frobenius norm, for |a| >= 1 and
+ * results whose singular values are about 1,
+ *   |O - definition| <= 2^-11 |a|^steps + 3e-3 |O|         (0.24 + 3e-3 |O| for the default; measured: half the first term)
+ * so 1e-3 to 4e-3 of the norm for a full-rank matrix of some hundred rows, but a seventh of it for a matrix of rank one
+ * (the gradient of one token).  The error is spread over all directions: with some hundred of them none gets more than 0.03
+ * of the 1 that the occupied ones have.
  *   X: [rows, cols] or [batch, rows, cols], any dtype; rows may be strided.  O: the same shape, F16 or BF16.
  *   O_s = 1 / kf(max(rows, cols)) (a matrix with singular values 1 has entries of about 1/sqrt(longer side)).
  *   A matrix of zeros gives zeros; one with an infinity or NaN gives NaN (and SCALIFY_DEV_NONFINITE_STAT).  A norm
