@@ -16,10 +16,9 @@
 //   gram:   A_d = (sigma^2 2^12) Z_d Z_d^T            symmetric: tiles on and above the diagonal
 //   poly:   D_d = (c 2^-12) A_d A_d^T + b A_d + 2^12 a I   likewise; b A_d + .. is added to the fp32 accumulator
 //   update: Z_d <- 2^-12 D_d Z_d                       Z_d is the MN-major operand: no transposed copy
-// The blocks of A and D below the diagonal: stored as mirror images where the symmetric products take more than one round of
-// tiles (the stores then run beside the next tile's products); else not stored, and read as MN-major operands from above the
-// diagonal (the layout is a matter of each K block's copies and descriptors).  4 x 8192 x 2048: 1.98 ms stored, 2.05 to 2.23
-// read; 12 x 768 x 2304, one round: 403 us stored (all CTAs write at once at the end of a product), 397 us read.
+// The blocks of A and D below the diagonal are not stored: they are read as MN-major operands from above it (the layout is a
+// matter of each K block's copies and descriptors).  Storing them as mirror images was slower at every size, in turns on one
+// GPU: 4 x 8192 x 2048 1.2 %, 96 x 1024 x 1024 2.6, 8 x 1280 x 2560 3.8, 12 x 768 x 2304 4.0, 48 x 768 x 768 6.9, 16 x 768 x 768 10.
 // Bound: the tensor pipe for large batches (S S L + S S S + 2 S S L flops a step); for few or small matrices the latency of
 // the chain of 3 `steps` products, which then runs as ONE launch (ns_chain_kernel).
 #include <cuda.h>
@@ -66,7 +65,6 @@ struct NsProduct {
   int S, N, K;               // output [S, N], contraction K
   int tiles_m, tiles_n;
   int tiles;                 // tiles of one matrix (symmetric: on and above the diagonal)
-  int mirror;                // symmetric matrices are stored whole (else only the 256-wide tiles on and above the diagonal)
   float alpha, b, diag;      // out = alpha acc (poly: + b A_d[r, c] + diag [r == c])
   __half* Y;                 // [batch][S][ldy]
   long long ldy;
@@ -98,12 +96,10 @@ __device__ __forceinline__ void ns_tile(const NsProduct& p, int t, int& mt, int&
 }
 
 // Whether K block kb of the operand's rows in tile `rt` is read MN-major: always for the update's Z, and for a block of A or D
-// below the diagonal when only the upper tiles exist
-template <int MODE> __device__ __forceinline__ bool a_transposed(const NsProduct& p, int kb, int rt) {
-  return MODE != kGram && !p.mirror && kb / (kTN / kTK) < rt;
-}
-template <int MODE> __device__ __forceinline__ bool b_transposed(const NsProduct& p, int kb, int rt) {
-  return MODE == kUpdate || (MODE == kPoly && !p.mirror && kb / (kTN / kTK) < rt);
+// below the diagonal (only their 256-wide tiles on and above it exist)
+template <int MODE> __device__ __forceinline__ bool a_transposed(int kb, int rt) { return MODE != kGram && kb / (kTN / kTK) < rt; }
+template <int MODE> __device__ __forceinline__ bool b_transposed(int kb, int rt) {
+  return MODE == kUpdate || (MODE == kPoly && kb / (kTN / kTK) < rt);
 }
 
 // What a CTA's three roles share: shared memory, barriers, and each role's place in the ring.
@@ -176,7 +172,7 @@ struct NsEngine {
       if (!mbar_wait(empty_bar + 8 * stage, phase ^ 1u, abort_flag)) return false;
       const uint32_t sa = smem_a + stage * C::kABytes, sb = smem_b + stage * C::kBBytes;
       uint32_t fb = full_bar + 8 * stage;
-      const bool a_mn = a_transposed<MODE>(p, kb, mt), b_mn = b_transposed<MODE>(p, kb, nt);
+      const bool a_mn = a_transposed<MODE>(kb, mt), b_mn = b_transposed<MODE>(kb, nt);
       if constexpr (NCTA == 2) {
         if (rank == 0u) mbar_expect_tx(fb, 2 * (C::kABytes + C::kBBytes));
         fb = map_to_cta(fb, leader);  // both CTAs' copies are counted on the leader's barrier
@@ -233,7 +229,7 @@ struct NsEngine {
     tc_fence_after();
     const uint32_t d_tmem = tmem_base + acc * kTN;
     for (int kb = 0; kb < num_kb; ++kb) {
-      const bool a_mn = a_transposed<MODE>(p, kb, mt), b_mn = b_transposed<MODE>(p, kb, nt);
+      const bool a_mn = a_transposed<MODE>(kb, mt), b_mn = b_transposed<MODE>(kb, nt);
       const uint32_t idesc = idesc0 | (uint32_t(a_mn) << 15) | (uint32_t(b_mn) << 16);
       const uint32_t a_inc = a_mn ? mn_inc : k_inc, b_inc = b_mn ? mn_inc : k_inc;
       const uint64_t ad0 = (a_mn ? a_desc_mn : a_desc_k) + static_cast<uint64_t>(stage * (C::kABytes >> 4));
@@ -319,25 +315,6 @@ struct NsEngine {
         if (c < n_chunks && row < p.S) {  // (rows are padded to whole chunks)
           st_bytes<32>(reinterpret_cast<char*>(yrow + c * 32), o);
           st_bytes<32>(reinterpret_cast<char*>(yrow + c * 32 + 16), o + 8);
-        }
-        if constexpr (MODE != kUpdate) {
-          // The mirror image: lanes 2i and 2i+1 exchange halves, after which the even one holds columns 0-15 and the odd one
-          // columns 16-31 of BOTH rows, two rows to a word; a store covers 64 bytes of two lines.
-          if (p.mirror && mt != nt) {
-            const bool odd = lane & 1;
-            const int cm = col0 + (odd ? 16 : 0), r2 = row & ~1;
-            const int left = c < n_chunks && r2 < p.S ? p.S - cm : 0;
-            char* ym = reinterpret_cast<char*>(p.Y + (static_cast<long long>(b) * p.S + cm) * p.ldy + r2);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const uint32_t mine = odd ? o[8 + i] : o[i], other = __shfl_xor_sync(0xFFFFFFFFu, odd ? o[i] : o[8 + i], 1);
-              const uint32_t lo = odd ? other : mine, hi = odd ? mine : other;  // rows r2, r2 + 1
-              const uint32_t w0 = __byte_perm(lo, hi, 0x5410), w1 = __byte_perm(lo, hi, 0x7632);
-              if (2 * i < left) st_raw<4>(ym, &w0);
-              if (2 * i + 1 < left) st_raw<4>(ym + p.ldy * 2, &w1);
-              ym += p.ldy * 4;
-            }
-          }
         }
       }
     }
@@ -962,8 +939,6 @@ static int run_batch(const MuonTable& tab, int count, const MuonHyper& h, void* 
     c.update[k].alpha = 1.0f / kGramScale;
   }
   const bool pairs = ns_ncta(s.S) == 2;
-  const int mirror = static_cast<long long>(c.gram.tiles) * count > sm_count() / (pairs ? 2 : 1) ? 1 : 0;
-  c.gram.mirror = c.poly.mirror = c.update[0].mirror = c.update[1].mirror = mirror;
   int size_log = -1;
   int rc = pairs ? choose_chain<2>(c, count, &size_log) : choose_chain<1>(c, count, &size_log);
   if (rc) return rc;
