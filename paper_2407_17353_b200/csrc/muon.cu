@@ -151,12 +151,8 @@ struct NsEngine {
   }
   // commit of the MMAs issued so far to a barrier of both CTAs of the pair
   __device__ __forceinline__ void commit(uint32_t bar) {
-    if constexpr (NCTA == 1) {
-      umma_commit(bar);
-    } else {
-      const uint16_t mask = static_cast<uint16_t>(3u << leader);
-      asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"(mask) : "memory");
-    }
+    if constexpr (NCTA == 1) umma_commit(bar);
+    else umma_commit_pair(bar, leader);
   }
 
   // ---- warp 0, lane 0: the operand blocks of one tile
@@ -502,15 +498,14 @@ __device__ __forceinline__ void muon_vec(const MuonWords<GDT, MDT>& w, const Muo
   if constexpr (MDT < 0) {
 #pragma unroll
     for (int e = 0; e < kVec; ++e) u[e] = g[e];
-    return;
   } else {
     decode_vec<MDT, kVec>(w.m, m);
-  }
 #pragma unroll
-  for (int e = 0; e < kVec; ++e) {
-    const float gg = f.fg * g[e];
-    m[e] = fmaf(f.fm, m[e], gg);
-    u[e] = p.nesterov ? fmaf(p.momentum, m[e], gg) : m[e];
+    for (int e = 0; e < kVec; ++e) {
+      const float gg = f.fg * g[e];
+      m[e] = fmaf(f.fm, m[e], gg);
+      u[e] = p.nesterov ? fmaf(p.momentum, m[e], gg) : m[e];
+    }
   }
 }
 
@@ -677,7 +672,6 @@ __global__ void __launch_bounds__(256) muon_update_kernel(const __grid_constant_
           float x[kVec];
           load_vec<DT>(wrow, col / kVec, n, w);
           decode_vec<DT, kVec>(w, x);
-#pragma unroll
           for (int e = 0; e < kVec; ++e) z[e] = round_through<DT>(fmaf(f.fw, x[e], -f.fo * z[e]));
         }
         store_vec<DT>(wrow, col / kVec, n, z);
