@@ -374,7 +374,8 @@ int scalify_scaled_layernorm_bwd_delayed(const scalify_array* G, const scalify_a
  * addition: H must be NULL and X is the stream that is normalised.  Y: any dtype.  Exactly one of Y and Ymx is given;
  * Ymx: rows of d = K elements, not transposed.  gamma: [d], F16/BF16/F32, or NULL.  rinv: optional fp32 [rows]
  * (device), needed by the backward call.  d <= 16384, any; rows may be strided.  A row of zeros gives zeros if
- * eps > 0; with no rows at all the output scale words alone are written.  The squares of H_d are fp32 (|H_d| up to 2^56; an infinity or NaN reaches its own row only).
+ * eps > 0; with no rows at all the output scale words alone are written.  The squares of H_d are fp32 (|H_d| up to
+ * 2^56, and with eps = 0 a row's largest not below 2^-60; an infinity or NaN reaches its own row only).
  * status: optional DEVICE word (SCALIFY_DEV_BAD_SCALE).
  * Errors: NULL, DTYPE, SHAPE, ALIGNMENT, UNSUPPORTED (both Y and Ymx, transposed Ymx), VALUE (eps < 0), ALIAS (an
  * output, rinv and the exponents among them, overlapping another array of the call other than as above, or a scale word

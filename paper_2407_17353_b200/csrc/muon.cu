@@ -11,8 +11,8 @@
 // FP16 rather than BF16 because the products run at the same rate and its 11 bits leave an eighth of the rounding error,
 // which the iteration passes on to small singular values multiplied by up to 3.4 a step: five steps turn the 2^-12 of a
 // rounding into 0.1 to 0.15 of absolute error in the Frobenius norm, whatever the matrix is (768 x 2304: rank 1 0.10, rank 64
-// 0.15, each of its directions at most 0.016), which is 1e-3 of a full-rank result and 0.15 of one of rank 1.  Low parts of Z, A
-// and D would take that away at three times the products.
+// 0.15, each of its directions at most 0.016), which is 1e-3 of a full-rank result and 0.15 of one of rank 1.  Low FP16 halves
+// of Z, A and D beside the high ones take that away and cost 1.8 to 2.2 times the call (three products for one; measured).
 //   gram:   A_d = (sigma^2 2^12) Z_d Z_d^T            symmetric: tiles on and above the diagonal
 //   poly:   D_d = (c 2^-12) A_d A_d^T + b A_d + 2^12 a I   likewise; b A_d + .. is added to the fp32 accumulator
 //   update: Z_d <- 2^-12 D_d Z_d                       Z_d is the MN-major operand: no transposed copy
@@ -324,7 +324,8 @@ struct NsEngine {
 // One product of the whole batch: persistent CTAs (pairs).  On expiry of a wait the CTA records SCALIFY_DEV_TIMEOUT, drains
 // its copies and MMAs, frees its tensor memory and returns.
 // 12 x 768 x 2304: gram 21 us (tensor pipe active 63%), poly 14 (31%), update 33 (59%): about 8 us of each are the first
-// copies, the last tile's epilogue and the hand-over to the next product.
+// copies, the last tile's epilogue and the hand-over to the next product.  1 x 8192 x 2048 (36, 36 and 256 tiles on 74 pairs):
+// 49 us (87% on the SMs that have a tile), 23 (48%), 60 (72%).
 template <int MODE, int NCTA>
 __global__ void __launch_bounds__(kNsThreads, 1) ns_product_kernel(const __grid_constant__ CUtensorMap map_a,
                                                                   const __grid_constant__ CUtensorMap map_b,
@@ -557,7 +558,8 @@ __global__ void __launch_bounds__(256) muon_norm_kernel(const __grid_constant__ 
 }
 
 // m' (stored once rounded) and Z_0 = u / (|u| + eps) / sigma in FP16, [S, L]; a 64 x 64 tile per block, turned over in shared
-// memory where the matrix is tall (12 x 768 x 2304: 28 us, 149 MB, 5.3 TB/s).  The new scale
+// memory where the matrix is tall (12 x 768 x 2304: 28 us, 149 MB, 5.3 TB/s; 1 x 2048 x 8192 20.1 us, the tall 1 x 8192 x 2048
+// 30.0: turning a tile meets 8-way bank conflicts, 25000 of 31600 wavefronts of shared memory per SM).  The new scale
 // words are written here (nothing of this launch reads the old ones).
 template <int GDT, int MDT>
 __global__ void __launch_bounds__(256) muon_momentum_kernel(const __grid_constant__ MuonTable tab, const MuonPass p) {
@@ -628,7 +630,8 @@ __global__ void __launch_bounds__(256) muon_momentum_kernel(const __grid_constan
   }
 }
 
-// w' = fw w - fo Z (and its copy), or the orthogonal matrix itself (12 x 768 x 2304, FP16 with an E4M3 copy: 25 us, 5.9 TB/s).
+// w' = fw w - fo Z (and its copy), or the orthogonal matrix itself (12 x 768 x 2304, FP16 with an E4M3 copy: 25 us, 5.9 TB/s;
+// 1 x 8192 x 2048 29.7 us, with the same bank conflicts as above).
 __global__ void __launch_bounds__(256) muon_update_kernel(const __grid_constant__ MuonTable tab, const MuonPass p) {
   asm volatile("griddepcontrol.launch_dependents;");  // a programmatic dependent may set up while this grid runs
   __shared__ __align__(16) __half s_tile[kPreTile][kPreTile + 8];

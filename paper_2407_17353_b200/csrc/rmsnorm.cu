@@ -23,8 +23,11 @@ namespace {
 
 constexpr int kWarpRows = 4;     // rows (warps) per block of the warp-per-row forms: forward ...
 constexpr int kBwdRows = 8;      // ... and backward (a line of column sums per block)
-// Longest row one warp holds.  8192 rows, us with a warp and with a block per row: d = 768 forward 11.8 and 12.6, backward
-// 19.6 and 20.5; d = 1024 forward 16.0 and 13.9, backward 25.7 and 23.4.
+// Longest row one warp holds, with three vectors per lane; a fourth costs more than the block form's barriers.  8192 rows of
+// BF16, us with a warp and with a block per row, forward, then backward: d = 512 7.6 and 9.6, 13.9 and 20.8; 640 10.7 and 12.3,
+// 18.7 and 19.2; 704 11.3 and 12.6, 18.8 and 19.9; 768 11.9 and 12.7, 19.3 and 20.0; 776 14.0 and 12.8, 23.5 and 20.8; 896 15.3 and
+// 13.4, 25.0 and 23.0; 1024 16.3 and 14.1, 26.0 and 24.4.  1000 rows with an fp32 stream: 512 3.8 both, 6.9 and 13.7; 640 4.5 and
+// 4.1, 8.2 and 10.0; 768 4.8 and 4.2, 8.3 and 10.0; 776 5.5 and 4.2, 10.6 and 10.3.
 constexpr int kWarpMaxD = 768;
 constexpr int kPrefetchThreads = 384;  // of the backward form that loads the next row ahead (168 registers a thread)
 constexpr int kBwdWarpBlocks = 2;      // resident blocks per SM of the backward warp-per-row form
@@ -225,8 +228,11 @@ __global__ void __launch_bounds__(BLOCK ? kBlockThreads : 32 * kWarpRows) add_rm
 // registers while it works on the current one, so that the two barriers of a row do not leave the memory idle; the form
 // for very long rows has no registers left for that and asks the L2 for its next row instead (4096 rows of 8192, BF16:
 // 100 us without, 90 with; the request costs the other form 1 to 4 us and gains it nothing).
-// Measured (bytes of G, Gr, H, dX and its 8-bit copy): 8192 x 768 BF16 19.4 us with its second launch (instruction issue;
-// 57 MB), 4099 x 5120 with an fp32 stream 57.8 us, 5.4 TB/s; 4099 x 5004 60.2 us; 4096 x 8192 BF16 90 us, 3.4 TB/s.
+// Measured (bytes of G, Gr, H, dX and its 8-bit copy): 8192 x 768 BF16 19.4 us with its second launch (57 MB, 2.9 TB/s: it waits
+// for memory, 16 warps per SM without a row ahead, 0.35 instructions issued per scheduler and cycle, 3.3 of a warp's 10.4 cycles
+// per instruction behind loads; 3.5 rows per warp make four rounds), 4099 x 5120 with an fp32 stream 57.8 us, 5.4 TB/s; 4099 x 5004
+// 60.2 us; 4096 x 8192 BF16 90 us, 3.4 TB/s (one block of 16 warps per SM waits for its row's words from the L2, and reads gamma
+// and Gr in the middle of the row: 765 MB of L2 traffic for 302 MB).
 template <int GDT, int HDT, int VPT, bool BLOCK>
 __global__ void __launch_bounds__(BLOCK ? (VPT == 2 ? kPrefetchThreads : kBlockThreads) : 32 * kBwdRows,
                                   BLOCK ? 1 : kBwdWarpBlocks) add_rmsnorm_bwd_kernel(const RmsNormBwdArgs a) {
@@ -350,7 +356,7 @@ __global__ void __launch_bounds__(BLOCK ? (VPT == 2 ? kPrefetchThreads : kBlockT
     } else {
       load_row(row, wg, wh, wr, rinv);
     }
-    // Two elements per instruction (two-wide fp32): the kernel is otherwise bound by instruction issue, not by HBM.
+    // Two elements per instruction (two-wide fp32): a row's arithmetic comes between its loads and the next row's.
     // dot = sum g gamma h;   dX = (G_s gamma_s/H_s/dX_s rinv) g gamma - (.. rinv^2 dot/d rinv) h + Gr (Gr_s/dX_s)
     float2 dot2 = make_float2(0.f, 0.f);
     const float2 rinv2 = make_float2(rinv, rinv);
