@@ -149,10 +149,15 @@ struct NsEngine {
       tmem_dealloc(tmem_base, kAccs * kTN);
     }
   }
-  // commit of the MMAs issued so far to a barrier of both CTAs of the pair
+  // commit of the MMAs issued so far to a barrier of both CTAs of the pair, which may be any pair of its cluster
+  // (umma_commit_pair is for clusters of one pair)
   __device__ __forceinline__ void commit(uint32_t bar) {
-    if constexpr (NCTA == 1) umma_commit(bar);
-    else umma_commit_pair(bar, leader);
+    if constexpr (NCTA == 1) {
+      umma_commit(bar);
+    } else {
+      const uint16_t mask = static_cast<uint16_t>(3u << leader);
+      asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"(mask) : "memory");
+    }
   }
 
   // ---- warp 0, lane 0: the operand blocks of one tile

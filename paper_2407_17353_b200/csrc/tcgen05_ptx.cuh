@@ -179,9 +179,9 @@ __device__ __forceinline__ void umma_f8_pair(uint32_t d_tmem, uint64_t adesc, ui
       ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-// arrives on the barrier at this shared-memory offset in BOTH CTAs of the pair (leader: its even rank in the cluster)
-__device__ __forceinline__ void umma_commit_pair(uint32_t bar, uint32_t leader = 0u) {
-  const uint16_t mask = static_cast<uint16_t>(3u << leader);
+// arrives on the barrier at this shared-memory offset in BOTH CTAs of the pair
+__device__ __forceinline__ void umma_commit_pair(uint32_t bar) {
+  const uint16_t mask = 3;
   asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                ::"r"(bar), "h"(mask) : "memory");
 }
