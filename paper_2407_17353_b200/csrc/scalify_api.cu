@@ -104,15 +104,17 @@ static Span span_of(const scalify_array* a) {
   if (rows) { s.width = static_cast<uintptr_t>(cols) * es; s.period = static_cast<uintptr_t>(ld) * es; }
   return s;
 }
-// (column slices of one buffer, rows alike far apart, do not overlap: b's bytes are [off, off + width) of each of a's periods;
-// nor does an unbroken range in the gap between two rows)
+// (column slices of one buffer, rows alike far apart or a multiple of that, do not overlap: b's bytes are [off, off + width) of
+// the smaller period; nor does an unbroken range in the gap between two rows)
 static bool overlap(Span a, Span b) {
   if (!(a.lo < b.hi && b.lo < a.hi)) return false;
-  if (a.period == 0) std::swap(a, b);
-  if (a.period == 0 || (b.period != 0 && a.period != b.period)) return true;
+  if (a.period == 0 || (b.period != 0 && b.period < a.period)) std::swap(a, b);  // a: the smaller period, if there is one
+  if (a.period == 0) return true;
   if (b.period == 0) {
     if (b.lo < a.lo) return true;
     b.width = b.hi - b.lo;
+  } else if (b.period % a.period != 0) {
+    return true;
   }
   const uintptr_t off = a.lo <= b.lo ? (b.lo - a.lo) % a.period : (a.period - (a.lo - b.lo) % a.period) % a.period;
   return off < a.width || off + b.width > a.period;
@@ -123,10 +125,10 @@ static bool disjoint_or_same(const scalify_array* out, int64_t out_ld, const sca
   if (!in || !overlap(span_of(out), span_of(in))) return true;
   return out->data == in->data && out->dtype == in->dtype && out_ld == in_ld;
 }
-// n plain elements of es bytes (a null pointer spans nothing)
+// n plain elements of es bytes (none, or a null pointer, span nothing)
 static Span span_of(const void* p, int64_t n, int es) {
   const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
-  return p ? Span{lo, lo + static_cast<uintptr_t>(n) * es, 0, 0} : Span{0, 0, 0, 0};
+  return p && n > 0 ? Span{lo, lo + static_cast<uintptr_t>(n) * es, 0, 0} : Span{0, 0, 0, 0};
 }
 static bool disjoint(const scalify_array* a, Span b) { return !a || !overlap(span_of(a), b); }
 static bool disjoint(const scalify_array* a, const scalify_array* b) { return !a || !b || !overlap(span_of(a), span_of(b)); }

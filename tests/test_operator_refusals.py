@@ -419,3 +419,20 @@ def test_muon_lists_whose_matrices_overlap_are_refused():
     cols = lambda first: (lambda k, i, dt, word: arr(17, dt, (64, 96), (512, 1), scale=word, offset=2 * first(i)) if k == "w" else None)  # noqa: E731,E501
     assert call(cols(lambda i: 96 * i)) == WORKSPACE    # three slices side by side
     assert call(cols(lambda i: 88 * i)) == ALIAS
+
+
+def test_slices_whose_row_strides_are_multiples_of_each_other():
+    """Every row of one half of a buffer's columns beside every other row of the other half: no overlap; across it: one."""
+    B = sc.BF16
+    g, h = arr(1, B, (8, 128)), arr(2, B, (8, 128))
+    dX = arr(3, B, (8, 128), (256, 1))
+
+    def call(offset, width, ld):
+        q = arr(3, sc.E5M2, (8, width), (ld, 1), offset=offset)   # (bytes; dX has rows of 256 bytes every 512)
+        return norm_bwd(G=arr(1, B, (8, width)), H=arr(2, B, (8, width)), dX=arr(3, B, (8, width), (256, 1)), dXq=q, stat=1)
+    assert norm_bwd(G=g, H=h, dX=dX, stat=1) == WORKSPACE
+    assert call(256, 128, 1024) == WORKSPACE and call(256 + 512, 128, 1024) == WORKSPACE and call(256 + 128, 128, 1024) == WORKSPACE
+    assert call(256, 128, 512) == WORKSPACE and call(256 - 16, 128, 1024) == ALIAS and call(512 - 16, 128, 1024) == ALIAS
+    assert call(256, 128, 768) == ALIAS   # rows that drift
+    assert norm_bwd(G=g, H=h, dX=arr(3, B, (8, 128), (1024, 1)), dXq=arr(3, sc.E5M2, (8, 128), (512, 1), offset=256), stat=1) == WORKSPACE
+    assert norm_bwd(G=g, H=h, dX=arr(3, B, (8, 128), (1024, 1)), dXq=arr(3, sc.E5M2, (8, 128), (512, 1), offset=128), stat=1) == ALIAS
