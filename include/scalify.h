@@ -617,7 +617,8 @@ int scalify_scaled_adam_step_cast(int n_tensors, const scalify_array* grads, sca
  * are held in FP16 (11 bits).  O is therefore a 16-bit array, and its error is ABSOLUTE where the matrix has directions with
  * little or nothing in them: what a rounding leaves there every step multiplies by a.  In the Frobenius norm, for |a| >= 1 and
  * results whose singular values are about 1,
- *   |O - definition| <= 2^-11 |a|^steps + 3e-3 |O|         (0.24 + 3e-3 |O| for the default; measured: half the first term)
+ *   |O - definition| <= 2^-11 |a|^steps + 3e-3 |O|         (0.24 + 3e-3 |O| for the default; measured: half the first term;
+ *                                                          the rounding of O to its own type comes on top)
  * so 1e-3 to 4e-3 of the norm for a full-rank matrix of some hundred rows, but a seventh of it for a matrix of rank one
  * (the gradient of one token).  The error is spread over all directions: with some hundred of them none gets more than 0.03
  * of the 1 that the occupied ones have.
