@@ -560,6 +560,70 @@ int scalify_scaled_cross_entropy(const scalify_array* logits, int64_t n_classes,
                                  scalify_array* dlogits, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Losses of the output layer z = H W^T WITHOUT its logits in memory, beside scalify_scaled_cross_entropy, which takes them
+ * (8192 tokens of a vocabulary of 50257: 823 MB in BF16, and as much again for their gradient).  The rules are the
+ * composition of the calls they replace: the matmul, the loss through logsumexp (Appendix B), two more matmuls.
+ *
+ *   z[t,v] = H_s W_s sum_k H_d[t,k] W_d[v,k]                                       (values; tensor cores, fp32)
+ *   lse[t] = log sum_v exp(z[t,v] / T),   p[t,v] = exp(z[t,v] / T - lse[t])        (T: temperature; cross entropy 1)
+ * Cross entropy:  loss[t] = lse[t] - z[t,target] + z_loss lse[t]^2.
+ * Distillation, from a teacher's k logits t_i = T_s T_d[t,i] at places ids[t,i]:
+ *   q_i = exp(t_i / T - teacher_lse[t]);  without teacher_lse: normalised over the row's entries (a softmax of them)
+ *   loss[t] = sum_i q_i (log q_i - log p[t,ids_i])
+ * With teacher_lse (of the teacher's WHOLE row, at this temperature: scalify_scaled_top_logits gives it) q are the teacher's
+ * own probabilities, and the mass outside the k entries takes no part.  No factor T^2 is applied.
+ *
+ *   H: [n, d], W: [vocab, d] (a tied embedding's layout): both F16, both BF16, or each E4M3 or E5M2.  Rows may be strided.
+ *   ids: DEVICE int64, [n] or [n, k] contiguous.  An entry equal to padding_id (INT64_MIN: none) is left out; so is any
+ *   other outside [0, vocab), which also sets SCALIFY_DEV_BAD_INDEX; so is a teacher's logit of -inf.  The same place twice
+ *   counts twice.  A row without entries has loss 0 and no gradient.
+ *   T: [n, k], F16, BF16 or F32 (rows may be strided), 1 <= k <= 256.  teacher_lse: DEVICE fp32 [n] or NULL.
+ *   loss, lse: DEVICE fp32 [n] (lse of every row; the gradient needs it).  mean: optional DEVICE word, the sum of the losses
+ *   (fp64, fixed order) over the number of rows that have entries; 0 if none has.
+ *   0 <= n <= 2^24, 1 <= vocab <= 2^24, 1 <= d <= 65536; z_loss >= 0 finite; temperature and its reciprocal normal numbers.
+ * The same call gives the same bits every time.  Infinities and NaN in H or W go through as the formulas have them.
+ *
+ * Gradients of sum_t g[t] loss[t] with respect to the VALUES of H and W:
+ *   D[t,v] = g[t] / T ((Q[t] + 2 z_loss lse[t]) p[t,v] - q[t,v]),  Q = sum q;      dH = D W,  dW = D^T H
+ *   D_s  = g_s p2(1/T)                                 (a scalar constant carries its power of two, Section 3.4)
+ *   dH_s = D_s W_s kf(vocab),   dW_s = D_s H_s kf(n)   (matmul rule)
+ *   grad: [n] F32, contiguous, or NULL: the gradient of `mean`, g = 1 / rows with entries, g_s = 1/n rounded down to a power
+ *   of two (as scalify_scaled_cross_entropy).  lse: of the forward call on the same arguments.
+ *   dH: [n, d], dW: [vocab, d], F16 or BF16 each; either may be NULL (a frozen layer).  Every row is written.
+ * The logits are computed again in pieces of the vocabulary (the workspace holds D of one piece, at most 64 MiB or 256
+ * columns, and the fp32 sums of dH).  D is rounded to BF16 (BF16 operands) or to FP16 at a power-of-two scale (the others;
+ * FP8 operands are widened to FP16 exactly), half a step of relative error each; sums are fp32.
+ * Errors: NULL, DTYPE, SHAPE, ALIGNMENT, VALUE, ALIAS (an output over an input or another output), WORKSPACE.
+ */
+/* Workspace of these calls (shapes and dtypes of H and W only; k = 0: cross entropy; >= 4096; 0 for arguments that the calls
+ * refuse).  A forward and a backward call on one stream may share one of the larger size; nothing is kept in it. */
+size_t scalify_linear_loss_workspace_bytes(const scalify_array* H, const scalify_array* W, int k, int backward);
+int scalify_scaled_linear_cross_entropy(const scalify_array* H, const scalify_array* W, const int64_t* ids, int64_t padding_id,
+                                        float z_loss, float* loss, float* lse, float* mean, void* workspace,
+                                        size_t workspace_bytes, void* stream);
+int scalify_scaled_linear_cross_entropy_bwd(const scalify_array* H, const scalify_array* W, const int64_t* ids,
+                                            int64_t padding_id, float z_loss, const float* lse, const scalify_array* grad,
+                                            scalify_array* dH, scalify_array* dW, void* workspace, size_t workspace_bytes,
+                                            void* stream);
+int scalify_scaled_linear_distill(const scalify_array* H, const scalify_array* W, const scalify_array* T, const int64_t* ids,
+                                  int64_t padding_id, const float* teacher_lse, float temperature, float* loss, float* lse,
+                                  float* mean, void* workspace, size_t workspace_bytes, void* stream);
+int scalify_scaled_linear_distill_bwd(const scalify_array* H, const scalify_array* W, const scalify_array* T, const int64_t* ids,
+                                      int64_t padding_id, const float* teacher_lse, float temperature, const float* lse,
+                                      const scalify_array* grad, scalify_array* dH, scalify_array* dW, void* workspace,
+                                      size_t workspace_bytes, void* stream);
+
+/*
+ * The k largest logits of every row, what a teacher hands to scalify_scaled_linear_distill:
+ *   V_d[r] = the k largest of X_d[r], in descending order, equal ones (0 and -0 are) by column;  V_s = X_s
+ *   ids[r] = their columns;   lse[r] = log sum_j exp(X_s X_d[r,j] / temperature)        (optional)
+ * A NaN counts as larger than everything (and makes lse NaN).  X: [n, vocab], F16, BF16 or F32; V: [n, k] of X's dtype; rows of
+ * both may be strided; ids: DEVICE int64 [n, k] contiguous; lse: DEVICE fp32 [n] or NULL.  1 <= k <= min(256, vocab),
+ * 0 <= n <= 2^24, vocab <= 2^24.  No workspace.  Errors: NULL, DTYPE, SHAPE, ALIGNMENT, VALUE (temperature), ALIAS.
+ */
+int scalify_scaled_top_logits(const scalify_array* X, float temperature, scalify_array* V, int64_t* ids, float* lse, void* stream);
+
+/*
  * Scaled Adam step over a list of tensors (Sections 1, 3 and 4; Table 3 row 4:
  * FP8 gradients, FP16 scaled optimizer state and master weights).  In value
  * space this is textbook Adam with bias correction:

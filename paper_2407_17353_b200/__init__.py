@@ -122,7 +122,15 @@ def lib() -> ctypes.CDLL:
         L.scalify_muon_workspace_bytes.restype = sz
         L.scalify_muon_workspace_bytes.argtypes = [i32, P]
         L.scalify_scaled_muon_step.argtypes = [i32, P, P, P, P, f32, f32, i32, f32, i32, vp, f32, i32, vp, sz, vp]
-        for name in ("scalify_orthogonalize", "scalify_scaled_muon_step", "scalify_scaled_add_rmsnorm", "scalify_scaled_add_rmsnorm_bwd", "scalify_scaled_embedding_lookup",
+        L.scalify_linear_loss_workspace_bytes.restype = sz
+        L.scalify_linear_loss_workspace_bytes.argtypes = [P, P, i32, i32]
+        L.scalify_scaled_linear_cross_entropy.argtypes = [vp, vp, vp, i64, f32, vp, vp, vp, vp, sz, vp]
+        L.scalify_scaled_linear_cross_entropy_bwd.argtypes = [vp, vp, vp, i64, f32, vp, vp, vp, vp, vp, sz, vp]
+        L.scalify_scaled_linear_distill.argtypes = [vp, vp, vp, vp, i64, vp, f32, vp, vp, vp, vp, sz, vp]
+        L.scalify_scaled_linear_distill_bwd.argtypes = [vp, vp, vp, vp, i64, vp, f32, vp, vp, vp, vp, vp, sz, vp]
+        L.scalify_scaled_top_logits.argtypes = [vp, f32, vp, vp, vp, vp]
+        for name in ("scalify_scaled_linear_cross_entropy", "scalify_scaled_linear_cross_entropy_bwd", "scalify_scaled_linear_distill",
+                     "scalify_scaled_linear_distill_bwd", "scalify_scaled_top_logits", "scalify_orthogonalize", "scalify_scaled_muon_step", "scalify_scaled_add_rmsnorm", "scalify_scaled_add_rmsnorm_bwd", "scalify_scaled_embedding_lookup",
                      "scalify_scaled_embedding_grad", "scalify_workspace_init", "scalify_check_status", "scalify_scaled_matmul", "scalify_scaled_matmul_delayed",
                      "scalify_statistic",
                      "scalify_rescale", "scalify_scaled_add", "scalify_scaled_layernorm",
@@ -710,3 +718,84 @@ def scalify_scaled_muon_step(tensors: MuonTensors, ws: Workspace, *, lr: float, 
     _same_device(name, ws.buf, tensors.keep[2][0].data)
     _call(name, tensors.device, stream, tensors.n, tensors.g, tensors.m, tensors.w, tensors.w_cast, float(lr), float(momentum),
           int(bool(nesterov)), float(weight_decay), int(steps), _coef(coef), float(eps), int(factor), ws.ptr, ws.nbytes)
+
+
+def scalify_linear_loss_workspace_bytes(H: ScaledTensor, W: ScaledTensor, *, k: int = 0, backward: bool = True) -> int:
+    """Workspace of the output layer's losses on H [n, d] and W [vocab, d] (k: a teacher's entries per row, 0: cross entropy)."""
+    n = int(lib().scalify_linear_loss_workspace_bytes(_ref(_desc(H)), _ref(_desc(W)), int(k), int(bool(backward))))
+    if n == 0:
+        raise ValueError("scalify_linear_loss_workspace_bytes: H [n, d] and W [vocab, d] of one 16-bit dtype or 8-bit ones, k up to 256")
+    return n
+
+
+def _loss_vectors(name: str, H: ScaledTensor, ids: torch.Tensor, shape, **vectors) -> None:
+    if ids.dtype != torch.int64 or not ids.is_contiguous() or tuple(ids.shape) != tuple(shape):
+        raise ValueError(f"{name}: ids must be a contiguous int64 tensor of shape {tuple(shape)}")
+    for what, t in vectors.items():
+        _rows_vector(name, t, 1 if what == "mean" else H.data.shape[0], what)
+
+
+def _pad_id(padding_id: Optional[int]) -> int:
+    return -(1 << 63) if padding_id is None else int(padding_id)
+
+
+def scalify_scaled_linear_cross_entropy(H: ScaledTensor, W: ScaledTensor, ids: torch.Tensor, loss: torch.Tensor,
+                                        lse: torch.Tensor, ws: Workspace, *, padding_id: Optional[int] = None,
+                                        z_loss: float = 0.0, mean: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Cross entropy of every row of H W^T against its id, without the logits in memory: loss and lse (fp32 [n]), and
+    optionally the mean over the rows whose id is not the padding.  H [n, d], W [vocab, d]."""
+    name = "scalify_scaled_linear_cross_entropy"
+    _loss_vectors(name, H, ids, H.data.shape[:1], loss=loss, lse=lse, mean=mean)
+    dev = _same_device(name, W.data, H.data, ids, loss, lse, mean, ws.buf)
+    _call(name, dev, stream, _addr(H), _addr(W), ids.data_ptr(), _pad_id(padding_id), float(z_loss), _ptr(loss), _ptr(lse),
+          _ptr(mean), ws.ptr, ws.nbytes)
+
+
+def scalify_scaled_linear_cross_entropy_bwd(H: ScaledTensor, W: ScaledTensor, ids: torch.Tensor, lse: torch.Tensor,
+                                            dH: Optional[ScaledTensor], dW: Optional[ScaledTensor], ws: Workspace, *,
+                                            grad: Optional[ScaledTensor] = None, padding_id: Optional[int] = None,
+                                            z_loss: float = 0.0, stream=None) -> None:
+    """Gradients of sum(grad * loss) (``grad``: F32 [n]; without it: of the mean) with respect to H and W; ``lse`` from the
+    forward call.  Either output may be None."""
+    name = "scalify_scaled_linear_cross_entropy_bwd"
+    _loss_vectors(name, H, ids, H.data.shape[:1], lse=lse)
+    dev = _same_device(name, W.data, H.data, ids, lse, _data(grad), _data(dH), _data(dW), ws.buf)
+    _call(name, dev, stream, _addr(H), _addr(W), ids.data_ptr(), _pad_id(padding_id), float(z_loss), _ptr(lse), _addr(grad),
+          _addr(dH), _addr(dW), ws.ptr, ws.nbytes)
+
+
+def scalify_scaled_linear_distill(H: ScaledTensor, W: ScaledTensor, T: ScaledTensor, ids: torch.Tensor, loss: torch.Tensor,
+                                  lse: torch.Tensor, ws: Workspace, *, teacher_lse: Optional[torch.Tensor] = None,
+                                  temperature: float = 1.0, padding_id: Optional[int] = None,
+                                  mean: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Divergence of softmax(H W^T / temperature) from a teacher's k top logits T [n, k] at the places ids [n, k], without the
+    student's logits in memory.  ``teacher_lse``: of the teacher's whole rows at this temperature (else the entries are
+    normalised among themselves)."""
+    name = "scalify_scaled_linear_distill"
+    _loss_vectors(name, H, ids, T.data.shape, loss=loss, lse=lse, mean=mean, teacher_lse=teacher_lse)
+    dev = _same_device(name, W.data, H.data, T.data, ids, teacher_lse, loss, lse, mean, ws.buf)
+    _call(name, dev, stream, _addr(H), _addr(W), _addr(T), ids.data_ptr(), _pad_id(padding_id), _ptr(teacher_lse),
+          float(temperature), _ptr(loss), _ptr(lse), _ptr(mean), ws.ptr, ws.nbytes)
+
+
+def scalify_scaled_linear_distill_bwd(H: ScaledTensor, W: ScaledTensor, T: ScaledTensor, ids: torch.Tensor, lse: torch.Tensor,
+                                      dH: Optional[ScaledTensor], dW: Optional[ScaledTensor], ws: Workspace, *,
+                                      teacher_lse: Optional[torch.Tensor] = None, temperature: float = 1.0,
+                                      grad: Optional[ScaledTensor] = None, padding_id: Optional[int] = None,
+                                      stream=None) -> None:
+    """Gradients of sum(grad * loss) (without ``grad``: of the mean) with respect to H and W; ``lse`` from the forward call."""
+    name = "scalify_scaled_linear_distill_bwd"
+    _loss_vectors(name, H, ids, T.data.shape, lse=lse, teacher_lse=teacher_lse)
+    dev = _same_device(name, W.data, H.data, T.data, ids, teacher_lse, lse, _data(grad), _data(dH), _data(dW), ws.buf)
+    _call(name, dev, stream, _addr(H), _addr(W), _addr(T), ids.data_ptr(), _pad_id(padding_id), _ptr(teacher_lse),
+          float(temperature), _ptr(lse), _addr(grad), _addr(dH), _addr(dW), ws.ptr, ws.nbytes)
+
+
+def scalify_scaled_top_logits(X: ScaledTensor, V: ScaledTensor, ids: torch.Tensor, *, lse: Optional[torch.Tensor] = None,
+                              temperature: float = 1.0, stream=None) -> None:
+    """The k largest of every row of X [n, vocab] in descending order (V [n, k], X's dtype), their columns (ids int64 [n, k])
+    and optionally the row's logsumexp at ``temperature``; equal ones by column."""
+    name = "scalify_scaled_top_logits"
+    _loss_vectors(name, X, ids, V.data.shape, lse=lse)
+    dev = _same_device(name, X.data, V.data, ids, lse)
+    _call(name, dev, stream, _addr(X), float(temperature), _addr(V), ids.data_ptr(), _ptr(lse))

@@ -1,0 +1,1194 @@
+// Losses of a language model's output layer z = H W^T, H [n, d], W [V, d], without its logits in memory: softmax cross
+// entropy, and the divergence from a teacher's top logits.  Both are
+//
+//   loss_t = sum_i q_i log q_i - sum_i q_i z[t,i]/T + Q lse_t (+ zeta lse_t^2),   lse_t = log sum_v exp(z[t,v]/T),  Q = sum q
+//   d loss_t / d z[t,v] = ((Q + 2 zeta lse_t) p[t,v] - q[t,v]) / T,               p = exp(z/T - lse)
+//
+// with a row's target distribution q given by few entries: one for cross entropy (q = 1), up to 256 for a teacher's.
+//
+// Logits kernel: tcgen05 on CTA pairs, 256 x 256 tiles, FP8 operands as kind::f8f6f4, 16-bit ones as kind::f16.  The
+//   epilogue warps read the fp32 logits from tensor memory while the next tile is multiplied.
+//   forward: running maximum and sum of a row over a run of tiles, in base 2 (one multiply-add and one exponential per
+//     element), and the sum of q z; one partial result per row and run, joined by a small kernel in a fixed order.
+//   gradient: the row's gradient D = g (Q p - q)/T of a PIECE of the vocabulary, in 16 bits.
+// Products kernel: of that piece, dW = D^T H and dH += D W in one launch (MN-major operands: nothing is transposed in memory;
+//   dH's sums over the pieces are fp32).
+//
+// D has the operands' type; FP8 operands are converted to FP16, which holds them exactly, and D is FP16.  FP16 has few
+// exponents, so D is stored times a power of two that brings the largest row coefficient to 2^13..2^14 (probabilities down to
+// 2^-28 keep all 11 bits).  Its rounding is at most half a step (FP16 2^-11, BF16 2^-8) per element, independent over the
+// vocabulary: it adds to dH and dW what rounding them once to that type does.
+#include <cuda.h>
+#include <limits.h>
+#include <math.h>
+
+#include "linear_loss.h"
+#include "scalify_common.cuh"
+#include "scalify_launch.h"
+#include "tcgen05_ptx.cuh"
+#include "vec8.cuh"
+
+namespace scalify {
+
+namespace {
+
+constexpr int kTM = 128;            // rows of the output tile per CTA; a pair takes 256
+constexpr int kTN = 256;            // columns of the output tile
+constexpr int kRowBytes = 128;      // a K block: one 128-byte swizzle row
+constexpr int kK16 = 64;            // ... in 16-bit elements
+constexpr int kAccs = 2;            // accumulators of 256 TMEM columns: the epilogue overlaps the next tile's products
+constexpr int kEpiWarps = 8;
+constexpr int kThreads = 64 + 32 * kEpiWarps;
+constexpr int kABytes = kTM * kRowBytes, kBBytes = kTN / 2 * kRowBytes;
+constexpr int kStages = 6;
+constexpr uint32_t kRing = kStages * (kABytes + kBBytes);
+constexpr size_t kSmem = size_t(kRing) + 1024 + 256;
+constexpr int kHalf = kTN / 2;      // columns of a tile that one epilogue warp takes
+constexpr int kChunks = kHalf / 32;
+
+template <bool F8>
+__device__ __forceinline__ void umma_pair(uint32_t d_tmem, uint64_t ad, uint64_t bd, uint32_t idesc, uint32_t acc) {
+  if constexpr (F8) {
+    umma_f8_pair(d_tmem, ad, bd, idesc, acc);
+  } else {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem), "l"(ad), "l"(bd), "r"(idesc), "r"(acc) : "memory");
+  }
+}
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Shared memory, barriers and each role's place in the ring.  Warp 0: TMA producer; warp 1: MMA issuer (of the pair's first
+// CTA); warps 2-9: epilogue.  Every wait is bounded.
+struct Engine {
+  uint32_t smem_a, smem_b, full_bar, empty_bar, acc_full, acc_empty, drain_bar, tmem_base;
+  volatile uint32_t* tmem_slot;
+  volatile uint32_t* abort_flag;
+  uint32_t rank;
+  int warp, lane;
+  uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
+  long long issued = 0;
+
+  __device__ __forceinline__ void set_up(uint8_t* smem_raw) {
+    const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+    uint8_t* bar_mem = smem_raw + (base - raw) + kRing;
+    smem_a = base;
+    smem_b = base + kStages * kABytes;
+    const uint32_t bars = base + kRing;
+    full_bar = bars;
+    empty_bar = bars + 8 * kStages;
+    acc_full = bars + 16 * kStages;
+    acc_empty = acc_full + 8 * kAccs;
+    drain_bar = acc_empty + 8 * kAccs;
+    tmem_slot = reinterpret_cast<volatile uint32_t*>(bar_mem + 16 * kStages + 16 * kAccs + 8);
+    abort_flag = tmem_slot + 1;
+    warp = threadIdx.x >> 5;
+    lane = threadIdx.x & 31;
+    rank = cluster_ctarank();
+    if (threadIdx.x == 0) {
+      for (int s = 0; s < kStages; ++s) { mbar_init(full_bar + 8 * s, 1); mbar_init(empty_bar + 8 * s, 1); }
+      for (int s = 0; s < kAccs; ++s) { mbar_init(acc_full + 8 * s, 1); mbar_init(acc_empty + 8 * s, kEpiWarps * 2); }
+      mbar_init(drain_bar, 1);
+      *abort_flag = 0u;
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), kAccs * kTN);
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();
+    tc_fence_after();
+    tmem_base = *tmem_slot;
+  }
+  __device__ __forceinline__ void tear_down() {
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();
+    if (warp == 1) {
+      tc_fence_after();
+      tmem_dealloc(tmem_base, kAccs * kTN);
+    }
+  }
+
+  // ---- warp 0, lane 0: the operand blocks of one tile.  Along K: a box of 128 bytes x 128 rows.  MN-major (16-bit only):
+  // two boxes of 64 columns x the 64 lines of this K block.
+  __device__ __forceinline__ bool produce(const CUtensorMap* ma, const CUtensorMap* mb, int m0, int n0, int num_kb, bool a_mn, bool b_mn) {
+    m0 += static_cast<int>(rank) * kTM;
+    n0 += static_cast<int>(rank) * (kTN / 2);
+    for (int kb = 0; kb < num_kb; ++kb) {
+      if (!mbar_wait(empty_bar + 8 * stage, phase ^ 1u, abort_flag)) return false;
+      const uint32_t sa = smem_a + stage * kABytes, sb = smem_b + stage * kBBytes;
+      if (rank == 0u) mbar_expect_tx(full_bar + 8 * stage, 2 * (kABytes + kBBytes));
+      const uint32_t fb = map_to_cta(full_bar + 8 * stage, 0u);  // both CTAs' copies are counted on the first one's barrier
+      auto load = [&](uint32_t dst, const CUtensorMap* m, int x_bytes, int y) { tma_load_3d_pair(dst, m, fb, x_bytes, y, 0); };
+      if (!a_mn) {
+        load(sa, ma, kb * kRowBytes, m0);
+      } else {
+#pragma unroll
+        for (int j = 0; j < kTM / kK16; ++j) load(sa + j * kK16 * kRowBytes, ma, (m0 + j * kK16) * 2, kb * kK16);
+      }
+      if (!b_mn) {
+        load(sb, mb, kb * kRowBytes, n0);
+      } else {
+#pragma unroll
+        for (int j = 0; j < kTN / 2 / kK16; ++j) load(sb + j * kK16 * kRowBytes, mb, (n0 + j * kK16) * 2, kb * kK16);
+      }
+      ++issued;
+      if (++stage == kStages) { stage = 0; phase ^= 1u; }
+    }
+    return true;
+  }
+  // after a timeout: wait (bounded) for the last use of every ring slot, so that no copy is in flight when the CTA exits
+  __device__ __forceinline__ void drain_copies() {
+    if (rank != 0u) return;
+    const int pending = issued < kStages ? static_cast<int>(issued) : kStages;
+    uint32_t s = stage, ph = phase;
+    for (int i = 0; i < pending; ++i) {
+      if (s == 0) { s = kStages - 1; ph ^= 1u; } else { --s; }
+      const unsigned long long t0 = global_timer_ns();
+      while (!mbar_try_wait(full_bar + 8 * s, ph) && global_timer_ns() - t0 < kWaitLimitNs) {}
+    }
+  }
+
+  // ---- warp 1, lane 0 of the pair's first CTA: the MMAs of one tile
+  template <bool F8>
+  __device__ __forceinline__ bool multiply(int num_kb, uint32_t idesc, bool a_mn, bool b_mn) {
+    const uint64_t a_desc = make_smem_desc(smem_a, a_mn ? kK16 * kRowBytes : 0u, 1024u);
+    const uint64_t b_desc = make_smem_desc(smem_b, b_mn ? kK16 * kRowBytes : 0u, 1024u);
+    const uint32_t a_inc = (a_mn ? 16 * kRowBytes : 32) >> 4, b_inc = (b_mn ? 16 * kRowBytes : 32) >> 4;  // per MMA: 32 bytes of K
+    idesc |= (uint32_t(a_mn) << 15) | (uint32_t(b_mn) << 16);
+    if (!mbar_wait(acc_empty + 8 * acc, acc_phase ^ 1u, abort_flag)) return false;
+    tc_fence_after();
+    const uint32_t d_tmem = tmem_base + acc * kTN;
+    for (int kb = 0; kb < num_kb; ++kb) {
+      const uint64_t ad0 = a_desc + static_cast<uint64_t>(stage * (kABytes >> 4));
+      const uint64_t bd0 = b_desc + static_cast<uint64_t>(stage * (kBBytes >> 4));
+      if (!mbar_wait(full_bar + 8 * stage, phase, abort_flag)) return false;
+      tc_fence_after();
+#pragma unroll
+      for (int k = 0; k < 4; ++k) umma_pair<F8>(d_tmem, ad0 + k * a_inc, bd0 + k * b_inc, idesc, (kb | k) != 0 ? 1u : 0u);
+      umma_commit_pair(empty_bar + 8 * stage);  // the slot is free (in both CTAs) once these MMAs have read it
+      if (++stage == kStages) { stage = 0; phase ^= 1u; }
+    }
+    umma_commit_pair(acc_full + 8 * acc);
+    if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
+    return true;
+  }
+  // after a timeout: all MMAs issued so far must retire before the tensor memory is freed
+  __device__ __forceinline__ void drain_multiplies() {
+    umma_commit_pair(drain_bar);
+    const unsigned long long t0 = global_timer_ns();
+    while (!mbar_try_wait(drain_bar, 0u) && global_timer_ns() - t0 < kWaitLimitNs) {}
+  }
+
+  // ---- warps 2-9: waits for the accumulator, gives it back
+  __device__ __forceinline__ bool wait_accumulator() {
+    if (!__all_sync(0xFFFFFFFFu, mbar_wait(acc_full + 8 * acc, acc_phase, abort_flag))) return false;
+    tc_fence_after();
+    return true;
+  }
+  __device__ __forceinline__ uint32_t accumulator(int half) const {  // this warp's lanes, its half of the columns
+    return tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16) + acc * kTN + half * kHalf;
+  }
+  __device__ __forceinline__ void release_accumulator() {
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive_cluster(map_to_cta(acc_empty + 8 * acc, 0u));
+    if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
+  }
+};
+
+// ------------------------------------------------------------------------------------------------- logits kernel
+struct Entry { int id; float q; };  // a row's target entries, those of even 128-column blocks first, each part sorted by id
+
+struct LogitsParams {
+  int n, cols;               // rows; columns (of this piece of the vocabulary)
+  long long col0;            // the piece's first column
+  int num_kb;
+  int tiles_m, tiles_n, run; // a work item: one row tile, `run` consecutive column tiles
+  long long items;
+  uint32_t idesc;
+  const float* h_scale; const float* w_scale;
+  float inv_temp;
+  // targets
+  const long long* ids; long long padding_id, vocab;  // cross entropy
+  const Entry* entries; const int2* counts; int k;    // distillation: [n][k]; even part, both
+  // forward: per run and half, and row
+  float2* partial;           // maximum (base-2 units), sum
+  float* dot;                // sum of q z
+  long long ld_part;
+  // gradient
+  const float* lse;
+  const float2* coef;        // of p and of q
+  uint16_t* D;
+  long long ldd;
+  uint32_t* status;
+};
+
+// The row's entries in this warp's half of the column tiles, in ascending order; the one after the current one is on its way.
+template <bool KD> struct Targets {
+  int id = INT_MAX;
+  float q = 0.f;
+  int next_id = INT_MAX;
+  float next_q = 0.f;
+  const Entry* at = nullptr;
+  const Entry* end = nullptr;
+  __device__ __forceinline__ void load_next() {
+    next_id = INT_MAX;
+    if (at < end) {
+      const int2 e = __ldg(reinterpret_cast<const int2*>(at));
+      next_id = e.x;
+      next_q = __int_as_float(e.y);
+      ++at;
+    }
+  }
+  // entries of columns >= first
+  __device__ __forceinline__ void start(const LogitsParams& p, int row, int half, long long first) {
+    id = INT_MAX;
+    if (row >= p.n) return;
+    if constexpr (!KD) {
+      const long long t = __ldg(p.ids + row);
+      if (t != p.padding_id && t >= first && t < p.vocab && ((t >> 7) & 1) == half) { id = static_cast<int>(t); q = 1.0f; }
+    } else {
+      const int2 c = __ldg(p.counts + row);
+      const Entry* e = p.entries + static_cast<long long>(row) * p.k;
+      int lo = half ? c.x : 0, hi = half ? c.y : c.x;
+      end = e + hi;
+      while (lo < hi) {
+        const int m = (lo + hi) >> 1;
+        if (__ldg(&e[m].id) < first) lo = m + 1; else hi = m;
+      }
+      at = e + lo;
+      load_next();
+      id = next_id; q = next_q;
+      load_next();
+    }
+  }
+  __device__ __forceinline__ void advance() {
+    if constexpr (!KD) {
+      id = INT_MAX;
+    } else {
+      id = next_id; q = next_q;
+      load_next();
+    }
+  }
+};
+
+// r[i], i in 0..31 known at run time only
+__device__ __forceinline__ float pick32(const uint32_t* r, int i) {
+  uint32_t a[16];
+#pragma unroll
+  for (int j = 0; j < 16; ++j) a[j] = (i & 16) ? r[j + 16] : r[j];
+#pragma unroll
+  for (int w = 8; w >= 1; w >>= 1)
+#pragma unroll
+    for (int j = 0; j < w; ++j) a[j] = (i & w) ? a[j + w] : a[j];
+  return __uint_as_float(a[0]);
+}
+
+template <bool F8, bool GRAD, bool KD, bool BF>
+__global__ void __launch_bounds__(kThreads, 1) logits_kernel(const __grid_constant__ CUtensorMap map_h,
+                                                             const __grid_constant__ CUtensorMap map_w, const LogitsParams p) {
+  asm volatile("griddepcontrol.launch_dependents;");  // the next kernel may set up while this one runs
+  extern __shared__ uint8_t smem_raw[];
+  Engine e;
+  if (threadIdx.x == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_h)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_w)) : "memory");
+  }
+  e.set_up(smem_raw);
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // nothing above touches what the kernel before writes
+  const int unit = blockIdx.x >> 1, num_units = gridDim.x >> 1;
+  bool timed_out = false;
+  if (e.warp == 0) {
+    if (e.lane == 0) {
+      for (long long item = unit; item < p.items && !timed_out; item += num_units) {
+        const int mt = static_cast<int>(item % p.tiles_m), nt0 = static_cast<int>(item / p.tiles_m) * p.run;
+        for (int nt = nt0; nt < min(nt0 + p.run, p.tiles_n) && !timed_out; ++nt)
+          timed_out = !e.produce(&map_h, &map_w, mt * 2 * kTM, nt * kTN, p.num_kb, false, false);
+      }
+      if (timed_out || *e.abort_flag) e.drain_copies();
+    }
+  } else if (e.warp == 1) {
+    if (e.lane == 0 && e.rank == 0u) {
+      for (long long item = unit; item < p.items && !timed_out; item += num_units) {
+        const int nt0 = static_cast<int>(item / p.tiles_m) * p.run;
+        for (int nt = nt0; nt < min(nt0 + p.run, p.tiles_n) && !timed_out; ++nt) timed_out = !e.template multiply<F8>(p.num_kb, p.idesc, false, false);
+      }
+      if (timed_out || *e.abort_flag) e.drain_multiplies();
+    }
+  } else {
+    const int half = (e.warp - 2) >> 2, quarter = e.warp & 3;
+    const float c2 = load_scale_after_wait(p.h_scale) * load_scale_after_wait(p.w_scale) * p.inv_temp * 1.4426950408889634f;
+    Targets<KD> target;
+    for (long long item = unit; item < p.items && !timed_out; item += num_units) {
+      const int mt = static_cast<int>(item % p.tiles_m), ng = static_cast<int>(item / p.tiles_m), nt0 = ng * p.run;
+      const int row = mt * 2 * kTM + static_cast<int>(e.rank) * kTM + quarter * 32 + e.lane;
+      target.start(p, row, half, p.col0 + static_cast<long long>(nt0) * kTN);
+      float top = -INFINITY, sum = 0.f, dot = 0.f;  // forward
+      float2 coef = make_float2(0.f, 0.f);          // gradient
+      float lse2 = 0.f;
+      if constexpr (GRAD) {
+        if (row < p.n) {
+          coef = __ldcg(p.coef + row);
+          lse2 = __ldcg(p.lse + row) * 1.4426950408889634f;
+        }
+      }
+      for (int nt = nt0; nt < min(nt0 + p.run, p.tiles_n); ++nt) {
+        if (!e.wait_accumulator()) { timed_out = true; break; }
+        const uint32_t t_addr = e.accumulator(half);
+        const int n0 = nt * kTN + half * kHalf;
+        const int n_chunks = max(0, min(kChunks, (p.cols - n0 + 31) / 32));  // chunks inside the matrix
+        uint32_t ra[32], rb[32];
+        auto work = [&](uint32_t* r, int c) {
+          const int c0 = n0 + c * 32, valid = p.cols - c0;
+          const long long g0 = p.col0 + c0;
+          if constexpr (!GRAD) {
+            while (__any_sync(0xFFFFFFFFu, target.id < g0 + 32)) {
+              const float z = pick32(r, static_cast<int>(target.id - g0) & 31);
+              if (target.id < g0 + 32) {
+                dot = fmaf(target.q, z, dot);
+                target.advance();
+              }
+            }
+            if (valid < 32) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (i >= valid) r[i] = 0xFF800000u;  // -inf
+            }
+            float m = __uint_as_float(r[0]);
+#pragma unroll
+            for (int i = 1; i < 32; ++i) m = fmaxf(m, __uint_as_float(r[i]));
+            m *= c2;
+            if (m > top) {  // (a row of -inf so far: sum is 0)
+              sum *= exp2_approx(top - m);
+              top = m;
+            }
+            const float shift = top == -INFINITY ? 0.f : -top;
+            float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < 32; ++i) s[i & 3] += exp2_approx(fmaf(__uint_as_float(r[i]), c2, shift));
+            sum += (s[0] + s[1]) + (s[2] + s[3]);
+          } else {
+            float v[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = coef.x * exp2_approx(fmaf(__uint_as_float(r[i]), c2, -lse2));
+            while (__any_sync(0xFFFFFFFFu, target.id < g0 + 32)) {
+              if (target.id < g0 + 32) {
+                const int at = static_cast<int>(target.id - g0);
+                const float bq = coef.y * target.q;
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                  if (i == at) v[i] -= bq;
+                target.advance();
+              }
+            }
+            uint32_t o[16];
+            encode_vec<BF ? SCALIFY_BF16 : SCALIFY_F16, 32>(v, o);
+            if (row < p.n) {
+              char* dst = reinterpret_cast<char*>(p.D + static_cast<long long>(row) * p.ldd + c0);  // (rows are padded to whole chunks)
+              st_bytes<32>(dst, o);
+              st_bytes<32>(dst + 32, o + 8);
+            }
+          }
+        };
+        if (n_chunks > 0) tmem_ld32(t_addr, ra);
+#pragma unroll 1
+        for (int c = 0; c < n_chunks; c += 2) {
+          tmem_ld_wait();
+          if (c + 1 < n_chunks) tmem_ld32(t_addr + (c + 1) * 32, rb);
+          work(ra, c);
+          if (c + 1 < n_chunks) {
+            tmem_ld_wait();
+            if (c + 2 < n_chunks) tmem_ld32(t_addr + (c + 2) * 32, ra);
+            work(rb, c + 1);
+          }
+        }
+        e.release_accumulator();
+      }
+      if constexpr (!GRAD) {
+        if (row < p.n && !timed_out) {
+          const long long o = static_cast<long long>(ng * 2 + half) * p.ld_part + row;
+          p.partial[o] = make_float2(top, sum);
+          p.dot[o] = dot;
+        }
+      }
+    }
+  }
+  if (timed_out) atomicOr(p.status, static_cast<uint32_t>(SCALIFY_DEV_TIMEOUT));
+  e.tear_down();
+}
+
+// ------------------------------------------------------------------------------------------------- products kernel
+enum { kFinal = 0, kAccFirst = 1, kAccNext = 2, kAccLast = 3 };  // what a product does with the fp32 sums of earlier pieces
+struct GradProduct {
+  int M, N, num_kb;
+  int tiles_m, tiles_n;
+  void* out;
+  long long ldo;
+  int out_dt;
+  float alpha;
+  int mode;
+  float* acc;           // [M][ld_acc]
+  long long ld_acc;
+};
+struct GradParams {
+  GradProduct dw, dh;   // D^T H and D W
+  int dw_tiles, dh_tiles;
+  bool dw_first;        // the product with the longer contraction goes first
+  uint32_t idesc;
+  const float* unit;    // 1 / the power of two that D is stored times
+  uint32_t* status;
+};
+
+__global__ void __launch_bounds__(kThreads, 1) loss_products_kernel(const __grid_constant__ CUtensorMap map_d_mn,
+                                                                    const __grid_constant__ CUtensorMap map_h_mn,
+                                                                    const __grid_constant__ CUtensorMap map_d_k,
+                                                                    const __grid_constant__ CUtensorMap map_w_mn, const GradParams p) {
+  asm volatile("griddepcontrol.launch_dependents;");  // the next kernel may set up while this one runs
+  extern __shared__ uint8_t smem_raw[];
+  Engine e;
+  if (threadIdx.x == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_d_mn)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_h_mn)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_d_k)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_w_mn)) : "memory");
+  }
+  e.set_up(smem_raw);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int unit = blockIdx.x >> 1, num_units = gridDim.x >> 1, tiles = p.dw_tiles + p.dh_tiles;
+  bool timed_out = false;
+  // tile -> product, row tile, column tile (column tiles of one row tile beside each other: they share the operand D)
+  auto locate = [&](int t, int& mt, int& nt) {
+    bool dw = p.dw_first;
+    const int first = dw ? p.dw_tiles : p.dh_tiles;
+    if (t >= first) { t -= first; dw = !dw; }
+    const int tn = dw ? p.dw.tiles_n : p.dh.tiles_n;
+    mt = t / tn;
+    nt = t - mt * tn;
+    return dw;
+  };
+  if (e.warp == 0) {
+    if (e.lane == 0) {
+      asm volatile("fence.proxy.async;" ::: "memory");  // the copies read what ordinary stores have written
+      for (int t = unit; t < tiles && !timed_out; t += num_units) {
+        int mt, nt;
+        if (locate(t, mt, nt)) timed_out = !e.produce(&map_d_mn, &map_h_mn, mt * 2 * kTM, nt * kTN, p.dw.num_kb, true, true);
+        else timed_out = !e.produce(&map_d_k, &map_w_mn, mt * 2 * kTM, nt * kTN, p.dh.num_kb, false, true);
+      }
+      if (timed_out || *e.abort_flag) e.drain_copies();
+    }
+  } else if (e.warp == 1) {
+    if (e.lane == 0 && e.rank == 0u) {
+      for (int t = unit; t < tiles && !timed_out; t += num_units) {
+        int mt, nt;
+        const bool dw = locate(t, mt, nt);
+        timed_out = !e.template multiply<false>(dw ? p.dw.num_kb : p.dh.num_kb, p.idesc, dw, true);
+      }
+      if (timed_out || *e.abort_flag) e.drain_multiplies();
+    }
+  } else {
+    const int half = (e.warp - 2) >> 2, quarter = e.warp & 3;
+    const float inv_unit = *reinterpret_cast<const volatile float*>(p.unit);
+    for (int t = unit; t < tiles; t += num_units) {
+      int mt, nt;
+      const bool dw = locate(t, mt, nt);
+      const GradProduct& g = dw ? p.dw : p.dh;
+      const float alpha = g.alpha * inv_unit;
+      const int n0 = nt * kTN + half * kHalf, row = mt * 2 * kTM + static_cast<int>(e.rank) * kTM + quarter * 32 + e.lane;
+      const int n_chunks = max(0, min(kChunks, (g.N - n0 + 31) / 32));
+      if (!e.wait_accumulator()) { timed_out = true; break; }
+      const uint32_t t_addr = e.accumulator(half);
+#pragma unroll 1
+      for (int c = 0; c < n_chunks; ++c) {
+        uint32_t r[32];
+        tmem_ld32(t_addr + c * 32, r);
+        const int col = n0 + c * 32;
+        float4* acc = reinterpret_cast<float4*>(g.acc + static_cast<long long>(row) * g.ld_acc + col);  // (padded to whole chunks)
+        float4 prev[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) prev[j] = g.mode >= kAccNext && row < g.M ? __ldcg(acc + j) : make_float4(0.f, 0.f, 0.f, 0.f);
+        tmem_ld_wait();
+        float v[32];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          v[4 * j] = __uint_as_float(r[4 * j]) + prev[j].x;
+          v[4 * j + 1] = __uint_as_float(r[4 * j + 1]) + prev[j].y;
+          v[4 * j + 2] = __uint_as_float(r[4 * j + 2]) + prev[j].z;
+          v[4 * j + 3] = __uint_as_float(r[4 * j + 3]) + prev[j].w;
+        }
+        if (row < g.M) {
+          if (g.mode == kAccFirst || g.mode == kAccNext) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) __stcg(acc + j, make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
+          } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] *= alpha;
+            uint16_t* dst = static_cast<uint16_t*>(g.out) + static_cast<long long>(row) * g.ldo + col;
+            uint32_t o[16];
+            if (g.out_dt == SCALIFY_BF16) encode_vec<SCALIFY_BF16, 32>(v, o);
+            else encode_vec<SCALIFY_F16, 32>(v, o);
+            if (col + 32 <= g.N) {
+              st_bytes<32>(reinterpret_cast<char*>(dst), o);
+              st_bytes<32>(reinterpret_cast<char*>(dst + 16), o + 8);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 32; ++i)
+                if (col + i < g.N) dst[i] = static_cast<uint16_t>((i & 1) ? o[i / 2] >> 16 : o[i / 2]);
+            }
+          }
+        }
+        __syncwarp();
+      }
+      e.release_accumulator();
+    }
+  }
+  if (timed_out) atomicOr(p.status, static_cast<uint32_t>(SCALIFY_DEV_TIMEOUT));
+  e.tear_down();
+}
+
+// ------------------------------------------------------------------------------------------------- small kernels
+// A teacher's entries: probabilities, sorted by (128-column block's parity, id), entries without a place in the vocabulary
+// or with no probability mass at all (a logit of -inf) left out.  One warp per row; the order by counting the smaller ones.
+struct TeacherParams {
+  long long n, vocab;
+  int k;
+  const long long* ids; long long padding_id;
+  const void* T; int t_dt; long long t_ld; const float* t_scale; const float* t_lse;
+  float inv_temp;
+  Entry* entries; int2* counts; float2* sums;  // sums: Q, sum q log q
+  uint32_t* status;
+};
+constexpr int kTeacherWarps = 4;
+__global__ void __launch_bounds__(32 * kTeacherWarps) teacher_kernel(const TeacherParams p) {
+  asm volatile("griddepcontrol.launch_dependents;");
+  __shared__ uint32_t s_key[kTeacherWarps][kLossMaxEntries];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long row = static_cast<long long>(blockIdx.x) * kTeacherWarps + warp;
+  if (row >= p.n) return;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  constexpr int kPer = kLossMaxEntries / 32;
+  const float scale = load_scale_after_wait(p.t_scale);
+  if (row == 0 && lane == 0 && !is_pow2_scale(scale)) atomicOr(p.status, static_cast<uint32_t>(SCALIFY_DEV_BAD_SCALE));
+  const float f = scale * p.inv_temp;
+  float t[kPer];
+  uint32_t key[kPer];
+  float top = -INFINITY;
+  bool bad = false;
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const int i = j * 32 + lane;
+    key[j] = 0xFFFFFFFFu;
+    t[j] = -INFINITY;
+    if (i < p.k) {
+      const long long id = p.ids[row * p.k + i];
+      if (id != p.padding_id) {
+        if (id < 0 || id >= p.vocab) {
+          bad = true;
+        } else {
+          const long long at = row * p.t_ld + i;
+          float x = p.t_dt == SCALIFY_F32 ? load_elem<SCALIFY_F32>(p.T, at)
+                    : p.t_dt == SCALIFY_BF16 ? load_elem<SCALIFY_BF16>(p.T, at) : load_elem<SCALIFY_F16>(p.T, at);
+          x *= f;
+          if (x != -INFINITY) {
+            t[j] = x;
+            key[j] = static_cast<uint32_t>(id) | (static_cast<uint32_t>((id >> 7) & 1) << 30);
+            top = x > top || x != x ? x : top;
+          }
+        }
+      }
+      s_key[warp][i] = key[j];
+    }
+  }
+  if (bad) atomicOr(p.status, static_cast<uint32_t>(SCALIFY_DEV_BAD_INDEX));
+  float norm;
+  if (p.t_lse) {
+    norm = __ldg(p.t_lse + row);
+  } else {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) s += key[j] != 0xFFFFFFFFu ? expf(t[j] - top) : 0.f;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+    norm = logf(s) + top;
+  }
+  __syncwarp();
+  int there = 0, even = 0;
+  float mass = 0.f, neg = 0.f;
+  Entry* out = p.entries + row * p.k;
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    if (j * 32 >= p.k) break;
+    const bool ok = key[j] != 0xFFFFFFFFu;
+    there += __popc(__ballot_sync(0xFFFFFFFFu, ok));
+    even += __popc(__ballot_sync(0xFFFFFFFFu, key[j] < (1u << 30)));
+    const float lq = t[j] - norm, q = ok ? expf(lq) : 0.f;
+    mass += q;
+    neg += ok && q != 0.f ? q * lq : 0.f;
+    int before = 0;
+    const int i = j * 32 + lane;
+    for (int m = 0; m < p.k; ++m) {
+      const uint32_t other = s_key[warp][m];
+      before += other < key[j] || (other == key[j] && m < i);
+    }
+    if (ok) out[before] = Entry{static_cast<int>(key[j] & 0x3FFFFFFFu), q};
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    mass += __shfl_xor_sync(0xFFFFFFFFu, mass, o);
+    neg += __shfl_xor_sync(0xFFFFFFFFu, neg, o);
+  }
+  if (lane == 0) {
+    p.counts[row] = make_int2(even, there);
+    p.sums[row] = make_float2(mass, neg);
+  }
+}
+
+// Whether a row counts, and (distillation) its Q and sum q log q
+__device__ __forceinline__ bool row_target(const long long* ids, long long padding_id, long long vocab, const int2* counts,
+                                           const float2* sums, long long row, float2* qe, bool* bad) {
+  if (counts) {
+    *qe = __ldcg(sums + row);
+    return __ldcg(counts + row).y > 0;
+  }
+  const long long t = __ldg(ids + row);
+  *qe = make_float2(1.f, 0.f);
+  if (t == padding_id) return false;
+  const bool ok = t >= 0 && t < vocab;
+  *bad = *bad || !ok;
+  return ok;
+}
+
+struct JoinParams {
+  long long n, vocab;
+  int slots;
+  const float2* partial; const float* dot; long long ld_part;
+  const float* h_scale; const float* w_scale;
+  float inv_temp, z_loss;
+  const long long* ids; long long padding_id;
+  const int2* counts; const float2* sums;
+  float* loss; float* lse; float* mean;
+  int rows_log;            // rows per block
+  double2* block_sums;     // sum of losses, rows that count
+  uint32_t* ticket; uint32_t* status;
+};
+constexpr int kJoinThreads = 256;
+// Joins a row's partial results: 256 >> rows_log threads share a row.  The mean is the sum of the blocks' fp64 sums, in order.
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const JoinParams p) {
+  asm volatile("griddepcontrol.launch_dependents;");
+  __shared__ float s_top[kJoinThreads], s_sum[kJoinThreads], s_dot[kJoinThreads];
+  __shared__ double s_a[kJoinThreads], s_b[kJoinThreads];
+  __shared__ bool s_last;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int rows = 1 << p.rows_log, lr = threadIdx.x & (rows - 1), part = threadIdx.x >> p.rows_log, parts = kJoinThreads >> p.rows_log;
+  const long long row = (static_cast<long long>(blockIdx.x) << p.rows_log) + lr;
+  float top = -INFINITY, sum = 0.f, dot = 0.f;
+  if (row < p.n) {
+    constexpr int kBatch = 8;  // loads in flight
+    for (int s0 = part; s0 < p.slots; s0 += parts * kBatch) {
+      float2 v[kBatch];
+      float d[kBatch];
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        const int s = s0 + j * parts;
+        const long long o = static_cast<long long>(s) * p.ld_part + row;
+        v[j] = s < p.slots ? __ldcg(p.partial + o) : make_float2(-INFINITY, 0.f);
+        d[j] = s < p.slots ? __ldcg(p.dot + o) : 0.f;
+      }
+      float m = top;
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) m = fmaxf(m, v[j].x);
+      const float shift = m == -INFINITY ? 0.f : m;
+      sum *= exp2f(top - shift);
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j) {
+        sum = fmaf(v[j].y, exp2f(v[j].x - shift), sum);
+        dot += d[j];
+      }
+      top = m;
+    }
+  }
+  s_top[threadIdx.x] = top; s_sum[threadIdx.x] = sum; s_dot[threadIdx.x] = dot;
+  __syncthreads();
+  double total = 0.0, count = 0.0;
+  if (part == 0 && row < p.n) {
+    for (int j = 1; j < parts; ++j) top = fmaxf(top, s_top[lr + (j << p.rows_log)]);
+    const float shift = top == -INFINITY ? 0.f : top;
+    sum = 0.f; dot = 0.f;
+    for (int j = 0; j < parts; ++j) {
+      const int o = lr + (j << p.rows_log);
+      sum = fmaf(s_sum[o], exp2f(s_top[o] - shift), sum);
+      dot += s_dot[o];
+    }
+    const float lse = (top + log2f(sum)) * 0.6931471805599453f;
+    const float hw = load_scale_after_wait(p.h_scale) * load_scale_after_wait(p.w_scale);
+    float2 qe;
+    bool bad = false;
+    const bool counts = row_target(p.ids, p.padding_id, p.vocab, p.counts, p.sums, row, &qe, &bad);
+    if (bad) atomicOr(p.status, static_cast<uint32_t>(SCALIFY_DEV_BAD_INDEX));
+    const float loss = counts ? qe.y + (qe.x * lse - dot * (hw * p.inv_temp)) + (p.z_loss > 0.f ? p.z_loss * lse * lse : 0.f) : 0.f;
+    p.loss[row] = loss;
+    p.lse[row] = lse;
+    total = loss;
+    count = counts ? 1.0 : 0.0;
+    if (row == 0 && (!is_pow2_scale(load_scale_after_wait(p.h_scale)) || !is_pow2_scale(load_scale_after_wait(p.w_scale))))
+      atomicOr(p.status, static_cast<uint32_t>(SCALIFY_DEV_BAD_SCALE));
+  }
+  if (!p.mean) return;
+  auto block_sum = [&]() {
+    s_a[threadIdx.x] = total; s_b[threadIdx.x] = count;
+    for (int o = kJoinThreads / 2; o; o >>= 1) {
+      __syncthreads();
+      if (static_cast<int>(threadIdx.x) < o) { s_a[threadIdx.x] += s_a[threadIdx.x + o]; s_b[threadIdx.x] += s_b[threadIdx.x + o]; }
+    }
+    __syncthreads();
+  };
+  block_sum();
+  if (threadIdx.x == 0) {
+    p.block_sums[blockIdx.x] = make_double2(s_a[0], s_b[0]);
+    __threadfence();
+    s_last = atomicAdd(p.ticket, 1u) == gridDim.x - 1;
+  }
+  __syncthreads();
+  if (!s_last) return;
+  __threadfence();
+  total = 0.0; count = 0.0;
+  for (unsigned b = threadIdx.x; b < gridDim.x; b += kJoinThreads) {
+    const double2 v = __ldcg(p.block_sums + b);
+    total += v.x; count += v.y;
+  }
+  block_sum();
+  if (threadIdx.x == 0) {
+    *p.mean = static_cast<float>(s_a[0] / (s_b[0] > 0.0 ? s_b[0] : 1.0));
+    *p.ticket = 0u;
+  }
+}
+
+struct CoefParams {
+  long long n, vocab;
+  const long long* ids; long long padding_id;
+  const int2* counts; const float2* sums;
+  const float* lse;
+  float z_loss, rest;       // rest: 1/T without its power of two
+  float inv_temp_p2;
+  const float* grad; const float* grad_scale;
+  float mean_p2;            // without grad: 1/n rounded down to a power of two
+  const float* h_scale; const float* w_scale;
+  float kf_vocab, kf_n;
+  float2* coef; float* inv_unit;
+  float* dh_scale; float* dw_scale;
+  uint32_t* status;
+};
+constexpr int kCoefThreads = 1024;
+// Row coefficients of p and of q, times the power of two that D is stored with; output scales.  One block.
+__global__ void __launch_bounds__(kCoefThreads) coef_kernel(const CoefParams p) {
+  asm volatile("griddepcontrol.launch_dependents;");
+  __shared__ int s_count[32];
+  __shared__ uint32_t s_top[32];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  bool bad = false;
+  float g_mean = 0.f;
+  if (!p.grad) {
+    int count = 0;
+    for (long long row = threadIdx.x; row < p.n; row += kCoefThreads) {
+      float2 qe;
+      count += row_target(p.ids, p.padding_id, p.vocab, p.counts, p.sums, row, &qe, &bad);
+    }
+    count = __reduce_add_sync(0xFFFFFFFFu, count);
+    if (lane == 0) s_count[warp] = count;
+    __syncthreads();
+    int total = 0;
+    for (int i = 0; i < 32; ++i) total += s_count[i];
+    g_mean = 1.0f / static_cast<float>(max(total, 1)) / p.mean_p2;
+  }
+  uint32_t top = 0u;
+  for (long long row = threadIdx.x; row < p.n; row += kCoefThreads) {
+    float2 qe;
+    float a = 0.f, b = 0.f;
+    if (row_target(p.ids, p.padding_id, p.vocab, p.counts, p.sums, row, &qe, &bad)) {
+      b = (p.grad ? __ldg(p.grad + row) : g_mean) * p.rest;
+      a = b * (qe.x + (p.z_loss > 0.f ? 2.f * p.z_loss * __ldg(p.lse + row) : 0.f));
+    }
+    p.coef[row] = make_float2(a, b);
+    const uint32_t m = max(__float_as_uint(fabsf(a)), __float_as_uint(fabsf(b * qe.x)));
+    if (m < 0x7F800000u) top = max(top, m);
+  }
+  if (bad) atomicOr(p.status, static_cast<uint32_t>(SCALIFY_DEV_BAD_INDEX));
+  top = __reduce_max_sync(0xFFFFFFFFu, top);
+  if (lane == 0) s_top[warp] = top;
+  __syncthreads();
+  for (int i = 0; i < 32; ++i) top = max(top, s_top[i]);
+  // the largest coefficient goes to [2^13, 2^14): |D| stays below 2^15
+  int ex = static_cast<int>(top >> 23) - 127;
+  if (top == 0u) ex = 13;
+  ex = min(max(13 - ex, -100), 100);
+  const float unit = __uint_as_float(static_cast<uint32_t>(127 + ex) << 23);
+  for (long long row = threadIdx.x; row < p.n; row += kCoefThreads) {
+    const float2 c = p.coef[row];  // (this thread wrote it)
+    p.coef[row] = make_float2(c.x * unit, c.y * unit);
+  }
+  if (threadIdx.x == 0) {
+    *p.inv_unit = 1.0f / unit;
+    const float hs = load_scale_after_wait(p.h_scale), ws = load_scale_after_wait(p.w_scale);
+    const float gs = p.grad ? load_scale_after_wait(p.grad_scale) : p.mean_p2;
+    if (!is_pow2_scale(hs) || !is_pow2_scale(ws) || !is_pow2_scale(gs)) atomicOr(p.status, static_cast<uint32_t>(SCALIFY_DEV_BAD_SCALE));
+    const float ds = gs * p.inv_temp_p2;
+    if (p.dh_scale) *p.dh_scale = ds * ws * p.kf_vocab;
+    if (p.dw_scale) *p.dw_scale = ds * hs * p.kf_n;
+  }
+}
+
+// FP8 rows -> FP16 (exact), of H and then of W
+struct WidenParams {
+  const void* src[2]; __half* dst[2];
+  long long ld[2], ldd, rows[2];
+  int dt[2];
+  int d;
+};
+__global__ void __launch_bounds__(256) widen_kernel(const WidenParams p) {
+  asm volatile("griddepcontrol.launch_dependents;");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int vecs = (p.d + kVec - 1) / kVec;
+  const long long total = (p.rows[0] + p.rows[1]) * vecs;
+  for (long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<long long>(gridDim.x) * 256) {
+    long long row = i / vecs;
+    const int v = static_cast<int>(i - row * vecs);
+    const int which = row >= p.rows[0];
+    if (which) row -= p.rows[0];
+    const char* src = static_cast<const char*>(p.src[which]) + row * p.ld[which];
+    uint32_t w[2], o[4];
+    float f[kVec];
+    load_vec<SCALIFY_E4M3>(src, v, p.d - v * kVec, w);
+    if (p.dt[which] == SCALIFY_E4M3) decode_vec<SCALIFY_E4M3, kVec>(w, f);
+    else decode_vec<SCALIFY_E5M2, kVec>(w, f);
+    encode_vec<SCALIFY_F16, kVec>(f, o);
+    st_raw<16>(p.dst[which] + row * p.ldd + v * kVec, o);
+  }
+}
+
+// No rows: dW is zero.
+__global__ void __launch_bounds__(256) zero_rows_kernel(uint16_t* out, long long ld, long long rows, int d) {
+  asm volatile("griddepcontrol.launch_dependents;");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  for (long long r = blockIdx.x; r < rows; r += gridDim.x)
+    for (int c = threadIdx.x; c < d; c += 256) out[r * ld + c] = 0;
+}
+
+// ------------------------------------------------------------------------------------------------- host side
+constexpr int kUnits = 74;            // CTA pairs of the GPU: sizes are planned for these, whatever the launch finds
+long long pad_to(long long x, long long m) { return (x + m - 1) / m * m; }
+size_t pad256(size_t x) { return (x + 255) / 256 * 256; }
+
+// Consecutive column tiles per work item: long runs write few partial results, short ones share the work evenly.
+int run_length(long long tiles_m, long long tiles_n) {
+  for (int run = 8; run > 1; run >>= 1)
+    if (tiles_m * ((tiles_n + run - 1) / run) >= 16 * kUnits) return run;
+  return 1;
+}
+// Columns of a piece of the vocabulary: D of at most 2^26 bytes (half the L2), whole tiles.
+long long piece_columns(long long n, long long vocab) {
+  const long long rows = pad_to(n < 1 ? 1 : n, 32);
+  long long cols = (1ll << 25) / rows / kTN * kTN;
+  if (cols < kTN) cols = kTN;
+  const long long all = pad_to(vocab, kTN);
+  if (cols >= all) return all;
+  const long long pieces = (all + cols - 1) / cols;
+  return pad_to((all + pieces - 1) / pieces, kTN);
+}
+
+struct Layout {
+  size_t partial, dot, sums_blocks, entries, counts, sums, coef, unit, h16, w16, D, acc, total;
+  long long ld_part, ld16, ldd, ld_acc, piece, pieces;
+  int slots, run;
+};
+Layout layout_of(long long n, long long vocab, long long d, int es, int k, bool backward) {
+  Layout l = {};
+  size_t at = kWsHeader;
+  auto take = [&](size_t bytes) { const size_t o = at; at += pad256(bytes); return o; };
+  const size_t rows = static_cast<size_t>(n);
+  const long long tm = (n + 2 * kTM - 1) / (2 * kTM), tn = (vocab + kTN - 1) / kTN;
+  if (k > 0) {
+    l.entries = take(rows * k * sizeof(Entry));
+    l.counts = take(rows * sizeof(int2));
+    l.sums = take(rows * sizeof(float2));
+  }
+  if (!backward) {
+    l.run = run_length(tm, tn);
+    l.slots = static_cast<int>((tn + l.run - 1) / l.run) * 2;
+    l.ld_part = pad_to(n, 32);
+    l.partial = take(static_cast<size_t>(l.slots) * l.ld_part * sizeof(float2));
+    l.dot = take(static_cast<size_t>(l.slots) * l.ld_part * sizeof(float));
+    l.sums_blocks = take((rows / 32 + 32) * sizeof(double2));
+  } else {
+    l.coef = take(rows * sizeof(float2));
+    l.unit = take(sizeof(float));
+    l.ld16 = pad_to(d, 8);
+    if (es == 1) {
+      l.h16 = take(rows * l.ld16 * 2);
+      l.w16 = take(static_cast<size_t>(vocab) * l.ld16 * 2);
+    }
+    l.piece = piece_columns(n, vocab);
+    l.pieces = (vocab + l.piece - 1) / l.piece;
+    l.ldd = l.piece;
+    l.D = take(rows * l.ldd * 2);
+    if (l.pieces > 1) {
+      l.ld_acc = pad_to(d, 32);
+      l.acc = take(rows * l.ld_acc * sizeof(float));
+    }
+  }
+  l.total = at < kWsMin ? kWsMin : at;
+  return l;
+}
+
+template <class K>
+int pair_config(K kernel, DeviceOnce& once, long long units, cudaStream_t st, cudaLaunchConfig_t* cfg, cudaLaunchAttribute* attrs) {
+  int most = 0;  // CTA pairs that fit the GPU
+  const int rc = device_once(once, &most, [&](int* v) {
+    SCALIFY_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem)));
+    cudaLaunchConfig_t q = {};
+    q.gridDim = dim3(static_cast<unsigned>(sm_count() / 2 * 2)); q.blockDim = dim3(kThreads); q.dynamicSmemBytes = kSmem;
+    cudaLaunchAttribute qa[1];
+    qa[0].id = cudaLaunchAttributeClusterDimension;
+    qa[0].val.clusterDim.x = 2; qa[0].val.clusterDim.y = 1; qa[0].val.clusterDim.z = 1;
+    q.attrs = qa; q.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &q) != cudaSuccess) { n = 0; cudaGetLastError(); }
+    *v = n;
+    return int(SCALIFY_OK);
+  });
+  if (rc) return rc;
+  if (most < 1) return SCALIFY_ERR_UNSUPPORTED;
+  attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attrs[0].val.programmaticStreamSerializationAllowed = 1;
+  attrs[1].id = cudaLaunchAttributeClusterDimension;
+  attrs[1].val.clusterDim.x = 2; attrs[1].val.clusterDim.y = 1; attrs[1].val.clusterDim.z = 1;
+  *cfg = {};
+  cfg->gridDim = dim3(static_cast<unsigned>((units < most ? units : most) * 2));
+  cfg->blockDim = dim3(kThreads); cfg->dynamicSmemBytes = kSmem; cfg->stream = st;
+  cfg->attrs = attrs; cfg->numAttrs = 2;
+  return SCALIFY_OK;
+}
+// An ordinary kernel of this file as a programmatic dependent
+template <class K, class P>
+int launch_small(K kernel, long long blocks, int threads, const P& p, cudaStream_t st) {
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(blocks)); cfg.blockDim = dim3(threads); cfg.stream = st;
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  SCALIFY_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, p));
+  return SCALIFY_OK;
+}
+
+template <bool F8, bool GRAD, bool KD, bool BF>
+int launch_logits_variant(const CUtensorMap& mh, const CUtensorMap& mw, const LogitsParams& p, cudaStream_t st) {
+  auto kernel = logits_kernel<F8, GRAD, KD, BF>;
+  static DeviceOnce once;
+  cudaLaunchConfig_t cfg;
+  cudaLaunchAttribute attrs[2];
+  const int rc = pair_config(kernel, once, p.items, st, &cfg, attrs);
+  if (rc) return rc;
+  SCALIFY_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, mh, mw, p));
+  return SCALIFY_OK;
+}
+template <bool GRAD, bool KD>
+int launch_logits(bool f8, bool bf, const CUtensorMap& mh, const CUtensorMap& mw, const LogitsParams& p, cudaStream_t st) {
+  if (f8) return launch_logits_variant<true, GRAD, KD, false>(mh, mw, p, st);
+  if constexpr (GRAD) {
+    if (bf) return launch_logits_variant<false, GRAD, KD, true>(mh, mw, p, st);
+  }
+  return launch_logits_variant<false, GRAD, KD, false>(mh, mw, p, st);
+}
+
+// operand formats of the instruction descriptor: kind::f16 F16 0, BF16 1; kind::f8f6f4 E4M3 0, E5M2 1
+uint32_t format_of(int dt) { return dt == SCALIFY_BF16 || dt == SCALIFY_E5M2 ? 1u : 0u; }
+uint32_t idesc_of(int a_dt, int b_dt) {
+  return (1u << 4) | (format_of(a_dt) << 7) | (format_of(b_dt) << 10) | (uint32_t(kTN >> 3) << 17) | (uint32_t(2 * kTM >> 4) << 24);
+}
+// [rows][cols] of es-byte elements, rows ld apart (one row alone may have any stride), in boxes of 128 bytes x box_rows
+int map_of(CUtensorMap* m, const void* base, long long rows, long long cols, long long ld, int es, uint32_t box_rows) {
+  const long long bytes = rows > 1 ? ld * es : pad_to(cols * es, 16);
+  return make_byte_map(m, base, static_cast<uint64_t>(cols) * es, static_cast<uint64_t>(rows), 1, static_cast<uint64_t>(bytes),
+                       static_cast<uint64_t>(bytes) * rows, kRowBytes, box_rows);
+}
+
+int prepare_teacher(const LinearLossArgs& a, const Layout& l, char* ws, cudaStream_t st) {
+  if (a.k == 0) return SCALIFY_OK;
+  TeacherParams t = {};
+  t.n = a.n; t.vocab = a.vocab; t.k = a.k;
+  t.ids = a.ids; t.padding_id = a.padding_id;
+  t.T = a.T; t.t_dt = a.t_dt; t.t_ld = a.t_ld; t.t_scale = a.t_scale; t.t_lse = a.t_lse;
+  t.inv_temp = a.inv_temp;
+  t.entries = reinterpret_cast<Entry*>(ws + l.entries);
+  t.counts = reinterpret_cast<int2*>(ws + l.counts);
+  t.sums = reinterpret_cast<float2*>(ws + l.sums);
+  t.status = ws_view(ws).status;
+  return launch_small(teacher_kernel, (a.n + kTeacherWarps - 1) / kTeacherWarps, 32 * kTeacherWarps, t, st);
+}
+
+LogitsParams logits_params(const LinearLossArgs& a, const Layout& l, char* ws) {
+  LogitsParams p = {};
+  const int es = elem_size(a.h_dt);
+  p.n = static_cast<int>(a.n);
+  p.num_kb = static_cast<int>((static_cast<long long>(a.d) * es + kRowBytes - 1) / kRowBytes);
+  p.tiles_m = static_cast<int>((a.n + 2 * kTM - 1) / (2 * kTM));
+  p.idesc = idesc_of(a.h_dt, a.w_dt);
+  p.h_scale = a.h_scale; p.w_scale = a.w_scale; p.inv_temp = a.inv_temp;
+  p.ids = a.ids; p.padding_id = a.padding_id; p.vocab = a.vocab;
+  if (a.k > 0) {
+    p.entries = reinterpret_cast<const Entry*>(ws + l.entries);
+    p.counts = reinterpret_cast<const int2*>(ws + l.counts);
+    p.k = a.k;
+  }
+  p.status = ws_view(ws).status;
+  return p;
+}
+
+}  // namespace
+
+size_t linear_loss_ws_bytes(long long n, long long vocab, long long d, int operand_bytes, int k, bool backward) {
+  return layout_of(n, vocab, d, operand_bytes, k, backward).total;
+}
+
+int launch_linear_loss(const LinearLossArgs& a, void* workspace, cudaStream_t st) {
+  char* ws = static_cast<char*>(workspace);
+  const int es = elem_size(a.h_dt);
+  const Layout l = layout_of(a.n, a.vocab, a.d, es, a.k, false);
+  if (a.n == 0) {
+    if (a.mean) SCALIFY_CUDA_TRY(cudaMemsetAsync(a.mean, 0, sizeof(float), st));
+    return SCALIFY_OK;
+  }
+  int rc = prepare_teacher(a, l, ws, st);
+  if (rc) return rc;
+  LogitsParams p = logits_params(a, l, ws);
+  p.cols = static_cast<int>(a.vocab);
+  p.tiles_n = static_cast<int>((a.vocab + kTN - 1) / kTN);
+  p.run = l.run;
+  p.items = static_cast<long long>(p.tiles_m) * (l.slots / 2);
+  p.partial = reinterpret_cast<float2*>(ws + l.partial);
+  p.dot = reinterpret_cast<float*>(ws + l.dot);
+  p.ld_part = l.ld_part;
+  CUtensorMap mh, mw;
+  rc = map_of(&mh, a.H, a.n, a.d, a.h_ld, es, kTM);
+  if (!rc) rc = map_of(&mw, a.W, a.vocab, a.d, a.w_ld, es, kTN / 2);
+  if (!rc) rc = a.k > 0 ? launch_logits<false, true>(es == 1, false, mh, mw, p, st) : launch_logits<false, false>(es == 1, false, mh, mw, p, st);
+  if (rc) return rc;
+  JoinParams j = {};
+  j.n = a.n; j.vocab = a.vocab; j.slots = l.slots;
+  j.partial = p.partial; j.dot = p.dot; j.ld_part = l.ld_part;
+  j.h_scale = a.h_scale; j.w_scale = a.w_scale; j.inv_temp = a.inv_temp; j.z_loss = a.z_loss;
+  j.ids = a.ids; j.padding_id = a.padding_id;
+  if (a.k > 0) {
+    j.counts = reinterpret_cast<const int2*>(ws + l.counts);
+    j.sums = reinterpret_cast<const float2*>(ws + l.sums);
+  }
+  j.loss = a.loss; j.lse = a.lse; j.mean = a.mean;
+  while (j.rows_log < 5 && (1ll << j.rows_log) < a.n) ++j.rows_log;
+  j.block_sums = reinterpret_cast<double2*>(ws + l.sums_blocks);
+  j.ticket = ws_view(ws).ticket;
+  j.status = ws_view(ws).status;
+  return launch_small(join_kernel, (a.n + (1ll << j.rows_log) - 1) >> j.rows_log, kJoinThreads, j, st);
+}
+
+int launch_linear_loss_bwd(const LinearLossArgs& a, void* workspace, cudaStream_t st) {
+  char* ws = static_cast<char*>(workspace);
+  const int es = elem_size(a.h_dt);
+  const Layout l = layout_of(a.n, a.vocab, a.d, es, a.k, true);
+  int rc = a.n > 0 ? prepare_teacher(a, l, ws, st) : SCALIFY_OK;
+  if (rc) return rc;
+  CoefParams c = {};
+  c.n = a.n; c.vocab = a.vocab; c.ids = a.ids; c.padding_id = a.padding_id;
+  if (a.k > 0) {
+    c.counts = reinterpret_cast<const int2*>(ws + l.counts);
+    c.sums = reinterpret_cast<const float2*>(ws + l.sums);
+  }
+  c.lse = a.lse; c.z_loss = a.z_loss; c.rest = a.inv_temp_rest; c.inv_temp_p2 = a.inv_temp_p2;
+  c.grad = a.grad; c.grad_scale = a.grad_scale;
+  int ex;
+  frexp(1.0 / static_cast<double>(a.n > 0 ? a.n : 1), &ex);
+  c.mean_p2 = static_cast<float>(ldexp(1.0, ex - 1));
+  c.h_scale = a.h_scale; c.w_scale = a.w_scale;
+  c.kf_vocab = kfactor(a.vocab); c.kf_n = kfactor(a.n > 0 ? a.n : 1);
+  c.coef = reinterpret_cast<float2*>(ws + l.coef);
+  c.inv_unit = reinterpret_cast<float*>(ws + l.unit);
+  c.dh_scale = a.dh_scale; c.dw_scale = a.dw_scale;
+  c.status = ws_view(ws).status;
+  rc = launch_small(coef_kernel, 1, kCoefThreads, c, st);
+  if (rc) return rc;
+  if (a.n == 0) {
+    if (!a.dW) return SCALIFY_OK;
+    zero_rows_kernel<<<static_cast<unsigned>(a.vocab < 4096 ? a.vocab : 4096), 256, 0, st>>>(static_cast<uint16_t*>(a.dW), a.dw_ld, a.vocab, a.d);
+    SCALIFY_CUDA_TRY(cudaGetLastError());
+    return SCALIFY_OK;
+  }
+  const char* h16 = static_cast<const char*>(a.H);
+  const char* w16 = static_cast<const char*>(a.W);
+  long long h16_ld = a.h_ld, w16_ld = a.w_ld;
+  if (es == 1) {
+    WidenParams w = {};
+    w.d = a.d; w.ldd = l.ld16;
+    w.src[0] = a.H; w.dst[0] = reinterpret_cast<__half*>(ws + l.h16); w.ld[0] = a.h_ld; w.rows[0] = a.dW ? a.n : 0; w.dt[0] = a.h_dt;
+    w.src[1] = a.W; w.dst[1] = reinterpret_cast<__half*>(ws + l.w16); w.ld[1] = a.w_ld; w.rows[1] = a.dH ? a.vocab : 0; w.dt[1] = a.w_dt;
+    const long long blocks = ((w.rows[0] + w.rows[1]) * ((a.d + kVec - 1) / kVec) + 255) / 256, most = 16ll * sm_count();
+    rc = launch_small(widen_kernel, blocks < most ? blocks : most, 256, w, st);
+    if (rc) return rc;
+    h16 = ws + l.h16; w16 = ws + l.w16;
+    h16_ld = w16_ld = l.ld16;
+  }
+  const bool bf = a.h_dt == SCALIFY_BF16;
+  const int d_dt = bf ? SCALIFY_BF16 : SCALIFY_F16;
+  uint16_t* D = reinterpret_cast<uint16_t*>(ws + l.D);
+  LogitsParams p = logits_params(a, l, ws);
+  p.lse = a.lse; p.coef = c.coef; p.D = D; p.ldd = l.ldd;
+  CUtensorMap mh, mw, d_mn, d_k, h_mn, w_mn;
+  rc = map_of(&mh, a.H, a.n, a.d, a.h_ld, es, kTM);
+  if (!rc) rc = map_of(&h_mn, h16, a.n, a.d, h16_ld, 2, kK16);
+  if (rc) return rc;
+  const long long row_tiles = p.tiles_m, d_tiles = (a.d + kTN - 1) / kTN;
+  for (long long i = 0; i < l.pieces; ++i) {
+    const long long v0 = i * l.piece, cols = a.vocab - v0 < l.piece ? a.vocab - v0 : l.piece;
+    p.col0 = v0; p.cols = static_cast<int>(cols);
+    p.tiles_n = static_cast<int>((cols + kTN - 1) / kTN);
+    p.run = run_length(p.tiles_m, p.tiles_n);
+    p.items = static_cast<long long>(p.tiles_m) * ((p.tiles_n + p.run - 1) / p.run);
+    rc = map_of(&mw, static_cast<const char*>(a.W) + v0 * a.w_ld * es, cols, a.d, a.w_ld, es, kTN / 2);
+    if (!rc) rc = a.k > 0 ? launch_logits<true, true>(es == 1, bf, mh, mw, p, st) : launch_logits<true, false>(es == 1, bf, mh, mw, p, st);
+    if (!rc) rc = map_of(&d_mn, D, a.n, cols, l.ldd, 2, kK16);
+    if (!rc) rc = map_of(&d_k, D, a.n, cols, l.ldd, 2, kTM);
+    if (!rc) rc = map_of(&w_mn, w16 + v0 * w16_ld * 2, cols, a.d, w16_ld, 2, kK16);
+    if (rc) return rc;
+    GradParams g = {};
+    g.dw.M = static_cast<int>(cols); g.dw.N = a.d; g.dw.num_kb = static_cast<int>((a.n + kK16 - 1) / kK16);
+    g.dw.tiles_m = static_cast<int>((cols + 2 * kTM - 1) / (2 * kTM)); g.dw.tiles_n = static_cast<int>(d_tiles);
+    g.dw.out = a.dW ? static_cast<char*>(a.dW) + v0 * a.dw_ld * 2 : nullptr; g.dw.ldo = a.dw_ld; g.dw.out_dt = a.dw_dt;
+    g.dw.alpha = 1.0f / c.kf_n; g.dw.mode = kFinal;
+    g.dh.M = static_cast<int>(a.n); g.dh.N = a.d; g.dh.num_kb = static_cast<int>((cols + kK16 - 1) / kK16);
+    g.dh.tiles_m = static_cast<int>(row_tiles); g.dh.tiles_n = static_cast<int>(d_tiles);
+    g.dh.out = a.dH; g.dh.ldo = a.dh_ld; g.dh.out_dt = a.dh_dt;
+    g.dh.alpha = 1.0f / c.kf_vocab;
+    g.dh.mode = l.pieces == 1 ? kFinal : i == 0 ? kAccFirst : i + 1 < l.pieces ? kAccNext : kAccLast;
+    g.dh.acc = reinterpret_cast<float*>(ws + l.acc); g.dh.ld_acc = l.ld_acc;
+    g.dw_tiles = a.dW ? g.dw.tiles_m * g.dw.tiles_n : 0;
+    g.dh_tiles = a.dH ? g.dh.tiles_m * g.dh.tiles_n : 0;
+    g.dw_first = g.dw.num_kb >= g.dh.num_kb;
+    g.idesc = idesc_of(d_dt, d_dt);
+    g.unit = c.inv_unit;
+    g.status = p.status;
+    static DeviceOnce once;
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attrs[2];
+    rc = pair_config(loss_products_kernel, once, static_cast<long long>(g.dw_tiles) + g.dh_tiles, st, &cfg, attrs);
+    if (rc) return rc;
+    SCALIFY_CUDA_TRY(cudaLaunchKernelEx(&cfg, loss_products_kernel, d_mn, h_mn, d_k, w_mn, g));
+  }
+  return SCALIFY_OK;
+}
+
+}  // namespace scalify

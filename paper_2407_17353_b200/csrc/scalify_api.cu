@@ -5,6 +5,7 @@
 
 #include <algorithm>
 
+#include "linear_loss.h"
 #include "scalify_common.cuh"
 #include "scalify_launch.h"
 #include <new>
@@ -1374,6 +1375,183 @@ int scalify_scaled_cross_entropy(const scalify_array* logits, int64_t n_classes,
                               reinterpret_cast<const long long*>(targets), n, logits->scale, loss,
                               dlogits ? dlogits->data : nullptr, dlogits ? dlogits->dtype : SCALIFY_F32,
                               dlogits ? dlogits->scale : nullptr, workspace, static_cast<cudaStream_t>(stream));
+}
+
+// ---------------------------------------------------------------- losses of the output layer without its logits
+namespace {
+// H, W: dtypes and shapes (an empty batch may have no memory)
+int check_output_layer(const scalify_array* H, const scalify_array* W, LinearLossArgs* a) {
+  if (!H || !W) return SCALIFY_ERR_NULL;
+  if (!valid_dtype(H->dtype) || !valid_dtype(W->dtype) || H->dtype == SCALIFY_F32 || W->dtype == SCALIFY_F32) return SCALIFY_ERR_DTYPE;
+  if (H->dtype != W->dtype && !(is_fp8(H->dtype) && is_fp8(W->dtype))) return SCALIFY_ERR_DTYPE;
+  if (H->ndim != 2 || W->ndim != 2 || H->shape[1] != W->shape[1]) return SCALIFY_ERR_SHAPE;
+  const int64_t n = H->shape[0], vocab = W->shape[0], d = W->shape[1];
+  if (n < 0 || n > kLossMaxRows || vocab < 1 || vocab > kLossMaxVocab || d < 1 || d > kLossMaxDim) return SCALIFY_ERR_SHAPE;
+  a->H = H->data; a->h_dt = H->dtype; a->h_ld = H->stride[0]; a->h_scale = H->scale;
+  a->W = W->data; a->w_dt = W->dtype; a->w_ld = W->stride[0]; a->w_scale = W->scale;
+  a->n = n; a->vocab = vocab; a->d = static_cast<int>(d);
+  return SCALIFY_OK;
+}
+// The arguments of all four calls, but for their outputs
+int check_linear_loss(const scalify_array* H, const scalify_array* W, const scalify_array* T, const int64_t* ids, int64_t padding_id,
+                      const float* teacher_lse, float temperature, float z_loss, bool distill, LinearLossArgs* a) {
+  int rc = check_output_layer(H, W, a);
+  if (!rc) rc = check_array(W);
+  if (!rc && a->n > 0) rc = check_array(H);
+  if (rc) return rc;
+  if (!ids && a->n > 0) return SCALIFY_ERR_NULL;
+  a->ids = reinterpret_cast<const long long*>(ids);
+  a->padding_id = padding_id;
+  if (!(z_loss >= 0.f) || isinf(z_loss)) return SCALIFY_ERR_VALUE;
+  a->z_loss = z_loss;
+  const float inv = 1.0f / temperature;
+  float whole_p2, whole_rest;
+  if (!split_constant(temperature, &whole_p2, &whole_rest) || !split_constant(inv, &a->inv_temp_p2, &a->inv_temp_rest)) return SCALIFY_ERR_VALUE;
+  a->inv_temp = inv;
+  if (!distill) return SCALIFY_OK;
+  if (!T) return SCALIFY_ERR_NULL;
+  if (a->n > 0) rc = check_array(T);
+  if (rc) return rc;
+  if (!is_wide(T->dtype)) return SCALIFY_ERR_DTYPE;
+  if (T->ndim != 2 || T->shape[0] != a->n || T->shape[1] < 1 || T->shape[1] > kLossMaxEntries) return SCALIFY_ERR_SHAPE;
+  a->k = static_cast<int>(T->shape[1]);
+  a->T = T->data; a->t_dt = T->dtype; a->t_ld = T->stride[0]; a->t_scale = T->scale; a->t_lse = teacher_lse;
+  return SCALIFY_OK;
+}
+// Whether the span of an output is apart from all inputs
+bool apart_from_inputs(Span out, const LinearLossArgs& a, const scalify_array* H, const scalify_array* W, const scalify_array* T) {
+  const scalify_array* arrays[3] = {H, W, T};
+  for (const scalify_array* x : arrays)
+    if (x && !disjoint(x, out)) return false;
+  return !overlap(out, span_of(a.ids, a.n * (a.k > 0 ? a.k : 1), 8)) && !overlap(out, span_of(a.t_lse, a.n, 4));
+}
+int linear_loss_forward(LinearLossArgs& a, const scalify_array* H, const scalify_array* W, const scalify_array* T, float* loss,
+                        float* lse, float* mean, void* workspace, size_t workspace_bytes, void* stream) {
+  if (a.n > 0 && (!loss || !lse)) return SCALIFY_ERR_NULL;
+  const Span out[3] = {span_of(loss, a.n, 4), span_of(lse, a.n, 4), span_of(mean, 1, 4)};
+  for (int i = 0; i < 3; ++i) {
+    if (!apart_from_inputs(out[i], a, H, W, T)) return SCALIFY_ERR_ALIAS;
+    for (int j = 0; j < i; ++j)
+      if (overlap(out[i], out[j])) return SCALIFY_ERR_ALIAS;
+  }
+  const int rc = check_ws(workspace, workspace_bytes, linear_loss_ws_bytes(a.n, a.vocab, a.d, elem_size(a.h_dt), a.k, false));
+  if (rc) return rc;
+  a.loss = loss; a.lse = lse; a.mean = mean;
+  return launch_linear_loss(a, workspace, static_cast<cudaStream_t>(stream));
+}
+int linear_loss_backward(LinearLossArgs& a, const scalify_array* H, const scalify_array* W, const scalify_array* T, const float* lse,
+                         const scalify_array* grad, scalify_array* dH, scalify_array* dW, void* workspace, size_t workspace_bytes,
+                         void* stream) {
+  if (!dH && !dW) return SCALIFY_ERR_NULL;
+  if (a.n > 0 && !lse) return SCALIFY_ERR_NULL;
+  scalify_array* const outs[2] = {dH, dW};
+  const int64_t rows[2] = {a.n, a.vocab};
+  Span spans[2] = {};
+  for (int i = 0; i < 2; ++i) {
+    const scalify_array* o = outs[i];
+    if (!o) continue;
+    int rc = rows[i] > 0 ? check_array(o) : SCALIFY_OK;
+    if (rc) return rc;
+    if (o->dtype != SCALIFY_F16 && o->dtype != SCALIFY_BF16) return SCALIFY_ERR_DTYPE;
+    if (o->ndim != 2 || o->shape[0] != rows[i] || o->shape[1] != a.d || !rows_apart(rows[i], a.d, o->stride[0])) return SCALIFY_ERR_SHAPE;
+    spans[i] = rows[i] > 0 ? span_of(o) : Span{0, 0, 0, 0};
+    if (!apart_from_inputs(spans[i], a, H, W, T) || overlap(spans[i], span_of(lse, a.n, 4))) return SCALIFY_ERR_ALIAS;
+  }
+  if (dH && dW && overlap(spans[0], spans[1])) return SCALIFY_ERR_ALIAS;
+  if (grad) {
+    int rc = a.n > 0 ? check_array(grad) : SCALIFY_OK;
+    if (rc) return rc;
+    if (grad->dtype != SCALIFY_F32) return SCALIFY_ERR_DTYPE;
+    if (grad->ndim != 1 || grad->shape[0] != a.n) return SCALIFY_ERR_SHAPE;
+    for (int i = 0; i < 2; ++i)
+      if (outs[i] && a.n > 0 && overlap(spans[i], span_of(grad))) return SCALIFY_ERR_ALIAS;
+    a.grad = static_cast<const float*>(grad->data);
+    a.grad_scale = grad->scale;
+    if (a.n == 0) a.grad = reinterpret_cast<const float*>(workspace);  // (not read: says whose scale it is)
+  }
+  const float* out_words[2] = {dH ? dH->scale : nullptr, dW ? dW->scale : nullptr};
+  const float* in_words[4] = {H->scale, W->scale, T ? T->scale : nullptr, grad ? grad->scale : nullptr};
+  int rc = check_scale_words(out_words, 2, in_words, 4);
+  if (rc) return rc;
+  rc = check_ws(workspace, workspace_bytes, linear_loss_ws_bytes(a.n, a.vocab, a.d, elem_size(a.h_dt), a.k, true));
+  if (rc) return rc;
+  a.lse = const_cast<float*>(lse);
+  if (dH) { a.dH = dH->data; a.dh_dt = dH->dtype; a.dh_ld = dH->stride[0]; a.dh_scale = dH->scale; }
+  if (dW) { a.dW = dW->data; a.dw_dt = dW->dtype; a.dw_ld = dW->stride[0]; a.dw_scale = dW->scale; }
+  return launch_linear_loss_bwd(a, workspace, static_cast<cudaStream_t>(stream));
+}
+}  // namespace
+
+size_t scalify_linear_loss_workspace_bytes(const scalify_array* H, const scalify_array* W, int k, int backward) {
+  LinearLossArgs a = {};
+  if (k < 0 || k > kLossMaxEntries || check_output_layer(H, W, &a)) return 0;
+  return linear_loss_ws_bytes(a.n, a.vocab, a.d, elem_size(a.h_dt), k, backward != 0);
+}
+
+int scalify_scaled_linear_cross_entropy(const scalify_array* H, const scalify_array* W, const int64_t* ids, int64_t padding_id,
+                                        float z_loss, float* loss, float* lse, float* mean, void* workspace,
+                                        size_t workspace_bytes, void* stream) {
+  LinearLossArgs a = {};
+  const int rc = check_linear_loss(H, W, nullptr, ids, padding_id, nullptr, 1.0f, z_loss, false, &a);
+  return rc ? rc : linear_loss_forward(a, H, W, nullptr, loss, lse, mean, workspace, workspace_bytes, stream);
+}
+
+int scalify_scaled_linear_cross_entropy_bwd(const scalify_array* H, const scalify_array* W, const int64_t* ids,
+                                            int64_t padding_id, float z_loss, const float* lse, const scalify_array* grad,
+                                            scalify_array* dH, scalify_array* dW, void* workspace, size_t workspace_bytes,
+                                            void* stream) {
+  LinearLossArgs a = {};
+  const int rc = check_linear_loss(H, W, nullptr, ids, padding_id, nullptr, 1.0f, z_loss, false, &a);
+  return rc ? rc : linear_loss_backward(a, H, W, nullptr, lse, grad, dH, dW, workspace, workspace_bytes, stream);
+}
+
+int scalify_scaled_linear_distill(const scalify_array* H, const scalify_array* W, const scalify_array* T, const int64_t* ids,
+                                  int64_t padding_id, const float* teacher_lse, float temperature, float* loss, float* lse,
+                                  float* mean, void* workspace, size_t workspace_bytes, void* stream) {
+  LinearLossArgs a = {};
+  const int rc = check_linear_loss(H, W, T, ids, padding_id, teacher_lse, temperature, 0.f, true, &a);
+  return rc ? rc : linear_loss_forward(a, H, W, T, loss, lse, mean, workspace, workspace_bytes, stream);
+}
+
+int scalify_scaled_linear_distill_bwd(const scalify_array* H, const scalify_array* W, const scalify_array* T, const int64_t* ids,
+                                      int64_t padding_id, const float* teacher_lse, float temperature, const float* lse,
+                                      const scalify_array* grad, scalify_array* dH, scalify_array* dW, void* workspace,
+                                      size_t workspace_bytes, void* stream) {
+  LinearLossArgs a = {};
+  const int rc = check_linear_loss(H, W, T, ids, padding_id, teacher_lse, temperature, 0.f, true, &a);
+  return rc ? rc : linear_loss_backward(a, H, W, T, lse, grad, dH, dW, workspace, workspace_bytes, stream);
+}
+
+int scalify_scaled_top_logits(const scalify_array* X, float temperature, scalify_array* V, int64_t* ids, float* lse, void* stream) {
+  if (!X || !V) return SCALIFY_ERR_NULL;
+  if (X->ndim != 2 || V->ndim != 2) return SCALIFY_ERR_SHAPE;
+  const int64_t n = X->shape[0], vocab = X->shape[1], k = V->shape[1];
+  int rc = SCALIFY_OK;
+  if (n != 0) {  // (an empty batch may have no memory)
+    rc = check_array(X);
+    if (!rc) rc = check_array(V);
+  }
+  if (rc) return rc;
+  if (!valid_dtype(X->dtype) || !is_wide(X->dtype) || V->dtype != X->dtype) return SCALIFY_ERR_DTYPE;
+  if (n < 0 || n > kLossMaxRows || vocab < 1 || vocab > kLossMaxVocab || k < 1 || k > vocab || k > kLossMaxEntries || V->shape[0] != n ||
+      !rows_apart(n, k, V->stride[0]))
+    return SCALIFY_ERR_SHAPE;
+  if (!ids && n > 0) return SCALIFY_ERR_NULL;
+  TopLogitsArgs a = {};
+  a.inv_temp = 1.0f / temperature;
+  float p2, rest;
+  if (!split_constant(temperature, &p2, &rest) || !split_constant(a.inv_temp, &p2, &rest)) return SCALIFY_ERR_VALUE;
+  if (n > 0) {
+    const Span sv = span_of(V), si = span_of(ids, n * k, 8), sl = span_of(lse, n, 4);
+    if (!disjoint(X, sv) || !disjoint(X, si) || !disjoint(X, sl) || overlap(sv, si) || overlap(sv, sl) || overlap(si, sl)) return SCALIFY_ERR_ALIAS;
+  }
+  if (V->scale && V->scale == X->scale) return SCALIFY_ERR_ALIAS;
+  a.X = X->data; a.dt = X->dtype; a.ld = X->stride[0]; a.x_scale = X->scale;
+  a.n = n; a.vocab = vocab; a.k = static_cast<int>(k);
+  a.V = V->data; a.v_ld = V->stride[0]; a.v_scale = V->scale;
+  a.ids = reinterpret_cast<long long*>(ids);
+  a.lse = lse;
+  return launch_top_logits(a, static_cast<cudaStream_t>(stream));
 }
 
 // ---------------------------------------------------------------- orthogonalisation and the Muon step

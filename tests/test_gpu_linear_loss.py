@@ -1,0 +1,280 @@
+"""Cross entropy and distillation of an output layer without its logits, against the plain 64-bit form and the bounds that
+tests/plain64_loss.py derives."""
+import pytest
+import torch
+
+import paper_2407_17353_b200 as sc
+import plain64 as p64
+import plain64_loss as pl
+from test_gpu_rmsnorm import gap_untouched, gen, put, rows_of
+
+pytestmark = pytest.mark.gpu
+BF16, F16, F32, E4M3, E5M2 = torch.bfloat16, torch.float16, torch.float32, torch.float8_e4m3fn, torch.float8_e5m2
+INF = float("inf")
+
+
+def rand(shape, seed, scale=1.0):
+    return scale * torch.randn(*shape, generator=gen(seed), device="cuda")
+
+
+def layer(n, vocab, d, ht, wt=None, seed=0, pad=0, size=1.0):
+    H, _ = put(rand((max(n, 1), d), seed, size), ht, pad)
+    W, _ = put(rand((vocab, d), seed + 1, size), wt or ht, pad)
+    return H[:n], W
+
+
+def check(H, W, ids, *, hs=0.5, ws=None, padding_id=-1, T=None, Ts=0.5, teacher_lse=None, temp=1.0, z_loss=0.0, grad=None,
+          gs=2.0 ** -7, out=BF16, out2=None, status=0, pad=0, mean=True, bars=True):
+    """Forward and backward against the 64-bit form."""
+    n, d = H.shape
+    vocab = W.shape[0]
+    ws = 2.0 ** -3 if ws is None else ws
+    Hs, Ws = sc.ScaledTensor.make(H, hs), sc.ScaledTensor.make(W, ws)
+    k = 0 if T is None else T.shape[1]
+    loss, lse = torch.full((n,), 5.0, device="cuda"), torch.full((n,), 5.0, device="cuda")
+    m = torch.full((1,), 5.0, device="cuda") if mean else None
+    wsp = sc.Workspace(max(sc.scalify_linear_loss_workspace_bytes(Hs, Ws, k=k, backward=b) for b in (False, True)))
+    dH, hbase = rows_of(max(n, 1), d, out, pad)
+    dW, wbase = rows_of(vocab, d, out2 or out, pad)
+    dHs, dWs = sc.ScaledTensor(dH[:n], torch.zeros(1, device="cuda")), sc.ScaledTensor(dW, torch.zeros(1, device="cuda"))
+    G = None if grad is None else sc.ScaledTensor.make(grad, gs)
+    if T is None:
+        opt = dict(padding_id=padding_id, z_loss=z_loss)
+        sc.scalify_scaled_linear_cross_entropy(Hs, Ws, ids, loss, lse, wsp, mean=m, **opt)
+        sc.scalify_scaled_linear_cross_entropy_bwd(Hs, Ws, ids, lse, dHs, dWs, wsp, grad=G, **opt)
+    else:
+        Tt = sc.ScaledTensor.make(T, Ts)
+        opt = dict(padding_id=padding_id, teacher_lse=teacher_lse, temperature=temp)
+        sc.scalify_scaled_linear_distill(Hs, Ws, Tt, ids, loss, lse, wsp, mean=m, **opt)
+        sc.scalify_scaled_linear_distill_bwd(Hs, Ws, Tt, ids, lse, dHs, dWs, wsp, grad=G, **opt)
+    assert wsp.check_status() == status
+    want = pl.linear_loss(H, hs, W, ws, ids, padding_id, None if T is None else T.double() * Ts, teacher_lse, temp, z_loss,
+                          grad, gs, BF16 if H.dtype == BF16 else F16)
+    assert dWs.scale_value() == want["dW_s"] and dHs.scale_value() == want["dH_s"]
+    assert gap_untouched(wbase, d) and gap_untouched(hbase, d)
+    if bars:
+        for name, got in (("lse", lse), ("loss", loss), ("mean", m)):
+            if got is not None:
+                err = (got.double() - want[name]).abs()
+                assert bool((err <= want["e_" + name]).all()), (name, float((err / want["e_" + name].clamp(min=1e-300)).max()))
+        for name, got in (("dH", dHs.data), ("dW", dWs.data)):
+            assert bool(p64.close(got, want[name], want["e_" + name]).all()), name
+    return loss, lse, m, dHs, dWs, want
+
+
+def ids_of(n, vocab, seed=3, some=True):
+    ids = torch.randint(0, vocab, (n,), generator=gen(seed), device="cuda")
+    if some and n > 4:
+        ids[n // 3] = -1
+        ids[-1] = vocab - 1
+        ids[0] = 0
+    return ids
+
+
+KINDS = [(BF16, BF16), (F16, F16), (E4M3, E4M3), (E5M2, E4M3)]
+SIZES = [(1, 1, 1), (1, 300, 64), (2, 127, 8), (37, 128, 100), (128, 129, 64), (129, 256, 192), (256, 257, 72), (300, 1000, 200),
+         (257, 5003, 768), (513, 640, 1032)]
+
+
+@pytest.mark.parametrize("ht,wt", KINDS)
+@pytest.mark.parametrize("n,vocab,d", SIZES)
+def test_cross_entropy(n, vocab, d, ht, wt):
+    H, W = layer(n, vocab, d, ht, wt, seed=n + d, pad=n % 2)
+    grad = rand((n,), 9) if n % 2 else None
+    check(H, W, ids_of(n, vocab), z_loss=1e-3 if d % 16 else 0.0, grad=grad, out=BF16 if ht == BF16 or n % 2 else F16, pad=d % 2,
+          mean=n != 2)
+
+
+def teacher(n, k, vocab, dtype, seed=4, pad=0):
+    T, _ = put(4 * rand((max(n, 1), k), seed), dtype, pad)
+    ids = torch.rand(max(n, 1), vocab, generator=gen(seed + 1), device="cuda").argsort(1)[:, :k].contiguous()
+    if n > 4 and k > 1:
+        ids[1, k // 2:] = -1      # a short row
+        ids[2] = -1               # a row without entries
+    return T[:n], ids[:n].contiguous()
+
+
+@pytest.mark.parametrize("ht,wt", KINDS)
+@pytest.mark.parametrize("n,vocab,d,k", [(1, 1, 1, 1), (1, 300, 64, 5), (37, 128, 100, 128), (129, 256, 192, 31), (256, 257, 72, 33),
+                                         (300, 1000, 200, 64), (257, 5003, 768, 256), (5, 2000, 40, 100)])
+def test_distill(n, vocab, d, k, ht, wt):
+    H, W = layer(n, vocab, d, ht, wt, seed=n + d, pad=n % 2)
+    T, ids = teacher(n, k, vocab, [BF16, F16, F32][(n + k) % 3], pad=k % 2)
+    tl = None
+    if (n + d) % 2:
+        tl = (torch.logsumexp(T.double() * 0.5 / 2.0, 1) + 0.1).float()
+    grad = rand((n,), 9) if n % 2 else None
+    check(H, W, ids, T=T, teacher_lse=tl, temp=2.0 if (n + d) % 2 else 1.7, grad=grad, out=BF16 if ht == BF16 else F16, pad=d % 2)
+
+
+def test_places_at_tile_borders_and_repeated():
+    n, vocab, d, k = 70, 1030, 64, 16
+    H, W = layer(n, vocab, d, F16)
+    T, _ = teacher(n, k, vocab, F32)
+    edge = torch.tensor([0, 31, 32, 127, 128, 255, 256, 383, 384, 511, 512, 1023, 1024, 1029, 1029, 128], device="cuda")
+    check(H, W, edge.repeat(n, 1).contiguous(), T=T, temp=1.0)           # one place twice, and every border
+    same = torch.full((n, k), 300, dtype=torch.int64, device="cuda")
+    check(H, W, same, T=T, temp=1.0, out=F16)                            # one place sixteen times
+    for t in edge.tolist():
+        check(H, W, torch.full((n,), t, dtype=torch.int64, device="cuda"))
+
+
+def test_all_entries_in_one_block_of_columns():
+    n, vocab, d = 130, 900, 64
+    H, W = layer(n, vocab, d, BF16)
+    T, _ = teacher(n, 128, vocab, BF16)
+    ids = (256 + torch.rand(n, 128, generator=gen(1), device="cuda").argsort(1)).contiguous()
+    check(H, W, ids, T=T, temp=3.0)
+
+
+@pytest.mark.parametrize("n,vocab,d,k", [(5000, 20011, 72, 0), (5000, 20011, 72, 20), (40000, 1100, 64, 0), (9000, 6000, 264, 3)])
+def test_several_pieces_and_long_runs(n, vocab, d, k):
+    H, W = layer(n, vocab, d, BF16 if k else F16, seed=d)
+    if k:
+        T, ids = teacher(n, k, vocab, BF16)
+        check(H, W, ids, T=T, temp=1.5, grad=rand((n,), 2))
+    else:
+        check(H, W, ids_of(n, vocab), out=F16, z_loss=1e-4)
+
+
+def test_padding_and_unknown_targets():
+    H, W = layer(40, 200, 64, BF16)
+    ids = ids_of(40, 200)
+    ids[5], ids[6] = -1, 7
+    check(H, W, ids, padding_id=-1)
+    check(H, W, ids, padding_id=7, status=sc.DEV_BAD_INDEX)
+    ids[8] = 200
+    check(H, W, ids, padding_id=-1, status=sc.DEV_BAD_INDEX)
+    ids[:] = -1
+    loss, _, m, dH, dW, _ = check(H, W, ids, padding_id=-1)   # no row counts
+    assert not loss.any() and float(m) == 0.0 and not dH.data.any() and not dW.data.any()
+    ids[:] = 1 << 40
+    check(H, W, ids, padding_id=-1, status=sc.DEV_BAD_INDEX)
+    T, tid = teacher(40, 6, 200, F32)
+    tid[9, 2], tid[10] = 200, -5
+    check(H, W, tid, T=T, status=sc.DEV_BAD_INDEX)
+
+
+def test_masked_teacher_logits():
+    H, W = layer(12, 300, 64, E4M3)
+    T, ids = teacher(12, 8, 300, F32)
+    ids = torch.rand(12, 300, generator=gen(5), device="cuda").argsort(1)[:, :8].contiguous()
+    T[0, 3] = -INF                       # no probability
+    T[1, :] = -INF                       # none at all: the row has no entries
+    T[2, 5:] = torch.finfo(F32).min      # the type's lowest value
+    T[3, :] = torch.finfo(F32).min       # throughout: a uniform distribution
+    ids[4, 2:], T[4, 2:] = -1, float("nan")   # what stands beside a left-out place does not matter
+    ids[5, 1:], T[5, 1:] = -1, INF
+    check(H, W, ids, T=T, temp=1.0)
+
+
+def test_no_rows():
+    W = layer(1, 50, 24, BF16)[1]
+    H = torch.empty(0, 24, dtype=BF16, device="cuda")
+    _, _, m, _, dW, _ = check(H, W, torch.empty(0, dtype=torch.int64, device="cuda"))
+    assert float(m) == 0.0 and not dW.data.any()
+    _, _, m, _, dW, _ = check(H, W, torch.empty(0, 3, dtype=torch.int64, device="cuda"), T=torch.empty(0, 3, device="cuda"))
+    assert float(m) == 0.0 and not dW.data.any()
+
+
+def test_large_and_small_logits_and_gradients():
+    H, W = layer(200, 700, 128, F16, size=4.0)
+    check(H, W, ids_of(200, 700), hs=1.0, ws=1.0, out=F16)              # logits of hundreds: one-hot probabilities
+    check(H, W, ids_of(200, 700), hs=2.0 ** -10, ws=2.0 ** -10, out=F16)   # none to speak of: uniform ones
+    g = rand((200,), 1)
+    for size in (2.0 ** -40, 2.0 ** 30):
+        check(H, W, ids_of(200, 700), grad=g * size, out=BF16, out2=BF16, ws=2.0 ** -7)
+    g[17] = 0.0
+    check(H, W, ids_of(200, 700), grad=g * torch.logspace(-6, 3, 200, device="cuda"), out=F16, ws=2.0 ** -7)
+
+
+def test_infinities_and_nan_stay_in_their_rows():
+    H, W = layer(300, 600, 64, BF16)
+    H[7, 3], H[200, 5] = float("nan"), INF
+    ids = ids_of(300, 600)
+    loss, lse, _, dH, _, _ = check(H, W, ids, bars=False)
+    bad = torch.zeros(300, dtype=torch.bool, device="cuda")
+    bad[7] = bad[200] = True
+    assert bool((lse.isfinite() == ~bad).all()) and bool((dH.data.isfinite().all(1) == ~bad).all())
+    # a class that a row rules out altogether
+    W2 = W.clone()
+    W2[5] = -INF
+    H2 = H.abs().nan_to_num(1.0, 1.0)
+    loss, lse, _, _, _, want = check(H2, W2, torch.where(ids == 5, 6, ids), bars=False)
+    assert bool(((lse.double() - want["lse"]).abs() < 1e-4).all())
+
+
+def test_frozen_sides_and_repeatability():
+    n, vocab, d = 300, 3000, 256
+    for ht in (E4M3, BF16):
+        H, W = layer(n, vocab, d, ht)
+        ids = ids_of(n, vocab)
+        _, lse, _, dH, dW, _ = check(H, W, ids)
+        Hs, Ws = sc.ScaledTensor.make(H, 0.5), sc.ScaledTensor.make(W, 2.0 ** -3)
+        wsp = sc.Workspace(sc.scalify_linear_loss_workspace_bytes(Hs, Ws))
+        a, b = sc.ScaledTensor.empty((n, d), BF16), sc.ScaledTensor.empty((vocab, d), BF16)
+        sc.scalify_scaled_linear_cross_entropy_bwd(Hs, Ws, ids, lse, a, None, wsp, padding_id=-1)
+        sc.scalify_scaled_linear_cross_entropy_bwd(Hs, Ws, ids, lse, None, b, wsp, padding_id=-1)
+        assert torch.equal(a.data, dH.data) and torch.equal(b.data, dW.data)
+        assert a.scale_value() == dH.scale_value() and b.scale_value() == dW.scale_value()
+
+
+def test_gradient_against_differences():
+    """The loss's own values, moved along a direction: central differences of the forward call (fp32 losses of some hundred
+    rows: their error over the step is the bound)."""
+    n, vocab, d, eps = 64, 500, 64, 2.0 ** -5
+    H, W = (x.float() for x in layer(n, vocab, d, F16))
+    ids = ids_of(n, vocab)
+    g = rand((n,), 3)
+    loss, _, _, dH, dW, want = check(H.half(), W.half(), ids, grad=g, gs=1.0, z_loss=1e-2, out=F16, hs=1.0, ws=0.125)
+    for name, X, D, s in (("H", H, dH, 1.0), ("W", W, dW, 0.125)):
+        delta = torch.sign(rand(X.shape, 8)) * eps
+        up, down = (X + delta).half(), (X - delta).half()     # what was added, after rounding
+        step = (up.double() - down.double()) * s
+        args = lambda Y: (Y, W.half()) if name == "H" else (H.half(), Y)  # noqa: E731
+        lu, ld = (check(*args(Y), ids, grad=g, gs=1.0, z_loss=1e-2, out=F16, hs=1.0, ws=0.125) for Y in (up, down))
+        diff = (g.double() * (lu[0].double() - ld[0].double())).sum()
+        along = (D.data.double() * D.scale_value() * step).sum()
+        # third-order term: bounded by the 64-bit losses at the same three points
+        diff64 = (g.double() * (lu[5]["loss"] - ld[5]["loss"])).sum()
+        along64 = (want["d" + name] * want["d%s_s" % name] * step).sum()
+        bound = (g.abs().double() * (lu[5]["e_loss"] + ld[5]["e_loss"])).sum() + (diff64 - along64).abs() \
+            + ((want["e_d" + name] + want["d" + name].abs() * 2.0 ** -11 + 2.0 ** -25) * want["d%s_s" % name] * step.abs()).sum()
+        assert abs(float(diff - along)) <= float(bound)
+        assert float((diff64 - along64).abs()) < 0.05 * float(along64.abs())   # the formula's own gradient
+
+
+def test_captured_and_replayed_on_another_stream():
+    n, vocab, d = 200, 2000, 128
+    H, W = layer(n, vocab, d, E4M3)
+    ids = ids_of(n, vocab)
+    Hs, Ws = sc.ScaledTensor.make(H, 0.5), sc.ScaledTensor.make(W, 2.0 ** -3)
+    wsp = sc.Workspace(max(sc.scalify_linear_loss_workspace_bytes(Hs, Ws, backward=b) for b in (False, True)))
+    loss, lse, m = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda"), torch.zeros(1, device="cuda")
+    dH, dW = sc.ScaledTensor.empty((n, d), BF16), sc.ScaledTensor.empty((vocab, d), BF16)
+
+    def step():
+        sc.scalify_scaled_linear_cross_entropy(Hs, Ws, ids, loss, lse, wsp, padding_id=-1, mean=m)
+        sc.scalify_scaled_linear_cross_entropy_bwd(Hs, Ws, ids, lse, dH, dW, wsp, padding_id=-1)
+
+    step()
+    torch.cuda.synchronize()
+    first = [t.clone() for t in (loss, lse, m, dH.data, dW.data)]
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    for t in (loss, lse, m, dH.data, dW.data):
+        t.zero_()
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(first, (loss, lse, m, dH.data, dW.data)))
+    H.copy_(layer(n, vocab, d, E4M3, seed=50)[0])   # other inputs in the same buffers
+    graph.replay()
+    torch.cuda.synchronize()
+    replayed = [t.clone() for t in (loss, lse, m, dH.data, dW.data)]
+    step()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(replayed, (loss, lse, m, dH.data, dW.data)))
+    assert not torch.equal(replayed[0], first[0])
