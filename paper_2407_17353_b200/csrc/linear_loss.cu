@@ -10,9 +10,10 @@
 //   epilogue warps read the fp32 logits from tensor memory while the next tile is multiplied.
 //   forward: running maximum and sum of a row over a run of tiles, in base 2 (one multiply-add and one exponential per
 //     element), and the sum of q z; one partial result per row and run, joined by a small kernel in a fixed order.
-//   gradient: the row's gradient D = g (Q p - q)/T of a PIECE of the vocabulary, in 16 bits.
-// Products kernel: of that piece, dW = D^T H and dH += D W in one launch (MN-major operands: nothing is transposed in memory;
-//   dH's sums over the pieces are fp32).
+// Gradient kernel: the logits again, of a PIECE of the vocabulary, now to the gradient D = g (Q p - q)/T in 16 bits; and, in
+//   the same launch, the products dW = D^T H and dH += D W of the piece before (MN-major operands: nothing is transposed in
+//   memory; dH's sums over the pieces are fp32).  The products' few long tiles alone leave pairs idle (8192 x 768, pieces of
+//   4096: 192 K blocks where 166 are the average); the logits' short ones fill them up.
 //
 // D has the operands' type; FP8 operands are converted to FP16, which holds them exactly, and D is FP16.  FP16 has few
 // exponents, so D is stored times a power of two that brings the largest row coefficient to 2^13..2^14 (probabilities down to
@@ -45,6 +46,7 @@ constexpr uint32_t kRing = kStages * (kABytes + kBBytes);
 constexpr size_t kSmem = size_t(kRing) + 1024 + 256;
 constexpr int kHalf = kTN / 2;      // columns of a tile that one epilogue warp takes
 constexpr int kChunks = kHalf / 32;
+constexpr float kLog2E = 1.4426950408889634f;
 
 template <bool F8>
 __device__ __forceinline__ void umma_pair(uint32_t d_tmem, uint64_t ad, uint64_t bd, uint32_t idesc, uint32_t acc) {
@@ -115,10 +117,10 @@ struct Engine {
 
   // ---- warp 0, lane 0: the operand blocks of one tile.  Along K: a box of 128 bytes x 128 rows.  MN-major (16-bit only):
   // two boxes of 64 columns x the 64 lines of this K block.
-  __device__ __forceinline__ bool produce(const CUtensorMap* ma, const CUtensorMap* mb, int m0, int n0, int num_kb, bool a_mn, bool b_mn) {
+  __device__ __forceinline__ bool produce(const CUtensorMap* ma, const CUtensorMap* mb, int m0, int n0, int kb0, int num_kb, bool a_mn, bool b_mn) {
     m0 += static_cast<int>(rank) * kTM;
     n0 += static_cast<int>(rank) * (kTN / 2);
-    for (int kb = 0; kb < num_kb; ++kb) {
+    for (int kb = kb0; kb < kb0 + num_kb; ++kb) {
       if (!mbar_wait(empty_bar + 8 * stage, phase ^ 1u, abort_flag)) return false;
       const uint32_t sa = smem_a + stage * kABytes, sb = smem_b + stage * kBBytes;
       if (rank == 0u) mbar_expect_tx(full_bar + 8 * stage, 2 * (kABytes + kBBytes));
@@ -190,8 +192,26 @@ struct Engine {
     tc_fence_after();
     return true;
   }
-  __device__ __forceinline__ uint32_t accumulator(int half) const {  // this warp's lanes, its half of the columns
-    return tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16) + acc * kTN + half * kHalf;
+  // f(32 columns of this lane's row, chunk) for the chunks of this warp's half that lie inside the matrix (`cols` of them
+  // from the half's first one); the next chunk is read while f works on the current one
+  template <class F> __device__ __forceinline__ void each_chunk(int half, int cols, F f) {
+    const uint32_t t_addr = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16) + acc * kTN + half * kHalf;
+    const int n_chunks = max(0, min(kChunks, (cols + 31) / 32));
+    uint32_t ra[32], rb[32];
+    if (n_chunks > 0) tmem_ld32(t_addr, ra);
+#pragma unroll 1
+    for (int c = 0; c < n_chunks; c += 2) {
+      tmem_ld_wait();
+      if (c + 1 < n_chunks) tmem_ld32(t_addr + (c + 1) * 32, rb);
+      f(ra, c);
+      __syncwarp();
+      if (c + 1 < n_chunks) {
+        tmem_ld_wait();
+        if (c + 2 < n_chunks) tmem_ld32(t_addr + (c + 2) * 32, ra);
+        f(rb, c + 1);
+        __syncwarp();
+      }
+    }
   }
   __device__ __forceinline__ void release_accumulator() {
     tc_fence_before();
@@ -289,7 +309,7 @@ __device__ __forceinline__ float pick32(const uint32_t* r, int i) {
   return __uint_as_float(a[0]);
 }
 
-template <bool F8, bool GRAD, bool KD, bool BF>
+template <bool F8, bool KD>
 __global__ void __launch_bounds__(kThreads, 1) logits_kernel(const __grid_constant__ CUtensorMap map_h,
                                                              const __grid_constant__ CUtensorMap map_w, const LogitsParams p) {
   asm volatile("griddepcontrol.launch_dependents;");  // the next kernel may set up while this one runs
@@ -308,7 +328,7 @@ __global__ void __launch_bounds__(kThreads, 1) logits_kernel(const __grid_consta
       for (long long item = unit; item < p.items && !timed_out; item += num_units) {
         const int mt = static_cast<int>(item % p.tiles_m), nt0 = static_cast<int>(item / p.tiles_m) * p.run;
         for (int nt = nt0; nt < min(nt0 + p.run, p.tiles_n) && !timed_out; ++nt)
-          timed_out = !e.produce(&map_h, &map_w, mt * 2 * kTM, nt * kTN, p.num_kb, false, false);
+          timed_out = !e.produce(&map_h, &map_w, mt * 2 * kTM, nt * kTN, 0, p.num_kb, false, false);
       }
       if (timed_out || *e.abort_flag) e.drain_copies();
     }
@@ -322,57 +342,188 @@ __global__ void __launch_bounds__(kThreads, 1) logits_kernel(const __grid_consta
     }
   } else {
     const int half = (e.warp - 2) >> 2, quarter = e.warp & 3;
-    const float c2 = load_scale_after_wait(p.h_scale) * load_scale_after_wait(p.w_scale) * p.inv_temp * 1.4426950408889634f;
+    const float c2 = load_scale_after_wait(p.h_scale) * load_scale_after_wait(p.w_scale) * p.inv_temp * kLog2E;
     Targets<KD> target;
     for (long long item = unit; item < p.items && !timed_out; item += num_units) {
       const int mt = static_cast<int>(item % p.tiles_m), ng = static_cast<int>(item / p.tiles_m), nt0 = ng * p.run;
       const int row = mt * 2 * kTM + static_cast<int>(e.rank) * kTM + quarter * 32 + e.lane;
-      target.start(p, row, half, p.col0 + static_cast<long long>(nt0) * kTN);
-      float top = -INFINITY, sum = 0.f, dot = 0.f;  // forward
-      float2 coef = make_float2(0.f, 0.f);          // gradient
-      float lse2 = 0.f;
-      if constexpr (GRAD) {
-        if (row < p.n) {
-          coef = __ldcg(p.coef + row);
-          lse2 = __ldcg(p.lse + row) * 1.4426950408889634f;
-        }
-      }
+      const bool warp_rows = row - e.lane < p.n;  // whether any of this warp's rows exists
+      target.start(p, row, half, static_cast<long long>(nt0) * kTN);
+      float top = -INFINITY, sum = 0.f, dot = 0.f;
       for (int nt = nt0; nt < min(nt0 + p.run, p.tiles_n); ++nt) {
         if (!e.wait_accumulator()) { timed_out = true; break; }
-        const uint32_t t_addr = e.accumulator(half);
         const int n0 = nt * kTN + half * kHalf;
-        const int n_chunks = max(0, min(kChunks, (p.cols - n0 + 31) / 32));  // chunks inside the matrix
-        uint32_t ra[32], rb[32];
-        auto work = [&](uint32_t* r, int c) {
+        e.each_chunk(half, warp_rows ? p.cols - n0 : 0, [&](uint32_t* r, int c) {
           const int c0 = n0 + c * 32, valid = p.cols - c0;
-          const long long g0 = p.col0 + c0;
-          if constexpr (!GRAD) {
-            while (__any_sync(0xFFFFFFFFu, target.id < g0 + 32)) {
-              const float z = pick32(r, static_cast<int>(target.id - g0) & 31);
-              if (target.id < g0 + 32) {
-                dot = fmaf(target.q, z, dot);
-                target.advance();
-              }
+          while (__any_sync(0xFFFFFFFFu, target.id < c0 + 32ll)) {
+            const float z = pick32(r, (target.id - c0) & 31);
+            if (target.id < c0 + 32ll) {
+              dot = fmaf(target.q, z, dot);
+              target.advance();
             }
-            if (valid < 32) {
+          }
+          if (valid < 32) {
 #pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (i >= valid) r[i] = 0xFF800000u;  // -inf
-            }
-            float m = __uint_as_float(r[0]);
+            for (int i = 0; i < 32; ++i)
+              if (i >= valid) r[i] = 0xFF800000u;  // -inf
+          }
+          float m = __uint_as_float(r[0]);
 #pragma unroll
-            for (int i = 1; i < 32; ++i) m = fmaxf(m, __uint_as_float(r[i]));
-            m *= c2;
-            if (m > top) {  // (a row of -inf so far: sum is 0)
-              sum *= exp2_approx(top - m);
-              top = m;
-            }
-            const float shift = top == -INFINITY ? 0.f : -top;
-            float s[4] = {0.f, 0.f, 0.f, 0.f};
+          for (int i = 1; i < 32; ++i) m = fmaxf(m, __uint_as_float(r[i]));
+          m *= c2;
+          if (m > top) {  // (a row of -inf so far: sum is 0)
+            sum *= exp2_approx(top - m);
+            top = m;
+          }
+          const float shift = top == -INFINITY ? 0.f : -top;
+          float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = 0; i < 32; ++i) s[i & 3] += exp2_approx(fmaf(__uint_as_float(r[i]), c2, shift));
-            sum += (s[0] + s[1]) + (s[2] + s[3]);
-          } else {
+          for (int i = 0; i < 32; ++i) s[i & 3] += exp2_approx(fmaf(__uint_as_float(r[i]), c2, shift));
+          sum += (s[0] + s[1]) + (s[2] + s[3]);
+        });
+        e.release_accumulator();
+      }
+      if (row < p.n && !timed_out) {
+        const long long o = static_cast<long long>(ng * 2 + half) * p.ld_part + row;
+        p.partial[o] = make_float2(top, sum);
+        p.dot[o] = dot;
+      }
+    }
+  }
+  if (timed_out) atomicOr(p.status, static_cast<uint32_t>(SCALIFY_DEV_TIMEOUT));
+  e.tear_down();
+}
+
+// ------------------------------------------------------------------------------------------------- gradient kernel
+// What the CTA pairs of one launch share: tiles of the products dW = D^T H and dH = D W of one piece of the vocabulary, and of
+// the logits (the gradient D) of the NEXT piece, which fill the pairs up to equal loads whatever the products' tiles leave.
+enum { kClassDw = 0, kClassDh = 1, kClassD = 2, kClasses = 3 };
+constexpr int kMaxUnits = 80;
+constexpr int kListed = 128;
+struct Schedule {
+  int order[kClasses];               // long tiles first
+  int total[kClasses];
+  int quota[kClasses][kMaxUnits];    // of every pair
+};
+// The j-th item of a pair: numbered so that the pairs work on neighbouring items and finish together (pairs with a smaller
+// quota join later): counted from the end, round b holds the pairs with a quota above b.
+__device__ __forceinline__ int scheduled_item(const Schedule& s, int cls, int unit, int units, int j) {
+  const int b = s.quota[cls][unit] - 1 - j;
+  int behind = 0;
+  for (int u = 0; u < units; ++u) {
+    const int q = s.quota[cls][u];
+    behind += min(q, b) + (u < unit && q > b);
+  }
+  return s.total[cls] - 1 - behind;
+}
+
+enum { kFinal = 0, kAccFirst = 1, kAccNext = 2, kAccLast = 3 };  // what a product does with the fp32 sums of earlier pieces
+struct GradProduct {
+  int M, N, num_kb;
+  int tiles_n;
+  int parts, part_kb;   // the contraction in parts, one plane of sums each
+  void* out;
+  long long ldo;
+  int out_dt;
+  float alpha;
+  int mode;
+  float* acc;           // [parts][M][ld_acc]
+  long long ld_acc;
+};
+struct GradParams {
+  Schedule schedule;
+  GradProduct product[2];  // dW, dH
+  LogitsParams logits;
+  uint32_t idesc;          // of the products
+  const float* unit;       // [0]: the power of two that D is stored times; [1]: what its products are multiplied by
+};
+struct GradMaps { CUtensorMap h, w, d_mn, h_mn, d_k, w_mn; };
+
+template <bool F8, bool KD, bool BF>
+__global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradParams p) {
+  asm volatile("griddepcontrol.launch_dependents;");  // the next kernel may set up while this one runs
+  extern __shared__ uint8_t smem_raw[];
+  Engine e;
+  const int unit = blockIdx.x >> 1, units = gridDim.x >> 1;
+  if (threadIdx.x < 6 && p.schedule.total[threadIdx.x < 2 ? kClassD : threadIdx.x < 4 ? kClassDw : kClassDh] > 0)  // (the others are not filled in)
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&maps.h + threadIdx.x)) : "memory");
+  __shared__ int s_item[kClasses][kListed];  // this pair's first items
+  for (int i = threadIdx.x; i < kClasses * kListed; i += kThreads)
+    if (i % kListed < p.schedule.quota[i / kListed][unit]) s_item[i / kListed][i % kListed] = scheduled_item(p.schedule, i / kListed, unit, units, i % kListed);
+  e.set_up(smem_raw);
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // nothing above touches what the kernel before writes
+  const LogitsParams& l = p.logits;
+  bool timed_out = false;
+  // every role walks the same items: f(class, item)
+  auto each_item = [&](auto f) {
+    for (int k = 0; k < kClasses && !timed_out; ++k) {
+      const int cls = p.schedule.order[k], mine = p.schedule.quota[cls][unit];
+      for (int j = 0; j < mine && !timed_out; ++j) f(cls, j < kListed ? s_item[cls][j] : scheduled_item(p.schedule, cls, unit, units, j));
+    }
+  };
+  // item of a product -> part, row tile, column tile (column tiles of one row tile beside each other: they share D)
+  auto locate = [&](const GradProduct& g, int item, int& part, int& mt, int& nt) {
+    part = item % g.parts;
+    nt = item / g.parts;
+    mt = nt / g.tiles_n;
+    nt -= mt * g.tiles_n;
+    return min(g.part_kb, g.num_kb - part * g.part_kb);  // K blocks
+  };
+  if (e.warp == 0) {
+    if (e.lane == 0) {
+      asm volatile("fence.proxy.async;" ::: "memory");  // the copies read what ordinary stores have written
+      each_item([&](int cls, int item) {
+        if (cls == kClassD) {
+          const int mt = item % l.tiles_m, nt0 = item / l.tiles_m * l.run;
+          for (int nt = nt0; nt < min(nt0 + l.run, l.tiles_n) && !timed_out; ++nt)
+            timed_out = !e.produce(&maps.h, &maps.w, mt * 2 * kTM, nt * kTN, 0, l.num_kb, false, false);
+        } else {
+          const GradProduct& g = p.product[cls];
+          int part, mt, nt;
+          const int kbs = locate(g, item, part, mt, nt);
+          timed_out = cls == kClassDw ? !e.produce(&maps.d_mn, &maps.h_mn, mt * 2 * kTM, nt * kTN, part * g.part_kb, kbs, true, true)
+                                      : !e.produce(&maps.d_k, &maps.w_mn, mt * 2 * kTM, nt * kTN, part * g.part_kb, kbs, false, true);
+        }
+      });
+      if (timed_out || *e.abort_flag) e.drain_copies();
+    }
+  } else if (e.warp == 1) {
+    if (e.lane == 0 && e.rank == 0u) {
+      each_item([&](int cls, int item) {
+        if (cls == kClassD) {
+          const int nt0 = item / l.tiles_m * l.run;
+          for (int nt = nt0; nt < min(nt0 + l.run, l.tiles_n) && !timed_out; ++nt) timed_out = !e.template multiply<F8>(l.num_kb, l.idesc, false, false);
+        } else {
+          int part, mt, nt;
+          const int kbs = locate(p.product[cls], item, part, mt, nt);
+          timed_out = !e.template multiply<false>(kbs, p.idesc, cls == kClassDw, true);
+        }
+      });
+      if (timed_out || *e.abort_flag) e.drain_multiplies();
+    }
+  } else {
+    const int half = (e.warp - 2) >> 2, quarter = e.warp & 3;
+    const int lane_row = static_cast<int>(e.rank) * kTM + quarter * 32 + e.lane;
+    const float c2 = load_scale_after_wait(l.h_scale) * load_scale_after_wait(l.w_scale) * l.inv_temp * kLog2E;
+    const float unit_d = reinterpret_cast<const volatile float*>(p.unit)[0], factor = reinterpret_cast<const volatile float*>(p.unit)[1];
+    each_item([&](int cls, int item) {
+      if (cls == kClassD) {
+        const int row = item % l.tiles_m * 2 * kTM + lane_row, nt0 = item / l.tiles_m * l.run;
+        Targets<KD> target;
+        target.start(l, row, half, l.col0 + static_cast<long long>(nt0) * kTN);
+        float2 coef = make_float2(0.f, 0.f);
+        float lse2 = 0.f;
+        if (row < l.n) {
+          coef = __ldcg(l.coef + row);
+          coef.x *= unit_d; coef.y *= unit_d;
+          lse2 = __ldcg(l.lse + row) * kLog2E;
+        }
+        for (int nt = nt0; nt < min(nt0 + l.run, l.tiles_n); ++nt) {
+          if (!e.wait_accumulator()) { timed_out = true; break; }
+          const int n0 = nt * kTN + half * kHalf;
+          e.each_chunk(half, row - e.lane < l.n ? l.cols - n0 : 0, [&](uint32_t* r, int c) {
+            const int c0 = n0 + c * 32;
+            const long long g0 = l.col0 + c0;
             float v[32];
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = coef.x * exp2_approx(fmaf(__uint_as_float(r[i]), c2, -lse2));
@@ -388,165 +539,64 @@ __global__ void __launch_bounds__(kThreads, 1) logits_kernel(const __grid_consta
             }
             uint32_t o[16];
             encode_vec<BF ? SCALIFY_BF16 : SCALIFY_F16, 32>(v, o);
-            if (row < p.n) {
-              char* dst = reinterpret_cast<char*>(p.D + static_cast<long long>(row) * p.ldd + c0);  // (rows are padded to whole chunks)
+            if (row < l.n) {
+              char* dst = reinterpret_cast<char*>(l.D + static_cast<long long>(row) * l.ldd + c0);  // (rows are padded to whole chunks)
               st_bytes<32>(dst, o);
               st_bytes<32>(dst + 32, o + 8);
             }
-          }
-        };
-        if (n_chunks > 0) tmem_ld32(t_addr, ra);
-#pragma unroll 1
-        for (int c = 0; c < n_chunks; c += 2) {
-          tmem_ld_wait();
-          if (c + 1 < n_chunks) tmem_ld32(t_addr + (c + 1) * 32, rb);
-          work(ra, c);
-          if (c + 1 < n_chunks) {
-            tmem_ld_wait();
-            if (c + 2 < n_chunks) tmem_ld32(t_addr + (c + 2) * 32, ra);
-            work(rb, c + 1);
-          }
+          });
+          e.release_accumulator();
         }
-        e.release_accumulator();
-      }
-      if constexpr (!GRAD) {
-        if (row < p.n && !timed_out) {
-          const long long o = static_cast<long long>(ng * 2 + half) * p.ld_part + row;
-          p.partial[o] = make_float2(top, sum);
-          p.dot[o] = dot;
-        }
-      }
-    }
-  }
-  if (timed_out) atomicOr(p.status, static_cast<uint32_t>(SCALIFY_DEV_TIMEOUT));
-  e.tear_down();
-}
-
-// ------------------------------------------------------------------------------------------------- products kernel
-enum { kFinal = 0, kAccFirst = 1, kAccNext = 2, kAccLast = 3 };  // what a product does with the fp32 sums of earlier pieces
-struct GradProduct {
-  int M, N, num_kb;
-  int tiles_m, tiles_n;
-  void* out;
-  long long ldo;
-  int out_dt;
-  float alpha;
-  int mode;
-  float* acc;           // [M][ld_acc]
-  long long ld_acc;
-};
-struct GradParams {
-  GradProduct dw, dh;   // D^T H and D W
-  int dw_tiles, dh_tiles;
-  bool dw_first;        // the product with the longer contraction goes first
-  uint32_t idesc;
-  const float* unit;    // 1 / the power of two that D is stored times
-  uint32_t* status;
-};
-
-__global__ void __launch_bounds__(kThreads, 1) loss_products_kernel(const __grid_constant__ CUtensorMap map_d_mn,
-                                                                    const __grid_constant__ CUtensorMap map_h_mn,
-                                                                    const __grid_constant__ CUtensorMap map_d_k,
-                                                                    const __grid_constant__ CUtensorMap map_w_mn, const GradParams p) {
-  asm volatile("griddepcontrol.launch_dependents;");  // the next kernel may set up while this one runs
-  extern __shared__ uint8_t smem_raw[];
-  Engine e;
-  if (threadIdx.x == 0) {
-    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_d_mn)) : "memory");
-    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_h_mn)) : "memory");
-    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_d_k)) : "memory");
-    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_w_mn)) : "memory");
-  }
-  e.set_up(smem_raw);
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int unit = blockIdx.x >> 1, num_units = gridDim.x >> 1, tiles = p.dw_tiles + p.dh_tiles;
-  bool timed_out = false;
-  // tile -> product, row tile, column tile (column tiles of one row tile beside each other: they share the operand D)
-  auto locate = [&](int t, int& mt, int& nt) {
-    bool dw = p.dw_first;
-    const int first = dw ? p.dw_tiles : p.dh_tiles;
-    if (t >= first) { t -= first; dw = !dw; }
-    const int tn = dw ? p.dw.tiles_n : p.dh.tiles_n;
-    mt = t / tn;
-    nt = t - mt * tn;
-    return dw;
-  };
-  if (e.warp == 0) {
-    if (e.lane == 0) {
-      asm volatile("fence.proxy.async;" ::: "memory");  // the copies read what ordinary stores have written
-      for (int t = unit; t < tiles && !timed_out; t += num_units) {
-        int mt, nt;
-        if (locate(t, mt, nt)) timed_out = !e.produce(&map_d_mn, &map_h_mn, mt * 2 * kTM, nt * kTN, p.dw.num_kb, true, true);
-        else timed_out = !e.produce(&map_d_k, &map_w_mn, mt * 2 * kTM, nt * kTN, p.dh.num_kb, false, true);
-      }
-      if (timed_out || *e.abort_flag) e.drain_copies();
-    }
-  } else if (e.warp == 1) {
-    if (e.lane == 0 && e.rank == 0u) {
-      for (int t = unit; t < tiles && !timed_out; t += num_units) {
-        int mt, nt;
-        const bool dw = locate(t, mt, nt);
-        timed_out = !e.template multiply<false>(dw ? p.dw.num_kb : p.dh.num_kb, p.idesc, dw, true);
-      }
-      if (timed_out || *e.abort_flag) e.drain_multiplies();
-    }
-  } else {
-    const int half = (e.warp - 2) >> 2, quarter = e.warp & 3;
-    const float inv_unit = *reinterpret_cast<const volatile float*>(p.unit);
-    for (int t = unit; t < tiles; t += num_units) {
-      int mt, nt;
-      const bool dw = locate(t, mt, nt);
-      const GradProduct& g = dw ? p.dw : p.dh;
-      const float alpha = g.alpha * inv_unit;
-      const int n0 = nt * kTN + half * kHalf, row = mt * 2 * kTM + static_cast<int>(e.rank) * kTM + quarter * 32 + e.lane;
-      const int n_chunks = max(0, min(kChunks, (g.N - n0 + 31) / 32));
-      if (!e.wait_accumulator()) { timed_out = true; break; }
-      const uint32_t t_addr = e.accumulator(half);
-#pragma unroll 1
-      for (int c = 0; c < n_chunks; ++c) {
-        uint32_t r[32];
-        tmem_ld32(t_addr + c * 32, r);
-        const int col = n0 + c * 32;
-        float4* acc = reinterpret_cast<float4*>(g.acc + static_cast<long long>(row) * g.ld_acc + col);  // (padded to whole chunks)
-        float4 prev[8];
+      } else {
+        const GradProduct& g = p.product[cls];
+        int part, mt, nt;
+        locate(g, item, part, mt, nt);
+        const float alpha = g.alpha * factor;
+        const int row = mt * 2 * kTM + lane_row, n0 = nt * kTN + half * kHalf;
+        const int mode = g.mode;
+        float* acc_row = g.acc + (static_cast<long long>(part) * g.M + row) * g.ld_acc + n0;  // (padded to whole chunks)
+        char* out_row = static_cast<char*>(g.out) + (static_cast<long long>(row) * g.ldo + n0) * 2;
+        if (!e.wait_accumulator()) { timed_out = true; return; }
+        e.each_chunk(half, row - e.lane < g.M ? g.N - n0 : 0, [&](uint32_t* r, int c) {
+          float v[32];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) prev[j] = g.mode >= kAccNext && row < g.M ? __ldcg(acc + j) : make_float4(0.f, 0.f, 0.f, 0.f);
-        tmem_ld_wait();
-        float v[32];
+          for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+          if (row < g.M) {
+            char* acc = reinterpret_cast<char*>(acc_row + c * 32);
+            if (mode >= kAccNext) {
+              uint32_t before[32];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          v[4 * j] = __uint_as_float(r[4 * j]) + prev[j].x;
-          v[4 * j + 1] = __uint_as_float(r[4 * j + 1]) + prev[j].y;
-          v[4 * j + 2] = __uint_as_float(r[4 * j + 2]) + prev[j].z;
-          v[4 * j + 3] = __uint_as_float(r[4 * j + 3]) + prev[j].w;
-        }
-        if (row < g.M) {
-          if (g.mode == kAccFirst || g.mode == kAccNext) {
+              for (int j = 0; j < 4; ++j) ld_bytes<32, false>(acc + j * 32, before + j * 8);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) __stcg(acc + j, make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
-          } else {
+              for (int i = 0; i < 32; ++i) v[i] += __uint_as_float(before[i]);
+            }
+            if (mode == kAccFirst || mode == kAccNext) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] *= alpha;
-            uint16_t* dst = static_cast<uint16_t*>(g.out) + static_cast<long long>(row) * g.ldo + col;
-            uint32_t o[16];
-            if (g.out_dt == SCALIFY_BF16) encode_vec<SCALIFY_BF16, 32>(v, o);
-            else encode_vec<SCALIFY_F16, 32>(v, o);
-            if (col + 32 <= g.N) {
-              st_bytes<32>(reinterpret_cast<char*>(dst), o);
-              st_bytes<32>(reinterpret_cast<char*>(dst + 16), o + 8);
+              for (int j = 0; j < 4; ++j) st_bytes<32>(acc + j * 32, reinterpret_cast<const uint32_t*>(v) + j * 8);
             } else {
 #pragma unroll
-              for (int i = 0; i < 32; ++i)
-                if (col + i < g.N) dst[i] = static_cast<uint16_t>((i & 1) ? o[i / 2] >> 16 : o[i / 2]);
+              for (int i = 0; i < 32; ++i) v[i] *= alpha;
+              uint32_t o[16];
+              if (g.out_dt == SCALIFY_BF16) encode_vec<SCALIFY_BF16, 32>(v, o);
+              else encode_vec<SCALIFY_F16, 32>(v, o);
+              const int left = g.N - n0 - c * 32;
+              char* dst = out_row + c * 64;
+              if (left >= 32) {
+                st_bytes<32>(dst, o);
+                st_bytes<32>(dst + 32, o + 8);
+              } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                  if (i < left) reinterpret_cast<uint16_t*>(dst)[i] = static_cast<uint16_t>((i & 1) ? o[i / 2] >> 16 : o[i / 2]);
+              }
             }
           }
-        }
-        __syncwarp();
+        });
+        e.release_accumulator();
       }
-      e.release_accumulator();
-    }
+    });
   }
-  if (timed_out) atomicOr(p.status, static_cast<uint32_t>(SCALIFY_DEV_TIMEOUT));
+  if (timed_out) atomicOr(l.status, static_cast<uint32_t>(SCALIFY_DEV_TIMEOUT));
   e.tear_down();
 }
 
@@ -678,14 +728,23 @@ struct JoinParams {
   uint32_t* ticket; uint32_t* status;
 };
 constexpr int kJoinThreads = 256;
-// Joins a row's partial results: 256 >> rows_log threads share a row.  The mean is the sum of the blocks' fp64 sums, in order.
+__device__ __forceinline__ void warp_sums(double& x, double& y) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
+    y += __shfl_xor_sync(0xFFFFFFFFu, y, o);
+  }
+}
+// Joins a row's partial results: 256 >> rows_log threads share a row (at most 32 rows a block, the first warp's).  The mean is
+// the sum of the blocks' fp64 sums, in a fixed order, by the block that is done last.
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const JoinParams p) {
   asm volatile("griddepcontrol.launch_dependents;");
   __shared__ float s_top[kJoinThreads], s_sum[kJoinThreads], s_dot[kJoinThreads];
-  __shared__ double s_a[kJoinThreads], s_b[kJoinThreads];
+  __shared__ double s_a[kJoinThreads / 32], s_b[kJoinThreads / 32];
   __shared__ bool s_last;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int rows = 1 << p.rows_log, lr = threadIdx.x & (rows - 1), part = threadIdx.x >> p.rows_log, parts = kJoinThreads >> p.rows_log;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const long long row = (static_cast<long long>(blockIdx.x) << p.rows_log) + lr;
   float top = -INFINITY, sum = 0.f, dot = 0.f;
   if (row < p.n) {
@@ -713,47 +772,58 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const JoinParams p) 
       top = m;
     }
   }
-  s_top[threadIdx.x] = top; s_sum[threadIdx.x] = sum; s_dot[threadIdx.x] = dot;
-  __syncthreads();
-  double total = 0.0, count = 0.0;
-  if (part == 0 && row < p.n) {
-    for (int j = 1; j < parts; ++j) top = fmaxf(top, s_top[lr + (j << p.rows_log)]);
-    const float shift = top == -INFINITY ? 0.f : top;
-    sum = 0.f; dot = 0.f;
-    for (int j = 0; j < parts; ++j) {
-      const int o = lr + (j << p.rows_log);
-      sum = fmaf(s_sum[o], exp2f(s_top[o] - shift), sum);
-      dot += s_dot[o];
+  // a row's threads in pairs: through shared memory while they lie in different warps, then by shuffles
+  auto join = [&](float top2, float sum2, float dot2) {
+    const float m = fmaxf(top, top2), shift = m == -INFINITY ? 0.f : m;
+    sum = sum * exp2f(top - shift) + sum2 * exp2f(top2 - shift);
+    dot += dot2;
+    top = m;
+  };
+  for (int half = parts / 2; half > 0; half /= 2) {
+    if (half << p.rows_log >= 32) {
+      __syncthreads();
+      s_top[threadIdx.x] = top; s_sum[threadIdx.x] = sum; s_dot[threadIdx.x] = dot;
+      __syncthreads();
+      const int other = threadIdx.x + (half << p.rows_log);
+      if (part < half) join(s_top[other], s_sum[other], s_dot[other]);
+    } else {
+      const float t2 = __shfl_down_sync(0xFFFFFFFFu, top, half << p.rows_log), s2 = __shfl_down_sync(0xFFFFFFFFu, sum, half << p.rows_log);
+      const float d2 = __shfl_down_sync(0xFFFFFFFFu, dot, half << p.rows_log);
+      if (part < half) join(t2, s2, d2);
     }
-    const float lse = (top + log2f(sum)) * 0.6931471805599453f;
-    const float hw = load_scale_after_wait(p.h_scale) * load_scale_after_wait(p.w_scale);
-    float2 qe;
-    bool bad = false;
-    const bool counts = row_target(p.ids, p.padding_id, p.vocab, p.counts, p.sums, row, &qe, &bad);
-    if (bad) atomicOr(p.status, static_cast<uint32_t>(SCALIFY_DEV_BAD_INDEX));
-    const float loss = counts ? qe.y + (qe.x * lse - dot * (hw * p.inv_temp)) + (p.z_loss > 0.f ? p.z_loss * lse * lse : 0.f) : 0.f;
-    p.loss[row] = loss;
-    p.lse[row] = lse;
-    total = loss;
-    count = counts ? 1.0 : 0.0;
-    if (row == 0 && (!is_pow2_scale(load_scale_after_wait(p.h_scale)) || !is_pow2_scale(load_scale_after_wait(p.w_scale))))
-      atomicOr(p.status, static_cast<uint32_t>(SCALIFY_DEV_BAD_SCALE));
+  }
+  double total = 0.0, count = 0.0;
+  if (warp == 0) {
+    if (part == 0 && row < p.n) {
+      const float lse = (top + log2f(sum)) * 0.6931471805599453f;
+      const float hw = load_scale_after_wait(p.h_scale) * load_scale_after_wait(p.w_scale);
+      float2 qe;
+      bool bad = false;
+      const bool counts = row_target(p.ids, p.padding_id, p.vocab, p.counts, p.sums, row, &qe, &bad);
+      if (bad) atomicOr(p.status, static_cast<uint32_t>(SCALIFY_DEV_BAD_INDEX));
+      const float loss = counts ? qe.y + (qe.x * lse - dot * (hw * p.inv_temp)) + (p.z_loss > 0.f ? p.z_loss * lse * lse : 0.f) : 0.f;
+      p.loss[row] = loss;
+      p.lse[row] = lse;
+      total = loss;
+      count = counts ? 1.0 : 0.0;
+      if (row == 0 && (!is_pow2_scale(load_scale_after_wait(p.h_scale)) || !is_pow2_scale(load_scale_after_wait(p.w_scale))))
+        atomicOr(p.status, static_cast<uint32_t>(SCALIFY_DEV_BAD_SCALE));
+    }
+    if (p.mean) {
+      warp_sums(total, count);
+      if (lane == 0) {
+        if (gridDim.x == 1) {
+          *p.mean = static_cast<float>(total / (count > 0.0 ? count : 1.0));
+          s_last = false;
+        } else {
+          p.block_sums[blockIdx.x] = make_double2(total, count);
+          __threadfence();
+          s_last = atomicAdd(p.ticket, 1u) == gridDim.x - 1;
+        }
+      }
+    }
   }
   if (!p.mean) return;
-  auto block_sum = [&]() {
-    s_a[threadIdx.x] = total; s_b[threadIdx.x] = count;
-    for (int o = kJoinThreads / 2; o; o >>= 1) {
-      __syncthreads();
-      if (static_cast<int>(threadIdx.x) < o) { s_a[threadIdx.x] += s_a[threadIdx.x + o]; s_b[threadIdx.x] += s_b[threadIdx.x + o]; }
-    }
-    __syncthreads();
-  };
-  block_sum();
-  if (threadIdx.x == 0) {
-    p.block_sums[blockIdx.x] = make_double2(s_a[0], s_b[0]);
-    __threadfence();
-    s_last = atomicAdd(p.ticket, 1u) == gridDim.x - 1;
-  }
   __syncthreads();
   if (!s_last) return;
   __threadfence();
@@ -762,13 +832,23 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const JoinParams p) 
     const double2 v = __ldcg(p.block_sums + b);
     total += v.x; count += v.y;
   }
-  block_sum();
+  warp_sums(total, count);
+  if (lane == 0) { s_a[warp] = total; s_b[warp] = count; }
+  __syncthreads();
   if (threadIdx.x == 0) {
-    *p.mean = static_cast<float>(s_a[0] / (s_b[0] > 0.0 ? s_b[0] : 1.0));
+    for (int i = 1; i < kJoinThreads / 32; ++i) { total += s_a[i]; count += s_b[i]; }
+    *p.mean = static_cast<float>(total / (count > 0.0 ? count : 1.0));
     *p.ticket = 0u;
   }
 }
 
+// FP8 rows -> FP16 (exact), of H and then of W
+struct WidenParams {
+  const void* src[2]; __half* dst[2];
+  long long ld[2], ldd, rows[2];
+  int dt[2];
+  int d;
+};
 struct CoefParams {
   long long n, vocab;
   const long long* ids; long long padding_id;
@@ -780,61 +860,97 @@ struct CoefParams {
   float mean_p2;            // without grad: 1/n rounded down to a power of two
   const float* h_scale; const float* w_scale;
   float kf_vocab, kf_n;
-  float2* coef; float* inv_unit;
+  float2* coef;
+  uint2* block_tops;        // per block: largest coefficient (bits), rows that count
+  float* unit;              // [0]: the power of two that D is stored times; [1]: what its products are multiplied by
   float* dh_scale; float* dw_scale;
-  uint32_t* status;
+  uint32_t* ticket; uint32_t* status;
+  int blocks;               // of the coefficients; the blocks behind them make the FP16 copies
+  WidenParams widen;
 };
-constexpr int kCoefThreads = 1024;
-// Row coefficients of p and of q, times the power of two that D is stored with; output scales.  One block.
-__global__ void __launch_bounds__(kCoefThreads) coef_kernel(const CoefParams p) {
+constexpr int kCoefThreads = 256;
+constexpr int kCoefBlocks = 256;
+__device__ __forceinline__ void widen_rows(const WidenParams& p, int block, int blocks) {
+  const int vecs = (p.d + 15) / 16;
+  const long long total = (p.rows[0] + p.rows[1]) * vecs;
+  for (long long i = static_cast<long long>(block) * kCoefThreads + threadIdx.x; i < total; i += static_cast<long long>(blocks) * kCoefThreads) {
+    long long row = i / vecs;
+    const int v = static_cast<int>(i - row * vecs), n = p.d - v * 16;
+    const int which = row >= p.rows[0];
+    if (which) row -= p.rows[0];
+    const char* src = static_cast<const char*>(p.src[which]) + row * p.ld[which];
+    uint32_t w[4] = {}, o[8];
+    float f[16];
+    if (n >= 16) {
+      ld_raw<16>(src + v * 16, w);
+    } else {
+      load_vec<SCALIFY_E4M3>(src, 2 * v, n, w);
+      if (n > kVec) load_vec<SCALIFY_E4M3>(src, 2 * v + 1, n - kVec, w + 2);
+    }
+    if (p.dt[which] == SCALIFY_E4M3) decode_vec<SCALIFY_E4M3, 16>(w, f);
+    else decode_vec<SCALIFY_E5M2, 16>(w, f);
+    encode_vec<SCALIFY_F16, 16>(f, o);
+    st_bytes<32>(reinterpret_cast<char*>(p.dst[which] + row * p.ldd + v * 16), o);  // (rows are padded to whole vectors)
+  }
+}
+// Row coefficients of p and of q in units of the upstream gradient (of the mean's, if there is none); the power of two that D
+// is stored times; output scales; FP16 copies of FP8 operands.
+__global__ void __launch_bounds__(kCoefThreads) coef_kernel(const __grid_constant__ CoefParams p) {
   asm volatile("griddepcontrol.launch_dependents;");
-  __shared__ int s_count[32];
-  __shared__ uint32_t s_top[32];
+  __shared__ uint32_t s_top[kCoefThreads / 32];
+  __shared__ int s_count[kCoefThreads / 32];
+  __shared__ bool s_last;
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (static_cast<int>(blockIdx.x) >= p.blocks) return widen_rows(p.widen, blockIdx.x - p.blocks, gridDim.x - p.blocks);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   bool bad = false;
-  float g_mean = 0.f;
-  if (!p.grad) {
-    int count = 0;
-    for (long long row = threadIdx.x; row < p.n; row += kCoefThreads) {
-      float2 qe;
-      count += row_target(p.ids, p.padding_id, p.vocab, p.counts, p.sums, row, &qe, &bad);
-    }
-    count = __reduce_add_sync(0xFFFFFFFFu, count);
-    if (lane == 0) s_count[warp] = count;
-    __syncthreads();
-    int total = 0;
-    for (int i = 0; i < 32; ++i) total += s_count[i];
-    g_mean = 1.0f / static_cast<float>(max(total, 1)) / p.mean_p2;
-  }
   uint32_t top = 0u;
-  for (long long row = threadIdx.x; row < p.n; row += kCoefThreads) {
+  int count = 0;
+  for (long long row = static_cast<long long>(blockIdx.x) * kCoefThreads + threadIdx.x; row < p.n; row += static_cast<long long>(p.blocks) * kCoefThreads) {
     float2 qe;
     float a = 0.f, b = 0.f;
     if (row_target(p.ids, p.padding_id, p.vocab, p.counts, p.sums, row, &qe, &bad)) {
-      b = (p.grad ? __ldg(p.grad + row) : g_mean) * p.rest;
+      b = (p.grad ? __ldg(p.grad + row) : 1.0f) * p.rest;
       a = b * (qe.x + (p.z_loss > 0.f ? 2.f * p.z_loss * __ldg(p.lse + row) : 0.f));
+      ++count;
     }
     p.coef[row] = make_float2(a, b);
     const uint32_t m = max(__float_as_uint(fabsf(a)), __float_as_uint(fabsf(b * qe.x)));
     if (m < 0x7F800000u) top = max(top, m);
   }
   if (bad) atomicOr(p.status, static_cast<uint32_t>(SCALIFY_DEV_BAD_INDEX));
-  top = __reduce_max_sync(0xFFFFFFFFu, top);
-  if (lane == 0) s_top[warp] = top;
-  __syncthreads();
-  for (int i = 0; i < 32; ++i) top = max(top, s_top[i]);
-  // the largest coefficient goes to [2^13, 2^14): |D| stays below 2^15
-  int ex = static_cast<int>(top >> 23) - 127;
-  if (top == 0u) ex = 13;
-  ex = min(max(13 - ex, -100), 100);
-  const float unit = __uint_as_float(static_cast<uint32_t>(127 + ex) << 23);
-  for (long long row = threadIdx.x; row < p.n; row += kCoefThreads) {
-    const float2 c = p.coef[row];  // (this thread wrote it)
-    p.coef[row] = make_float2(c.x * unit, c.y * unit);
-  }
+  auto block_join = [&]() {  // in the first thread
+    top = __reduce_max_sync(0xFFFFFFFFu, top);
+    count = __reduce_add_sync(0xFFFFFFFFu, count);
+    if (lane == 0) { s_top[warp] = top; s_count[warp] = count; }
+    __syncthreads();
+    if (threadIdx.x == 0)
+      for (int i = 1; i < kCoefThreads / 32; ++i) { top = max(top, s_top[i]); count += s_count[i]; }
+  };
+  block_join();
   if (threadIdx.x == 0) {
-    *p.inv_unit = 1.0f / unit;
+    p.block_tops[blockIdx.x] = make_uint2(top, static_cast<uint32_t>(count));
+    __threadfence();
+    s_last = atomicAdd(p.ticket, 1u) == static_cast<uint32_t>(p.blocks - 1);
+  }
+  __syncthreads();
+  if (!s_last) return;
+  __threadfence();
+  top = 0u; count = 0;
+  if (static_cast<int>(threadIdx.x) < p.blocks) {
+    const uint2 v = __ldcg(p.block_tops + threadIdx.x);
+    top = v.x; count = static_cast<int>(v.y);
+  }
+  block_join();
+  if (threadIdx.x == 0) {
+    *p.ticket = 0u;
+    // the largest coefficient goes to [2^13, 2^14): |D| stays below 2^15
+    int ex = static_cast<int>(top >> 23) - 127;
+    if (top == 0u) ex = 13;
+    ex = min(max(13 - ex, -100), 100);
+    const float unit = __uint_as_float(static_cast<uint32_t>(127 + ex) << 23);
+    p.unit[0] = unit;
+    p.unit[1] = (p.grad ? 1.0f : 1.0f / static_cast<float>(max(count, 1)) / p.mean_p2) / unit;
     const float hs = load_scale_after_wait(p.h_scale), ws = load_scale_after_wait(p.w_scale);
     const float gs = p.grad ? load_scale_after_wait(p.grad_scale) : p.mean_p2;
     if (!is_pow2_scale(hs) || !is_pow2_scale(ws) || !is_pow2_scale(gs)) atomicOr(p.status, static_cast<uint32_t>(SCALIFY_DEV_BAD_SCALE));
@@ -844,31 +960,32 @@ __global__ void __launch_bounds__(kCoefThreads) coef_kernel(const CoefParams p) 
   }
 }
 
-// FP8 rows -> FP16 (exact), of H and then of W
-struct WidenParams {
-  const void* src[2]; __half* dst[2];
-  long long ld[2], ldd, rows[2];
-  int dt[2];
-  int d;
+// The sums of dH's planes, in order -> dH
+struct PlanesParams {
+  const float* acc; long long ld_acc; int planes;
+  int M, N;
+  void* out; long long ldo; int out_dt;
+  float alpha; const float* unit;
 };
-__global__ void __launch_bounds__(256) widen_kernel(const WidenParams p) {
+__global__ void __launch_bounds__(256) planes_kernel(const PlanesParams p) {
   asm volatile("griddepcontrol.launch_dependents;");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int vecs = (p.d + kVec - 1) / kVec;
-  const long long total = (p.rows[0] + p.rows[1]) * vecs;
-  for (long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<long long>(gridDim.x) * 256) {
-    long long row = i / vecs;
-    const int v = static_cast<int>(i - row * vecs);
-    const int which = row >= p.rows[0];
-    if (which) row -= p.rows[0];
-    const char* src = static_cast<const char*>(p.src[which]) + row * p.ld[which];
-    uint32_t w[2], o[4];
-    float f[kVec];
-    load_vec<SCALIFY_E4M3>(src, v, p.d - v * kVec, w);
-    if (p.dt[which] == SCALIFY_E4M3) decode_vec<SCALIFY_E4M3, kVec>(w, f);
-    else decode_vec<SCALIFY_E5M2, kVec>(w, f);
-    encode_vec<SCALIFY_F16, kVec>(f, o);
-    st_raw<16>(p.dst[which] + row * p.ldd + v * kVec, o);
+  const int vecs = (p.N + kVec - 1) / kVec;
+  const float alpha = p.alpha * *reinterpret_cast<const volatile float*>(p.unit + 1);
+  for (long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x; i < static_cast<long long>(p.M) * vecs; i += static_cast<long long>(gridDim.x) * 256) {
+    const int row = static_cast<int>(i / vecs), v = static_cast<int>(i - static_cast<long long>(row) * vecs);
+    float f[kVec] = {};
+#pragma unroll 4
+    for (int s = 0; s < p.planes; ++s) {
+      const float4* a = reinterpret_cast<const float4*>(p.acc + (static_cast<long long>(s) * p.M + row) * p.ld_acc + v * kVec);
+      const float4 x = __ldcg(a), y = __ldcg(a + 1);  // (rows are padded to whole vectors)
+      f[0] += x.x; f[1] += x.y; f[2] += x.z; f[3] += x.w; f[4] += y.x; f[5] += y.y; f[6] += y.z; f[7] += y.w;
+    }
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) f[e] *= alpha;
+    char* out = static_cast<char*>(p.out) + static_cast<long long>(row) * p.ldo * 2;
+    if (p.out_dt == SCALIFY_BF16) store_vec<SCALIFY_BF16>(out, v, p.N - v * kVec, f);
+    else store_vec<SCALIFY_F16>(out, v, p.N - v * kVec, f);
   }
 }
 
@@ -886,26 +1003,40 @@ long long pad_to(long long x, long long m) { return (x + m - 1) / m * m; }
 size_t pad256(size_t x) { return (x + 255) / 256 * 256; }
 
 // Consecutive column tiles per work item: long runs write few partial results, short ones share the work evenly.
-int run_length(long long tiles_m, long long tiles_n) {
-  for (int run = 8; run > 1; run >>= 1)
-    if (tiles_m * ((tiles_n + run - 1) / run) >= 16 * kUnits) return run;
+int run_length(long long tiles_m, long long tiles_n, int longest, int per_unit) {
+  for (int run = longest; run > 1; run >>= 1)
+    if (tiles_m * ((tiles_n + run - 1) / run) >= per_unit * kUnits) return run;
   return 1;
 }
-// Columns of a piece of the vocabulary: D of at most 2^26 bytes (half the L2), whole tiles.
+// Columns of a piece of the vocabulary: D of at most 2^27 bytes, two pieces of which are in memory; whole tiles.
+// (8192 x 50257 x 768: half and a quarter of it take 4 and 8 % longer, twice of it 2 % less.)
 long long piece_columns(long long n, long long vocab) {
   const long long rows = pad_to(n < 1 ? 1 : n, 32);
-  long long cols = (1ll << 25) / rows / kTN * kTN;
+  long long cols = (1ll << 26) / rows / kTN * kTN;
   if (cols < kTN) cols = kTN;
   const long long all = pad_to(vocab, kTN);
   if (cols >= all) return all;
   const long long pieces = (all + cols - 1) / cols;
   return pad_to((all + pieces - 1) / pieces, kTN);
 }
+// K blocks that a tile's start and end cost beside its own
+constexpr int kTileCost = 3;
+// Parts of dH's contraction where the whole vocabulary is one piece: few tiles of a long contraction would keep few CTA pairs
+// busy; a part is at most half of a pair's load.
+int dh_parts(long long n, long long vocab, long long d) {
+  const double tm = static_cast<double>((n + 2 * kTM - 1) / (2 * kTM)), tn = static_cast<double>((d + kTN - 1) / kTN), tv = static_cast<double>((vocab + kTN - 1) / kTN);
+  const double kb_v = static_cast<double>((vocab + kK16 - 1) / kK16), kb_n = static_cast<double>((n + kK16 - 1) / kK16);
+  const double load = (tm * tn * (kb_v + kTileCost) + tv * tn * (kb_n + kTileCost)) / kUnits;
+  long long parts = static_cast<long long>(ceil(2.0 * kb_v / load)), most = static_cast<long long>(kb_v / 16);
+  if (parts > 32) parts = 32;
+  if (parts > most) parts = most;
+  return parts < 1 ? 1 : static_cast<int>(parts);
+}
 
 struct Layout {
-  size_t partial, dot, sums_blocks, entries, counts, sums, coef, unit, h16, w16, D, acc, total;
+  size_t partial, dot, sums_blocks, entries, counts, sums, coef, tops, unit, h16, w16, D[2], acc, total;
   long long ld_part, ld16, ldd, ld_acc, piece, pieces;
-  int slots, run;
+  int slots, run, parts;
 };
 Layout layout_of(long long n, long long vocab, long long d, int es, int k, bool backward) {
   Layout l = {};
@@ -919,7 +1050,7 @@ Layout layout_of(long long n, long long vocab, long long d, int es, int k, bool 
     l.sums = take(rows * sizeof(float2));
   }
   if (!backward) {
-    l.run = run_length(tm, tn);
+    l.run = run_length(tm, tn, 8, 16);
     l.slots = static_cast<int>((tn + l.run - 1) / l.run) * 2;
     l.ld_part = pad_to(n, 32);
     l.partial = take(static_cast<size_t>(l.slots) * l.ld_part * sizeof(float2));
@@ -927,8 +1058,9 @@ Layout layout_of(long long n, long long vocab, long long d, int es, int k, bool 
     l.sums_blocks = take((rows / 32 + 32) * sizeof(double2));
   } else {
     l.coef = take(rows * sizeof(float2));
-    l.unit = take(sizeof(float));
-    l.ld16 = pad_to(d, 8);
+    l.tops = take(kCoefBlocks * sizeof(uint2));
+    l.unit = take(2 * sizeof(float));
+    l.ld16 = pad_to(d, 16);
     if (es == 1) {
       l.h16 = take(rows * l.ld16 * 2);
       l.w16 = take(static_cast<size_t>(vocab) * l.ld16 * 2);
@@ -936,10 +1068,12 @@ Layout layout_of(long long n, long long vocab, long long d, int es, int k, bool 
     l.piece = piece_columns(n, vocab);
     l.pieces = (vocab + l.piece - 1) / l.piece;
     l.ldd = l.piece;
-    l.D = take(rows * l.ldd * 2);
-    if (l.pieces > 1) {
+    l.D[0] = take(rows * l.ldd * 2);
+    l.D[1] = l.pieces > 1 ? take(rows * l.ldd * 2) : l.D[0];
+    l.parts = l.pieces == 1 && n > 0 ? dh_parts(n, vocab, d) : 1;
+    if (l.pieces > 1 || l.parts > 1) {
       l.ld_acc = pad_to(d, 32);
-      l.acc = take(rows * l.ld_acc * sizeof(float));
+      l.acc = take(l.parts * rows * l.ld_acc * sizeof(float));
     }
   }
   l.total = at < kWsMin ? kWsMin : at;
@@ -947,7 +1081,7 @@ Layout layout_of(long long n, long long vocab, long long d, int es, int k, bool 
 }
 
 template <class K>
-int pair_config(K kernel, DeviceOnce& once, long long units, cudaStream_t st, cudaLaunchConfig_t* cfg, cudaLaunchAttribute* attrs) {
+int pair_config(K kernel, DeviceOnce& once, long long items, cudaStream_t st, cudaLaunchConfig_t* cfg, cudaLaunchAttribute* attrs, int* units) {
   int most = 0;  // CTA pairs that fit the GPU
   const int rc = device_once(once, &most, [&](int* v) {
     SCALIFY_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem)));
@@ -969,7 +1103,9 @@ int pair_config(K kernel, DeviceOnce& once, long long units, cudaStream_t st, cu
   attrs[1].id = cudaLaunchAttributeClusterDimension;
   attrs[1].val.clusterDim.x = 2; attrs[1].val.clusterDim.y = 1; attrs[1].val.clusterDim.z = 1;
   *cfg = {};
-  cfg->gridDim = dim3(static_cast<unsigned>((units < most ? units : most) * 2));
+  *units = static_cast<int>(items < most ? items : most);
+  if (*units > kMaxUnits) *units = kMaxUnits;
+  cfg->gridDim = dim3(static_cast<unsigned>(*units * 2));
   cfg->blockDim = dim3(kThreads); cfg->dynamicSmemBytes = kSmem; cfg->stream = st;
   cfg->attrs = attrs; cfg->numAttrs = 2;
   return SCALIFY_OK;
@@ -987,24 +1123,78 @@ int launch_small(K kernel, long long blocks, int threads, const P& p, cudaStream
   return SCALIFY_OK;
 }
 
-template <bool F8, bool GRAD, bool KD, bool BF>
-int launch_logits_variant(const CUtensorMap& mh, const CUtensorMap& mw, const LogitsParams& p, cudaStream_t st) {
-  auto kernel = logits_kernel<F8, GRAD, KD, BF>;
+template <bool F8, bool KD>
+int launch_logits(const CUtensorMap& mh, const CUtensorMap& mw, const LogitsParams& p, cudaStream_t st) {
+  auto kernel = logits_kernel<F8, KD>;
   static DeviceOnce once;
   cudaLaunchConfig_t cfg;
   cudaLaunchAttribute attrs[2];
-  const int rc = pair_config(kernel, once, p.items, st, &cfg, attrs);
+  int units = 0;
+  const int rc = pair_config(kernel, once, p.items, st, &cfg, attrs, &units);
   if (rc) return rc;
   SCALIFY_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, mh, mw, p));
   return SCALIFY_OK;
 }
-template <bool GRAD, bool KD>
-int launch_logits(bool f8, bool bf, const CUtensorMap& mh, const CUtensorMap& mw, const LogitsParams& p, cudaStream_t st) {
-  if (f8) return launch_logits_variant<true, GRAD, KD, false>(mh, mw, p, st);
-  if constexpr (GRAD) {
-    if (bf) return launch_logits_variant<false, GRAD, KD, true>(mh, mw, p, st);
+
+// Every class's items over the pairs, long ones first, so that the loads become as equal as whole items allow.
+void fill_schedule(Schedule& s, const long long (&items)[kClasses], const double (&cost)[kClasses], int units) {
+  double load[kMaxUnits] = {};
+  for (int i = 0; i < kClasses; ++i) s.order[i] = i;
+  for (int i = 1; i < kClasses; ++i)
+    for (int j = i; j > 0 && cost[s.order[j]] > cost[s.order[j - 1]]; --j) { const int t = s.order[j]; s.order[j] = s.order[j - 1]; s.order[j - 1] = t; }
+  for (int i = 0; i < kClasses; ++i) {
+    const int c = s.order[i];
+    s.total[c] = static_cast<int>(items[c]);
+    for (int u = 0; u < units; ++u) s.quota[c][u] = 0;
+    if (items[c] == 0) continue;
+    // the highest level up to which whole items fit, then one more for the least loaded pairs
+    double lo = 0.0, hi = 0.0;
+    for (int u = 0; u < units; ++u) hi = load[u] > hi ? load[u] : hi;
+    hi += cost[c] * (static_cast<double>(items[c]) / units + 2.0);
+    auto fits = [&](double level) {
+      long long n = 0;
+      for (int u = 0; u < units; ++u) n += level > load[u] ? static_cast<long long>((level - load[u]) / cost[c]) : 0;
+      return n;
+    };
+    for (int it = 0; it < 60; ++it) {
+      const double mid = 0.5 * (lo + hi);
+      if (fits(mid) <= items[c]) lo = mid; else hi = mid;
+    }
+    long long left = items[c];
+    for (int u = 0; u < units; ++u) {
+      const int q = lo > load[u] ? static_cast<int>((lo - load[u]) / cost[c]) : 0;
+      s.quota[c][u] = q;
+      load[u] += q * cost[c];
+      left -= q;
+    }
+    while (left > 0) {
+      int best = 0;
+      for (int u = 1; u < units; ++u)
+        if (load[u] < load[best]) best = u;
+      ++s.quota[c][best];
+      load[best] += cost[c];
+      --left;
+    }
   }
-  return launch_logits_variant<false, GRAD, KD, false>(mh, mw, p, st);
+}
+
+template <bool F8, bool KD, bool BF>
+int launch_grad(const GradMaps& m, GradParams& p, const long long (&items)[kClasses], const double (&cost)[kClasses], cudaStream_t st) {
+  auto kernel = loss_grad_kernel<F8, KD, BF>;
+  static DeviceOnce once;
+  cudaLaunchConfig_t cfg;
+  cudaLaunchAttribute attrs[2];
+  int units = 0;
+  const int rc = pair_config(kernel, once, items[0] + items[1] + items[2], st, &cfg, attrs, &units);
+  if (rc) return rc;
+  fill_schedule(p.schedule, items, cost, units);
+  SCALIFY_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, m, p));
+  return SCALIFY_OK;
+}
+int launch_grad(bool f8, bool kd, bool bf, const GradMaps& m, GradParams& p, const long long (&items)[kClasses], const double (&cost)[kClasses], cudaStream_t st) {
+  if (f8) return kd ? launch_grad<true, true, false>(m, p, items, cost, st) : launch_grad<true, false, false>(m, p, items, cost, st);
+  if (bf) return kd ? launch_grad<false, true, true>(m, p, items, cost, st) : launch_grad<false, false, true>(m, p, items, cost, st);
+  return kd ? launch_grad<false, true, false>(m, p, items, cost, st) : launch_grad<false, false, false>(m, p, items, cost, st);
 }
 
 // operand formats of the instruction descriptor: kind::f16 F16 0, BF16 1; kind::f8f6f4 E4M3 0, E5M2 1
@@ -1078,7 +1268,10 @@ int launch_linear_loss(const LinearLossArgs& a, void* workspace, cudaStream_t st
   CUtensorMap mh, mw;
   rc = map_of(&mh, a.H, a.n, a.d, a.h_ld, es, kTM);
   if (!rc) rc = map_of(&mw, a.W, a.vocab, a.d, a.w_ld, es, kTN / 2);
-  if (!rc) rc = a.k > 0 ? launch_logits<false, true>(es == 1, false, mh, mw, p, st) : launch_logits<false, false>(es == 1, false, mh, mw, p, st);
+  if (!rc) {
+    if (es == 1) rc = a.k > 0 ? launch_logits<true, true>(mh, mw, p, st) : launch_logits<true, false>(mh, mw, p, st);
+    else rc = a.k > 0 ? launch_logits<false, true>(mh, mw, p, st) : launch_logits<false, false>(mh, mw, p, st);
+  }
   if (rc) return rc;
   JoinParams j = {};
   j.n = a.n; j.vocab = a.vocab; j.slots = l.slots;
@@ -1117,10 +1310,26 @@ int launch_linear_loss_bwd(const LinearLossArgs& a, void* workspace, cudaStream_
   c.h_scale = a.h_scale; c.w_scale = a.w_scale;
   c.kf_vocab = kfactor(a.vocab); c.kf_n = kfactor(a.n > 0 ? a.n : 1);
   c.coef = reinterpret_cast<float2*>(ws + l.coef);
-  c.inv_unit = reinterpret_cast<float*>(ws + l.unit);
+  c.block_tops = reinterpret_cast<uint2*>(ws + l.tops);
+  c.unit = reinterpret_cast<float*>(ws + l.unit);
   c.dh_scale = a.dh_scale; c.dw_scale = a.dw_scale;
-  c.status = ws_view(ws).status;
-  rc = launch_small(coef_kernel, 1, kCoefThreads, c, st);
+  c.ticket = ws_view(ws).ticket; c.status = ws_view(ws).status;
+  c.blocks = static_cast<int>(a.n < kCoefThreads ? 1 : a.n > kCoefThreads * kCoefBlocks ? kCoefBlocks : (a.n + kCoefThreads - 1) / kCoefThreads);
+  const char* h16 = static_cast<const char*>(a.H);
+  const char* w16 = static_cast<const char*>(a.W);
+  long long h16_ld = a.h_ld, w16_ld = a.w_ld, widen_blocks = 0;
+  if (es == 1 && a.n > 0) {
+    WidenParams& w = c.widen;
+    w.d = a.d; w.ldd = l.ld16;
+    w.src[0] = a.H; w.dst[0] = reinterpret_cast<__half*>(ws + l.h16); w.ld[0] = a.h_ld; w.rows[0] = a.dW ? a.n : 0; w.dt[0] = a.h_dt;
+    w.src[1] = a.W; w.dst[1] = reinterpret_cast<__half*>(ws + l.w16); w.ld[1] = a.w_ld; w.rows[1] = a.dH ? a.vocab : 0; w.dt[1] = a.w_dt;
+    const long long most = 16ll * sm_count();
+    widen_blocks = ((w.rows[0] + w.rows[1]) * ((a.d + 15) / 16) + kCoefThreads - 1) / kCoefThreads;
+    if (widen_blocks > most) widen_blocks = most;
+    h16 = ws + l.h16; w16 = ws + l.w16;
+    h16_ld = w16_ld = l.ld16;
+  }
+  rc = launch_small(coef_kernel, c.blocks + widen_blocks, kCoefThreads, c, st);
   if (rc) return rc;
   if (a.n == 0) {
     if (!a.dW) return SCALIFY_OK;
@@ -1128,67 +1337,70 @@ int launch_linear_loss_bwd(const LinearLossArgs& a, void* workspace, cudaStream_
     SCALIFY_CUDA_TRY(cudaGetLastError());
     return SCALIFY_OK;
   }
-  const char* h16 = static_cast<const char*>(a.H);
-  const char* w16 = static_cast<const char*>(a.W);
-  long long h16_ld = a.h_ld, w16_ld = a.w_ld;
-  if (es == 1) {
-    WidenParams w = {};
-    w.d = a.d; w.ldd = l.ld16;
-    w.src[0] = a.H; w.dst[0] = reinterpret_cast<__half*>(ws + l.h16); w.ld[0] = a.h_ld; w.rows[0] = a.dW ? a.n : 0; w.dt[0] = a.h_dt;
-    w.src[1] = a.W; w.dst[1] = reinterpret_cast<__half*>(ws + l.w16); w.ld[1] = a.w_ld; w.rows[1] = a.dH ? a.vocab : 0; w.dt[1] = a.w_dt;
-    const long long blocks = ((w.rows[0] + w.rows[1]) * ((a.d + kVec - 1) / kVec) + 255) / 256, most = 16ll * sm_count();
-    rc = launch_small(widen_kernel, blocks < most ? blocks : most, 256, w, st);
-    if (rc) return rc;
-    h16 = ws + l.h16; w16 = ws + l.w16;
-    h16_ld = w16_ld = l.ld16;
-  }
   const bool bf = a.h_dt == SCALIFY_BF16;
   const int d_dt = bf ? SCALIFY_BF16 : SCALIFY_F16;
-  uint16_t* D = reinterpret_cast<uint16_t*>(ws + l.D);
-  LogitsParams p = logits_params(a, l, ws);
-  p.lse = a.lse; p.coef = c.coef; p.D = D; p.ldd = l.ldd;
-  CUtensorMap mh, mw, d_mn, d_k, h_mn, w_mn;
-  rc = map_of(&mh, a.H, a.n, a.d, a.h_ld, es, kTM);
-  if (!rc) rc = map_of(&h_mn, h16, a.n, a.d, h16_ld, 2, kK16);
+  GradParams g = {};
+  GradMaps m = {};
+  LogitsParams& p = g.logits;
+  p = logits_params(a, l, ws);
+  p.lse = a.lse; p.coef = c.coef; p.ldd = l.ldd;
+  const int row_tiles = p.tiles_m, d_tiles = static_cast<int>((a.d + kTN - 1) / kTN);
+  GradProduct &dw = g.product[kClassDw], &dh = g.product[kClassDh];
+  dw.N = dh.N = a.d;
+  dw.tiles_n = dh.tiles_n = d_tiles;
+  dw.num_kb = dw.part_kb = static_cast<int>((a.n + kK16 - 1) / kK16);
+  dw.parts = 1;
+  dw.ldo = a.dw_ld; dw.out_dt = a.dw_dt; dw.alpha = 1.0f / c.kf_n; dw.mode = kFinal;
+  dh.M = static_cast<int>(a.n);
+  dh.out = a.dH; dh.ldo = a.dh_ld; dh.out_dt = a.dh_dt; dh.alpha = 1.0f / c.kf_vocab;
+  dh.acc = reinterpret_cast<float*>(ws + l.acc); dh.ld_acc = l.ld_acc;
+  g.idesc = idesc_of(d_dt, d_dt);
+  g.unit = c.unit;
+  rc = map_of(&m.h, a.H, a.n, a.d, a.h_ld, es, kTM);
+  if (!rc) rc = map_of(&m.h_mn, h16, a.n, a.d, h16_ld, 2, kK16);
   if (rc) return rc;
-  const long long row_tiles = p.tiles_m, d_tiles = (a.d + kTN - 1) / kTN;
-  for (long long i = 0; i < l.pieces; ++i) {
-    const long long v0 = i * l.piece, cols = a.vocab - v0 < l.piece ? a.vocab - v0 : l.piece;
-    p.col0 = v0; p.cols = static_cast<int>(cols);
-    p.tiles_n = static_cast<int>((cols + kTN - 1) / kTN);
-    p.run = run_length(p.tiles_m, p.tiles_n);
-    p.items = static_cast<long long>(p.tiles_m) * ((p.tiles_n + p.run - 1) / p.run);
-    rc = map_of(&mw, static_cast<const char*>(a.W) + v0 * a.w_ld * es, cols, a.d, a.w_ld, es, kTN / 2);
-    if (!rc) rc = a.k > 0 ? launch_logits<true, true>(es == 1, bf, mh, mw, p, st) : launch_logits<true, false>(es == 1, bf, mh, mw, p, st);
-    if (!rc) rc = map_of(&d_mn, D, a.n, cols, l.ldd, 2, kK16);
-    if (!rc) rc = map_of(&d_k, D, a.n, cols, l.ldd, 2, kTM);
-    if (!rc) rc = map_of(&w_mn, w16 + v0 * w16_ld * 2, cols, a.d, w16_ld, 2, kK16);
+  // launch i: the products of piece i - 1 and the logits of piece i
+  for (long long i = 0; i <= l.pieces; ++i) {
+    long long items[kClasses] = {};
+    double cost[kClasses] = {};
+    if (i < l.pieces) {
+      const long long v0 = i * l.piece, cols = a.vocab - v0 < l.piece ? a.vocab - v0 : l.piece;
+      p.col0 = v0; p.cols = static_cast<int>(cols);
+      p.tiles_n = static_cast<int>((cols + kTN - 1) / kTN);
+      // distillation looks up a row's place in its entries once per item: longer ones where there are enough
+      p.run = a.k > 0 ? run_length(row_tiles, p.tiles_n, 4, 8) : 1;
+      p.D = reinterpret_cast<uint16_t*>(ws + l.D[i & 1]);
+      items[kClassD] = static_cast<long long>(row_tiles) * ((p.tiles_n + p.run - 1) / p.run);
+      cost[kClassD] = p.run * (p.num_kb + kTileCost);
+      rc = map_of(&m.w, static_cast<const char*>(a.W) + v0 * a.w_ld * es, cols, a.d, a.w_ld, es, kTN / 2);
+    }
+    if (!rc && i > 0) {
+      const long long v0 = (i - 1) * l.piece, cols = a.vocab - v0 < l.piece ? a.vocab - v0 : l.piece;
+      const uint16_t* D = reinterpret_cast<const uint16_t*>(ws + l.D[(i - 1) & 1]);
+      dw.M = static_cast<int>(cols);
+      dw.out = a.dW ? static_cast<char*>(a.dW) + v0 * a.dw_ld * 2 : nullptr;
+      dh.num_kb = static_cast<int>((cols + kK16 - 1) / kK16);
+      dh.part_kb = (dh.num_kb + l.parts - 1) / l.parts;
+      dh.parts = (dh.num_kb + dh.part_kb - 1) / dh.part_kb;
+      dh.mode = l.pieces > 1 ? (i == 1 ? kAccFirst : i < l.pieces ? kAccNext : kAccLast) : dh.parts > 1 ? kAccFirst : kFinal;
+      if (a.dW) items[kClassDw] = (cols + 2 * kTM - 1) / (2 * kTM) * d_tiles;
+      if (a.dH) items[kClassDh] = static_cast<long long>(row_tiles) * d_tiles * dh.parts;
+      cost[kClassDw] = dw.num_kb + kTileCost;
+      cost[kClassDh] = dh.part_kb + kTileCost;
+      rc = map_of(&m.d_mn, D, a.n, cols, l.ldd, 2, kK16);
+      if (!rc) rc = map_of(&m.d_k, D, a.n, cols, l.ldd, 2, kTM);
+      if (!rc) rc = map_of(&m.w_mn, w16 + v0 * w16_ld * 2, cols, a.d, w16_ld, 2, kK16);
+    }
+    if (!rc) rc = launch_grad(es == 1, a.k > 0, bf, m, g, items, cost, st);
     if (rc) return rc;
-    GradParams g = {};
-    g.dw.M = static_cast<int>(cols); g.dw.N = a.d; g.dw.num_kb = static_cast<int>((a.n + kK16 - 1) / kK16);
-    g.dw.tiles_m = static_cast<int>((cols + 2 * kTM - 1) / (2 * kTM)); g.dw.tiles_n = static_cast<int>(d_tiles);
-    g.dw.out = a.dW ? static_cast<char*>(a.dW) + v0 * a.dw_ld * 2 : nullptr; g.dw.ldo = a.dw_ld; g.dw.out_dt = a.dw_dt;
-    g.dw.alpha = 1.0f / c.kf_n; g.dw.mode = kFinal;
-    g.dh.M = static_cast<int>(a.n); g.dh.N = a.d; g.dh.num_kb = static_cast<int>((cols + kK16 - 1) / kK16);
-    g.dh.tiles_m = static_cast<int>(row_tiles); g.dh.tiles_n = static_cast<int>(d_tiles);
-    g.dh.out = a.dH; g.dh.ldo = a.dh_ld; g.dh.out_dt = a.dh_dt;
-    g.dh.alpha = 1.0f / c.kf_vocab;
-    g.dh.mode = l.pieces == 1 ? kFinal : i == 0 ? kAccFirst : i + 1 < l.pieces ? kAccNext : kAccLast;
-    g.dh.acc = reinterpret_cast<float*>(ws + l.acc); g.dh.ld_acc = l.ld_acc;
-    g.dw_tiles = a.dW ? g.dw.tiles_m * g.dw.tiles_n : 0;
-    g.dh_tiles = a.dH ? g.dh.tiles_m * g.dh.tiles_n : 0;
-    g.dw_first = g.dw.num_kb >= g.dh.num_kb;
-    g.idesc = idesc_of(d_dt, d_dt);
-    g.unit = c.inv_unit;
-    g.status = p.status;
-    static DeviceOnce once;
-    cudaLaunchConfig_t cfg;
-    cudaLaunchAttribute attrs[2];
-    rc = pair_config(loss_products_kernel, once, static_cast<long long>(g.dw_tiles) + g.dh_tiles, st, &cfg, attrs);
-    if (rc) return rc;
-    SCALIFY_CUDA_TRY(cudaLaunchKernelEx(&cfg, loss_products_kernel, d_mn, h_mn, d_k, w_mn, g));
   }
-  return SCALIFY_OK;
+  if (!a.dH || l.pieces > 1 || dh.parts == 1) return SCALIFY_OK;
+  PlanesParams q = {};
+  q.acc = dh.acc; q.ld_acc = dh.ld_acc; q.planes = dh.parts;
+  q.M = dh.M; q.N = dh.N; q.out = dh.out; q.ldo = dh.ldo; q.out_dt = dh.out_dt;
+  q.alpha = dh.alpha; q.unit = g.unit;
+  const long long blocks = (a.n * ((a.d + kVec - 1) / kVec) + 255) / 256, most = 8ll * sm_count();
+  return launch_small(planes_kernel, blocks < most ? blocks : most, 256, q, st);
 }
 
 }  // namespace scalify
