@@ -33,25 +33,35 @@ namespace scalify {
 
 namespace {
 
-constexpr int kTM = 128;            // rows of the output tile per CTA; a pair takes 256
+constexpr int kTM = 128;            // rows of the output tile per CTA
 constexpr int kTN = 256;            // columns of the output tile
 constexpr int kRowBytes = 128;      // a K block: one 128-byte swizzle row
 constexpr int kK16 = 64;            // ... in 16-bit elements
 constexpr int kAccs = 2;            // accumulators of 256 TMEM columns: the epilogue overlaps the next tile's products
 constexpr int kEpiWarps = 8;
 constexpr int kThreads = 64 + 32 * kEpiWarps;
-constexpr int kABytes = kTM * kRowBytes, kBBytes = kTN / 2 * kRowBytes;
-constexpr int kStages = 6;
-constexpr uint32_t kRing = kStages * (kABytes + kBBytes);
-constexpr size_t kSmem = size_t(kRing) + 1024 + 256;
-constexpr int kHalf = kTN / 2;      // columns of a tile that one epilogue warp takes
-constexpr int kChunks = kHalf / 32;
+// Two CTAs (an SM pair) share a tile of 256 rows, each with its own rows of A and half of B; batches of at most 128 rows leave
+// the second CTA's rows empty, so one CTA alone takes a tile of 128 rows and all of B there: twice the weights per MMA.
+template <int NCTA> struct Cfg {
+  static constexpr int kTileM = kTM * NCTA;
+  static constexpr int kBRows = kTN / NCTA;
+  static constexpr int kABytes = kTM * kRowBytes, kBBytes = kBRows * kRowBytes;
+  static constexpr int kStages = NCTA == 1 ? 4 : 6;
+  static constexpr uint32_t kRing = kStages * (kABytes + kBBytes);
+  static constexpr size_t kSmem = size_t(kRing) + 1024 + 256;
+};
 constexpr float kLog2E = 1.4426950408889634f;
 
-template <bool F8>
-__device__ __forceinline__ void umma_pair(uint32_t d_tmem, uint64_t ad, uint64_t bd, uint32_t idesc, uint32_t acc) {
-  if constexpr (F8) {
+template <bool F8, int NCTA>
+__device__ __forceinline__ void umma(uint32_t d_tmem, uint64_t ad, uint64_t bd, uint32_t idesc, uint32_t acc) {
+  if constexpr (F8 && NCTA == 2) {
     umma_f8_pair(d_tmem, ad, bd, idesc, acc);
+  } else if constexpr (F8) {
+    umma_f8(d_tmem, ad, bd, idesc, acc);
+  } else if constexpr (NCTA == 1) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem), "l"(ad), "l"(bd), "r"(idesc), "r"(acc) : "memory");
   } else {
     asm volatile(
         "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
@@ -66,7 +76,9 @@ __device__ __forceinline__ float exp2_approx(float x) {
 
 // Shared memory, barriers and each role's place in the ring.  Warp 0: TMA producer; warp 1: MMA issuer (of the pair's first
 // CTA); warps 2-9: epilogue.  Every wait is bounded.
-struct Engine {
+template <int NCTA> struct Engine {
+  using C = Cfg<NCTA>;
+  static constexpr int kABytes = C::kABytes, kBBytes = C::kBBytes, kStages = C::kStages;
   uint32_t smem_a, smem_b, full_bar, empty_bar, acc_full, acc_empty, drain_bar, tmem_base;
   volatile uint32_t* tmem_slot;
   volatile uint32_t* abort_flag;
@@ -77,10 +89,10 @@ struct Engine {
 
   __device__ __forceinline__ void set_up(uint8_t* smem_raw) {
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-    uint8_t* bar_mem = smem_raw + (base - raw) + kRing;
+    uint8_t* bar_mem = smem_raw + (base - raw) + C::kRing;
     smem_a = base;
     smem_b = base + kStages * kABytes;
-    const uint32_t bars = base + kRing;
+    const uint32_t bars = base + C::kRing;
     full_bar = bars;
     empty_bar = bars + 8 * kStages;
     acc_full = bars + 16 * kStages;
@@ -90,10 +102,10 @@ struct Engine {
     abort_flag = tmem_slot + 1;
     warp = threadIdx.x >> 5;
     lane = threadIdx.x & 31;
-    rank = cluster_ctarank();
+    rank = NCTA == 2 ? cluster_ctarank() : 0u;
     if (threadIdx.x == 0) {
       for (int s = 0; s < kStages; ++s) { mbar_init(full_bar + 8 * s, 1); mbar_init(empty_bar + 8 * s, 1); }
-      for (int s = 0; s < kAccs; ++s) { mbar_init(acc_full + 8 * s, 1); mbar_init(acc_empty + 8 * s, kEpiWarps * 2); }
+      for (int s = 0; s < kAccs; ++s) { mbar_init(acc_full + 8 * s, 1); mbar_init(acc_empty + 8 * s, kEpiWarps * NCTA); }
       mbar_init(drain_bar, 1);
       *abort_flag = 0u;
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -101,14 +113,14 @@ struct Engine {
     if (warp == 1) tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), kAccs * kTN);
     tc_fence_before();
     __syncthreads();
-    cluster_sync_all();
+    if constexpr (NCTA == 2) cluster_sync_all();
     tc_fence_after();
     tmem_base = *tmem_slot;
   }
   __device__ __forceinline__ void tear_down() {
     tc_fence_before();
     __syncthreads();
-    cluster_sync_all();
+    if constexpr (NCTA == 2) cluster_sync_all();
     if (warp == 1) {
       tc_fence_after();
       tmem_dealloc(tmem_base, kAccs * kTN);
@@ -116,16 +128,20 @@ struct Engine {
   }
 
   // ---- warp 0, lane 0: the operand blocks of one tile.  Along K: a box of 128 bytes x 128 rows.  MN-major (16-bit only):
-  // two boxes of 64 columns x the 64 lines of this K block.
-  __device__ __forceinline__ bool produce(const CUtensorMap* ma, const CUtensorMap* mb, int m0, int n0, int kb0, int num_kb, bool a_mn, bool b_mn) {
+  // boxes of 64 columns x the 64 lines of this K block.
+  __device__ __forceinline__ bool produce(const CUtensorMap* ma, const CUtensorMap* mb, int m0, int n0, int width, int kb0, int num_kb, bool a_mn, bool b_mn) {
     m0 += static_cast<int>(rank) * kTM;
-    n0 += static_cast<int>(rank) * (kTN / 2);
+    n0 += static_cast<int>(rank) * (width / 2);
     for (int kb = kb0; kb < kb0 + num_kb; ++kb) {
       if (!mbar_wait(empty_bar + 8 * stage, phase ^ 1u, abort_flag)) return false;
       const uint32_t sa = smem_a + stage * kABytes, sb = smem_b + stage * kBBytes;
-      if (rank == 0u) mbar_expect_tx(full_bar + 8 * stage, 2 * (kABytes + kBBytes));
-      const uint32_t fb = map_to_cta(full_bar + 8 * stage, 0u);  // both CTAs' copies are counted on the first one's barrier
-      auto load = [&](uint32_t dst, const CUtensorMap* m, int x_bytes, int y) { tma_load_3d_pair(dst, m, fb, x_bytes, y, 0); };
+      uint32_t fb = full_bar + 8 * stage;
+      if (rank == 0u) mbar_expect_tx(fb, NCTA * kABytes + width * kRowBytes);
+      if constexpr (NCTA == 2) fb = map_to_cta(fb, 0u);  // both CTAs' copies are counted on the first one's barrier
+      auto load = [&](uint32_t dst, const CUtensorMap* m, int x_bytes, int y) {
+        if constexpr (NCTA == 2) tma_load_3d_pair(dst, m, fb, x_bytes, y, 0);
+        else tma_load_3d(dst, m, fb, x_bytes, y, 0);
+      };
       if (!a_mn) {
         load(sa, ma, kb * kRowBytes, m0);
       } else {
@@ -136,7 +152,7 @@ struct Engine {
         load(sb, mb, kb * kRowBytes, n0);
       } else {
 #pragma unroll
-        for (int j = 0; j < kTN / 2 / kK16; ++j) load(sb + j * kK16 * kRowBytes, mb, (n0 + j * kK16) * 2, kb * kK16);
+        for (int j = 0; j < C::kBRows / kK16; ++j) load(sb + j * kK16 * kRowBytes, mb, (n0 + j * kK16) * 2, kb * kK16);
       }
       ++issued;
       if (++stage == kStages) { stage = 0; phase ^= 1u; }
@@ -155,9 +171,13 @@ struct Engine {
     }
   }
 
+  __device__ __forceinline__ static void commit(uint32_t bar) {
+    if constexpr (NCTA == 2) umma_commit_pair(bar);
+    else umma_commit(bar);
+  }
   // ---- warp 1, lane 0 of the pair's first CTA: the MMAs of one tile
   template <bool F8>
-  __device__ __forceinline__ bool multiply(int num_kb, uint32_t idesc, bool a_mn, bool b_mn) {
+  __device__ __forceinline__ bool multiply(int num_kb, uint32_t idesc, bool a_mn, bool b_mn) {  // (idesc has the width)
     const uint64_t a_desc = make_smem_desc(smem_a, a_mn ? kK16 * kRowBytes : 0u, 1024u);
     const uint64_t b_desc = make_smem_desc(smem_b, b_mn ? kK16 * kRowBytes : 0u, 1024u);
     const uint32_t a_inc = (a_mn ? 16 * kRowBytes : 32) >> 4, b_inc = (b_mn ? 16 * kRowBytes : 32) >> 4;  // per MMA: 32 bytes of K
@@ -171,17 +191,17 @@ struct Engine {
       if (!mbar_wait(full_bar + 8 * stage, phase, abort_flag)) return false;
       tc_fence_after();
 #pragma unroll
-      for (int k = 0; k < 4; ++k) umma_pair<F8>(d_tmem, ad0 + k * a_inc, bd0 + k * b_inc, idesc, (kb | k) != 0 ? 1u : 0u);
-      umma_commit_pair(empty_bar + 8 * stage);  // the slot is free (in both CTAs) once these MMAs have read it
+      for (int k = 0; k < 4; ++k) umma<F8, NCTA>(d_tmem, ad0 + k * a_inc, bd0 + k * b_inc, idesc, (kb | k) != 0 ? 1u : 0u);
+      commit(empty_bar + 8 * stage);  // the slot is free (in both CTAs) once these MMAs have read it
       if (++stage == kStages) { stage = 0; phase ^= 1u; }
     }
-    umma_commit_pair(acc_full + 8 * acc);
+    commit(acc_full + 8 * acc);
     if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
     return true;
   }
   // after a timeout: all MMAs issued so far must retire before the tensor memory is freed
   __device__ __forceinline__ void drain_multiplies() {
-    umma_commit_pair(drain_bar);
+    commit(drain_bar);
     const unsigned long long t0 = global_timer_ns();
     while (!mbar_try_wait(drain_bar, 0u) && global_timer_ns() - t0 < kWaitLimitNs) {}
   }
@@ -194,9 +214,9 @@ struct Engine {
   }
   // f(32 columns of this lane's row, chunk) for the chunks of this warp's half that lie inside the matrix (`cols` of them
   // from the half's first one); the next chunk is read while f works on the current one
-  template <class F> __device__ __forceinline__ void each_chunk(int half, int cols, F f) {
-    const uint32_t t_addr = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16) + acc * kTN + half * kHalf;
-    const int n_chunks = max(0, min(kChunks, (cols + 31) / 32));
+  template <class F> __device__ __forceinline__ void each_chunk(int half, int half_cols, int cols, F f) {
+    const uint32_t t_addr = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16) + acc * kTN + half * half_cols;
+    const int n_chunks = max(0, min(half_cols, cols) + 31) / 32;
     uint32_t ra[32], rb[32];
     if (n_chunks > 0) tmem_ld32(t_addr, ra);
 #pragma unroll 1
@@ -216,21 +236,26 @@ struct Engine {
   __device__ __forceinline__ void release_accumulator() {
     tc_fence_before();
     __syncwarp();
-    if (lane == 0) mbar_arrive_cluster(map_to_cta(acc_empty + 8 * acc, 0u));
+    if (lane == 0) {
+      if constexpr (NCTA == 2) mbar_arrive_cluster(map_to_cta(acc_empty + 8 * acc, 0u));
+      else mbar_arrive(acc_empty + 8 * acc);
+    }
     if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
   }
 };
 
 // ------------------------------------------------------------------------------------------------- logits kernel
-struct Entry { int id; float q; };  // a row's target entries, those of even 128-column blocks first, each part sorted by id
+struct Entry { int id; float q; };  // a row's target entries, those of the tiles' first halves first, each part sorted by id
 
 struct LogitsParams {
   int n, cols;               // rows; columns (of this piece of the vocabulary)
   long long col0;            // the piece's first column
   int num_kb;
+  int half_cols;             // of a tile: what one epilogue warp takes (32 to 128)
   int tiles_m, tiles_n, run; // a work item: one row tile, `run` consecutive column tiles
   long long items;
   uint32_t idesc;
+  bool early;                // the kernel before writes nothing that the products read: they need not wait for it
   const float* h_scale; const float* w_scale;
   float inv_temp;
   // targets
@@ -271,7 +296,7 @@ template <bool KD> struct Targets {
     if (row >= p.n) return;
     if constexpr (!KD) {
       const long long t = __ldg(p.ids + row);
-      if (t != p.padding_id && t >= first && t < p.vocab && ((t >> 7) & 1) == half) { id = static_cast<int>(t); q = 1.0f; }
+      if (t != p.padding_id && t >= first && t < p.vocab && (static_cast<uint32_t>(t) / p.half_cols & 1u) == static_cast<uint32_t>(half)) { id = static_cast<int>(t); q = 1.0f; }
     } else {
       const int2 c = __ldg(p.counts + row);
       const Entry* e = p.entries + static_cast<long long>(row) * p.k;
@@ -309,26 +334,27 @@ __device__ __forceinline__ float pick32(const uint32_t* r, int i) {
   return __uint_as_float(a[0]);
 }
 
-template <bool F8, bool KD>
+template <int NCTA, bool F8, bool KD>
 __global__ void __launch_bounds__(kThreads, 1) logits_kernel(const __grid_constant__ CUtensorMap map_h,
                                                              const __grid_constant__ CUtensorMap map_w, const LogitsParams p) {
   asm volatile("griddepcontrol.launch_dependents;");  // the next kernel may set up while this one runs
   extern __shared__ uint8_t smem_raw[];
-  Engine e;
+  Engine<NCTA> e;
   if (threadIdx.x == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_h)) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_w)) : "memory");
   }
   e.set_up(smem_raw);
-  asm volatile("griddepcontrol.wait;" ::: "memory");  // nothing above touches what the kernel before writes
-  const int unit = blockIdx.x >> 1, num_units = gridDim.x >> 1;
+  // nothing above touches what the kernel before writes
+  if (!p.early || e.warp >= 2) asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int unit = blockIdx.x / NCTA, num_units = gridDim.x / NCTA;
   bool timed_out = false;
   if (e.warp == 0) {
     if (e.lane == 0) {
       for (long long item = unit; item < p.items && !timed_out; item += num_units) {
         const int mt = static_cast<int>(item % p.tiles_m), nt0 = static_cast<int>(item / p.tiles_m) * p.run;
         for (int nt = nt0; nt < min(nt0 + p.run, p.tiles_n) && !timed_out; ++nt)
-          timed_out = !e.produce(&map_h, &map_w, mt * 2 * kTM, nt * kTN, 0, p.num_kb, false, false);
+          timed_out = !e.produce(&map_h, &map_w, mt * Cfg<NCTA>::kTileM, nt * 2 * p.half_cols, 2 * p.half_cols, 0, p.num_kb, false, false);
       }
       if (timed_out || *e.abort_flag) e.drain_copies();
     }
@@ -346,14 +372,14 @@ __global__ void __launch_bounds__(kThreads, 1) logits_kernel(const __grid_consta
     Targets<KD> target;
     for (long long item = unit; item < p.items && !timed_out; item += num_units) {
       const int mt = static_cast<int>(item % p.tiles_m), ng = static_cast<int>(item / p.tiles_m), nt0 = ng * p.run;
-      const int row = mt * 2 * kTM + static_cast<int>(e.rank) * kTM + quarter * 32 + e.lane;
+      const int row = mt * Cfg<NCTA>::kTileM + static_cast<int>(e.rank) * kTM + quarter * 32 + e.lane;
       const bool warp_rows = row - e.lane < p.n;  // whether any of this warp's rows exists
-      target.start(p, row, half, static_cast<long long>(nt0) * kTN);
+      target.start(p, row, half, static_cast<long long>(nt0) * 2 * p.half_cols);
       float top = -INFINITY, sum = 0.f, dot = 0.f;
       for (int nt = nt0; nt < min(nt0 + p.run, p.tiles_n); ++nt) {
         if (!e.wait_accumulator()) { timed_out = true; break; }
-        const int n0 = nt * kTN + half * kHalf;
-        e.each_chunk(half, warp_rows ? p.cols - n0 : 0, [&](uint32_t* r, int c) {
+        const int n0 = (2 * nt + half) * p.half_cols;
+        e.each_chunk(half, p.half_cols, warp_rows ? p.cols - n0 : 0, [&](uint32_t* r, int c) {
           const int c0 = n0 + c * 32, valid = p.cols - c0;
           while (__any_sync(0xFFFFFFFFu, target.id < c0 + 32ll)) {
             const float z = pick32(r, (target.id - c0) & 31);
@@ -398,7 +424,7 @@ __global__ void __launch_bounds__(kThreads, 1) logits_kernel(const __grid_consta
 // What the CTA pairs of one launch share: tiles of the products dW = D^T H and dH = D W of one piece of the vocabulary, and of
 // the logits (the gradient D) of the NEXT piece, which fill the pairs up to equal loads whatever the products' tiles leave.
 enum { kClassDw = 0, kClassDh = 1, kClassD = 2, kClasses = 3 };
-constexpr int kMaxUnits = 80;
+constexpr int kMaxUnits = 160;
 constexpr int kListed = 128;
 struct Schedule {
   int order[kClasses];               // long tiles first
@@ -439,19 +465,20 @@ struct GradParams {
 };
 struct GradMaps { CUtensorMap h, w, d_mn, h_mn, d_k, w_mn; };
 
-template <bool F8, bool KD, bool BF>
+template <int NCTA, bool F8, bool KD, bool BF>
 __global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradParams p) {
   asm volatile("griddepcontrol.launch_dependents;");  // the next kernel may set up while this one runs
   extern __shared__ uint8_t smem_raw[];
-  Engine e;
-  const int unit = blockIdx.x >> 1, units = gridDim.x >> 1;
+  Engine<NCTA> e;
+  const int unit = blockIdx.x / NCTA, units = gridDim.x / NCTA;
   if (threadIdx.x < 6 && p.schedule.total[threadIdx.x < 2 ? kClassD : threadIdx.x < 4 ? kClassDw : kClassDh] > 0)  // (the others are not filled in)
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&maps.h + threadIdx.x)) : "memory");
   __shared__ int s_item[kClasses][kListed];  // this pair's first items
   for (int i = threadIdx.x; i < kClasses * kListed; i += kThreads)
     if (i % kListed < p.schedule.quota[i / kListed][unit]) s_item[i / kListed][i % kListed] = scheduled_item(p.schedule, i / kListed, unit, units, i % kListed);
   e.set_up(smem_raw);
-  asm volatile("griddepcontrol.wait;" ::: "memory");  // nothing above touches what the kernel before writes
+  // nothing above touches what the kernel before writes
+  if (!p.logits.early || e.warp >= 2) asm volatile("griddepcontrol.wait;" ::: "memory");
   const LogitsParams& l = p.logits;
   bool timed_out = false;
   // every role walks the same items: f(class, item)
@@ -476,13 +503,13 @@ __global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_con
         if (cls == kClassD) {
           const int mt = item % l.tiles_m, nt0 = item / l.tiles_m * l.run;
           for (int nt = nt0; nt < min(nt0 + l.run, l.tiles_n) && !timed_out; ++nt)
-            timed_out = !e.produce(&maps.h, &maps.w, mt * 2 * kTM, nt * kTN, 0, l.num_kb, false, false);
+            timed_out = !e.produce(&maps.h, &maps.w, mt * Cfg<NCTA>::kTileM, nt * 2 * l.half_cols, 2 * l.half_cols, 0, l.num_kb, false, false);
         } else {
           const GradProduct& g = p.product[cls];
           int part, mt, nt;
           const int kbs = locate(g, item, part, mt, nt);
-          timed_out = cls == kClassDw ? !e.produce(&maps.d_mn, &maps.h_mn, mt * 2 * kTM, nt * kTN, part * g.part_kb, kbs, true, true)
-                                      : !e.produce(&maps.d_k, &maps.w_mn, mt * 2 * kTM, nt * kTN, part * g.part_kb, kbs, false, true);
+          timed_out = cls == kClassDw ? !e.produce(&maps.d_mn, &maps.h_mn, mt * Cfg<NCTA>::kTileM, nt * kTN, kTN, part * g.part_kb, kbs, true, true)
+                                      : !e.produce(&maps.d_k, &maps.w_mn, mt * Cfg<NCTA>::kTileM, nt * kTN, kTN, part * g.part_kb, kbs, false, true);
         }
       });
       if (timed_out || *e.abort_flag) e.drain_copies();
@@ -508,9 +535,9 @@ __global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_con
     const float unit_d = reinterpret_cast<const volatile float*>(p.unit)[0], factor = reinterpret_cast<const volatile float*>(p.unit)[1];
     each_item([&](int cls, int item) {
       if (cls == kClassD) {
-        const int row = item % l.tiles_m * 2 * kTM + lane_row, nt0 = item / l.tiles_m * l.run;
+        const int row = item % l.tiles_m * Cfg<NCTA>::kTileM + lane_row, nt0 = item / l.tiles_m * l.run;
         Targets<KD> target;
-        target.start(l, row, half, l.col0 + static_cast<long long>(nt0) * kTN);
+        target.start(l, row, half, l.col0 + static_cast<long long>(nt0) * 2 * l.half_cols);
         float2 coef = make_float2(0.f, 0.f);
         float lse2 = 0.f;
         if (row < l.n) {
@@ -520,8 +547,8 @@ __global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_con
         }
         for (int nt = nt0; nt < min(nt0 + l.run, l.tiles_n); ++nt) {
           if (!e.wait_accumulator()) { timed_out = true; break; }
-          const int n0 = nt * kTN + half * kHalf;
-          e.each_chunk(half, row - e.lane < l.n ? l.cols - n0 : 0, [&](uint32_t* r, int c) {
+          const int n0 = (2 * nt + half) * l.half_cols;
+          e.each_chunk(half, l.half_cols, row - e.lane < l.n ? l.cols - n0 : 0, [&](uint32_t* r, int c) {
             const int c0 = n0 + c * 32;
             const long long g0 = l.col0 + c0;
             float v[32];
@@ -552,12 +579,12 @@ __global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_con
         int part, mt, nt;
         locate(g, item, part, mt, nt);
         const float alpha = g.alpha * factor;
-        const int row = mt * 2 * kTM + lane_row, n0 = nt * kTN + half * kHalf;
+        const int row = mt * Cfg<NCTA>::kTileM + lane_row, n0 = nt * kTN + half * (kTN / 2);
         const int mode = g.mode;
         float* acc_row = g.acc + (static_cast<long long>(part) * g.M + row) * g.ld_acc + n0;  // (padded to whole chunks)
         char* out_row = static_cast<char*>(g.out) + (static_cast<long long>(row) * g.ldo + n0) * 2;
         if (!e.wait_accumulator()) { timed_out = true; return; }
-        e.each_chunk(half, row - e.lane < g.M ? g.N - n0 : 0, [&](uint32_t* r, int c) {
+        e.each_chunk(half, kTN / 2, row - e.lane < g.M ? g.N - n0 : 0, [&](uint32_t* r, int c) {
           float v[32];
 #pragma unroll
           for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
@@ -601,7 +628,7 @@ __global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_con
 }
 
 // ------------------------------------------------------------------------------------------------- small kernels
-// A teacher's entries: probabilities, sorted by (128-column block's parity, id), entries without a place in the vocabulary
+// A teacher's entries: probabilities, sorted by (half of its tile, id), entries without a place in the vocabulary
 // or with no probability mass at all (a logit of -inf) left out.  One warp per row; the order by counting the smaller ones.
 struct TeacherParams {
   long long n, vocab;
@@ -609,17 +636,18 @@ struct TeacherParams {
   const long long* ids; long long padding_id;
   const void* T; int t_dt; long long t_ld; const float* t_scale; const float* t_lse;
   float inv_temp;
+  int half_cols;
   Entry* entries; int2* counts; float2* sums;  // sums: Q, sum q log q
   uint32_t* status;
 };
 constexpr int kTeacherWarps = 4;
 __global__ void __launch_bounds__(32 * kTeacherWarps) teacher_kernel(const TeacherParams p) {
-  asm volatile("griddepcontrol.launch_dependents;");
   __shared__ uint32_t s_key[kTeacherWarps][kLossMaxEntries];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const long long row = static_cast<long long>(blockIdx.x) * kTeacherWarps + warp;
-  if (row >= p.n) return;
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;");  // (behind the wait: a dependent may read what was there before this kernel)
+  if (row >= p.n) return;
   constexpr int kPer = kLossMaxEntries / 32;
   const float scale = load_scale_after_wait(p.t_scale);
   if (row == 0 && lane == 0 && !is_pow2_scale(scale)) atomicOr(p.status, static_cast<uint32_t>(SCALIFY_DEV_BAD_SCALE));
@@ -645,7 +673,7 @@ __global__ void __launch_bounds__(32 * kTeacherWarps) teacher_kernel(const Teach
           x *= f;
           if (x != -INFINITY) {
             t[j] = x;
-            key[j] = static_cast<uint32_t>(id) | (static_cast<uint32_t>((id >> 7) & 1) << 30);
+            key[j] = static_cast<uint32_t>(id) | (static_cast<uint32_t>(id) / p.half_cols & 1u) << 30;
             top = x > top || x != x ? x : top;
           }
         }
@@ -896,11 +924,11 @@ __device__ __forceinline__ void widen_rows(const WidenParams& p, int block, int 
 // Row coefficients of p and of q in units of the upstream gradient (of the mean's, if there is none); the power of two that D
 // is stored times; output scales; FP16 copies of FP8 operands.
 __global__ void __launch_bounds__(kCoefThreads) coef_kernel(const __grid_constant__ CoefParams p) {
-  asm volatile("griddepcontrol.launch_dependents;");
   __shared__ uint32_t s_top[kCoefThreads / 32];
   __shared__ int s_count[kCoefThreads / 32];
   __shared__ bool s_last;
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;");  // (behind the wait: a dependent may read what was there before this kernel)
   if (static_cast<int>(blockIdx.x) >= p.blocks) return widen_rows(p.widen, blockIdx.x - p.blocks, gridDim.x - p.blocks);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   bool bad = false;
@@ -998,14 +1026,29 @@ __global__ void __launch_bounds__(256) zero_rows_kernel(uint16_t* out, long long
 }
 
 // ------------------------------------------------------------------------------------------------- host side
-constexpr int kUnits = 74;            // CTA pairs of the GPU: sizes are planned for these, whatever the launch finds
+// CTAs per tile, and the pairs (or CTAs) of the GPU, which sizes are planned for, whatever the launch finds.
+int ctas_of(long long n) { return n <= kTM ? 1 : 2; }
+int units_of(long long n) { return 148 / ctas_of(n); }
+long long row_tiles(long long rows, int ctas) { return (rows + kTM * ctas - 1) / (kTM * ctas); }
 long long pad_to(long long x, long long m) { return (x + m - 1) / m * m; }
 size_t pad256(size_t x) { return (x + 255) / 256 * 256; }
 
+// Columns of a logits tile.  A batch of one row tile has the vocabulary's tiles alone to share, each CTA with few of them:
+// their width is chosen for equal shares (37 rows, vocabulary 50257, 148 CTAs: two rounds of 256 columns or of 192).
+int tile_columns(long long n, long long vocab) {
+  if (ctas_of(n) == 2) return kTN;
+  int best = kTN;
+  long long least = 0;
+  for (int w = kTN; w >= 64; w -= 64) {
+    const long long tiles = (vocab + w - 1) / w, cost = (tiles + units_of(n) - 1) / units_of(n) * (w + 16);
+    if (w == kTN || cost < least) { best = w; least = cost; }
+  }
+  return best;
+}
 // Consecutive column tiles per work item: long runs write few partial results, short ones share the work evenly.
-int run_length(long long tiles_m, long long tiles_n, int longest, int per_unit) {
+int run_length(long long tiles_m, long long tiles_n, int longest, int items) {
   for (int run = longest; run > 1; run >>= 1)
-    if (tiles_m * ((tiles_n + run - 1) / run) >= per_unit * kUnits) return run;
+    if (tiles_m * ((tiles_n + run - 1) / run) >= items) return run;
   return 1;
 }
 // Columns of a piece of the vocabulary: D of at most 2^27 bytes, two pieces of which are in memory; whole tiles.
@@ -1024,9 +1067,10 @@ constexpr int kTileCost = 3;
 // Parts of dH's contraction where the whole vocabulary is one piece: few tiles of a long contraction would keep few CTA pairs
 // busy; a part is at most half of a pair's load.
 int dh_parts(long long n, long long vocab, long long d) {
-  const double tm = static_cast<double>((n + 2 * kTM - 1) / (2 * kTM)), tn = static_cast<double>((d + kTN - 1) / kTN), tv = static_cast<double>((vocab + kTN - 1) / kTN);
+  const int ctas = ctas_of(n);
+  const double tm = static_cast<double>(row_tiles(n, ctas)), tn = static_cast<double>((d + kTN - 1) / kTN), tv = static_cast<double>(row_tiles(vocab, ctas));
   const double kb_v = static_cast<double>((vocab + kK16 - 1) / kK16), kb_n = static_cast<double>((n + kK16 - 1) / kK16);
-  const double load = (tm * tn * (kb_v + kTileCost) + tv * tn * (kb_n + kTileCost)) / kUnits;
+  const double load = (tm * tn * (kb_v + kTileCost) + tv * tn * (kb_n + kTileCost)) / units_of(n);
   long long parts = static_cast<long long>(ceil(2.0 * kb_v / load)), most = static_cast<long long>(kb_v / 16);
   if (parts > 32) parts = 32;
   if (parts > most) parts = most;
@@ -1036,26 +1080,27 @@ int dh_parts(long long n, long long vocab, long long d) {
 struct Layout {
   size_t partial, dot, sums_blocks, entries, counts, sums, coef, tops, unit, h16, w16, D[2], acc, total;
   long long ld_part, ld16, ldd, ld_acc, piece, pieces;
-  int slots, run, parts;
+  int slots, run, parts, width;
 };
 Layout layout_of(long long n, long long vocab, long long d, int es, int k, bool backward) {
   Layout l = {};
   size_t at = kWsHeader;
   auto take = [&](size_t bytes) { const size_t o = at; at += pad256(bytes); return o; };
   const size_t rows = static_cast<size_t>(n);
-  const long long tm = (n + 2 * kTM - 1) / (2 * kTM), tn = (vocab + kTN - 1) / kTN;
+  l.width = tile_columns(n, vocab);
+  const long long tm = row_tiles(n, ctas_of(n)), tn = (vocab + l.width - 1) / l.width;
   if (k > 0) {
     l.entries = take(rows * k * sizeof(Entry));
     l.counts = take(rows * sizeof(int2));
     l.sums = take(rows * sizeof(float2));
   }
   if (!backward) {
-    l.run = run_length(tm, tn, 8, 16);
+    l.run = run_length(tm, tn, 8, 16 * units_of(n));
     l.slots = static_cast<int>((tn + l.run - 1) / l.run) * 2;
     l.ld_part = pad_to(n, 32);
     l.partial = take(static_cast<size_t>(l.slots) * l.ld_part * sizeof(float2));
     l.dot = take(static_cast<size_t>(l.slots) * l.ld_part * sizeof(float));
-    l.sums_blocks = take((rows / 32 + 32) * sizeof(double2));
+    l.sums_blocks = take((rows / 4 + 1) * sizeof(double2));
   } else {
     l.coef = take(rows * sizeof(float2));
     l.tops = take(kCoefBlocks * sizeof(uint2));
@@ -1068,6 +1113,7 @@ Layout layout_of(long long n, long long vocab, long long d, int es, int k, bool 
     l.piece = piece_columns(n, vocab);
     l.pieces = (vocab + l.piece - 1) / l.piece;
     l.ldd = l.piece;
+    if (l.pieces > 1) l.width = kTN;  // (pieces begin with a tile)
     l.D[0] = take(rows * l.ldd * 2);
     l.D[1] = l.pieces > 1 ? take(rows * l.ldd * 2) : l.D[0];
     l.parts = l.pieces == 1 && n > 0 ? dh_parts(n, vocab, d) : 1;
@@ -1080,16 +1126,16 @@ Layout layout_of(long long n, long long vocab, long long d, int es, int k, bool 
   return l;
 }
 
-template <class K>
-int pair_config(K kernel, DeviceOnce& once, long long items, cudaStream_t st, cudaLaunchConfig_t* cfg, cudaLaunchAttribute* attrs, int* units) {
-  int most = 0;  // CTA pairs that fit the GPU
+template <int NCTA, class K>
+int unit_config(K kernel, DeviceOnce& once, long long items, cudaStream_t st, cudaLaunchConfig_t* cfg, cudaLaunchAttribute* attrs, int* units) {
+  int most = 0;  // CTAs (pairs) that fit the GPU
   const int rc = device_once(once, &most, [&](int* v) {
-    SCALIFY_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem)));
+    SCALIFY_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(Cfg<NCTA>::kSmem)));
     cudaLaunchConfig_t q = {};
-    q.gridDim = dim3(static_cast<unsigned>(sm_count() / 2 * 2)); q.blockDim = dim3(kThreads); q.dynamicSmemBytes = kSmem;
+    q.gridDim = dim3(static_cast<unsigned>(sm_count() / NCTA * NCTA)); q.blockDim = dim3(kThreads); q.dynamicSmemBytes = Cfg<NCTA>::kSmem;
     cudaLaunchAttribute qa[1];
     qa[0].id = cudaLaunchAttributeClusterDimension;
-    qa[0].val.clusterDim.x = 2; qa[0].val.clusterDim.y = 1; qa[0].val.clusterDim.z = 1;
+    qa[0].val.clusterDim.x = NCTA; qa[0].val.clusterDim.y = 1; qa[0].val.clusterDim.z = 1;
     q.attrs = qa; q.numAttrs = 1;
     int n = 0;
     if (cudaOccupancyMaxActiveClusters(&n, kernel, &q) != cudaSuccess) { n = 0; cudaGetLastError(); }
@@ -1101,12 +1147,12 @@ int pair_config(K kernel, DeviceOnce& once, long long items, cudaStream_t st, cu
   attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attrs[0].val.programmaticStreamSerializationAllowed = 1;
   attrs[1].id = cudaLaunchAttributeClusterDimension;
-  attrs[1].val.clusterDim.x = 2; attrs[1].val.clusterDim.y = 1; attrs[1].val.clusterDim.z = 1;
+  attrs[1].val.clusterDim.x = NCTA; attrs[1].val.clusterDim.y = 1; attrs[1].val.clusterDim.z = 1;
   *cfg = {};
   *units = static_cast<int>(items < most ? items : most);
   if (*units > kMaxUnits) *units = kMaxUnits;
-  cfg->gridDim = dim3(static_cast<unsigned>(*units * 2));
-  cfg->blockDim = dim3(kThreads); cfg->dynamicSmemBytes = kSmem; cfg->stream = st;
+  cfg->gridDim = dim3(static_cast<unsigned>(*units * NCTA));
+  cfg->blockDim = dim3(kThreads); cfg->dynamicSmemBytes = Cfg<NCTA>::kSmem; cfg->stream = st;
   cfg->attrs = attrs; cfg->numAttrs = 2;
   return SCALIFY_OK;
 }
@@ -1123,17 +1169,23 @@ int launch_small(K kernel, long long blocks, int threads, const P& p, cudaStream
   return SCALIFY_OK;
 }
 
-template <bool F8, bool KD>
-int launch_logits(const CUtensorMap& mh, const CUtensorMap& mw, const LogitsParams& p, cudaStream_t st) {
-  auto kernel = logits_kernel<F8, KD>;
+template <int NCTA, bool F8, bool KD>
+int launch_logits_variant(const CUtensorMap& mh, const CUtensorMap& mw, const LogitsParams& p, cudaStream_t st) {
+  auto kernel = logits_kernel<NCTA, F8, KD>;
   static DeviceOnce once;
   cudaLaunchConfig_t cfg;
   cudaLaunchAttribute attrs[2];
   int units = 0;
-  const int rc = pair_config(kernel, once, p.items, st, &cfg, attrs, &units);
+  const int rc = unit_config<NCTA>(kernel, once, p.items, st, &cfg, attrs, &units);
   if (rc) return rc;
   SCALIFY_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, mh, mw, p));
   return SCALIFY_OK;
+}
+
+template <int NCTA>
+int launch_logits(bool f8, bool kd, const CUtensorMap& mh, const CUtensorMap& mw, const LogitsParams& p, cudaStream_t st) {
+  if (f8) return kd ? launch_logits_variant<NCTA, true, true>(mh, mw, p, st) : launch_logits_variant<NCTA, true, false>(mh, mw, p, st);
+  return kd ? launch_logits_variant<NCTA, false, true>(mh, mw, p, st) : launch_logits_variant<NCTA, false, false>(mh, mw, p, st);
 }
 
 // Every class's items over the pairs, long ones first, so that the loads become as equal as whole items allow.
@@ -1178,29 +1230,30 @@ void fill_schedule(Schedule& s, const long long (&items)[kClasses], const double
   }
 }
 
-template <bool F8, bool KD, bool BF>
-int launch_grad(const GradMaps& m, GradParams& p, const long long (&items)[kClasses], const double (&cost)[kClasses], cudaStream_t st) {
-  auto kernel = loss_grad_kernel<F8, KD, BF>;
+template <int NCTA, bool F8, bool KD, bool BF>
+int launch_grad_variant(const GradMaps& m, GradParams& p, const long long (&items)[kClasses], const double (&cost)[kClasses], cudaStream_t st) {
+  auto kernel = loss_grad_kernel<NCTA, F8, KD, BF>;
   static DeviceOnce once;
   cudaLaunchConfig_t cfg;
   cudaLaunchAttribute attrs[2];
   int units = 0;
-  const int rc = pair_config(kernel, once, items[0] + items[1] + items[2], st, &cfg, attrs, &units);
+  const int rc = unit_config<NCTA>(kernel, once, items[0] + items[1] + items[2], st, &cfg, attrs, &units);
   if (rc) return rc;
   fill_schedule(p.schedule, items, cost, units);
   SCALIFY_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, m, p));
   return SCALIFY_OK;
 }
+template <int NCTA>
 int launch_grad(bool f8, bool kd, bool bf, const GradMaps& m, GradParams& p, const long long (&items)[kClasses], const double (&cost)[kClasses], cudaStream_t st) {
-  if (f8) return kd ? launch_grad<true, true, false>(m, p, items, cost, st) : launch_grad<true, false, false>(m, p, items, cost, st);
-  if (bf) return kd ? launch_grad<false, true, true>(m, p, items, cost, st) : launch_grad<false, false, true>(m, p, items, cost, st);
-  return kd ? launch_grad<false, true, false>(m, p, items, cost, st) : launch_grad<false, false, false>(m, p, items, cost, st);
+  if (f8) return kd ? launch_grad_variant<NCTA, true, true, false>(m, p, items, cost, st) : launch_grad_variant<NCTA, true, false, false>(m, p, items, cost, st);
+  if (bf) return kd ? launch_grad_variant<NCTA, false, true, true>(m, p, items, cost, st) : launch_grad_variant<NCTA, false, false, true>(m, p, items, cost, st);
+  return kd ? launch_grad_variant<NCTA, false, true, false>(m, p, items, cost, st) : launch_grad_variant<NCTA, false, false, false>(m, p, items, cost, st);
 }
 
 // operand formats of the instruction descriptor: kind::f16 F16 0, BF16 1; kind::f8f6f4 E4M3 0, E5M2 1
 uint32_t format_of(int dt) { return dt == SCALIFY_BF16 || dt == SCALIFY_E5M2 ? 1u : 0u; }
-uint32_t idesc_of(int a_dt, int b_dt) {
-  return (1u << 4) | (format_of(a_dt) << 7) | (format_of(b_dt) << 10) | (uint32_t(kTN >> 3) << 17) | (uint32_t(2 * kTM >> 4) << 24);
+uint32_t idesc_of(int a_dt, int b_dt, int ctas, int width) {
+  return (1u << 4) | (format_of(a_dt) << 7) | (format_of(b_dt) << 10) | (uint32_t(width >> 3) << 17) | (uint32_t(ctas * kTM >> 4) << 24);
 }
 // [rows][cols] of es-byte elements, rows ld apart (one row alone may have any stride), in boxes of 128 bytes x box_rows
 int map_of(CUtensorMap* m, const void* base, long long rows, long long cols, long long ld, int es, uint32_t box_rows) {
@@ -1216,6 +1269,7 @@ int prepare_teacher(const LinearLossArgs& a, const Layout& l, char* ws, cudaStre
   t.ids = a.ids; t.padding_id = a.padding_id;
   t.T = a.T; t.t_dt = a.t_dt; t.t_ld = a.t_ld; t.t_scale = a.t_scale; t.t_lse = a.t_lse;
   t.inv_temp = a.inv_temp;
+  t.half_cols = l.width / 2;
   t.entries = reinterpret_cast<Entry*>(ws + l.entries);
   t.counts = reinterpret_cast<int2*>(ws + l.counts);
   t.sums = reinterpret_cast<float2*>(ws + l.sums);
@@ -1228,8 +1282,9 @@ LogitsParams logits_params(const LinearLossArgs& a, const Layout& l, char* ws) {
   const int es = elem_size(a.h_dt);
   p.n = static_cast<int>(a.n);
   p.num_kb = static_cast<int>((static_cast<long long>(a.d) * es + kRowBytes - 1) / kRowBytes);
-  p.tiles_m = static_cast<int>((a.n + 2 * kTM - 1) / (2 * kTM));
-  p.idesc = idesc_of(a.h_dt, a.w_dt);
+  p.tiles_m = static_cast<int>(row_tiles(a.n, ctas_of(a.n)));
+  p.idesc = idesc_of(a.h_dt, a.w_dt, ctas_of(a.n), l.width);
+  p.half_cols = l.width / 2;
   p.h_scale = a.h_scale; p.w_scale = a.w_scale; p.inv_temp = a.inv_temp;
   p.ids = a.ids; p.padding_id = a.padding_id; p.vocab = a.vocab;
   if (a.k > 0) {
@@ -1258,8 +1313,9 @@ int launch_linear_loss(const LinearLossArgs& a, void* workspace, cudaStream_t st
   int rc = prepare_teacher(a, l, ws, st);
   if (rc) return rc;
   LogitsParams p = logits_params(a, l, ws);
+  p.early = a.k > 0;  // (after the teacher kernel)
   p.cols = static_cast<int>(a.vocab);
-  p.tiles_n = static_cast<int>((a.vocab + kTN - 1) / kTN);
+  p.tiles_n = static_cast<int>((a.vocab + l.width - 1) / l.width);
   p.run = l.run;
   p.items = static_cast<long long>(p.tiles_m) * (l.slots / 2);
   p.partial = reinterpret_cast<float2*>(ws + l.partial);
@@ -1267,10 +1323,9 @@ int launch_linear_loss(const LinearLossArgs& a, void* workspace, cudaStream_t st
   p.ld_part = l.ld_part;
   CUtensorMap mh, mw;
   rc = map_of(&mh, a.H, a.n, a.d, a.h_ld, es, kTM);
-  if (!rc) rc = map_of(&mw, a.W, a.vocab, a.d, a.w_ld, es, kTN / 2);
+  if (!rc) rc = map_of(&mw, a.W, a.vocab, a.d, a.w_ld, es, l.width / ctas_of(a.n));
   if (!rc) {
-    if (es == 1) rc = a.k > 0 ? launch_logits<true, true>(mh, mw, p, st) : launch_logits<true, false>(mh, mw, p, st);
-    else rc = a.k > 0 ? launch_logits<false, true>(mh, mw, p, st) : launch_logits<false, false>(mh, mw, p, st);
+    rc = ctas_of(a.n) == 2 ? launch_logits<2>(es == 1, a.k > 0, mh, mw, p, st) : launch_logits<1>(es == 1, a.k > 0, mh, mw, p, st);
   }
   if (rc) return rc;
   JoinParams j = {};
@@ -1284,6 +1339,7 @@ int launch_linear_loss(const LinearLossArgs& a, void* workspace, cudaStream_t st
   }
   j.loss = a.loss; j.lse = a.lse; j.mean = a.mean;
   while (j.rows_log < 5 && (1ll << j.rows_log) < a.n) ++j.rows_log;
+  while (j.rows_log > 2 && l.slots > 8 * (kJoinThreads >> j.rows_log)) --j.rows_log;  // one round of loads where it can be
   j.block_sums = reinterpret_cast<double2*>(ws + l.sums_blocks);
   j.ticket = ws_view(ws).ticket;
   j.status = ws_view(ws).status;
@@ -1344,7 +1400,7 @@ int launch_linear_loss_bwd(const LinearLossArgs& a, void* workspace, cudaStream_
   LogitsParams& p = g.logits;
   p = logits_params(a, l, ws);
   p.lse = a.lse; p.coef = c.coef; p.ldd = l.ldd;
-  const int row_tiles = p.tiles_m, d_tiles = static_cast<int>((a.d + kTN - 1) / kTN);
+  const int ctas = ctas_of(a.n), n_tiles = p.tiles_m, d_tiles = static_cast<int>((a.d + kTN - 1) / kTN);
   GradProduct &dw = g.product[kClassDw], &dh = g.product[kClassDh];
   dw.N = dh.N = a.d;
   dw.tiles_n = dh.tiles_n = d_tiles;
@@ -1354,25 +1410,26 @@ int launch_linear_loss_bwd(const LinearLossArgs& a, void* workspace, cudaStream_
   dh.M = static_cast<int>(a.n);
   dh.out = a.dH; dh.ldo = a.dh_ld; dh.out_dt = a.dh_dt; dh.alpha = 1.0f / c.kf_vocab;
   dh.acc = reinterpret_cast<float*>(ws + l.acc); dh.ld_acc = l.ld_acc;
-  g.idesc = idesc_of(d_dt, d_dt);
+  g.idesc = idesc_of(d_dt, d_dt, ctas, kTN);
   g.unit = c.unit;
   rc = map_of(&m.h, a.H, a.n, a.d, a.h_ld, es, kTM);
   if (!rc) rc = map_of(&m.h_mn, h16, a.n, a.d, h16_ld, 2, kK16);
   if (rc) return rc;
   // launch i: the products of piece i - 1 and the logits of piece i
   for (long long i = 0; i <= l.pieces; ++i) {
+    p.early = i == 0;  // (after the coefficients)
     long long items[kClasses] = {};
     double cost[kClasses] = {};
     if (i < l.pieces) {
       const long long v0 = i * l.piece, cols = a.vocab - v0 < l.piece ? a.vocab - v0 : l.piece;
       p.col0 = v0; p.cols = static_cast<int>(cols);
-      p.tiles_n = static_cast<int>((cols + kTN - 1) / kTN);
+      p.tiles_n = static_cast<int>((cols + l.width - 1) / l.width);
       // distillation looks up a row's place in its entries once per item: longer ones where there are enough
-      p.run = a.k > 0 ? run_length(row_tiles, p.tiles_n, 4, 8) : 1;
+      p.run = a.k > 0 ? run_length(n_tiles, p.tiles_n, 4, 8 * units_of(a.n)) : 1;
       p.D = reinterpret_cast<uint16_t*>(ws + l.D[i & 1]);
-      items[kClassD] = static_cast<long long>(row_tiles) * ((p.tiles_n + p.run - 1) / p.run);
+      items[kClassD] = static_cast<long long>(n_tiles) * ((p.tiles_n + p.run - 1) / p.run);
       cost[kClassD] = p.run * (p.num_kb + kTileCost);
-      rc = map_of(&m.w, static_cast<const char*>(a.W) + v0 * a.w_ld * es, cols, a.d, a.w_ld, es, kTN / 2);
+      rc = map_of(&m.w, static_cast<const char*>(a.W) + v0 * a.w_ld * es, cols, a.d, a.w_ld, es, l.width / ctas);
     }
     if (!rc && i > 0) {
       const long long v0 = (i - 1) * l.piece, cols = a.vocab - v0 < l.piece ? a.vocab - v0 : l.piece;
@@ -1383,15 +1440,15 @@ int launch_linear_loss_bwd(const LinearLossArgs& a, void* workspace, cudaStream_
       dh.part_kb = (dh.num_kb + l.parts - 1) / l.parts;
       dh.parts = (dh.num_kb + dh.part_kb - 1) / dh.part_kb;
       dh.mode = l.pieces > 1 ? (i == 1 ? kAccFirst : i < l.pieces ? kAccNext : kAccLast) : dh.parts > 1 ? kAccFirst : kFinal;
-      if (a.dW) items[kClassDw] = (cols + 2 * kTM - 1) / (2 * kTM) * d_tiles;
-      if (a.dH) items[kClassDh] = static_cast<long long>(row_tiles) * d_tiles * dh.parts;
+      if (a.dW) items[kClassDw] = row_tiles(cols, ctas) * d_tiles;
+      if (a.dH) items[kClassDh] = static_cast<long long>(n_tiles) * d_tiles * dh.parts;
       cost[kClassDw] = dw.num_kb + kTileCost;
       cost[kClassDh] = dh.part_kb + kTileCost;
       rc = map_of(&m.d_mn, D, a.n, cols, l.ldd, 2, kK16);
       if (!rc) rc = map_of(&m.d_k, D, a.n, cols, l.ldd, 2, kTM);
       if (!rc) rc = map_of(&m.w_mn, w16 + v0 * w16_ld * 2, cols, a.d, w16_ld, 2, kK16);
     }
-    if (!rc) rc = launch_grad(es == 1, a.k > 0, bf, m, g, items, cost, st);
+    if (!rc) rc = ctas == 2 ? launch_grad<2>(es == 1, a.k > 0, bf, m, g, items, cost, st) : launch_grad<1>(es == 1, a.k > 0, bf, m, g, items, cost, st);
     if (rc) return rc;
   }
   if (!a.dH || l.pieces > 1 || dh.parts == 1) return SCALIFY_OK;
