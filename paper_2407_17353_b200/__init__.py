@@ -577,11 +577,16 @@ def _addr(t: Optional[ScaledTensor]):
     return t.__dict__["_desc_cache"][6]
 
 
+_functions = {}
+
+
 def _call(name: str, device: int, stream, *args) -> None:
     """Calls an entry point with ``device`` current (its stream is that device's current one unless given)."""
     if device < 0:
         raise ValueError(f"{name}: arrays must be on a CUDA device")
-    fn = getattr(lib(), name)
+    fn = _functions.get(name)
+    if fn is None:
+        fn = _functions[name] = getattr(lib(), name)
     st = torch._C._cuda_getCurrentRawStream(device) if stream is None else _stream(stream)
     if device == torch.cuda.current_device():
         code = fn(*args, st)
@@ -728,11 +733,18 @@ def scalify_linear_loss_workspace_bytes(H: ScaledTensor, W: ScaledTensor, *, k: 
     return n
 
 
-def _loss_vectors(name: str, H: ScaledTensor, ids: torch.Tensor, shape, **vectors) -> None:
-    if ids.dtype != torch.int64 or not ids.is_contiguous() or tuple(ids.shape) != tuple(shape):
+def _loss_vectors(name: str, n: int, ids: torch.Tensor, shape, loss=None, lse=None, mean=None, teacher_lse=None) -> None:
+    """ids of this shape, fp32 vectors of n elements (mean: one)."""
+    if ids.dtype is not torch.int64 or ids.shape != shape or not ids.is_contiguous():
         raise ValueError(f"{name}: ids must be a contiguous int64 tensor of shape {tuple(shape)}")
-    for what, t in vectors.items():
-        _rows_vector(name, t, 1 if what == "mean" else H.data.shape[0], what)
+    if loss is not None:
+        _rows_vector(name, loss, n, "loss")
+    if lse is not None:
+        _rows_vector(name, lse, n, "lse")
+    if mean is not None:
+        _rows_vector(name, mean, 1, "mean")
+    if teacher_lse is not None:
+        _rows_vector(name, teacher_lse, n, "teacher_lse")
 
 
 def _pad_id(padding_id: Optional[int]) -> int:
@@ -745,7 +757,8 @@ def scalify_scaled_linear_cross_entropy(H: ScaledTensor, W: ScaledTensor, ids: t
     """Cross entropy of every row of H W^T against its id, without the logits in memory: loss and lse (fp32 [n]), and
     optionally the mean over the rows whose id is not the padding.  H [n, d], W [vocab, d]."""
     name = "scalify_scaled_linear_cross_entropy"
-    _loss_vectors(name, H, ids, H.data.shape[:1], loss=loss, lse=lse, mean=mean)
+    shape = H.data.shape[:1]
+    _loss_vectors(name, shape[0], ids, shape, loss, lse, mean)
     dev = _same_device(name, W.data, H.data, ids, loss, lse, mean, ws.buf)
     _call(name, dev, stream, _addr(H), _addr(W), ids.data_ptr(), _pad_id(padding_id), float(z_loss), _ptr(loss), _ptr(lse),
           _ptr(mean), ws.ptr, ws.nbytes)
@@ -758,7 +771,8 @@ def scalify_scaled_linear_cross_entropy_bwd(H: ScaledTensor, W: ScaledTensor, id
     """Gradients of sum(grad * loss) (``grad``: F32 [n]; without it: of the mean) with respect to H and W; ``lse`` from the
     forward call.  Either output may be None."""
     name = "scalify_scaled_linear_cross_entropy_bwd"
-    _loss_vectors(name, H, ids, H.data.shape[:1], lse=lse)
+    shape = H.data.shape[:1]
+    _loss_vectors(name, shape[0], ids, shape, None, lse)
     dev = _same_device(name, W.data, H.data, ids, lse, _data(grad), _data(dH), _data(dW), ws.buf)
     _call(name, dev, stream, _addr(H), _addr(W), ids.data_ptr(), _pad_id(padding_id), float(z_loss), _ptr(lse), _addr(grad),
           _addr(dH), _addr(dW), ws.ptr, ws.nbytes)
@@ -772,7 +786,8 @@ def scalify_scaled_linear_distill(H: ScaledTensor, W: ScaledTensor, T: ScaledTen
     student's logits in memory.  ``teacher_lse``: of the teacher's whole rows at this temperature (else the entries are
     normalised among themselves)."""
     name = "scalify_scaled_linear_distill"
-    _loss_vectors(name, H, ids, T.data.shape, loss=loss, lse=lse, mean=mean, teacher_lse=teacher_lse)
+    shape = T.data.shape
+    _loss_vectors(name, shape[0], ids, shape, loss, lse, mean, teacher_lse)
     dev = _same_device(name, W.data, H.data, T.data, ids, teacher_lse, loss, lse, mean, ws.buf)
     _call(name, dev, stream, _addr(H), _addr(W), _addr(T), ids.data_ptr(), _pad_id(padding_id), _ptr(teacher_lse),
           float(temperature), _ptr(loss), _ptr(lse), _ptr(mean), ws.ptr, ws.nbytes)
@@ -785,7 +800,8 @@ def scalify_scaled_linear_distill_bwd(H: ScaledTensor, W: ScaledTensor, T: Scale
                                       stream=None) -> None:
     """Gradients of sum(grad * loss) (without ``grad``: of the mean) with respect to H and W; ``lse`` from the forward call."""
     name = "scalify_scaled_linear_distill_bwd"
-    _loss_vectors(name, H, ids, T.data.shape, lse=lse, teacher_lse=teacher_lse)
+    shape = T.data.shape
+    _loss_vectors(name, shape[0], ids, shape, None, lse, None, teacher_lse)
     dev = _same_device(name, W.data, H.data, T.data, ids, teacher_lse, lse, _data(grad), _data(dH), _data(dW), ws.buf)
     _call(name, dev, stream, _addr(H), _addr(W), _addr(T), ids.data_ptr(), _pad_id(padding_id), _ptr(teacher_lse),
           float(temperature), _ptr(lse), _addr(grad), _addr(dH), _addr(dW), ws.ptr, ws.nbytes)
@@ -796,6 +812,7 @@ def scalify_scaled_top_logits(X: ScaledTensor, V: ScaledTensor, ids: torch.Tenso
     """The k largest of every row of X [n, vocab] in descending order (V [n, k], X's dtype), their columns (ids int64 [n, k])
     and optionally the row's logsumexp at ``temperature``; equal ones by column."""
     name = "scalify_scaled_top_logits"
-    _loss_vectors(name, X, ids, V.data.shape, lse=lse)
+    shape = V.data.shape
+    _loss_vectors(name, shape[0], ids, shape, None, lse)
     dev = _same_device(name, X.data, V.data, ids, lse)
     _call(name, dev, stream, _addr(X), float(temperature), _addr(V), ids.data_ptr(), _ptr(lse))

@@ -49,6 +49,7 @@ template <int NCTA> struct Cfg {
   static constexpr int kStages = NCTA == 1 ? 4 : 6;
   static constexpr uint32_t kRing = kStages * (kABytes + kBBytes);
   static constexpr size_t kSmem = size_t(kRing) + 1024 + 256;
+  static constexpr size_t kStaging = size_t(kEpiWarps) * 32 * 128;  // of the distillation kernels: 32 values per lane
 };
 constexpr float kLog2E = 1.4426950408889634f;
 
@@ -74,6 +75,26 @@ __device__ __forceinline__ float exp2_approx(float x) {
   return y;
 }
 
+// 32 values of this lane's row in shared memory, where one whose place is known at run time only can be reached: 16-byte pieces
+// exchanged within a row so that the lanes' accesses meet different banks.
+struct LaneRow {
+  uint32_t* row;
+  int lane;
+  __device__ __forceinline__ uint4* piece(int j) const { return reinterpret_cast<uint4*>(row) + (j ^ (lane & 7)); }
+  __device__ __forceinline__ void put(const uint32_t* r) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) *piece(j) = make_uint4(r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]);
+  }
+  __device__ __forceinline__ void get(uint32_t* r) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint4 v = *piece(j);
+      r[4 * j] = v.x; r[4 * j + 1] = v.y; r[4 * j + 2] = v.z; r[4 * j + 3] = v.w;
+    }
+  }
+  __device__ __forceinline__ float& at(int i) const { return reinterpret_cast<float*>(piece(i >> 2))[i & 3]; }
+};
+
 // Shared memory, barriers and each role's place in the ring.  Warp 0: TMA producer; warp 1: MMA issuer (of the pair's first
 // CTA); warps 2-9: epilogue.  Every wait is bounded.
 template <int NCTA> struct Engine {
@@ -82,6 +103,7 @@ template <int NCTA> struct Engine {
   uint32_t smem_a, smem_b, full_bar, empty_bar, acc_full, acc_empty, drain_bar, tmem_base;
   volatile uint32_t* tmem_slot;
   volatile uint32_t* abort_flag;
+  uint8_t* stage_mem;
   uint32_t rank;
   int warp, lane;
   uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
@@ -100,6 +122,7 @@ template <int NCTA> struct Engine {
     drain_bar = acc_empty + 8 * kAccs;
     tmem_slot = reinterpret_cast<volatile uint32_t*>(bar_mem + 16 * kStages + 16 * kAccs + 8);
     abort_flag = tmem_slot + 1;
+    stage_mem = bar_mem + 256;
     warp = threadIdx.x >> 5;
     lane = threadIdx.x & 31;
     rank = NCTA == 2 ? cluster_ctarank() : 0u;
@@ -206,6 +229,7 @@ template <int NCTA> struct Engine {
     while (!mbar_try_wait(drain_bar, 0u) && global_timer_ns() - t0 < kWaitLimitNs) {}
   }
 
+  __device__ __forceinline__ LaneRow staging() const { return LaneRow{reinterpret_cast<uint32_t*>(stage_mem + ((warp - 2) * 32 + lane) * 128), lane}; }
   // ---- warps 2-9: waits for the accumulator, gives it back
   __device__ __forceinline__ bool wait_accumulator() {
     if (!__all_sync(0xFFFFFFFFu, mbar_wait(acc_full + 8 * acc, acc_phase, abort_flag))) return false;
@@ -260,7 +284,8 @@ struct LogitsParams {
   float inv_temp;
   // targets
   const long long* ids; long long padding_id, vocab;  // cross entropy
-  const Entry* entries; const int2* counts; int k;    // distillation: [n][k]; even part, both
+  const Entry* entries; const int2* counts; int k;    // distillation: [n][k]; entries in first halves, in both
+  const uint16_t* table; int bins, bin_tiles;         // [n][2][bins]: where a bin of bin_tiles tiles begins, per half
   // forward: per run and half, and row
   float2* partial;           // maximum (base-2 units), sum
   float* dot;                // sum of q z
@@ -290,7 +315,7 @@ template <bool KD> struct Targets {
       ++at;
     }
   }
-  // entries of columns >= first
+  // entries of the tile with the given first column, and of those behind it
   __device__ __forceinline__ void start(const LogitsParams& p, int row, int half, long long first) {
     id = INT_MAX;
     if (row >= p.n) return;
@@ -298,18 +323,19 @@ template <bool KD> struct Targets {
       const long long t = __ldg(p.ids + row);
       if (t != p.padding_id && t >= first && t < p.vocab && (static_cast<uint32_t>(t) / p.half_cols & 1u) == static_cast<uint32_t>(half)) { id = static_cast<int>(t); q = 1.0f; }
     } else {
+      const uint32_t bin = static_cast<uint32_t>(first) / (2 * p.half_cols * p.bin_tiles);
       const int2 c = __ldg(p.counts + row);
       const Entry* e = p.entries + static_cast<long long>(row) * p.k;
-      int lo = half ? c.x : 0, hi = half ? c.y : c.x;
-      end = e + hi;
-      while (lo < hi) {
-        const int m = (lo + hi) >> 1;
-        if (__ldg(&e[m].id) < first) lo = m + 1; else hi = m;
-      }
-      at = e + lo;
-      load_next();
-      id = next_id; q = next_q;
-      load_next();
+      at = e + __ldg(p.table + static_cast<long long>(row) * 2 * p.bins + half * p.bins + bin);
+      end = e + (half ? c.y : c.x);
+      if (p.bin_tiles > 1)
+        while (at < end && __ldg(&at->id) < first) ++at;
+      int2 u = make_int2(INT_MAX, 0), v = make_int2(INT_MAX, 0);
+      if (at < end) u = __ldg(reinterpret_cast<const int2*>(at));
+      if (at + 1 < end) v = __ldg(reinterpret_cast<const int2*>(at + 1));
+      id = u.x; q = __int_as_float(u.y);
+      next_id = v.x; next_q = __int_as_float(v.y);
+      at += 2;
     }
   }
   __device__ __forceinline__ void advance() {
@@ -370,6 +396,7 @@ __global__ void __launch_bounds__(kThreads, 1) logits_kernel(const __grid_consta
     const int half = (e.warp - 2) >> 2, quarter = e.warp & 3;
     const float c2 = load_scale_after_wait(p.h_scale) * load_scale_after_wait(p.w_scale) * p.inv_temp * kLog2E;
     Targets<KD> target;
+    const LaneRow lane_row = e.staging();
     for (long long item = unit; item < p.items && !timed_out; item += num_units) {
       const int mt = static_cast<int>(item % p.tiles_m), ng = static_cast<int>(item / p.tiles_m), nt0 = ng * p.run;
       const int row = mt * Cfg<NCTA>::kTileM + static_cast<int>(e.rank) * kTM + quarter * 32 + e.lane;
@@ -381,11 +408,20 @@ __global__ void __launch_bounds__(kThreads, 1) logits_kernel(const __grid_consta
         const int n0 = (2 * nt + half) * p.half_cols;
         e.each_chunk(half, p.half_cols, warp_rows ? p.cols - n0 : 0, [&](uint32_t* r, int c) {
           const int c0 = n0 + c * 32, valid = p.cols - c0;
-          while (__any_sync(0xFFFFFFFFu, target.id < c0 + 32ll)) {
-            const float z = pick32(r, (target.id - c0) & 31);
-            if (target.id < c0 + 32ll) {
-              dot = fmaf(target.q, z, dot);
-              target.advance();
+          if (__any_sync(0xFFFFFFFFu, target.id < c0 + 32ll)) {
+            if constexpr (KD) {
+              lane_row.put(r);
+              while (target.id < c0 + 32ll) {
+                dot = fmaf(target.q, lane_row.at(target.id - c0), dot);
+                target.advance();
+              }
+              __syncwarp();
+            } else {
+              const float z = pick32(r, (target.id - c0) & 31);
+              if (target.id < c0 + 32ll) {
+                dot = z;
+                target.advance();
+              }
             }
           }
           if (valid < 32) {
@@ -530,12 +566,13 @@ __global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_con
     }
   } else {
     const int half = (e.warp - 2) >> 2, quarter = e.warp & 3;
-    const int lane_row = static_cast<int>(e.rank) * kTM + quarter * 32 + e.lane;
+    const int own_row = static_cast<int>(e.rank) * kTM + quarter * 32 + e.lane;
+    const LaneRow lane_row = e.staging();
     const float c2 = load_scale_after_wait(l.h_scale) * load_scale_after_wait(l.w_scale) * l.inv_temp * kLog2E;
     const float unit_d = reinterpret_cast<const volatile float*>(p.unit)[0], factor = reinterpret_cast<const volatile float*>(p.unit)[1];
     each_item([&](int cls, int item) {
       if (cls == kClassD) {
-        const int row = item % l.tiles_m * Cfg<NCTA>::kTileM + lane_row, nt0 = item / l.tiles_m * l.run;
+        const int row = item % l.tiles_m * Cfg<NCTA>::kTileM + own_row, nt0 = item / l.tiles_m * l.run;
         Targets<KD> target;
         target.start(l, row, half, l.col0 + static_cast<long long>(nt0) * 2 * l.half_cols);
         float2 coef = make_float2(0.f, 0.f);
@@ -554,13 +591,20 @@ __global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_con
             float v[32];
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = coef.x * exp2_approx(fmaf(__uint_as_float(r[i]), c2, -lse2));
-            while (__any_sync(0xFFFFFFFFu, target.id < g0 + 32)) {
-              if (target.id < g0 + 32) {
+            if (__any_sync(0xFFFFFFFFu, target.id < g0 + 32)) {
+              if constexpr (KD) {
+                lane_row.put(reinterpret_cast<const uint32_t*>(v));
+                while (target.id < g0 + 32) {
+                  lane_row.at(static_cast<int>(target.id - g0)) -= coef.y * target.q;
+                  target.advance();
+                }
+                __syncwarp();
+                lane_row.get(reinterpret_cast<uint32_t*>(v));
+              } else if (target.id < g0 + 32) {
                 const int at = static_cast<int>(target.id - g0);
-                const float bq = coef.y * target.q;
 #pragma unroll
                 for (int i = 0; i < 32; ++i)
-                  if (i == at) v[i] -= bq;
+                  if (i == at) v[i] -= coef.y;
                 target.advance();
               }
             }
@@ -579,7 +623,7 @@ __global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_con
         int part, mt, nt;
         locate(g, item, part, mt, nt);
         const float alpha = g.alpha * factor;
-        const int row = mt * Cfg<NCTA>::kTileM + lane_row, n0 = nt * kTN + half * (kTN / 2);
+        const int row = mt * Cfg<NCTA>::kTileM + own_row, n0 = nt * kTN + half * (kTN / 2);
         const int mode = g.mode;
         float* acc_row = g.acc + (static_cast<long long>(part) * g.M + row) * g.ld_acc + n0;  // (padded to whole chunks)
         char* out_row = static_cast<char*>(g.out) + (static_cast<long long>(row) * g.ldo + n0) * 2;
@@ -637,12 +681,15 @@ struct TeacherParams {
   const void* T; int t_dt; long long t_ld; const float* t_scale; const float* t_lse;
   float inv_temp;
   int half_cols;
+  uint16_t* table; int bins, bin_tiles;
   Entry* entries; int2* counts; float2* sums;  // sums: Q, sum q log q
   uint32_t* status;
 };
 constexpr int kTeacherWarps = 4;
+constexpr int kMaxBins = 256;
 __global__ void __launch_bounds__(32 * kTeacherWarps) teacher_kernel(const TeacherParams p) {
   __shared__ uint32_t s_key[kTeacherWarps][kLossMaxEntries];
+  __shared__ int s_bin[kTeacherWarps][2 * kMaxBins];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const long long row = static_cast<long long>(blockIdx.x) * kTeacherWarps + warp;
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -695,7 +742,27 @@ __global__ void __launch_bounds__(32 * kTeacherWarps) teacher_kernel(const Teach
     for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
     norm = logf(s) + top;
   }
+  for (int i = lane; i < 2 * p.bins; i += 32) s_bin[warp][i] = 0;
   __syncwarp();
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    if (key[j] == 0xFFFFFFFFu) continue;
+    const uint32_t block = (key[j] & 0x3FFFFFFFu) / static_cast<uint32_t>(p.half_cols);  // 2 tile + half
+    atomicAdd(&s_bin[warp][(block & 1u) * p.bins + (block >> 1) / p.bin_tiles], 1);
+  }
+  __syncwarp();
+  int begin = 0;
+  for (int i0 = 0; i0 < 2 * p.bins; i0 += 32) {
+    const int i = i0 + lane, mine = i < 2 * p.bins ? s_bin[warp][i] : 0;
+    int upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+      if (lane >= o) upto += u;
+    }
+    if (i < 2 * p.bins) p.table[row * 2 * p.bins + i] = static_cast<uint16_t>(begin + upto - mine);
+    begin += __shfl_sync(0xFFFFFFFFu, upto, 31);
+  }
   int there = 0, even = 0;
   float mass = 0.f, neg = 0.f;
   Entry* out = p.entries + row * p.k;
@@ -1078,9 +1145,9 @@ int dh_parts(long long n, long long vocab, long long d) {
 }
 
 struct Layout {
-  size_t partial, dot, sums_blocks, entries, counts, sums, coef, tops, unit, h16, w16, D[2], acc, total;
+  size_t partial, dot, sums_blocks, entries, counts, sums, table, coef, tops, unit, h16, w16, D[2], acc, total;
   long long ld_part, ld16, ldd, ld_acc, piece, pieces;
-  int slots, run, parts, width;
+  int slots, run, parts, width, bins, bin_tiles;
 };
 Layout layout_of(long long n, long long vocab, long long d, int es, int k, bool backward) {
   Layout l = {};
@@ -1088,11 +1155,19 @@ Layout layout_of(long long n, long long vocab, long long d, int es, int k, bool 
   auto take = [&](size_t bytes) { const size_t o = at; at += pad256(bytes); return o; };
   const size_t rows = static_cast<size_t>(n);
   l.width = tile_columns(n, vocab);
+  if (backward) {
+    l.piece = piece_columns(n, vocab);
+    l.pieces = (vocab + l.piece - 1) / l.piece;
+    if (l.pieces > 1) l.width = kTN;  // (pieces begin with a tile)
+  }
   const long long tm = row_tiles(n, ctas_of(n)), tn = (vocab + l.width - 1) / l.width;
   if (k > 0) {
+    l.bin_tiles = static_cast<int>((tn + kMaxBins - 1) / kMaxBins);
+    l.bins = static_cast<int>((tn + l.bin_tiles - 1) / l.bin_tiles);
     l.entries = take(rows * k * sizeof(Entry));
     l.counts = take(rows * sizeof(int2));
     l.sums = take(rows * sizeof(float2));
+    l.table = take(rows * 2 * l.bins * sizeof(uint16_t));
   }
   if (!backward) {
     l.run = run_length(tm, tn, 8, 16 * units_of(n));
@@ -1110,10 +1185,7 @@ Layout layout_of(long long n, long long vocab, long long d, int es, int k, bool 
       l.h16 = take(rows * l.ld16 * 2);
       l.w16 = take(static_cast<size_t>(vocab) * l.ld16 * 2);
     }
-    l.piece = piece_columns(n, vocab);
-    l.pieces = (vocab + l.piece - 1) / l.piece;
     l.ldd = l.piece;
-    if (l.pieces > 1) l.width = kTN;  // (pieces begin with a tile)
     l.D[0] = take(rows * l.ldd * 2);
     l.D[1] = l.pieces > 1 ? take(rows * l.ldd * 2) : l.D[0];
     l.parts = l.pieces == 1 && n > 0 ? dh_parts(n, vocab, d) : 1;
@@ -1126,13 +1198,14 @@ Layout layout_of(long long n, long long vocab, long long d, int es, int k, bool 
   return l;
 }
 
-template <int NCTA, class K>
+template <int NCTA, bool KD, class K>
 int unit_config(K kernel, DeviceOnce& once, long long items, cudaStream_t st, cudaLaunchConfig_t* cfg, cudaLaunchAttribute* attrs, int* units) {
+  constexpr size_t kBytes = Cfg<NCTA>::kSmem + (KD ? Cfg<NCTA>::kStaging : 0);
   int most = 0;  // CTAs (pairs) that fit the GPU
   const int rc = device_once(once, &most, [&](int* v) {
-    SCALIFY_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(Cfg<NCTA>::kSmem)));
+    SCALIFY_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kBytes)));
     cudaLaunchConfig_t q = {};
-    q.gridDim = dim3(static_cast<unsigned>(sm_count() / NCTA * NCTA)); q.blockDim = dim3(kThreads); q.dynamicSmemBytes = Cfg<NCTA>::kSmem;
+    q.gridDim = dim3(static_cast<unsigned>(sm_count() / NCTA * NCTA)); q.blockDim = dim3(kThreads); q.dynamicSmemBytes = kBytes;
     cudaLaunchAttribute qa[1];
     qa[0].id = cudaLaunchAttributeClusterDimension;
     qa[0].val.clusterDim.x = NCTA; qa[0].val.clusterDim.y = 1; qa[0].val.clusterDim.z = 1;
@@ -1152,7 +1225,7 @@ int unit_config(K kernel, DeviceOnce& once, long long items, cudaStream_t st, cu
   *units = static_cast<int>(items < most ? items : most);
   if (*units > kMaxUnits) *units = kMaxUnits;
   cfg->gridDim = dim3(static_cast<unsigned>(*units * NCTA));
-  cfg->blockDim = dim3(kThreads); cfg->dynamicSmemBytes = Cfg<NCTA>::kSmem; cfg->stream = st;
+  cfg->blockDim = dim3(kThreads); cfg->dynamicSmemBytes = kBytes; cfg->stream = st;
   cfg->attrs = attrs; cfg->numAttrs = 2;
   return SCALIFY_OK;
 }
@@ -1176,7 +1249,7 @@ int launch_logits_variant(const CUtensorMap& mh, const CUtensorMap& mw, const Lo
   cudaLaunchConfig_t cfg;
   cudaLaunchAttribute attrs[2];
   int units = 0;
-  const int rc = unit_config<NCTA>(kernel, once, p.items, st, &cfg, attrs, &units);
+  const int rc = unit_config<NCTA, KD>(kernel, once, p.items, st, &cfg, attrs, &units);
   if (rc) return rc;
   SCALIFY_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, mh, mw, p));
   return SCALIFY_OK;
@@ -1237,7 +1310,7 @@ int launch_grad_variant(const GradMaps& m, GradParams& p, const long long (&item
   cudaLaunchConfig_t cfg;
   cudaLaunchAttribute attrs[2];
   int units = 0;
-  const int rc = unit_config<NCTA>(kernel, once, items[0] + items[1] + items[2], st, &cfg, attrs, &units);
+  const int rc = unit_config<NCTA, KD>(kernel, once, items[0] + items[1] + items[2], st, &cfg, attrs, &units);
   if (rc) return rc;
   fill_schedule(p.schedule, items, cost, units);
   SCALIFY_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, m, p));
@@ -1270,6 +1343,8 @@ int prepare_teacher(const LinearLossArgs& a, const Layout& l, char* ws, cudaStre
   t.T = a.T; t.t_dt = a.t_dt; t.t_ld = a.t_ld; t.t_scale = a.t_scale; t.t_lse = a.t_lse;
   t.inv_temp = a.inv_temp;
   t.half_cols = l.width / 2;
+  t.table = reinterpret_cast<uint16_t*>(ws + l.table);
+  t.bins = l.bins; t.bin_tiles = l.bin_tiles;
   t.entries = reinterpret_cast<Entry*>(ws + l.entries);
   t.counts = reinterpret_cast<int2*>(ws + l.counts);
   t.sums = reinterpret_cast<float2*>(ws + l.sums);
@@ -1291,6 +1366,8 @@ LogitsParams logits_params(const LinearLossArgs& a, const Layout& l, char* ws) {
     p.entries = reinterpret_cast<const Entry*>(ws + l.entries);
     p.counts = reinterpret_cast<const int2*>(ws + l.counts);
     p.k = a.k;
+    p.table = reinterpret_cast<const uint16_t*>(ws + l.table);
+    p.bins = l.bins; p.bin_tiles = l.bin_tiles;
   }
   p.status = ws_view(ws).status;
   return p;

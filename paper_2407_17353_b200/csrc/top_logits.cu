@@ -96,9 +96,9 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) top_logits_kernel(con
   constexpr int kWords = kVec * ElemBytes<DT>::v / 4, kWarps = THREADS / 32;
   constexpr int kBits = DT == SCALIFY_F32 ? 32 : DT == SCALIFY_BF16 ? 16 : 19;  // leading bits of a key that can differ
   using Slot = typename SlotOf<DT>::type;
-  extern __shared__ uint32_t s_raw[];
-  Slot* s_slot = reinterpret_cast<Slot*>(s_raw);  // [turns / per][THREADS]
-  __shared__ __align__(16) uint64_t s_list[kTopList];  // a candidate's key, and its place, inverted
+  extern __shared__ __align__(16) uint32_t s_raw[];
+  Slot* s_slot = reinterpret_cast<Slot*>(s_raw);                // [turns / per][THREADS]
+  uint64_t* s_list = reinterpret_cast<uint64_t*>(s_raw);        // then, in their place: a candidate's key, and its place, inverted
   __shared__ float s_m[kWarps], s_s[kWarps];
   __shared__ uint32_t s_mine[THREADS], s_bound;
   __shared__ int s_hit[kTopHits], s_hits, s_count, s_scan[kWarps];
@@ -188,8 +188,15 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) top_logits_kernel(con
     uint32_t key[kWarps], bound = 0u;
 #pragma unroll
     for (int i = 0; i < kWarps; ++i) key[i] = s_mine[i * 32 + lane];
+    uint32_t all = 0xFFFFFFFFu, any = 0u;  // bits that every key has, and that some have: the search begins where they differ
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) { all &= key[i]; any |= key[i]; }
+    all = __reduce_and_sync(0xFFFFFFFFu, all);
+    any = __reduce_or_sync(0xFFFFFFFFu, any);
+    const int first = all == any ? 14 : (31 - __clz(all ^ any)) & ~1;  // (both are even numbers of the bit pairs below)
+    bound = first >= 30 ? 0u : all & (0xFFFFFFFFu << (first + 2));
 #pragma unroll 1
-    for (int b = 30; b >= 16; b -= 2) {
+    for (int b = first; b >= 16; b -= 2) {
       int n1 = 0, n2 = 0, n3 = 0;
       const uint32_t t1 = bound | (1u << b), t2 = bound | (2u << b), t3 = bound | (3u << b);
 #pragma unroll
@@ -271,9 +278,9 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) top_logits_kernel(con
     for (int v0 = 0; v0 < vecs && count < p.k; v0 += THREADS) {  // ties, in order of place
       const int v = v0 + threadIdx.x;
       uint32_t ties = 0u;
+      float f[kVec] = {};
       if (v < vecs) {
         uint32_t w[kWords];
-        float f[kVec];
         load_vec<DT>(x, v, vocab - v * kVec, w);
         decode_vec<DT, kVec>(w, f);
 #pragma unroll
@@ -301,7 +308,7 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) top_logits_kernel(con
       for (int i = 0; i < kVec; ++i) {
         if (ties >> i & 1u) {
           const int at = count + before;
-          if (at < p.k) s_list[at] = static_cast<uint64_t>(kth) << 32 | ~static_cast<uint32_t>(v * kVec + i);
+          if (at < p.k) s_list[at] = static_cast<uint64_t>(sort_key(f[i])) << 32 | ~static_cast<uint32_t>(v * kVec + i);
           ++before;
         }
       }
@@ -311,11 +318,8 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) top_logits_kernel(con
   }
   // ---- order: few candidates count those before them, many are sorted
   auto put = [&](int rank, uint64_t c) {
-    const uint32_t id = ~static_cast<uint32_t>(c);
-    p.ids[row * p.k + rank] = id;
-    const long long o = row * p.v_ld + rank;
-    if constexpr (DT == SCALIFY_F32) static_cast<float*>(p.V)[o] = reinterpret_cast<const float*>(x)[id];
-    else static_cast<uint16_t*>(p.V)[o] = reinterpret_cast<const uint16_t*>(x)[id];
+    p.ids[row * p.k + rank] = static_cast<uint32_t>(~c);
+    store_elem<DT>(p.V, row * p.v_ld + rank, key_value(static_cast<uint32_t>(c >> 32)));  // (exact: it was of this type)
   };
   if (count <= kTopCounted) {
     if (static_cast<int>(threadIdx.x) == count && (count & 1)) s_list[count] = 0u;
@@ -357,9 +361,10 @@ __global__ void copy_scale_kernel(const float* from, float* to) {
 template <int DT, int THREADS>
 int launch_variant(const TopLogitsArgs& a, cudaStream_t st) {
   using Slot = typename SlotOf<DT>::type;
-  constexpr int kMost = kSlots * THREADS * static_cast<int>(sizeof(Slot));
+  constexpr int kMost = kSlots * THREADS * static_cast<int>(sizeof(Slot)) > kTopList * 8 ? kSlots * THREADS * static_cast<int>(sizeof(Slot)) : kTopList * 8;
   const long long turns = ((a.vocab + kVec - 1) / kVec + THREADS - 1) / THREADS;
-  const int bytes = static_cast<int>(turns < kSlots ? turns : kSlots) * THREADS * static_cast<int>(sizeof(Slot));
+  int bytes = static_cast<int>(turns < kSlots ? turns : kSlots) * THREADS * static_cast<int>(sizeof(Slot));
+  if (bytes < kTopList * 8) bytes = kTopList * 8;
   auto kernel = top_logits_kernel<DT, THREADS>;
   static DeviceOnce once;
   const int rc = device_once(once, nullptr, [&](int*) {
