@@ -44,13 +44,17 @@ constexpr int kThreads = 64 + 32 * kEpiWarps;
 // the second CTA's rows empty, so one CTA alone takes a tile of 128 rows and all of B there: twice the weights per MMA.
 template <int NCTA> struct Cfg {
   static constexpr int kTileM = kTM * NCTA;
-  static constexpr int kBRows = kTN / NCTA;
-  static constexpr int kABytes = kTM * kRowBytes, kBBytes = kBRows * kRowBytes;
-  static constexpr int kStages = NCTA == 1 ? 4 : 6;
-  static constexpr uint32_t kRing = kStages * (kABytes + kBBytes);
+  static constexpr int kABytes = kTM * kRowBytes, kBBytes = kTN / NCTA * kRowBytes;
+  static constexpr uint32_t kRing = 6 * (kTM + kTN / 2) * kRowBytes;
   static constexpr size_t kSmem = size_t(kRing) + 1024 + 256;
   static constexpr size_t kStaging = size_t(kEpiWarps) * 32 * 128;  // of the distillation kernels: 32 values per lane
 };
+// The operand ring.  A single CTA's logits want as many weights in flight as fit, and its batch fills few of A's 128 rows: A
+// takes only those (the MMAs read on into what lies behind them, which decides rows that nobody looks at), B the tile's width.
+struct Ring {
+  int stages, a_bytes, b_bytes;  // of a stage: multiples of 1024
+};
+constexpr int kMaxStages = 12;
 constexpr float kLog2E = 1.4426950408889634f;
 
 template <bool F8, int NCTA>
@@ -99,7 +103,7 @@ struct LaneRow {
 // CTA); warps 2-9: epilogue.  Every wait is bounded.
 template <int NCTA> struct Engine {
   using C = Cfg<NCTA>;
-  static constexpr int kABytes = C::kABytes, kBBytes = C::kBBytes, kStages = C::kStages;
+  int stages, a_bytes, b_bytes;
   uint32_t smem_a, smem_b, full_bar, empty_bar, acc_full, acc_empty, drain_bar, tmem_base;
   volatile uint32_t* tmem_slot;
   volatile uint32_t* abort_flag;
@@ -109,25 +113,28 @@ template <int NCTA> struct Engine {
   uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
   long long issued = 0;
 
-  __device__ __forceinline__ void set_up(uint8_t* smem_raw) {
+  __device__ __forceinline__ void set_up(uint8_t* smem_raw, const Ring& ring) {
+    stages = NCTA == 2 ? 6 : ring.stages;  // (pairs always have whole tiles)
+    a_bytes = NCTA == 2 ? C::kABytes : ring.a_bytes;
+    b_bytes = NCTA == 2 ? C::kBBytes : ring.b_bytes;
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
     uint8_t* bar_mem = smem_raw + (base - raw) + C::kRing;
     smem_a = base;
-    smem_b = base + kStages * kABytes;
+    smem_b = base + stages * a_bytes;
     const uint32_t bars = base + C::kRing;
     full_bar = bars;
-    empty_bar = bars + 8 * kStages;
-    acc_full = bars + 16 * kStages;
+    empty_bar = bars + 8 * kMaxStages;
+    acc_full = bars + 16 * kMaxStages;
     acc_empty = acc_full + 8 * kAccs;
     drain_bar = acc_empty + 8 * kAccs;
-    tmem_slot = reinterpret_cast<volatile uint32_t*>(bar_mem + 16 * kStages + 16 * kAccs + 8);
+    tmem_slot = reinterpret_cast<volatile uint32_t*>(bar_mem + 16 * kMaxStages + 16 * kAccs + 8);
     abort_flag = tmem_slot + 1;
     stage_mem = bar_mem + 256;
     warp = threadIdx.x >> 5;
     lane = threadIdx.x & 31;
     rank = NCTA == 2 ? cluster_ctarank() : 0u;
     if (threadIdx.x == 0) {
-      for (int s = 0; s < kStages; ++s) { mbar_init(full_bar + 8 * s, 1); mbar_init(empty_bar + 8 * s, 1); }
+      for (int s = 0; s < stages; ++s) { mbar_init(full_bar + 8 * s, 1); mbar_init(empty_bar + 8 * s, 1); }
       for (int s = 0; s < kAccs; ++s) { mbar_init(acc_full + 8 * s, 1); mbar_init(acc_empty + 8 * s, kEpiWarps * NCTA); }
       mbar_init(drain_bar, 1);
       *abort_flag = 0u;
@@ -152,14 +159,14 @@ template <int NCTA> struct Engine {
 
   // ---- warp 0, lane 0: the operand blocks of one tile.  Along K: a box of 128 bytes x 128 rows.  MN-major (16-bit only):
   // boxes of 64 columns x the 64 lines of this K block.
-  __device__ __forceinline__ bool produce(const CUtensorMap* ma, const CUtensorMap* mb, int m0, int n0, int width, int kb0, int num_kb, bool a_mn, bool b_mn) {
+  __device__ __forceinline__ bool produce(const CUtensorMap* ma, const CUtensorMap* mb, int m0, int n0, int height, int width, int kb0, int num_kb, bool a_mn, bool b_mn) {
     m0 += static_cast<int>(rank) * kTM;
     n0 += static_cast<int>(rank) * (width / 2);
     for (int kb = kb0; kb < kb0 + num_kb; ++kb) {
       if (!mbar_wait(empty_bar + 8 * stage, phase ^ 1u, abort_flag)) return false;
-      const uint32_t sa = smem_a + stage * kABytes, sb = smem_b + stage * kBBytes;
+      const uint32_t sa = smem_a + stage * a_bytes, sb = smem_b + stage * b_bytes;
       uint32_t fb = full_bar + 8 * stage;
-      if (rank == 0u) mbar_expect_tx(fb, NCTA * kABytes + width * kRowBytes);
+      if (rank == 0u) mbar_expect_tx(fb, NCTA * height * kRowBytes + width * kRowBytes);
       if constexpr (NCTA == 2) fb = map_to_cta(fb, 0u);  // both CTAs' copies are counted on the first one's barrier
       auto load = [&](uint32_t dst, const CUtensorMap* m, int x_bytes, int y) {
         if constexpr (NCTA == 2) tma_load_3d_pair(dst, m, fb, x_bytes, y, 0);
@@ -175,20 +182,20 @@ template <int NCTA> struct Engine {
         load(sb, mb, kb * kRowBytes, n0);
       } else {
 #pragma unroll
-        for (int j = 0; j < C::kBRows / kK16; ++j) load(sb + j * kK16 * kRowBytes, mb, (n0 + j * kK16) * 2, kb * kK16);
+        for (int j = 0; j < kTN / NCTA / kK16; ++j) load(sb + j * kK16 * kRowBytes, mb, (n0 + j * kK16) * 2, kb * kK16);
       }
       ++issued;
-      if (++stage == kStages) { stage = 0; phase ^= 1u; }
+      if (++stage == stages) { stage = 0; phase ^= 1u; }
     }
     return true;
   }
   // after a timeout: wait (bounded) for the last use of every ring slot, so that no copy is in flight when the CTA exits
   __device__ __forceinline__ void drain_copies() {
     if (rank != 0u) return;
-    const int pending = issued < kStages ? static_cast<int>(issued) : kStages;
+    const int pending = issued < stages ? static_cast<int>(issued) : stages;
     uint32_t s = stage, ph = phase;
     for (int i = 0; i < pending; ++i) {
-      if (s == 0) { s = kStages - 1; ph ^= 1u; } else { --s; }
+      if (s == 0) { s = stages - 1; ph ^= 1u; } else { --s; }
       const unsigned long long t0 = global_timer_ns();
       while (!mbar_try_wait(full_bar + 8 * s, ph) && global_timer_ns() - t0 < kWaitLimitNs) {}
     }
@@ -209,14 +216,14 @@ template <int NCTA> struct Engine {
     tc_fence_after();
     const uint32_t d_tmem = tmem_base + acc * kTN;
     for (int kb = 0; kb < num_kb; ++kb) {
-      const uint64_t ad0 = a_desc + static_cast<uint64_t>(stage * (kABytes >> 4));
-      const uint64_t bd0 = b_desc + static_cast<uint64_t>(stage * (kBBytes >> 4));
+      const uint64_t ad0 = a_desc + static_cast<uint64_t>(stage * (a_bytes >> 4));
+      const uint64_t bd0 = b_desc + static_cast<uint64_t>(stage * (b_bytes >> 4));
       if (!mbar_wait(full_bar + 8 * stage, phase, abort_flag)) return false;
       tc_fence_after();
 #pragma unroll
       for (int k = 0; k < 4; ++k) umma<F8, NCTA>(d_tmem, ad0 + k * a_inc, bd0 + k * b_inc, idesc, (kb | k) != 0 ? 1u : 0u);
       commit(empty_bar + 8 * stage);  // the slot is free (in both CTAs) once these MMAs have read it
-      if (++stage == kStages) { stage = 0; phase ^= 1u; }
+      if (++stage == stages) { stage = 0; phase ^= 1u; }
     }
     commit(acc_full + 8 * acc);
     if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
@@ -275,6 +282,8 @@ struct LogitsParams {
   int n, cols;               // rows; columns (of this piece of the vocabulary)
   long long col0;            // the piece's first column
   int num_kb;
+  Ring ring;
+  int box_rows;              // rows of A that are copied
   int half_cols;             // of a tile: what one epilogue warp takes (32 to 128)
   int tiles_m, tiles_n, run; // a work item: one row tile, `run` consecutive column tiles
   long long items;
@@ -370,7 +379,7 @@ __global__ void __launch_bounds__(kThreads, 1) logits_kernel(const __grid_consta
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_h)) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_w)) : "memory");
   }
-  e.set_up(smem_raw);
+  e.set_up(smem_raw, p.ring);
   // nothing above touches what the kernel before writes
   if (!p.early || e.warp >= 2) asm volatile("griddepcontrol.wait;" ::: "memory");
   const int unit = blockIdx.x / NCTA, num_units = gridDim.x / NCTA;
@@ -380,7 +389,7 @@ __global__ void __launch_bounds__(kThreads, 1) logits_kernel(const __grid_consta
       for (long long item = unit; item < p.items && !timed_out; item += num_units) {
         const int mt = static_cast<int>(item % p.tiles_m), nt0 = static_cast<int>(item / p.tiles_m) * p.run;
         for (int nt = nt0; nt < min(nt0 + p.run, p.tiles_n) && !timed_out; ++nt)
-          timed_out = !e.produce(&map_h, &map_w, mt * Cfg<NCTA>::kTileM, nt * 2 * p.half_cols, 2 * p.half_cols, 0, p.num_kb, false, false);
+          timed_out = !e.produce(&map_h, &map_w, mt * Cfg<NCTA>::kTileM, nt * 2 * p.half_cols, p.box_rows, 2 * p.half_cols, 0, p.num_kb, false, false);
       }
       if (timed_out || *e.abort_flag) e.drain_copies();
     }
@@ -512,7 +521,7 @@ __global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_con
   __shared__ int s_item[kClasses][kListed];  // this pair's first items
   for (int i = threadIdx.x; i < kClasses * kListed; i += kThreads)
     if (i % kListed < p.schedule.quota[i / kListed][unit]) s_item[i / kListed][i % kListed] = scheduled_item(p.schedule, i / kListed, unit, units, i % kListed);
-  e.set_up(smem_raw);
+  e.set_up(smem_raw, p.logits.ring);
   // nothing above touches what the kernel before writes
   if (!p.logits.early || e.warp >= 2) asm volatile("griddepcontrol.wait;" ::: "memory");
   const LogitsParams& l = p.logits;
@@ -539,13 +548,13 @@ __global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_con
         if (cls == kClassD) {
           const int mt = item % l.tiles_m, nt0 = item / l.tiles_m * l.run;
           for (int nt = nt0; nt < min(nt0 + l.run, l.tiles_n) && !timed_out; ++nt)
-            timed_out = !e.produce(&maps.h, &maps.w, mt * Cfg<NCTA>::kTileM, nt * 2 * l.half_cols, 2 * l.half_cols, 0, l.num_kb, false, false);
+            timed_out = !e.produce(&maps.h, &maps.w, mt * Cfg<NCTA>::kTileM, nt * 2 * l.half_cols, l.box_rows, 2 * l.half_cols, 0, l.num_kb, false, false);
         } else {
           const GradProduct& g = p.product[cls];
           int part, mt, nt;
           const int kbs = locate(g, item, part, mt, nt);
-          timed_out = cls == kClassDw ? !e.produce(&maps.d_mn, &maps.h_mn, mt * Cfg<NCTA>::kTileM, nt * kTN, kTN, part * g.part_kb, kbs, true, true)
-                                      : !e.produce(&maps.d_k, &maps.w_mn, mt * Cfg<NCTA>::kTileM, nt * kTN, kTN, part * g.part_kb, kbs, false, true);
+          timed_out = cls == kClassDw ? !e.produce(&maps.d_mn, &maps.h_mn, mt * Cfg<NCTA>::kTileM, nt * kTN, kTM, kTN, part * g.part_kb, kbs, true, true)
+                                      : !e.produce(&maps.d_k, &maps.w_mn, mt * Cfg<NCTA>::kTileM, nt * kTN, kTM, kTN, part * g.part_kb, kbs, false, true);
         }
       });
       if (timed_out || *e.abort_flag) e.drain_copies();
@@ -688,7 +697,7 @@ struct TeacherParams {
 constexpr int kTeacherWarps = 4;
 constexpr int kMaxBins = 256;
 __global__ void __launch_bounds__(32 * kTeacherWarps) teacher_kernel(const TeacherParams p) {
-  __shared__ uint32_t s_key[kTeacherWarps][kLossMaxEntries];
+  __shared__ __align__(16) uint32_t s_key[kTeacherWarps][kLossMaxEntries];
   __shared__ int s_bin[kTeacherWarps][2 * kMaxBins];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const long long row = static_cast<long long>(blockIdx.x) * kTeacherWarps + warp;
@@ -725,8 +734,8 @@ __global__ void __launch_bounds__(32 * kTeacherWarps) teacher_kernel(const Teach
           }
         }
       }
-      s_key[warp][i] = key[j];
     }
+    s_key[warp][i] = key[j];  // (behind the last one: larger than any)
   }
   if (bad) atomicOr(p.status, static_cast<uint32_t>(SCALIFY_DEV_BAD_INDEX));
   float norm;
@@ -775,12 +784,19 @@ __global__ void __launch_bounds__(32 * kTeacherWarps) teacher_kernel(const Teach
     const float lq = t[j] - norm, q = ok ? expf(lq) : 0.f;
     mass += q;
     neg += ok && q != 0.f ? q * lq : 0.f;
+    // how many go before it: the smaller keys, and equal ones with a smaller place
     int before = 0;
-    const int i = j * 32 + lane;
-    for (int m = 0; m < p.k; ++m) {
-      const uint32_t other = s_key[warp][m];
-      before += other < key[j] || (other == key[j] && m < i);
+    for (int jm = 0; jm * 32 < p.k; ++jm) {
+      const uint4* others = reinterpret_cast<const uint4*>(s_key[warp] + jm * 32);
+      const uint32_t limit = key[j] + (jm < j ? 1u : 0u);
+#pragma unroll
+      for (int m = 0; m < 8; ++m) {
+        const uint4 o = others[m];
+        before += (o.x < limit) + (o.y < limit) + (o.z < limit) + (o.w < limit);
+      }
     }
+    // (equal ones of its own 32: few, if any)
+    for (uint32_t same = __match_any_sync(0xFFFFFFFFu, key[j]) & ((1u << lane) - 1u); same && ok; same &= same - 1u) ++before;
     if (ok) out[before] = Entry{static_cast<int>(key[j] & 0x3FFFFFFFu), q};
   }
 #pragma unroll
@@ -1352,8 +1368,17 @@ int prepare_teacher(const LinearLossArgs& a, const Layout& l, char* ws, cudaStre
   return launch_small(teacher_kernel, (a.n + kTeacherWarps - 1) / kTeacherWarps, 32 * kTeacherWarps, t, st);
 }
 
+// (whole: a launch with tiles of the products)
+Ring ring_of(int ctas, int box_rows, int width, bool whole) {
+  Ring r = {0, whole ? kTM * kRowBytes : box_rows * kRowBytes, (whole ? kTN : width) / ctas * kRowBytes};
+  r.stages = static_cast<int>(Cfg<1>::kRing / (r.a_bytes + r.b_bytes));
+  if (r.stages > kMaxStages) r.stages = kMaxStages;
+  return r;
+}
 LogitsParams logits_params(const LinearLossArgs& a, const Layout& l, char* ws) {
   LogitsParams p = {};
+  p.box_rows = ctas_of(a.n) == 2 ? kTM : static_cast<int>(pad_to(a.n, 8));
+  p.ring = ring_of(ctas_of(a.n), p.box_rows, l.width, false);
   const int es = elem_size(a.h_dt);
   p.n = static_cast<int>(a.n);
   p.num_kb = static_cast<int>((static_cast<long long>(a.d) * es + kRowBytes - 1) / kRowBytes);
@@ -1399,7 +1424,7 @@ int launch_linear_loss(const LinearLossArgs& a, void* workspace, cudaStream_t st
   p.dot = reinterpret_cast<float*>(ws + l.dot);
   p.ld_part = l.ld_part;
   CUtensorMap mh, mw;
-  rc = map_of(&mh, a.H, a.n, a.d, a.h_ld, es, kTM);
+  rc = map_of(&mh, a.H, a.n, a.d, a.h_ld, es, p.box_rows);
   if (!rc) rc = map_of(&mw, a.W, a.vocab, a.d, a.w_ld, es, l.width / ctas_of(a.n));
   if (!rc) {
     rc = ctas_of(a.n) == 2 ? launch_logits<2>(es == 1, a.k > 0, mh, mw, p, st) : launch_logits<1>(es == 1, a.k > 0, mh, mw, p, st);
@@ -1489,12 +1514,13 @@ int launch_linear_loss_bwd(const LinearLossArgs& a, void* workspace, cudaStream_
   dh.acc = reinterpret_cast<float*>(ws + l.acc); dh.ld_acc = l.ld_acc;
   g.idesc = idesc_of(d_dt, d_dt, ctas, kTN);
   g.unit = c.unit;
-  rc = map_of(&m.h, a.H, a.n, a.d, a.h_ld, es, kTM);
+  rc = map_of(&m.h, a.H, a.n, a.d, a.h_ld, es, p.box_rows);
   if (!rc) rc = map_of(&m.h_mn, h16, a.n, a.d, h16_ld, 2, kK16);
   if (rc) return rc;
   // launch i: the products of piece i - 1 and the logits of piece i
   for (long long i = 0; i <= l.pieces; ++i) {
     p.early = i == 0;  // (after the coefficients)
+    p.ring = ring_of(ctas, p.box_rows, l.width, i > 0);
     long long items[kClasses] = {};
     double cost[kClasses] = {};
     if (i < l.pieces) {
