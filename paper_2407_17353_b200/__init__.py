@@ -573,6 +573,12 @@ def _addr(t: Optional[ScaledTensor]):
     """Address of a ScaledTensor's descriptor (kept alive on the object), None for None."""
     if t is None:
         return None
+    cached = t.__dict__.get("_desc_cache")
+    if cached is not None:
+        d, scale = t.data, t.scale
+        if (cached[0] == d.data_ptr() and cached[1] == (0 if scale is None else scale.data_ptr()) and cached[2] is d.dtype
+                and cached[3] == d.shape and cached[4] == d.stride()):
+            return cached[6]
     _desc(t)
     return t.__dict__["_desc_cache"][6]
 
@@ -607,7 +613,7 @@ def _same_device(name: str, first: torch.Tensor, *others) -> int:
 
 
 def _rows_vector(name: str, t: Optional[torch.Tensor], n: int, what: str, dtype=torch.float32) -> None:
-    if t is not None and (t.dtype != dtype or t.numel() != n or not t.is_contiguous()):
+    if t is not None and (t.dtype is not dtype or t.numel() != n or not t.is_contiguous()):
         raise ValueError(f"{name}: {what} must be a contiguous {dtype} tensor of {n} elements")
 
 

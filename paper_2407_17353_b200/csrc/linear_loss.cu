@@ -696,15 +696,15 @@ struct TeacherParams {
 };
 constexpr int kTeacherWarps = 4;
 constexpr int kMaxBins = 256;
+template <int kPer>  // entries per lane
 __global__ void __launch_bounds__(32 * kTeacherWarps) teacher_kernel(const TeacherParams p) {
-  __shared__ __align__(16) uint32_t s_key[kTeacherWarps][kLossMaxEntries];
+  __shared__ __align__(16) uint32_t s_key[kTeacherWarps][32 * kPer];
   __shared__ int s_bin[kTeacherWarps][2 * kMaxBins];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const long long row = static_cast<long long>(blockIdx.x) * kTeacherWarps + warp;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");  // (behind the wait: a dependent may read what was there before this kernel)
   if (row >= p.n) return;
-  constexpr int kPer = kLossMaxEntries / 32;
   const float scale = load_scale_after_wait(p.t_scale);
   if (row == 0 && lane == 0 && !is_pow2_scale(scale)) atomicOr(p.status, static_cast<uint32_t>(SCALIFY_DEV_BAD_SCALE));
   const float f = scale * p.inv_temp;
@@ -712,28 +712,28 @@ __global__ void __launch_bounds__(32 * kTeacherWarps) teacher_kernel(const Teach
   uint32_t key[kPer];
   float top = -INFINITY;
   bool bad = false;
+  long long id[kPer];
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {  // (all loads at once)
+    const int i = j * 32 + lane;
+    id[j] = i < p.k ? p.ids[row * p.k + i] : p.padding_id;
+    const long long at = row * p.t_ld + i;
+    t[j] = i >= p.k ? 0.f
+           : p.t_dt == SCALIFY_F32 ? load_elem<SCALIFY_F32>(p.T, at)
+           : p.t_dt == SCALIFY_BF16 ? load_elem<SCALIFY_BF16>(p.T, at) : load_elem<SCALIFY_F16>(p.T, at);
+  }
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {
     const int i = j * 32 + lane;
+    const bool known = id[j] >= 0 && id[j] < p.vocab, wanted = i < p.k && id[j] != p.padding_id;
+    const float x = t[j] * f;
+    bad = bad || (wanted && !known);
     key[j] = 0xFFFFFFFFu;
     t[j] = -INFINITY;
-    if (i < p.k) {
-      const long long id = p.ids[row * p.k + i];
-      if (id != p.padding_id) {
-        if (id < 0 || id >= p.vocab) {
-          bad = true;
-        } else {
-          const long long at = row * p.t_ld + i;
-          float x = p.t_dt == SCALIFY_F32 ? load_elem<SCALIFY_F32>(p.T, at)
-                    : p.t_dt == SCALIFY_BF16 ? load_elem<SCALIFY_BF16>(p.T, at) : load_elem<SCALIFY_F16>(p.T, at);
-          x *= f;
-          if (x != -INFINITY) {
-            t[j] = x;
-            key[j] = static_cast<uint32_t>(id) | (static_cast<uint32_t>(id) / p.half_cols & 1u) << 30;
-            top = x > top || x != x ? x : top;
-          }
-        }
-      }
+    if (wanted && known && x != -INFINITY) {
+      t[j] = x;
+      key[j] = static_cast<uint32_t>(id[j]) | (static_cast<uint32_t>(id[j]) / p.half_cols & 1u) << 30;
+      top = x > top || x != x ? x : top;
     }
     s_key[warp][i] = key[j];  // (behind the last one: larger than any)
   }
@@ -777,7 +777,6 @@ __global__ void __launch_bounds__(32 * kTeacherWarps) teacher_kernel(const Teach
   Entry* out = p.entries + row * p.k;
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {
-    if (j * 32 >= p.k) break;
     const bool ok = key[j] != 0xFFFFFFFFu;
     there += __popc(__ballot_sync(0xFFFFFFFFu, ok));
     even += __popc(__ballot_sync(0xFFFFFFFFu, key[j] < (1u << 30)));
@@ -786,7 +785,8 @@ __global__ void __launch_bounds__(32 * kTeacherWarps) teacher_kernel(const Teach
     neg += ok && q != 0.f ? q * lq : 0.f;
     // how many go before it: the smaller keys, and equal ones with a smaller place
     int before = 0;
-    for (int jm = 0; jm * 32 < p.k; ++jm) {
+#pragma unroll (kPer <= 2 ? kPer : 1)
+    for (int jm = 0; jm < kPer; ++jm) {
       const uint4* others = reinterpret_cast<const uint4*>(s_key[warp] + jm * 32);
       const uint32_t limit = key[j] + (jm < j ? 1u : 0u);
 #pragma unroll
@@ -1365,7 +1365,11 @@ int prepare_teacher(const LinearLossArgs& a, const Layout& l, char* ws, cudaStre
   t.counts = reinterpret_cast<int2*>(ws + l.counts);
   t.sums = reinterpret_cast<float2*>(ws + l.sums);
   t.status = ws_view(ws).status;
-  return launch_small(teacher_kernel, (a.n + kTeacherWarps - 1) / kTeacherWarps, 32 * kTeacherWarps, t, st);
+  const long long blocks = (a.n + kTeacherWarps - 1) / kTeacherWarps;
+  if (a.k <= 32) return launch_small(teacher_kernel<1>, blocks, 32 * kTeacherWarps, t, st);
+  if (a.k <= 64) return launch_small(teacher_kernel<2>, blocks, 32 * kTeacherWarps, t, st);
+  if (a.k <= 128) return launch_small(teacher_kernel<4>, blocks, 32 * kTeacherWarps, t, st);
+  return launch_small(teacher_kernel<kLossMaxEntries / 32>, blocks, 32 * kTeacherWarps, t, st);
 }
 
 // (whole: a launch with tiles of the products)
