@@ -23,6 +23,8 @@
 #include <limits.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "linear_loss.h"
 #include "scalify_common.cuh"
 #include "scalify_launch.h"
@@ -55,6 +57,7 @@ struct Ring {
   int stages, a_bytes, b_bytes;  // of a stage: multiples of 1024
 };
 constexpr int kMaxStages = 12;
+constexpr int kLongKb = 24, kSegmentKb = 16;  // K blocks of a long contraction, and of its parts
 constexpr float kLog2E = 1.4426950408889634f;
 
 template <bool F8, int NCTA>
@@ -264,6 +267,23 @@ template <int NCTA> struct Engine {
       }
     }
   }
+  // f(32 columns of this lane's row, chunk as a constant) for every chunk of this warp's half
+  template <class F> __device__ __forceinline__ void each_chunk_in_order(int half, int half_cols, F f) {
+    const uint32_t t_addr = tmem_base + (static_cast<uint32_t>((warp & 3) * 32) << 16) + acc * kTN + half * half_cols;
+    uint32_t r[32];
+    auto one = [&](auto chunk) {
+      constexpr int c = decltype(chunk)::value;
+      if (c * 32 < half_cols) {
+        tmem_ld32(t_addr + c * 32, r);
+        tmem_ld_wait();
+        f(r, chunk);
+      }
+    };
+    one(std::integral_constant<int, 0>());
+    one(std::integral_constant<int, 1>());
+    one(std::integral_constant<int, 2>());
+    one(std::integral_constant<int, 3>());
+  }
   __device__ __forceinline__ void release_accumulator() {
     tc_fence_before();
     __syncwarp();
@@ -369,7 +389,10 @@ __device__ __forceinline__ float pick32(const uint32_t* r, int i) {
   return __uint_as_float(a[0]);
 }
 
-template <int NCTA, bool F8, bool KD>
+// LONG: the tensor cores add up with truncation, an error that grows with the number of additions and the sums' size, and the
+// losses are fp32: from kLongKb K blocks on, every kSegmentKb of them go to an accumulator of their own, and the epilogue warps
+// add those up in registers while the next ones are filled (d = 4096: relative errors of lse and loss 1.3e-6 and 2.0e-6 in one accumulator, 3e-7 and 4.5e-7 so, in the same time).
+template <int NCTA, bool F8, bool KD, bool LONG>
 __global__ void __launch_bounds__(kThreads, 1) logits_kernel(const __grid_constant__ CUtensorMap map_h,
                                                              const __grid_constant__ CUtensorMap map_w, const LogitsParams p) {
   asm volatile("griddepcontrol.launch_dependents;");  // the next kernel may set up while this one runs
@@ -397,7 +420,13 @@ __global__ void __launch_bounds__(kThreads, 1) logits_kernel(const __grid_consta
     if (e.lane == 0 && e.rank == 0u) {
       for (long long item = unit; item < p.items && !timed_out; item += num_units) {
         const int nt0 = static_cast<int>(item / p.tiles_m) * p.run;
-        for (int nt = nt0; nt < min(nt0 + p.run, p.tiles_n) && !timed_out; ++nt) timed_out = !e.template multiply<F8>(p.num_kb, p.idesc, false, false);
+        for (int nt = nt0; nt < min(nt0 + p.run, p.tiles_n) && !timed_out; ++nt) {
+          if constexpr (LONG) {
+            for (int kb = 0; kb < p.num_kb && !timed_out; kb += kSegmentKb) timed_out = !e.template multiply<F8>(min(kSegmentKb, p.num_kb - kb), p.idesc, false, false);
+          } else {
+            timed_out = !e.template multiply<F8>(p.num_kb, p.idesc, false, false);
+          }
+        }
       }
       if (timed_out || *e.abort_flag) e.drain_multiplies();
     }
@@ -413,9 +442,8 @@ __global__ void __launch_bounds__(kThreads, 1) logits_kernel(const __grid_consta
       target.start(p, row, half, static_cast<long long>(nt0) * 2 * p.half_cols);
       float top = -INFINITY, sum = 0.f, dot = 0.f;
       for (int nt = nt0; nt < min(nt0 + p.run, p.tiles_n); ++nt) {
-        if (!e.wait_accumulator()) { timed_out = true; break; }
         const int n0 = (2 * nt + half) * p.half_cols;
-        e.each_chunk(half, p.half_cols, warp_rows ? p.cols - n0 : 0, [&](uint32_t* r, int c) {
+        auto work = [&](uint32_t* r, int c) {
           const int c0 = n0 + c * 32, valid = p.cols - c0;
           if (__any_sync(0xFFFFFFFFu, target.id < c0 + 32ll)) {
             if constexpr (KD) {
@@ -451,8 +479,28 @@ __global__ void __launch_bounds__(kThreads, 1) logits_kernel(const __grid_consta
 #pragma unroll
           for (int i = 0; i < 32; ++i) s[i & 3] += exp2_approx(fmaf(__uint_as_float(r[i]), c2, shift));
           sum += (s[0] + s[1]) + (s[2] + s[3]);
-        });
-        e.release_accumulator();
+        };
+        const int cols = warp_rows ? p.cols - n0 : 0;
+        if constexpr (LONG) {
+          float z[kTN / 64][32];
+          for (int kb = 0; kb < p.num_kb && !timed_out; kb += kSegmentKb) {
+            if (!e.wait_accumulator()) { timed_out = true; break; }
+            e.each_chunk_in_order(half, p.half_cols, [&](const uint32_t* r, auto chunk) {
+              constexpr int c = decltype(chunk)::value;
+#pragma unroll
+              for (int i = 0; i < 32; ++i) z[c][i] = kb == 0 ? __uint_as_float(r[i]) : z[c][i] + __uint_as_float(r[i]);
+            });
+            e.release_accumulator();
+          }
+          if (timed_out) break;
+#pragma unroll
+          for (int c = 0; c < kTN / 64; ++c)
+            if (c * 32 < min(p.half_cols, cols)) work(reinterpret_cast<uint32_t*>(z[c]), c);
+        } else {
+          if (!e.wait_accumulator()) { timed_out = true; break; }
+          e.each_chunk(half, p.half_cols, cols, work);
+          e.release_accumulator();
+        }
       }
       if (row < p.n && !timed_out) {
         const long long o = static_cast<long long>(ng * 2 + half) * p.ld_part + row;
@@ -1258,9 +1306,9 @@ int launch_small(K kernel, long long blocks, int threads, const P& p, cudaStream
   return SCALIFY_OK;
 }
 
-template <int NCTA, bool F8, bool KD>
+template <int NCTA, bool F8, bool KD, bool LONG>
 int launch_logits_variant(const CUtensorMap& mh, const CUtensorMap& mw, const LogitsParams& p, cudaStream_t st) {
-  auto kernel = logits_kernel<NCTA, F8, KD>;
+  auto kernel = logits_kernel<NCTA, F8, KD, LONG>;
   static DeviceOnce once;
   cudaLaunchConfig_t cfg;
   cudaLaunchAttribute attrs[2];
@@ -1271,10 +1319,14 @@ int launch_logits_variant(const CUtensorMap& mh, const CUtensorMap& mw, const Lo
   return SCALIFY_OK;
 }
 
+template <int NCTA, bool LONG>
+int launch_logits(bool f8, bool kd, const CUtensorMap& mh, const CUtensorMap& mw, const LogitsParams& p, cudaStream_t st) {
+  if (f8) return kd ? launch_logits_variant<NCTA, true, true, LONG>(mh, mw, p, st) : launch_logits_variant<NCTA, true, false, LONG>(mh, mw, p, st);
+  return kd ? launch_logits_variant<NCTA, false, true, LONG>(mh, mw, p, st) : launch_logits_variant<NCTA, false, false, LONG>(mh, mw, p, st);
+}
 template <int NCTA>
 int launch_logits(bool f8, bool kd, const CUtensorMap& mh, const CUtensorMap& mw, const LogitsParams& p, cudaStream_t st) {
-  if (f8) return kd ? launch_logits_variant<NCTA, true, true>(mh, mw, p, st) : launch_logits_variant<NCTA, true, false>(mh, mw, p, st);
-  return kd ? launch_logits_variant<NCTA, false, true>(mh, mw, p, st) : launch_logits_variant<NCTA, false, false>(mh, mw, p, st);
+  return p.num_kb > kLongKb ? launch_logits<NCTA, true>(f8, kd, mh, mw, p, st) : launch_logits<NCTA, false>(f8, kd, mh, mw, p, st);
 }
 
 // Every class's items over the pairs, long ones first, so that the loads become as equal as whole items allow.
@@ -1405,7 +1457,10 @@ LogitsParams logits_params(const LinearLossArgs& a, const Layout& l, char* ws) {
 }  // namespace
 
 size_t linear_loss_ws_bytes(long long n, long long vocab, long long d, int operand_bytes, int k, bool backward) {
-  return layout_of(n, vocab, d, operand_bytes, k, backward).total;
+  const size_t forward = layout_of(n, vocab, d, operand_bytes, k, false).total;
+  if (!backward) return forward;
+  const size_t both = layout_of(n, vocab, d, operand_bytes, k, true).total;
+  return both > forward ? both : forward;
 }
 
 int launch_linear_loss(const LinearLossArgs& a, void* workspace, cudaStream_t st) {

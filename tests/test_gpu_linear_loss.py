@@ -137,6 +137,15 @@ def test_several_pieces_and_long_runs(n, vocab, d, k):
         check(H, W, ids_of(n, vocab), out=F16, z_loss=1e-4)
 
 
+@pytest.mark.parametrize("ht,wt", KINDS)
+@pytest.mark.parametrize("n,vocab,d", [(37, 300, 4104), (130, 500, 4104), (300, 260, 1544)])
+def test_long_contractions(n, vocab, d, ht, wt):
+    H, W = layer(n, vocab, d, ht, wt, seed=d)
+    check(H, W, ids_of(n, vocab), ws=2.0 ** -5, grad=rand((n,), 9))
+    T, ids = teacher(n, 20, vocab, BF16, pad=1)
+    check(H, W, ids, ws=2.0 ** -5, T=T, temp=2.0)
+
+
 def test_padding_and_unknown_targets():
     H, W = layer(40, 200, 64, BF16)
     ids = ids_of(40, 200)
