@@ -49,7 +49,7 @@ template <int NCTA> struct Cfg {
   static constexpr int kABytes = kTM * kRowBytes, kBBytes = kTN / NCTA * kRowBytes;
   static constexpr uint32_t kRing = 6 * (kTM + kTN / 2) * kRowBytes;
   static constexpr size_t kSmem = size_t(kRing) + 1024 + 256;
-  static constexpr size_t kStaging = size_t(kEpiWarps) * 32 * 128;  // of the distillation kernels: 32 values per lane
+  static constexpr size_t kStaging = size_t(kEpiWarps) * 32 * 128;  // of the distillation and the gradient kernels: 32 values per lane
 };
 // The operand ring.  A single CTA's logits want as many weights in flight as fit, and its batch fills few of A's 128 rows: A
 // takes only those (the MMAs read on into what lies behind them, which decides rows that nobody looks at), B the tile's width.
@@ -100,6 +100,24 @@ struct LaneRow {
     }
   }
   __device__ __forceinline__ float& at(int i) const { return reinterpret_cast<float*>(piece(i >> 2))[i & 3]; }
+  // 32 16-bit values per lane -> 32 rows of memory from (x bytes, y) on, by the store engine (which leaves out what lies past
+  // the matrix): a warp's own stores would meet 32 lines per instruction, beside its exponentials (distillation step 8192 x 768
+  // 1920 -> 1834 us).  Two tiles in turns (`flip`); every store of the tile
+  // before the last one has left shared memory before its place is taken.  All lanes of the warp.
+  __device__ __forceinline__ void store(const uint32_t* o, const CUtensorMap* map, int x_bytes, int y, uint32_t& flip) const {
+    if (lane == 0) bulk_wait_read<1>();
+    __syncwarp();
+    uint4* tile = reinterpret_cast<uint4*>(row - lane * 32) + flip * 128;
+    flip ^= 1u;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) tile[lane * 4 + (j ^ ((lane >> 1) & 3))] = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+    fence_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      tma_store_3d(map, smem_u32(tile), x_bytes, y, 0);
+      bulk_commit();
+    }
+  }
 };
 
 // Shared memory, barriers and each role's place in the ring.  Warp 0: TMA producer; warp 1: MMA issuer (of the pair's first
@@ -116,15 +134,17 @@ template <int NCTA> struct Engine {
   uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
   long long issued = 0;
 
-  __device__ __forceinline__ void set_up(uint8_t* smem_raw, const Ring& ring) {
+  __device__ __forceinline__ void set_up(uint8_t* smem_raw, const Ring& ring, bool staging) {
     stages = NCTA == 2 ? 6 : ring.stages;  // (pairs always have whole tiles)
     a_bytes = NCTA == 2 ? C::kABytes : ring.a_bytes;
     b_bytes = NCTA == 2 ? C::kBBytes : ring.b_bytes;
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-    uint8_t* bar_mem = smem_raw + (base - raw) + C::kRing;
+    stage_mem = smem_raw + (base - raw) + C::kRing;  // (the store engine's swizzle wants 512-byte boundaries)
+    const uint32_t bar_at = C::kRing + (staging ? C::kStaging : 0);
+    uint8_t* bar_mem = smem_raw + (base - raw) + bar_at;
     smem_a = base;
     smem_b = base + stages * a_bytes;
-    const uint32_t bars = base + C::kRing;
+    const uint32_t bars = base + bar_at;
     full_bar = bars;
     empty_bar = bars + 8 * kMaxStages;
     acc_full = bars + 16 * kMaxStages;
@@ -132,7 +152,6 @@ template <int NCTA> struct Engine {
     drain_bar = acc_empty + 8 * kAccs;
     tmem_slot = reinterpret_cast<volatile uint32_t*>(bar_mem + 16 * kMaxStages + 16 * kAccs + 8);
     abort_flag = tmem_slot + 1;
-    stage_mem = bar_mem + 256;
     warp = threadIdx.x >> 5;
     lane = threadIdx.x & 31;
     rank = NCTA == 2 ? cluster_ctarank() : 0u;
@@ -322,8 +341,6 @@ struct LogitsParams {
   // gradient
   const float* lse;
   const float2* coef;        // of p and of q
-  uint16_t* D;
-  long long ldd;
   uint32_t* status;
 };
 
@@ -331,48 +348,47 @@ struct LogitsParams {
 template <bool KD> struct Targets {
   int id = INT_MAX;
   float q = 0.f;
-  int next_id = INT_MAX;
-  float next_q = 0.f;
+  static constexpr int kAhead = 3;  // entries on their way: frequent tokens give a row many in a few tiles
+  int2 ahead[kAhead];
   const Entry* at = nullptr;
   const Entry* end = nullptr;
-  __device__ __forceinline__ void load_next() {
-    next_id = INT_MAX;
-    if (at < end) {
-      const int2 e = __ldg(reinterpret_cast<const int2*>(at));
-      next_id = e.x;
-      next_q = __int_as_float(e.y);
-      ++at;
-    }
-  }
+  __device__ __forceinline__ int2 load(const Entry* e) const { return e < end ? __ldg(reinterpret_cast<const int2*>(e)) : make_int2(INT_MAX, 0); }
   // entries of the tile with the given first column, and of those behind it
   __device__ __forceinline__ void start(const LogitsParams& p, int row, int half, long long first) {
     id = INT_MAX;
-    if (row >= p.n) return;
     if constexpr (!KD) {
+      if (row >= p.n) return;
       const long long t = __ldg(p.ids + row);
       if (t != p.padding_id && t >= first && t < p.vocab && (static_cast<uint32_t>(t) / p.half_cols & 1u) == static_cast<uint32_t>(half)) { id = static_cast<int>(t); q = 1.0f; }
     } else {
-      const uint32_t bin = static_cast<uint32_t>(first) / (2 * p.half_cols * p.bin_tiles);
-      const int2 c = __ldg(p.counts + row);
-      const Entry* e = p.entries + static_cast<long long>(row) * p.k;
-      at = e + __ldg(p.table + static_cast<long long>(row) * 2 * p.bins + half * p.bins + bin);
-      end = e + (half ? c.y : c.x);
-      if (p.bin_tiles > 1)
-        while (at < end && __ldg(&at->id) < first) ++at;
-      int2 u = make_int2(INT_MAX, 0), v = make_int2(INT_MAX, 0);
-      if (at < end) u = __ldg(reinterpret_cast<const int2*>(at));
-      if (at + 1 < end) v = __ldg(reinterpret_cast<const int2*>(at + 1));
-      id = u.x; q = __int_as_float(u.y);
-      next_id = v.x; next_q = __int_as_float(v.y);
-      at += 2;
+      at = end = nullptr;
+      if (row < p.n) {
+        const uint32_t bin = static_cast<uint32_t>(first) / (2 * p.half_cols * p.bin_tiles);
+        const int2 c = __ldg(p.counts + row);
+        const Entry* e = p.entries + static_cast<long long>(row) * p.k;
+        at = e + __ldg(p.table + static_cast<long long>(row) * 2 * p.bins + half * p.bins + bin);
+        end = e + (half ? c.y : c.x);
+        if (p.bin_tiles > 1)
+          while (at < end && __ldg(&at->id) < first) ++at;
+      }
+      const int2 e0 = load(at);
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) ahead[i] = load(at + 1 + i);
+      at += 1 + kAhead;
+      id = e0.x;
+      q = __int_as_float(e0.y);
     }
   }
   __device__ __forceinline__ void advance() {
     if constexpr (!KD) {
       id = INT_MAX;
     } else {
-      id = next_id; q = next_q;
-      load_next();
+      id = ahead[0].x;
+      q = __int_as_float(ahead[0].y);
+#pragma unroll
+      for (int i = 0; i + 1 < kAhead; ++i) ahead[i] = ahead[i + 1];
+      ahead[kAhead - 1] = load(at);
+      ++at;
     }
   }
 };
@@ -402,7 +418,7 @@ __global__ void __launch_bounds__(kThreads, 1) logits_kernel(const __grid_consta
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_h)) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map_w)) : "memory");
   }
-  e.set_up(smem_raw, p.ring);
+  e.set_up(smem_raw, p.ring, KD);
   // nothing above touches what the kernel before writes
   if (!p.early || e.warp >= 2) asm volatile("griddepcontrol.wait;" ::: "memory");
   const int unit = blockIdx.x / NCTA, num_units = gridDim.x / NCTA;
@@ -518,7 +534,7 @@ __global__ void __launch_bounds__(kThreads, 1) logits_kernel(const __grid_consta
 // the logits (the gradient D) of the NEXT piece, which fill the pairs up to equal loads whatever the products' tiles leave.
 enum { kClassDw = 0, kClassDh = 1, kClassD = 2, kClasses = 3 };
 constexpr int kMaxUnits = 160;
-constexpr int kListed = 128;
+constexpr int kListed = 48;
 struct Schedule {
   int order[kClasses];               // long tiles first
   int total[kClasses];
@@ -556,7 +572,15 @@ struct GradParams {
   uint32_t idesc;          // of the products
   const float* unit;       // [0]: the power of two that D is stored times; [1]: what its products are multiplied by
 };
-struct GradMaps { CUtensorMap h, w, d_mn, h_mn, d_k, w_mn; };
+struct GradItem { int mt, nt, part; };  // row tile, (first) column tile, part of the contraction
+__device__ __forceinline__ GradItem grad_item(const GradParams& p, int cls, int item) {
+  if (cls == kClassD) return GradItem{item % p.logits.tiles_m, item / p.logits.tiles_m * p.logits.run, 0};
+  // (column tiles of one row tile beside each other: they share D)
+  const GradProduct& g = p.product[cls];
+  const int t = item / g.parts, mt = t / g.tiles_n;
+  return GradItem{mt, t - mt * g.tiles_n, item - t * g.parts};
+}
+struct GradMaps { CUtensorMap h, w, d_mn, h_mn, d_k, w_mn, d_out; };
 
 template <int NCTA, bool F8, bool KD, bool BF>
 __global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradParams p) {
@@ -566,10 +590,12 @@ __global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_con
   const int unit = blockIdx.x / NCTA, units = gridDim.x / NCTA;
   if (threadIdx.x < 6 && p.schedule.total[threadIdx.x < 2 ? kClassD : threadIdx.x < 4 ? kClassDw : kClassDh] > 0)  // (the others are not filled in)
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&maps.h + threadIdx.x)) : "memory");
-  __shared__ int s_item[kClasses][kListed];  // this pair's first items
-  for (int i = threadIdx.x; i < kClasses * kListed; i += kThreads)
-    if (i % kListed < p.schedule.quota[i / kListed][unit]) s_item[i / kListed][i % kListed] = scheduled_item(p.schedule, i / kListed, unit, units, i % kListed);
-  e.set_up(smem_raw, p.logits.ring);
+  __shared__ GradItem s_item[kClasses][kListed];  // this pair's first items
+  for (int i = threadIdx.x; i < kClasses * kListed; i += kThreads) {
+    const int cls = i / kListed, j = i % kListed;
+    if (j < p.schedule.quota[cls][unit]) s_item[cls][j] = grad_item(p, cls, scheduled_item(p.schedule, cls, unit, units, j));
+  }
+  e.set_up(smem_raw, p.logits.ring, true);
   // nothing above touches what the kernel before writes
   if (!p.logits.early || e.warp >= 2) asm volatile("griddepcontrol.wait;" ::: "memory");
   const LogitsParams& l = p.logits;
@@ -578,45 +604,33 @@ __global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_con
   auto each_item = [&](auto f) {
     for (int k = 0; k < kClasses && !timed_out; ++k) {
       const int cls = p.schedule.order[k], mine = p.schedule.quota[cls][unit];
-      for (int j = 0; j < mine && !timed_out; ++j) f(cls, j < kListed ? s_item[cls][j] : scheduled_item(p.schedule, cls, unit, units, j));
+      for (int j = 0; j < mine && !timed_out; ++j) f(cls, j < kListed ? s_item[cls][j] : grad_item(p, cls, scheduled_item(p.schedule, cls, unit, units, j)));
     }
   };
-  // item of a product -> part, row tile, column tile (column tiles of one row tile beside each other: they share D)
-  auto locate = [&](const GradProduct& g, int item, int& part, int& mt, int& nt) {
-    part = item % g.parts;
-    nt = item / g.parts;
-    mt = nt / g.tiles_n;
-    nt -= mt * g.tiles_n;
-    return min(g.part_kb, g.num_kb - part * g.part_kb);  // K blocks
-  };
+  auto part_kbs = [&](const GradProduct& g, int part) { return min(g.part_kb, g.num_kb - part * g.part_kb); };
   if (e.warp == 0) {
     if (e.lane == 0) {
       asm volatile("fence.proxy.async;" ::: "memory");  // the copies read what ordinary stores have written
-      each_item([&](int cls, int item) {
+      each_item([&](int cls, const GradItem& item) {
         if (cls == kClassD) {
-          const int mt = item % l.tiles_m, nt0 = item / l.tiles_m * l.run;
-          for (int nt = nt0; nt < min(nt0 + l.run, l.tiles_n) && !timed_out; ++nt)
-            timed_out = !e.produce(&maps.h, &maps.w, mt * Cfg<NCTA>::kTileM, nt * 2 * l.half_cols, l.box_rows, 2 * l.half_cols, 0, l.num_kb, false, false);
+          for (int nt = item.nt; nt < min(item.nt + l.run, l.tiles_n) && !timed_out; ++nt)
+            timed_out = !e.produce(&maps.h, &maps.w, item.mt * Cfg<NCTA>::kTileM, nt * 2 * l.half_cols, l.box_rows, 2 * l.half_cols, 0, l.num_kb, false, false);
         } else {
           const GradProduct& g = p.product[cls];
-          int part, mt, nt;
-          const int kbs = locate(g, item, part, mt, nt);
-          timed_out = cls == kClassDw ? !e.produce(&maps.d_mn, &maps.h_mn, mt * Cfg<NCTA>::kTileM, nt * kTN, kTM, kTN, part * g.part_kb, kbs, true, true)
-                                      : !e.produce(&maps.d_k, &maps.w_mn, mt * Cfg<NCTA>::kTileM, nt * kTN, kTM, kTN, part * g.part_kb, kbs, false, true);
+          const int m0 = item.mt * Cfg<NCTA>::kTileM, n0 = item.nt * kTN, kbs = part_kbs(g, item.part);
+          timed_out = cls == kClassDw ? !e.produce(&maps.d_mn, &maps.h_mn, m0, n0, kTM, kTN, item.part * g.part_kb, kbs, true, true)
+                                      : !e.produce(&maps.d_k, &maps.w_mn, m0, n0, kTM, kTN, item.part * g.part_kb, kbs, false, true);
         }
       });
       if (timed_out || *e.abort_flag) e.drain_copies();
     }
   } else if (e.warp == 1) {
     if (e.lane == 0 && e.rank == 0u) {
-      each_item([&](int cls, int item) {
+      each_item([&](int cls, const GradItem& item) {
         if (cls == kClassD) {
-          const int nt0 = item / l.tiles_m * l.run;
-          for (int nt = nt0; nt < min(nt0 + l.run, l.tiles_n) && !timed_out; ++nt) timed_out = !e.template multiply<F8>(l.num_kb, l.idesc, false, false);
+          for (int nt = item.nt; nt < min(item.nt + l.run, l.tiles_n) && !timed_out; ++nt) timed_out = !e.template multiply<F8>(l.num_kb, l.idesc, false, false);
         } else {
-          int part, mt, nt;
-          const int kbs = locate(p.product[cls], item, part, mt, nt);
-          timed_out = !e.template multiply<false>(kbs, p.idesc, cls == kClassDw, true);
+          timed_out = !e.template multiply<false>(part_kbs(p.product[cls], item.part), p.idesc, cls == kClassDw, true);
         }
       });
       if (timed_out || *e.abort_flag) e.drain_multiplies();
@@ -625,11 +639,12 @@ __global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_con
     const int half = (e.warp - 2) >> 2, quarter = e.warp & 3;
     const int own_row = static_cast<int>(e.rank) * kTM + quarter * 32 + e.lane;
     const LaneRow lane_row = e.staging();
+    uint32_t flip = 0;
     const float c2 = load_scale_after_wait(l.h_scale) * load_scale_after_wait(l.w_scale) * l.inv_temp * kLog2E;
     const float unit_d = reinterpret_cast<const volatile float*>(p.unit)[0], factor = reinterpret_cast<const volatile float*>(p.unit)[1];
-    each_item([&](int cls, int item) {
+    each_item([&](int cls, const GradItem& item) {
       if (cls == kClassD) {
-        const int row = item % l.tiles_m * Cfg<NCTA>::kTileM + own_row, nt0 = item / l.tiles_m * l.run;
+        const int row = item.mt * Cfg<NCTA>::kTileM + own_row, nt0 = item.nt;
         Targets<KD> target;
         target.start(l, row, half, l.col0 + static_cast<long long>(nt0) * 2 * l.half_cols);
         float2 coef = make_float2(0.f, 0.f);
@@ -650,6 +665,8 @@ __global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_con
             for (int i = 0; i < 32; ++i) v[i] = coef.x * exp2_approx(fmaf(__uint_as_float(r[i]), c2, -lse2));
             if (__any_sync(0xFFFFFFFFu, target.id < g0 + 32)) {
               if constexpr (KD) {
+                if (e.lane == 0) bulk_wait_read<0>();
+                __syncwarp();
                 lane_row.put(reinterpret_cast<const uint32_t*>(v));
                 while (target.id < g0 + 32) {
                   lane_row.at(static_cast<int>(target.id - g0)) -= coef.y * target.q;
@@ -667,48 +684,46 @@ __global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_con
             }
             uint32_t o[16];
             encode_vec<BF ? SCALIFY_BF16 : SCALIFY_F16, 32>(v, o);
-            if (row < l.n) {
-              char* dst = reinterpret_cast<char*>(l.D + static_cast<long long>(row) * l.ldd + c0);  // (rows are padded to whole chunks)
-              st_bytes<32>(dst, o);
-              st_bytes<32>(dst + 32, o + 8);
-            }
+            lane_row.store(o, &maps.d_out, c0 * 2, row - e.lane, flip);
           });
           e.release_accumulator();
         }
       } else {
         const GradProduct& g = p.product[cls];
-        int part, mt, nt;
-        locate(g, item, part, mt, nt);
         const float alpha = g.alpha * factor;
-        const int row = mt * Cfg<NCTA>::kTileM + own_row, n0 = nt * kTN + half * (kTN / 2);
+        const int row = item.mt * Cfg<NCTA>::kTileM + own_row, n0 = item.nt * kTN + half * (kTN / 2);
         const int mode = g.mode;
-        float* acc_row = g.acc + (static_cast<long long>(part) * g.M + row) * g.ld_acc + n0;  // (padded to whole chunks)
         char* out_row = static_cast<char*>(g.out) + (static_cast<long long>(row) * g.ldo + n0) * 2;
+        float* acc_row = g.acc + (static_cast<long long>(item.part) * g.M + row) * g.ld_acc + n0;  // (padded to whole chunks)
         if (!e.wait_accumulator()) { timed_out = true; return; }
         e.each_chunk(half, kTN / 2, row - e.lane < g.M ? g.N - n0 : 0, [&](uint32_t* r, int c) {
           float v[32];
 #pragma unroll
           for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
-          if (row < g.M) {
-            char* acc = reinterpret_cast<char*>(acc_row + c * 32);
-            if (mode >= kAccNext) {
-              uint32_t before[32];
+          char* acc = reinterpret_cast<char*>(acc_row + c * 32);
+          if (mode >= kAccNext && row < g.M) {
+            uint32_t before[32];
 #pragma unroll
-              for (int j = 0; j < 4; ++j) ld_bytes<32, false>(acc + j * 32, before + j * 8);
+            for (int j = 0; j < 4; ++j) ld_bytes<32, false>(acc + j * 32, before + j * 8);
 #pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] += __uint_as_float(before[i]);
-            }
-            if (mode == kAccFirst || mode == kAccNext) {
+            for (int i = 0; i < 32; ++i) v[i] += __uint_as_float(before[i]);
+          }
+          if (mode == kAccFirst || mode == kAccNext) {
+            if (row < g.M) {
 #pragma unroll
               for (int j = 0; j < 4; ++j) st_bytes<32>(acc + j * 32, reinterpret_cast<const uint32_t*>(v) + j * 8);
-            } else {
+            }
+          } else {
 #pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] *= alpha;
-              uint32_t o[16];
-              if (g.out_dt == SCALIFY_BF16) encode_vec<SCALIFY_BF16, 32>(v, o);
-              else encode_vec<SCALIFY_F16, 32>(v, o);
-              const int left = g.N - n0 - c * 32;
-              char* dst = out_row + c * 64;
+            for (int i = 0; i < 32; ++i) v[i] *= alpha;
+            uint32_t o[16];
+            if (g.out_dt == SCALIFY_BF16) encode_vec<SCALIFY_BF16, 32>(v, o);
+            else encode_vec<SCALIFY_F16, 32>(v, o);
+            // (straight from registers: where a tile is little but its store, the store engine would also have to fetch the next
+            // ones' operands; 256 and 100 rows, vocabulary 50257 and 115392: 89 and 139 us so, 106 and 168 through it)
+            const int left = g.N - n0 - c * 32;
+            char* dst = out_row + c * 64;
+            if (row < g.M) {
               if (left >= 32) {
                 st_bytes<32>(dst, o);
                 st_bytes<32>(dst + 32, o + 8);
@@ -723,6 +738,7 @@ __global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_con
         e.release_accumulator();
       }
     });
+    if (e.lane == 0) bulk_wait_all();  // every store of this warp has completed
   }
   if (timed_out) atomicOr(l.status, static_cast<uint32_t>(SCALIFY_DEV_TIMEOUT));
   e.tear_down();
@@ -1129,22 +1145,35 @@ struct PlanesParams {
 __global__ void __launch_bounds__(256) planes_kernel(const PlanesParams p) {
   asm volatile("griddepcontrol.launch_dependents;");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int vecs = (p.N + kVec - 1) / kVec;
+  const int vecs = (p.N + 3) / 4;
   const float alpha = p.alpha * *reinterpret_cast<const volatile float*>(p.unit + 1);
+  const long long plane = static_cast<long long>(p.M) * p.ld_acc;
   for (long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x; i < static_cast<long long>(p.M) * vecs; i += static_cast<long long>(gridDim.x) * 256) {
-    const int row = static_cast<int>(i / vecs), v = static_cast<int>(i - static_cast<long long>(row) * vecs);
-    float f[kVec] = {};
-#pragma unroll 4
-    for (int s = 0; s < p.planes; ++s) {
-      const float4* a = reinterpret_cast<const float4*>(p.acc + (static_cast<long long>(s) * p.M + row) * p.ld_acc + v * kVec);
-      const float4 x = __ldcg(a), y = __ldcg(a + 1);  // (rows are padded to whole vectors)
-      f[0] += x.x; f[1] += x.y; f[2] += x.z; f[3] += x.w; f[4] += y.x; f[5] += y.y; f[6] += y.z; f[7] += y.w;
-    }
+    const int row = static_cast<int>(i / vecs), c = static_cast<int>(i - static_cast<long long>(row) * vecs) * 4;
+    const float* a = p.acc + row * p.ld_acc + c;  // (rows are padded to whole vectors)
+    float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+    constexpr int kBatch = 8;  // loads in flight: few rows are a matter of latency
+    for (int s0 = 0; s0 < p.planes; s0 += kBatch) {
+      float4 v[kBatch];
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) f[e] *= alpha;
-    char* out = static_cast<char*>(p.out) + static_cast<long long>(row) * p.ldo * 2;
-    if (p.out_dt == SCALIFY_BF16) store_vec<SCALIFY_BF16>(out, v, p.N - v * kVec, f);
-    else store_vec<SCALIFY_F16>(out, v, p.N - v * kVec, f);
+      for (int s = 0; s < kBatch; ++s)
+        v[s] = s0 + s < p.planes ? __ldcg(reinterpret_cast<const float4*>(a + (s0 + s) * plane)) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int s = 0; s < kBatch; ++s) { f.x += v[s].x; f.y += v[s].y; f.z += v[s].z; f.w += v[s].w; }
+    }
+    const float x[4] = {f.x * alpha, f.y * alpha, f.z * alpha, f.w * alpha};
+    const long long o = row * p.ldo + c;
+    if (c + 4 <= p.N) {
+      uint32_t w[2];
+      if (p.out_dt == SCALIFY_BF16) encode_vec<SCALIFY_BF16, 4>(x, w);
+      else encode_vec<SCALIFY_F16, 4>(x, w);
+      st_raw<8>(static_cast<uint16_t*>(p.out) + o, w);
+    } else {
+      for (int e = 0; e < p.N - c; ++e) {
+        if (p.out_dt == SCALIFY_BF16) store_elem<SCALIFY_BF16>(p.out, o + e, x[e]);
+        else store_elem<SCALIFY_F16>(p.out, o + e, x[e]);
+      }
+    }
   }
 }
 
@@ -1262,9 +1291,9 @@ Layout layout_of(long long n, long long vocab, long long d, int es, int k, bool 
   return l;
 }
 
-template <int NCTA, bool KD, class K>
+template <int NCTA, bool STAGING, class K>
 int unit_config(K kernel, DeviceOnce& once, long long items, cudaStream_t st, cudaLaunchConfig_t* cfg, cudaLaunchAttribute* attrs, int* units) {
-  constexpr size_t kBytes = Cfg<NCTA>::kSmem + (KD ? Cfg<NCTA>::kStaging : 0);
+  constexpr size_t kBytes = Cfg<NCTA>::kSmem + (STAGING ? Cfg<NCTA>::kStaging : 0);
   int most = 0;  // CTAs (pairs) that fit the GPU
   const int rc = device_once(once, &most, [&](int* v) {
     SCALIFY_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kBytes)));
@@ -1378,7 +1407,7 @@ int launch_grad_variant(const GradMaps& m, GradParams& p, const long long (&item
   cudaLaunchConfig_t cfg;
   cudaLaunchAttribute attrs[2];
   int units = 0;
-  const int rc = unit_config<NCTA, KD>(kernel, once, items[0] + items[1] + items[2], st, &cfg, attrs, &units);
+  const int rc = unit_config<NCTA, true>(kernel, once, items[0] + items[1] + items[2], st, &cfg, attrs, &units);
   if (rc) return rc;
   fill_schedule(p.schedule, items, cost, units);
   SCALIFY_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, m, p));
@@ -1401,6 +1430,11 @@ int map_of(CUtensorMap* m, const void* base, long long rows, long long cols, lon
   const long long bytes = rows > 1 ? ld * es : pad_to(cols * es, 16);
   return make_byte_map(m, base, static_cast<uint64_t>(cols) * es, static_cast<uint64_t>(rows), 1, static_cast<uint64_t>(bytes),
                        static_cast<uint64_t>(bytes) * rows, kRowBytes, box_rows);
+}
+
+// D [rows][cols], for stores of 32 rows x 32 columns (a ragged last 16 bytes is written whole: D's rows are padded)
+int d_store_map(CUtensorMap* m, const void* base, long long rows, long long cols, long long ld) {
+  return make_byte_map(m, base, static_cast<uint64_t>(cols) * 2, static_cast<uint64_t>(rows), 1, static_cast<uint64_t>(ld) * 2, static_cast<uint64_t>(ld) * 2 * rows, 64, 32);
 }
 
 int prepare_teacher(const LinearLossArgs& a, const Layout& l, char* ws, cudaStream_t st) {
@@ -1560,7 +1594,7 @@ int launch_linear_loss_bwd(const LinearLossArgs& a, void* workspace, cudaStream_
   GradMaps m = {};
   LogitsParams& p = g.logits;
   p = logits_params(a, l, ws);
-  p.lse = a.lse; p.coef = c.coef; p.ldd = l.ldd;
+  p.lse = a.lse; p.coef = c.coef;
   const int ctas = ctas_of(a.n), n_tiles = p.tiles_m, d_tiles = static_cast<int>((a.d + kTN - 1) / kTN);
   GradProduct &dw = g.product[kClassDw], &dh = g.product[kClassDh];
   dw.N = dh.N = a.d;
@@ -1588,16 +1622,15 @@ int launch_linear_loss_bwd(const LinearLossArgs& a, void* workspace, cudaStream_
       p.tiles_n = static_cast<int>((cols + l.width - 1) / l.width);
       // distillation looks up a row's place in its entries once per item: longer ones where there are enough
       p.run = a.k > 0 ? run_length(n_tiles, p.tiles_n, 4, 8 * units_of(a.n)) : 1;
-      p.D = reinterpret_cast<uint16_t*>(ws + l.D[i & 1]);
       items[kClassD] = static_cast<long long>(n_tiles) * ((p.tiles_n + p.run - 1) / p.run);
       cost[kClassD] = p.run * (p.num_kb + kTileCost);
-      rc = map_of(&m.w, static_cast<const char*>(a.W) + v0 * a.w_ld * es, cols, a.d, a.w_ld, es, l.width / ctas);
+      rc = d_store_map(&m.d_out, ws + l.D[i & 1], a.n, cols, l.ldd);
+      if (!rc) rc = map_of(&m.w, static_cast<const char*>(a.W) + v0 * a.w_ld * es, cols, a.d, a.w_ld, es, l.width / ctas);
     }
     if (!rc && i > 0) {
       const long long v0 = (i - 1) * l.piece, cols = a.vocab - v0 < l.piece ? a.vocab - v0 : l.piece;
       const uint16_t* D = reinterpret_cast<const uint16_t*>(ws + l.D[(i - 1) & 1]);
       dw.M = static_cast<int>(cols);
-      dw.out = a.dW ? static_cast<char*>(a.dW) + v0 * a.dw_ld * 2 : nullptr;
       dh.num_kb = static_cast<int>((cols + kK16 - 1) / kK16);
       dh.part_kb = (dh.num_kb + l.parts - 1) / l.parts;
       dh.parts = (dh.num_kb + dh.part_kb - 1) / dh.part_kb;
@@ -1606,6 +1639,7 @@ int launch_linear_loss_bwd(const LinearLossArgs& a, void* workspace, cudaStream_
       if (a.dH) items[kClassDh] = static_cast<long long>(n_tiles) * d_tiles * dh.parts;
       cost[kClassDw] = dw.num_kb + kTileCost;
       cost[kClassDh] = dh.part_kb + kTileCost;
+      dw.out = a.dW ? static_cast<char*>(a.dW) + v0 * a.dw_ld * 2 : nullptr;
       rc = map_of(&m.d_mn, D, a.n, cols, l.ldd, 2, kK16);
       if (!rc) rc = map_of(&m.d_k, D, a.n, cols, l.ldd, 2, kTM);
       if (!rc) rc = map_of(&m.w_mn, w16 + v0 * w16_ld * 2, cols, a.d, w16_ld, 2, kK16);
@@ -1616,9 +1650,9 @@ int launch_linear_loss_bwd(const LinearLossArgs& a, void* workspace, cudaStream_
   if (!a.dH || l.pieces > 1 || dh.parts == 1) return SCALIFY_OK;
   PlanesParams q = {};
   q.acc = dh.acc; q.ld_acc = dh.ld_acc; q.planes = dh.parts;
-  q.M = dh.M; q.N = dh.N; q.out = dh.out; q.ldo = dh.ldo; q.out_dt = dh.out_dt;
+  q.M = dh.M; q.N = dh.N; q.out = a.dH; q.ldo = a.dh_ld; q.out_dt = dh.out_dt;
   q.alpha = dh.alpha; q.unit = g.unit;
-  const long long blocks = (a.n * ((a.d + kVec - 1) / kVec) + 255) / 256, most = 8ll * sm_count();
+  const long long blocks = (a.n * ((a.d + 3) / 4) + 255) / 256, most = 8ll * sm_count();
   return launch_small(planes_kernel, blocks < most ? blocks : most, 256, q, st);
 }
 
