@@ -758,19 +758,39 @@ struct TeacherParams {
   Entry* entries; int2* counts; float2* sums;  // sums: Q, sum q log q
   uint32_t* status;
 };
-constexpr int kTeacherWarps = 4;
 constexpr int kMaxBins = 256;
-template <int kPer>  // entries per lane
-__global__ void __launch_bounds__(32 * kTeacherWarps) teacher_kernel(const TeacherParams p) {
-  __shared__ __align__(16) uint32_t s_key[kTeacherWarps][32 * kPer];
-  __shared__ int s_bin[kTeacherWarps][2 * kMaxBins];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long row = static_cast<long long>(blockIdx.x) * kTeacherWarps + warp;
+// TEAM warps share a row, kPer entries per lane; a block takes one row of several warps or four rows of one.
+template <int kPer, int TEAM>
+__global__ void __launch_bounds__(TEAM == 1 ? 128 : 32 * TEAM) teacher_kernel(const TeacherParams p) {
+  constexpr int kRows = TEAM == 1 ? 4 : 1;
+  __shared__ uint64_t s_entry[kRows][32 * kPer * TEAM];  // key, then place, bin after bin
+  __shared__ int s_bin[kRows][2 * kMaxBins];
+  __shared__ float s_part[4][TEAM];
+  __shared__ int s_count[2][TEAM];
+  const int warp = TEAM == 1 ? threadIdx.x >> 5 : 0, lane = threadIdx.x & 31;  // (warp: the row of the block)
+  const int member = TEAM == 1 ? 0 : threadIdx.x >> 5, first = member * 32 + lane;
+  const long long row = static_cast<long long>(blockIdx.x) * kRows + warp;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;");  // (behind the wait: a dependent may read what was there before this kernel)
   if (row >= p.n) return;
+  auto sync = [] {
+    if constexpr (TEAM == 1) __syncwarp();
+    else __syncthreads();
+  };
+  // over the row, in all its threads
+  auto row_sum = [&](float x, int slot) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
+    if constexpr (TEAM > 1) {
+      if (lane == 0) s_part[slot][member] = x;
+      __syncthreads();
+      x = 0.f;
+      for (int i = 0; i < TEAM; ++i) x += s_part[slot][i];
+    }
+    return x;
+  };
   const float scale = load_scale_after_wait(p.t_scale);
-  if (row == 0 && lane == 0 && !is_pow2_scale(scale)) atomicOr(p.status, static_cast<uint32_t>(SCALIFY_DEV_BAD_SCALE));
+  if (row == 0 && first == 0 && !is_pow2_scale(scale)) atomicOr(p.status, static_cast<uint32_t>(SCALIFY_DEV_BAD_SCALE));
   const float f = scale * p.inv_temp;
   float t[kPer];
   uint32_t key[kPer];
@@ -779,7 +799,7 @@ __global__ void __launch_bounds__(32 * kTeacherWarps) teacher_kernel(const Teach
   long long id[kPer];
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {  // (all loads at once)
-    const int i = j * 32 + lane;
+    const int i = j * 32 * TEAM + first;
     id[j] = i < p.k ? p.ids[row * p.k + i] : p.padding_id;
     const long long at = row * p.t_ld + i;
     t[j] = i >= p.k ? 0.f
@@ -788,7 +808,7 @@ __global__ void __launch_bounds__(32 * kTeacherWarps) teacher_kernel(const Teach
   }
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {
-    const int i = j * 32 + lane;
+    const int i = j * 32 * TEAM + first;
     const bool known = id[j] >= 0 && id[j] < p.vocab, wanted = i < p.k && id[j] != p.padding_id;
     const float x = t[j] * f;
     bad = bad || (wanted && !known);
@@ -799,7 +819,6 @@ __global__ void __launch_bounds__(32 * kTeacherWarps) teacher_kernel(const Teach
       key[j] = static_cast<uint32_t>(id[j]) | (static_cast<uint32_t>(id[j]) / p.half_cols & 1u) << 30;
       top = x > top || x != x ? x : top;
     }
-    s_key[warp][i] = key[j];  // (behind the last one: larger than any)
   }
   if (bad) atomicOr(p.status, static_cast<uint32_t>(SCALIFY_DEV_BAD_INDEX));
   float norm;
@@ -808,24 +827,29 @@ __global__ void __launch_bounds__(32 * kTeacherWarps) teacher_kernel(const Teach
   } else {
 #pragma unroll
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    if constexpr (TEAM > 1) {
+      if (lane == 0) s_part[0][member] = top;
+      __syncthreads();
+      for (int i = 0; i < TEAM; ++i) top = fmaxf(top, s_part[0][i]);
+    }
     float s = 0.f;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) s += key[j] != 0xFFFFFFFFu ? expf(t[j] - top) : 0.f;
-#pragma unroll
-    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-    norm = logf(s) + top;
+    norm = logf(row_sum(s, 1)) + top;
   }
-  for (int i = lane; i < 2 * p.bins; i += 32) s_bin[warp][i] = 0;
-  __syncwarp();
+  for (int i = first; i < 2 * p.bins; i += 32 * TEAM) s_bin[warp][i] = 0;
+  sync();
+  // counted by bins; a bin's entries come after those of the bins before it, in any order at first
+  int bin[kPer], slot[kPer];
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {
-    if (key[j] == 0xFFFFFFFFu) continue;
     const uint32_t block = (key[j] & 0x3FFFFFFFu) / static_cast<uint32_t>(p.half_cols);  // 2 tile + half
-    atomicAdd(&s_bin[warp][(block & 1u) * p.bins + (block >> 1) / p.bin_tiles], 1);
+    bin[j] = static_cast<int>((block & 1u) * p.bins + (block >> 1) / p.bin_tiles);
+    if (key[j] != 0xFFFFFFFFu) slot[j] = atomicAdd(&s_bin[warp][bin[j]], 1);
   }
-  __syncwarp();
+  sync();
   int begin = 0;
-  for (int i0 = 0; i0 < 2 * p.bins; i0 += 32) {
+  for (int i0 = 0; i0 < 2 * p.bins && member == 0; i0 += 32) {
     const int i = i0 + lane, mine = i < 2 * p.bins ? s_bin[warp][i] : 0;
     int upto = mine;
 #pragma unroll
@@ -833,9 +857,18 @@ __global__ void __launch_bounds__(32 * kTeacherWarps) teacher_kernel(const Teach
       const int u = __shfl_up_sync(0xFFFFFFFFu, upto, o);
       if (lane >= o) upto += u;
     }
-    if (i < 2 * p.bins) p.table[row * 2 * p.bins + i] = static_cast<uint16_t>(begin + upto - mine);
+    if (i < 2 * p.bins) {
+      p.table[row * 2 * p.bins + i] = static_cast<uint16_t>(begin + upto - mine);
+      s_bin[warp][i] = (begin + upto - mine) << 16 | mine;
+    }
     begin += __shfl_sync(0xFFFFFFFFu, upto, 31);
   }
+  sync();
+#pragma unroll
+  for (int j = 0; j < kPer; ++j)
+    if (key[j] != 0xFFFFFFFFu)
+      s_entry[warp][(s_bin[warp][bin[j]] >> 16) + slot[j]] = static_cast<uint64_t>(key[j]) << 32 | static_cast<uint32_t>(j * 32 * TEAM + first);
+  sync();
   int there = 0, even = 0;
   float mass = 0.f, neg = 0.f;
   Entry* out = p.entries + row * p.k;
@@ -847,28 +880,23 @@ __global__ void __launch_bounds__(32 * kTeacherWarps) teacher_kernel(const Teach
     const float lq = t[j] - norm, q = ok ? expf(lq) : 0.f;
     mass += q;
     neg += ok && q != 0.f ? q * lq : 0.f;
-    // how many go before it: the smaller keys, and equal ones with a smaller place
-    int before = 0;
-#pragma unroll (kPer <= 2 ? kPer : 1)
-    for (int jm = 0; jm < kPer; ++jm) {
-      const uint4* others = reinterpret_cast<const uint4*>(s_key[warp] + jm * 32);
-      const uint32_t limit = key[j] + (jm < j ? 1u : 0u);
-#pragma unroll
-      for (int m = 0; m < 8; ++m) {
-        const uint4 o = others[m];
-        before += (o.x < limit) + (o.y < limit) + (o.z < limit) + (o.w < limit);
-      }
+    if (ok) {  // its place within the bin: by id, equal ones by place
+      const uint64_t mine = static_cast<uint64_t>(key[j]) << 32 | static_cast<uint32_t>(j * 32 * TEAM + first);
+      const int b = s_bin[warp][bin[j]], begins = b >> 16, many = b & 0xFFFF;
+      int before = begins;
+      for (int m = 0; m < many; ++m) before += s_entry[warp][begins + m] < mine;
+      out[before] = Entry{static_cast<int>(key[j] & 0x3FFFFFFFu), q};
     }
-    // (equal ones of its own 32: few, if any)
-    for (uint32_t same = __match_any_sync(0xFFFFFFFFu, key[j]) & ((1u << lane) - 1u); same && ok; same &= same - 1u) ++before;
-    if (ok) out[before] = Entry{static_cast<int>(key[j] & 0x3FFFFFFFu), q};
   }
-#pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    mass += __shfl_xor_sync(0xFFFFFFFFu, mass, o);
-    neg += __shfl_xor_sync(0xFFFFFFFFu, neg, o);
+  mass = row_sum(mass, 2);
+  neg = row_sum(neg, 3);
+  if constexpr (TEAM > 1) {
+    if (lane == 0) { s_count[0][member] = even; s_count[1][member] = there; }
+    __syncthreads();
+    even = there = 0;
+    for (int i = 0; i < TEAM; ++i) { even += s_count[0][i]; there += s_count[1][i]; }
   }
-  if (lane == 0) {
+  if (first == 0) {
     p.counts[row] = make_int2(even, there);
     p.sums[row] = make_float2(mass, neg);
   }
@@ -1451,11 +1479,11 @@ int prepare_teacher(const LinearLossArgs& a, const Layout& l, char* ws, cudaStre
   t.counts = reinterpret_cast<int2*>(ws + l.counts);
   t.sums = reinterpret_cast<float2*>(ws + l.sums);
   t.status = ws_view(ws).status;
-  const long long blocks = (a.n + kTeacherWarps - 1) / kTeacherWarps;
-  if (a.k <= 32) return launch_small(teacher_kernel<1>, blocks, 32 * kTeacherWarps, t, st);
-  if (a.k <= 64) return launch_small(teacher_kernel<2>, blocks, 32 * kTeacherWarps, t, st);
-  if (a.k <= 128) return launch_small(teacher_kernel<4>, blocks, 32 * kTeacherWarps, t, st);
-  return launch_small(teacher_kernel<kLossMaxEntries / 32>, blocks, 32 * kTeacherWarps, t, st);
+  // (one warp per row up to 64 entries, four or eight beyond: one row of 200 takes 7 us, with one warp 22)
+  if (a.k <= 32) return launch_small(teacher_kernel<1, 1>, (a.n + 3) / 4, 128, t, st);
+  if (a.k <= 64) return launch_small(teacher_kernel<2, 1>, (a.n + 3) / 4, 128, t, st);
+  if (a.k <= 128) return launch_small(teacher_kernel<1, 4>, a.n, 128, t, st);
+  return launch_small(teacher_kernel<1, 8>, a.n, 256, t, st);
 }
 
 // (whole: a launch with tiles of the products)
