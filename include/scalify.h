@@ -582,6 +582,8 @@ int scalify_scaled_cross_entropy(const scalify_array* logits, int64_t n_classes,
  *   (fp64, fixed order) over the number of rows that have entries; 0 if none has.
  *   0 <= n <= 2^24, 1 <= vocab <= 2^24, 1 <= d <= 65536; z_loss >= 0 finite; temperature and its reciprocal normal numbers.
  * The same call gives the same bits every time.  Infinities and NaN in H or W go through as the formulas have them.
+ * Accuracy: the logits are fp32 sums of exact products on the tensor cores, which truncate (d = 4096, 16-bit operands: loss and
+ * lse within 5e-7 of their size in the norm; d = 768, FP8: 7e-8).
  *
  * Gradients of sum_t g[t] loss[t] with respect to the VALUES of H and W:
  *   D[t,v] = g[t] / T ((Q[t] + 2 z_loss lse[t]) p[t,v] - q[t,v]),  Q = sum q;      dH = D W,  dW = D^T H
@@ -590,13 +592,14 @@ int scalify_scaled_cross_entropy(const scalify_array* logits, int64_t n_classes,
  *   grad: [n] F32, contiguous, or NULL: the gradient of `mean`, g = 1 / rows with entries, g_s = 1/n rounded down to a power
  *   of two (as scalify_scaled_cross_entropy).  lse: of the forward call on the same arguments.
  *   dH: [n, d], dW: [vocab, d], F16 or BF16 each; either may be NULL (a frozen layer).  Every row is written.
- * The logits are computed again in pieces of the vocabulary (the workspace holds D of one piece, at most 64 MiB or 256
- * columns, and the fp32 sums of dH).  D is rounded to BF16 (BF16 operands) or to FP16 at a power-of-two scale (the others;
+ * The logits are computed again in pieces of the vocabulary (the workspace holds D of two pieces, each at most 128 MiB or 256
+ * columns, the fp32 sums of dH, and FP16 copies of FP8 operands).  D is rounded to BF16 (BF16 operands) or to FP16 at a power-of-two scale (the others;
  * FP8 operands are widened to FP16 exactly), half a step of relative error each; sums are fp32.
  * Errors: NULL, DTYPE, SHAPE, ALIGNMENT, VALUE, ALIAS (an output over an input or another output), WORKSPACE.
  */
 /* Workspace of these calls (shapes and dtypes of H and W only; k = 0: cross entropy; >= 4096; 0 for arguments that the calls
- * refuse).  A forward and a backward call on one stream may share one of the larger size; nothing is kept in it. */
+ * refuse).  backward != 0: enough for the forward call too, so that a step's calls on one stream share one workspace; nothing
+ * is kept in it between calls. */
 size_t scalify_linear_loss_workspace_bytes(const scalify_array* H, const scalify_array* W, int k, int backward);
 int scalify_scaled_linear_cross_entropy(const scalify_array* H, const scalify_array* W, const int64_t* ids, int64_t padding_id,
                                         float z_loss, float* loss, float* lse, float* mean, void* workspace,
