@@ -573,7 +573,8 @@ int scalify_scaled_cross_entropy(const scalify_array* logits, int64_t n_classes,
  * With teacher_lse (of the teacher's WHOLE row, at this temperature: scalify_scaled_top_logits gives it) q are the teacher's
  * own probabilities, and the mass outside the k entries takes no part.  No factor T^2 is applied.
  *
- *   H: [n, d], W: [vocab, d] (a tied embedding's layout): both F16, both BF16, or each E4M3 or E5M2.  Rows may be strided.
+ *   H: [n, d], W: [vocab, d] (a tied embedding's layout): both F16, both BF16, or each E4M3 or E5M2.  Rows may be strided, but
+ *   do not overlap (no broadcast).
  *   ids: DEVICE int64, [n] or [n, k] contiguous.  An entry equal to padding_id (INT64_MIN: none) is left out; so is any
  *   other outside [0, vocab), which also sets SCALIFY_DEV_BAD_INDEX; so is a teacher's logit of -inf.  The same place twice
  *   counts twice.  A row without entries has loss 0 and no gradient.
@@ -581,7 +582,8 @@ int scalify_scaled_cross_entropy(const scalify_array* logits, int64_t n_classes,
  *   loss, lse: DEVICE fp32 [n] (lse of every row; the gradient needs it).  mean: optional DEVICE word, the sum of the losses
  *   (fp64, fixed order) over the number of rows that have entries; 0 if none has.
  *   0 <= n <= 2^24, 1 <= vocab <= 2^24, 1 <= d <= 65536; z_loss >= 0 finite; temperature and its reciprocal normal numbers.
- * The same call gives the same bits every time.  Infinities and NaN in H or W go through as the formulas have them.
+ * The same call gives the same bits every time.  Infinities and NaN in H or W go through as the formulas have them
+ * (a row of H without entries, too, has to be finite: its gradient 0 is multiplied with it for dW).
  * Accuracy: the logits are fp32 sums of exact products on the tensor cores, which truncate (d = 4096, 16-bit operands: loss and
  * lse within 5e-7 of their size in the norm; d = 768, FP8: 7e-8).
  *

@@ -465,7 +465,7 @@ __global__ void __launch_bounds__(kThreads, 1) logits_kernel(const __grid_consta
             if constexpr (KD) {
               lane_row.put(r);
               while (target.id < c0 + 32ll) {
-                dot = fmaf(target.q, lane_row.at(target.id - c0), dot);
+                if (target.q != 0.f) dot = fmaf(target.q, lane_row.at(target.id - c0), dot);  // (0 times -inf is nothing)
                 target.advance();
               }
               __syncwarp();
@@ -1533,9 +1533,12 @@ int launch_linear_loss(const LinearLossArgs& a, void* workspace, cudaStream_t st
     if (a.mean) SCALIFY_CUDA_TRY(cudaMemsetAsync(a.mean, 0, sizeof(float), st));
     return SCALIFY_OK;
   }
-  int rc = prepare_teacher(a, l, ws, st);
-  if (rc) return rc;
   LogitsParams p = logits_params(a, l, ws);
+  CUtensorMap mh, mw;
+  int rc = map_of(&mh, a.H, a.n, a.d, a.h_ld, es, p.box_rows);
+  if (!rc) rc = map_of(&mw, a.W, a.vocab, a.d, a.w_ld, es, l.width / ctas_of(a.n));
+  if (!rc) rc = prepare_teacher(a, l, ws, st);
+  if (rc) return rc;
   p.early = a.k > 0;  // (after the teacher kernel)
   p.cols = static_cast<int>(a.vocab);
   p.tiles_n = static_cast<int>((a.vocab + l.width - 1) / l.width);
@@ -1544,12 +1547,7 @@ int launch_linear_loss(const LinearLossArgs& a, void* workspace, cudaStream_t st
   p.partial = reinterpret_cast<float2*>(ws + l.partial);
   p.dot = reinterpret_cast<float*>(ws + l.dot);
   p.ld_part = l.ld_part;
-  CUtensorMap mh, mw;
-  rc = map_of(&mh, a.H, a.n, a.d, a.h_ld, es, p.box_rows);
-  if (!rc) rc = map_of(&mw, a.W, a.vocab, a.d, a.w_ld, es, l.width / ctas_of(a.n));
-  if (!rc) {
-    rc = ctas_of(a.n) == 2 ? launch_logits<2>(es == 1, a.k > 0, mh, mw, p, st) : launch_logits<1>(es == 1, a.k > 0, mh, mw, p, st);
-  }
+  rc = ctas_of(a.n) == 2 ? launch_logits<2>(es == 1, a.k > 0, mh, mw, p, st) : launch_logits<1>(es == 1, a.k > 0, mh, mw, p, st);
   if (rc) return rc;
   JoinParams j = {};
   j.n = a.n; j.vocab = a.vocab; j.slots = l.slots;

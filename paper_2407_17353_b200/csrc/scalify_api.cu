@@ -1387,6 +1387,7 @@ int check_output_layer(const scalify_array* H, const scalify_array* W, LinearLos
   if (H->ndim != 2 || W->ndim != 2 || H->shape[1] != W->shape[1]) return SCALIFY_ERR_SHAPE;
   const int64_t n = H->shape[0], vocab = W->shape[0], d = W->shape[1];
   if (n < 0 || n > kLossMaxRows || vocab < 1 || vocab > kLossMaxVocab || d < 1 || d > kLossMaxDim) return SCALIFY_ERR_SHAPE;
+  if (!rows_apart(n, d, H->stride[0]) || !rows_apart(vocab, d, W->stride[0])) return SCALIFY_ERR_SHAPE;  // (the operand copies want strides)
   a->H = H->data; a->h_dt = H->dtype; a->h_ld = H->stride[0]; a->h_scale = H->scale;
   a->W = W->data; a->w_dt = W->dtype; a->w_ld = W->stride[0]; a->w_scale = W->scale;
   a->n = n; a->vocab = vocab; a->d = static_cast<int>(d);

@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) top_logits_kernel(con
   const long long row = blockIdx.x;
   const char* x = static_cast<const char*>(p.X) + row * p.ld * ElemBytes<DT>::v;
   const int vocab = static_cast<int>(p.vocab), vecs = (vocab + kVec - 1) / kVec;
-  const float c2 = load_scale_after_wait(p.x_scale) * p.inv_temp * 1.4426950408889634f;
+  const float scale = load_scale_after_wait(p.x_scale) * p.inv_temp, c2 = scale * 1.4426950408889634f;
   // ---- first pass: the thread's maximum and sum; the maxima of its vectors, `per` vectors to a slot
   const int turns = (vecs + THREADS - 1) / THREADS, per = (turns + kSlots - 1) / kSlots;
   float top = -INFINITY, sum = 0.f;  // the sum is relative to top * c2
@@ -160,6 +160,11 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) top_logits_kernel(con
         if (t0 + j >= turns) break;
         float f[kVec];
         decode_vec<DT, kVec>(w[j], f);
+        if (fabsf(shift) > 1024.f) {  // (rows of the type's lowest value and the like: its rounding would count, so differences first)
+#pragma unroll
+          for (int i = 0; i < kVec; ++i) s.x += ex2((f[i] - top) * c2);
+          continue;
+        }
 #pragma unroll
         for (int i = 0; i < kVec; i += 2) {
           const float2 y = fma2(make_float2(f[i], f[i + 1]), make_float2(c2, c2), make_float2(shift, shift));
@@ -214,7 +219,7 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) top_logits_kernel(con
     s *= ex2((m - (most == -INFINITY ? 0.f : most)) * c2);
 #pragma unroll
     for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-    if (lane == 0) p.lse[row] = (most * c2 + log2f(s)) * 0.6931471805599453f;
+    if (lane == 0) p.lse[row] = fmaf(most, scale, logf(s));
   }
   __syncthreads();
   const uint32_t bound = s_bound;

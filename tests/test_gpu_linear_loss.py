@@ -177,6 +177,24 @@ def test_masked_teacher_logits():
     check(H, W, ids, T=T, temp=1.0)
 
 
+def test_a_class_that_is_ruled_out_and_has_no_mass():
+    H, W = layer(64, 300, 64, BF16)
+    H = H.abs() + 0.5
+    W[9] = -INF                                          # every row's logit 9 is -inf
+    T = torch.randn(64, 8, device="cuda", generator=gen(1))
+    T[:, 2] = -3e30                                      # and the teacher gives it no mass
+    ids = torch.rand(64, 300, generator=gen(5), device="cuda").argsort(1)[:, :8].contiguous()
+    ids[ids == 9] = 10
+    ids[:, 2] = 9
+    Hs, Ws, Ts = sc.ScaledTensor.make(H, 0.5), sc.ScaledTensor.make(W, 2.0 ** -3), sc.ScaledTensor.make(T, 0.5)
+    loss, lse = torch.empty(64, device="cuda"), torch.empty(64, device="cuda")
+    wsp = sc.Workspace(sc.scalify_linear_loss_workspace_bytes(Hs, Ws, k=8))
+    sc.scalify_scaled_linear_distill(Hs, Ws, Ts, ids, loss, lse, wsp)
+    W[9] = 0.0
+    want = pl.linear_loss(H, 0.5, torch.cat([W[:9], W[10:]]), 2.0 ** -3, torch.where(ids == 9, -1, ids - (ids > 9).long()), -1, T.double() * 0.5)
+    assert bool(((loss.double() - want["loss"]).abs() <= want["e_loss"]).all())
+
+
 def test_no_rows():
     W = layer(1, 50, 24, BF16)[1]
     H = torch.empty(0, 24, dtype=BF16, device="cuda")

@@ -18,6 +18,20 @@ def test_long_batches(n, vocab, d):
     check(H, W, ids_of(n, vocab), out=F16, grad=torch.randn(n, generator=gen(1), device="cuda"))
 
 
+@pytest.mark.parametrize("n,k", [(5, 0), (120, 0), (120, 30)])
+def test_large_vocabularies(n, k):
+    """Single-CTA tiles over several pieces, more tiles than the entries' table has bins."""
+    vocab, d = 600011, 16
+    H, W = layer(n, vocab, d, F16)
+    if k:
+        T = torch.randn(n, 32, generator=gen(3), device="cuda")[:, :k]
+        ids = torch.randint(0, vocab, (n, k), generator=gen(4), device="cuda")
+        ids[:, ::3] = torch.randint(0, 3000, (n, k // 3), generator=gen(5), device="cuda")   # many in few bins
+        check(H, W, ids, T=T, temp=2.0, out=F16)
+    else:
+        check(H, W, ids_of(n, vocab), out=F16)
+
+
 def test_weights_past_2_31_elements():
     n, vocab, d = 70, 70003, 32768
     assert vocab * d > 1 << 31

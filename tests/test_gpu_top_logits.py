@@ -73,6 +73,25 @@ def test_infinities_nan_and_lowest_values(dt):
         check(X, k, s=1.0)
 
 
+@pytest.mark.parametrize("dt", [BF16, F16, F32])
+def test_rows_of_the_lowest_value(dt):
+    """What an additive mask leaves of a row: the lowest finite value throughout, or but for one place; and the largest."""
+    low = torch.finfo(dt).min
+    X = torch.full((5, 5000), low, device="cuda", dtype=dt)
+    X[1, 4321] = 2.0
+    X[2] = -low
+    X[3, ::2] = low / 2
+    X[4, 7:] = -INF
+    V, ids = sc.ScaledTensor.empty((5, 8), dt), torch.zeros(5, 8, dtype=torch.int64, device="cuda")
+    lse = torch.zeros(5, device="cuda")
+    for temp in (1.0, 2.0):
+        sc.scalify_scaled_top_logits(sc.ScaledTensor.make(X, 1.0), V, ids, lse=lse, temperature=temp)
+        want, places = pl.top_logits(X, 8)
+        assert torch.equal(V.data, want) and torch.equal(ids, places)
+        ref = torch.logsumexp(X.double() / temp, 1)
+        assert bool(((lse.double() - ref).abs() <= 2.0 ** -22 * ref.abs() + 2.0 ** -18).all())
+
+
 def test_subnormal_and_huge_values():
     for dt in (BF16, F16, F32):
         tiny = torch.finfo(dt).smallest_normal

@@ -51,6 +51,7 @@ def test_operands(call):
     assert call(H=arr(1, B, (4, 64), offset=8)) == ALIGN
     assert call(H=arr(1, B, (4, 64), (68, 1))) == ALIGN
     assert call(W=arr(2, B, (100, 64), (64, 2))) == ALIGN
+    assert call(H=arr(1, B, (4, 64), (0, 1))) == SHAPE and call(W=arr(2, B, (100, 64), (56, 1))) == SHAPE   # overlapping rows
     assert call(ws=None) == WORKSPACE and call(nb=4095) == WORKSPACE and call(ws=WS + 128) == WORKSPACE
 
 
