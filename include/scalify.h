@@ -595,8 +595,9 @@ int scalify_scaled_cross_entropy(const scalify_array* logits, int64_t n_classes,
  *   of two (as scalify_scaled_cross_entropy).  lse: of the forward call on the same arguments.
  *   dH: [n, d], dW: [vocab, d], F16 or BF16 each; either may be NULL (a frozen layer).  Every row is written.
  * The logits are computed again in pieces of the vocabulary (the workspace holds D of two pieces, each at most 128 MiB or 256
- * columns, the fp32 sums of dH, and FP16 copies of FP8 operands).  D is rounded to BF16 (BF16 operands) or to FP16 at a power-of-two scale (the others;
- * FP8 operands are widened to FP16 exactly), half a step of relative error each; sums are fp32.
+ * columns, the fp32 sums of dH, and FP16 copies of FP8 operands).  D is rounded to BF16 (BF16 operands) or to FP16 (the others;
+ * FP8 operands are widened to FP16 exactly), half a step of relative error each, at a scale that brings the largest row
+ * coefficient to 2^14; for at most 16 rows a second half keeps what that rounding leaves out.  Sums are fp32.
  * Errors: NULL, DTYPE, SHAPE, ALIGNMENT, VALUE, ALIAS (an output over an input or another output), WORKSPACE.
  */
 /* Workspace of these calls (shapes and dtypes of H and W only; k = 0: cross entropy; >= 4096; 0 for arguments that the calls

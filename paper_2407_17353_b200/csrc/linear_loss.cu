@@ -16,9 +16,9 @@
 //   4096: 192 K blocks where 166 are the average); the logits' short ones fill them up.
 //
 // D has the operands' type; FP8 operands are converted to FP16, which holds them exactly, and D is FP16.  FP16 has few
-// exponents, so D is stored times a power of two that brings the largest row coefficient to 2^13..2^14 (probabilities down to
-// 2^-28 keep all 11 bits).  Its rounding is at most half a step (FP16 2^-11, BF16 2^-8) per element, independent over the
-// vocabulary: it adds to dH and dW what rounding them once to that type does.
+// exponents, so D is stored at a scale that brings the largest row coefficient to 2^14 (probabilities down to 2^-28 keep all 11
+// bits).  Its rounding is at most half a step (FP16 2^-11, BF16 2^-8) per element, independent over the
+// vocabulary: it adds to dH and dW what rounding them once to that type does.  (Few rows: kFewRows.)
 #include <cuda.h>
 #include <limits.h>
 #include <math.h>
@@ -57,7 +57,12 @@ struct Ring {
   int stages, a_bytes, b_bytes;  // of a stage: multiples of 1024
 };
 constexpr int kMaxStages = 12;
-constexpr int kLongKb = 24, kSegmentKb = 16;  // K blocks of a long contraction, and of its parts
+// K blocks from which on a contraction is long, and of its parts.  Sums of 256 (a single CTA, which waits for its weights anyway)
+// and of 768 values in the tensor cores' 32 bits leave the loss with the error that it has from rounding the result (2 rows of
+// 3269: 3.4e-6 with parts of 512, 7.6e-6 with parts of 1024, 1.3e-6 so); parts in contractions of 768 values, too, would make
+// 37 x 50257 x 768 41 instead of 29 us, which then waits for the additions.
+template <int NCTA> constexpr int kLongKb = NCTA == 1 ? 12 : 24;
+template <int NCTA> constexpr int kSegmentKb = NCTA == 1 ? 4 : 12;
 constexpr float kLog2E = 1.4426950408889634f;
 
 template <bool F8, int NCTA>
@@ -82,6 +87,13 @@ __device__ __forceinline__ float exp2_approx(float x) {
   return y;
 }
 
+// One lane of the whole warp, the same one each time: the store engine's calls and the waits for them.  (A branch on the lane
+// instead loses stores: with work on the same values behind it, no byte of the tile was written.)
+__device__ __forceinline__ bool elected_lane() {
+  uint32_t one;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.b32 %0, 1, 0, p;\n}" : "=r"(one));
+  return one != 0u;
+}
 // 32 values of this lane's row in shared memory, where one whose place is known at run time only can be reached: 16-byte pieces
 // exchanged within a row so that the lanes' accesses meet different banks.
 struct LaneRow {
@@ -105,7 +117,7 @@ struct LaneRow {
   // 1920 -> 1834 us).  Two tiles in turns (`flip`); every store of the tile
   // before the last one has left shared memory before its place is taken.  All lanes of the warp.
   __device__ __forceinline__ void store(const uint32_t* o, const CUtensorMap* map, int x_bytes, int y, uint32_t& flip) const {
-    if (lane == 0) bulk_wait_read<1>();
+    if (elected_lane()) bulk_wait_read<1>();
     __syncwarp();
     uint4* tile = reinterpret_cast<uint4*>(row - lane * 32) + flip * 128;
     flip ^= 1u;
@@ -113,7 +125,7 @@ struct LaneRow {
     for (int j = 0; j < 4; ++j) tile[lane * 4 + (j ^ ((lane >> 1) & 3))] = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
     fence_async_smem();
     __syncwarp();
-    if (lane == 0) {
+    if (elected_lane()) {
       tma_store_3d(map, smem_u32(tile), x_bytes, y, 0);
       bulk_commit();
     }
@@ -341,6 +353,7 @@ struct LogitsParams {
   // gradient
   const float* lse;
   const float2* coef;        // of p and of q
+  uint16_t* d_low; long long ldd;  // the second half of D, if it has one: rows of whole tiles
   uint32_t* status;
 };
 
@@ -407,7 +420,8 @@ __device__ __forceinline__ float pick32(const uint32_t* r, int i) {
 
 // LONG: the tensor cores add up with truncation, an error that grows with the number of additions and the sums' size, and the
 // losses are fp32: from kLongKb K blocks on, every kSegmentKb of them go to an accumulator of their own, and the epilogue warps
-// add those up in registers while the next ones are filled (d = 4096: relative errors of lse and loss 1.3e-6 and 2.0e-6 in one accumulator, 3e-7 and 4.5e-7 so, in the same time).
+// add those up in registers while the next ones are filled (d = 4096: relative errors of lse and loss 1.3e-6 and 2.0e-6 in one
+// accumulator, 3e-7 and 4.5e-7 in parts of 16 blocks, in the same time).
 template <int NCTA, bool F8, bool KD, bool LONG>
 __global__ void __launch_bounds__(kThreads, 1) logits_kernel(const __grid_constant__ CUtensorMap map_h,
                                                              const __grid_constant__ CUtensorMap map_w, const LogitsParams p) {
@@ -438,7 +452,7 @@ __global__ void __launch_bounds__(kThreads, 1) logits_kernel(const __grid_consta
         const int nt0 = static_cast<int>(item / p.tiles_m) * p.run;
         for (int nt = nt0; nt < min(nt0 + p.run, p.tiles_n) && !timed_out; ++nt) {
           if constexpr (LONG) {
-            for (int kb = 0; kb < p.num_kb && !timed_out; kb += kSegmentKb) timed_out = !e.template multiply<F8>(min(kSegmentKb, p.num_kb - kb), p.idesc, false, false);
+            for (int kb = 0; kb < p.num_kb && !timed_out; kb += kSegmentKb<NCTA>) timed_out = !e.template multiply<F8>(min(kSegmentKb<NCTA>, p.num_kb - kb), p.idesc, false, false);
           } else {
             timed_out = !e.template multiply<F8>(p.num_kb, p.idesc, false, false);
           }
@@ -499,7 +513,7 @@ __global__ void __launch_bounds__(kThreads, 1) logits_kernel(const __grid_consta
         const int cols = warp_rows ? p.cols - n0 : 0;
         if constexpr (LONG) {
           float z[kTN / 64][32];
-          for (int kb = 0; kb < p.num_kb && !timed_out; kb += kSegmentKb) {
+          for (int kb = 0; kb < p.num_kb && !timed_out; kb += kSegmentKb<NCTA>) {
             if (!e.wait_accumulator()) { timed_out = true; break; }
             e.each_chunk_in_order(half, p.half_cols, [&](const uint32_t* r, auto chunk) {
               constexpr int c = decltype(chunk)::value;
@@ -570,7 +584,7 @@ struct GradParams {
   GradProduct product[2];  // dW, dH
   LogitsParams logits;
   uint32_t idesc;          // of the products
-  const float* unit;       // [0]: the power of two that D is stored times; [1]: what its products are multiplied by
+  const float* unit;       // [0]: what D is stored times; [1]: what its products are multiplied by
 };
 struct GradItem { int mt, nt, part; };  // row tile, (first) column tile, part of the contraction
 __device__ __forceinline__ GradItem grad_item(const GradParams& p, int cls, int item) {
@@ -665,7 +679,7 @@ __global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_con
             for (int i = 0; i < 32; ++i) v[i] = coef.x * exp2_approx(fmaf(__uint_as_float(r[i]), c2, -lse2));
             if (__any_sync(0xFFFFFFFFu, target.id < g0 + 32)) {
               if constexpr (KD) {
-                if (e.lane == 0) bulk_wait_read<0>();
+                if (elected_lane()) bulk_wait_read<0>();
                 __syncwarp();
                 lane_row.put(reinterpret_cast<const uint32_t*>(v));
                 while (target.id < g0 + 32) {
@@ -682,8 +696,24 @@ __global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_con
                 target.advance();
               }
             }
+            constexpr int kD = BF ? SCALIFY_BF16 : SCALIFY_F16;
             uint32_t o[16];
-            encode_vec<BF ? SCALIFY_BF16 : SCALIFY_F16, 32>(v, o);
+            if (NCTA == 1 && l.d_low != nullptr) {
+              char* low = reinterpret_cast<char*>(l.d_low + row * l.ldd + c0);  // (rows are whole tiles)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                float high[8];
+                uint32_t rest[4];
+                encode_vec<kD, 8>(v + 8 * j, o + 4 * j);
+                decode_vec<kD, 8>(o + 4 * j, high);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) high[i] = v[8 * j + i] - high[i];
+                encode_vec<kD, 8>(high, rest);
+                if (row < l.n) st_bytes<16>(low + j * 16, rest);
+              }
+            } else {
+              encode_vec<kD, 32>(v, o);
+            }
             lane_row.store(o, &maps.d_out, c0 * 2, row - e.lane, flip);
           });
           e.release_accumulator();
@@ -738,7 +768,7 @@ __global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_con
         e.release_accumulator();
       }
     });
-    if (e.lane == 0) bulk_wait_all();  // every store of this warp has completed
+    if (elected_lane()) bulk_wait_all();  // every store of this warp has completed
   }
   if (timed_out) atomicOr(l.status, static_cast<uint32_t>(SCALIFY_DEV_TIMEOUT));
   e.tear_down();
@@ -1045,11 +1075,12 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const JoinParams p) 
   }
 }
 
-// FP8 rows -> FP16 (exact), of H and then of W
+// FP8 rows -> FP16 (exact), of H and then of W; H (16-bit rows too) as often as D has halves
 struct WidenParams {
   const void* src[2]; __half* dst[2];
   long long ld[2], ldd, rows[2];
   int dt[2];
+  long long n;   // rows of H itself
   int d;
 };
 struct CoefParams {
@@ -1065,7 +1096,7 @@ struct CoefParams {
   float kf_vocab, kf_n;
   float2* coef;
   uint2* block_tops;        // per block: largest coefficient (bits), rows that count
-  float* unit;              // [0]: the power of two that D is stored times; [1]: what its products are multiplied by
+  float* unit;              // [0]: what D is stored times; [1]: what its products are multiplied by
   float* dh_scale; float* dw_scale;
   uint32_t* ticket; uint32_t* status;
   int blocks;               // of the coefficients; the blocks behind them make the FP16 copies
@@ -1081,22 +1112,29 @@ __device__ __forceinline__ void widen_rows(const WidenParams& p, int block, int 
     const int v = static_cast<int>(i - row * vecs), n = p.d - v * 16;
     const int which = row >= p.rows[0];
     if (which) row -= p.rows[0];
-    const char* src = static_cast<const char*>(p.src[which]) + row * p.ld[which];
-    uint32_t w[4] = {}, o[8];
-    float f[16];
-    if (n >= 16) {
-      ld_raw<16>(src + v * 16, w);
+    const long long from = which == 0 && row >= p.n ? row - p.n : row;
+    uint32_t w[4] = {}, o[8] = {};
+    if (p.dt[which] >= SCALIFY_F16) {
+      const char* src = static_cast<const char*>(p.src[which]) + from * p.ld[which] * 2;
+      load_vec<SCALIFY_F16>(src, 2 * v, n, o);
+      if (n > kVec) load_vec<SCALIFY_F16>(src, 2 * v + 1, n - kVec, o + 4);
     } else {
-      load_vec<SCALIFY_E4M3>(src, 2 * v, n, w);
-      if (n > kVec) load_vec<SCALIFY_E4M3>(src, 2 * v + 1, n - kVec, w + 2);
+      const char* src = static_cast<const char*>(p.src[which]) + from * p.ld[which];
+      float f[16];
+      if (n >= 16) {
+        ld_raw<16>(src + v * 16, w);
+      } else {
+        load_vec<SCALIFY_E4M3>(src, 2 * v, n, w);
+        if (n > kVec) load_vec<SCALIFY_E4M3>(src, 2 * v + 1, n - kVec, w + 2);
+      }
+      if (p.dt[which] == SCALIFY_E4M3) decode_vec<SCALIFY_E4M3, 16>(w, f);
+      else decode_vec<SCALIFY_E5M2, 16>(w, f);
+      encode_vec<SCALIFY_F16, 16>(f, o);
     }
-    if (p.dt[which] == SCALIFY_E4M3) decode_vec<SCALIFY_E4M3, 16>(w, f);
-    else decode_vec<SCALIFY_E5M2, 16>(w, f);
-    encode_vec<SCALIFY_F16, 16>(f, o);
     st_bytes<32>(reinterpret_cast<char*>(p.dst[which] + row * p.ldd + v * 16), o);  // (rows are padded to whole vectors)
   }
 }
-// Row coefficients of p and of q in units of the upstream gradient (of the mean's, if there is none); the power of two that D
+// Row coefficients of p and of q in units of the upstream gradient (of the mean's, if there is none); what D
 // is stored times; output scales; FP16 copies of FP8 operands.
 __global__ void __launch_bounds__(kCoefThreads) coef_kernel(const __grid_constant__ CoefParams p) {
   __shared__ uint32_t s_top[kCoefThreads / 32];
@@ -1147,11 +1185,14 @@ __global__ void __launch_bounds__(kCoefThreads) coef_kernel(const __grid_constan
   block_join();
   if (threadIdx.x == 0) {
     *p.ticket = 0u;
-    // the largest coefficient goes to [2^13, 2^14): |D| stays below 2^15
+    // The largest coefficient goes to 2^14: |D| stays at or below 2^15.  Not by a power of two: the entries at the targets,
+    // which decide the gradients' error, are that coefficient times nearly 1, rounded in steps of 2^-8 (BF16) of themselves just
+    // below a power of two and of twice that just above it (22 x 675 x 112: 2.3e-3 of the norm of dH, 2.8e-3 by a power of two;
+    // 1.6e-3 is the rounding of the result).
     int ex = static_cast<int>(top >> 23) - 127;
-    if (top == 0u) ex = 13;
-    ex = min(max(13 - ex, -100), 100);
-    const float unit = __uint_as_float(static_cast<uint32_t>(127 + ex) << 23);
+    if (top == 0u) ex = 14;
+    ex = min(max(14 - ex, -100), 100);
+    const float unit = __uint_as_float(static_cast<uint32_t>(127 + ex) << 23) / __uint_as_float((top & 0x7FFFFFu) | 0x3F800000u);
     p.unit[0] = unit;
     p.unit[1] = (p.grad ? 1.0f : 1.0f / static_cast<float>(max(count, 1)) / p.mean_p2) / unit;
     const float hs = load_scale_after_wait(p.h_scale), ws = load_scale_after_wait(p.w_scale);
@@ -1239,6 +1280,13 @@ int run_length(long long tiles_m, long long tiles_n, int longest, int items) {
     if (tiles_m * ((tiles_n + run - 1) / run) >= items) return run;
   return 1;
 }
+// Few rows: D in two halves of its type, the second of what the first one's rounding left out, as rows of their own: dW's
+// contraction is over both (H twice), dH's sums are added at the end.  One rounding of D adds about as much to the gradients'
+// error as rounding the gradients themselves; with few rows, where a few entries of D decide, more (2 x 1646 x 136, BF16: 2.7e-3
+// of the norm where 1.6e-3 is the output's own).  The second half costs 4 to 10 % of few rows' time (3 x 115392 x 672:
+// 133 -> 145 us); 64 x 50257 x 768 would take 92 instead of 72.
+constexpr int kFewRows = 16;
+int halves_of(long long n) { return n > 0 && n <= kFewRows ? 2 : 1; }
 // Columns of a piece of the vocabulary: D of at most 2^27 bytes, two pieces of which are in memory; whole tiles.
 // (8192 x 50257 x 768: half and a quarter of it take 4 and 8 % longer, twice of it 2 % less.)
 long long piece_columns(long long n, long long vocab) {
@@ -1268,7 +1316,7 @@ int dh_parts(long long n, long long vocab, long long d) {
 struct Layout {
   size_t partial, dot, sums_blocks, entries, counts, sums, table, coef, tops, unit, h16, w16, D[2], acc, total;
   long long ld_part, ld16, ldd, ld_acc, piece, pieces;
-  int slots, run, parts, width, bins, bin_tiles;
+  int slots, run, parts, width, bins, bin_tiles, halves;
 };
 Layout layout_of(long long n, long long vocab, long long d, int es, int k, bool backward) {
   Layout l = {};
@@ -1277,7 +1325,8 @@ Layout layout_of(long long n, long long vocab, long long d, int es, int k, bool 
   const size_t rows = static_cast<size_t>(n);
   l.width = tile_columns(n, vocab);
   if (backward) {
-    l.piece = piece_columns(n, vocab);
+    l.halves = halves_of(n);
+    l.piece = piece_columns(n * l.halves, vocab);
     l.pieces = (vocab + l.piece - 1) / l.piece;
     if (l.pieces > 1) l.width = kTN;  // (pieces begin with a tile)
   }
@@ -1302,17 +1351,16 @@ Layout layout_of(long long n, long long vocab, long long d, int es, int k, bool 
     l.tops = take(kCoefBlocks * sizeof(uint2));
     l.unit = take(2 * sizeof(float));
     l.ld16 = pad_to(d, 16);
-    if (es == 1) {
-      l.h16 = take(rows * l.ld16 * 2);
-      l.w16 = take(static_cast<size_t>(vocab) * l.ld16 * 2);
-    }
+    const size_t d_rows = rows * l.halves;
+    if (es == 1 || l.halves > 1) l.h16 = take(d_rows * l.ld16 * 2);
+    if (es == 1) l.w16 = take(static_cast<size_t>(vocab) * l.ld16 * 2);
     l.ldd = l.piece;
-    l.D[0] = take(rows * l.ldd * 2);
-    l.D[1] = l.pieces > 1 ? take(rows * l.ldd * 2) : l.D[0];
+    l.D[0] = take(d_rows * l.ldd * 2);
+    l.D[1] = l.pieces > 1 ? take(d_rows * l.ldd * 2) : l.D[0];
     l.parts = l.pieces == 1 && n > 0 ? dh_parts(n, vocab, d) : 1;
-    if (l.pieces > 1 || l.parts > 1) {
+    if (l.pieces > 1 || l.parts > 1 || l.halves > 1) {
       l.ld_acc = pad_to(d, 32);
-      l.acc = take(l.parts * rows * l.ld_acc * sizeof(float));
+      l.acc = take(l.parts * d_rows * l.ld_acc * sizeof(float));
     }
   }
   l.total = at < kWsMin ? kWsMin : at;
@@ -1383,7 +1431,7 @@ int launch_logits(bool f8, bool kd, const CUtensorMap& mh, const CUtensorMap& mw
 }
 template <int NCTA>
 int launch_logits(bool f8, bool kd, const CUtensorMap& mh, const CUtensorMap& mw, const LogitsParams& p, cudaStream_t st) {
-  return p.num_kb > kLongKb ? launch_logits<NCTA, true>(f8, kd, mh, mw, p, st) : launch_logits<NCTA, false>(f8, kd, mh, mw, p, st);
+  return p.num_kb > kLongKb<NCTA> ? launch_logits<NCTA, true>(f8, kd, mh, mw, p, st) : launch_logits<NCTA, false>(f8, kd, mh, mw, p, st);
 }
 
 // Every class's items over the pairs, long ones first, so that the loads become as equal as whole items allow.
@@ -1595,16 +1643,17 @@ int launch_linear_loss_bwd(const LinearLossArgs& a, void* workspace, cudaStream_
   const char* h16 = static_cast<const char*>(a.H);
   const char* w16 = static_cast<const char*>(a.W);
   long long h16_ld = a.h_ld, w16_ld = a.w_ld, widen_blocks = 0;
-  if (es == 1 && a.n > 0) {
+  if ((es == 1 || l.halves > 1) && a.n > 0) {
     WidenParams& w = c.widen;
-    w.d = a.d; w.ldd = l.ld16;
-    w.src[0] = a.H; w.dst[0] = reinterpret_cast<__half*>(ws + l.h16); w.ld[0] = a.h_ld; w.rows[0] = a.dW ? a.n : 0; w.dt[0] = a.h_dt;
-    w.src[1] = a.W; w.dst[1] = reinterpret_cast<__half*>(ws + l.w16); w.ld[1] = a.w_ld; w.rows[1] = a.dH ? a.vocab : 0; w.dt[1] = a.w_dt;
+    w.d = a.d; w.ldd = l.ld16; w.n = a.n;
+    w.src[0] = a.H; w.dst[0] = reinterpret_cast<__half*>(ws + l.h16); w.ld[0] = a.h_ld; w.rows[0] = a.dW ? a.n * l.halves : 0; w.dt[0] = a.h_dt;
+    w.src[1] = a.W; w.dst[1] = reinterpret_cast<__half*>(ws + l.w16); w.ld[1] = a.w_ld; w.rows[1] = a.dH && es == 1 ? a.vocab : 0; w.dt[1] = a.w_dt;
     const long long most = 16ll * sm_count();
     widen_blocks = ((w.rows[0] + w.rows[1]) * ((a.d + 15) / 16) + kCoefThreads - 1) / kCoefThreads;
     if (widen_blocks > most) widen_blocks = most;
-    h16 = ws + l.h16; w16 = ws + l.w16;
-    h16_ld = w16_ld = l.ld16;
+    h16 = ws + l.h16;
+    h16_ld = l.ld16;
+    if (es == 1) { w16 = ws + l.w16; w16_ld = l.ld16; }
   }
   rc = launch_small(coef_kernel, c.blocks + widen_blocks, kCoefThreads, c, st);
   if (rc) return rc;
@@ -1620,21 +1669,22 @@ int launch_linear_loss_bwd(const LinearLossArgs& a, void* workspace, cudaStream_
   GradMaps m = {};
   LogitsParams& p = g.logits;
   p = logits_params(a, l, ws);
-  p.lse = a.lse; p.coef = c.coef;
+  p.lse = a.lse; p.coef = c.coef; p.ldd = l.ldd;
+  const long long d_rows = a.n * l.halves;  // (at most one row tile where there are two halves)
   const int ctas = ctas_of(a.n), n_tiles = p.tiles_m, d_tiles = static_cast<int>((a.d + kTN - 1) / kTN);
   GradProduct &dw = g.product[kClassDw], &dh = g.product[kClassDh];
   dw.N = dh.N = a.d;
   dw.tiles_n = dh.tiles_n = d_tiles;
-  dw.num_kb = dw.part_kb = static_cast<int>((a.n + kK16 - 1) / kK16);
+  dw.num_kb = dw.part_kb = static_cast<int>((d_rows + kK16 - 1) / kK16);
   dw.parts = 1;
   dw.ldo = a.dw_ld; dw.out_dt = a.dw_dt; dw.alpha = 1.0f / c.kf_n; dw.mode = kFinal;
-  dh.M = static_cast<int>(a.n);
+  dh.M = static_cast<int>(d_rows);
   dh.out = a.dH; dh.ldo = a.dh_ld; dh.out_dt = a.dh_dt; dh.alpha = 1.0f / c.kf_vocab;
   dh.acc = reinterpret_cast<float*>(ws + l.acc); dh.ld_acc = l.ld_acc;
   g.idesc = idesc_of(d_dt, d_dt, ctas, kTN);
   g.unit = c.unit;
   rc = map_of(&m.h, a.H, a.n, a.d, a.h_ld, es, p.box_rows);
-  if (!rc) rc = map_of(&m.h_mn, h16, a.n, a.d, h16_ld, 2, kK16);
+  if (!rc) rc = map_of(&m.h_mn, h16, d_rows, a.d, h16_ld, 2, kK16);
   if (rc) return rc;
   // launch i: the products of piece i - 1 and the logits of piece i
   for (long long i = 0; i <= l.pieces; ++i) {
@@ -1651,6 +1701,7 @@ int launch_linear_loss_bwd(const LinearLossArgs& a, void* workspace, cudaStream_
       items[kClassD] = static_cast<long long>(n_tiles) * ((p.tiles_n + p.run - 1) / p.run);
       cost[kClassD] = p.run * (p.num_kb + kTileCost);
       rc = d_store_map(&m.d_out, ws + l.D[i & 1], a.n, cols, l.ldd);
+      if (l.halves > 1) p.d_low = reinterpret_cast<uint16_t*>(ws + l.D[i & 1]) + a.n * l.ldd;
       if (!rc) rc = map_of(&m.w, static_cast<const char*>(a.W) + v0 * a.w_ld * es, cols, a.d, a.w_ld, es, l.width / ctas);
     }
     if (!rc && i > 0) {
@@ -1660,23 +1711,23 @@ int launch_linear_loss_bwd(const LinearLossArgs& a, void* workspace, cudaStream_
       dh.num_kb = static_cast<int>((cols + kK16 - 1) / kK16);
       dh.part_kb = (dh.num_kb + l.parts - 1) / l.parts;
       dh.parts = (dh.num_kb + dh.part_kb - 1) / dh.part_kb;
-      dh.mode = l.pieces > 1 ? (i == 1 ? kAccFirst : i < l.pieces ? kAccNext : kAccLast) : dh.parts > 1 ? kAccFirst : kFinal;
+      dh.mode = i == 1 && (l.pieces > 1 || dh.parts > 1 || l.halves > 1) ? kAccFirst : i == 1 ? kFinal : i < l.pieces || l.halves > 1 ? kAccNext : kAccLast;
       if (a.dW) items[kClassDw] = row_tiles(cols, ctas) * d_tiles;
       if (a.dH) items[kClassDh] = static_cast<long long>(n_tiles) * d_tiles * dh.parts;
       cost[kClassDw] = dw.num_kb + kTileCost;
       cost[kClassDh] = dh.part_kb + kTileCost;
       dw.out = a.dW ? static_cast<char*>(a.dW) + v0 * a.dw_ld * 2 : nullptr;
-      rc = map_of(&m.d_mn, D, a.n, cols, l.ldd, 2, kK16);
-      if (!rc) rc = map_of(&m.d_k, D, a.n, cols, l.ldd, 2, kTM);
+      rc = map_of(&m.d_mn, D, d_rows, cols, l.ldd, 2, kK16);
+      if (!rc) rc = map_of(&m.d_k, D, d_rows, cols, l.ldd, 2, kTM);
       if (!rc) rc = map_of(&m.w_mn, w16 + v0 * w16_ld * 2, cols, a.d, w16_ld, 2, kK16);
     }
     if (!rc) rc = ctas == 2 ? launch_grad<2>(es == 1, a.k > 0, bf, m, g, items, cost, st) : launch_grad<1>(es == 1, a.k > 0, bf, m, g, items, cost, st);
     if (rc) return rc;
   }
-  if (!a.dH || l.pieces > 1 || dh.parts == 1) return SCALIFY_OK;
+  if (!a.dH || dh.parts * l.halves == 1) return SCALIFY_OK;
   PlanesParams q = {};
-  q.acc = dh.acc; q.ld_acc = dh.ld_acc; q.planes = dh.parts;
-  q.M = dh.M; q.N = dh.N; q.out = a.dH; q.ldo = a.dh_ld; q.out_dt = dh.out_dt;
+  q.acc = dh.acc; q.ld_acc = dh.ld_acc; q.planes = dh.parts * l.halves;  // of a.n rows each
+  q.M = static_cast<int>(a.n); q.N = dh.N; q.out = a.dH; q.ldo = a.dh_ld; q.out_dt = dh.out_dt;
   q.alpha = dh.alpha; q.unit = g.unit;
   const long long blocks = (a.n * ((a.d + 3) / 4) + 255) / 256, most = 8ll * sm_count();
   return launch_small(planes_kernel, blocks < most ? blocks : most, 256, q, st);

@@ -11,7 +11,7 @@ which is also the absolute error of log p, hence the relative one of p."""
 import torch
 
 U = 2.0 ** -24
-QUANTUM = {torch.float16: 2.0 ** -24, torch.bfloat16: 2.0 ** -133}
+QUANTUM = {torch.float16: 2.0 ** -24, torch.bfloat16: 2.0 ** -133, torch.float32: 2.0 ** -149}
 
 
 def p2(c):
