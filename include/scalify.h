@@ -601,8 +601,9 @@ int scalify_scaled_cross_entropy(const scalify_array* logits, int64_t n_classes,
  * Errors: NULL, DTYPE, SHAPE, ALIGNMENT, VALUE, ALIAS (an output over an input or another output), WORKSPACE.
  */
 /* Workspace of these calls (shapes and dtypes of H and W only; k = 0: cross entropy; >= 4096; 0 for arguments that the calls
- * refuse).  backward != 0: enough for the forward call too, so that a step's calls on one stream share one workspace; nothing
- * is kept in it between calls. */
+ * refuse).  Enough for every batch of at most H's rows (it never falls as the rows grow), so that one for the longest batch
+ * serves all.  backward != 0: enough for the forward call too, so that a step's calls on one stream share one workspace;
+ * nothing is kept in it between calls. */
 size_t scalify_linear_loss_workspace_bytes(const scalify_array* H, const scalify_array* W, int k, int backward);
 int scalify_scaled_linear_cross_entropy(const scalify_array* H, const scalify_array* W, const int64_t* ids, int64_t padding_id,
                                         float z_loss, float* loss, float* lse, float* mean, void* workspace,

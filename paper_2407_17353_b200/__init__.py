@@ -732,7 +732,8 @@ def scalify_scaled_muon_step(tensors: MuonTensors, ws: Workspace, *, lr: float, 
 
 
 def scalify_linear_loss_workspace_bytes(H: ScaledTensor, W: ScaledTensor, *, k: int = 0, backward: bool = True) -> int:
-    """Workspace of the output layer's losses on H [n, d] and W [vocab, d] (k: a teacher's entries per row, 0: cross entropy)."""
+    """Workspace of the output layer's losses on H [n, d] and W [vocab, d] (k: a teacher's entries per row, 0: cross entropy);
+    enough for every batch of at most n rows."""
     n = int(lib().scalify_linear_loss_workspace_bytes(_ref(_desc(H)), _ref(_desc(W)), int(k), int(bool(backward))))
     if n == 0:
         raise ValueError("scalify_linear_loss_workspace_bytes: H [n, d] and W [vocab, d] of one 16-bit dtype or 8-bit ones, k up to 256")

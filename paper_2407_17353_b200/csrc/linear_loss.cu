@@ -1274,6 +1274,9 @@ int tile_columns(long long n, long long vocab) {
   }
   return best;
 }
+// The forward call's longest run, and the items that there have to be.
+constexpr int kLongestRun = 8;
+int run_items(int ctas) { return 16 * (148 / ctas); }
 // Consecutive column tiles per work item: long runs write few partial results, short ones share the work evenly.
 int run_length(long long tiles_m, long long tiles_n, int longest, int items) {
   for (int run = longest; run > 1; run >>= 1)
@@ -1289,9 +1292,10 @@ constexpr int kFewRows = 16;
 int halves_of(long long n) { return n > 0 && n <= kFewRows ? 2 : 1; }
 // Columns of a piece of the vocabulary: D of at most 2^27 bytes, two pieces of which are in memory; whole tiles.
 // (8192 x 50257 x 768: half and a quarter of it take 4 and 8 % longer, twice of it 2 % less.)
+constexpr long long kPieceElems = 1ll << 26;
 long long piece_columns(long long n, long long vocab) {
   const long long rows = pad_to(n < 1 ? 1 : n, 32);
-  long long cols = (1ll << 26) / rows / kTN * kTN;
+  long long cols = kPieceElems / rows / kTN * kTN;
   if (cols < kTN) cols = kTN;
   const long long all = pad_to(vocab, kTN);
   if (cols >= all) return all;
@@ -1340,7 +1344,7 @@ Layout layout_of(long long n, long long vocab, long long d, int es, int k, bool 
     l.table = take(rows * 2 * l.bins * sizeof(uint16_t));
   }
   if (!backward) {
-    l.run = run_length(tm, tn, 8, 16 * units_of(n));
+    l.run = run_length(tm, tn, kLongestRun, run_items(ctas_of(n)));
     l.slots = static_cast<int>((tn + l.run - 1) / l.run) * 2;
     l.ld_part = pad_to(n, 32);
     l.partial = take(static_cast<size_t>(l.slots) * l.ld_part * sizeof(float2));
@@ -1355,8 +1359,11 @@ Layout layout_of(long long n, long long vocab, long long d, int es, int k, bool 
     if (es == 1 || l.halves > 1) l.h16 = take(d_rows * l.ld16 * 2);
     if (es == 1) l.w16 = take(static_cast<size_t>(vocab) * l.ld16 * 2);
     l.ldd = l.piece;
-    l.D[0] = take(d_rows * l.ldd * 2);
-    l.D[1] = l.pieces > 1 ? take(d_rows * l.ldd * 2) : l.D[0];
+    // (from three pieces on as much as a piece may take, not what this batch's takes: the size must not fall as batches grow)
+    size_t d_bytes = d_rows * l.ldd * 2;
+    if (l.pieces > 2 && d_bytes < kPieceElems * 2) d_bytes = kPieceElems * 2;
+    l.D[0] = take(d_bytes);
+    l.D[1] = l.pieces > 1 ? take(d_bytes) : l.D[0];
     l.parts = l.pieces == 1 && n > 0 ? dh_parts(n, vocab, d) : 1;
     if (l.pieces > 1 || l.parts > 1 || l.halves > 1) {
       l.ld_acc = pad_to(d, 32);
@@ -1566,11 +1573,37 @@ LogitsParams logits_params(const LinearLossArgs& a, const Layout& l, char* ws) {
 
 }  // namespace
 
-size_t linear_loss_ws_bytes(long long n, long long vocab, long long d, int operand_bytes, int k, bool backward) {
+size_t linear_loss_ws_need(long long n, long long vocab, long long d, int operand_bytes, int k, bool backward) {
   const size_t forward = layout_of(n, vocab, d, operand_bytes, k, false).total;
   if (!backward) return forward;
   const size_t both = layout_of(n, vocab, d, operand_bytes, k, true).total;
   return both > forward ? both : forward;
+}
+
+// The most that a batch of at most n rows needs, so that a workspace for the longest batch serves every other.  The need falls only
+// where the plan changes: behind the last batch with two halves of D, with one CTA per tile, of each run length, of each number
+// of parts of dH, and with one piece of the vocabulary.  Between those it grows, so they are what is looked at.
+size_t linear_loss_ws_bytes(long long n, long long vocab, long long d, int operand_bytes, int k, bool backward) {
+  size_t most = 0;
+  auto look = [&](long long rows) {
+    const size_t need = linear_loss_ws_need(rows < n ? rows : n, vocab, d, operand_bytes, k, backward);
+    if (need > most) most = need;
+  };
+  look(n);
+  look(kFewRows);
+  look(kTM);
+  const long long tiles_n = (vocab + kTN - 1) / kTN, tile_m = 2 * kTM;
+  for (int run = 2; run <= kLongestRun; run *= 2) {  // the last batch with runs shorter than this
+    const long long per = (tiles_n + run - 1) / run;
+    look((run_items(2) + per - 1) / per * tile_m - tile_m);
+  }
+  if (!backward) return most;
+  const long long all = pad_to(vocab, kTN), one_piece = all == kTN ? n : kPieceElems / all / 32 * 32;
+  look(one_piece);
+  // (parts: the same for all batches of as many K blocks; one where there are two tiles for each unit)
+  const long long d_tiles = (d + kTN - 1) / kTN;
+  for (long long rows = kK16; rows < n && rows < one_piece && row_tiles(rows, ctas_of(rows)) * d_tiles < 2 * units_of(rows); rows += kK16) look(rows);
+  return most;
 }
 
 int launch_linear_loss(const LinearLossArgs& a, void* workspace, cudaStream_t st) {

@@ -38,6 +38,8 @@ struct LinearLossArgs {
   long long dh_ld, dw_ld;
   float* dh_scale; float* dw_scale;
 };
+// What a call on n rows needs, and the most that a call on at most n rows does.
+size_t linear_loss_ws_need(long long n, long long vocab, long long d, int operand_bytes, int k, bool backward);
 size_t linear_loss_ws_bytes(long long n, long long vocab, long long d, int operand_bytes, int k, bool backward);
 int launch_linear_loss(const LinearLossArgs& a, void* ws, cudaStream_t st);
 int launch_linear_loss_bwd(const LinearLossArgs& a, void* ws, cudaStream_t st);

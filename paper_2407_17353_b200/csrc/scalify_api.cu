@@ -1435,7 +1435,7 @@ int linear_loss_forward(LinearLossArgs& a, const scalify_array* H, const scalify
     for (int j = 0; j < i; ++j)
       if (overlap(out[i], out[j])) return SCALIFY_ERR_ALIAS;
   }
-  const int rc = check_ws(workspace, workspace_bytes, linear_loss_ws_bytes(a.n, a.vocab, a.d, elem_size(a.h_dt), a.k, false));
+  const int rc = check_ws(workspace, workspace_bytes, linear_loss_ws_need(a.n, a.vocab, a.d, elem_size(a.h_dt), a.k, false));
   if (rc) return rc;
   a.loss = loss; a.lse = lse; a.mean = mean;
   return launch_linear_loss(a, workspace, static_cast<cudaStream_t>(stream));
@@ -1474,7 +1474,7 @@ int linear_loss_backward(LinearLossArgs& a, const scalify_array* H, const scalif
   const float* in_words[4] = {H->scale, W->scale, T ? T->scale : nullptr, grad ? grad->scale : nullptr};
   int rc = check_scale_words(out_words, 2, in_words, 4);
   if (rc) return rc;
-  rc = check_ws(workspace, workspace_bytes, linear_loss_ws_bytes(a.n, a.vocab, a.d, elem_size(a.h_dt), a.k, true));
+  rc = check_ws(workspace, workspace_bytes, linear_loss_ws_need(a.n, a.vocab, a.d, elem_size(a.h_dt), a.k, true));
   if (rc) return rc;
   a.lse = const_cast<float*>(lse);
   if (dH) { a.dH = dH->data; a.dh_dt = dH->dtype; a.dh_ld = dH->stride[0]; a.dh_scale = dH->scale; }
