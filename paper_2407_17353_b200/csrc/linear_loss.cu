@@ -64,6 +64,7 @@ constexpr int kMaxStages = 12;
 template <int NCTA> constexpr int kLongKb = NCTA == 1 ? 12 : 24;
 template <int NCTA> constexpr int kSegmentKb = NCTA == 1 ? 4 : 12;
 constexpr float kLog2E = 1.4426950408889634f;
+constexpr float kLargest = 3.402823466e38f;  // of fp32
 
 template <bool F8, int NCTA>
 __device__ __forceinline__ void umma(uint32_t d_tmem, uint64_t ad, uint64_t bd, uint32_t idesc, uint32_t acc) {
@@ -499,7 +500,8 @@ __global__ void __launch_bounds__(kThreads, 1) logits_kernel(const __grid_consta
           float m = __uint_as_float(r[0]);
 #pragma unroll
           for (int i = 1; i < 32; ++i) m = fmaxf(m, __uint_as_float(r[i]));
-          m *= c2;
+          // (a row with +inf: relative to the largest finite number, to which finite exponents are nothing and infinite ones inf)
+          m = fminf(m * c2, kLargest);
           if (m > top) {  // (a row of -inf so far: sum is 0)
             sum *= exp2_approx(top - m);
             top = m;
@@ -1034,7 +1036,8 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const JoinParams p) 
       bool bad = false;
       const bool counts = row_target(p.ids, p.padding_id, p.vocab, p.counts, p.sums, row, &qe, &bad);
       if (bad) atomicOr(p.status, static_cast<uint32_t>(SCALIFY_DEV_BAD_INDEX));
-      const float loss = counts ? qe.y + (qe.x * lse - dot * (hw * p.inv_temp)) + (p.z_loss > 0.f ? p.z_loss * lse * lse : 0.f) : 0.f;
+      const float mass = qe.x != 0.f ? qe.x * lse : 0.f;  // (0 times inf is nothing)
+      const float loss = counts ? qe.y + (mass - dot * (hw * p.inv_temp)) + (p.z_loss > 0.f ? p.z_loss * lse * lse : 0.f) : 0.f;
       p.loss[row] = loss;
       p.lse[row] = lse;
       total = loss;
