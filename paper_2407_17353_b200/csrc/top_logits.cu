@@ -146,8 +146,11 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) top_logits_kernel(con
       }
       most = word_max<DT>(most, m);
     }
-    const float m = word_top<DT>(most);
-    nan = nan || m != m;
+    const float largest = word_top<DT>(most);
+    nan = nan || largest != largest;
+    // (+inf: relative to the largest finite number, to which finite exponents are nothing and infinite ones infinite; as a bound
+    // for the selection it is only lower)
+    const float m = fminf(largest, 3.402823466e38f);
     if (m > top) {
       sum *= ex2((top - m) * c2);
       top = m;
