@@ -63,6 +63,12 @@ constexpr int kMaxStages = 12;
 // 37 x 50257 x 768 41 instead of 29 us, which then waits for the additions.
 template <int NCTA> constexpr int kLongKb = NCTA == 1 ? 12 : 24;
 template <int NCTA> constexpr int kSegmentKb = NCTA == 1 ? 4 : 12;
+// K blocks of one accumulator in the gradient kernel, of the logits and of the products.  The tensor cores drop what lies below the
+// running sum's last bits, of every product: by measurement 2^-25 of the sum per product and 2^-23 per addition at most, so that
+// a sum of N products of one sign loses N 2^-27 of itself on average.  In one accumulator a batch of 2^22 rows left dW off by
+// 2.6e-2 and a vocabulary of 2^22 dH by 1.3e-2; 256 blocks lose 1e-4, less than what rounding the result to FP16 does (128 blocks
+// would make the step 4096 x 4096, whose pieces have 252, 1.2 % slower).
+constexpr int kLogitKb = 64, kSumKb = 256;
 constexpr float kLog2E = 1.4426950408889634f;
 constexpr float kLargest = 3.402823466e38f;  // of fp32
 
@@ -340,6 +346,41 @@ template <int NCTA> struct Engine {
     one(std::integral_constant<int, 2>());
     one(std::integral_constant<int, 3>());
   }
+  // f(32 columns of this lane's row, chunk) of one tile; SUMS: its contraction may take several accumulators, whose sums so far
+  // wait in memory, of which every lane reads back only what it has written itself (`sums`: this warp's, a chunk after the other, pieces of
+  // 16 bytes lane by lane).
+  template <bool SUMS, class F> __device__ __forceinline__ bool tile_chunks(int num_kb, int part_kb, int half, int half_cols, int cols, float* sums, F f) {
+    if constexpr (!SUMS) {
+      if (!wait_accumulator()) return false;
+      each_chunk(half, half_cols, cols, f);
+      release_accumulator();
+      return true;
+    }
+    for (int kb = 0; kb < num_kb; kb += part_kb) {
+      if (!wait_accumulator()) return false;
+      const bool first = kb == 0, last = kb + part_kb >= num_kb;
+      each_chunk(half, half_cols, cols, [&](uint32_t* r, int c) {
+        char* at = reinterpret_cast<char*>(sums) + c * 4096 + lane * 16;
+        if (!first) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            uint32_t before[4];
+            ld_raw<16>(at + j * 512, before);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[4 * j + i] = __float_as_uint(__uint_as_float(r[4 * j + i]) + __uint_as_float(before[i]));
+          }
+        }
+        if (last) {
+          f(r, c);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) st_raw<16>(at + j * 512, r + 4 * j);
+        }
+      });
+      release_accumulator();
+    }
+    return true;
+  }
   __device__ __forceinline__ void release_accumulator() {
     tc_fence_before();
     __syncwarp();
@@ -573,7 +614,9 @@ __global__ void __launch_bounds__(kThreads, 1) logits_kernel(const __grid_consta
 // What the CTA pairs of one launch share: tiles of the products dW = D^T H and dH = D W of one piece of the vocabulary, and of
 // the logits (the gradient D) of the NEXT piece, which fill the pairs up to equal loads whatever the products' tiles leave.
 enum { kClassDw = 0, kClassDh = 1, kClassD = 2, kClasses = 3 };
-constexpr int kMaxUnits = 160;
+constexpr int kSms = 148;         // of the GPU, which sizes are planned for, whatever the launch finds
+constexpr int kMaxUnits = kSms;
+constexpr int kWarpSums = 4 * 32 * 32;
 constexpr int kListed = 48;
 struct Schedule {
   int order[kClasses];               // long tiles first
@@ -611,6 +654,7 @@ struct GradParams {
   LogitsParams logits;
   uint32_t idesc;          // of the products
   const float* unit;       // [0]: what D is stored times; [1]: what its products are multiplied by
+  float* sums;             // per CTA and epilogue warp four chunks, where a contraction takes several accumulators
 };
 struct GradItem { int mt, nt, part; };  // row tile, (first) column tile, part of the contraction
 __device__ __forceinline__ GradItem grad_item(const GradParams& p, int cls, int item) {
@@ -622,7 +666,9 @@ __device__ __forceinline__ GradItem grad_item(const GradParams& p, int cls, int 
 }
 struct GradMaps { CUtensorMap h, w, d_mn, h_mn, d_k, w_mn, d_out; };
 
-template <int NCTA, bool F8, bool KD, bool BF>
+// SUMS: the logits' contraction is longer than kLogitKb blocks, or a product's than kSumKb.  (A kernel of its own: the test for it in
+// the epilogue costs the FP8 step 8192 x 768 3 %.)
+template <int NCTA, bool F8, bool KD, bool BF, bool SUMS>
 __global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradParams p) {
   asm volatile("griddepcontrol.launch_dependents;");  // the next kernel may set up while this one runs
   extern __shared__ uint8_t smem_raw[];
@@ -666,11 +712,14 @@ __global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_con
     }
   } else if (e.warp == 1) {
     if (e.lane == 0 && e.rank == 0u) {
+      const int logit_kb = SUMS ? kLogitKb : INT_MAX / 2, sum_kb = SUMS ? kSumKb : INT_MAX / 2;
       each_item([&](int cls, const GradItem& item) {
         if (cls == kClassD) {
-          for (int nt = item.nt; nt < min(item.nt + l.run, l.tiles_n) && !timed_out; ++nt) timed_out = !e.template multiply<F8>(l.num_kb, l.idesc, false, false);
+          for (int nt = item.nt; nt < min(item.nt + l.run, l.tiles_n); ++nt)
+            for (int kb = 0; kb < l.num_kb && !timed_out; kb += logit_kb) timed_out = !e.template multiply<F8>(min(logit_kb, l.num_kb - kb), l.idesc, false, false);
         } else {
-          timed_out = !e.template multiply<false>(part_kbs(p.product[cls], item.part), p.idesc, cls == kClassDw, true);
+          const int kbs = part_kbs(p.product[cls], item.part);
+          for (int kb = 0; kb < kbs && !timed_out; kb += sum_kb) timed_out = !e.template multiply<false>(min(sum_kb, kbs - kb), p.idesc, cls == kClassDw, true);
         }
       });
       if (timed_out || *e.abort_flag) e.drain_multiplies();
@@ -680,6 +729,7 @@ __global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_con
     const int own_row = static_cast<int>(e.rank) * kTM + quarter * 32 + e.lane;
     const LaneRow lane_row = e.staging();
     uint32_t flip = 0;
+    float* const sums = p.sums + (static_cast<long long>(blockIdx.x) * kEpiWarps + (e.warp - 2)) * kWarpSums;
     const float c2 = load_scale_after_wait(l.h_scale) * load_scale_after_wait(l.w_scale) * l.inv_temp * kLog2E;
     const float unit_d = reinterpret_cast<const volatile float*>(p.unit)[0], factor = reinterpret_cast<const volatile float*>(p.unit)[1];
     each_item([&](int cls, const GradItem& item) {
@@ -695,9 +745,8 @@ __global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_con
           lse2 = __ldcg(l.lse + row) * kLog2E;
         }
         for (int nt = nt0; nt < min(nt0 + l.run, l.tiles_n); ++nt) {
-          if (!e.wait_accumulator()) { timed_out = true; break; }
           const int n0 = (2 * nt + half) * l.half_cols;
-          e.each_chunk(half, l.half_cols, row - e.lane < l.n ? l.cols - n0 : 0, [&](uint32_t* r, int c) {
+          timed_out = !e.template tile_chunks<SUMS>(l.num_kb, kLogitKb, half, l.half_cols, row - e.lane < l.n ? l.cols - n0 : 0, sums, [&](uint32_t* r, int c) {
             const int c0 = n0 + c * 32;
             const long long g0 = l.col0 + c0;
             float v[32];
@@ -742,7 +791,7 @@ __global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_con
             }
             lane_row.store(o, &maps.d_out, c0 * 2, row - e.lane, flip);
           });
-          e.release_accumulator();
+          if (timed_out) break;
         }
       } else {
         const GradProduct& g = p.product[cls];
@@ -751,8 +800,7 @@ __global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_con
         const int mode = g.mode;
         char* out_row = static_cast<char*>(g.out) + (static_cast<long long>(row) * g.ldo + n0) * 2;
         float* acc_row = g.acc + (static_cast<long long>(item.part) * g.M + row) * g.ld_acc + n0;  // (padded to whole chunks)
-        if (!e.wait_accumulator()) { timed_out = true; return; }
-        e.each_chunk(half, kTN / 2, row - e.lane < g.M ? g.N - n0 : 0, [&](uint32_t* r, int c) {
+        timed_out = !e.template tile_chunks<SUMS>(part_kbs(g, item.part), kSumKb, half, kTN / 2, row - e.lane < g.M ? g.N - n0 : 0, sums, [&](uint32_t* r, int c) {
           float v[32];
 #pragma unroll
           for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
@@ -791,7 +839,6 @@ __global__ void __launch_bounds__(kThreads, 1) loss_grad_kernel(const __grid_con
             }
           }
         });
-        e.release_accumulator();
       }
     });
     if (elected_lane()) bulk_wait_all();  // every store of this warp has completed
@@ -1282,9 +1329,9 @@ __global__ void __launch_bounds__(256) zero_rows_kernel(uint16_t* out, long long
 }
 
 // ------------------------------------------------------------------------------------------------- host side
-// CTAs per tile, and the pairs (or CTAs) of the GPU, which sizes are planned for, whatever the launch finds.
+// CTAs per tile, and the pairs (or CTAs) of the GPU.
 int ctas_of(long long n) { return n <= kTM ? 1 : 2; }
-int units_of(long long n) { return 148 / ctas_of(n); }
+int units_of(long long n) { return kSms / ctas_of(n); }
 long long row_tiles(long long rows, int ctas) { return (rows + kTM * ctas - 1) / (kTM * ctas); }
 long long pad_to(long long x, long long m) { return (x + m - 1) / m * m; }
 size_t pad256(size_t x) { return (x + 255) / 256 * 256; }
@@ -1303,7 +1350,7 @@ int tile_columns(long long n, long long vocab) {
 }
 // The forward call's longest run, and the items that there have to be.
 constexpr int kLongestRun = 8;
-int run_items(int ctas) { return 16 * (148 / ctas); }
+int run_items(int ctas) { return 16 * (kSms / ctas); }
 // Consecutive column tiles per work item: long runs write few partial results, short ones share the work evenly.
 int run_length(long long tiles_m, long long tiles_n, int longest, int items) {
   for (int run = longest; run > 1; run >>= 1)
@@ -1344,8 +1391,11 @@ int dh_parts(long long n, long long vocab, long long d) {
   return parts < 1 ? 1 : static_cast<int>(parts);
 }
 
+// K blocks of the logits
+long long row_kbs(long long d, int es) { return (d * es + kRowBytes - 1) / kRowBytes; }
+
 struct Layout {
-  size_t partial, dot, sums_blocks, entries, counts, sums, table, coef, tops, unit, h16, w16, D[2], acc, total;
+  size_t partial, dot, sums_blocks, entries, counts, sums, table, coef, tops, unit, h16, w16, D[2], acc, sums_long, total;
   long long ld_part, ld16, ldd, ld_acc, piece, pieces;
   int slots, run, parts, width, bins, bin_tiles, halves;
 };
@@ -1396,6 +1446,10 @@ Layout layout_of(long long n, long long vocab, long long d, int es, int k, bool 
       l.ld_acc = pad_to(d, 32);
       l.acc = take(l.parts * d_rows * l.ld_acc * sizeof(float));
     }
+    // (the widest that as many pieces can be: the size must not fall as batches grow)
+    const long long widest = l.pieces > 1 ? kPieceElems / pad_to(n > 0 ? n * l.halves : 1, 32) : l.piece;
+    const long long dh_kb = (widest / kK16 + l.parts - 1) / l.parts, dw_kb = (static_cast<long long>(d_rows) + kK16 - 1) / kK16;
+    if (n > 0 && (dh_kb > kSumKb || dw_kb > kSumKb || row_kbs(d, es) > kLogitKb)) l.sums_long = take(static_cast<size_t>(kSms) * kEpiWarps * kWarpSums * sizeof(float));
   }
   l.total = at < kWsMin ? kWsMin : at;
   return l;
@@ -1426,7 +1480,7 @@ int unit_config(K kernel, DeviceOnce& once, long long items, cudaStream_t st, cu
   attrs[1].val.clusterDim.x = NCTA; attrs[1].val.clusterDim.y = 1; attrs[1].val.clusterDim.z = 1;
   *cfg = {};
   *units = static_cast<int>(items < most ? items : most);
-  if (*units > kMaxUnits) *units = kMaxUnits;
+  if (*units > kSms / NCTA) *units = kSms / NCTA;
   cfg->gridDim = dim3(static_cast<unsigned>(*units * NCTA));
   cfg->blockDim = dim3(kThreads); cfg->dynamicSmemBytes = kBytes; cfg->stream = st;
   cfg->attrs = attrs; cfg->numAttrs = 2;
@@ -1510,9 +1564,9 @@ void fill_schedule(Schedule& s, const long long (&items)[kClasses], const double
   }
 }
 
-template <int NCTA, bool F8, bool KD, bool BF>
+template <int NCTA, bool F8, bool KD, bool BF, bool SUMS>
 int launch_grad_variant(const GradMaps& m, GradParams& p, const long long (&items)[kClasses], const double (&cost)[kClasses], cudaStream_t st) {
-  auto kernel = loss_grad_kernel<NCTA, F8, KD, BF>;
+  auto kernel = loss_grad_kernel<NCTA, F8, KD, BF, SUMS>;
   static DeviceOnce once;
   cudaLaunchConfig_t cfg;
   cudaLaunchAttribute attrs[2];
@@ -1523,11 +1577,17 @@ int launch_grad_variant(const GradMaps& m, GradParams& p, const long long (&item
   SCALIFY_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, m, p));
   return SCALIFY_OK;
 }
+template <int NCTA, bool SUMS>
+int launch_grad(bool f8, bool kd, bool bf, const GradMaps& m, GradParams& p, const long long (&items)[kClasses], const double (&cost)[kClasses], cudaStream_t st) {
+  if (f8) return kd ? launch_grad_variant<NCTA, true, true, false, SUMS>(m, p, items, cost, st) : launch_grad_variant<NCTA, true, false, false, SUMS>(m, p, items, cost, st);
+  if (bf) return kd ? launch_grad_variant<NCTA, false, true, true, SUMS>(m, p, items, cost, st) : launch_grad_variant<NCTA, false, false, true, SUMS>(m, p, items, cost, st);
+  return kd ? launch_grad_variant<NCTA, false, true, false, SUMS>(m, p, items, cost, st) : launch_grad_variant<NCTA, false, false, false, SUMS>(m, p, items, cost, st);
+}
 template <int NCTA>
 int launch_grad(bool f8, bool kd, bool bf, const GradMaps& m, GradParams& p, const long long (&items)[kClasses], const double (&cost)[kClasses], cudaStream_t st) {
-  if (f8) return kd ? launch_grad_variant<NCTA, true, true, false>(m, p, items, cost, st) : launch_grad_variant<NCTA, true, false, false>(m, p, items, cost, st);
-  if (bf) return kd ? launch_grad_variant<NCTA, false, true, true>(m, p, items, cost, st) : launch_grad_variant<NCTA, false, false, true>(m, p, items, cost, st);
-  return kd ? launch_grad_variant<NCTA, false, true, false>(m, p, items, cost, st) : launch_grad_variant<NCTA, false, false, false>(m, p, items, cost, st);
+  const bool sums = (items[kClassD] > 0 && p.logits.num_kb > kLogitKb) || (items[kClassDw] > 0 && p.product[kClassDw].part_kb > kSumKb) ||
+                    (items[kClassDh] > 0 && p.product[kClassDh].part_kb > kSumKb);
+  return sums ? launch_grad<NCTA, true>(f8, kd, bf, m, p, items, cost, st) : launch_grad<NCTA, false>(f8, kd, bf, m, p, items, cost, st);
 }
 
 // operand formats of the instruction descriptor: kind::f16 F16 0, BF16 1; kind::f8f6f4 E4M3 0, E5M2 1
@@ -1581,7 +1641,7 @@ LogitsParams logits_params(const LinearLossArgs& a, const Layout& l, char* ws) {
   p.ring = ring_of(ctas_of(a.n), p.box_rows, l.width, false);
   const int es = elem_size(a.h_dt);
   p.n = static_cast<int>(a.n);
-  p.num_kb = static_cast<int>((static_cast<long long>(a.d) * es + kRowBytes - 1) / kRowBytes);
+  p.num_kb = static_cast<int>(row_kbs(a.d, es));
   p.tiles_m = static_cast<int>(row_tiles(a.n, ctas_of(a.n)));
   p.idesc = idesc_of(a.h_dt, a.w_dt, ctas_of(a.n), l.width);
   p.half_cols = l.width / 2;
@@ -1609,7 +1669,7 @@ size_t linear_loss_ws_need(long long n, long long vocab, long long d, int operan
 
 // The most that a batch of at most n rows needs, so that a workspace for the longest batch serves every other.  The need falls only
 // where the plan changes: behind the last batch with two halves of D, with one CTA per tile, of each run length, of each number
-// of parts of dH, and with one piece of the vocabulary.  Between those it grows, so they are what is looked at.
+// of parts of dH, with one piece of the vocabulary, and with pieces longer than an accumulator's sum.  Between those it grows, so they are what is looked at.
 size_t linear_loss_ws_bytes(long long n, long long vocab, long long d, int operand_bytes, int k, bool backward) {
   size_t most = 0;
   auto look = [&](long long rows) {
@@ -1627,6 +1687,7 @@ size_t linear_loss_ws_bytes(long long n, long long vocab, long long d, int opera
   if (!backward) return most;
   const long long all = pad_to(vocab, kTN), one_piece = all == kTN ? n : kPieceElems / all / 32 * 32;
   look(one_piece);
+  look(kPieceElems / ((kSumKb + 1) * kK16) / 32 * 32);  // the last batch with pieces that take several accumulators
   // (parts: the same for all batches of as many K blocks; one where there are two tiles for each unit)
   const long long d_tiles = (d + kTN - 1) / kTN;
   for (long long rows = kK16; rows < n && rows < one_piece && row_tiles(rows, ctas_of(rows)) * d_tiles < 2 * units_of(rows); rows += kK16) look(rows);
@@ -1743,6 +1804,7 @@ int launch_linear_loss_bwd(const LinearLossArgs& a, void* workspace, cudaStream_
   dh.acc = reinterpret_cast<float*>(ws + l.acc); dh.ld_acc = l.ld_acc;
   g.idesc = idesc_of(d_dt, d_dt, ctas, kTN);
   g.unit = c.unit;
+  g.sums = reinterpret_cast<float*>(ws + l.sums_long);  // (not touched where the layout has none)
   rc = map_of(&m.h, a.H, a.n, a.d, a.h_ld, es, p.box_rows);
   if (!rc) rc = map_of(&m.h_mn, h16, d_rows, a.d, h16_ld, 2, kK16);
   if (rc) return rc;
