@@ -12,7 +12,7 @@ import torch
 import paper_2407_17353_b200 as sc
 import plain64_loss as pl
 from test_gpu_linear_loss import check, ids_of, layer, rand
-from test_gpu_rmsnorm import gen
+from test_gpu_rmsnorm import gen, put
 
 pytestmark = pytest.mark.gpu
 BF16, F16, F32, E4M3, E5M2 = torch.bfloat16, torch.float16, torch.float32, torch.float8_e4m3fn, torch.float8_e5m2
@@ -24,7 +24,7 @@ def lost(additions, longest, terms=16):
 
 
 def positive(shape, dtype, seed):
-    return rand(shape, seed).abs().clamp(min=2.0 ** -6).to(dtype)
+    return put(rand(shape, seed).abs().clamp(min=2.0 ** -6), dtype)[0]
 
 
 def exponents(lse, z):
@@ -122,3 +122,49 @@ def test_parts_at_ragged_sizes(n, vocab, d, ht, wt):
     T = 4 * rand((n, 24), 1)
     ids = torch.randint(0, vocab, (n, 24), generator=gen(2), device="cuda")
     check(H, W, ids, ws=2.0 ** -5, T=T, temp=2.0, out=BF16 if ht == BF16 else F16)
+
+
+@pytest.mark.parametrize("dtype", [F16, E4M3])
+@pytest.mark.parametrize("n,vocab,d", [(7, 20011, 24), (20, 20011, 24), (100, 20011, 264), (300, 20011, 72), (5000, 20011, 72), (2500, 30000, 40),
+                                       (17000, 1000, 72)])
+def test_every_block_of_a_contraction_counts(n, vocab, d, dtype):
+    """Terms of one sign and about one size: a K block of 64 left out or taken twice, at the border of a part, a piece or an
+    accumulator, changes a gradient by 64 / n or 64 / vocab of itself, more than the bar."""
+    hs, ws = 2.0 ** -3, 2.0 ** -3
+    H, W = positive((n, d), dtype, 8), positive((vocab, d), dtype, 9)
+    ids = torch.randint(0, vocab, (n,), generator=gen(7), device="cuda")
+    _, _, _, dH, dW, _ = check(H, W, ids, hs=hs, ws=ws, z_loss=PENALTY, out=F16, bars=False)
+    fine = pl.linear_loss(H, hs, W, ws, ids, z_loss=PENALTY, d_type=F32)
+    most = 2 * exponents(fine["lse"], fine["lse"]) + 2 * 2.0 ** -11   # (D rounded, and the result)
+    for got, name, terms in ((dH, "dH", vocab), (dW, "dW", n)):
+        bar = most + lost(-(-terms // 16), 1024)
+        assert terms < 256 or 64 / terms > 1.5 * bar
+        assert relative(got.data, fine[name]) <= bar
+
+
+def test_hidden_gradient_of_weights_past_2_31_elements():
+    """dH of weights beyond 32-bit offsets, all of it (logits of one sign, as above)."""
+    n, vocab, d, hs, ws = 70, 70003, 32768, 2.0 ** -5, 2.0 ** -6
+    assert vocab * d > 1 << 31
+    H = positive((n, d), E4M3, 1)
+    W = torch.empty(vocab, d, dtype=E4M3, device="cuda")
+    for i in range(0, vocab, 8192):
+        W[i:i + 8192] = positive((min(8192, vocab - i), d), E4M3, 2 + i)
+    ids = ids_of(n, vocab)
+    Hs, Ws = sc.ScaledTensor.make(H, hs), sc.ScaledTensor.make(W, ws)
+    loss, lse = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    wsp = sc.Workspace(sc.scalify_linear_loss_workspace_bytes(Hs, Ws))
+    dH = sc.ScaledTensor.empty((n, d), F16)
+    sc.scalify_scaled_linear_cross_entropy(Hs, Ws, ids, loss, lse, wsp, padding_id=-1, z_loss=PENALTY)
+    sc.scalify_scaled_linear_cross_entropy_bwd(Hs, Ws, ids, lse, dH, None, wsp, padding_id=-1, z_loss=PENALTY)
+    assert wsp.check_status() == 0
+    z = torch.cat([H.double() @ W[i:i + 4096].double().T * (hs * ws) for i in range(0, vocab, 4096)], 1)
+    want = torch.logsumexp(z, 1)
+    there = ids >= 0
+    m, unit = int(there.sum()), pl.p2(1.0 / n)
+    D = torch.exp(z - want[:, None]) * (1 + 2 * PENALTY * want)[:, None] * there[:, None]
+    D[torch.arange(n, device="cuda")[there], ids[there]] -= 1.0
+    ref = sum(D[:, i:i + 4096] @ W[i:i + 4096].double() for i in range(0, vocab, 4096)) / m / unit / pl.kf(vocab)
+    assert dH.scale_value() == unit * ws * pl.kf(vocab)
+    bar = (lost(d // 32, 256, 32) + lost(d // 32, 48, 32)) * float(z.max()) + 2 * exponents(want, z) + 2 * 2.0 ** -11 + lost(vocab // 16, 1024)
+    assert relative(dH.data, ref) <= bar
