@@ -1419,22 +1419,31 @@ int check_linear_loss(const scalify_array* H, const scalify_array* W, const scal
   a->T = T->data; a->t_dt = T->dtype; a->t_ld = T->stride[0]; a->t_scale = T->scale; a->t_lse = teacher_lse;
   return SCALIFY_OK;
 }
-// Whether the span of an output is apart from all inputs
-bool apart_from_inputs(Span out, const LinearLossArgs& a, const scalify_array* H, const scalify_array* W, const scalify_array* T) {
-  const scalify_array* arrays[3] = {H, W, T};
-  for (const scalify_array* x : arrays)
-    if (x && !disjoint(x, out)) return false;
-  return !overlap(out, span_of(a.ids, a.n * (a.k > 0 ? a.k : 1), 8)) && !overlap(out, span_of(a.t_lse, a.n, 4));
+// Whether no output lies over another one or over an input (data and scale words alike).
+bool all_apart(const Span* out, int n_out, const Span* in, int n_in) {
+  for (int i = 0; i < n_out; ++i) {
+    for (int j = 0; j < i; ++j)
+      if (overlap(out[i], out[j])) return false;
+    for (int j = 0; j < n_in; ++j)
+      if (overlap(out[i], in[j])) return false;
+  }
+  return true;
+}
+Span word_of(const scalify_array* a) { return a ? span_of(a->scale, 1, 4) : Span{0, 0, 0, 0}; }
+Span data_of(const scalify_array* a) { return a ? span_of(a) : Span{0, 0, 0, 0}; }
+constexpr int kLossInputs = 8;
+void loss_inputs(Span (&in)[kLossInputs], const LinearLossArgs& a, const scalify_array* H, const scalify_array* W, const scalify_array* T) {
+  const Span all[kLossInputs] = {data_of(H), word_of(H), data_of(W), word_of(W), data_of(T), word_of(T),
+                                 span_of(a.ids, a.n * (a.k > 0 ? a.k : 1), 8), span_of(a.t_lse, a.n, 4)};
+  for (int i = 0; i < kLossInputs; ++i) in[i] = all[i];
 }
 int linear_loss_forward(LinearLossArgs& a, const scalify_array* H, const scalify_array* W, const scalify_array* T, float* loss,
                         float* lse, float* mean, void* workspace, size_t workspace_bytes, void* stream) {
   if (a.n > 0 && (!loss || !lse)) return SCALIFY_ERR_NULL;
   const Span out[3] = {span_of(loss, a.n, 4), span_of(lse, a.n, 4), span_of(mean, 1, 4)};
-  for (int i = 0; i < 3; ++i) {
-    if (!apart_from_inputs(out[i], a, H, W, T)) return SCALIFY_ERR_ALIAS;
-    for (int j = 0; j < i; ++j)
-      if (overlap(out[i], out[j])) return SCALIFY_ERR_ALIAS;
-  }
+  Span in[kLossInputs];
+  loss_inputs(in, a, H, W, T);
+  if (!all_apart(out, 3, in, kLossInputs)) return SCALIFY_ERR_ALIAS;
   const int rc = check_ws(workspace, workspace_bytes, linear_loss_ws_need(a.n, a.vocab, a.d, elem_size(a.h_dt), a.k, false));
   if (rc) return rc;
   a.loss = loss; a.lse = lse; a.mean = mean;
@@ -1447,34 +1456,28 @@ int linear_loss_backward(LinearLossArgs& a, const scalify_array* H, const scalif
   if (a.n > 0 && !lse) return SCALIFY_ERR_NULL;
   scalify_array* const outs[2] = {dH, dW};
   const int64_t rows[2] = {a.n, a.vocab};
-  Span spans[2] = {};
   for (int i = 0; i < 2; ++i) {
     const scalify_array* o = outs[i];
     if (!o) continue;
-    int rc = rows[i] > 0 ? check_array(o) : SCALIFY_OK;
+    const int rc = rows[i] > 0 ? check_array(o) : SCALIFY_OK;
     if (rc) return rc;
     if (o->dtype != SCALIFY_F16 && o->dtype != SCALIFY_BF16) return SCALIFY_ERR_DTYPE;
     if (o->ndim != 2 || o->shape[0] != rows[i] || o->shape[1] != a.d || !rows_apart(rows[i], a.d, o->stride[0])) return SCALIFY_ERR_SHAPE;
-    spans[i] = rows[i] > 0 ? span_of(o) : Span{0, 0, 0, 0};
-    if (!apart_from_inputs(spans[i], a, H, W, T) || overlap(spans[i], span_of(lse, a.n, 4))) return SCALIFY_ERR_ALIAS;
   }
-  if (dH && dW && overlap(spans[0], spans[1])) return SCALIFY_ERR_ALIAS;
   if (grad) {
-    int rc = a.n > 0 ? check_array(grad) : SCALIFY_OK;
+    const int rc = a.n > 0 ? check_array(grad) : SCALIFY_OK;
     if (rc) return rc;
     if (grad->dtype != SCALIFY_F32) return SCALIFY_ERR_DTYPE;
     if (grad->ndim != 1 || grad->shape[0] != a.n) return SCALIFY_ERR_SHAPE;
-    for (int i = 0; i < 2; ++i)
-      if (outs[i] && a.n > 0 && overlap(spans[i], span_of(grad))) return SCALIFY_ERR_ALIAS;
     a.grad = static_cast<const float*>(grad->data);
     a.grad_scale = grad->scale;
     if (a.n == 0) a.grad = reinterpret_cast<const float*>(workspace);  // (not read: says whose scale it is)
   }
-  const float* out_words[2] = {dH ? dH->scale : nullptr, dW ? dW->scale : nullptr};
-  const float* in_words[4] = {H->scale, W->scale, T ? T->scale : nullptr, grad ? grad->scale : nullptr};
-  int rc = check_scale_words(out_words, 2, in_words, 4);
-  if (rc) return rc;
-  rc = check_ws(workspace, workspace_bytes, linear_loss_ws_need(a.n, a.vocab, a.d, elem_size(a.h_dt), a.k, true));
+  const Span out[4] = {data_of(dH), word_of(dH), data_of(dW), word_of(dW)};
+  Span in[kLossInputs], more[3] = {span_of(lse, a.n, 4), data_of(grad), word_of(grad)};
+  loss_inputs(in, a, H, W, T);
+  if (!all_apart(out, 4, in, kLossInputs) || !all_apart(out, 4, more, 3)) return SCALIFY_ERR_ALIAS;
+  const int rc = check_ws(workspace, workspace_bytes, linear_loss_ws_need(a.n, a.vocab, a.d, elem_size(a.h_dt), a.k, true));
   if (rc) return rc;
   a.lse = const_cast<float*>(lse);
   if (dH) { a.dH = dH->data; a.dh_dt = dH->dtype; a.dh_ld = dH->stride[0]; a.dh_scale = dH->scale; }
@@ -1542,11 +1545,8 @@ int scalify_scaled_top_logits(const scalify_array* X, float temperature, scalify
   a.inv_temp = 1.0f / temperature;
   float p2, rest;
   if (!split_constant(temperature, &p2, &rest) || !split_constant(a.inv_temp, &p2, &rest)) return SCALIFY_ERR_VALUE;
-  if (n > 0) {
-    const Span sv = span_of(V), si = span_of(ids, n * k, 8), sl = span_of(lse, n, 4);
-    if (!disjoint(X, sv) || !disjoint(X, si) || !disjoint(X, sl) || overlap(sv, si) || overlap(sv, sl) || overlap(si, sl)) return SCALIFY_ERR_ALIAS;
-  }
-  if (V->scale && V->scale == X->scale) return SCALIFY_ERR_ALIAS;
+  const Span out[4] = {data_of(V), word_of(V), span_of(ids, n * k, 8), span_of(lse, n, 4)}, in[2] = {data_of(X), word_of(X)};
+  if (!all_apart(out, 4, in, 2)) return SCALIFY_ERR_ALIAS;
   a.X = X->data; a.dt = X->dtype; a.ld = X->stride[0]; a.x_scale = X->scale;
   a.n = n; a.vocab = vocab; a.k = static_cast<int>(k);
   a.V = V->data; a.v_ld = V->stride[0]; a.v_scale = V->scale;
