@@ -654,7 +654,7 @@ def scalify_scaled_add_rmsnorm_bwd(G: ScaledTensor, Gr: Optional[ScaledTensor], 
 def _token_ids(name: str, ids: torch.Tensor, padding_id: Optional[int]) -> int:
     if ids.dtype != torch.int64 or not ids.is_contiguous():
         raise ValueError(f"{name}: ids must be a contiguous int64 tensor")
-    return -(1 << 63) if padding_id is None else int(padding_id)
+    return _pad_id(padding_id)
 
 
 def scalify_scaled_embedding_lookup(ids: torch.Tensor, wte: ScaledTensor, Y: ScaledTensor, *, c: float = 1.0,
@@ -755,7 +755,10 @@ def _loss_vectors(name: str, n: int, ids: torch.Tensor, shape, loss=None, lse=No
 
 
 def _pad_id(padding_id: Optional[int]) -> int:
-    return -(1 << 63) if padding_id is None else int(padding_id)
+    p = -(1 << 63) if padding_id is None else int(padding_id)
+    if not -(1 << 63) <= p < 1 << 63:
+        raise ValueError(f"padding_id {p} is no int64")
+    return p
 
 
 def scalify_scaled_linear_cross_entropy(H: ScaledTensor, W: ScaledTensor, ids: torch.Tensor, loss: torch.Tensor,
