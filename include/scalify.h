@@ -582,13 +582,14 @@ int scalify_scaled_cross_entropy(const scalify_array* logits, int64_t n_classes,
  *   loss, lse: DEVICE fp32 [n] (lse of every row; the gradient needs it).  mean: optional DEVICE word, the sum of the losses
  *   (fp64, fixed order) over the number of rows that have entries; 0 if none has.
  *   0 <= n <= 2^24, 1 <= vocab <= 2^24, 1 <= d <= 65536; z_loss >= 0 finite; temperature and its reciprocal normal numbers.
- * The same call gives the same bits every time.  Infinities and NaN in H or W go through as the formulas have them
- * (a row of H without entries, too, has to be finite: its gradient 0 is multiplied with it for dW).
+ * The same call gives the same bits every time.  Infinities and NaN in H or W go through as the formulas have them: lse of a row
+ * whose logits hold +inf is +inf, of -inf throughout -inf, with a NaN NaN; an entry with q = 0 adds nothing to the loss.  (A row
+ * of H without entries, too, has to be finite: its gradient 0 is multiplied with it for dW.)
  * Accuracy: all sums are fp32.  The tensor cores that form the long ones drop, of every product, what lies below 2^-25 of the sum
  * so far: N products of one sign lose about N 2^-27 of their sum (8-bit operands' products have fewer digits and lose less).  So
  * one accumulator takes at most 1536 products of a logit here and 4096 in the gradients (8-bit operands: twice as many), and 16384
- * of the gradients' own sums over rows or vocabulary; those parts are added in fp32 (d = 4096, 16-bit operands: loss and lse
- * within 5e-7 of their size in the norm; d = 768, FP8: 7e-8).
+ * of the gradients' own sums over rows or vocabulary; those parts are added in fp32 (loss and lse, in the norm: operands of
+ * either sign 2.6e-7 of their size, 8-bit ones 7e-8; of one sign 1.1e-6 and 2e-7).
  *
  * Gradients of sum_t g[t] loss[t] with respect to the VALUES of H and W:
  *   D[t,v] = g[t] / T ((Q[t] + 2 z_loss lse[t]) p[t,v] - q[t,v]),  Q = sum q;      dH = D W,  dW = D^T H
@@ -600,7 +601,9 @@ int scalify_scaled_cross_entropy(const scalify_array* logits, int64_t n_classes,
  * The logits are computed again in pieces of the vocabulary (the workspace holds D of two pieces, each at most 128 MiB or 256
  * columns, the fp32 sums of dH, and FP16 copies of FP8 operands).  D is rounded to BF16 (BF16 operands) or to FP16 (the others;
  * FP8 operands are widened to FP16 exactly), half a step of relative error each, at a scale that brings the largest row
- * coefficient to 2^14; for at most 16 rows a second half keeps what that rounding leaves out.  Sums are fp32.
+ * coefficient to 2^14: about as much error as rounding the results once (BF16 2.4e-3 of the norm instead of 1.7e-3, FP16
+ * 2.5e-4 instead of 2.1e-4), and FP16 entries below 2^-38 of the largest coefficient count as zero.  For at most 16 rows a second
+ * half keeps what that rounding leaves out.  Sums are fp32 (as above).
  * Errors: NULL, DTYPE, SHAPE, ALIGNMENT, VALUE, ALIAS (an output over an input or another output), WORKSPACE.
  */
 /* Workspace of these calls (shapes and dtypes of H and W only; k = 0: cross entropy; >= 4096; 0 for arguments that the calls
@@ -627,7 +630,8 @@ int scalify_scaled_linear_distill_bwd(const scalify_array* H, const scalify_arra
  * The k largest logits of every row, what a teacher hands to scalify_scaled_linear_distill:
  *   V_d[r] = the k largest of X_d[r], in descending order, equal ones (0 and -0 are) by column;  V_s = X_s
  *   ids[r] = their columns;   lse[r] = log sum_j exp(X_s X_d[r,j] / temperature)        (optional)
- * A NaN counts as larger than everything (and makes lse NaN).  X: [n, vocab], F16, BF16 or F32; V: [n, k] of X's dtype; rows of
+ * A NaN counts as larger than everything (and makes lse NaN; without one, +inf makes it +inf).
+ * X: [n, vocab], F16, BF16 or F32; V: [n, k] of X's dtype; rows of
  * both may be strided; ids: DEVICE int64 [n, k] contiguous; lse: DEVICE fp32 [n] or NULL.  1 <= k <= min(256, vocab),
  * 0 <= n <= 2^24, vocab <= 2^24.  No workspace.  Errors: NULL, DTYPE, SHAPE, ALIGNMENT, VALUE (temperature), ALIAS.
  */

@@ -12,13 +12,17 @@
 //     element), and the sum of q z; one partial result per row and run, joined by a small kernel in a fixed order.
 // Gradient kernel: the logits again, of a PIECE of the vocabulary, now to the gradient D = g (Q p - q)/T in 16 bits; and, in
 //   the same launch, the products dW = D^T H and dH += D W of the piece before (MN-major operands: nothing is transposed in
-//   memory; dH's sums over the pieces are fp32).  The products' few long tiles alone leave pairs idle (8192 x 768, pieces of
-//   4096: 192 K blocks where 166 are the average); the logits' short ones fill them up.
+//   memory; dH's sums over the pieces are fp32).  The products' few long tiles alone leave pairs idle (8192 x 50257 x 768, pieces of
+//   7424 columns: 183 tiles on 74 pairs, 357 K blocks for some where 308 are the average); the logits' short ones fill them up.
+//   (A vocabulary of one piece has one launch of logits and one of products.)
 //
 // D has the operands' type; FP8 operands are converted to FP16, which holds them exactly, and D is FP16.  FP16 has few
-// exponents, so D is stored at a scale that brings the largest row coefficient to 2^14 (probabilities down to 2^-28 keep all 11
-// bits).  Its rounding is at most half a step (FP16 2^-11, BF16 2^-8) per element, independent over the
-// vocabulary: it adds to dH and dW what rounding them once to that type does.  (Few rows: kFewRows.)
+// exponents, so D is stored at a scale that brings the largest row coefficient to 2^14: probabilities down to 2^-28 keep all 11
+// bits in that row, entries below 2^-38 of the largest coefficient are lost.  Its rounding is at most half a step (FP16 2^-11,
+// BF16 2^-8) per element, independent over the vocabulary: it adds to dH and dW about what rounding them once to that type does
+// (8192 x 50257 x 768, BF16: 2.3e-3 of their norm instead of 1.6e-3).  More digits would cost more than they are worth beside that
+// rounding: TF32 operands run at half the rate, two halves of D are half as much again (few rows: kFewRows), and FP16 copies of BF16
+// operands would lose BF16's range.
 #include <cuda.h>
 #include <limits.h>
 #include <math.h>
@@ -57,17 +61,18 @@ struct Ring {
   int stages, a_bytes, b_bytes;  // of a stage: multiples of 1024
 };
 constexpr int kMaxStages = 12;
-// K blocks from which on a contraction is long, and of its parts.  Sums of 256 (a single CTA, which waits for its weights anyway)
-// and of 768 values in the tensor cores' 32 bits leave the loss with the error that it has from rounding the result (2 rows of
-// 3269: 3.4e-6 with parts of 512, 7.6e-6 with parts of 1024, 1.3e-6 so); parts in contractions of 768 values, too, would make
-// 37 x 50257 x 768 41 instead of 29 us, which then waits for the additions.
+// K blocks (of 64 16-bit or 128 8-bit values) from which on a contraction is long in the forward call, and of its parts.  Sums of 256
+// 16-bit values (a single CTA, which waits for its weights anyway) and of 768 in the tensor cores' 32 bits leave the loss with the
+// error that it has from rounding the result (2 rows of 3269: 3.4e-6 with parts of 512, 7.6e-6 with parts of 1024, 1.3e-6 so);
+// parts in contractions of 768 values, too, would make 37 x 50257 x 768 41 instead of 29 us, which then waits for the additions.
 template <int NCTA> constexpr int kLongKb = NCTA == 1 ? 12 : 24;
 template <int NCTA> constexpr int kSegmentKb = NCTA == 1 ? 4 : 12;
 // K blocks of one accumulator in the gradient kernel, of the logits and of the products.  The tensor cores drop what lies below the
 // running sum's last bits, of every product: by measurement 2^-25 of the sum per product and 2^-23 per addition at most, so that
 // a sum of N products of one sign loses N 2^-27 of itself on average.  In one accumulator a batch of 2^22 rows left dW off by
-// 2.6e-2 and a vocabulary of 2^22 dH by 1.3e-2; 256 blocks lose 1e-4, less than what rounding the result to FP16 does (128 blocks
-// would make the step 4096 x 4096, whose pieces have 252, 1.2 % slower).
+// 2.6e-2 and a vocabulary of 2^22 dH by 1.3e-2; 256 blocks lose 1e-4, less than what rounding the result to FP16 does, and 64
+// blocks of logits 2.5e-5 of a logit (128 blocks of a product would make the step 4096 x 4096, whose pieces have 252, 1.2 % slower).
+// Parts cost 2000 x 32003 x 8192 3.5 % (3.51 -> 3.63 ms) and 40000 x 20000 x 768 1.5 % (5.05 -> 5.13 ms).
 constexpr int kLogitKb = 64, kSumKb = 256;
 constexpr float kLog2E = 1.4426950408889634f;
 constexpr float kLargest = 3.402823466e38f;  // of fp32
@@ -118,8 +123,10 @@ __device__ __forceinline__ long long ld_written(const long long* p) {
   return v;
 }
 
-// One lane of the whole warp, the same one each time: the store engine's calls and the waits for them.  (A branch on the lane
-// instead loses stores: with work on the same values behind it, no byte of the tile was written.)
+// One lane of the whole warp, the same one each time (same mask, same leader): the store engine's calls and the waits for them,
+// whose groups belong to the thread that made them.  (All lanes get here together: the election waits for them.  A branch on the
+// lane would be as good by the rules; compiled into an earlier form of these kernels it left tiles unwritten, for a reason that
+// their source does not show.)
 __device__ __forceinline__ bool elected_lane() {
   uint32_t one;
   asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.b32 %0, 1, 0, p;\n}" : "=r"(one));
@@ -354,30 +361,30 @@ template <int NCTA> struct Engine {
       if (!wait_accumulator()) return false;
       each_chunk(half, half_cols, cols, f);
       release_accumulator();
-      return true;
-    }
-    for (int kb = 0; kb < num_kb; kb += part_kb) {
-      if (!wait_accumulator()) return false;
-      const bool first = kb == 0, last = kb + part_kb >= num_kb;
-      each_chunk(half, half_cols, cols, [&](uint32_t* r, int c) {
-        char* at = reinterpret_cast<char*>(sums) + c * 4096 + lane * 16;
-        if (!first) {
+    } else {
+      for (int kb = 0; kb < num_kb; kb += part_kb) {
+        if (!wait_accumulator()) return false;
+        const bool first = kb == 0, last = kb + part_kb >= num_kb;
+        each_chunk(half, half_cols, cols, [&](uint32_t* r, int c) {
+          char* at = reinterpret_cast<char*>(sums) + c * 4096 + lane * 16;
+          if (!first) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            uint32_t before[4];
-            ld_raw<16>(at + j * 512, before);
+            for (int j = 0; j < 8; ++j) {
+              uint32_t before[4];
+              ld_raw<16>(at + j * 512, before);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) r[4 * j + i] = __float_as_uint(__uint_as_float(r[4 * j + i]) + __uint_as_float(before[i]));
+              for (int i = 0; i < 4; ++i) r[4 * j + i] = __float_as_uint(__uint_as_float(r[4 * j + i]) + __uint_as_float(before[i]));
+            }
           }
-        }
-        if (last) {
-          f(r, c);
-        } else {
+          if (last) {
+            f(r, c);
+          } else {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) st_raw<16>(at + j * 512, r + 4 * j);
-        }
-      });
-      release_accumulator();
+            for (int j = 0; j < 8; ++j) st_raw<16>(at + j * 512, r + 4 * j);
+          }
+        });
+        release_accumulator();
+      }
     }
     return true;
   }
@@ -486,8 +493,9 @@ __device__ __forceinline__ float pick32(const uint32_t* r, int i) {
 
 // LONG: the tensor cores add up with truncation, an error that grows with the number of additions and the sums' size, and the
 // losses are fp32: from kLongKb K blocks on, every kSegmentKb of them go to an accumulator of their own, and the epilogue warps
-// add those up in registers while the next ones are filled (d = 4096: relative errors of lse and loss 1.3e-6 and 2.0e-6 in one
-// accumulator, 3e-7 and 4.5e-7 in parts of 16 blocks, in the same time).
+// add those up in registers while the next ones are filled (4096 x 128000 x 4096, 16 bits: errors of lse and loss 1.3e-6 and 2.0e-6
+// of their norm in one accumulator; 2000 x 5000 x 4096 in these parts 1.2e-7 and 1.6e-7; in the same time).  Three or four chunks of
+// sums beside the work on one: 136 bytes of registers spill, 264 with a teacher's entries.
 template <int NCTA, bool F8, bool KD, bool LONG>
 __global__ void __launch_bounds__(kThreads, 1) logits_kernel(const __grid_constant__ CUtensorMap map_h,
                                                              const __grid_constant__ CUtensorMap map_w, const LogitsParams p) {
@@ -1359,9 +1367,12 @@ int run_length(long long tiles_m, long long tiles_n, int longest, int items) {
 }
 // Few rows: D in two halves of its type, the second of what the first one's rounding left out, as rows of their own: dW's
 // contraction is over both (H twice), dH's sums are added at the end.  One rounding of D adds about as much to the gradients'
-// error as rounding the gradients themselves; with few rows, where a few entries of D decide, more (2 x 1646 x 136, BF16: 2.7e-3
-// of the norm where 1.6e-3 is the output's own).  The second half costs 4 to 10 % of few rows' time (3 x 115392 x 672:
-// 133 -> 145 us); 64 x 50257 x 768 would take 92 instead of 72.
+// error as rounding the gradients themselves; with few rows, where a few entries of D decide, up to twice that (2 x 1646 x 136,
+// BF16: 2.7e-3 of the norm where 1.6e-3 is the output's own).  Both sides, BF16, loss and gradients from a graph with cold caches,
+// one half against two: 50257 x 768: 3 rows 98 and 107 us, dH off by 2.0e-3 and 1.65e-3 (three draws: 1.8e-3 to 2.0e-3); 16 rows
+// 102 and 114, 1.95e-3 and 1.66e-3; 32 rows 102 and 117, 1.88e-3 and 1.66e-3; 64 rows 102 and 123, 1.86e-3 and 1.66e-3.
+// 115392 x 672: 3 rows 182 and 197 us, 16 rows 186 and 201, 64 rows 188 and 207.  Beyond 16 rows the error no longer depends on the
+// draw, and the cost grows.
 constexpr int kFewRows = 16;
 int halves_of(long long n) { return n > 0 && n <= kFewRows ? 2 : 1; }
 // Columns of a piece of the vocabulary: D of at most 2^27 bytes, two pieces of which are in memory; whole tiles.
@@ -1669,7 +1680,8 @@ size_t linear_loss_ws_need(long long n, long long vocab, long long d, int operan
 
 // The most that a batch of at most n rows needs, so that a workspace for the longest batch serves every other.  The need falls only
 // where the plan changes: behind the last batch with two halves of D, with one CTA per tile, of each run length, of each number
-// of parts of dH, with one piece of the vocabulary, and with pieces longer than an accumulator's sum.  Between those it grows, so they are what is looked at.
+// of parts of dH, with one piece of the vocabulary, and with pieces longer than an accumulator's sum.  Between those it grows, so
+// they are what is looked at.
 size_t linear_loss_ws_bytes(long long n, long long vocab, long long d, int operand_bytes, int k, bool backward) {
   size_t most = 0;
   auto look = [&](long long rows) {
