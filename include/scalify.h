@@ -588,8 +588,8 @@ int scalify_scaled_cross_entropy(const scalify_array* logits, int64_t n_classes,
  * Accuracy: all sums are fp32.  The tensor cores that form the long ones drop, of every product, what lies below 2^-25 of the sum
  * so far: N products of one sign lose about N 2^-27 of their sum (8-bit operands' products have fewer digits and lose less).  So
  * one accumulator takes at most 1536 products of a logit here and 4096 in the gradients (8-bit operands: twice as many), and 16384
- * of the gradients' own sums over rows or vocabulary; those parts are added in fp32 (loss and lse, in the norm: operands of
- * either sign 2.6e-7 of their size, 8-bit ones 7e-8; of one sign 1.1e-6 and 2e-7).
+ * of the gradients' own sums over rows or vocabulary; those parts are added in fp32 (loss and lse, in the norm, d up to
+ * 4096: operands of either sign 2.6e-7 of their size, 8-bit ones 7e-8; of one sign 1.1e-6 and 2e-7; d = 65536: 9e-7).
  *
  * Gradients of sum_t g[t] loss[t] with respect to the VALUES of H and W:
  *   D[t,v] = g[t] / T ((Q[t] + 2 z_loss lse[t]) p[t,v] - q[t,v]),  Q = sum q;      dH = D W,  dW = D^T H
